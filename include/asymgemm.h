@@ -589,6 +589,87 @@ void ag_kv_destroy(ag_kv_cache* kv);
 ag_status attention_decode_persistent(const void* Q, const ag_kv_cache* kv, const int32_t* kv_len, void* O, int B,
                                       int H_q, const ag_plan* plan, void* cuda_stream);
 
+/* ---- 4-bit key/value cache in pages ----------------------------------------------------------------------------------
+ * A cache that requests grow in, share and leave again: pages of AG_KV4_PAGE tokens (all KV heads of one layer) in a buffer of
+ * the caller, 4-bit codes with a (scale, base) pair for every 32 elements - 0.31 of the bytes of bf16.  The functions below work
+ * on device arrays only: nothing waits for the host, nothing is allocated, every call is asynchronous on cuda_stream and may be
+ * captured into a graph.  Calls that change the same pages or tables must be ordered by the caller (one stream).
+ * Pages lie where the buffer puts them (the hardware's interleaved placement): a page is read as contiguous runs of 80 D bytes.
+ *
+ * Quantisation: a group of 32 consecutive elements with smallest value lo and largest hi has scale s = bf16((hi - lo) / 15)
+ * and codes rint((x - lo) / s) clamped to 0..15 (0 when s = 0); an element stands for s * code + lo.  A group that holds a value which is not
+ * finite, or whose hi - lo is not, stands for NaN throughout.
+ *
+ * Layout: page p starts at byte p * ag_kv4_page_bytes; KV head h of it is the block of 80 D bytes at h * 80 D:
+ *   [0, 32 D) codes of K, [32 D, 64 D) codes of V, [64 D, 72 D) (scale, base) pairs of bf16 of K, [token][D / 32], [72 D, 80 D) of V.
+ *   Codes: four runs of 16 tokens, 8 D bytes each, low nibble first.  Token 8 h + g of a run, element 32 q + 8 t + i of K: byte
+ *   h 4 D + (4 g + t) D / 8 + 4 q + i / 2.  Token 8 h + 2 t + e, element 16 i + 8 j + g of V: byte h 4 D + (4 g + t) D / 8 + e D / 16 + j D / 32 + i / 2.
+ */
+#define AG_KV4_PAGE 64
+#define AG_KV4_MAX_ROWS 1024   /* rows that one call of ag_kv4_extend / _fork / _free may name */
+
+typedef struct {
+    void* pages;      /* device, 16-byte aligned, n_pages * ag_kv4_page_bytes(H_kv, D) bytes */
+    int64_t n_pages;  /* 1 .. 2^25 - 1 */
+    int32_t H_kv;     /* 1 .. 1024 */
+    int32_t D;        /* head dimension, 64 or 128 */
+} ag_kv4_pool;
+
+/* Which pages a row (a request's place in the tables) holds.  An empty row has len 0 and entries -1; a page with count 0 is free.
+ * Several pools (layers) may share one table: call the functions that change it once, and copy the pages of the other layers with
+ * the list that ag_kv4_compact returns. */
+typedef struct {
+    int32_t* page_of;   /* device [n_rows][max_pages]: page of the row's tokens 64 c .. 64 c + 63, -1 = none */
+    int32_t* len;       /* device [n_rows]: tokens */
+    int32_t* refs;      /* device [n_pages]: rows that hold the page */
+    int32_t n_rows, max_pages;
+} ag_kv4_table;
+
+/* Bytes of a page; 0 for a shape that is not supported. */
+size_t ag_kv4_page_bytes(int H_kv, int D);
+/*
+ * ag_kv4_store / ag_kv4_load - quantise the key and value rows of tokens into the cache / read what the cache holds back as bf16
+ * (rounded once from s * code + lo).
+ *   K, V    device, token i's rows at K + i * k_stride, [H_kv][D] bf16; 16-byte aligned; strides in elements, multiples of 8, at
+ *           least H_kv * D (K and V may be parts of one fused projection)
+ *   slot    device [n_tokens]: 64 * page + place in the page; values outside 0 .. 64 n_pages - 1 (-1, say) skip the token: nothing is
+ *           stored, or the token's rows of K and V are left as they were.  A slot named twice by one store holds a mixture of the two tokens
+ * Errors: AG_ERR_ARG, AG_ERR_UNSUPPORTED_ARCH, AG_ERR_CUDA.
+ */
+ag_status ag_kv4_store(const ag_kv4_pool* pool, const void* K, const void* V, int64_t n_tokens, int64_t k_stride, int64_t v_stride,
+                       const int32_t* slot, void* cuda_stream);
+ag_status ag_kv4_load(const ag_kv4_pool* pool, const int32_t* slot, int64_t n_tokens, void* K, void* V, int64_t k_stride, int64_t v_stride,
+                      void* cuda_stream);
+/*
+ * ag_kv4_extend - make room for new tokens: row[i] grows by new_off[i + 1] - new_off[i] tokens (new_off as the q_off of attention_prompt_persistent).
+ * Free pages are dealt in ascending order, request by request; a request whose pages are not all there (counting those of the
+ * requests in front of it, granted or not) is refused and its row stays as it is.  Refused too: a row outside the table, a row named
+ * earlier in the same call, a length that max_pages cannot hold.  Never reports an error for these: ok[i] = 0.
+ *   row, ok  device [n], new_off device [n + 1] ascending;  n <= AG_KV4_MAX_ROWS
+ *   slot     device [n_tokens], out: the slot of token j (of request i when new_off[i] <= j < new_off[i + 1]), -1 where its request was
+ *            refused or no request has it
+ */
+ag_status ag_kv4_extend(const ag_kv4_pool* pool, const ag_kv4_table* table, const int32_t* row, const int32_t* new_off, int n, int32_t* slot,
+                        int64_t n_tokens, int32_t* ok, void* cuda_stream);
+/*
+ * ag_kv4_fork - row dst[i], empty so far, becomes a copy of row src[i]: it shares the full pages (their counts go up) and gets a copy of the
+ * open last page, so that both can grow on their own.  The tables are read as they were before the call.  Refused (ok[i] = 0, nothing
+ * changes): a row outside the table, dst[i] not empty, equal to src[i] or named earlier in the call, no free page for the copy (dealt
+ * as in ag_kv4_extend).  n <= AG_KV4_MAX_ROWS.
+ */
+ag_status ag_kv4_fork(const ag_kv4_pool* pool, const ag_kv4_table* table, const int32_t* src, const int32_t* dst, int n, int32_t* ok,
+                      void* cuda_stream);
+/* ag_kv4_free - give up rows: their pages' counts go down, the rows become empty.  Rows outside the table are passed over; a row named
+ * twice is given up once.  n <= AG_KV4_MAX_ROWS. */
+ag_status ag_kv4_free(const ag_kv4_pool* pool, const ag_kv4_table* table, const int32_t* row, int n, void* cuda_stream);
+/*
+ * ag_kv4_compact - move the pages in use to the front of the buffer: with n_used pages in use, the k-th used page from page n_used
+ * on goes to the k-th free page below it (contents, count and every table entry).
+ *   moved  device [n_pages], out: where page p is now, -1 for a page that was free (for tables of the caller's own, or for other
+ *          layers' buffers)
+ */
+ag_status ag_kv4_compact(const ag_kv4_pool* pool, const ag_kv4_table* table, int32_t* moved, void* cuda_stream);
+
 /*
  * ag_wait_probe - self test of the bounded device-side wait that every kernel of this library
  * uses: one thread waits on a barrier that nothing signals, gives up after limit_ns

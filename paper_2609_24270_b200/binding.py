@@ -31,6 +31,7 @@ EXPORTED = [
     "ag_topo_load", "ag_group_desc_create", "ag_group_desc_destroy", "ag_pack_weights_grouped",
     "gemm_persistent_grouped", "ag_strerror", "ag_last_cuda_error",
     "ag_kernel_launch_count", "ag_kv_pack", "ag_kv_info", "ag_kv_append", "ag_kv_destroy", "attention_decode_persistent",
+    "ag_kv4_page_bytes", "ag_kv4_store", "ag_kv4_load", "ag_kv4_extend", "ag_kv4_fork", "ag_kv4_free", "ag_kv4_compact",
 ]
 
 
@@ -87,6 +88,19 @@ class Policy(C.Structure):
                 ("splitk_in_memory", C.c_int32), ("sm_select", C.c_int32), ("pair_lists", C.c_int32), ("overlap_launches", C.c_int32), ("cluster_size", C.c_int32), ("die_quota", C.c_int32), ("decode_shaped", C.c_int32), ("ring_stages", C.c_int32),
                 ("avoid_sm_mask", C.c_uint64 * 4),
                 ("a", OperandDesc), ("b", OperandDesc), ("c", OperandDesc)]
+
+
+AG_KV4_PAGE, AG_KV4_MAX_ROWS = 64, 1024
+
+
+class KV4Pool(C.Structure):
+    """Pages of the 4-bit key/value cache: KV4Pool(device pointer, n_pages, H_kv, D)."""
+    _fields_ = [("pages", C.c_void_p), ("n_pages", C.c_int64), ("H_kv", C.c_int32), ("D", C.c_int32)]
+
+
+class KV4Table(C.Structure):
+    """Page tables on the device: KV4Table(page_of [n_rows][max_pages], len [n_rows], refs [n_pages], n_rows, max_pages)."""
+    _fields_ = [("page_of", C.c_void_p), ("len", C.c_void_p), ("refs", C.c_void_p), ("n_rows", C.c_int32), ("max_pages", C.c_int32)]
 
 
 class AgError(RuntimeError):
@@ -157,6 +171,15 @@ def lib() -> C.CDLL:
     L.ag_kv_destroy.argtypes = [vp]
     L.ag_kv_destroy.restype = None
     L.attention_decode_persistent.argtypes = [vp, vp, vp, vp, C.c_int, C.c_int, vp, vp]
+    pool, table, i64 = C.POINTER(KV4Pool), C.POINTER(KV4Table), C.c_int64
+    L.ag_kv4_page_bytes.argtypes = [C.c_int, C.c_int]
+    L.ag_kv4_page_bytes.restype = sz
+    L.ag_kv4_store.argtypes = [pool, vp, vp, i64, i64, i64, vp, vp]
+    L.ag_kv4_load.argtypes = [pool, vp, i64, vp, vp, i64, i64, vp]
+    L.ag_kv4_extend.argtypes = [pool, table, vp, vp, C.c_int, vp, i64, vp, vp]
+    L.ag_kv4_fork.argtypes = [pool, table, vp, vp, C.c_int, vp, vp]
+    L.ag_kv4_free.argtypes = [pool, table, vp, C.c_int, vp]
+    L.ag_kv4_compact.argtypes = [pool, table, vp, vp]
     L.ag_cluster_capacity.argtypes = [vp, C.POINTER(TopoMap), C.c_int, C.POINTER(C.c_int32)]
     L.ag_probe_cluster_layout.argtypes = [C.c_int, C.c_int, vp]
     L.ag_topo_save.argtypes = [C.POINTER(TopoMap), C.c_char_p]
@@ -563,6 +586,48 @@ def kv_pack(k_ptr: int, v_ptr: int, B: int, H_kv: int, L: int, plan: Plan, amap:
 def attention_decode(q_ptr: int, kv: KVCache, kv_len_ptr, o_ptr: int, B: int, H_q: int, plan: Plan, stream: int = 0):
     _check(lib().attention_decode_persistent(q_ptr, kv.handle, kv_len_ptr, o_ptr, B, H_q, plan.handle, stream),
            "attention_decode_persistent")
+
+
+# ---- 4-bit key/value cache in pages -----------------------------------------------------------------
+def kv4_page_bytes(H_kv: int, D: int) -> int:
+    return int(lib().ag_kv4_page_bytes(H_kv, D))
+
+
+def kv4_store(pool: KV4Pool, k_ptr: int, v_ptr: int, slot_ptr: int, n_tokens: int, k_stride: int | None = None,
+              v_stride: int | None = None, stream: int = 0):
+    """Quantise n_tokens rows of K and V ([H_kv][D] bf16, strides in elements) into the slots slot[i] = 64 * page + place."""
+    w = pool.H_kv * pool.D
+    _check(lib().ag_kv4_store(C.byref(pool), k_ptr, v_ptr, n_tokens, w if k_stride is None else k_stride,
+                              w if v_stride is None else v_stride, slot_ptr, stream), "ag_kv4_store")
+
+
+def kv4_load(pool: KV4Pool, slot_ptr: int, n_tokens: int, k_ptr: int, v_ptr: int, k_stride: int | None = None,
+             v_stride: int | None = None, stream: int = 0):
+    """Read the rows in the slots back as bf16."""
+    w = pool.H_kv * pool.D
+    _check(lib().ag_kv4_load(C.byref(pool), slot_ptr, n_tokens, k_ptr, v_ptr, w if k_stride is None else k_stride,
+                             w if v_stride is None else v_stride, stream), "ag_kv4_load")
+
+
+def kv4_extend(pool: KV4Pool, table: KV4Table, row_ptr: int, new_off_ptr: int, n: int, slot_ptr: int, n_tokens: int, ok_ptr: int,
+               stream: int = 0):
+    """Room for new_off[i + 1] - new_off[i] more tokens in row[i]; writes every new token's slot and ok[i]."""
+    _check(lib().ag_kv4_extend(C.byref(pool), C.byref(table), row_ptr, new_off_ptr, n, slot_ptr, n_tokens, ok_ptr, stream),
+           "ag_kv4_extend")
+
+
+def kv4_fork(pool: KV4Pool, table: KV4Table, src_ptr: int, dst_ptr: int, n: int, ok_ptr: int, stream: int = 0):
+    """Row dst[i] becomes a copy of row src[i] that shares its full pages."""
+    _check(lib().ag_kv4_fork(C.byref(pool), C.byref(table), src_ptr, dst_ptr, n, ok_ptr, stream), "ag_kv4_fork")
+
+
+def kv4_free(pool: KV4Pool, table: KV4Table, row_ptr: int, n: int, stream: int = 0):
+    _check(lib().ag_kv4_free(C.byref(pool), C.byref(table), row_ptr, n, stream), "ag_kv4_free")
+
+
+def kv4_compact(pool: KV4Pool, table: KV4Table, moved_ptr: int, stream: int = 0):
+    """Moves the used pages to the front; moved[p] = the new place of page p, -1 for a free one."""
+    _check(lib().ag_kv4_compact(C.byref(pool), C.byref(table), moved_ptr, stream), "ag_kv4_compact")
 
 
 def suggest_k_splits(N: int, K: int, sm_budget: int, overlapping_full_chip: bool = False) -> int:

@@ -1,0 +1,530 @@
+// The paged 4-bit key/value cache: quantising new tokens into pages, reading them back, and the device-side page tables
+// (growing rows, forking, freeing, compacting).  Nothing here waits on the host or spins on the device; every call may be captured
+// into a graph.  All page bookkeeping is in integers and does not depend on the order of blocks or atomics.
+#include <string.h>
+
+#include <algorithm>
+
+#include "kv4.cuh"
+
+namespace ag {
+
+// ---- store and load ---------------------------------------------------------------------------------------------------
+// Quantisation of a group x_0 .. x_31: lo = min, s = bf16((max - lo) / 15), code = rint((x - lo) / s) in 0 .. 15, and an element
+// stands for s code + lo.  lo is an element, so it is a bf16 already; s is rounded to bf16 first and the codes are taken for the
+// rounded one, so that the rounding costs at most 2^-9 of a step.  All in 32 bits with IEEE rounding: the codes do not depend on the kernel.
+// A group with a value that is not finite, or whose range is not, stands for NaN throughout.
+//
+// D / 8 lanes hold a row (eight elements, one 16-byte load each); a lane's eight K codes are one word of the page, the V codes
+// are transposed across lanes (kv4_transpose) so that a lane writes whole words of the fragment order as well.
+template <int D>
+__global__ void __launch_bounds__(256) k_kv4_store(uint8_t* __restrict__ pages, long long n_slots, int H_kv, const uint16_t* __restrict__ K,
+                                                   const uint16_t* __restrict__ V, long long n_tokens, long long k_stride, long long v_stride,
+                                                   const int32_t* __restrict__ slot) {
+    constexpr int L = D / 8;                                        // lanes of a row
+    const long long task = ((long long)blockIdx.x * blockDim.x + threadIdx.x) / L;      // ((token, head), K or V)
+    const int l = threadIdx.x % L;
+    const int which = (int)(task & 1);
+    const long long th = task >> 1;
+    const long long tok = th / H_kv;
+    const int head = (int)(th - tok * H_kv);
+    const int at = tok < n_tokens ? slot[tok] : -1;
+    const bool live = at >= 0 && at < n_slots;
+    uint4 raw = make_uint4(0, 0, 0, 0);
+    if (live) raw = *reinterpret_cast<const uint4*>((which ? V + tok * v_stride : K + tok * k_stride) + head * D + l * 8);
+    float x[8] = {bf16_lo(raw.x), bf16_hi(raw.x), bf16_lo(raw.y), bf16_hi(raw.y), bf16_lo(raw.z), bf16_hi(raw.z), bf16_lo(raw.w), bf16_hi(raw.w)};
+    float lo = x[0], hi = x[0], odd = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        lo = fminf(lo, x[i]);
+        hi = fmaxf(hi, x[i]);
+        odd = fmaf(x[i], 0.f, odd);                                 // NaN as soon as one element is not finite
+    }
+#pragma unroll
+    for (int o = 1; o < 4; o <<= 1) {
+        lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+        hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+        odd += __shfl_xor_sync(0xffffffffu, odd, o);
+    }
+    const __nv_bfloat16 sb = __float2bfloat16_rn(__fdiv_rn(__fsub_rn(hi, lo), 15.f) + odd);
+    const float s = __bfloat162float(sb);
+    const bool fine = s <= 3.4e38f;                                 // false for NaN and infinity
+    uint32_t w = 0;
+    if (fine && s > 0.f) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int c = min(15, __float2int_rn(__fdiv_rn(__fsub_rn(x[i], lo), s)));
+            w |= (uint32_t)c << (4 * i);
+        }
+    }
+    const uint32_t wt = kv4_transpose<D / 16, 2>(w, l >> 1);        // lanes of equal parity hold elements 16 i + 8 (l & 1) + j
+    if (!live) return;
+    uint8_t* block = pages + ((size_t)(at / KV4_PAGE) * H_kv + head) * kv4_head_bytes(D);
+    const int r = at % KV4_PAGE;
+    if (which == 0) {
+        *reinterpret_cast<uint32_t*>(block + kv4_k_word<D>(r, l >> 2, l & 3)) = w;
+    } else if (D == 128) {
+        *reinterpret_cast<uint32_t*>(block + kv4_v_word<D>(r, l & 1, l >> 1)) = wt;
+    } else {
+        *reinterpret_cast<uint16_t*>(block + kv4_v_word<D>(r, l & 1, l >> 1)) = (uint16_t)wt;
+        *reinterpret_cast<uint16_t*>(block + kv4_v_word<D>(r, l & 1, 4 + (l >> 1))) = (uint16_t)(wt >> 16);
+    }
+    if ((l & 3) == 0) {
+        const uint32_t nan = 0x7fc07fc0u;
+        const uint32_t pair = (uint32_t)__bfloat16_as_ushort(sb) | (__float_as_uint(lo) & 0xffff0000u);
+        *reinterpret_cast<uint32_t*>(block + kv4_scale_word<D>(which, r, l >> 2)) = fine ? pair : nan;
+    }
+}
+
+template <int D>
+__global__ void __launch_bounds__(256) k_kv4_load(const uint8_t* __restrict__ pages, long long n_slots, int H_kv, uint16_t* __restrict__ K,
+                                                  uint16_t* __restrict__ V, long long n_tokens, long long k_stride, long long v_stride,
+                                                  const int32_t* __restrict__ slot) {
+    constexpr int L = D / 8;
+    const long long task = ((long long)blockIdx.x * blockDim.x + threadIdx.x) / L;
+    const int l = threadIdx.x % L;
+    const int which = (int)(task & 1);
+    const long long th = task >> 1;
+    const long long tok = th / H_kv;
+    const int head = (int)(th - tok * H_kv);
+    const int at = tok < n_tokens ? slot[tok] : -1;
+    const bool live = at >= 0 && at < n_slots;
+    const uint8_t* block = pages + ((size_t)(live ? at / KV4_PAGE : 0) * H_kv + head) * kv4_head_bytes(D);
+    const int r = live ? at % KV4_PAGE : 0;
+    uint32_t w = 0, pair = 0;
+    if (live) {
+        if (which == 0) w = *reinterpret_cast<const uint32_t*>(block + kv4_k_word<D>(r, l >> 2, l & 3));
+        else if (D == 128) w = *reinterpret_cast<const uint32_t*>(block + kv4_v_word<D>(r, l & 1, l >> 1));
+        else w = *reinterpret_cast<const uint16_t*>(block + kv4_v_word<D>(r, l & 1, l >> 1)) |
+                 (uint32_t)*reinterpret_cast<const uint16_t*>(block + kv4_v_word<D>(r, l & 1, 4 + (l >> 1))) << 16;
+        pair = *reinterpret_cast<const uint32_t*>(block + kv4_scale_word<D>(which, r, l >> 2));
+    }
+    const uint32_t wt = kv4_transpose<D / 16, 2>(w, l >> 1);
+    if (which) w = wt;
+    if (!live) return;
+    uint32_t out[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(fmaf((float)((w >> (8 * i)) & 15u), bf16_lo(pair), bf16_hi(pair)),
+                                                       fmaf((float)((w >> (8 * i + 4)) & 15u), bf16_lo(pair), bf16_hi(pair)));
+        out[i] = *reinterpret_cast<const uint32_t*>(&v);
+    }
+    *reinterpret_cast<uint4*>((which ? V + tok * v_stride : K + tok * k_stride) + head * D + l * 8) = make_uint4(out[0], out[1], out[2], out[3]);
+}
+
+// ---- page tables ------------------------------------------------------------------------------------------------------
+constexpr int KT_THREADS = 1024;
+constexpr int KT_MAX = AG_KV4_MAX_ROWS;              // requests of one call: one thread each
+constexpr int KT_INLINE_TOKENS = 8192;               // up to so many slots are written by the allocating block itself
+
+// exclusive sum over the block of one value per thread; *total = the sum
+template <class T>
+__device__ __forceinline__ T block_scan(T v, T* warp_sum, T* total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    T inc = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const T u = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += u;
+    }
+    __syncthreads();                                 // warp_sum may still be read from the scan before
+    if (lane == 31) warp_sum[warp] = inc;
+    __syncthreads();
+    if (warp == 0) {
+        T s = warp_sum[lane];
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const T u = __shfl_up_sync(0xffffffffu, s, o);
+            if (lane >= o) s += u;
+        }
+        warp_sum[lane] = s;
+    }
+    __syncthreads();
+    *total = warp_sum[31];
+    return inc - v + (warp ? warp_sum[warp - 1] : 0);
+}
+
+// the pages of thread i: [i per, (i + 1) per)
+__device__ __forceinline__ int pages_per_thread(int n_pages) { return (n_pages + KT_THREADS - 1) / KT_THREADS; }
+
+struct TableArgs {
+    int32_t *page_of, *len, *refs;
+    int n_rows, max_pages, n_pages;
+};
+
+// Request i (thread i) wants need[i] pages; free pages are dealt in ascending order to the requests in order, request i getting the
+// ranks before[i] .. before[i] + need[i] - 1.  A request is granted when all of them exist.  Ends with the pages entered in the
+// tables (column first[i] on) and counted.  Returns whether this thread's request is granted.
+struct GrantShared {
+    long long warp_sum64[32];
+    long long before[KT_MAX];                        // 64 bits: 1024 requests of up to 2^25 pages each
+    int warp_sum[32];
+    int need[KT_MAX], first[KT_MAX], row[KT_MAX];
+};
+__device__ inline bool grant_pages(const TableArgs& t, int n, int need, int first, int row, GrantShared* sh) {
+    long long total_need;
+    int total_free;
+    const long long before = block_scan((long long)need, sh->warp_sum64, &total_need);
+    sh->before[threadIdx.x] = before;
+    sh->need[threadIdx.x] = need;
+    sh->first[threadIdx.x] = first;
+    sh->row[threadIdx.x] = row;
+    const int per = pages_per_thread(t.n_pages);
+    const long long p0 = (long long)threadIdx.x * per;
+    const int p1 = (int)min((long long)t.n_pages, p0 + per);
+    int mine = 0;
+    for (int p = (int)p0; p < p1; ++p) mine += t.refs[p] <= 0;
+    int rank = block_scan(mine, sh->warp_sum, &total_free);       // (its barriers also publish before, need, first, row)
+    for (int p = (int)p0; p < p1 && rank < total_need; ++p) {
+        if (t.refs[p] > 0) continue;
+        int a = 0, b = n - 1;                                       // the last request with before <= rank
+        while (a < b) {
+            const int m = (a + b + 1) >> 1;
+            if (sh->before[m] <= rank) a = m; else b = m - 1;
+        }
+        const int k = (int)(rank - sh->before[a]);
+        if (k < sh->need[a] && sh->before[a] + sh->need[a] <= total_free) {
+            t.page_of[(size_t)sh->row[a] * t.max_pages + sh->first[a] + k] = p;
+            t.refs[p] = 1;
+        }
+        ++rank;
+    }
+    return before + need <= total_free;
+}
+
+// slot of token j: request i with new_off[i] <= j < new_off[i + 1], position len - new + j - new_off[i] (len: after the call)
+__device__ __forceinline__ int slot_of(const TableArgs& t, const int32_t* row, const int32_t* new_off, const int32_t* ok, int n, int j) {
+    if (j < new_off[0] || j >= new_off[n]) return -1;
+    int a = 0, b = n - 1;
+    while (a < b) {
+        const int m = (a + b + 1) >> 1;
+        if (new_off[m] <= j) a = m; else b = m - 1;
+    }
+    if (!ok[a] || j >= new_off[a + 1]) return -1;
+    const int r = row[a];
+    const int pos = t.len[r] - (new_off[a + 1] - j);
+    if (pos < 0) return -1;
+    const int page = t.page_of[(size_t)r * t.max_pages + pos / KV4_PAGE];
+    return page >= 0 && page < t.n_pages ? page * KV4_PAGE + pos % KV4_PAGE : -1;
+}
+
+__global__ void __launch_bounds__(KT_THREADS) k_kv4_extend(const TableArgs t, const int32_t* __restrict__ row, const int32_t* __restrict__ new_off,
+                                                           int n, int32_t* __restrict__ slot, int inline_tokens, int32_t* ok) {
+    __shared__ GrantShared sh;
+    dep_release();
+    const int i = threadIdx.x;
+    sh.row[i] = i < n ? row[i] : -1;
+    __syncthreads();
+    int r = -1, need = 0, first = 0;
+    long long len0 = 0, fresh = 0;
+    if (i < n) {
+        r = sh.row[i];
+        fresh = (long long)new_off[i + 1] - new_off[i];
+        bool fine = r >= 0 && r < t.n_rows && fresh >= 0 && new_off[i] >= 0;
+        for (int j = 0; j < i && fine; ++j) fine = sh.row[j] != r;         // a row named twice: only the first time counts
+        if (fine) {
+            len0 = t.len[r];
+            fine = len0 >= 0 && len0 + fresh <= (long long)t.max_pages * KV4_PAGE;
+        }
+        if (fine) {
+            first = (int)((len0 + KV4_PAGE - 1) / KV4_PAGE);
+            need = (int)((len0 + fresh + KV4_PAGE - 1) / KV4_PAGE) - first;
+        } else {
+            r = -1;
+        }
+    }
+    __syncthreads();
+    const bool granted = grant_pages(t, n, need, first, r, &sh) && r >= 0;
+    if (granted) t.len[r] = (int)(len0 + fresh);
+    if (i < n) ok[i] = granted ? 1 : 0;
+    __syncthreads();                                                       // tables and ok are complete for this block
+    for (int j = i; j < inline_tokens; j += KT_THREADS) slot[j] = slot_of(t, row, new_off, ok, n, j);
+}
+
+__global__ void __launch_bounds__(256) k_kv4_slots(const TableArgs t, const int32_t* row, const int32_t* new_off, int n,
+                                                   int32_t* __restrict__ slot, int n_tokens, const int32_t* ok) {
+    dep_wait();
+    const int j = blockIdx.x * 256 + threadIdx.x;
+    if (j < n_tokens) slot[j] = slot_of(t, row, new_off, ok, n, j);
+}
+
+__global__ void __launch_bounds__(KT_THREADS) k_kv4_fork_plan(const TableArgs t, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
+                                                              int n, int32_t* __restrict__ ok) {
+    __shared__ GrantShared sh;
+    dep_release();
+    const int i = threadIdx.x;
+    sh.row[i] = i < n ? dst[i] : -1;
+    __syncthreads();
+    int r = -1, need = 0, first = 0, len = 0;
+    if (i < n) {
+        const int s = src[i];
+        r = sh.row[i];
+        bool fine = r >= 0 && r < t.n_rows && s >= 0 && s < t.n_rows && s != r;
+        for (int j = 0; j < i && fine; ++j) fine = sh.row[j] != r;
+        if (fine) {
+            len = t.len[s];
+            fine = t.len[r] == 0 && len >= 0 && (long long)len <= (long long)t.max_pages * KV4_PAGE;
+        }
+        if (fine) {
+            first = len / KV4_PAGE;
+            need = len % KV4_PAGE > 0;
+        } else {
+            r = -1;
+        }
+    }
+    __syncthreads();
+    const bool granted = grant_pages(t, n, need, first, r, &sh) && r >= 0;
+    if (granted) t.len[r] = len;                                           // every thread has read its lengths (barriers in grant_pages)
+    if (i < n) ok[i] = granted ? 1 : 0;
+}
+
+// copies `units` pieces of 16 bytes, a block's threads side by side, four loads in flight a thread
+__device__ __forceinline__ void copy16(uint4* __restrict__ to, const uint4* __restrict__ from, int units) {
+    int i = threadIdx.x;
+    const int step = blockDim.x;
+    for (; i + 3 * step < units; i += 4 * step) {
+        const uint4 a = from[i], b = from[i + step], c = from[i + 2 * step], d = from[i + 3 * step];
+        to[i] = a;
+        to[i + step] = b;
+        to[i + 2 * step] = c;
+        to[i + 3 * step] = d;
+    }
+    for (; i < units; i += step) to[i] = from[i];
+}
+
+// block (request, part): part 0 also shares the full pages; every part copies its share of the open page
+__global__ void __launch_bounds__(256) k_kv4_fork_copy(const TableArgs t, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
+                                                       const int32_t* __restrict__ ok, uint8_t* __restrict__ pages, size_t page_bytes, int parts) {
+    dep_wait();
+    const int i = blockIdx.x / parts, part = blockIdx.x - i * parts;
+    if (!ok[i]) return;
+    const int r = dst[i], len = t.len[r];
+    const int32_t* from = t.page_of + (size_t)src[i] * t.max_pages;
+    int32_t* to = t.page_of + (size_t)r * t.max_pages;
+    const int full = len / KV4_PAGE;
+    if (part == 0) {
+        for (int c = threadIdx.x; c < full; c += blockDim.x) {
+            const int p = from[c];
+            to[c] = p;
+            if (p >= 0 && p < t.n_pages) atomicAdd(&t.refs[p], 1);
+        }
+    }
+    if (len % KV4_PAGE) {
+        const int a = from[full], b = to[full];
+        if (a < 0 || a >= t.n_pages || b < 0 || b >= t.n_pages) return;
+        const int units = (int)(page_bytes / 16), u0 = (int)((long long)units * part / parts), u1 = (int)((long long)units * (part + 1) / parts);
+        copy16(reinterpret_cast<uint4*>(pages + (size_t)b * page_bytes) + u0, reinterpret_cast<const uint4*>(pages + (size_t)a * page_bytes) + u0, u1 - u0);
+    }
+}
+
+// a page is given back by whoever takes it out of the table, so that a row named twice gives it back once
+__global__ void __launch_bounds__(256) k_kv4_free(const TableArgs t, const int32_t* __restrict__ row) {
+    const int r = row[blockIdx.x];
+    if (r < 0 || r >= t.n_rows) return;
+    int32_t* entry = t.page_of + (size_t)r * t.max_pages;
+    for (int c = threadIdx.x; c < t.max_pages; c += blockDim.x) {
+        if (entry[c] < 0) continue;
+        const int p = atomicExch(&entry[c], -1);
+        if (p >= 0 && p < t.n_pages) atomicSub(&t.refs[p], 1);
+    }
+    if (threadIdx.x == 0) t.len[r] = 0;
+}
+
+// Where every page goes: with n_used pages in use, the k-th used page above n_used takes the k-th free page below.
+__global__ void __launch_bounds__(KT_THREADS) k_kv4_compact_plan(const TableArgs t, int32_t* __restrict__ moved) {
+    __shared__ int warp_sum[32];
+    __shared__ int holes_before[KT_THREADS + 1];
+    dep_release();
+    const int per = pages_per_thread(t.n_pages);
+    const long long p0 = (long long)threadIdx.x * per;
+    const int p1 = (int)min((long long)t.n_pages, p0 + per);
+    int used = 0, n_used, n_holes, n_movers;
+    for (int p = (int)p0; p < p1; ++p) used += t.refs[p] > 0;
+    block_scan(used, warp_sum, &n_used);
+    int holes = 0, movers = 0;
+    for (int p = (int)p0; p < p1; ++p) {
+        if (p < n_used) holes += t.refs[p] <= 0;
+        else movers += t.refs[p] > 0;
+    }
+    holes_before[threadIdx.x] = block_scan(holes, warp_sum, &n_holes);
+    int rank = block_scan(movers, warp_sum, &n_movers);                    // n_movers = n_holes
+    if (threadIdx.x == 0) holes_before[KT_THREADS] = n_holes;
+    __syncthreads();
+    for (int p = (int)p0; p < p1; ++p) {
+        int to = -1;
+        if (t.refs[p] > 0) {
+            to = p;
+            if (p >= n_used) {
+                int a = 0, b = KT_THREADS - 1;                              // the thread whose pages hold hole number `rank`
+                while (a < b) {
+                    const int m = (a + b + 1) >> 1;
+                    if (holes_before[m] <= rank) a = m; else b = m - 1;
+                }
+                int k = rank - holes_before[a];
+                for (int q = a * per;; ++q)
+                    if (t.refs[q] <= 0 && k-- == 0) { to = q; break; }
+                ++rank;
+            }
+        }
+        moved[p] = to;
+    }
+}
+
+// page (and its count) by page, in parts; and the tables, entry by entry
+__global__ void __launch_bounds__(256) k_kv4_compact_move(const TableArgs t, const int32_t* __restrict__ moved, uint8_t* __restrict__ pages,
+                                                          size_t page_bytes, int parts) {
+    dep_wait();
+    const long long n_entries = (long long)t.n_rows * t.max_pages, step = (long long)gridDim.x * blockDim.x;
+    for (long long e = (long long)blockIdx.x * blockDim.x + threadIdx.x; e < n_entries; e += step) {
+        const int p = t.page_of[e];
+        if (p >= 0) t.page_of[e] = p < t.n_pages ? moved[p] : -1;
+    }
+    const int units = (int)(page_bytes / 16);
+    const long long n_work = (long long)t.n_pages * parts;
+    for (long long w = blockIdx.x; w < n_work; w += gridDim.x) {
+        const int p = (int)(w / parts), part = (int)(w - (long long)p * parts);
+        const int to = moved[p];
+        if (to < 0 || to == p) continue;
+        const int u0 = (int)((long long)units * part / parts), u1 = (int)((long long)units * (part + 1) / parts);
+        copy16(reinterpret_cast<uint4*>(pages + (size_t)to * page_bytes) + u0, reinterpret_cast<const uint4*>(pages + (size_t)p * page_bytes) + u0, u1 - u0);
+        if (part == 0 && threadIdx.x == 0) {
+            t.refs[to] = t.refs[p];
+            t.refs[p] = 0;
+        }
+    }
+}
+
+static TableArgs table_args(const ag_kv4_pool* pool, const ag_kv4_table* t) {
+    return TableArgs{t->page_of, t->len, t->refs, t->n_rows, t->max_pages, (int)pool->n_pages};
+}
+
+// Launch that may come up while the launch before it on the stream finishes; the kernel itself waits for it (dep_wait).
+template <class... P, class... A>
+static cudaError_t launch_dependent(void (*kernel)(P...), unsigned grid, unsigned block, cudaStream_t stream, A... args) {
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof cfg);
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(block);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}
+
+}  // namespace ag
+
+using namespace ag;
+
+extern "C" size_t ag_kv4_page_bytes(int H_kv, int D) {
+    if (H_kv < 1 || H_kv > 1024 || (D != 64 && D != 128)) return 0;
+    return (size_t)H_kv * kv4_head_bytes(D);
+}
+
+static ag_status kv4_rows(bool store, const ag_kv4_pool* pool, const void* K, const void* V, int64_t n_tokens, int64_t k_stride, int64_t v_stride,
+                          const int32_t* slot, void* cuda_stream) {
+    if (!kv4_pool_ok(pool) || n_tokens < 0 || n_tokens > (1ll << 31) - 1) return AG_ERR_ARG;
+    if (n_tokens == 0) return AG_OK;
+    const int64_t width = (int64_t)pool->H_kv * pool->D;
+    if (!K || !V || !slot || (((uintptr_t)K | (uintptr_t)V) & 15u) || ((uintptr_t)slot & 3u) || k_stride < width || v_stride < width || (k_stride % 8) || (v_stride % 8))
+        return AG_ERR_ARG;
+    const long long threads = (long long)n_tokens * pool->H_kv * 2 * (pool->D / 8), blocks = (threads + 255) / 256;
+    if (blocks > 0x7fffffffll) return AG_ERR_ARG;
+    ag_status st = check_arch();
+    if (st != AG_OK) return st;
+    cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
+    const long long n_slots = (long long)pool->n_pages * KV4_PAGE;
+    uint8_t* pages = (uint8_t*)pool->pages;
+    if (store) {
+        auto kernel = pool->D == 128 ? k_kv4_store<128> : k_kv4_store<64>;
+        kernel<<<(unsigned)blocks, 256, 0, stream>>>(pages, n_slots, pool->H_kv, (const uint16_t*)K, (const uint16_t*)V, n_tokens, k_stride, v_stride, slot);
+    } else {
+        auto kernel = pool->D == 128 ? k_kv4_load<128> : k_kv4_load<64>;
+        kernel<<<(unsigned)blocks, 256, 0, stream>>>(pages, n_slots, pool->H_kv, (uint16_t*)const_cast<void*>(K), (uint16_t*)const_cast<void*>(V), n_tokens,
+                                                     k_stride, v_stride, slot);
+    }
+    count_launch();
+    AG_CUDA(cudaGetLastError());
+    return AG_OK;
+}
+
+extern "C" ag_status ag_kv4_store(const ag_kv4_pool* pool, const void* K, const void* V, int64_t n_tokens, int64_t k_stride, int64_t v_stride,
+                                  const int32_t* slot, void* cuda_stream) {
+    return kv4_rows(true, pool, K, V, n_tokens, k_stride, v_stride, slot, cuda_stream);
+}
+
+extern "C" ag_status ag_kv4_load(const ag_kv4_pool* pool, const int32_t* slot, int64_t n_tokens, void* K, void* V, int64_t k_stride, int64_t v_stride,
+                                 void* cuda_stream) {
+    return kv4_rows(false, pool, K, V, n_tokens, k_stride, v_stride, slot, cuda_stream);
+}
+
+extern "C" ag_status ag_kv4_extend(const ag_kv4_pool* pool, const ag_kv4_table* table, const int32_t* row, const int32_t* new_off, int n, int32_t* slot,
+                                   int64_t n_tokens, int32_t* ok, void* cuda_stream) {
+    if (!kv4_pool_ok(pool) || !kv4_table_ok(table) || n < 0 || n > KT_MAX || n_tokens < 0 || n_tokens > (1ll << 31) - 1) return AG_ERR_ARG;
+    if (n == 0 && n_tokens == 0) return AG_OK;
+    if (!row || !new_off || !ok || (n_tokens > 0 && !slot) || n == 0) return AG_ERR_ARG;
+    ag_status st = check_arch();
+    if (st != AG_OK) return st;
+    cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
+    const TableArgs t = table_args(pool, table);
+    const bool one = n_tokens <= KT_INLINE_TOKENS;
+    k_kv4_extend<<<1, KT_THREADS, 0, stream>>>(t, row, new_off, n, slot, one ? (int)n_tokens : 0, ok);
+    AG_CUDA(cudaGetLastError());
+    count_launch();
+    if (!one) {
+        AG_CUDA(launch_dependent(k_kv4_slots, (unsigned)((n_tokens + 255) / 256), 256, stream, t, row, new_off, n, slot, (int)n_tokens, ok));
+        count_launch();
+    }
+    return AG_OK;
+}
+
+extern "C" ag_status ag_kv4_fork(const ag_kv4_pool* pool, const ag_kv4_table* table, const int32_t* src, const int32_t* dst, int n, int32_t* ok,
+                                 void* cuda_stream) {
+    if (!kv4_pool_ok(pool) || !kv4_table_ok(table) || n < 0 || n > KT_MAX) return AG_ERR_ARG;
+    if (n == 0) return AG_OK;
+    if (!src || !dst || !ok) return AG_ERR_ARG;
+    ag_status st = check_arch();
+    if (st != AG_OK) return st;
+    cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
+    const TableArgs t = table_args(pool, table);
+    const size_t page_bytes = ag_kv4_page_bytes(pool->H_kv, pool->D);
+    k_kv4_fork_plan<<<1, KT_THREADS, 0, stream>>>(t, src, dst, n, ok);
+    AG_CUDA(cudaGetLastError());
+    count_launch();
+    const int parts = (int)std::max<size_t>(1, page_bytes / 16384);       // a block copies 16 to 32 KB
+    AG_CUDA(launch_dependent(k_kv4_fork_copy, (unsigned)(n * parts), 256, stream, t, src, dst, (const int32_t*)ok, (uint8_t*)pool->pages, page_bytes, parts));
+    count_launch();
+    return AG_OK;
+}
+
+extern "C" ag_status ag_kv4_free(const ag_kv4_pool* pool, const ag_kv4_table* table, const int32_t* row, int n, void* cuda_stream) {
+    if (!kv4_pool_ok(pool) || !kv4_table_ok(table) || n < 0 || n > KT_MAX) return AG_ERR_ARG;
+    if (n == 0) return AG_OK;
+    if (!row) return AG_ERR_ARG;
+    ag_status st = check_arch();
+    if (st != AG_OK) return st;
+    k_kv4_free<<<(unsigned)n, 256, 0, reinterpret_cast<cudaStream_t>(cuda_stream)>>>(table_args(pool, table), row);
+    AG_CUDA(cudaGetLastError());
+    count_launch();
+    return AG_OK;
+}
+
+extern "C" ag_status ag_kv4_compact(const ag_kv4_pool* pool, const ag_kv4_table* table, int32_t* moved, void* cuda_stream) {
+    if (!kv4_pool_ok(pool) || !kv4_table_ok(table) || !moved || ((uintptr_t)moved & 3u)) return AG_ERR_ARG;
+    ag_status st = check_arch();
+    if (st != AG_OK) return st;
+    cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
+    const TableArgs t = table_args(pool, table);
+    const size_t page_bytes = ag_kv4_page_bytes(pool->H_kv, pool->D);
+    k_kv4_compact_plan<<<1, KT_THREADS, 0, stream>>>(t, moved);
+    AG_CUDA(cudaGetLastError());
+    count_launch();
+    const int parts = (int)std::max<size_t>(1, page_bytes / 16384);
+    const long long work = std::max((long long)t.n_pages * parts, ((long long)t.n_rows * t.max_pages + 255) / 256);
+    AG_CUDA(launch_dependent(k_kv4_compact_move, (unsigned)std::min<long long>(work, 148 * 8), 256, stream, t, (const int32_t*)moved, (uint8_t*)pool->pages,
+                             page_bytes, parts));
+    count_launch();
+    return AG_OK;
+}
