@@ -671,6 +671,23 @@ ag_status ag_kv4_free(const ag_kv4_pool* pool, const ag_kv4_table* table, const 
 ag_status ag_kv4_compact(const ag_kv4_pool* pool, const ag_kv4_table* table, int32_t* moved, void* cuda_stream);
 
 /*
+ * attention_decode_kv4 - O[b][hq][:] = softmax_j(Q[b][hq] . K[j] / sqrt(D)) V[j] over the tokens j of table row row[b], K and V what the cache
+ * holds of KV head hq / (H_q / H_kv): the decode step on the 4-bit cache.  The values are s * code + lo (keys without further
+ * rounding, values rounded to bf16), probabilities are rounded to bf16, sums and softmax statistics are in 32 bits.
+ *   Q, O       device, [B][H_q][D] bf16, 16-byte aligned; H_q a multiple of H_kv, H_q / H_kv <= 1024
+ *   row        device [B], or NULL for row b (then B <= table->n_rows); a row outside the table, or an empty one, gives zeros
+ *   table      lengths are clamped to 0 .. 64 max_pages; tokens whose page is not one of the pool's are left out
+ *   workspace  device, 16-byte aligned, ag_attention_decode_kv4_workspace bytes (0 for many requests or short rows: may be NULL then).
+ *              Its contents mean nothing between calls; calls that may run at the same time need one each
+ * Asynchronous on cuda_stream, may be captured into a graph (lengths and tables are read when it runs).  The split of a long row depends
+ * on the shape (B, heads, max_pages) and the row's length alone, so results are reproducible bit for bit.
+ * Errors: AG_ERR_ARG, AG_ERR_UNSUPPORTED_ARCH, AG_ERR_CUDA.
+ */
+ag_status attention_decode_kv4(const void* Q, const ag_kv4_pool* pool, const ag_kv4_table* table, const int32_t* row, void* O, int B, int H_q,
+                               void* workspace, size_t workspace_bytes, void* cuda_stream);
+size_t ag_attention_decode_kv4_workspace(int B, int H_q, int H_kv, int D, int max_pages);
+
+/*
  * ag_wait_probe - self test of the bounded device-side wait that every kernel of this library
  * uses: one thread waits on a barrier that nothing signals, gives up after limit_ns
  * (<= 1 second) and the call returns AG_ERR_TIMEOUT, with the time actually waited in *waited_ns

@@ -32,6 +32,7 @@ EXPORTED = [
     "gemm_persistent_grouped", "ag_strerror", "ag_last_cuda_error",
     "ag_kernel_launch_count", "ag_kv_pack", "ag_kv_info", "ag_kv_append", "ag_kv_destroy", "attention_decode_persistent",
     "ag_kv4_page_bytes", "ag_kv4_store", "ag_kv4_load", "ag_kv4_extend", "ag_kv4_fork", "ag_kv4_free", "ag_kv4_compact",
+    "attention_decode_kv4", "ag_attention_decode_kv4_workspace",
 ]
 
 
@@ -180,6 +181,9 @@ def lib() -> C.CDLL:
     L.ag_kv4_fork.argtypes = [pool, table, vp, vp, C.c_int, vp, vp]
     L.ag_kv4_free.argtypes = [pool, table, vp, C.c_int, vp]
     L.ag_kv4_compact.argtypes = [pool, table, vp, vp]
+    L.attention_decode_kv4.argtypes = [vp, pool, table, vp, vp, C.c_int, C.c_int, vp, sz, vp]
+    L.ag_attention_decode_kv4_workspace.argtypes = [C.c_int] * 5
+    L.ag_attention_decode_kv4_workspace.restype = sz
     L.ag_cluster_capacity.argtypes = [vp, C.POINTER(TopoMap), C.c_int, C.POINTER(C.c_int32)]
     L.ag_probe_cluster_layout.argtypes = [C.c_int, C.c_int, vp]
     L.ag_topo_save.argtypes = [C.POINTER(TopoMap), C.c_char_p]
@@ -628,6 +632,17 @@ def kv4_free(pool: KV4Pool, table: KV4Table, row_ptr: int, n: int, stream: int =
 def kv4_compact(pool: KV4Pool, table: KV4Table, moved_ptr: int, stream: int = 0):
     """Moves the used pages to the front; moved[p] = the new place of page p, -1 for a free one."""
     _check(lib().ag_kv4_compact(C.byref(pool), C.byref(table), moved_ptr, stream), "ag_kv4_compact")
+
+
+def attention_decode_kv4_workspace(B: int, H_q: int, H_kv: int, D: int, max_pages: int) -> int:
+    return int(lib().ag_attention_decode_kv4_workspace(B, H_q, H_kv, D, max_pages))
+
+
+def attention_decode_kv4(q_ptr: int, pool: KV4Pool, table: KV4Table, row_ptr, o_ptr: int, B: int, H_q: int, workspace_ptr=None,
+                         workspace_bytes: int = 0, stream: int = 0):
+    """One query token per request over the 4-bit cache; request b reads table row row[b] (row_ptr None: row b)."""
+    _check(lib().attention_decode_kv4(q_ptr, C.byref(pool), C.byref(table), row_ptr, o_ptr, B, H_q, workspace_ptr, workspace_bytes, stream),
+           "attention_decode_kv4")
 
 
 def suggest_k_splits(N: int, K: int, sm_budget: int, overlapping_full_chip: bool = False) -> int:
