@@ -1,20 +1,25 @@
 // Single-token attention over the paged 4-bit key/value cache (layout: kv4.cuh).
 //
 // Per request, KV head and page of 64 keys, with the code u and the pair (s, b) of every element (value s u + b), G query heads:
-//     S[key][q]  = sum over groups of 32 d:  s (sum_d u q_d) + b (sum_d q_d)      m16n8k16 MMA: 16 keys x 8 heads x 16 d
+//     S[key][q]  = sum over groups of 32 d:  s (sum_d u q_d) + b (sum_d q_d)      m16n8k16 MMA (fp16): 16 keys x 8 heads x 16 d
 //     P = 2^((S - max) log2 e / sqrt D)                                           running maximum and sum per warp
-//     O[d][q]   += sum_key V[key][d] P[key][q]                                    m16n8k16 MMA: 16 d x 8 heads x 16 keys
-// A code becomes a bf16 operand without arithmetic: 0x4300 | u is 128 + u.  For K the 128 leaves with the base, exactly (the
-// group's sum of q is known in 32 bits): scores carry no rounding besides the 32-bit sums.  V is rounded to bf16 once (its scale varies
-// along the contraction), P once; the sums are in 32 bits.
+//     O[d][q]   += sum_key V[key][d] P[key][q]                                    m16n8k16 MMA (bf16): 16 d x 8 heads x 16 keys
+// A code of K becomes an fp16 operand with one logic instruction, 0x6400 | u = 1024 + u or 0x5400 | u << 4 = 64 + u; what that adds to the
+// scores leaves again, together with the bases' part, through two MMAs of the pairs against sums over q kept in three bf16 parts (24
+// bits), so scores carry no rounding besides the 32-bit sums.  V varies its scale along the contraction: its codes become 128 + u
+// (bf16 0x4300 | u) and then s u + b, rounded to bf16 once; P enters as two bf16 parts, 16 bits.  (An fp8 MMA would take the codes as they
+// are, but mma.sync on this chip converts fp8 operands to fp16 first: measured, slower than the above.)
 //
 // Bound by memory: 1.25 D bytes per key and head.  A byte costs about ten times the arithmetic instructions of a bf16 cache's, so
 // the operands are unpacked in registers, straight into the MMA's fragments - tcgen05.mma would want them in shared memory, one more
 // write and read of the unpacked (four times larger) tile.  The cache stores the codes in fragment order, so a warp's share of a
-// page is read with one conflict-free vector load a lane.  Every warp owns its pages (page w, w + 8, ... of the block's range) and one
-// buffer each for K and V, refilled by 16-byte asynchronous copies as soon as it has been read: K of the next page comes in during the softmax and
-// V's products, V during the next page's scores, with 16 warps an SM in different phases.  No block-wide step until the warps' results are
-// put together.  Long requests are cut into splits (blocks); a second kernel joins them.
+// page is read with conflict-free vector loads.
+//
+// Work: all pages of all (request, KV head) units in one line, cut into equal runs, one per warp, every warp of the launch resident at
+// once (two blocks of eight warps per SM).  A warp walks its run alone - one buffer each for K and V, refilled by 16-byte asynchronous
+// copies as soon as it has been read: K of the next page comes in during the softmax and V's products, V during the next page's scores, while
+// the SM's other warps are in other phases.  Uneven lengths, few long requests and many short ones are the same case.  A unit that one warp has
+// to itself is written at once; otherwise the warps leave their parts in the workspace, in fragment order, for a second kernel to join.
 #include <string.h>
 
 #include <algorithm>
@@ -24,32 +29,49 @@
 namespace ag {
 
 constexpr int DK_WARPS = 8;
-constexpr int DK_MAXSPLIT = 128;
+constexpr int DK_THREADS = DK_WARPS * 32;
+// parts of a unit that the joining block adds up side by side
+__host__ __device__ constexpr int dk_join_lanes(int D, int NB) { return NB * D * 2 * 4 > 1024 ? 2 : 4; }
 
 struct DecodeKv4Args {
     const uint16_t* Q;            // [B][H_q][D]
     uint16_t* O;                  // [B][H_q][D]
     const uint8_t* pages;
     const int32_t *page_of, *len, *row;
-    float* part;                  // [units][splits][heads of a block][D] (splits > 1)
-    float2* stats;                // [units][splits][heads of a block]: maximum (in units of log2), sum
-    int n_pages, H_kv, G, n_rows, max_pages, n_split, h_blocks;
+    float4* part;                 // [2 per warp][NB][D / 16][32 lanes]: unnormalised outputs in fragment order
+    float2* stats;                // [2 per warp][8 NB]: maximum (in units of log2), sum
+    int2* pieces;                 // [units]: first warp of the unit, number of warps
+    int B, n_pages, H_kv, G, n_rows, max_pages, h_blocks, n_warps;
     float scale_log2e;
 };
-
 __device__ __forceinline__ float ex2_ftz(float v) {      // 2^v, relative error 2^-22; 2^-inf = 0
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
 __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_bf16_new(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_f16_new(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ uint32_t movm_trans(uint32_t v) {      // 8 x 8 matrix of 16-bit elements, transposed across the warp
     uint32_t r;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
     return r;
 }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
@@ -57,13 +79,22 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-// nibbles `shift / 4` of both halves of w, each as the bf16 128 + u
-__device__ __forceinline__ uint32_t codes128(uint32_t w, int shift) { return ((w >> shift) & 0x000f000fu) | 0x43004300u; }
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t mask, uint32_t bits) {      // (a & mask) | bits in one instruction
+    uint32_t r;
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(a), "r"(mask), "r"(bits));
+    return r;
+}
+// bf16 128 + u in both halves -> s u + b in bf16, rounded once
 __device__ __forceinline__ uint32_t dequant2(uint32_t c128, uint32_t s, uint32_t b) {
-    const __nv_bfloat162 m128 = __halves2bfloat162(__ushort_as_bfloat16(0xC300), __ushort_as_bfloat16(0xC300));
-    const __nv_bfloat162 u = __hadd2(*reinterpret_cast<const __nv_bfloat162*>(&c128), m128);
-    const __nv_bfloat162 v = __hfma2(u, *reinterpret_cast<const __nv_bfloat162*>(&s), *reinterpret_cast<const __nv_bfloat162*>(&b));
-    return *reinterpret_cast<const uint32_t*>(&v);
+    uint32_t u, v;
+    asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(u) : "r"(c128), "r"(0xC300C300u));
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(v) : "r"(u), "r"(s), "r"(b));
+    return v;
 }
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(reinterpret_cast<uint64_t>(src)) : "memory");
@@ -72,116 +103,218 @@ __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commi
 template <int N>
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// pages of a request that split `sp` of a unit covers; a split gets at least DK_WARPS pages
-__device__ __forceinline__ int splits_in_use(int n_page, int n_split) { return max(1, min(n_split, (n_page + DK_WARPS - 1) / DK_WARPS)); }
-
-template <int D, int NB>
-constexpr int dk_smem_bytes() {
-    return DK_WARPS * kv4_head_bytes(D) > DK_WARPS * 8 * NB * (D + 4) * 4 ? DK_WARPS * kv4_head_bytes(D) : DK_WARPS * 8 * NB * (D + 4) * 4;
+__device__ __forceinline__ int row_tokens(const DecodeKv4Args& x, int b, int* row) {
+    const int r = x.row ? x.row[b] : b;
+    *row = r;
+    return r >= 0 && r < x.n_rows ? min(max(x.len[r], 0), x.max_pages * KV4_PAGE) : 0;
 }
+__device__ __forceinline__ int pages_of(int tokens) { return (tokens + KV4_PAGE - 1) / KV4_PAGE; }
+// the warp whose run holds place `at` of the line: run w begins at total * w / n
+__device__ __forceinline__ int run_holding(long long at, long long total, int n) { return (int)(((at + 1) * n - 1) / total); }
+
+template <int D>
+constexpr int dk_smem_bytes() { return DK_WARPS * kv4_head_bytes(D); }
 
 template <int D, int NB>
-__global__ void __launch_bounds__(DK_WARPS * 32, NB == 1 ? 2 : 1) k_attn_decode_kv4(const DecodeKv4Args x) {
+__global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4(const DecodeKv4Args x) {
     constexpr int NG = D / 32;                     // groups of a row
     constexpr int MT = D / 16;                     // tiles of 16 d
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ float2 warp_stat[DK_WARPS][8 * NB];
+    __shared__ long long before[DK_THREADS + 1];   // pages (of one KV head) in front of the share of requests that thread i counts
+    __shared__ long long warp_sum[DK_WARPS];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     dep_release();
-    const int sp = blockIdx.x % x.n_split, unit = blockIdx.x / x.n_split;
-    const int hb = unit % x.h_blocks, bh = unit / x.h_blocks;
-    const int h = bh % x.H_kv, b = bh / x.H_kv;
-    const int r = x.row ? x.row[b] : b;
-    const bool known = r >= 0 && r < x.n_rows;
-    const int len = known ? min(max(x.len[r], 0), x.max_pages * KV4_PAGE) : 0;
-    const int n_page = (len + KV4_PAGE - 1) / KV4_PAGE;
-    const int in_use = splits_in_use(n_page, x.n_split);
-    if (sp >= in_use) return;                      // (the joining kernel knows)
-    const int p_begin = (int)((long long)n_page * sp / in_use), p_end = (int)((long long)n_page * (sp + 1) / in_use);
-    const int head0 = hb * 8 * NB;                 // first query head of the block, of the KV head's G
-    const uint16_t* q_rows = x.Q + ((size_t)b * x.H_kv + h) * x.G * D;
 
-    // ---- queries as B operands: lane (g, t) holds head g, elements 32 grp + 8 t + {0, 4}, {1, 5}, {2, 6}, {3, 7}
-    uint32_t qf[NB][NG][4];
-    float qsum[NB][NG][2];                         // sums of q over a group, heads 2 t and 2 t + 1
+    // ---- this warp's run: places run, run + 1, ... of the line of pages; order: request, KV head (and block of query heads), page
+    const int heads = x.H_kv * x.h_blocks;
+    const int per = (x.B + DK_THREADS - 1) / DK_THREADS;
+    {
+        long long n = 0;
+        for (int b = threadIdx.x * per, e = min(x.B, b + per), r; b < e; ++b) n += pages_of(row_tokens(x, b, &r));
+        long long inc = n;
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-        const int head = head0 + nb * 8 + g;
-#pragma unroll
-        for (int grp = 0; grp < NG; ++grp) {
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (head < x.G) v = *reinterpret_cast<const uint4*>(q_rows + (size_t)head * D + grp * 32 + t * 8);
-            qf[nb][grp][0] = __byte_perm(v.x, v.z, 0x5410);
-            qf[nb][grp][1] = __byte_perm(v.x, v.z, 0x7632);
-            qf[nb][grp][2] = __byte_perm(v.y, v.w, 0x5410);
-            qf[nb][grp][3] = __byte_perm(v.y, v.w, 0x7632);
-            float s = ((bf16_lo(v.x) + bf16_hi(v.x)) + (bf16_lo(v.y) + bf16_hi(v.y))) + ((bf16_lo(v.z) + bf16_hi(v.z)) + (bf16_lo(v.w) + bf16_hi(v.w)));
-            s += __shfl_xor_sync(0xffffffffu, s, 1);
-            s += __shfl_xor_sync(0xffffffffu, s, 2);
-            qsum[nb][grp][0] = __shfl_sync(0xffffffffu, s, 8 * t);
-            qsum[nb][grp][1] = __shfl_sync(0xffffffffu, s, 8 * t + 4);
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long u = __shfl_up_sync(0xffffffffu, inc, o);
+            if (lane >= o) inc += u;
         }
+        if (lane == 31) warp_sum[warp] = inc;
+        __syncthreads();
+        long long add = 0;
+#pragma unroll
+        for (int w = 0; w < DK_WARPS; ++w) add += w < warp ? warp_sum[w] : 0;
+        before[threadIdx.x] = add + inc - n;
+        if (threadIdx.x == DK_THREADS - 1) before[DK_THREADS] = add + inc;
+        __syncthreads();
     }
+    const long long total = before[DK_THREADS] * heads;
+    const int n_runs = (int)min((long long)x.n_warps, total);
+    const int me = blockIdx.x + gridDim.x * warp;  // neighbouring runs on different SMs: few pages spread over the chip
+    if (me >= n_runs) return;
+    const long long begin = total * me / n_runs;
+    int left = (int)(total * (me + 1) / n_runs - begin);
 
     uint8_t* kbuf = smem + warp * kv4_head_bytes(D);          // codes of K, then K's pairs
     uint8_t* vbuf = kbuf + 40 * D;
     const uint32_t kbuf_a = smem_u32(kbuf), vbuf_a = smem_u32(vbuf);
-    const int32_t* ids = x.page_of + (size_t)(known ? r : 0) * x.max_pages;
-    int id_batch = 0;
-    // this warp's n-th page: its id and the keys of it that count
-    auto page_at = [&](int n, int& id, int& nv) {
-        const int p = p_begin + warp + n * DK_WARPS;
-        if ((n & 31) == 0) {
-            const int pl = p + lane * DK_WARPS;
-            id_batch = pl < p_end ? ids[pl] : -1;
-        }
-        id = __shfl_sync(0xffffffffu, id_batch, n & 31);
-        nv = p < p_end && id >= 0 && id < x.n_pages ? min(KV4_PAGE, len - p * KV4_PAGE) : 0;
-    };
     // copies the runs of 16 tokens that hold keys: codes (8 D bytes a run) and pairs (2 D bytes a run)
-    auto fetch = [&](int which, int id, int nv) {
+    auto fetch = [&](int which, const uint8_t* src, int nv) {
         if (nv > 0) {
-            const uint8_t* src = x.pages + ((size_t)id * x.H_kv + h) * kv4_head_bytes(D);
             const uint32_t dst = which ? vbuf_a : kbuf_a;
-            const int runs = (nv + 15) >> 4;
             const uint8_t* codes = src + which * 32 * D + lane * 16;
             const uint8_t* pairs = src + 64 * D + which * 8 * D + lane * 16;
+            if (nv > 48) {
 #pragma unroll
-            for (int j = 0; j < 32 * D / 512; ++j)
-                if (j * 512 < runs * 8 * D) cp_async16(dst + j * 512 + lane * 16, codes + j * 512);
+                for (int j = 0; j < 32 * D / 512; ++j) cp_async16(dst + j * 512 + lane * 16, codes + j * 512);
 #pragma unroll
-            for (int j = 0; j < 8 * D / 512; ++j)
-                if (j * 512 + lane * 16 < runs * 2 * D) cp_async16(dst + 32 * D + j * 512 + lane * 16, pairs + j * 512);
+                for (int j = 0; j < 8 * D / 512; ++j) cp_async16(dst + 32 * D + j * 512 + lane * 16, pairs + j * 512);
+            } else {
+                const int runs = (nv + 15) >> 4;
+                for (int j = lane * 16; j < runs * 8 * D; j += 512) cp_async16(dst + j, codes + (j - lane * 16));
+                for (int j = lane * 16; j < runs * 2 * D; j += 512) cp_async16(dst + 32 * D + j, pairs + (j - lane * 16));
+            }
         }
         cp_async_commit();
     };
 
+    // ---- the page to be fetched next: request b, head hh (KV head, block), page p of np
+    int b, hh, p, np, len, row;
+    {
+        const long long at = begin / heads;
+        int lo = 0, hi = DK_THREADS - 1;           // the last share that begins at or in front of it
+        while (lo < hi) {
+            const int m = (lo + hi + 1) >> 1;
+            if (before[m] <= at) lo = m; else hi = m - 1;
+        }
+        b = lo * per;
+        long long in_front = before[lo];
+        while (true) {
+            len = row_tokens(x, b, &row);
+            np = pages_of(len);
+            if (in_front + np > at) break;
+            in_front += np;
+            ++b;
+        }
+        const long long rest = begin - in_front * heads;
+        hh = (int)(rest / np);
+        p = (int)(rest - (long long)hh * np);
+    }
+    long long unit_begin = begin - p;              // place of the unit's first page
+    int id_batch = 0, id_first = -64;              // ids of pages id_first + lane of the row (reloaded as p leaves them)
+    const uint8_t* src_next = nullptr;
+    int nv_next = 0;
+    auto locate = [&]() {                          // source and number of keys of page p
+        if (p < id_first || p >= id_first + 32) {
+            id_first = p;
+            id_batch = p + lane < np ? x.page_of[(size_t)row * x.max_pages + p + lane] : -1;
+        }
+        const int id = __shfl_sync(0xffffffffu, id_batch, p - id_first);
+        nv_next = id >= 0 && id < x.n_pages ? min(KV4_PAGE, len - p * KV4_PAGE) : 0;
+        src_next = x.pages + ((size_t)(nv_next ? id : 0) * x.H_kv + hh / x.h_blocks) * kv4_head_bytes(D);
+    };
+    locate();
+    fetch(0, src_next, nv_next);
+    fetch(1, src_next, nv_next);
+
+    uint32_t qf[NB][NG][4];
+    uint32_t qb[NB][2], qs[NB][2];
+    float unscale[NB][2];                          // log2 e / (c sqrt D) of heads 2 t and 2 t + 1
     float o[NB][MT][4];
     float m[NB][2], l[NB][2];
+    bool fresh = true;                             // the page in hand is the first of a unit for this warp
+    while (left > 0) {
+        const int b_now = b, hh_now = hh, p_now = p, np_now = np, nv = nv_next;
+        const int head0 = hh_now % x.h_blocks * 8 * NB;       // first query head of the block, of the KV head's G
+        const long long unit_now = unit_begin;
+        if (fresh) {
+            const uint16_t* q_rows = x.Q + ((size_t)b_now * x.H_kv + hh_now / x.h_blocks) * x.G * D;
+            // ---- queries as B operands: q times a power of two c (the head's largest |q| between 128 and 256) in fp16, exact down to
+            // 2^-22 of the largest.  Lane (g, t) holds head g, elements 32 grp + 8 t + {0, 4}, {1, 5}, {2, 6}, {3, 7}.  Even elements meet
+            // 1024 + u, odd ones 64 + u (see the scores): what the 1024 and 64 add is taken out with the bases, by MMAs of the
+            // pairs against the groups' sums of q (qb) and of what is added (qs), 24 bits each in three bf16 parts.
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
+            for (int nb = 0; nb < NB; ++nb) {
+                const int head = head0 + nb * 8 + g;
+                float q[NG][8], top = 0.f;
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+                for (int grp = 0; grp < NG; ++grp) {
+                    uint4 v = make_uint4(0, 0, 0, 0);
+                    if (head < x.G) v = *reinterpret_cast<const uint4*>(q_rows + (size_t)head * D + grp * 32 + t * 8);
+                    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-            for (int c = 0; c < 4; ++c) o[nb][i][c] = 0.f;
-        m[nb][0] = m[nb][1] = -INFINITY;
-        l[nb][0] = l[nb][1] = 0.f;
-    }
-    const int n_mine = p_end - p_begin > warp ? (p_end - p_begin - warp + DK_WARPS - 1) / DK_WARPS : 0;
-    int id, nv, id_next = -1, nv_next = 0;
-    if (n_mine > 0) {
-        page_at(0, id, nv);
-        fetch(0, id, nv);
-        fetch(1, id, nv);
-    }
-    for (int n = 0; n < n_mine; ++n) {
+                    for (int i = 0; i < 4; ++i) {
+                        q[grp][2 * i] = bf16_lo(w[i]);
+                        q[grp][2 * i + 1] = bf16_hi(w[i]);
+                        top = fmaxf(top, fmaxf(fabsf(q[grp][2 * i]), fabsf(q[grp][2 * i + 1])));
+                    }
+                }
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                const uint32_t e = min(246u, 261u - (__float_as_uint(top) >> 23));        // exponent field of c
+                const float c = __uint_as_float(e << 23);
+                uint32_t sums[NG][3], adds[NG][3];         // parts, as bf16 bits
+#pragma unroll
+                for (int grp = 0; grp < NG; ++grp) {
+                    float even = 0.f, odd = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 8; i += 2) {
+                        q[grp][i] *= c;
+                        q[grp][i + 1] *= c;
+                        even += q[grp][i];
+                        odd += q[grp][i + 1];
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) qf[nb][grp][i] = pack_f16(q[grp][i], q[grp][i + 4]);
+#pragma unroll
+                    for (int w = 1; w < 4; w <<= 1) {
+                        even += __shfl_xor_sync(0xffffffffu, even, w);
+                        odd += __shfl_xor_sync(0xffffffffu, odd, w);
+                    }
+                    float sum = even + odd, add = -1024.f * even - 64.f * odd;
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) {
+                        const __nv_bfloat16 a = __float2bfloat16_rn(sum), d = __float2bfloat16_rn(add);
+                        sums[grp][k] = __bfloat16_as_ushort(a);
+                        adds[grp][k] = __bfloat16_as_ushort(d);
+                        sum -= __bfloat162float(a);
+                        add -= __bfloat162float(d);
+                    }
+                }
+                if (D == 128) {      // k = 2 t, 2 t + 1: groups 2 (t & 1), + 1 of part t / 2; k + 8: of part 2 (t < 2)
+                    const int lo = 0, hi = NG - 2;
+                    const uint32_t s0 = t < 2 ? sums[lo][0] | sums[lo + 1][0] << 16 : sums[lo][1] | sums[lo + 1][1] << 16;
+                    const uint32_t s1 = t < 2 ? sums[hi][0] | sums[hi + 1][0] << 16 : sums[hi][1] | sums[hi + 1][1] << 16;
+                    const uint32_t a0 = t < 2 ? adds[lo][0] | adds[lo + 1][0] << 16 : adds[lo][1] | adds[lo + 1][1] << 16;
+                    const uint32_t a1 = t < 2 ? adds[hi][0] | adds[hi + 1][0] << 16 : adds[hi][1] | adds[hi + 1][1] << 16;
+                    qb[nb][0] = (t & 1) ? s1 : s0;
+                    qs[nb][0] = (t & 1) ? a1 : a0;
+                    qb[nb][1] = t >= 2 ? 0u : (t & 1) ? sums[hi][2] | sums[hi + 1][2] << 16 : sums[lo][2] | sums[lo + 1][2] << 16;
+                    qs[nb][1] = t >= 2 ? 0u : (t & 1) ? adds[hi][2] | adds[hi + 1][2] << 16 : adds[lo][2] | adds[lo + 1][2] << 16;
+                } else {             // both groups, part t
+                    qb[nb][0] = t == 0 ? sums[0][0] | sums[1][0] << 16 : t == 1 ? sums[0][1] | sums[1][1] << 16 : t == 2 ? sums[0][2] | sums[1][2] << 16 : 0u;
+                    qs[nb][0] = t == 0 ? adds[0][0] | adds[1][0] << 16 : t == 1 ? adds[0][1] | adds[1][1] << 16 : t == 2 ? adds[0][2] | adds[1][2] << 16 : 0u;
+                    qb[nb][1] = qs[nb][1] = 0u;
+                }
+                const float f = x.scale_log2e * __uint_as_float((254u - e) << 23);
+                unscale[nb][0] = __shfl_sync(0xffffffffu, f, 8 * t);
+                unscale[nb][1] = __shfl_sync(0xffffffffu, f, 8 * t + 4);
+            }
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) o[nb][i][c] = 0.f;
+                m[nb][0] = m[nb][1] = -INFINITY;
+                l[nb][0] = l[nb][1] = 0.f;
+            }
+        }
         cp_async_wait<1>();                        // K of this page has landed
         __syncwarp();
         float s[NB][4][4];
 #pragma unroll
         for (int run = 0; run < 4; ++run) {
             if (run * 16 < nv) {
-                uint32_t w[2][NG], sb[2][NG];      // rows g and g + 8 of the run
+                uint32_t w[2][NG], sb[2][NG], bb[2], ss[2];     // rows g and g + 8 of the run: codes, pairs, two groups' bases and scales as A operands
 #pragma unroll
                 for (int hh = 0; hh < 2; ++hh) {
                     const uint8_t* at = kbuf + run * 8 * D + hh * 4 * D + lane * (D / 8);
@@ -189,68 +322,95 @@ __global__ void __launch_bounds__(DK_WARPS * 32, NB == 1 ? 2 : 1) k_attn_decode_
                     if (D == 128) {
                         *reinterpret_cast<uint4*>(&w[hh][0]) = *reinterpret_cast<const uint4*>(at);
                         *reinterpret_cast<uint4*>(&sb[hh][0]) = *reinterpret_cast<const uint4*>(ps);
+                        const uint2 two = *reinterpret_cast<const uint2*>(ps + (t & 1) * 8);
+                        bb[hh] = __byte_perm(two.x, two.y, 0x7632);
+                        ss[hh] = __byte_perm(two.x, two.y, 0x5410);
                     } else {
                         *reinterpret_cast<uint2*>(&w[hh][0]) = *reinterpret_cast<const uint2*>(at);
                         *reinterpret_cast<uint2*>(&sb[hh][0]) = *reinterpret_cast<const uint2*>(ps);
+                        bb[hh] = __byte_perm(sb[hh][0], sb[hh][1], 0x7632);
+                        ss[hh] = __byte_perm(sb[hh][0], sb[hh][1], 0x5410);
                     }
                 }
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) s[nb][run][c] = 0.f;
+                for (int nb = 0; nb < NB; ++nb) {
+                    mma_bf16_new(s[nb][run], bb[0], bb[1], D == 128 ? bb[0] : 0u, D == 128 ? bb[1] : 0u, qb[nb][0], qb[nb][1]);
+                    mma_bf16(s[nb][run], ss[0], ss[1], D == 128 ? ss[0] : 0u, D == 128 ? ss[1] : 0u, qs[nb][0], qs[nb][1]);
+                }
 #pragma unroll
                 for (int grp = 0; grp < NG; ++grp) {
                     const float s0 = bf16_lo(sb[0][grp]), s1 = bf16_lo(sb[1][grp]);
-                    const float b0 = fmaf(-128.f, s0, bf16_hi(sb[0][grp])), b1 = fmaf(-128.f, s1, bf16_hi(sb[1][grp]));
-                    uint32_t a[8];
+                    // fp16 0x6400 | u = 1024 + u; 0x5400 | u << 4 = 64 + u: two nibbles of a half word without a shift
+                    uint32_t a[2][4];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        a[2 * k] = codes128(w[0][grp], 4 * k);
-                        a[2 * k + 1] = codes128(w[1][grp], 4 * k);
+                    for (int hh = 0; hh < 2; ++hh) {
+                        const uint32_t w8 = w[hh][grp] >> 8;
+                        a[hh][0] = and_or(w[hh][grp], 0x000f000fu, 0x64006400u);
+                        a[hh][1] = and_or(w[hh][grp], 0x00f000f0u, 0x54005400u);
+                        a[hh][2] = and_or(w8, 0x000f000fu, 0x64006400u);
+                        a[hh][3] = and_or(w8, 0x00f000f0u, 0x54005400u);
                     }
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb) {
-                        float acc[4] = {0.f, 0.f, 0.f, 0.f};
-                        mma_bf16(acc, a[0], a[1], a[2], a[3], qf[nb][grp][0], qf[nb][grp][1]);
-                        mma_bf16(acc, a[4], a[5], a[6], a[7], qf[nb][grp][2], qf[nb][grp][3]);
-                        s[nb][run][0] += fmaf(s0, acc[0], b0 * qsum[nb][grp][0]);
-                        s[nb][run][1] += fmaf(s0, acc[1], b0 * qsum[nb][grp][1]);
-                        s[nb][run][2] += fmaf(s1, acc[2], b1 * qsum[nb][grp][0]);
-                        s[nb][run][3] += fmaf(s1, acc[3], b1 * qsum[nb][grp][1]);
+                        float acc[4];
+                        mma_f16_new(acc, a[0][0], a[1][0], a[0][1], a[1][1], qf[nb][grp][0], qf[nb][grp][1]);
+                        mma_f16(acc, a[0][2], a[1][2], a[0][3], a[1][3], qf[nb][grp][2], qf[nb][grp][3]);
+                        s[nb][run][0] = fmaf(s0, acc[0], s[nb][run][0]);
+                        s[nb][run][1] = fmaf(s0, acc[1], s[nb][run][1]);
+                        s[nb][run][2] = fmaf(s1, acc[2], s[nb][run][2]);
+                        s[nb][run][3] = fmaf(s1, acc[3], s[nb][run][3]);
                     }
                 }
             }
         }
         __syncwarp();                              // every lane has read K
-        if (n + 1 < n_mine) page_at(n + 1, id_next, nv_next);
-        else nv_next = 0;
-        fetch(0, id_next, nv_next);
+        // ---- on to the next page: same unit, next head, next request that has any
+        --left;
+        nv_next = 0;
+        if (left > 0) {
+            if (++p == np) {
+                unit_begin += np;
+                p = 0;
+                if (++hh == heads) {
+                    hh = 0;
+                    do {
+                        ++b;
+                        len = row_tokens(x, b, &row);
+                        np = pages_of(len);
+                    } while (np == 0);
+                    id_first = -64;
+                }
+            }
+            locate();
+        }
+        fetch(0, src_next, nv_next);
         if (nv > 0) {
-            // ---- softmax: keys past the end count as -inf
+            // ---- softmax, with the running maximum in the scores' own units; keys past the end count as -inf
+            if (nv < KV4_PAGE) {
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int run = 0; run < 4; ++run)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+                            if (run * 16 + g + (c >> 1) * 8 >= nv) s[nb][run][c] = -INFINITY;
+            }
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
                 float top[2] = {m[nb][0], m[nb][1]};
 #pragma unroll
                 for (int run = 0; run < 4; ++run)
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const float v = run * 16 + g + (c >> 1) * 8 < nv ? s[nb][run][c] * x.scale_log2e : -INFINITY;
-                        s[nb][run][c] = v;
-                        top[c & 1] = fmaxf(top[c & 1], v);
-                    }
+                    for (int c = 0; c < 4; ++c) top[c & 1] = fmaxf(top[c & 1], s[nb][run][c]);
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
 #pragma unroll
                     for (int w = 4; w < 32; w <<= 1) top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], w));
-                float f[2], ref[2];
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    ref[e] = top[e] == -INFINITY ? 0.f : top[e];
-                    f[e] = ex2_ftz(m[nb][e] - ref[e]);
-                }
                 if (__any_sync(0xffffffffu, top[0] != m[nb][0] || top[1] != m[nb][1])) {
+                    float f[2];
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
+                        f[e] = top[e] == m[nb][e] ? 1.f : ex2_ftz((m[nb][e] - top[e]) * unscale[nb][e]);
                         l[nb][e] *= f[e];
                         m[nb][e] = top[e];
                     }
@@ -259,26 +419,36 @@ __global__ void __launch_bounds__(DK_WARPS * 32, NB == 1 ? 2 : 1) k_attn_decode_
 #pragma unroll
                         for (int c = 0; c < 4; ++c) o[nb][i][c] *= f[c & 1];
                 }
+                float ref[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) ref[e] = m[nb][e] == -INFINITY ? 0.f : m[nb][e] * unscale[nb][e];
 #pragma unroll
                 for (int run = 0; run < 4; ++run)
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        s[nb][run][c] = ex2_ftz(s[nb][run][c] - ref[c & 1]);
+                        s[nb][run][c] = ex2_ftz(fmaf(s[nb][run][c], unscale[nb][c & 1], -ref[c & 1]));
                         l[nb][c & 1] += s[nb][run][c];
                     }
             }
         }
         cp_async_wait<1>();                        // V of this page has landed
         __syncwarp();
+        if (nv < KV4_PAGE) {                       // what lies behind the last key may be anything: it must not meet a probability of zero as NaN
+            for (int i = nv * NG + lane; i < (nv + 15) / 16 * 16 * NG; i += 32) *reinterpret_cast<uint32_t*>(vbuf + 32 * D + i * 4) = 0u;
+            __syncwarp();
+        }
 #pragma unroll
         for (int run = 0; run < 4; ++run) {
             if (run * 16 < nv) {
-                uint32_t pf[NB][2];
+                uint32_t pf[NB][4];                // probabilities as B operands, high parts and low parts
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) {
-                    pf[nb][0] = movm_trans(pack_bf16(s[nb][run][0], s[nb][run][1]));
-                    pf[nb][1] = movm_trans(pack_bf16(s[nb][run][2], s[nb][run][3]));
-                }
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const uint32_t hi = pack_bf16(s[nb][run][2 * e], s[nb][run][2 * e + 1]);
+                        pf[nb][e] = movm_trans(hi);
+                        pf[nb][2 + e] = movm_trans(pack_bf16(s[nb][run][2 * e] - bf16_lo(hi), s[nb][run][2 * e + 1] - bf16_hi(hi)));
+                    }
                 uint32_t xs[2][2][NG / 2], vs[2][NG], vb[2][NG];       // codes by (h, j): two keys side by side; pairs of scales and of bases
 #pragma unroll
                 for (int hh = 0; hh < 2; ++hh) {
@@ -301,13 +471,6 @@ __global__ void __launch_bounds__(DK_WARPS * 32, NB == 1 ? 2 : 1) k_attn_decode_
                         *reinterpret_cast<uint2*>(&pa[0][0]) = *reinterpret_cast<const uint2*>(ps);
                         *reinterpret_cast<uint2*>(&pa[1][0]) = *reinterpret_cast<const uint2*>(ps + 8);
                     }
-                    if (nv < KV4_PAGE) {           // what lies behind the last key may be anything: it must not meet a probability of zero as NaN
-#pragma unroll
-                        for (int e = 0; e < 2; ++e)
-                            if (key + e >= nv)
-#pragma unroll
-                                for (int grp = 0; grp < NG; ++grp) pa[e][grp] = 0;
-                    }
 #pragma unroll
                     for (int grp = 0; grp < NG; ++grp) {
                         vs[hh][grp] = __byte_perm(pa[0][grp], pa[1][grp], 0x5410);
@@ -317,114 +480,142 @@ __global__ void __launch_bounds__(DK_WARPS * 32, NB == 1 ? 2 : 1) k_attn_decode_
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
                     const int grp = i >> 1, half = i >> 2, sh = 4 * (i & 3);
-                    const uint32_t a0 = dequant2(codes128(xs[0][0][half], sh), vs[0][grp], vb[0][grp]);
-                    const uint32_t a1 = dequant2(codes128(xs[0][1][half], sh), vs[0][grp], vb[0][grp]);
-                    const uint32_t a2 = dequant2(codes128(xs[1][0][half], sh), vs[1][grp], vb[1][grp]);
-                    const uint32_t a3 = dequant2(codes128(xs[1][1][half], sh), vs[1][grp], vb[1][grp]);
+                    const uint32_t a0 = dequant2(and_or(xs[0][0][half] >> sh, 0x000f000fu, 0x43004300u), vs[0][grp], vb[0][grp]);
+                    const uint32_t a1 = dequant2(and_or(xs[0][1][half] >> sh, 0x000f000fu, 0x43004300u), vs[0][grp], vb[0][grp]);
+                    const uint32_t a2 = dequant2(and_or(xs[1][0][half] >> sh, 0x000f000fu, 0x43004300u), vs[1][grp], vb[1][grp]);
+                    const uint32_t a3 = dequant2(and_or(xs[1][1][half] >> sh, 0x000f000fu, 0x43004300u), vs[1][grp], vb[1][grp]);
 #pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) mma_bf16(o[nb][i], a0, a1, a2, a3, pf[nb][0], pf[nb][1]);
+                    for (int nb = 0; nb < NB; ++nb) {
+                        mma_bf16(o[nb][i], a0, a1, a2, a3, pf[nb][0], pf[nb][1]);
+                        mma_bf16(o[nb][i], a0, a1, a2, a3, pf[nb][2], pf[nb][3]);
+                    }
                 }
             }
         }
         __syncwarp();                              // every lane has read V
-        fetch(1, id_next, nv_next);
-        id = id_next;
-        nv = nv_next;
+        fetch(1, src_next, nv_next);
+
+        // ---- the end of the unit, or of this warp's share of it
+        fresh = p_now + 1 == np_now;
+        if (fresh || left == 0) {
+            const int unit = b_now * heads + hh_now;
+            const int w0 = run_holding(unit_now, total, n_runs), w1 = run_holding(unit_now + np_now - 1, total, n_runs);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int w = 4; w < 32; w <<= 1) l[nb][e] += __shfl_xor_sync(0xffffffffu, l[nb][e], w);
+            if (w0 == me && lane == 0) x.pieces[unit] = make_int2(w0, w1 - w0 + 1);
+            if (w0 == w1) {
+                // all of it: lanes (g, t) have heads 2 t, 2 t + 1 of d = 16 i + g, + 8; transposed, head g of d = 16 i + 2 t, + 1, ...
+                uint16_t* out = x.O + ((size_t)(b_now * x.H_kv + hh_now / x.h_blocks) * x.G + head0) * D;
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    const float r0 = l[nb][0] == 0.f ? 0.f : 1.f / l[nb][0], r1 = l[nb][1] == 0.f ? 0.f : 1.f / l[nb][1];
+#pragma unroll
+                    for (int i = 0; i < MT; ++i)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const uint32_t v = movm_trans(pack_bf16(o[nb][i][2 * e] * r0, o[nb][i][2 * e + 1] * r1));
+                            if (head0 + nb * 8 + g < x.G) *reinterpret_cast<uint32_t*>(out + (nb * 8 + g) * D + i * 16 + e * 8 + 2 * t) = v;
+                        }
+                }
+            } else {
+                const size_t slot = 2 * (size_t)me + (w0 == me ? 1 : 0);
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        if (g == 0) x.stats[slot * 8 * NB + nb * 8 + 2 * t + e] = make_float2(m[nb][e] == -INFINITY ? -INFINITY : m[nb][e] * unscale[nb][e], l[nb][e]);
+                    if (head0 + nb * 8 + 2 * t < x.G)
+#pragma unroll
+                        for (int i = 0; i < MT; ++i)
+                            x.part[((slot * NB + nb) * MT + i) * 32 + lane] = make_float4(o[nb][i][0], o[nb][i][1], o[nb][i][2], o[nb][i][3]);
+                }
+            }
+        }
     }
     cp_async_wait<0>();
+}
 
-    // ---- put the warps together: maxima and sums, then the outputs through shared memory
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-#pragma unroll
-            for (int w = 4; w < 32; w <<= 1) l[nb][e] += __shfl_xor_sync(0xffffffffu, l[nb][e], w);
-            if (g == 0) warp_stat[warp][nb * 8 + 2 * t + e] = make_float2(m[nb][e], l[nb][e]);
+// adds a part (maximum pm, sum pl, two outputs) to what has been joined so far; pl = 0: a part without keys
+__device__ __forceinline__ void join_part(float& m, float& l, float& a, float& b, float pm, float pl, float pa, float pb) {
+    if (pl == 0.f) return;
+    const float top = fmaxf(m, pm);
+    const float f = l == 0.f ? 0.f : ex2_ftz(m - top), pf = pm == top ? 1.f : ex2_ftz(pm - top);
+    l = fmaf(f, l, pf * pl);
+    a = fmaf(f, a, pf * pa);
+    b = fmaf(f, b, pf * pb);
+    m = top;
+}
+
+// One block per unit, thread (j, y): fragment j of the output, parts y, y + LANES, ...:  O = sum_c 2^(m_c - m) O_c / sum_c 2^(m_c - m) l_c.
+// A part without a key that counts has m_c = -inf, l_c = 0 and is left out; requests without keys get zeros.
+template <int D, int NB>
+__global__ void __launch_bounds__(NB * D * 2 * dk_join_lanes(D, NB)) k_attn_join_kv4(const DecodeKv4Args x) {
+    constexpr int MT = D / 16, NF = NB * MT * 32, LANES = dk_join_lanes(D, NB);
+    __shared__ float4 acc[LANES - 1][NF];
+    __shared__ float4 stat[LANES - 1][NF];
+    dep_wait();
+    const int heads = x.H_kv * x.h_blocks, b = blockIdx.x / heads, hh = blockIdx.x - b * heads;
+    const int j = threadIdx.x, y = threadIdx.y, lane = j & 31, g = lane >> 2, t = lane & 3, i = (j >> 5) % MT, nb = (j >> 5) / MT;
+    int row;
+    const bool empty = row_tokens(x, b, &row) == 0;
+    const int2 pc = empty ? make_int2(0, 0) : x.pieces[blockIdx.x];
+    if (pc.y == 1) return;                         // written already
+    const int head = hh % x.h_blocks * 8 * NB + nb * 8 + 2 * t;
+    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (head < x.G) {
+        auto slot = [&](int c) { return 2 * (size_t)(pc.x + c) + (c == 0 ? 1 : 0); };
+#pragma unroll 4
+        for (int c = y; c < pc.y; c += LANES) {
+            const float4 st = __ldcg(reinterpret_cast<const float4*>(&x.stats[slot(c) * 8 * NB + nb * 8 + 2 * t]));
+            const float4 u = __ldcg(&x.part[((slot(c) * NB + nb) * MT + i) * 32 + lane]);
+            join_part(m0, l0, v.x, v.z, st.x, st.y, u.x, u.z);
+            join_part(m1, l1, v.y, v.w, st.z, st.w, u.y, u.w);
         }
-    __syncthreads();                               // also: every warp is done with its buffers
-    float* osum = reinterpret_cast<float*>(smem);
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-        float top[2] = {-INFINITY, -INFINITY}, f[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-#pragma unroll
-            for (int w = 0; w < DK_WARPS; ++w) top[e] = fmaxf(top[e], warp_stat[w][nb * 8 + 2 * t + e].x);
-            f[e] = m[nb][e] == -INFINITY ? 0.f : ex2_ftz(m[nb][e] - top[e]);
-        }
-        float* to = osum + ((size_t)warp * 8 * NB + nb * 8 + 2 * t) * (D + 4) + g;
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int c = 0; c < 4; ++c) to[(c & 1) * (D + 4) + i * 16 + (c >> 1) * 8] = f[c & 1] == 0.f ? 0.f : o[nb][i][c] * f[c & 1];
+    }
+    if (y > 0) {
+        acc[y - 1][j] = v;
+        stat[y - 1][j] = make_float4(m0, l0, m1, l1);
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < 8 * NB * D; i += DK_WARPS * 32) {
-        const int q = i / D, d = i - q * D;
-        if (head0 + q >= x.G) break;
-        float top = -INFINITY, sum = 0.f, acc = 0.f;
+    if (y > 0 || head >= x.G) return;
 #pragma unroll
-        for (int w = 0; w < DK_WARPS; ++w) top = fmaxf(top, warp_stat[w][q].x);
-#pragma unroll
-        for (int w = 0; w < DK_WARPS; ++w) {
-            const float2 st = warp_stat[w][q];
-            if (st.y != 0.f) sum = fmaf(st.y, ex2_ftz(st.x - top), sum);      // 0: the warp had no keys
-            acc += osum[((size_t)w * 8 * NB + q) * (D + 4) + d];
-        }
-        if (x.n_split == 1) {
-            const __nv_bfloat16 v = __float2bfloat16_rn(n_page == 0 || sum == 0.f ? 0.f : acc / sum);
-            x.O[((size_t)bh * x.G + head0 + q) * D + d] = __bfloat16_as_ushort(v);
-        } else {
-            const size_t at = ((size_t)unit * x.n_split + sp) * 8 * NB + q;
-            x.part[at * D + d] = acc;
-            if (d == 0) x.stats[at] = make_float2(top, sum);
-        }
+    for (int k = 0; k < LANES - 1; ++k) {
+        const float4 u = acc[k][j], st = stat[k][j];
+        join_part(m0, l0, v.x, v.z, st.x, st.y, u.x, u.z);
+        join_part(m1, l1, v.y, v.w, st.z, st.w, u.y, u.w);
+    }
+    const float r0 = l0 == 0.f ? 0.f : 1.f / l0, r1 = l1 == 0.f ? 0.f : 1.f / l1;
+    uint16_t* out = x.O + ((size_t)(b * x.H_kv + hh / x.h_blocks) * x.G + head) * D + 16 * i + g;
+    out[0] = __bfloat16_as_ushort(__float2bfloat16_rn(v.x * r0));
+    out[8] = __bfloat16_as_ushort(__float2bfloat16_rn(v.z * r0));
+    if (head + 1 < x.G) {
+        out[D] = __bfloat16_as_ushort(__float2bfloat16_rn(v.y * r1));
+        out[D + 8] = __bfloat16_as_ushort(__float2bfloat16_rn(v.w * r1));
     }
 }
 
-// One block per (request, query head), thread = d: O = sum_c 2^(m_c - m) O_c / sum_c 2^(m_c - m) l_c over the splits in use.
-template <int D>
-__global__ void __launch_bounds__(D) k_attn_join_kv4(const DecodeKv4Args x, int heads) {
-    dep_wait();
-    const int q = blockIdx.x % x.G, bh = blockIdx.x / x.G, b = bh / x.H_kv, d = threadIdx.x;
-    const int r = x.row ? x.row[b] : b;
-    const int len = r >= 0 && r < x.n_rows ? min(max(x.len[r], 0), x.max_pages * KV4_PAGE) : 0;
-    const int in_use = splits_in_use((len + KV4_PAGE - 1) / KV4_PAGE, x.n_split);
-    const size_t at = ((size_t)(bh * x.h_blocks + q / heads) * x.n_split) * heads + q % heads;
-    float m = -INFINITY;
-    for (int c = 0; c < in_use; ++c) m = fmaxf(m, __ldcg(&x.stats[at + (size_t)c * heads]).x);
-    float num = 0.f, den = 0.f;
-#pragma unroll 4
-    for (int c = 0; c < in_use; ++c) {
-        const float2 st = __ldcg(&x.stats[at + (size_t)c * heads]);
-        const float v = __ldcg(&x.part[(at + (size_t)c * heads) * D + d]);
-        if (st.y != 0.f) {
-            const float w = ex2_ftz(st.x - m);
-            num = fmaf(w, v, num);
-            den = fmaf(w, st.y, den);
-        }
-    }
-    x.O[((size_t)bh * x.G + q) * D + d] = __bfloat16_as_ushort(__float2bfloat16_rn(den == 0.f ? 0.f : num / den));
-}
-
-// Heads of a block (8 or 16 rows of the MMA's N side), blocks per KV head, splits per unit - from the shape alone, so that the
-// workspace can be sized without a device.  Splits: enough blocks for four rounds of two blocks on each of 148 SMs, none below DK_WARPS pages.
+// Blocks of query heads (8 or 16 rows of the MMA's N side), warps - from the shape alone, so that the workspace can be sized without a
+// device.  Every warp is resident at once: 148 SMs times two blocks of eight warps with 8 heads, one with 16 (255 registers a thread).
 struct DecodeKv4Shape {
-    int heads, h_blocks, n_split;
+    int nb, h_blocks, n_blocks;
     long long units;
 };
 static bool decode_kv4_shape(long long B, int H_q, int H_kv, int D, int max_pages, DecodeKv4Shape* s) {
     if (B < 1 || H_kv < 1 || H_kv > 1024 || H_q < H_kv || H_q % H_kv || (D != 64 && D != 128) || max_pages < 1 || max_pages >= (1 << 25)) return false;
     const int G = H_q / H_kv;
     if (G > 1024) return false;
-    s->heads = G <= 8 ? 8 : 16;
-    s->h_blocks = (G + s->heads - 1) / s->heads;
+    s->nb = G <= 8 ? 1 : 2;
+    s->h_blocks = (G + 8 * s->nb - 1) / (8 * s->nb);
     s->units = B * H_kv * s->h_blocks;
-    const long long want = std::max(1ll, 4 * 2 * 148 / s->units);
-    s->n_split = (int)std::min<long long>(std::min<long long>(want, DK_MAXSPLIT), (max_pages + DK_WARPS - 1) / DK_WARPS);
-    return s->units * s->n_split <= 0x7fffffffll && B * H_q <= 0x7fffffffll;
+    s->n_blocks = (int)std::min<long long>(s->nb == 1 ? 2 * 148 : 148, s->units * max_pages);
+    return s->units <= 0x7fffffffll;
 }
+static size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 
 }  // namespace ag
 
@@ -432,8 +623,9 @@ using namespace ag;
 
 extern "C" size_t ag_attention_decode_kv4_workspace(int B, int H_q, int H_kv, int D, int max_pages) {
     DecodeKv4Shape s;
-    if (!decode_kv4_shape(B, H_q, H_kv, D, max_pages, &s) || s.n_split == 1) return 0;
-    return (size_t)s.units * s.n_split * s.heads * (sizeof(float2) + sizeof(float) * D);
+    if (!decode_kv4_shape(B, H_q, H_kv, D, max_pages, &s)) return 0;
+    const size_t slots = 2 * (size_t)s.n_blocks * DK_WARPS, heads = 8 * s.nb;
+    return slots * heads * D * sizeof(float) + align256(slots * heads * sizeof(float2)) + s.units * sizeof(int2);
 }
 
 extern "C" ag_status attention_decode_kv4(const void* Q, const ag_kv4_pool* pool, const ag_kv4_table* table, const int32_t* row, void* O, int B, int H_q,
@@ -445,53 +637,49 @@ extern "C" ag_status attention_decode_kv4(const void* Q, const ag_kv4_pool* pool
         (!row && B > table->n_rows))
         return AG_ERR_ARG;
     const size_t need = ag_attention_decode_kv4_workspace(B, H_q, pool->H_kv, pool->D, table->max_pages);
-    if (need > 0 && (!workspace || ((uintptr_t)workspace & 15u) || workspace_bytes < need)) return AG_ERR_ARG;
+    if (!workspace || ((uintptr_t)workspace & 15u) || workspace_bytes < need) return AG_ERR_ARG;
     ag_status st = check_arch();
     if (st != AG_OK) return st;
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
+    const size_t slots = 2 * (size_t)s.n_blocks * DK_WARPS;
     DecodeKv4Args x;
     memset(&x, 0, sizeof x);
     x.Q = (const uint16_t*)Q;
     x.O = (uint16_t*)O;
     x.pages = (const uint8_t*)pool->pages;
     x.page_of = table->page_of; x.len = table->len; x.row = row;
-    x.n_pages = (int)pool->n_pages; x.H_kv = pool->H_kv; x.G = H_q / pool->H_kv;
-    x.n_rows = table->n_rows; x.max_pages = table->max_pages;
-    x.n_split = s.n_split; x.h_blocks = s.h_blocks;
+    x.part = (float4*)workspace;
+    x.stats = (float2*)((uint8_t*)workspace + slots * 8 * s.nb * pool->D * sizeof(float));
+    x.pieces = (int2*)((uint8_t*)x.stats + align256(slots * 8 * s.nb * sizeof(float2)));
+    x.B = B; x.n_pages = (int)pool->n_pages; x.H_kv = pool->H_kv; x.G = H_q / pool->H_kv;
+    x.n_rows = table->n_rows; x.max_pages = table->max_pages; x.h_blocks = s.h_blocks;
+    x.n_warps = s.n_blocks * DK_WARPS;
     x.scale_log2e = 1.4426950408889634f / sqrtf((float)pool->D);
-    if (need > 0) {
-        x.stats = (float2*)workspace;
-        x.part = (float*)((uint8_t*)workspace + (size_t)s.units * s.n_split * s.heads * sizeof(float2));
-    }
-    const bool wide = s.heads == 16;
-    void (*kernel)(DecodeKv4Args) = pool->D == 128 ? (wide ? k_attn_decode_kv4<128, 2> : k_attn_decode_kv4<128, 1>)
-                                                   : (wide ? k_attn_decode_kv4<64, 2> : k_attn_decode_kv4<64, 1>);
-    const int smem = pool->D == 128 ? (wide ? dk_smem_bytes<128, 2>() : dk_smem_bytes<128, 1>()) : (wide ? dk_smem_bytes<64, 2>() : dk_smem_bytes<64, 1>());
+    void (*kernel)(DecodeKv4Args) = pool->D == 128 ? (s.nb == 2 ? k_attn_decode_kv4<128, 2> : k_attn_decode_kv4<128, 1>)
+                                                   : (s.nb == 2 ? k_attn_decode_kv4<64, 2> : k_attn_decode_kv4<64, 1>);
+    void (*join)(DecodeKv4Args) = pool->D == 128 ? (s.nb == 2 ? k_attn_join_kv4<128, 2> : k_attn_join_kv4<128, 1>)
+                                                 : (s.nb == 2 ? k_attn_join_kv4<64, 2> : k_attn_join_kv4<64, 1>);
     static std::atomic<unsigned long long> attr_done{0};
     const cudaError_t attr_err = once_per_device(attr_done, [] {
-        cudaError_t e = cudaFuncSetAttribute(k_attn_decode_kv4<128, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, dk_smem_bytes<128, 1>());
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(k_attn_decode_kv4<128, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, dk_smem_bytes<128, 2>());
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(k_attn_decode_kv4<64, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, dk_smem_bytes<64, 1>());
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(k_attn_decode_kv4<64, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, dk_smem_bytes<64, 2>());
-        return e;
+        cudaError_t e = cudaFuncSetAttribute(k_attn_decode_kv4<128, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, dk_smem_bytes<128>());
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(k_attn_decode_kv4<128, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, dk_smem_bytes<128>());
+        return e;                                  // D = 64 needs 40 KB, which every kernel may have
     });
     if (attr_err != cudaSuccess) return cuda_fail(attr_err);
-    kernel<<<(unsigned)(s.units * s.n_split), DK_WARPS * 32, smem, stream>>>(x);
+    kernel<<<(unsigned)s.n_blocks, DK_THREADS, pool->D == 128 ? dk_smem_bytes<128>() : dk_smem_bytes<64>(), stream>>>(x);
     AG_CUDA(cudaGetLastError());
     count_launch();
-    if (s.n_split > 1) {
-        cudaLaunchConfig_t cfg;
-        memset(&cfg, 0, sizeof cfg);
-        cfg.gridDim = dim3((unsigned)((long long)B * H_q));
-        cfg.blockDim = dim3(pool->D);
-        cfg.stream = stream;
-        cudaLaunchAttribute attr[1];
-        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[0].val.programmaticStreamSerializationAllowed = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = 1;
-        AG_CUDA(cudaLaunchKernelEx(&cfg, pool->D == 128 ? k_attn_join_kv4<128> : k_attn_join_kv4<64>, x, s.heads));
-        count_launch();
-    }
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof cfg);
+    cfg.gridDim = dim3((unsigned)s.units);
+    cfg.blockDim = dim3(s.nb * pool->D * 2, dk_join_lanes(pool->D, s.nb));
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    AG_CUDA(cudaLaunchKernelEx(&cfg, join, x));
+    count_launch();
     return AG_OK;
 }

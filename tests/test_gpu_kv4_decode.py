@@ -1,8 +1,9 @@
 """Single-token attention over the 4-bit cache against its 64-bit oracle.
 
-Tolerance: an output is sum_j p_j v_j / sum_j p_j.  v_j and p_j are each rounded to bf16 once, by at most half a step: 2^-8 relative.  Scores are
-32-bit sums over D products with the base taken out again, off by less than 2^-22 * (sum |q u| s + 128 s |sum q|) < 1e-3 for the inputs here, which
-moves p by less than 2^-9 relative.  Together 5 * 2^-9 * sum p |v| / sum p (from the oracle, with |v|); the output's own rounding adds 2^-8 |want|."""
+Tolerance: an output is sum_j p_j v_j / sum_j p_j.  v_j is rounded to bf16 once, by at most half a step: 2^-8 relative; p_j is kept to 16 bits.
+Scores are 32-bit sums that carry up to 1024 q s on the way: |error| <= 2^-23 * 1024 * sum |q| s / sqrt D =: e, and for the inputs here (sum |q| s < 200 at
+D = 128, half at 64) e < 1.2 * 2^-9; an output moves by at most 2 e sum p |v| / sum p.  Together less than 5 * 2^-9 of sum p |v| / sum p (from the
+oracle, with |v|); the output's own rounding adds 2^-8 |want|."""
 import numpy as np
 import pytest
 import torch

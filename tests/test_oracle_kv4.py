@@ -152,12 +152,11 @@ def test_refusals_of_the_decode_attention():
     for change in (dict(Q=None), dict(O=None), dict(Q=P + 8), dict(O=P + 4), dict(B=-1), dict(B=5), dict(H_q=7), dict(H_q=1), dict(H_q=0), dict(row=P + 2),
                    dict(pool=None), dict(table=None), dict(H_q=2 * 1025)):
         assert L.attention_decode_kv4(*{**good, **change}.values()) == ag.AG_ERR_ARG, change
-    _, long_table = pool_and_table(max_pages=1000)
-    need = ag.attention_decode_kv4_workspace(2, 8, 2, 128, 1000)
+    need = ag.attention_decode_kv4_workspace(2, 8, 2, 128, 8)
     assert need > 0
     for change in (dict(ws=None), dict(wsb=need - 1), dict(ws=P + 8)):
-        assert L.attention_decode_kv4(*{**good, "table": r(long_table), **change}.values()) == ag.AG_ERR_ARG, change
+        assert L.attention_decode_kv4(*{**good, **change}.values()) == ag.AG_ERR_ARG, change
     assert L.attention_decode_kv4(*{**good, "B": 0}.values()) == ag.AG_OK
-    # short rows and many requests need none; shapes that are refused have size 0
-    assert ag.attention_decode_kv4_workspace(2, 8, 2, 128, 8) == 0 and ag.attention_decode_kv4_workspace(1000, 32, 8, 128, 1000) == 0
+    # two parts of 8 heads a warp, 2 * 148 * 8 warps at most; shapes that are refused have size 0
+    assert ag.attention_decode_kv4_workspace(1000, 32, 8, 128, 1000) == 2 * 2 * 148 * 8 * 8 * (128 * 4 + 8) + 1000 * 8 * 8
     assert ag.attention_decode_kv4_workspace(2, 7, 2, 128, 1000) == 0 and ag.attention_decode_kv4_workspace(2, 8, 2, 96, 1000) == 0
