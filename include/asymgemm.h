@@ -20,8 +20,8 @@
  *   - A handle (plan, affinity map, packed weights, group descriptor) may be used by one host
  *     thread at a time; launches of one plan must not overlap on the device (use one plan per
  *     stream).  Different plans may run concurrently on disjoint SM sets (avoid_sm_mask).
- *   - gemm_persistent, gemm_persistent_packed, gemm_persistent_grouped, gemm_persistent_noalloc and
- *     attention_decode_persistent return AG_ERR_ARG, and queue nothing, when cuda_stream is being captured: every launch carries
+ *   - gemm_persistent, gemm_persistent_packed, gemm_persistent_grouped, gemm_persistent_noalloc,
+ *     attention_decode_persistent and attention_prompt_persistent return AG_ERR_ARG, and queue nothing, when cuda_stream is being captured: every launch carries
  *     a launch number (epoch) in its kernel parameters, by which the thread blocks take their places
  *     in the plan; a replayed graph would repeat an old number and no block would join.
  *   - Environment: AG_DEBUG=1 makes topo_discover print its bandwidth measurements and any
@@ -588,6 +588,33 @@ void ag_kv_destroy(ag_kv_cache* kv);
  */
 ag_status attention_decode_persistent(const void* Q, const ag_kv_cache* kv, const int32_t* kv_len, void* O, int B,
                                       int H_q, const ag_plan* plan, void* cuda_stream);
+
+/* ---- attention over whole prompts --------------------------------------------------------------------------------------
+ * The other side of serving: every token of a prompt attends to the keys in front of it.  Sequences of different lengths lie packed
+ * one behind the other; a sequence may have more keys than queries (a later chunk of a prompt, with its past).  Runs on the SMs of a
+ * plan, so that prompts and decoding can share a chip (Section 7.1.2); of the plan only the SM set counts - its units and shape are not
+ * looked at, work comes from a queue of the call's own units, sequences with many keys first.
+ */
+typedef struct {
+    const void *Q, *K, *V;  /* device, bf16: token i's rows at Q + i * q_stride, [H_q][D] (K, V: [H_kv][D]); 16-byte aligned */
+    void* O;                /* device, bf16, as Q; rows of tokens that belong to no sequence are left as they were */
+    int64_t q_stride, k_stride, v_stride, o_stride;  /* elements between tokens, multiples of 8, at least the row (parts of one fused
+                                                        projection are fine) */
+    int32_t H_q, H_kv, D;   /* D = 64 or 128; H_q / H_kv = 1 .. 64, every KV head serves H_q / H_kv consecutive query heads */
+    int32_t n_seq;
+    const int32_t* q_off;   /* device [n_seq + 1], ascending: sequence i owns tokens q_off[i] .. q_off[i + 1] - 1 of Q and O */
+    const int32_t* kv_off;  /* the same for K and V; NULL = q_off */
+    int64_t q_tokens, kv_tokens;  /* tokens that Q and O, K and V have (below 2^30); offsets beyond are clamped */
+    int32_t causal;         /* 1: token i of a sequence with n queries and m keys sees keys 0 .. m - n + i; 0: all of them */
+    float scale;            /* 0 = 1 / sqrt(D) */
+} ag_prompt_attention;
+/*
+ * attention_prompt_persistent - O = softmax(scale Q K^T) V, per sequence and head.  A token that sees no key (no keys at all, or more
+ * queries than keys) gets zeros.  What a token does not see (other sequences, later keys) has no influence, whatever it holds.  Scores, softmax statistics and outputs
+ * are accumulated in 32 bits, probabilities are rounded to bf16.
+ * One launch per 1024 sequences.  Asynchronous on cuda_stream.  Errors as gemm_persistent; device-side status via ag_last_status.
+ */
+ag_status attention_prompt_persistent(const ag_prompt_attention* a, const ag_plan* plan, void* cuda_stream);
 
 /* ---- 4-bit key/value cache in pages ----------------------------------------------------------------------------------
  * A cache that requests grow in, share and leave again: pages of AG_KV4_PAGE tokens (all KV heads of one layer) in a buffer of

@@ -73,3 +73,28 @@ def gqa_decode_loops(Q, K, V, kv_len=None) -> np.ndarray:
             for t in range(D):
                 O[b, hq, t] = sum(e[j] * float(V[b, h, j, t]) for j in range(n)) / z
     return O
+
+
+def prompt(Q, K, V, q_off, kv_off=None, causal=True, scale=None):
+    """Attention over packed sequences.  Q [Tq, Hq, D], K and V [Tk, Hkv, D] as bf16 bits; sequence i owns tokens
+    q_off[i] .. q_off[i + 1] - 1 and keys kv_off[i] .. kv_off[i + 1] - 1 (default: the same).  Causal: query i of n sees keys 0 .. m - n + i
+    of m.  Returns (O, mass) in float64, mass = sum_j p_j |v_j|; a row that sees no key, or belongs to no sequence, gives zeros."""
+    Q, K, V = bf16_to_f64(Q), bf16_to_f64(K), bf16_to_f64(V)
+    kv_off = q_off if kv_off is None else kv_off
+    group = Q.shape[1] // K.shape[1]
+    scale = 1.0 / math.sqrt(Q.shape[2]) if scale is None else scale
+    O, mass = np.zeros(Q.shape), np.zeros(Q.shape)
+    for a, b, c, d in zip(q_off[:-1], q_off[1:], kv_off[:-1], kv_off[1:]):
+        n, m = b - a, d - c
+        if n <= 0 or m <= 0:
+            continue
+        sees = np.arange(m)[None] <= (m - n + np.arange(n))[:, None] if causal else np.ones((n, m), dtype=bool)
+        some = sees.any(axis=1)
+        for hq in range(Q.shape[1]):
+            h = hq // group
+            s = np.where(sees, (Q[a:b, hq] @ K[c:d, h].T) * scale, -np.inf)[some]
+            p = np.exp(s - s.max(axis=1, keepdims=True))
+            p /= p.sum(axis=1, keepdims=True)
+            O[a:b, hq][some] = p @ V[c:d, h]
+            mass[a:b, hq][some] = p @ np.abs(V[c:d, h])
+    return O, mass

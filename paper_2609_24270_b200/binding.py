@@ -32,7 +32,7 @@ EXPORTED = [
     "gemm_persistent_grouped", "ag_strerror", "ag_last_cuda_error",
     "ag_kernel_launch_count", "ag_kv_pack", "ag_kv_info", "ag_kv_append", "ag_kv_destroy", "attention_decode_persistent",
     "ag_kv4_page_bytes", "ag_kv4_store", "ag_kv4_load", "ag_kv4_extend", "ag_kv4_fork", "ag_kv4_free", "ag_kv4_compact",
-    "attention_decode_kv4", "ag_attention_decode_kv4_workspace",
+    "attention_decode_kv4", "ag_attention_decode_kv4_workspace", "attention_prompt_persistent",
 ]
 
 
@@ -102,6 +102,14 @@ class KV4Pool(C.Structure):
 class KV4Table(C.Structure):
     """Page tables on the device: KV4Table(page_of [n_rows][max_pages], len [n_rows], refs [n_pages], n_rows, max_pages)."""
     _fields_ = [("page_of", C.c_void_p), ("len", C.c_void_p), ("refs", C.c_void_p), ("n_rows", C.c_int32), ("max_pages", C.c_int32)]
+
+
+class PromptAttention(C.Structure):
+    _fields_ = [("Q", C.c_void_p), ("K", C.c_void_p), ("V", C.c_void_p), ("O", C.c_void_p),
+                ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64), ("o_stride", C.c_int64),
+                ("H_q", C.c_int32), ("H_kv", C.c_int32), ("D", C.c_int32), ("n_seq", C.c_int32),
+                ("q_off", C.c_void_p), ("kv_off", C.c_void_p), ("q_tokens", C.c_int64), ("kv_tokens", C.c_int64),
+                ("causal", C.c_int32), ("scale", C.c_float)]
 
 
 class AgError(RuntimeError):
@@ -181,6 +189,7 @@ def lib() -> C.CDLL:
     L.ag_kv4_fork.argtypes = [pool, table, vp, vp, C.c_int, vp, vp]
     L.ag_kv4_free.argtypes = [pool, table, vp, C.c_int, vp]
     L.ag_kv4_compact.argtypes = [pool, table, vp, vp]
+    L.attention_prompt_persistent.argtypes = [C.POINTER(PromptAttention), vp, vp]
     L.attention_decode_kv4.argtypes = [vp, pool, table, vp, vp, C.c_int, C.c_int, vp, sz, vp]
     L.ag_attention_decode_kv4_workspace.argtypes = [C.c_int] * 5
     L.ag_attention_decode_kv4_workspace.restype = sz
@@ -590,6 +599,16 @@ def kv_pack(k_ptr: int, v_ptr: int, B: int, H_kv: int, L: int, plan: Plan, amap:
 def attention_decode(q_ptr: int, kv: KVCache, kv_len_ptr, o_ptr: int, B: int, H_q: int, plan: Plan, stream: int = 0):
     _check(lib().attention_decode_persistent(q_ptr, kv.handle, kv_len_ptr, o_ptr, B, H_q, plan.handle, stream),
            "attention_decode_persistent")
+
+
+def attention_prompt(q_ptr: int, k_ptr: int, v_ptr: int, o_ptr: int, H_q: int, H_kv: int, D: int, q_off_ptr: int, kv_off_ptr, n_seq: int,
+                     q_tokens: int, kv_tokens: int, plan: Plan, causal: bool = True, scale: float = 0.0, q_stride: int | None = None,
+                     k_stride: int | None = None, v_stride: int | None = None, o_stride: int | None = None, stream: int = 0):
+    """Attention over packed sequences (bf16, [tokens][heads][D], strides in elements between tokens) on the SMs of the plan."""
+    a = PromptAttention(q_ptr, k_ptr, v_ptr, o_ptr, H_q * D if q_stride is None else q_stride, H_kv * D if k_stride is None else k_stride,
+                        H_kv * D if v_stride is None else v_stride, H_q * D if o_stride is None else o_stride, H_q, H_kv, D, n_seq,
+                        q_off_ptr, kv_off_ptr, q_tokens, kv_tokens, 1 if causal else 0, scale)
+    _check(lib().attention_prompt_persistent(C.byref(a), plan.handle, stream), "attention_prompt_persistent")
 
 
 # ---- 4-bit key/value cache in pages -----------------------------------------------------------------
