@@ -3,12 +3,13 @@
 // Per request, KV head and page of 64 keys, with the code u and the pair (s, b) of every element (value s u + b), G query heads:
 //     S[key][q]  = sum over groups of 32 d:  s (sum_d u q_d) + b (sum_d q_d)      m16n8k16 MMA (fp16): 16 keys x 8 heads x 16 d
 //     P = 2^((S - max) log2 e / sqrt D)                                           running maximum and sum per warp
-//     O[d][q]   += sum_key V[key][d] P[key][q]                                    m16n8k16 MMA (bf16): 16 d x 8 heads x 16 keys
+//     O[d][q]   += sum_key V[key][d] P[key][q]                                    m16n8k16 MMA (fp16): 16 d x 8 heads x 16 keys
 // A code of K becomes an fp16 operand with one logic instruction, 0x6400 | u = 1024 + u or 0x5400 | u << 4 = 64 + u; what that adds to the
 // scores leaves again, together with the bases' part, through two MMAs of the pairs against sums over q kept in three bf16 parts (24
-// bits), so scores carry no rounding besides the 32-bit sums.  V varies its scale along the contraction: its codes become 128 + u
-// (bf16 0x4300 | u) and then s u + b, rounded to bf16 once; P enters as two bf16 parts, 16 bits.  (An fp8 MMA would take the codes as they
-// are, but mma.sync on this chip converts fp8 operands to fp16 first: measured, slower than the above.)
+// bits), so scores carry no rounding besides the 32-bit sums.  V varies its scale along the contraction: its codes become 16 + u
+// (0x4C00 | u << 6) and then s u + b with one multiply-add, in fp16 under a power of two that follows the largest value, rounded at 2^-12;
+// P, times 2^10, is fp16 as well.  (An fp8 MMA would take the codes as they are, but mma.sync on this chip converts fp8 operands to fp16
+// first: measured, slower than the above.)
 //
 // Bound by memory: 1.25 D bytes per key and head.  A byte costs about ten times the arithmetic instructions of a bf16 cache's, so
 // the operands are unpacked in registers, straight into the MMA's fragments - tcgen05.mma would want them in shared memory, one more
@@ -18,8 +19,9 @@
 // Work: all pages of all (request, KV head) units in one line, cut into equal runs, one per warp, every warp of the launch resident at
 // once (two blocks of eight warps per SM).  A warp walks its run alone - one buffer each for K and V, refilled by 16-byte asynchronous
 // copies as soon as it has been read: K of the next page comes in during the softmax and V's products, V during the next page's scores, while
-// the SM's other warps are in other phases.  Uneven lengths, few long requests and many short ones are the same case.  A unit that one warp has
-// to itself is written at once; otherwise the warps leave their parts in the workspace, in fragment order, for a second kernel to join.
+// the SM's other warps are in other phases.  Uneven lengths, few long requests and many short ones are the same case.  Warps of a block that
+// share a unit put their parts together at the end (fragment order, through the workspace); a unit that goes beyond a block is left in one
+// part per block for a second kernel.
 #include <string.h>
 
 #include <algorithm>
@@ -30,7 +32,7 @@ namespace ag {
 
 constexpr int DK_WARPS = 8;
 constexpr int DK_THREADS = DK_WARPS * 32;
-// parts of a unit that the joining block adds up side by side
+// parts of a unit that the joining block can add up side by side (block of 2 D NB threads by so many, at most 1024)
 __host__ __device__ constexpr int dk_join_lanes(int D, int NB) { return NB * D * 2 * 4 > 1024 ? 2 : 4; }
 
 struct DecodeKv4Args {
@@ -38,10 +40,11 @@ struct DecodeKv4Args {
     uint16_t* O;                  // [B][H_q][D]
     const uint8_t* pages;
     const int32_t *page_of, *len, *row;
-    float4* part;                 // [2 per warp][NB][D / 16][32 lanes]: unnormalised outputs in fragment order
-    float2* stats;                // [2 per warp][8 NB]: maximum (in units of log2), sum
-    int2* pieces;                 // [units]: first warp of the unit, number of warps
-    int B, n_pages, H_kv, G, n_rows, max_pages, h_blocks, n_warps;
+    float4* part;                 // [slots][NB][D / 16][32 lanes]: unnormalised outputs in fragment order; slots: 2 per warp, 2 per block
+    float2* stats;                // [slots][8 NB]: maximum (in units of log2), sum
+    int2* pieces;                 // [units]: first block of the unit, number of blocks
+    int B, n_pages, H_kv, G, n_rows, max_pages, h_blocks, n_blocks;
+    int aligned;                  // 1: block = unit (short rows, few units)
     float scale_log2e;
 };
 __device__ __forceinline__ float ex2_ftz(float v) {      // 2^v, relative error 2^-22; 2^-inf = 0
@@ -89,12 +92,10 @@ __device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t mask, uint32_t b
     asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(a), "r"(mask), "r"(bits));
     return r;
 }
-// bf16 128 + u in both halves -> s u + b in bf16, rounded once
-__device__ __forceinline__ uint32_t dequant2(uint32_t c128, uint32_t s, uint32_t b) {
-    uint32_t u, v;
-    asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(u) : "r"(c128), "r"(0xC300C300u));
-    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(v) : "r"(u), "r"(s), "r"(b));
-    return v;
+__device__ __forceinline__ uint32_t fma_f16x2(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t r;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    return r;
 }
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(reinterpret_cast<uint64_t>(src)) : "memory");
@@ -112,6 +113,17 @@ __device__ __forceinline__ int pages_of(int tokens) { return (tokens + KV4_PAGE 
 // the warp whose run holds place `at` of the line: run w begins at total * w / n
 __device__ __forceinline__ int run_holding(long long at, long long total, int n) { return (int)(((at + 1) * n - 1) / total); }
 
+// f a + g b, where a factor of zero means "not there", whatever stands beside it
+__device__ __forceinline__ float weighted(float f, float a, float g, float b) { return (f == 0.f ? 0.f : f * a) + (g == 0.f ? 0.f : g * b); }
+// A part (maximum pm, sum pl) joins what there is (m, l): factors f of the outputs so far and g of the part's.  pl = 0: a part without keys, g = 0.
+__device__ __forceinline__ void join_weights(float& m, float& l, float pm, float pl, float& f, float& g) {
+    const float top = fmaxf(m, pm);
+    f = l == 0.f ? 0.f : m == top ? 1.f : ex2_ftz(m - top);
+    g = pl == 0.f ? 0.f : pm == top ? 1.f : ex2_ftz(pm - top);
+    l = weighted(f, l, g, pl);
+    m = pl == 0.f ? m : top;
+}
+
 template <int D>
 constexpr int dk_smem_bytes() { return DK_WARPS * kv4_head_bytes(D); }
 
@@ -122,15 +134,33 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ long long before[DK_THREADS + 1];   // pages (of one KV head) in front of the share of requests that thread i counts
     __shared__ long long warp_sum[DK_WARPS];
+    __shared__ int slot_unit[2 * DK_WARPS];        // units that a warp has only a part of: one that began before its run, one that goes on behind it
+    __shared__ int slot_ends[2 * DK_WARPS];        // the part includes the unit's last page
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     dep_release();
 
-    // ---- this warp's run: places run, run + 1, ... of the line of pages; order: request, KV head (and block of query heads), page
+    // ---- this block's run, cut into the warps' runs: places of the line of pages; order: request, KV head (and block of query heads), page
     const int heads = x.H_kv * x.h_blocks;
     const int per = (x.B + DK_THREADS - 1) / DK_THREADS;
-    {
+    long long total = 0, block_begin, block_end, first_unit_begin = 0;
+    int n_blocks = x.n_blocks, b, hh = 0, p = 0, np, len, row;     // request b, KV head and block hh, page p of np
+    if (x.aligned) {
+        b = blockIdx.x / heads;
+        hh = blockIdx.x - b * heads;
+        len = row_tokens(x, b, &row);
+        np = pages_of(len);
+        block_begin = 0;
+        block_end = np;
+        if (np == 0) {
+            for (int i = threadIdx.x; i < 8 * NB * D; i += DK_THREADS) {
+                const int head = hh % x.h_blocks * 8 * NB + i / D;
+                if (head < x.G) x.O[((size_t)(b * x.H_kv + hh / x.h_blocks) * x.G + head) * D + i % D] = 0;
+            }
+            return;
+        }
+    } else {
         long long n = 0;
-        for (int b = threadIdx.x * per, e = min(x.B, b + per), r; b < e; ++b) n += pages_of(row_tokens(x, b, &r));
+        for (int i = threadIdx.x * per, e = min(x.B, i + per), r; i < e; ++i) n += pages_of(row_tokens(x, i, &r));
         long long inc = n;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -145,13 +175,18 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
         before[threadIdx.x] = add + inc - n;
         if (threadIdx.x == DK_THREADS - 1) before[DK_THREADS] = add + inc;
         __syncthreads();
+        total = before[DK_THREADS] * heads;
+        n_blocks = (int)min((long long)x.n_blocks, (total + DK_WARPS - 1) / DK_WARPS);      // at least a page for every warp
+        if ((int)blockIdx.x >= n_blocks) return;
+        block_begin = total * blockIdx.x / n_blocks;
+        block_end = total * (blockIdx.x + 1) / n_blocks;
+        b = 0;
+        len = np = row = 0;
     }
-    const long long total = before[DK_THREADS] * heads;
-    const int n_runs = (int)min((long long)x.n_warps, total);
-    const int me = blockIdx.x + gridDim.x * warp;  // neighbouring runs on different SMs: few pages spread over the chip
-    if (me >= n_runs) return;
-    const long long begin = total * me / n_runs;
-    int left = (int)(total * (me + 1) / n_runs - begin);
+    if (threadIdx.x < 2 * DK_WARPS) slot_unit[threadIdx.x] = -1;
+    __syncthreads();
+    const long long begin = block_begin + (block_end - block_begin) * warp / DK_WARPS;
+    int left = (int)(block_begin + (block_end - block_begin) * (warp + 1) / DK_WARPS - begin);
 
     uint8_t* kbuf = smem + warp * kv4_head_bytes(D);          // codes of K, then K's pairs
     uint8_t* vbuf = kbuf + 40 * D;
@@ -176,9 +211,10 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
         cp_async_commit();
     };
 
-    // ---- the page to be fetched next: request b, head hh (KV head, block), page p of np
-    int b, hh, p, np, len, row;
-    {
+    // ---- the first page of the run
+    if (x.aligned) {
+        p = (int)begin;
+    } else if (left > 0) {
         const long long at = begin / heads;
         int lo = 0, hi = DK_THREADS - 1;           // the last share that begins at or in front of it
         while (lo < hi) {
@@ -197,8 +233,10 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
         const long long rest = begin - in_front * heads;
         hh = (int)(rest / np);
         p = (int)(rest - (long long)hh * np);
+        first_unit_begin = begin - p;
     }
-    long long unit_begin = begin - p;              // place of the unit's first page
+    long long unit_begin = first_unit_begin;       // place of the unit's first page
+    const int p_first = p;
     int id_batch = 0, id_first = -64;              // ids of pages id_first + lane of the row (reloaded as p leaves them)
     const uint8_t* src_next = nullptr;
     int nv_next = 0;
@@ -211,16 +249,45 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
         nv_next = id >= 0 && id < x.n_pages ? min(KV4_PAGE, len - p * KV4_PAGE) : 0;
         src_next = x.pages + ((size_t)(nv_next ? id : 0) * x.H_kv + hh / x.h_blocks) * kv4_head_bytes(D);
     };
-    locate();
-    fetch(0, src_next, nv_next);
-    fetch(1, src_next, nv_next);
+    if (left > 0) {
+        locate();
+        fetch(0, src_next, nv_next);
+        fetch(1, src_next, nv_next);
+    }
 
     uint32_t qf[NB][NG][4];
     uint32_t qb[NB][2], qs[NB][2];
     float unscale[NB][2];                          // log2 e / (c sqrt D) of heads 2 t and 2 t + 1
     float o[NB][MT][4];
     float m[NB][2], l[NB][2];
+    int v_exp = 0;                                 // outputs are kept times 2^(13 - v_exp)
     bool fresh = true;                             // the page in hand is the first of a unit for this warp
+    bool whole = p_first == 0;                     // this warp has had the unit from its first page
+    // the outputs in hand, normalised.  Lanes (g, t) have heads 2 t, 2 t + 1 of d = 16 i + g, + 8; transposed, head g of d = 16 i + 2 t, + 1, ...
+    auto write_unit = [&](int unit) {
+        const int bu = unit / heads, hu = unit - bu * heads, head0 = hu % x.h_blocks * 8 * NB;
+        uint16_t* out = x.O + ((size_t)(bu * x.H_kv + hu / x.h_blocks) * x.G + head0) * D;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            const float r0 = l[nb][0] == 0.f ? 0.f : 1.f / l[nb][0], r1 = l[nb][1] == 0.f ? 0.f : 1.f / l[nb][1];
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const uint32_t v = movm_trans(pack_bf16(o[nb][i][2 * e] * r0, o[nb][i][2 * e + 1] * r1));
+                    if (head0 + nb * 8 + g < x.G) *reinterpret_cast<uint32_t*>(out + (nb * 8 + g) * D + i * 16 + e * 8 + 2 * t) = v;
+                }
+        }
+    };
+    auto write_part = [&](size_t slot) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            if (g == 0) *reinterpret_cast<float4*>(&x.stats[slot * 8 * NB + nb * 8 + 2 * t]) = make_float4(m[nb][0], l[nb][0], m[nb][1], l[nb][1]);
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+                x.part[((slot * NB + nb) * MT + i) * 32 + lane] = make_float4(o[nb][i][0], o[nb][i][1], o[nb][i][2], o[nb][i][3]);
+        }
+    };
     while (left > 0) {
         const int b_now = b, hh_now = hh, p_now = p, np_now = np, nv = nv_next;
         const int head0 = hh_now % x.h_blocks * 8 * NB;       // first query head of the block, of the KV head's G
@@ -307,6 +374,7 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
                 m[nb][0] = m[nb][1] = -INFINITY;
                 l[nb][0] = l[nb][1] = 0.f;
             }
+            v_exp = -100;
         }
         cp_async_wait<1>();                        // K of this page has landed
         __syncwarp();
@@ -421,7 +489,7 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
                 }
                 float ref[2];
 #pragma unroll
-                for (int e = 0; e < 2; ++e) ref[e] = m[nb][e] == -INFINITY ? 0.f : m[nb][e] * unscale[nb][e];
+                for (int e = 0; e < 2; ++e) ref[e] = m[nb][e] == -INFINITY ? 0.f : fmaf(m[nb][e], unscale[nb][e], -10.f);      // P is kept times 2^10: fp16 then holds it down to 2^-34
 #pragma unroll
                 for (int run = 0; run < 4; ++run)
 #pragma unroll
@@ -433,62 +501,94 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
         }
         cp_async_wait<1>();                        // V of this page has landed
         __syncwarp();
-        if (nv < KV4_PAGE) {                       // what lies behind the last key may be anything: it must not meet a probability of zero as NaN
-            for (int i = nv * NG + lane; i < (nv + 15) / 16 * 16 * NG; i += 32) *reinterpret_cast<uint32_t*>(vbuf + 32 * D + i * 4) = 0u;
+        if (nv > 0) {
+            // The pairs of two keys side by side (s, s') and (c, c'), c = b - 16 s, in fp16 times 2^(13 - v_exp): |b| + 31 s, the largest a value
+            // can be, stays below 2^15.  Lane = pair of keys; in place.  What lies behind the last key may be anything and becomes zero.
+            uint32_t* at = reinterpret_cast<uint32_t*>(vbuf + 32 * D) + lane * 2 * NG;
+            uint32_t w[2][NG];
+            float top = 0.f;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                if (D == 128) *reinterpret_cast<uint4*>(&w[e][0]) = *reinterpret_cast<const uint4*>(at + e * NG);
+                else *reinterpret_cast<uint2*>(&w[e][0]) = *reinterpret_cast<const uint2*>(at + e * NG);
+#pragma unroll
+                for (int grp = 0; grp < NG; ++grp) {
+                    if (2 * lane + e >= nv) w[e][grp] = 0u;
+                    top = fmaxf(top, fmaf(31.f, fabsf(bf16_lo(w[e][grp])), fabsf(bf16_hi(w[e][grp]))));
+                }
+            }
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+            const int e_top = max(-100, (int)(__float_as_uint(top) >> 23) - 127);
+            if (e_top > v_exp + 1) {               // larger values than before: the outputs so far move to the new exponent (the same for all lanes)
+                const float f = v_exp < e_top - 126 ? 0.f : __uint_as_float((uint32_t)(127 + v_exp - e_top) << 23);
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int i = 0; i < MT; ++i)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) o[nb][i][c] *= f;
+                v_exp = e_top;
+            }
+            const float k = __uint_as_float((uint32_t)(127 + 13 - v_exp) << 23);
+            uint32_t sc[2][NG];
+#pragma unroll
+            for (int grp = 0; grp < NG; ++grp) {
+                const float s0 = bf16_lo(w[0][grp]) * k, s1 = bf16_lo(w[1][grp]) * k;
+                sc[0][grp] = pack_f16(s0, s1);
+                sc[1][grp] = pack_f16(fmaf(bf16_hi(w[0][grp]), k, -16.f * s0), fmaf(bf16_hi(w[1][grp]), k, -16.f * s1));
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                if (D == 128) *reinterpret_cast<uint4*>(at + e * NG) = *reinterpret_cast<const uint4*>(&sc[e][0]);
+                else *reinterpret_cast<uint2*>(at + e * NG) = *reinterpret_cast<const uint2*>(&sc[e][0]);
+            }
             __syncwarp();
         }
 #pragma unroll
         for (int run = 0; run < 4; ++run) {
             if (run * 16 < nv) {
-                uint32_t pf[NB][4];                // probabilities as B operands, high parts and low parts
+                uint32_t pf[NB][2];                // probabilities as B operands
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const uint32_t hi = pack_bf16(s[nb][run][2 * e], s[nb][run][2 * e + 1]);
-                        pf[nb][e] = movm_trans(hi);
-                        pf[nb][2 + e] = movm_trans(pack_bf16(s[nb][run][2 * e] - bf16_lo(hi), s[nb][run][2 * e + 1] - bf16_hi(hi)));
-                    }
-                uint32_t xs[2][2][NG / 2], vs[2][NG], vb[2][NG];       // codes by (h, j): two keys side by side; pairs of scales and of bases
+                    for (int e = 0; e < 2; ++e) pf[nb][e] = movm_trans(pack_f16(s[nb][run][2 * e], s[nb][run][2 * e + 1]));
+                uint32_t xs[2][2][NG / 2], vs[2][NG], vc[2][NG];       // codes by (h, j): two keys side by side; pairs of scales and of bases
 #pragma unroll
-                for (int hh = 0; hh < 2; ++hh) {
-                    const uint8_t* at = vbuf + run * 8 * D + hh * 4 * D + lane * (D / 8);
-                    const int key = run * 16 + hh * 8 + 2 * t;
-                    const uint8_t* ps = vbuf + 32 * D + key * (D / 8);
-                    uint32_t pa[2][NG];
+                for (int hh2 = 0; hh2 < 2; ++hh2) {
+                    const uint8_t* at = vbuf + run * 8 * D + hh2 * 4 * D + lane * (D / 8);
+                    const uint8_t* ps = vbuf + 32 * D + (run * 8 + hh2 * 4 + t) * (D / 4);
                     if (D == 128) {
                         const uint4 v = *reinterpret_cast<const uint4*>(at);
-                        xs[hh][0][0] = __byte_perm(v.x, v.z, 0x5410);
-                        xs[hh][0][NG / 2 - 1] = __byte_perm(v.x, v.z, 0x7632);
-                        xs[hh][1][0] = __byte_perm(v.y, v.w, 0x5410);
-                        xs[hh][1][NG / 2 - 1] = __byte_perm(v.y, v.w, 0x7632);
-                        *reinterpret_cast<uint4*>(&pa[0][0]) = *reinterpret_cast<const uint4*>(ps);
-                        *reinterpret_cast<uint4*>(&pa[1][0]) = *reinterpret_cast<const uint4*>(ps + 16);
+                        xs[hh2][0][0] = __byte_perm(v.x, v.z, 0x5410);
+                        xs[hh2][0][NG / 2 - 1] = __byte_perm(v.x, v.z, 0x7632);
+                        xs[hh2][1][0] = __byte_perm(v.y, v.w, 0x5410);
+                        xs[hh2][1][NG / 2 - 1] = __byte_perm(v.y, v.w, 0x7632);
+                        *reinterpret_cast<uint4*>(&vs[hh2][0]) = *reinterpret_cast<const uint4*>(ps);
+                        *reinterpret_cast<uint4*>(&vc[hh2][0]) = *reinterpret_cast<const uint4*>(ps + 16);
                     } else {
                         const uint2 v = *reinterpret_cast<const uint2*>(at);
-                        xs[hh][0][0] = __byte_perm(v.x, v.y, 0x5410);
-                        xs[hh][1][0] = __byte_perm(v.x, v.y, 0x7632);
-                        *reinterpret_cast<uint2*>(&pa[0][0]) = *reinterpret_cast<const uint2*>(ps);
-                        *reinterpret_cast<uint2*>(&pa[1][0]) = *reinterpret_cast<const uint2*>(ps + 8);
-                    }
-#pragma unroll
-                    for (int grp = 0; grp < NG; ++grp) {
-                        vs[hh][grp] = __byte_perm(pa[0][grp], pa[1][grp], 0x5410);
-                        vb[hh][grp] = __byte_perm(pa[0][grp], pa[1][grp], 0x7632);
+                        xs[hh2][0][0] = __byte_perm(v.x, v.y, 0x5410);
+                        xs[hh2][1][0] = __byte_perm(v.x, v.y, 0x7632);
+                        *reinterpret_cast<uint2*>(&vs[hh2][0]) = *reinterpret_cast<const uint2*>(ps);
+                        *reinterpret_cast<uint2*>(&vc[hh2][0]) = *reinterpret_cast<const uint2*>(ps + 8);
                     }
                 }
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
-                    const int grp = i >> 1, half = i >> 2, sh = 4 * (i & 3);
-                    const uint32_t a0 = dequant2(and_or(xs[0][0][half] >> sh, 0x000f000fu, 0x43004300u), vs[0][grp], vb[0][grp]);
-                    const uint32_t a1 = dequant2(and_or(xs[0][1][half] >> sh, 0x000f000fu, 0x43004300u), vs[0][grp], vb[0][grp]);
-                    const uint32_t a2 = dequant2(and_or(xs[1][0][half] >> sh, 0x000f000fu, 0x43004300u), vs[1][grp], vb[1][grp]);
-                    const uint32_t a3 = dequant2(and_or(xs[1][1][half] >> sh, 0x000f000fu, 0x43004300u), vs[1][grp], vb[1][grp]);
+                    // fp16 0x4C00 | u << 6 = 16 + u, and (16 + u) s + c = s u + b, rounded once
+                    const int grp = i >> 1, half = i >> 2, k = i & 3;
+                    uint32_t a[2][2];
 #pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) {
-                        mma_bf16(o[nb][i], a0, a1, a2, a3, pf[nb][0], pf[nb][1]);
-                        mma_bf16(o[nb][i], a0, a1, a2, a3, pf[nb][2], pf[nb][3]);
-                    }
+                    for (int hh2 = 0; hh2 < 2; ++hh2)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const uint32_t w = xs[hh2][j][half];
+                            const uint32_t c = and_or(k == 0 ? w << 6 : k == 1 ? w << 2 : k == 2 ? w >> 2 : w >> 6, 0x03c003c0u, 0x4c004c00u);
+                            a[hh2][j] = fma_f16x2(c, vs[hh2][grp], vc[hh2][grp]);
+                        }
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) mma_f16(o[nb][i], a[0][0], a[0][1], a[1][0], a[1][1], pf[nb][0], pf[nb][1]);
                 }
             }
         }
@@ -496,61 +596,93 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
         fetch(1, src_next, nv_next);
 
         // ---- the end of the unit, or of this warp's share of it
-        fresh = p_now + 1 == np_now;
-        if (fresh || left == 0) {
-            const int unit = b_now * heads + hh_now;
-            const int w0 = run_holding(unit_now, total, n_runs), w1 = run_holding(unit_now + np_now - 1, total, n_runs);
+        const bool ends = p_now + 1 == np_now;
+        if (ends || left == 0) {
+            const float unexp = __uint_as_float((uint32_t)(127 - 13 + v_exp) << 23);
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
+            for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
-                for (int e = 0; e < 2; ++e)
+                for (int e = 0; e < 2; ++e) {
 #pragma unroll
                     for (int w = 4; w < 32; w <<= 1) l[nb][e] += __shfl_xor_sync(0xffffffffu, l[nb][e], w);
-            if (w0 == me && lane == 0) x.pieces[unit] = make_int2(w0, w1 - w0 + 1);
-            if (w0 == w1) {
-                // all of it: lanes (g, t) have heads 2 t, 2 t + 1 of d = 16 i + g, + 8; transposed, head g of d = 16 i + 2 t, + 1, ...
-                uint16_t* out = x.O + ((size_t)(b_now * x.H_kv + hh_now / x.h_blocks) * x.G + head0) * D;
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb) {
-                    const float r0 = l[nb][0] == 0.f ? 0.f : 1.f / l[nb][0], r1 = l[nb][1] == 0.f ? 0.f : 1.f / l[nb][1];
-#pragma unroll
-                    for (int i = 0; i < MT; ++i)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const uint32_t v = movm_trans(pack_bf16(o[nb][i][2 * e] * r0, o[nb][i][2 * e + 1] * r1));
-                            if (head0 + nb * 8 + g < x.G) *reinterpret_cast<uint32_t*>(out + (nb * 8 + g) * D + i * 16 + e * 8 + 2 * t) = v;
-                        }
+                    m[nb][e] = m[nb][e] == -INFINITY ? -INFINITY : m[nb][e] * unscale[nb][e];      // in units of log2 from here on
                 }
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) o[nb][i][c] *= unexp;
+            }
+            const int unit = b_now * heads + hh_now;
+            if (whole && ends) {
+                write_unit(unit);
+                if (!x.aligned && lane == 0) x.pieces[unit] = make_int2(blockIdx.x, 1);
             } else {
-                const size_t slot = 2 * (size_t)me + (w0 == me ? 1 : 0);
+                const int slot = 2 * warp + (whole ? 1 : 0);
+                write_part(2 * DK_WARPS * (size_t)blockIdx.x + slot);
+                if (lane == 0) {
+                    slot_unit[slot] = unit;
+                    slot_ends[slot] = ends;
+                    if (whole && !x.aligned) {
+                        const int last = run_holding(unit_now + np_now - 1, total, n_blocks);
+                        x.pieces[unit] = make_int2(blockIdx.x, last - (int)blockIdx.x + 1);
+                    }
+                }
+            }
+            whole = true;                          // whatever comes next begins in this warp's run
+        }
+        fresh = ends;
+    }
+    cp_async_wait<0>();
+
+    // ---- parts of one unit that several warps of the block have: the warp with the first one adds them up
+    __syncthreads();
+#pragma unroll 1
+    for (int k = 0; k < 2; ++k) {
+        const int own = 2 * warp + k, unit = slot_unit[own];
+        if (unit < 0) continue;
+        bool first = true;
+        for (int c = 0; c < own; ++c) first &= slot_unit[c] != unit;
+        if (!first) continue;
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) {
+        for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        if (g == 0) x.stats[slot * 8 * NB + nb * 8 + 2 * t + e] = make_float2(m[nb][e] == -INFINITY ? -INFINITY : m[nb][e] * unscale[nb][e], l[nb][e]);
-                    if (head0 + nb * 8 + 2 * t < x.G)
+            for (int i = 0; i < MT; ++i)
 #pragma unroll
-                        for (int i = 0; i < MT; ++i)
-                            x.part[((slot * NB + nb) * MT + i) * 32 + lane] = make_float4(o[nb][i][0], o[nb][i][1], o[nb][i][2], o[nb][i][3]);
+                for (int c = 0; c < 4; ++c) o[nb][i][c] = 0.f;
+            m[nb][0] = m[nb][1] = -INFINITY;
+            l[nb][0] = l[nb][1] = 0.f;
+        }
+        bool ends = false;
+#pragma unroll 1
+        for (int c = own; c < 2 * DK_WARPS; ++c) {
+            if (slot_unit[c] != unit) continue;
+            ends |= slot_ends[c] != 0;
+            const size_t slot = 2 * DK_WARPS * (size_t)blockIdx.x + c;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                const float4 st = __ldcg(reinterpret_cast<const float4*>(&x.stats[slot * 8 * NB + nb * 8 + 2 * t]));
+                float4 u[MT];
+#pragma unroll
+                for (int i = 0; i < MT; ++i) u[i] = __ldcg(&x.part[((slot * NB + nb) * MT + i) * 32 + lane]);
+                float f0, f1, g0, g1;
+                join_weights(m[nb][0], l[nb][0], st.x, st.y, f0, g0);
+                join_weights(m[nb][1], l[nb][1], st.z, st.w, f1, g1);
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    o[nb][i][0] = weighted(f0, o[nb][i][0], g0, u[i].x);
+                    o[nb][i][1] = weighted(f1, o[nb][i][1], g1, u[i].y);
+                    o[nb][i][2] = weighted(f0, o[nb][i][2], g0, u[i].z);
+                    o[nb][i][3] = weighted(f1, o[nb][i][3], g1, u[i].w);
                 }
             }
         }
+        const bool starts = own & 1 || (x.aligned != 0);
+        if (starts && ends) write_unit(unit);
+        else write_part(2 * DK_WARPS * (size_t)x.n_blocks + 2 * (size_t)blockIdx.x + (starts ? 1 : 0));
     }
-    cp_async_wait<0>();
 }
 
-// adds a part (maximum pm, sum pl, two outputs) to what has been joined so far; pl = 0: a part without keys
-__device__ __forceinline__ void join_part(float& m, float& l, float& a, float& b, float pm, float pl, float pa, float pb) {
-    if (pl == 0.f) return;
-    const float top = fmaxf(m, pm);
-    const float f = l == 0.f ? 0.f : ex2_ftz(m - top), pf = pm == top ? 1.f : ex2_ftz(pm - top);
-    l = fmaf(f, l, pf * pl);
-    a = fmaf(f, a, pf * pa);
-    b = fmaf(f, b, pf * pb);
-    m = top;
-}
-
-// One block per unit, thread (j, y): fragment j of the output, parts y, y + LANES, ...:  O = sum_c 2^(m_c - m) O_c / sum_c 2^(m_c - m) l_c.
+// One block per unit, thread (j, y): fragment j of the output, parts y, y + blockDim.y, ...:  O = sum_c 2^(m_c - m) O_c / sum_c 2^(m_c - m) l_c.
 // A part without a key that counts has m_c = -inf, l_c = 0 and is left out; requests without keys get zeros.
 template <int D, int NB>
 __global__ void __launch_bounds__(NB * D * 2 * dk_join_lanes(D, NB)) k_attn_join_kv4(const DecodeKv4Args x) {
@@ -567,27 +699,32 @@ __global__ void __launch_bounds__(NB * D * 2 * dk_join_lanes(D, NB)) k_attn_join
     const int head = hh % x.h_blocks * 8 * NB + nb * 8 + 2 * t;
     float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto join = [&](const float4& st, const float4& u) {
+        float f0, f1, g0, g1;
+        join_weights(m0, l0, st.x, st.y, f0, g0);
+        join_weights(m1, l1, st.z, st.w, f1, g1);
+        v.x = weighted(f0, v.x, g0, u.x);
+        v.y = weighted(f1, v.y, g1, u.y);
+        v.z = weighted(f0, v.z, g0, u.z);
+        v.w = weighted(f1, v.w, g1, u.w);
+    };
     if (head < x.G) {
-        auto slot = [&](int c) { return 2 * (size_t)(pc.x + c) + (c == 0 ? 1 : 0); };
+        auto slot = [&](int c) { return 2 * DK_WARPS * (size_t)x.n_blocks + 2 * (size_t)(pc.x + c) + (c == 0 ? 1 : 0); };
 #pragma unroll 4
-        for (int c = y; c < pc.y; c += LANES) {
+        for (int c = y; c < pc.y; c += blockDim.y) {
             const float4 st = __ldcg(reinterpret_cast<const float4*>(&x.stats[slot(c) * 8 * NB + nb * 8 + 2 * t]));
             const float4 u = __ldcg(&x.part[((slot(c) * NB + nb) * MT + i) * 32 + lane]);
-            join_part(m0, l0, v.x, v.z, st.x, st.y, u.x, u.z);
-            join_part(m1, l1, v.y, v.w, st.z, st.w, u.y, u.w);
+            join(st, u);
         }
     }
     if (y > 0) {
         acc[y - 1][j] = v;
         stat[y - 1][j] = make_float4(m0, l0, m1, l1);
     }
-    __syncthreads();
+    if (blockDim.y > 1) __syncthreads();
     if (y > 0 || head >= x.G) return;
-#pragma unroll
-    for (int k = 0; k < LANES - 1; ++k) {
-        const float4 u = acc[k][j], st = stat[k][j];
-        join_part(m0, l0, v.x, v.z, st.x, st.y, u.x, u.z);
-        join_part(m1, l1, v.y, v.w, st.z, st.w, u.y, u.w);
+    for (int k = 0; k < (int)blockDim.y - 1; ++k) {
+        join(stat[k][j], acc[k][j]);
     }
     const float r0 = l0 == 0.f ? 0.f : 1.f / l0, r1 = l1 == 0.f ? 0.f : 1.f / l1;
     uint16_t* out = x.O + ((size_t)(b * x.H_kv + hh / x.h_blocks) * x.G + head) * D + 16 * i + g;
@@ -602,8 +739,9 @@ __global__ void __launch_bounds__(NB * D * 2 * dk_join_lanes(D, NB)) k_attn_join
 // Blocks of query heads (8 or 16 rows of the MMA's N side), warps - from the shape alone, so that the workspace can be sized without a
 // device.  Every warp is resident at once: 148 SMs times two blocks of eight warps with 8 heads, one with 16 (255 registers a thread).
 struct DecodeKv4Shape {
-    int nb, h_blocks, n_blocks;
+    int nb, h_blocks, n_blocks, aligned;
     long long units;
+    size_t slots() const { return (2 * DK_WARPS + 2) * (size_t)n_blocks; }
 };
 static bool decode_kv4_shape(long long B, int H_q, int H_kv, int D, int max_pages, DecodeKv4Shape* s) {
     if (B < 1 || H_kv < 1 || H_kv > 1024 || H_q < H_kv || H_q % H_kv || (D != 64 && D != 128) || max_pages < 1 || max_pages >= (1 << 25)) return false;
@@ -612,7 +750,10 @@ static bool decode_kv4_shape(long long B, int H_q, int H_kv, int D, int max_page
     s->nb = G <= 8 ? 1 : 2;
     s->h_blocks = (G + 8 * s->nb - 1) / (8 * s->nb);
     s->units = B * H_kv * s->h_blocks;
-    s->n_blocks = (int)std::min<long long>(s->nb == 1 ? 2 * 148 : 148, s->units * max_pages);
+    const int most = s->nb == 1 ? 2 * 148 : 148;
+    // up to 16 pages a row and a block for every unit: two pages a warp at most, and no second launch
+    s->aligned = max_pages <= 2 * DK_WARPS && s->units <= most;
+    s->n_blocks = s->aligned ? (int)s->units : (int)std::min<long long>(most, (s->units * max_pages + DK_WARPS - 1) / DK_WARPS);
     return s->units <= 0x7fffffffll;
 }
 static size_t align256(size_t n) { return (n + 255) / 256 * 256; }
@@ -624,8 +765,7 @@ using namespace ag;
 extern "C" size_t ag_attention_decode_kv4_workspace(int B, int H_q, int H_kv, int D, int max_pages) {
     DecodeKv4Shape s;
     if (!decode_kv4_shape(B, H_q, H_kv, D, max_pages, &s)) return 0;
-    const size_t slots = 2 * (size_t)s.n_blocks * DK_WARPS, heads = 8 * s.nb;
-    return slots * heads * D * sizeof(float) + align256(slots * heads * sizeof(float2)) + s.units * sizeof(int2);
+    return s.slots() * 8 * s.nb * D * sizeof(float) + align256(s.slots() * 8 * s.nb * sizeof(float2)) + s.units * sizeof(int2);
 }
 
 extern "C" ag_status attention_decode_kv4(const void* Q, const ag_kv4_pool* pool, const ag_kv4_table* table, const int32_t* row, void* O, int B, int H_q,
@@ -641,7 +781,6 @@ extern "C" ag_status attention_decode_kv4(const void* Q, const ag_kv4_pool* pool
     ag_status st = check_arch();
     if (st != AG_OK) return st;
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
-    const size_t slots = 2 * (size_t)s.n_blocks * DK_WARPS;
     DecodeKv4Args x;
     memset(&x, 0, sizeof x);
     x.Q = (const uint16_t*)Q;
@@ -649,11 +788,11 @@ extern "C" ag_status attention_decode_kv4(const void* Q, const ag_kv4_pool* pool
     x.pages = (const uint8_t*)pool->pages;
     x.page_of = table->page_of; x.len = table->len; x.row = row;
     x.part = (float4*)workspace;
-    x.stats = (float2*)((uint8_t*)workspace + slots * 8 * s.nb * pool->D * sizeof(float));
-    x.pieces = (int2*)((uint8_t*)x.stats + align256(slots * 8 * s.nb * sizeof(float2)));
+    x.stats = (float2*)((uint8_t*)workspace + s.slots() * 8 * s.nb * pool->D * sizeof(float));
+    x.pieces = (int2*)((uint8_t*)x.stats + align256(s.slots() * 8 * s.nb * sizeof(float2)));
     x.B = B; x.n_pages = (int)pool->n_pages; x.H_kv = pool->H_kv; x.G = H_q / pool->H_kv;
     x.n_rows = table->n_rows; x.max_pages = table->max_pages; x.h_blocks = s.h_blocks;
-    x.n_warps = s.n_blocks * DK_WARPS;
+    x.n_blocks = s.n_blocks; x.aligned = s.aligned;
     x.scale_log2e = 1.4426950408889634f / sqrtf((float)pool->D);
     void (*kernel)(DecodeKv4Args) = pool->D == 128 ? (s.nb == 2 ? k_attn_decode_kv4<128, 2> : k_attn_decode_kv4<128, 1>)
                                                    : (s.nb == 2 ? k_attn_decode_kv4<64, 2> : k_attn_decode_kv4<64, 1>);
@@ -669,10 +808,12 @@ extern "C" ag_status attention_decode_kv4(const void* Q, const ag_kv4_pool* pool
     kernel<<<(unsigned)s.n_blocks, DK_THREADS, pool->D == 128 ? dk_smem_bytes<128>() : dk_smem_bytes<64>(), stream>>>(x);
     AG_CUDA(cudaGetLastError());
     count_launch();
+    if (s.aligned) return AG_OK;
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof cfg);
     cfg.gridDim = dim3((unsigned)s.units);
-    cfg.blockDim = dim3(s.nb * pool->D * 2, dk_join_lanes(pool->D, s.nb));
+    // a unit has about n_blocks / units parts: added side by side where that is many, one after the other where units are many
+    cfg.blockDim = dim3(s.nb * pool->D * 2, s.units >= 2 * 148 ? 1 : dk_join_lanes(pool->D, s.nb));
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
