@@ -124,6 +124,13 @@ __device__ __forceinline__ void join_weights(float& m, float& l, float pm, float
     m = pl == 0.f ? m : top;
 }
 
+// Where a warp is in the line of pages, apart from the page itself: needed once a page or once a unit, so it does not take registers.
+// Every lane writes the same values.
+struct WarpWalk {
+    long long unit_begin, now_begin;               // place of the first page of the unit to be fetched from next / of the unit in hand
+    int b, hh, len, row, now_unit, now_pages;
+};
+
 template <int D>
 constexpr int dk_smem_bytes() { return DK_WARPS * kv4_head_bytes(D); }
 
@@ -136,6 +143,7 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
     __shared__ long long warp_sum[DK_WARPS];
     __shared__ int slot_unit[2 * DK_WARPS];        // units that a warp has only a part of: one that began before its run, one that goes on behind it
     __shared__ int slot_ends[2 * DK_WARPS];        // the part includes the unit's last page
+    __shared__ WarpWalk walk[DK_WARPS];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     dep_release();
 
@@ -235,7 +243,13 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
         p = (int)(rest - (long long)hh * np);
         first_unit_begin = begin - p;
     }
-    long long unit_begin = first_unit_begin;       // place of the unit's first page
+    WarpWalk* at = &walk[warp];
+    at->unit_begin = first_unit_begin;
+    at->b = b;
+    at->hh = hh;
+    at->len = len;
+    at->row = row;
+    __syncwarp();
     const int p_first = p;
     int id_batch = 0, id_first = -64;              // ids of pages id_first + lane of the row (reloaded as p leaves them)
     const uint8_t* src_next = nullptr;
@@ -243,11 +257,11 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
     auto locate = [&]() {                          // source and number of keys of page p
         if (p < id_first || p >= id_first + 32) {
             id_first = p;
-            id_batch = p + lane < np ? x.page_of[(size_t)row * x.max_pages + p + lane] : -1;
+            id_batch = p + lane < np ? x.page_of[(size_t)at->row * x.max_pages + p + lane] : -1;
         }
         const int id = __shfl_sync(0xffffffffu, id_batch, p - id_first);
-        nv_next = id >= 0 && id < x.n_pages ? min(KV4_PAGE, len - p * KV4_PAGE) : 0;
-        src_next = x.pages + ((size_t)(nv_next ? id : 0) * x.H_kv + hh / x.h_blocks) * kv4_head_bytes(D);
+        nv_next = id >= 0 && id < x.n_pages ? min(KV4_PAGE, at->len - p * KV4_PAGE) : 0;
+        src_next = x.pages + ((size_t)(nv_next ? id : 0) * x.H_kv + at->hh / x.h_blocks) * kv4_head_bytes(D);
     };
     if (left > 0) {
         locate();
@@ -289,10 +303,13 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
         }
     };
     while (left > 0) {
-        const int b_now = b, hh_now = hh, p_now = p, np_now = np, nv = nv_next;
-        const int head0 = hh_now % x.h_blocks * 8 * NB;       // first query head of the block, of the KV head's G
-        const long long unit_now = unit_begin;
+        const int nv = nv_next;
         if (fresh) {
+            const int b_now = at->b, hh_now = at->hh;
+            const int head0 = hh_now % x.h_blocks * 8 * NB;       // first query head of the block, of the KV head's G
+            at->now_unit = b_now * heads + hh_now;
+            at->now_pages = np;
+            at->now_begin = at->unit_begin;
             const uint16_t* q_rows = x.Q + ((size_t)b_now * x.H_kv + hh_now / x.h_blocks) * x.G * D;
             // ---- queries as B operands: q times a power of two c (the head's largest |q| between 128 and 256) in fp16, exact down to
             // 2^-22 of the largest.  Lane (g, t) holds head g, elements 32 grp + 8 t + {0, 4}, {1, 5}, {2, 6}, {3, 7}.  Even elements meet
@@ -378,10 +395,11 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
         }
         cp_async_wait<1>();                        // K of this page has landed
         __syncwarp();
+        // (the runs behind the last key are computed with the others: what they hold does not count, see below)
         float s[NB][4][4];
+        if (nv > 0) {
 #pragma unroll
-        for (int run = 0; run < 4; ++run) {
-            if (run * 16 < nv) {
+            for (int run = 0; run < 4; ++run) {
                 uint32_t w[2][NG], sb[2][NG], bb[2], ss[2];     // rows g and g + 8 of the run: codes, pairs, two groups' bases and scales as A operands
 #pragma unroll
                 for (int hh = 0; hh < 2; ++hh) {
@@ -433,21 +451,31 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
         }
         __syncwarp();                              // every lane has read K
         // ---- on to the next page: same unit, next head, next request that has any
+        const bool ends = p + 1 == np;
         --left;
         nv_next = 0;
         if (left > 0) {
-            if (++p == np) {
-                unit_begin += np;
+            ++p;
+            if (ends) {
+                int bn = at->b, hn = at->hh + 1, rn, ln;
+                const long long next_begin = at->unit_begin + np;
+                __syncwarp();                      // every lane has read them
+                at->unit_begin = next_begin;
                 p = 0;
-                if (++hh == heads) {
-                    hh = 0;
+                if (hn == heads) {
+                    hn = 0;
                     do {
-                        ++b;
-                        len = row_tokens(x, b, &row);
-                        np = pages_of(len);
+                        ++bn;
+                        ln = row_tokens(x, bn, &rn);
+                        np = pages_of(ln);
                     } while (np == 0);
                     id_first = -64;
+                    at->b = bn;
+                    at->len = ln;
+                    at->row = rn;
                 }
+                at->hh = hn;
+                __syncwarp();
             }
             locate();
         }
@@ -504,13 +532,13 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
         if (nv > 0) {
             // The pairs of two keys side by side (s, s') and (c, c'), c = b - 16 s, in fp16 times 2^(13 - v_exp): |b| + 31 s, the largest a value
             // can be, stays below 2^15.  Lane = pair of keys; in place.  What lies behind the last key may be anything and becomes zero.
-            uint32_t* at = reinterpret_cast<uint32_t*>(vbuf + 32 * D) + lane * 2 * NG;
+            uint32_t* pairs = reinterpret_cast<uint32_t*>(vbuf + 32 * D) + lane * 2 * NG;
             uint32_t w[2][NG];
             float top = 0.f;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                if (D == 128) *reinterpret_cast<uint4*>(&w[e][0]) = *reinterpret_cast<const uint4*>(at + e * NG);
-                else *reinterpret_cast<uint2*>(&w[e][0]) = *reinterpret_cast<const uint2*>(at + e * NG);
+                if (D == 128) *reinterpret_cast<uint4*>(&w[e][0]) = *reinterpret_cast<const uint4*>(pairs + e * NG);
+                else *reinterpret_cast<uint2*>(&w[e][0]) = *reinterpret_cast<const uint2*>(pairs + e * NG);
 #pragma unroll
                 for (int grp = 0; grp < NG; ++grp) {
                     if (2 * lane + e >= nv) w[e][grp] = 0u;
@@ -540,14 +568,12 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
             }
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                if (D == 128) *reinterpret_cast<uint4*>(at + e * NG) = *reinterpret_cast<const uint4*>(&sc[e][0]);
-                else *reinterpret_cast<uint2*>(at + e * NG) = *reinterpret_cast<const uint2*>(&sc[e][0]);
+                if (D == 128) *reinterpret_cast<uint4*>(pairs + e * NG) = *reinterpret_cast<const uint4*>(&sc[e][0]);
+                else *reinterpret_cast<uint2*>(pairs + e * NG) = *reinterpret_cast<const uint2*>(&sc[e][0]);
             }
             __syncwarp();
-        }
 #pragma unroll
-        for (int run = 0; run < 4; ++run) {
-            if (run * 16 < nv) {
+            for (int run = 0; run < 4; ++run) {
                 uint32_t pf[NB][2];                // probabilities as B operands
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb)
@@ -596,7 +622,6 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
         fetch(1, src_next, nv_next);
 
         // ---- the end of the unit, or of this warp's share of it
-        const bool ends = p_now + 1 == np_now;
         if (ends || left == 0) {
             const float unexp = __uint_as_float((uint32_t)(127 - 13 + v_exp) << 23);
 #pragma unroll
@@ -612,7 +637,7 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
 #pragma unroll
                     for (int c = 0; c < 4; ++c) o[nb][i][c] *= unexp;
             }
-            const int unit = b_now * heads + hh_now;
+            const int unit = at->now_unit;
             if (whole && ends) {
                 write_unit(unit);
                 if (!x.aligned && lane == 0) x.pieces[unit] = make_int2(blockIdx.x, 1);
@@ -623,7 +648,7 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
                     slot_unit[slot] = unit;
                     slot_ends[slot] = ends;
                     if (whole && !x.aligned) {
-                        const int last = run_holding(unit_now + np_now - 1, total, n_blocks);
+                        const int last = run_holding(at->now_begin + at->now_pages - 1, total, n_blocks);
                         x.pieces[unit] = make_int2(blockIdx.x, last - (int)blockIdx.x + 1);
                     }
                 }
