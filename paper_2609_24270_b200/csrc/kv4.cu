@@ -17,104 +17,140 @@ namespace ag {
 //
 // D / 8 lanes hold a row (eight elements, one 16-byte load each); a lane's eight K codes are one word of the page, the V codes
 // are transposed across lanes (kv4_transpose) so that a lane writes whole words of the fragment order as well.
-template <int D>
-__global__ void __launch_bounds__(256) k_kv4_store(uint8_t* __restrict__ pages, long long n_slots, int H_kv, const uint16_t* __restrict__ K,
-                                                   const uint16_t* __restrict__ V, long long n_tokens, long long k_stride, long long v_stride,
-                                                   const int32_t* __restrict__ slot) {
-    constexpr int L = D / 8;                                        // lanes of a row
-    const long long task = ((long long)blockIdx.x * blockDim.x + threadIdx.x) / L;      // ((token, head), K or V)
-    const int l = threadIdx.x % L;
-    const int which = (int)(task & 1);
-    const long long th = task >> 1;
-    const long long tok = th / H_kv;
-    const int head = (int)(th - tok * H_kv);
-    const int at = tok < n_tokens ? slot[tok] : -1;
-    const bool live = at >= 0 && at < n_slots;
-    uint4 raw = make_uint4(0, 0, 0, 0);
-    if (live) raw = *reinterpret_cast<const uint4*>((which ? V + tok * v_stride : K + tok * k_stride) + head * D + l * 8);
-    float x[8] = {bf16_lo(raw.x), bf16_hi(raw.x), bf16_lo(raw.y), bf16_hi(raw.y), bf16_lo(raw.z), bf16_hi(raw.z), bf16_lo(raw.w), bf16_hi(raw.w)};
-    float lo = x[0], hi = x[0], odd = 0.f;
+//
+// A block takes U times 128 / L neighbouring tokens of one head: the words of neighbouring V rows share sectors, and U rows a lane are in
+// flight together (a row's chain slot -> page -> row is some 2 us long: one row a lane moved 2.9 TB/s, four are bound by the memory).
+constexpr int KS_THREADS = 256;
+constexpr int KS_ROWS = 4;                           // U of large calls; small ones take 1, for more blocks
+
+template <int D, int U>
+__global__ void __launch_bounds__(KS_THREADS) k_kv4_store(uint8_t* __restrict__ pages, long long n_slots, int H_kv, const uint16_t* __restrict__ K,
+                                                          const uint16_t* __restrict__ V, long long n_tokens, long long k_stride, long long v_stride,
+                                                          const int32_t* __restrict__ slot) {
+    constexpr int L = D / 8, TOK = KS_THREADS / 2 / L;              // lanes of a row, tokens of the block side by side
+    const int l = threadIdx.x % L, which = threadIdx.x / L & 1;
+    const int head = blockIdx.x % H_kv;
+    const long long tok0 = (long long)(blockIdx.x / H_kv) * (TOK * U) + threadIdx.x / (2 * L);
+    const uint16_t* from = (which ? V : K) + head * D + l * 8;
+    const long long stride = which ? v_stride : k_stride;
+    int at[U];
+    uint4 raw[U];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        lo = fminf(lo, x[i]);
-        hi = fmaxf(hi, x[i]);
-        odd = fmaf(x[i], 0.f, odd);                                 // NaN as soon as one element is not finite
+    for (int u = 0; u < U; ++u) {
+        const long long tok = tok0 + u * TOK;
+        at[u] = tok < n_tokens ? slot[tok] : -1;
+        if (at[u] >= n_slots) at[u] = -1;
+        raw[u] = make_uint4(0, 0, 0, 0);
+        if (tok < n_tokens) raw[u] = *reinterpret_cast<const uint4*>(from + tok * stride);
     }
 #pragma unroll
-    for (int o = 1; o < 4; o <<= 1) {
-        lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-        hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-        odd += __shfl_xor_sync(0xffffffffu, odd, o);
-    }
-    const __nv_bfloat16 sb = __float2bfloat16_rn(__fdiv_rn(__fsub_rn(hi, lo), 15.f) + odd);
-    const float s = __bfloat162float(sb);
-    const bool fine = s <= 3.4e38f;                                 // false for NaN and infinity
-    uint32_t w = 0;
-    if (fine && s > 0.f) {
+    for (int u = 0; u < U; ++u) {
+        const float x[8] = {bf16_lo(raw[u].x), bf16_hi(raw[u].x), bf16_lo(raw[u].y), bf16_hi(raw[u].y),
+                            bf16_lo(raw[u].z), bf16_hi(raw[u].z), bf16_lo(raw[u].w), bf16_hi(raw[u].w)};
+        float lo = x[0], hi = x[0], odd = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int c = min(15, __float2int_rn(__fdiv_rn(__fsub_rn(x[i], lo), s)));
-            w |= (uint32_t)c << (4 * i);
+            lo = fminf(lo, x[i]);
+            hi = fmaxf(hi, x[i]);
+            odd = fmaf(x[i], 0.f, odd);                             // NaN as soon as one element is not finite
         }
-    }
-    const uint32_t wt = kv4_transpose<D / 16, 2>(w, l >> 1);        // lanes of equal parity hold elements 16 i + 8 (l & 1) + j
-    if (!live) return;
-    uint8_t* block = pages + ((size_t)(at / KV4_PAGE) * H_kv + head) * kv4_head_bytes(D);
-    const int r = at % KV4_PAGE;
-    if (which == 0) {
-        *reinterpret_cast<uint32_t*>(block + kv4_k_word<D>(r, l >> 2, l & 3)) = w;
-    } else if (D == 128) {
-        *reinterpret_cast<uint32_t*>(block + kv4_v_word<D>(r, l & 1, l >> 1)) = wt;
-    } else {
-        *reinterpret_cast<uint16_t*>(block + kv4_v_word<D>(r, l & 1, l >> 1)) = (uint16_t)wt;
-        *reinterpret_cast<uint16_t*>(block + kv4_v_word<D>(r, l & 1, 4 + (l >> 1))) = (uint16_t)(wt >> 16);
-    }
-    if ((l & 3) == 0) {
-        const uint32_t nan = 0x7fc07fc0u;
-        const uint32_t pair = (uint32_t)__bfloat16_as_ushort(sb) | (__float_as_uint(lo) & 0xffff0000u);
-        *reinterpret_cast<uint32_t*>(block + kv4_scale_word<D>(which, r, l >> 2)) = fine ? pair : nan;
+#pragma unroll
+        for (int o = 1; o < 4; o <<= 1) {
+            lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+            hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+            odd += __shfl_xor_sync(0xffffffffu, odd, o);
+        }
+        const __nv_bfloat16 sb = __float2bfloat16_rn(__fdiv_rn(__fsub_rn(hi, lo), 15.f) + odd);
+        const float s = __bfloat162float(sb);
+        const bool fine = s <= 3.4e38f;                             // false for NaN and infinity
+        uint32_t w = 0;
+        if (fine && s > 0.f) {
+            // rint((x - lo) / s) without dividing: a candidate c from the reciprocal, settled by the remainder x - lo - c s (exact: c has 4 bits, s
+            // has 8).  Near a border, half a step away from two codes, the quotient's own rounding decides, so it is taken as defined.
+            const float r = __frcp_rn(s), border = 0.4999f * s;
+            if (r <= 3.4e38f) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float d = __fsub_rn(x[i], lo), q = __fmaf_rn(d, r, 12582912.f);   // 1.5 * 2^23: the sum's low bits are the rounded quotient
+                    uint32_t c = __float_as_uint(q) & 15u;
+                    if (fabsf(__fmaf_rn(__fsub_rn(12582912.f, q), s, d)) > border) c = (uint32_t)min(15, __float2int_rn(__fdiv_rn(d, s)));
+                    w |= c << (4 * i);
+                }
+            } else {                                                // the smallest scales have no reciprocal in 32 bits
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w |= (uint32_t)min(15, __float2int_rn(__fdiv_rn(__fsub_rn(x[i], lo), s))) << (4 * i);
+            }
+        }
+        const uint32_t wt = kv4_transpose<D / 16, 2>(w, l >> 1);    // lanes of equal parity hold elements 16 i + 8 (l & 1) + j
+        if (at[u] < 0) continue;
+        uint8_t* block = pages + ((size_t)(at[u] / KV4_PAGE) * H_kv + head) * kv4_head_bytes(D);
+        const int r = at[u] % KV4_PAGE;
+        if (which == 0) {
+            *reinterpret_cast<uint32_t*>(block + kv4_k_word<D>(r, l >> 2, l & 3)) = w;
+        } else if (D == 128) {
+            *reinterpret_cast<uint32_t*>(block + kv4_v_word<D>(r, l & 1, l >> 1)) = wt;
+        } else {
+            *reinterpret_cast<uint16_t*>(block + kv4_v_word<D>(r, l & 1, l >> 1)) = (uint16_t)wt;
+            *reinterpret_cast<uint16_t*>(block + kv4_v_word<D>(r, l & 1, 4 + (l >> 1))) = (uint16_t)(wt >> 16);
+        }
+        if ((l & 3) == 0) {
+            const uint32_t nan = 0x7fc07fc0u;
+            const uint32_t pair = (uint32_t)__bfloat16_as_ushort(sb) | (__float_as_uint(lo) & 0xffff0000u);
+            *reinterpret_cast<uint32_t*>(block + kv4_scale_word<D>(which, r, l >> 2)) = fine ? pair : nan;
+        }
     }
 }
 
-template <int D>
-__global__ void __launch_bounds__(256) k_kv4_load(const uint8_t* __restrict__ pages, long long n_slots, int H_kv, uint16_t* __restrict__ K,
-                                                  uint16_t* __restrict__ V, long long n_tokens, long long k_stride, long long v_stride,
-                                                  const int32_t* __restrict__ slot) {
-    constexpr int L = D / 8;
-    const long long task = ((long long)blockIdx.x * blockDim.x + threadIdx.x) / L;
-    const int l = threadIdx.x % L;
-    const int which = (int)(task & 1);
-    const long long th = task >> 1;
-    const long long tok = th / H_kv;
-    const int head = (int)(th - tok * H_kv);
-    const int at = tok < n_tokens ? slot[tok] : -1;
-    const bool live = at >= 0 && at < n_slots;
-    const uint8_t* block = pages + ((size_t)(live ? at / KV4_PAGE : 0) * H_kv + head) * kv4_head_bytes(D);
-    const int r = live ? at % KV4_PAGE : 0;
-    uint32_t w = 0, pair = 0;
-    if (live) {
-        if (which == 0) w = *reinterpret_cast<const uint32_t*>(block + kv4_k_word<D>(r, l >> 2, l & 3));
-        else if (D == 128) w = *reinterpret_cast<const uint32_t*>(block + kv4_v_word<D>(r, l & 1, l >> 1));
-        else w = *reinterpret_cast<const uint16_t*>(block + kv4_v_word<D>(r, l & 1, l >> 1)) |
-                 (uint32_t)*reinterpret_cast<const uint16_t*>(block + kv4_v_word<D>(r, l & 1, 4 + (l >> 1))) << 16;
-        pair = *reinterpret_cast<const uint32_t*>(block + kv4_scale_word<D>(which, r, l >> 2));
-    }
-    const uint32_t wt = kv4_transpose<D / 16, 2>(w, l >> 1);
-    if (which) w = wt;
-    if (!live) return;
-    uint32_t out[4];
+template <int D, int U>
+__global__ void __launch_bounds__(KS_THREADS) k_kv4_load(const uint8_t* __restrict__ pages, long long n_slots, int H_kv, uint16_t* __restrict__ K,
+                                                         uint16_t* __restrict__ V, long long n_tokens, long long k_stride, long long v_stride,
+                                                         const int32_t* __restrict__ slot) {
+    constexpr int L = D / 8, TOK = KS_THREADS / 2 / L;
+    const int l = threadIdx.x % L, which = threadIdx.x / L & 1;
+    const int head = blockIdx.x % H_kv;
+    const long long tok0 = (long long)(blockIdx.x / H_kv) * (TOK * U) + threadIdx.x / (2 * L);
+    uint16_t* to = (which ? V : K) + head * D + l * 8;
+    const long long stride = which ? v_stride : k_stride;
+    int at[U];
+    uint32_t w[U], pair[U];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const __nv_bfloat162 v = __floats2bfloat162_rn(fmaf((float)((w >> (8 * i)) & 15u), bf16_lo(pair), bf16_hi(pair)),
-                                                       fmaf((float)((w >> (8 * i + 4)) & 15u), bf16_lo(pair), bf16_hi(pair)));
-        out[i] = *reinterpret_cast<const uint32_t*>(&v);
+    for (int u = 0; u < U; ++u) {
+        const long long tok = tok0 + u * TOK;
+        at[u] = tok < n_tokens ? slot[tok] : -1;
+        if (at[u] >= n_slots) at[u] = -1;
     }
-    *reinterpret_cast<uint4*>((which ? V + tok * v_stride : K + tok * k_stride) + head * D + l * 8) = make_uint4(out[0], out[1], out[2], out[3]);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        w[u] = pair[u] = 0;
+        if (at[u] >= 0) {
+            const uint8_t* block = pages + ((size_t)(at[u] / KV4_PAGE) * H_kv + head) * kv4_head_bytes(D);
+            const int r = at[u] % KV4_PAGE;
+            if (which == 0) w[u] = *reinterpret_cast<const uint32_t*>(block + kv4_k_word<D>(r, l >> 2, l & 3));
+            else if (D == 128) w[u] = *reinterpret_cast<const uint32_t*>(block + kv4_v_word<D>(r, l & 1, l >> 1));
+            else w[u] = *reinterpret_cast<const uint16_t*>(block + kv4_v_word<D>(r, l & 1, l >> 1)) |
+                        (uint32_t)*reinterpret_cast<const uint16_t*>(block + kv4_v_word<D>(r, l & 1, 4 + (l >> 1))) << 16;
+            pair[u] = *reinterpret_cast<const uint32_t*>(block + kv4_scale_word<D>(which, r, l >> 2));
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const uint32_t wt = kv4_transpose<D / 16, 2>(w[u], l >> 1), c = which ? wt : w[u];
+        if (at[u] < 0) continue;
+        uint32_t out[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 v = __floats2bfloat162_rn(fmaf((float)((c >> (8 * i)) & 15u), bf16_lo(pair[u]), bf16_hi(pair[u])),
+                                                           fmaf((float)((c >> (8 * i + 4)) & 15u), bf16_lo(pair[u]), bf16_hi(pair[u])));
+            out[i] = *reinterpret_cast<const uint32_t*>(&v);
+        }
+        *reinterpret_cast<uint4*>(to + (tok0 + u * TOK) * stride) = make_uint4(out[0], out[1], out[2], out[3]);
+    }
 }
 
 // ---- page tables ------------------------------------------------------------------------------------------------------
 constexpr int KT_THREADS = 1024;
 constexpr int KT_MAX = AG_KV4_MAX_ROWS;              // requests of one call: one thread each
+constexpr int KT_HOLES = 4096;                       // holes that compaction lists in shared memory; it looks for those beyond
 constexpr int KT_INLINE_TOKENS = 8192;               // up to so many slots are written by the allocating block itself
 
 // exclusive sum over the block of one value per thread; *total = the sum
@@ -192,6 +228,30 @@ __device__ inline bool grant_pages(const TableArgs& t, int n, int need, int firs
     return before + need <= total_free;
 }
 
+// Whether request i is the first of the call that names `key` (a row; -1: none).  Open addressing in shared memory, twice as many places as requests.
+struct FirstShared {
+    int key[2 * KT_MAX], first[2 * KT_MAX];
+};
+__device__ inline bool is_first(int key, FirstShared* sh) {
+    for (int i = threadIdx.x; i < 2 * KT_MAX; i += KT_THREADS) {
+        sh->key[i] = -1;
+        sh->first[i] = KT_MAX;
+    }
+    __syncthreads();
+    uint32_t at = 0;
+    if (key >= 0) {
+        at = (uint32_t)key * 2654435761u >> 21;                            // 11 bits
+        static_assert(2 * KT_MAX == 1 << 11, "places of the table");
+        for (int tries = 0; tries < 2 * KT_MAX; ++tries, at = (at + 1) & (2 * KT_MAX - 1)) {
+            const int seen = atomicCAS(&sh->key[at], -1, key);
+            if (seen == -1 || seen == key) break;
+        }
+        atomicMin(&sh->first[at], (int)threadIdx.x);
+    }
+    __syncthreads();
+    return key >= 0 && sh->first[at] == (int)threadIdx.x;
+}
+
 // slot of token j: request i with new_off[i] <= j < new_off[i + 1], position len - new + j - new_off[i] (len: after the call)
 __device__ __forceinline__ int slot_of(const TableArgs& t, const int32_t* row, const int32_t* new_off, const int32_t* ok, int n, int j) {
     if (j < new_off[0] || j >= new_off[n]) return -1;
@@ -210,18 +270,16 @@ __device__ __forceinline__ int slot_of(const TableArgs& t, const int32_t* row, c
 
 __global__ void __launch_bounds__(KT_THREADS) k_kv4_extend(const TableArgs t, const int32_t* __restrict__ row, const int32_t* __restrict__ new_off,
                                                            int n, int32_t* __restrict__ slot, int inline_tokens, int32_t* ok) {
-    __shared__ GrantShared sh;
+    __shared__ union { GrantShared grant; FirstShared first; } sh;
     dep_release();
     const int i = threadIdx.x;
-    sh.row[i] = i < n ? row[i] : -1;
-    __syncthreads();
-    int r = -1, need = 0, first = 0;
+    int r = i < n ? row[i] : -1;
+    const bool first_time = is_first(r, &sh.first);                        // a row named twice: only the first time counts
+    int need = 0, first = 0;
     long long len0 = 0, fresh = 0;
     if (i < n) {
-        r = sh.row[i];
         fresh = (long long)new_off[i + 1] - new_off[i];
-        bool fine = r >= 0 && r < t.n_rows && fresh >= 0 && new_off[i] >= 0;
-        for (int j = 0; j < i && fine; ++j) fine = sh.row[j] != r;         // a row named twice: only the first time counts
+        bool fine = first_time && r < t.n_rows && fresh >= 0 && new_off[i] >= 0;
         if (fine) {
             len0 = t.len[r];
             fine = len0 >= 0 && len0 + fresh <= (long long)t.max_pages * KV4_PAGE;
@@ -234,7 +292,7 @@ __global__ void __launch_bounds__(KT_THREADS) k_kv4_extend(const TableArgs t, co
         }
     }
     __syncthreads();
-    const bool granted = grant_pages(t, n, need, first, r, &sh) && r >= 0;
+    const bool granted = grant_pages(t, n, need, first, r, &sh.grant) && r >= 0;
     if (granted) t.len[r] = (int)(len0 + fresh);
     if (i < n) ok[i] = granted ? 1 : 0;
     __syncthreads();                                                       // tables and ok are complete for this block
@@ -250,17 +308,15 @@ __global__ void __launch_bounds__(256) k_kv4_slots(const TableArgs t, const int3
 
 __global__ void __launch_bounds__(KT_THREADS) k_kv4_fork_plan(const TableArgs t, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
                                                               int n, int32_t* __restrict__ ok) {
-    __shared__ GrantShared sh;
+    __shared__ union { GrantShared grant; FirstShared first; } sh;
     dep_release();
     const int i = threadIdx.x;
-    sh.row[i] = i < n ? dst[i] : -1;
-    __syncthreads();
-    int r = -1, need = 0, first = 0, len = 0;
+    int r = i < n ? dst[i] : -1;
+    const bool first_time = is_first(r, &sh.first);
+    int need = 0, first = 0, len = 0;
     if (i < n) {
         const int s = src[i];
-        r = sh.row[i];
-        bool fine = r >= 0 && r < t.n_rows && s >= 0 && s < t.n_rows && s != r;
-        for (int j = 0; j < i && fine; ++j) fine = sh.row[j] != r;
+        bool fine = first_time && r < t.n_rows && s >= 0 && s < t.n_rows && s != r;
         if (fine) {
             len = t.len[s];
             fine = t.len[r] == 0 && len >= 0 && (long long)len <= (long long)t.max_pages * KV4_PAGE;
@@ -273,7 +329,7 @@ __global__ void __launch_bounds__(KT_THREADS) k_kv4_fork_plan(const TableArgs t,
         }
     }
     __syncthreads();
-    const bool granted = grant_pages(t, n, need, first, r, &sh) && r >= 0;
+    const bool granted = grant_pages(t, n, need, first, r, &sh.grant) && r >= 0;
     if (granted) t.len[r] = len;                                           // every thread has read its lengths (barriers in grant_pages)
     if (i < n) ok[i] = granted ? 1 : 0;
 }
@@ -334,6 +390,7 @@ __global__ void __launch_bounds__(256) k_kv4_free(const TableArgs t, const int32
 __global__ void __launch_bounds__(KT_THREADS) k_kv4_compact_plan(const TableArgs t, int32_t* __restrict__ moved) {
     __shared__ int warp_sum[32];
     __shared__ int holes_before[KT_THREADS + 1];
+    __shared__ int hole[KT_HOLES];                                         // the first so many holes, in order
     dep_release();
     const int per = pages_per_thread(t.n_pages);
     const long long p0 = (long long)threadIdx.x * per;
@@ -346,7 +403,13 @@ __global__ void __launch_bounds__(KT_THREADS) k_kv4_compact_plan(const TableArgs
         if (p < n_used) holes += t.refs[p] <= 0;
         else movers += t.refs[p] > 0;
     }
-    holes_before[threadIdx.x] = block_scan(holes, warp_sum, &n_holes);
+    int hole_rank = block_scan(holes, warp_sum, &n_holes);
+    holes_before[threadIdx.x] = hole_rank;
+    for (int p = (int)p0; p < min(p1, n_used); ++p)
+        if (t.refs[p] <= 0) {
+            if (hole_rank < KT_HOLES) hole[hole_rank] = p;
+            ++hole_rank;
+        }
     int rank = block_scan(movers, warp_sum, &n_movers);                    // n_movers = n_holes
     if (threadIdx.x == 0) holes_before[KT_THREADS] = n_holes;
     __syncthreads();
@@ -355,14 +418,18 @@ __global__ void __launch_bounds__(KT_THREADS) k_kv4_compact_plan(const TableArgs
         if (t.refs[p] > 0) {
             to = p;
             if (p >= n_used) {
-                int a = 0, b = KT_THREADS - 1;                              // the thread whose pages hold hole number `rank`
-                while (a < b) {
-                    const int m = (a + b + 1) >> 1;
-                    if (holes_before[m] <= rank) a = m; else b = m - 1;
+                if (rank < KT_HOLES) {
+                    to = hole[rank];
+                } else {
+                    int a = 0, b = KT_THREADS - 1;                          // the thread whose pages hold hole number `rank`
+                    while (a < b) {
+                        const int m = (a + b + 1) >> 1;
+                        if (holes_before[m] <= rank) a = m; else b = m - 1;
+                    }
+                    int k = rank - holes_before[a];
+                    for (int q = a * per; q < n_used; ++q)
+                        if (t.refs[q] <= 0 && k-- == 0) { to = q; break; }
                 }
-                int k = rank - holes_before[a];
-                for (int q = a * per;; ++q)
-                    if (t.refs[q] <= 0 && k-- == 0) { to = q; break; }
                 ++rank;
             }
         }
@@ -430,7 +497,11 @@ static ag_status kv4_rows(bool store, const ag_kv4_pool* pool, const void* K, co
     const int64_t width = (int64_t)pool->H_kv * pool->D;
     if (!K || !V || !slot || (((uintptr_t)K | (uintptr_t)V) & 15u) || ((uintptr_t)slot & 3u) || k_stride < width || v_stride < width || (k_stride % 8) || (v_stride % 8))
         return AG_ERR_ARG;
-    const long long threads = (long long)n_tokens * pool->H_kv * 2 * (pool->D / 8), blocks = (threads + 255) / 256;
+    // four rows a lane once that leaves two rounds of blocks for 148 SMs
+    const int one = KS_THREADS / 2 / (pool->D / 8);
+    const bool many = n_tokens * pool->H_kv >= 2ll * 148 * 8 * KS_ROWS * one;
+    const int block_tokens = one * (many ? KS_ROWS : 1);
+    const long long blocks = (n_tokens + block_tokens - 1) / block_tokens * pool->H_kv;
     if (blocks > 0x7fffffffll) return AG_ERR_ARG;
     ag_status st = check_arch();
     if (st != AG_OK) return st;
@@ -438,12 +509,12 @@ static ag_status kv4_rows(bool store, const ag_kv4_pool* pool, const void* K, co
     const long long n_slots = (long long)pool->n_pages * KV4_PAGE;
     uint8_t* pages = (uint8_t*)pool->pages;
     if (store) {
-        auto kernel = pool->D == 128 ? k_kv4_store<128> : k_kv4_store<64>;
-        kernel<<<(unsigned)blocks, 256, 0, stream>>>(pages, n_slots, pool->H_kv, (const uint16_t*)K, (const uint16_t*)V, n_tokens, k_stride, v_stride, slot);
+        auto kernel = pool->D == 128 ? (many ? k_kv4_store<128, KS_ROWS> : k_kv4_store<128, 1>) : (many ? k_kv4_store<64, KS_ROWS> : k_kv4_store<64, 1>);
+        kernel<<<(unsigned)blocks, KS_THREADS, 0, stream>>>(pages, n_slots, pool->H_kv, (const uint16_t*)K, (const uint16_t*)V, n_tokens, k_stride, v_stride, slot);
     } else {
-        auto kernel = pool->D == 128 ? k_kv4_load<128> : k_kv4_load<64>;
-        kernel<<<(unsigned)blocks, 256, 0, stream>>>(pages, n_slots, pool->H_kv, (uint16_t*)const_cast<void*>(K), (uint16_t*)const_cast<void*>(V), n_tokens,
-                                                     k_stride, v_stride, slot);
+        auto kernel = pool->D == 128 ? (many ? k_kv4_load<128, KS_ROWS> : k_kv4_load<128, 1>) : (many ? k_kv4_load<64, KS_ROWS> : k_kv4_load<64, 1>);
+        kernel<<<(unsigned)blocks, KS_THREADS, 0, stream>>>(pages, n_slots, pool->H_kv, (uint16_t*)const_cast<void*>(K), (uint16_t*)const_cast<void*>(V), n_tokens,
+                                                            k_stride, v_stride, slot);
     }
     count_launch();
     AG_CUDA(cudaGetLastError());

@@ -118,6 +118,30 @@ def test_store_and_load_bit_for_bit(H_kv, D, n):
         assert (np.delete(got, live, 0) == 7.0).all()
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_large_calls_equal_small_ones(D):
+    """Calls with several rows per lane (the last block not full) against the same rows in small calls, which the test above pins."""
+    H, n_pages = 2, 600
+    n = n_pages * 64 - 5
+    c = Cache(n_pages, H, D, 1, 1)
+    gen = torch.Generator(device="cuda").manual_seed(D)
+    K, V = (torch.randn(n, H, D, device="cuda", generator=gen).bfloat16() for _ in range(2))
+    slot = torch.randperm(n_pages * 64, device="cuda", generator=gen)[:n].int()
+    slot[::97] = -1
+    ag.kv4_store(c.pool, K.data_ptr(), V.data_ptr(), slot.data_ptr(), n)
+    once = c.d["pages"].clone()
+    c.d["pages"].copy_(torch.from_numpy(c.pages))
+    step = 1000
+    for i in range(0, n, step):
+        ag.kv4_store(c.pool, K[i:].data_ptr(), V[i:].data_ptr(), slot[i:].data_ptr(), min(step, n - i))
+    assert torch.equal(once, c.d["pages"])
+    back, parts = torch.full((2, n, H, D), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((2, n, H, D), 7.0, dtype=torch.bfloat16, device="cuda")
+    ag.kv4_load(c.pool, slot.data_ptr(), n, back[0].data_ptr(), back[1].data_ptr())
+    for i in range(0, n, step):
+        ag.kv4_load(c.pool, slot[i:].data_ptr(), min(step, n - i), parts[0, i:].data_ptr(), parts[1, i:].data_ptr())
+    assert torch.equal(back, parts) and (back[:, ::97] == 7.0).all() and (back[0, 1:90] - K[1:90]).abs().max() < 0.6
+
+
 def test_tables_follow_the_oracle_through_a_long_history():
     rng = np.random.default_rng(5)
     c = Cache(40, 2, 64, 12, 9)
