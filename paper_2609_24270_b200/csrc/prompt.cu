@@ -31,6 +31,9 @@ constexpr int PA_THREADS = 384;           // warps 0-3 softmax of tile 0, 4-7 of
 constexpr int PA_MAXSEQ = 1024;           // sequences of one launch
 constexpr int PA_CONSUMERS = 8 + 3;       // warps that read the unit: softmax, MMA, K, V
 constexpr float PA_LAZY = 8.f;
+// One pair in eight takes its exponentials from the multiply-add units (exp2_cubic): at 8192 tokens x 32 heads, D = 128, 464 us with none,
+// 456 with one, 459 with two, 475 with three; D = 64: 440, 396, 449, 446.
+constexpr int PA_CUBIC = 1;
 
 struct PromptArgs {
     uint16_t* O;
@@ -53,7 +56,7 @@ struct PromptCtl {
     uint64_t tail, mma_drain;
     int unit[4];                          // sequence (in order of work), KV head, first token; sequence -1: the end
     uint32_t tmem_base;
-    int abort_flag, member;
+    int abort_flag, member, slot;
     int blocks_before[PA_MAXSEQ + 1];     // units of one head in front of the i-th sequence of work
     PromptSeq seq[PA_MAXSEQ];
     int warp_sum[PA_THREADS / 32];
@@ -93,6 +96,50 @@ __device__ __forceinline__ float exp2_fast(float v) {     // 2^v, relative error
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
+}
+// pairs of floats in one register pair: two results for one issue slot
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pack2(float a, float b) {
+    f32x2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpack2(f32x2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+// 2^x on the multiply-add units: x = n + f with n the nearest integer, 2^f by the cubic with the smallest largest relative error on
+// [-1/2, 1/2] (7.5e-5, from an exchange algorithm; bf16 rounds at 2e-3), 2^n through the exponent field, which is 0 for
+// n = -127: what is below 2^-126.5, a masked key's -inf among it, gives exactly 0.  NaN stays NaN.
+__device__ __forceinline__ f32x2 exp2_cubic(f32x2 v) {
+    float v0, v1, t0, t1;
+    unpack2(v, v0, v1);
+    const f32x2 x = pack2(max_nan(v0, -127.f), max_nan(v1, -127.f));
+    constexpr float M = 12582912.f + 127.f;                // 1.5 * 2^23: the sum's low bits are n + 127
+    const f32x2 t = add2(x, pack2(M, M));
+    const f32x2 f = fma2(add2(t, pack2(-M, -M)), pack2(-1.f, -1.f), x);
+    f32x2 q = fma2(f, pack2(0.05517167f, 0.05517167f), pack2(0.24261112f, 0.24261112f));
+    q = fma2(q, f, pack2(0.69326099f, 0.69326099f));
+    q = fma2(q, f, pack2(0.99992807f, 0.99992807f));
+    unpack2(t, t0, t1);
+    return mul2(q, pack2(__uint_as_float(__float_as_uint(t0) << 23), __uint_as_float(__float_as_uint(t1) << 23)));
 }
 __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
     uint32_t r;
@@ -160,7 +207,7 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     PromptCtl* ctl = reinterpret_cast<PromptCtl*>(smem + 2 * C::q_bytes + PA_STAGES * C::kv_bytes);
     volatile int* abort_flag = &ctl->abort_flag;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    if (tid == 0) {
+    if (tid == 32) {
         ctl->abort_flag = 0;
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&ctl->q_full[i]), 1);
@@ -181,36 +228,60 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         prefetch_tmap(&tm_q);
         prefetch_tmap(&tm_k);
         prefetch_tmap(&tm_v);
+    } else if (tid == 64) {
+        // join the plan: the slot of this block's SM, unless another block has it
+        const int slot = p.quick[smid()].x;
+        ctl->slot = slot;
+        ctl->member = slot >= 0 && atomicMax(&p.claimed[slot], p.epoch) < p.epoch;
     }
-    if (join_plan(p, &ctl->member) < 0) return;
-
     // ---- order of work: sequences by falling number of keys (ties in the given order), each from its last tokens to its first, so that
-    // long units come first and short ones fill the end
+    // long units come first and short ones fill the end.  Up to 32 sequences are put in order by one warp while the others set up.
     const int block_tokens = 2 * x.tpt;
-    for (int i = tid; i < x.n_seq; i += PA_THREADS) {
+    auto seq_at = [&](int i) {
         // offsets are clamped: whatever they hold, nothing outside the tensors is read as a sequence
         const int q0 = (int)min(max((long long)x.q_off[i], 0ll), x.q_tokens), q1 = (int)min((long long)x.q_off[i + 1], x.q_tokens);
         const int k0 = (int)min(max((long long)x.kv_off[i], 0ll), x.kv_tokens), k1 = (int)min((long long)x.kv_off[i + 1], x.kv_tokens);
-        ctl->seq[i] = PromptSeq{q0, max(0, q1 - q0), k0, max(0, k1 - k0)};
-    }
-    __syncthreads();
-    int rank[(PA_MAXSEQ + PA_THREADS - 1) / PA_THREADS];
-    PromptSeq mine[(PA_MAXSEQ + PA_THREADS - 1) / PA_THREADS];
-#pragma unroll
-    for (int k = 0; k < (PA_MAXSEQ + PA_THREADS - 1) / PA_THREADS; ++k) {
-        const int i = tid + k * PA_THREADS;
-        rank[k] = -1;
-        if (i < x.n_seq) {
-            mine[k] = ctl->seq[i];
-            rank[k] = 0;
-            for (int j = 0; j < x.n_seq; ++j) rank[k] += ctl->seq[j].k_len > mine[k].k_len || (ctl->seq[j].k_len == mine[k].k_len && j < i);
+        return PromptSeq{q0, max(0, q1 - q0), k0, max(0, k1 - k0)};
+    };
+    const bool few = x.n_seq <= 32;
+    if (few) {
+        if (warp == 0) {
+            PromptSeq mine{0, 0, 0, -1};
+            if (lane < x.n_seq) mine = seq_at(lane);
+            int rank = 0;
+            for (int j = 0; j < x.n_seq; ++j) {
+                const int other = __shfl_sync(0xffffffffu, mine.k_len, j);
+                rank += other > mine.k_len || (other == mine.k_len && j < lane);
+            }
+            if (lane < x.n_seq) ctl->seq[rank] = mine;
         }
+    } else {
+        for (int i = tid; i < x.n_seq; i += PA_THREADS) ctl->seq[i] = seq_at(i);
     }
     __syncthreads();
+    if (!ctl->member) {
+        if (ctl->slot < 0) wait_until_manned(p);
+        return;
+    }
+    if (!few) {
+        int rank[(PA_MAXSEQ + PA_THREADS - 1) / PA_THREADS];
+        PromptSeq mine[(PA_MAXSEQ + PA_THREADS - 1) / PA_THREADS];
 #pragma unroll
-    for (int k = 0; k < (PA_MAXSEQ + PA_THREADS - 1) / PA_THREADS; ++k)
-        if (rank[k] >= 0) ctl->seq[rank[k]] = mine[k];
-    __syncthreads();
+        for (int k = 0; k < (PA_MAXSEQ + PA_THREADS - 1) / PA_THREADS; ++k) {
+            const int i = tid + k * PA_THREADS;
+            rank[k] = -1;
+            if (i < x.n_seq) {
+                mine[k] = ctl->seq[i];
+                rank[k] = 0;
+                for (int j = 0; j < x.n_seq; ++j) rank[k] += ctl->seq[j].k_len > mine[k].k_len || (ctl->seq[j].k_len == mine[k].k_len && j < i);
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < (PA_MAXSEQ + PA_THREADS - 1) / PA_THREADS; ++k)
+            if (rank[k] >= 0) ctl->seq[rank[k]] = mine[k];
+        __syncthreads();
+    }
     if (warp == 0) {
         int sum = 0;
         for (int i0 = 0; i0 < x.n_seq; i0 += 32) {
@@ -251,15 +322,44 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         return true;
     };
 
+    // The softmax threads hold a row of 128 scores: 2 x 128 x 208 + 128 x 88 registers, as many as 384 x 168 at launch.
+    if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     if (warp == 9) {
-        // ------------------------------------------------ units from the queue, and their query rows
-        const int n_units_head = ctl->blocks_before[x.n_seq];
-        const int n_units = n_units_head * x.H_kv;
+        // ------------------------------------------------ units, and their query rows
+        // Unit i < b is the first one of the block in slot i, without asking anybody; the others come from the queue; at last the first units of
+        // planned SMs that never got a block (whose slots are then taken, so that the plan counts as manned).
+        const int n_units = ctl->blocks_before[x.n_seq] * x.H_kv;
         uint32_t nq[2] = {0, 0};
+        int phase = 0, scan = 0;
         for (uint32_t it = 0;; ++it) {
-            int u = 0;
-            if (lane == 0) u = pop_queue(&p.ctrl->die_head[0], p.epoch, n_units);
-            u = __shfl_sync(0xffffffffu, u, 0);
+            int u = -1;
+            if (phase == 0) {
+                phase = 1;
+                if (ctl->slot < n_units) u = ctl->slot;
+            }
+            if (u < 0 && phase == 1) {
+                if (n_units > p.b) {
+                    if (lane == 0) u = pop_queue(&p.ctrl->die_head[0], p.epoch, n_units - p.b);
+                    u = __shfl_sync(0xffffffffu, u, 0);
+                    if (u >= 0) u += p.b;
+                }
+                if (u < 0) phase = 2;
+            }
+            while (u < 0 && scan < p.b) {
+                const int i = scan + lane;
+                const unsigned open = __ballot_sync(0xffffffffu, i < p.b && !slot_taken(p, i));
+                if (!open) {
+                    scan += 32;
+                    continue;
+                }
+                const int slot = scan + __ffs(open) - 1;
+                int got = 0;
+                if (lane == 0) got = atomicMax(&p.claimed[slot], p.epoch) < p.epoch;
+                got = __shfl_sync(0xffffffffu, got, 0);
+                if (got && slot < n_units) u = slot;
+                scan = slot + 1;
+            }
             int seq = -1, head = 0, t0 = 0;
             if (u >= 0) {
                 const int e = u / x.H_kv;
@@ -286,12 +386,7 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                 mbar_arrive(smem_u32(&ctl->unit_full));
             }
             __syncwarp();
-            if (seq < 0) {
-                // whatever planned SM has not got a block yet is not needed any more: its slot is taken, so that the plan counts as manned
-                for (int i = lane; i < p.b; i += 32)
-                    if (!slot_taken(p, i)) atomicMax(&p.claimed[i], p.epoch);
-                break;
-            }
+            if (seq < 0) break;
             const PromptSeq s = ctl->seq[seq];
             for (int w = 0; w < 2; ++w) {
                 if (key_tiles(x, s, t0, w) == 0) continue;
@@ -363,7 +458,7 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
             const uint64_t t0 = globaltimer_ns();
             while (globaltimer_ns() - t0 < 2000000ull) __nanosleep(1000);
         }
-    } else if (warp == 8) {
+    } else {
         // ------------------------------------------------ MMA issuer (the warp runs converged, one elected lane issues)
         const uint64_t dk_t = make_smem_desc(0, 16, 1024, 2);                  // Q, K: K-major, 128-byte swizzle
         const uint64_t dv_t = make_smem_desc(0, PA_N * 128, 1024, 2);          // V: N-major, 64-column blocks 16 KB apart
@@ -459,7 +554,9 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
             }
             __syncwarp();
         }
+    }
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         // ------------------------------------------------ softmax and epilogue: thread = row of tile w = tensor-memory lane
         const int w = warp >> 2, r = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
@@ -496,11 +593,12 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                         for (int i = 0; i < 32; ++i)
                             if (c * 32 + i > rel) sv[c][i] = 0xff800000u;
                 }
-                float top = -INFINITY;
+                float top4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
+                for (int i = 0; i < 32; ++i)
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(sv[c][i]));
+                    for (int c = 0; c < 4; ++c) top4[c] = fmaxf(top4[c], __uint_as_float(sv[c][i]));
+                const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3]));
                 const bool grow = top > m && !((top - m) * x.scale_log2e <= PA_LAZY);
                 if (j == 0) {
                     m = top;
@@ -527,20 +625,31 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                     tmem_st_wait();
                 }
                 m_s = m == -INFINITY ? 0.f : m * x.scale_log2e;
-                float sum0 = 0.f, sum1 = 0.f;
+                f32x2 sum = pack2(0.f, 0.f);
+                const f32x2 scale2 = pack2(x.scale_log2e, x.scale_log2e), ref2 = pack2(-m_s, -m_s);
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     uint32_t pv[32];
 #pragma unroll
                     for (int i = 0; i < 32; ++i) {
-                        const float a = exp2_fast(fmaf(__uint_as_float(sv[half * 2 + (i >> 4)][(2 * i) & 31]), x.scale_log2e, -m_s));
-                        const float b = exp2_fast(fmaf(__uint_as_float(sv[half * 2 + (i >> 4)][(2 * i + 1) & 31]), x.scale_log2e, -m_s));
-                        sum0 += a;
-                        sum1 += b;
+                        float a = __uint_as_float(sv[half * 2 + (i >> 4)][(2 * i) & 31]), b = __uint_as_float(sv[half * 2 + (i >> 4)][(2 * i + 1) & 31]);
+                        f32x2 v = fma2(pack2(a, b), scale2, ref2);
+                        if (i % 8 >= 8 - PA_CUBIC) {
+                            v = exp2_cubic(v);
+                            unpack2(v, a, b);
+                        } else {
+                            unpack2(v, a, b);
+                            a = exp2_fast(a);
+                            b = exp2_fast(b);
+                            v = pack2(a, b);
+                        }
+                        sum = add2(sum, v);
                         pv[i] = bf16_pair(a, b);
                     }
                     tmem_st_32x32(t_s + half * 32, pv);
                 }
+                float sum0, sum1;
+                unpack2(sum, sum0, sum1);
                 l += sum0 + sum1;
                 tmem_st_wait();
                 tc_fence_before();

@@ -127,6 +127,18 @@ def test_foreign_values_never_enter():
     assert np.isnan(got[60:179, :4, 5]).all() and np.isfinite(got[50:60]).all() and np.isfinite(got[50:179, 4:]).all()
 
 
+def test_later_values_however_large_never_enter():
+    """The largest finite values in later tokens of the same sequence: a masked probability has to be zero, not nearly zero."""
+    n = 200
+    Q, K, V = rows(n, 8, 128, 30), rows(n, 2, 128, 31), rows(n, 2, 128, 32)
+    clean = run(Q, K, V, offsets([n]))
+    V2 = V.copy()
+    V2[150:] = 0x7F7F
+    V2[150:, 0, ::2] = 0xFF7F
+    got = run(Q, K, V2, offsets([n]))
+    assert np.array_equal(got[:150], clean[:150])
+
+
 def test_parts_of_a_fused_projection():
     n, Hq, Hkv, D = 150, 6, 2, 64
     qkv = rows(n, Hq + 2 * Hkv, D, 16)
@@ -153,8 +165,8 @@ def test_on_sm_budgets_and_again_and_again():
         check(got, *want)
         first = got if first is None else first
         assert np.array_equal(got, first)     # who computes a unit does not matter
-    plan = plan_for(20)
-    plan.set_grid(9)                          # fewer blocks than planned SMs: the queue is drained by those there are
+    plan = plan_for()
+    plan.set_grid(9)                          # fewer blocks than planned SMs (the whole chip: every block lands on one): they drain the queue
     got = run(Q, K, V, offsets(lens), plan=plan)
     plan.set_grid(0)
     assert np.array_equal(got, first)
