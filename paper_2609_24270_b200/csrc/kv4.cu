@@ -20,6 +20,17 @@ namespace ag {
 //
 // A block takes U times 128 / L neighbouring tokens of one head: the words of neighbouring V rows share sectors, and U rows a lane are in
 // flight together (a row's chain slot -> page -> row is some 2 us long: one row a lane moved 2.9 TB/s, four are bound by the memory).
+__device__ __forceinline__ uint32_t min_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+
 constexpr int KS_THREADS = 256;
 constexpr int KS_ROWS = 4;                           // U of large calls; small ones take 1, for more blocks
 
@@ -28,70 +39,73 @@ __global__ void __launch_bounds__(KS_THREADS) k_kv4_store(uint8_t* __restrict__ 
                                                           const uint16_t* __restrict__ V, long long n_tokens, long long k_stride, long long v_stride,
                                                           const int32_t* __restrict__ slot) {
     constexpr int L = D / 8, TOK = KS_THREADS / 2 / L;              // lanes of a row, tokens of the block side by side
-    const int l = threadIdx.x % L, which = threadIdx.x / L & 1;
+    const int l = threadIdx.x % L, which = threadIdx.x / 32 & 1;    // a warp has rows of K or rows of V
     const int head = blockIdx.x % H_kv;
-    const long long tok0 = (long long)(blockIdx.x / H_kv) * (TOK * U) + threadIdx.x / (2 * L);
-    const uint16_t* from = (which ? V : K) + head * D + l * 8;
+    const long long tok0 = (long long)(blockIdx.x / H_kv) * (TOK * U) + threadIdx.x / 64 * (32 / L) + threadIdx.x % 32 / L;
     const long long stride = which ? v_stride : k_stride;
+    const uint16_t* from = (which ? V : K) + head * D + l * 8 + tok0 * stride;
+    const int rest = (int)min(n_tokens - tok0, (long long)TOK * U);  // tokens of the block from this lane's first on
+    const int32_t* slots = slot + tok0;
     int at[U];
     uint4 raw[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const long long tok = tok0 + u * TOK;
-        at[u] = tok < n_tokens ? slot[tok] : -1;
-        if (at[u] >= n_slots) at[u] = -1;
+        at[u] = -1;
         raw[u] = make_uint4(0, 0, 0, 0);
-        if (tok < n_tokens) raw[u] = *reinterpret_cast<const uint4*>(from + tok * stride);
+        if (u * TOK < rest) {
+            at[u] = slots[u * TOK];
+            raw[u] = *reinterpret_cast<const uint4*>(from);
+        }
+        from += TOK * stride;
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const float x[8] = {bf16_lo(raw[u].x), bf16_hi(raw[u].x), bf16_lo(raw[u].y), bf16_hi(raw[u].y),
-                            bf16_lo(raw[u].z), bf16_hi(raw[u].z), bf16_lo(raw[u].w), bf16_hi(raw[u].w)};
-        float lo = x[0], hi = x[0], odd = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            lo = fminf(lo, x[i]);
-            hi = fmaxf(hi, x[i]);
-            odd = fmaf(x[i], 0.f, odd);                             // NaN as soon as one element is not finite
-        }
+        // extremes of the group, in pairs; NaN wins, and an infinity makes the range infinite or NaN
+        uint32_t lo2 = min_bf16x2(min_bf16x2(raw[u].x, raw[u].y), min_bf16x2(raw[u].z, raw[u].w));
+        uint32_t hi2 = max_bf16x2(max_bf16x2(raw[u].x, raw[u].y), max_bf16x2(raw[u].z, raw[u].w));
 #pragma unroll
         for (int o = 1; o < 4; o <<= 1) {
-            lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-            hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-            odd += __shfl_xor_sync(0xffffffffu, odd, o);
+            lo2 = min_bf16x2(lo2, __shfl_xor_sync(0xffffffffu, lo2, o));
+            hi2 = max_bf16x2(hi2, __shfl_xor_sync(0xffffffffu, hi2, o));
         }
-        const __nv_bfloat16 sb = __float2bfloat16_rn(__fdiv_rn(__fsub_rn(hi, lo), 15.f) + odd);
+        const float lo = bf16_lo(min_bf16x2(lo2, lo2 >> 16)), hi = bf16_lo(max_bf16x2(hi2, hi2 >> 16));
+        const __nv_bfloat16 sb = __float2bfloat16_rn(__fdiv_rn(__fsub_rn(hi, lo), 15.f));
         const float s = __bfloat162float(sb);
         const bool fine = s <= 3.4e38f;                             // false for NaN and infinity
+        // rint((x - lo) / s): the quotient from the correctly rounded reciprocal and one step on the exact remainder, which is the correctly
+        // rounded quotient (Markstein) while nothing over- or underflows; four codes are gathered as one number in base 16.
+        const uint32_t in[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
         uint32_t w = 0;
-        if (fine && s > 0.f) {
-            // rint((x - lo) / s) without dividing: a candidate c from the reciprocal, settled by the remainder x - lo - c s (exact: c has 4 bits, s
-            // has 8).  Near a border, half a step away from two codes, the quotient's own rounding decides, so it is taken as defined.
-            const float r = __frcp_rn(s), border = 0.4999f * s;
-            if (r <= 3.4e38f) {
+        if (s >= 0x1p-90f && s <= 0x1p100f) {
+            constexpr float M = 12582912.f;                         // 1.5 * 2^23: adding it rounds to an integer, halves to even
+            const float inv = __frcp_rn(s);
+            float number[2] = {0.f, 0.f};
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float d = __fsub_rn(x[i], lo), q = __fmaf_rn(d, r, 12582912.f);   // 1.5 * 2^23: the sum's low bits are the rounded quotient
-                    uint32_t c = __float_as_uint(q) & 15u;
-                    if (fabsf(__fmaf_rn(__fsub_rn(12582912.f, q), s, d)) > border) c = (uint32_t)min(15, __float2int_rn(__fdiv_rn(d, s)));
-                    w |= c << (4 * i);
-                }
-            } else {                                                // the smallest scales have no reciprocal in 32 bits
-#pragma unroll
-                for (int i = 0; i < 8; ++i) w |= (uint32_t)min(15, __float2int_rn(__fdiv_rn(__fsub_rn(x[i], lo), s))) << (4 * i);
+            for (int i = 7; i >= 0; --i) {
+                const float d = __fsub_rn(i & 1 ? bf16_hi(in[i >> 1]) : bf16_lo(in[i >> 1]), lo);
+                const float q1 = __fmul_rn(d, inv), q = __fmaf_rn(__fmaf_rn(-q1, s, d), inv, q1);
+                number[i >> 2] = __fmaf_rn(number[i >> 2], 16.f, __fsub_rn(__fadd_rn(q, M), M));
+            }
+            w = __byte_perm(__float_as_uint(number[0] + 8388608.f), __float_as_uint(number[1] + 8388608.f), 0x5410);
+        } else if (fine && s > 0.f) {
+#pragma unroll 1
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t two = i < 4 ? (i < 2 ? in[0] : in[1]) : (i < 6 ? in[2] : in[3]);
+                const float d = __fsub_rn(i & 1 ? bf16_hi(two) : bf16_lo(two), lo);
+                w |= (uint32_t)min(15, __float2int_rn(__fdiv_rn(d, s))) << (4 * i);
             }
         }
-        const uint32_t wt = kv4_transpose<D / 16, 2>(w, l >> 1);    // lanes of equal parity hold elements 16 i + 8 (l & 1) + j
-        if (at[u] < 0) continue;
+        if (which) w = kv4_transpose<D / 16, 2>(w, l >> 1);         // lanes of equal parity hold elements 16 i + 8 (l & 1) + j
+        if (at[u] < 0 || at[u] >= n_slots) continue;
         uint8_t* block = pages + ((size_t)(at[u] / KV4_PAGE) * H_kv + head) * kv4_head_bytes(D);
         const int r = at[u] % KV4_PAGE;
         if (which == 0) {
             *reinterpret_cast<uint32_t*>(block + kv4_k_word<D>(r, l >> 2, l & 3)) = w;
         } else if (D == 128) {
-            *reinterpret_cast<uint32_t*>(block + kv4_v_word<D>(r, l & 1, l >> 1)) = wt;
+            *reinterpret_cast<uint32_t*>(block + kv4_v_word<D>(r, l & 1, l >> 1)) = w;
         } else {
-            *reinterpret_cast<uint16_t*>(block + kv4_v_word<D>(r, l & 1, l >> 1)) = (uint16_t)wt;
-            *reinterpret_cast<uint16_t*>(block + kv4_v_word<D>(r, l & 1, 4 + (l >> 1))) = (uint16_t)(wt >> 16);
+            *reinterpret_cast<uint16_t*>(block + kv4_v_word<D>(r, l & 1, l >> 1)) = (uint16_t)w;
+            *reinterpret_cast<uint16_t*>(block + kv4_v_word<D>(r, l & 1, 4 + (l >> 1))) = (uint16_t)(w >> 16);
         }
         if ((l & 3) == 0) {
             const uint32_t nan = 0x7fc07fc0u;
@@ -106,17 +120,18 @@ __global__ void __launch_bounds__(KS_THREADS) k_kv4_load(const uint8_t* __restri
                                                          uint16_t* __restrict__ V, long long n_tokens, long long k_stride, long long v_stride,
                                                          const int32_t* __restrict__ slot) {
     constexpr int L = D / 8, TOK = KS_THREADS / 2 / L;
-    const int l = threadIdx.x % L, which = threadIdx.x / L & 1;
+    const int l = threadIdx.x % L, which = threadIdx.x / 32 & 1;    // a warp has rows of K or rows of V
     const int head = blockIdx.x % H_kv;
-    const long long tok0 = (long long)(blockIdx.x / H_kv) * (TOK * U) + threadIdx.x / (2 * L);
-    uint16_t* to = (which ? V : K) + head * D + l * 8;
+    const long long tok0 = (long long)(blockIdx.x / H_kv) * (TOK * U) + threadIdx.x / 64 * (32 / L) + threadIdx.x % 32 / L;
     const long long stride = which ? v_stride : k_stride;
+    uint16_t* to = (which ? V : K) + head * D + l * 8 + tok0 * stride;
+    const int rest = (int)min(n_tokens - tok0, (long long)TOK * U);
+    const int32_t* slots = slot + tok0;
     int at[U];
     uint32_t w[U], pair[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const long long tok = tok0 + u * TOK;
-        at[u] = tok < n_tokens ? slot[tok] : -1;
+        at[u] = u * TOK < rest ? slots[u * TOK] : -1;
         if (at[u] >= n_slots) at[u] = -1;
     }
 #pragma unroll
@@ -134,16 +149,21 @@ __global__ void __launch_bounds__(KS_THREADS) k_kv4_load(const uint8_t* __restri
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const uint32_t wt = kv4_transpose<D / 16, 2>(w[u], l >> 1), c = which ? wt : w[u];
+        uint32_t c = w[u];
+        if (which) c = kv4_transpose<D / 16, 2>(c, l >> 1);
+        uint16_t* row = to;
+        to += TOK * stride;
         if (at[u] < 0) continue;
-        uint32_t out[4];
+        // two elements at a time, i and i + 4: bf16 0x4300 | u is 128 + u; u and s u + b in bf16, the latter rounded once
+        const uint32_t s2 = __byte_perm(pair[u], 0, 0x1010), b2 = __byte_perm(pair[u], 0, 0x3232);
+        uint32_t v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const __nv_bfloat162 v = __floats2bfloat162_rn(fmaf((float)((c >> (8 * i)) & 15u), bf16_lo(pair[u]), bf16_hi(pair[u])),
-                                                           fmaf((float)((c >> (8 * i + 4)) & 15u), bf16_lo(pair[u]), bf16_hi(pair[u])));
-            out[i] = *reinterpret_cast<const uint32_t*>(&v);
+            const uint32_t c128 = ((c >> (4 * i)) & 0x000f000fu) | 0x43004300u;
+            asm("{\n .reg .b32 t;\n add.rn.bf16x2 t, %1, %2;\n fma.rn.bf16x2 %0, t, %3, %4;\n}" : "=r"(v[i]) : "r"(c128), "r"(0xC300C300u), "r"(s2), "r"(b2));
         }
-        *reinterpret_cast<uint4*>(to + (tok0 + u * TOK) * stride) = make_uint4(out[0], out[1], out[2], out[3]);
+        uint32_t out[4] = {__byte_perm(v[0], v[1], 0x5410), __byte_perm(v[2], v[3], 0x5410), __byte_perm(v[0], v[1], 0x7632), __byte_perm(v[2], v[3], 0x7632)};
+        *reinterpret_cast<uint4*>(row) = make_uint4(out[0], out[1], out[2], out[3]);
     }
 }
 

@@ -19,11 +19,11 @@ __host__ __device__ constexpr int kv4_head_bytes(int D) { return 80 * D; }
 // byte offset, inside a head's block, of the codes of token `tok` for lane part (g of the operand, t) and of its scales
 template <int D>
 __device__ __forceinline__ int kv4_k_word(int tok, int grp, int t) {         // elements 32 grp + 8 t + 0 .. 7 of K: one word
-    return (tok >> 4) * 8 * D + ((tok >> 3) & 1) * 4 * D + (4 * (tok & 7) + t) * (D / 8) + 4 * grp;
+    return tok * (D / 2) + t * (D / 8) + 4 * grp;                            // = (tok / 16) 8 D + (tok / 8 % 2) 4 D + (4 (tok % 8) + t) D / 8 + 4 grp
 }
 template <int D>
 __device__ __forceinline__ int kv4_v_word(int tok, int hi, int g) {          // elements 16 i + 8 hi + g of V, all i: D / 32 bytes
-    return 32 * D + (tok >> 4) * 8 * D + ((tok >> 3) & 1) * 4 * D + (4 * g + ((tok & 7) >> 1)) * (D / 8) + (tok & 1) * (D / 16) + hi * (D / 32);
+    return 32 * D + (tok >> 3) * 4 * D + (4 * g + ((tok >> 1) & 3)) * (D / 8) + (tok & 1) * (D / 16) + hi * (D / 32);
 }
 template <int D>
 __device__ __forceinline__ int kv4_scale_word(int which, int tok, int grp) { // (scale, base) as a pair of bf16
