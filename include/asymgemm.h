@@ -704,8 +704,7 @@ ag_status ag_kv4_compact(const ag_kv4_pool* pool, const ag_kv4_table* table, int
  *   Q, O       device, [B][H_q][D] bf16, 16-byte aligned; H_q a multiple of H_kv, H_q / H_kv <= 1024
  *   row        device [B], or NULL for row b (then B <= table->n_rows); a row outside the table, or an empty one, gives zeros
  *   table      lengths are clamped to 0 .. 64 max_pages; tokens whose page is not one of the pool's are left out
- *   workspace  device, 16-byte aligned, ag_attention_decode_kv4_workspace bytes (at most about 40 MB, and 8 bytes per request and KV
- *              head).  Its contents mean nothing between calls; calls that may run at the same time need one each
+ *   workspace  device, 16-byte aligned, ag_attention_decode_kv4_workspace bytes (at most about 25 MB).  Its contents mean nothing between calls; calls that may run at the same time need one each
  * Asynchronous on cuda_stream, may be captured into a graph (lengths and tables are read when it runs).  The work is split by
  * the shape and the lengths of the whole batch, nothing else, so results are reproducible bit for bit; a request's bits may change with
  * the other requests of its batch.

@@ -42,7 +42,7 @@ struct DecodeKv4Args {
     const int32_t *page_of, *len, *row;
     float4* part;                 // [slots][NB][D / 16][32 lanes]: unnormalised outputs in fragment order; slots: 2 per warp, 2 per block
     float2* stats;                // [slots][8 NB]: maximum (in units of log2), sum
-    int2* pieces;                 // [units]: first block of the unit, number of blocks
+    int2* crossing;               // [blocks]: the unit that begins in the block and goes on beyond it (-1: none), the blocks that it has
     int B, n_pages, H_kv, G, n_rows, max_pages, h_blocks, n_blocks;
     int aligned;                  // 1: block = unit (short rows, few units)
     float scale_log2e;
@@ -141,10 +141,12 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ long long before[DK_THREADS + 1];   // pages (of one KV head) in front of the share of requests that thread i counts
     __shared__ long long warp_sum[DK_WARPS];
+    __shared__ int tokens_of[DK_THREADS], row_of[DK_THREADS];      // of the requests, up to DK_THREADS of them
     __shared__ int slot_unit[2 * DK_WARPS];        // units that a warp has only a part of: one that began before its run, one that goes on behind it
     __shared__ int slot_ends[2 * DK_WARPS];        // the part includes the unit's last page
     __shared__ WarpWalk walk[DK_WARPS];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    dep_wait();
     dep_release();
 
     // ---- this block's run, cut into the warps' runs: places of the line of pages; order: request, KV head (and block of query heads), page
@@ -168,7 +170,15 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
         }
     } else {
         long long n = 0;
-        for (int i = threadIdx.x * per, e = min(x.B, i + per), r; i < e; ++i) n += pages_of(row_tokens(x, i, &r));
+        if (per == 1) {
+            int r = 0, tokens = 0;
+            if ((int)threadIdx.x < x.B) tokens = row_tokens(x, threadIdx.x, &r);
+            tokens_of[threadIdx.x] = tokens;
+            row_of[threadIdx.x] = r;
+            n = pages_of(tokens);
+        } else {
+            for (int i = threadIdx.x * per, e = min(x.B, i + per), r; i < e; ++i) n += pages_of(row_tokens(x, i, &r));
+        }
         long long inc = n;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -185,12 +195,20 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
         __syncthreads();
         total = before[DK_THREADS] * heads;
         n_blocks = (int)min((long long)x.n_blocks, (total + DK_WARPS - 1) / DK_WARPS);      // at least a page for every warp
-        if ((int)blockIdx.x >= n_blocks) return;
+        if ((int)blockIdx.x >= n_blocks) {
+            if (threadIdx.x == 0) x.crossing[blockIdx.x] = make_int2(-1, 0);
+            return;
+        }
         block_begin = total * blockIdx.x / n_blocks;
         block_end = total * (blockIdx.x + 1) / n_blocks;
         b = 0;
         len = np = row = 0;
     }
+    auto request = [&](int i, int* r) {            // tokens and row of request i (not in aligned launches)
+        if (per > 1) return row_tokens(x, i, r);
+        *r = row_of[i];
+        return tokens_of[i];
+    };
     if (threadIdx.x < 2 * DK_WARPS) slot_unit[threadIdx.x] = -1;
     __syncthreads();
     const long long begin = block_begin + (block_end - block_begin) * warp / DK_WARPS;
@@ -232,7 +250,7 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
         b = lo * per;
         long long in_front = before[lo];
         while (true) {
-            len = row_tokens(x, b, &row);
+            len = request(b, &row);
             np = pages_of(len);
             if (in_front + np > at) break;
             in_front += np;
@@ -335,49 +353,47 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
                 const uint32_t e = min(246u, 261u - (__float_as_uint(top) >> 23));        // exponent field of c
                 const float c = __uint_as_float(e << 23);
-                uint32_t sums[NG][3], adds[NG][3];         // parts, as bf16 bits
+                float even[NG], odd[NG];
 #pragma unroll
                 for (int grp = 0; grp < NG; ++grp) {
-                    float even = 0.f, odd = 0.f;
+                    even[grp] = odd[grp] = 0.f;
 #pragma unroll
                     for (int i = 0; i < 8; i += 2) {
                         q[grp][i] *= c;
                         q[grp][i + 1] *= c;
-                        even += q[grp][i];
-                        odd += q[grp][i + 1];
+                        even[grp] += q[grp][i];
+                        odd[grp] += q[grp][i + 1];
                     }
 #pragma unroll
                     for (int i = 0; i < 4; ++i) qf[nb][grp][i] = pack_f16(q[grp][i], q[grp][i + 4]);
 #pragma unroll
                     for (int w = 1; w < 4; w <<= 1) {
-                        even += __shfl_xor_sync(0xffffffffu, even, w);
-                        odd += __shfl_xor_sync(0xffffffffu, odd, w);
+                        even[grp] += __shfl_xor_sync(0xffffffffu, even[grp], w);
+                        odd[grp] += __shfl_xor_sync(0xffffffffu, odd[grp], w);
                     }
-                    float sum = even + odd, add = -1024.f * even - 64.f * odd;
+                }
+                // D = 128: k = 2 t, 2 t + 1 are groups 2 (t & 1), + 1 of part t / 2, k + 8 part 2 of them (t < 2); D = 64: both groups, part t
+                const bool upper = D == 128 && (t & 1);
+                const int part = D == 128 ? t >> 1 : t;
+                uint32_t sums[3], adds[3];                 // the lane's two groups, bf16 side by side
+                {
+                    const float e0 = upper ? even[NG - 2] : even[0], e1 = upper ? even[NG - 1] : even[1];
+                    const float o0 = upper ? odd[NG - 2] : odd[0], o1 = upper ? odd[NG - 1] : odd[1];
+                    float s0 = e0 + o0, s1 = e1 + o1, a0 = -1024.f * e0 - 64.f * o0, a1 = -1024.f * e1 - 64.f * o1;
 #pragma unroll
                     for (int k = 0; k < 3; ++k) {
-                        const __nv_bfloat16 a = __float2bfloat16_rn(sum), d = __float2bfloat16_rn(add);
-                        sums[grp][k] = __bfloat16_as_ushort(a);
-                        adds[grp][k] = __bfloat16_as_ushort(d);
-                        sum -= __bfloat162float(a);
-                        add -= __bfloat162float(d);
+                        sums[k] = pack_bf16(s0, s1);
+                        adds[k] = pack_bf16(a0, a1);
+                        s0 -= bf16_lo(sums[k]);
+                        s1 -= bf16_hi(sums[k]);
+                        a0 -= bf16_lo(adds[k]);
+                        a1 -= bf16_hi(adds[k]);
                     }
                 }
-                if (D == 128) {      // k = 2 t, 2 t + 1: groups 2 (t & 1), + 1 of part t / 2; k + 8: of part 2 (t < 2)
-                    const int lo = 0, hi = NG - 2;
-                    const uint32_t s0 = t < 2 ? sums[lo][0] | sums[lo + 1][0] << 16 : sums[lo][1] | sums[lo + 1][1] << 16;
-                    const uint32_t s1 = t < 2 ? sums[hi][0] | sums[hi + 1][0] << 16 : sums[hi][1] | sums[hi + 1][1] << 16;
-                    const uint32_t a0 = t < 2 ? adds[lo][0] | adds[lo + 1][0] << 16 : adds[lo][1] | adds[lo + 1][1] << 16;
-                    const uint32_t a1 = t < 2 ? adds[hi][0] | adds[hi + 1][0] << 16 : adds[hi][1] | adds[hi + 1][1] << 16;
-                    qb[nb][0] = (t & 1) ? s1 : s0;
-                    qs[nb][0] = (t & 1) ? a1 : a0;
-                    qb[nb][1] = t >= 2 ? 0u : (t & 1) ? sums[hi][2] | sums[hi + 1][2] << 16 : sums[lo][2] | sums[lo + 1][2] << 16;
-                    qs[nb][1] = t >= 2 ? 0u : (t & 1) ? adds[hi][2] | adds[hi + 1][2] << 16 : adds[lo][2] | adds[lo + 1][2] << 16;
-                } else {             // both groups, part t
-                    qb[nb][0] = t == 0 ? sums[0][0] | sums[1][0] << 16 : t == 1 ? sums[0][1] | sums[1][1] << 16 : t == 2 ? sums[0][2] | sums[1][2] << 16 : 0u;
-                    qs[nb][0] = t == 0 ? adds[0][0] | adds[1][0] << 16 : t == 1 ? adds[0][1] | adds[1][1] << 16 : t == 2 ? adds[0][2] | adds[1][2] << 16 : 0u;
-                    qb[nb][1] = qs[nb][1] = 0u;
-                }
+                qb[nb][0] = part == 0 ? sums[0] : part == 1 ? sums[1] : part == 2 ? sums[2] : 0u;
+                qs[nb][0] = part == 0 ? adds[0] : part == 1 ? adds[1] : part == 2 ? adds[2] : 0u;
+                qb[nb][1] = D == 128 && t < 2 ? sums[2] : 0u;
+                qs[nb][1] = D == 128 && t < 2 ? adds[2] : 0u;
                 const float f = x.scale_log2e * __uint_as_float((254u - e) << 23);
                 unscale[nb][0] = __shfl_sync(0xffffffffu, f, 8 * t);
                 unscale[nb][1] = __shfl_sync(0xffffffffu, f, 8 * t + 4);
@@ -466,7 +482,7 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
                     hn = 0;
                     do {
                         ++bn;
-                        ln = row_tokens(x, bn, &rn);
+                        ln = request(bn, &rn);
                         np = pages_of(ln);
                     } while (np == 0);
                     id_first = -64;
@@ -640,18 +656,19 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
             const int unit = at->now_unit;
             if (whole && ends) {
                 write_unit(unit);
-                if (!x.aligned && lane == 0) x.pieces[unit] = make_int2(blockIdx.x, 1);
             } else {
                 const int slot = 2 * warp + (whole ? 1 : 0);
                 write_part(2 * DK_WARPS * (size_t)blockIdx.x + slot);
                 if (lane == 0) {
                     slot_unit[slot] = unit;
                     slot_ends[slot] = ends;
-                    if (whole && !x.aligned) {
-                        const int last = run_holding(at->now_begin + at->now_pages - 1, total, n_blocks);
-                        x.pieces[unit] = make_int2(blockIdx.x, last - (int)blockIdx.x + 1);
-                    }
                 }
+            }
+            if (left == 0 && warp == DK_WARPS - 1 && lane == 0 && !x.aligned) {      // the block's last page (no warp behind this one's has any)
+                int2 cross = make_int2(-1, 0);
+                if (!ends && at->now_begin >= block_begin)
+                    cross = make_int2(unit, run_holding(at->now_begin + at->now_pages - 1, total, n_blocks) - (int)blockIdx.x + 1);
+                x.crossing[blockIdx.x] = cross;
             }
             whole = true;                          // whatever comes next begins in this warp's run
         }
@@ -707,20 +724,24 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
     }
 }
 
-// One block per unit, thread (j, y): fragment j of the output, parts y, y + blockDim.y, ...:  O = sum_c 2^(m_c - m) O_c / sum_c 2^(m_c - m) l_c.
-// A part without a key that counts has m_c = -inf, l_c = 0 and is left out; requests without keys get zeros.
+// Block i joins the unit that began in block i of the main kernel and went on beyond it, thread (j, y): fragment j of the output, parts y,
+// y + blockDim.y, ...:  O = sum_c 2^(m_c - m) O_c / sum_c 2^(m_c - m) l_c.  A part without a key that counts has m_c = -inf, l_c = 0 and is left out.
+// Requests without keys get their zeros here too.
 template <int D, int NB>
 __global__ void __launch_bounds__(NB * D * 2 * dk_join_lanes(D, NB)) k_attn_join_kv4(const DecodeKv4Args x) {
     constexpr int MT = D / 16, NF = NB * MT * 32, LANES = dk_join_lanes(D, NB);
     __shared__ float4 acc[LANES - 1][NF];
     __shared__ float4 stat[LANES - 1][NF];
     dep_wait();
-    const int heads = x.H_kv * x.h_blocks, b = blockIdx.x / heads, hh = blockIdx.x - b * heads;
     const int j = threadIdx.x, y = threadIdx.y, lane = j & 31, g = lane >> 2, t = lane & 3, i = (j >> 5) % MT, nb = (j >> 5) / MT;
-    int row;
-    const bool empty = row_tokens(x, b, &row) == 0;
-    const int2 pc = empty ? make_int2(0, 0) : x.pieces[blockIdx.x];
-    if (pc.y == 1) return;                         // written already
+    const int2 pc = x.crossing[blockIdx.x];
+    for (int r, b = blockIdx.x; b < x.B; b += gridDim.x)
+        if (row_tokens(x, b, &r) == 0) {
+            uint4* out = reinterpret_cast<uint4*>(x.O + (size_t)b * x.H_kv * x.G * D);
+            for (int k = y * blockDim.x + j; k < x.H_kv * x.G * D / 8; k += blockDim.x * blockDim.y) out[k] = make_uint4(0, 0, 0, 0);
+        }
+    if (pc.x < 0) return;
+    const int heads = x.H_kv * x.h_blocks, b = pc.x / heads, hh = pc.x - b * heads;
     const int head = hh % x.h_blocks * 8 * NB + nb * 8 + 2 * t;
     float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -734,7 +755,7 @@ __global__ void __launch_bounds__(NB * D * 2 * dk_join_lanes(D, NB)) k_attn_join
         v.w = weighted(f1, v.w, g1, u.w);
     };
     if (head < x.G) {
-        auto slot = [&](int c) { return 2 * DK_WARPS * (size_t)x.n_blocks + 2 * (size_t)(pc.x + c) + (c == 0 ? 1 : 0); };
+        auto slot = [&](int c) { return 2 * DK_WARPS * (size_t)x.n_blocks + 2 * (size_t)(blockIdx.x + c) + (c == 0 ? 1 : 0); };
 #pragma unroll 4
         for (int c = y; c < pc.y; c += blockDim.y) {
             const float4 st = __ldcg(reinterpret_cast<const float4*>(&x.stats[slot(c) * 8 * NB + nb * 8 + 2 * t]));
@@ -790,7 +811,7 @@ using namespace ag;
 extern "C" size_t ag_attention_decode_kv4_workspace(int B, int H_q, int H_kv, int D, int max_pages) {
     DecodeKv4Shape s;
     if (!decode_kv4_shape(B, H_q, H_kv, D, max_pages, &s)) return 0;
-    return s.slots() * 8 * s.nb * D * sizeof(float) + align256(s.slots() * 8 * s.nb * sizeof(float2)) + s.units * sizeof(int2);
+    return s.slots() * 8 * s.nb * D * sizeof(float) + align256(s.slots() * 8 * s.nb * sizeof(float2)) + (size_t)s.n_blocks * sizeof(int2);
 }
 
 extern "C" ag_status attention_decode_kv4(const void* Q, const ag_kv4_pool* pool, const ag_kv4_table* table, const int32_t* row, void* O, int B, int H_q,
@@ -814,7 +835,7 @@ extern "C" ag_status attention_decode_kv4(const void* Q, const ag_kv4_pool* pool
     x.page_of = table->page_of; x.len = table->len; x.row = row;
     x.part = (float4*)workspace;
     x.stats = (float2*)((uint8_t*)workspace + s.slots() * 8 * s.nb * pool->D * sizeof(float));
-    x.pieces = (int2*)((uint8_t*)x.stats + align256(s.slots() * 8 * s.nb * sizeof(float2)));
+    x.crossing = (int2*)((uint8_t*)x.stats + align256(s.slots() * 8 * s.nb * sizeof(float2)));
     x.B = B; x.n_pages = (int)pool->n_pages; x.H_kv = pool->H_kv; x.G = H_q / pool->H_kv;
     x.n_rows = table->n_rows; x.max_pages = table->max_pages; x.h_blocks = s.h_blocks;
     x.n_blocks = s.n_blocks; x.aligned = s.aligned;
@@ -830,21 +851,23 @@ extern "C" ag_status attention_decode_kv4(const void* Q, const ag_kv4_pool* pool
         return e;                                  // D = 64 needs 40 KB, which every kernel may have
     });
     if (attr_err != cudaSuccess) return cuda_fail(attr_err);
-    kernel<<<(unsigned)s.n_blocks, DK_THREADS, pool->D == 128 ? dk_smem_bytes<128>() : dk_smem_bytes<64>(), stream>>>(x);
-    AG_CUDA(cudaGetLastError());
-    count_launch();
-    if (s.aligned) return AG_OK;
-    cudaLaunchConfig_t cfg;
-    memset(&cfg, 0, sizeof cfg);
-    cfg.gridDim = dim3((unsigned)s.units);
-    // a unit has about n_blocks / units parts: added side by side where that is many, one after the other where units are many
-    cfg.blockDim = dim3(s.nb * pool->D * 2, s.units >= 2 * 148 ? 1 : dk_join_lanes(pool->D, s.nb));
-    cfg.stream = stream;
+    // both launches may come up while the one before them on the stream finishes, and wait for it on the device
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof cfg);
+    cfg.gridDim = dim3((unsigned)s.n_blocks);
+    cfg.blockDim = dim3(DK_THREADS);
+    cfg.dynamicSmemBytes = pool->D == 128 ? dk_smem_bytes<128>() : dk_smem_bytes<64>();
+    cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
+    AG_CUDA(cudaLaunchKernelEx(&cfg, kernel, x));
+    count_launch();
+    if (s.aligned) return AG_OK;
+    cfg.blockDim = dim3(s.nb * pool->D * 2, dk_join_lanes(pool->D, s.nb));
+    cfg.dynamicSmemBytes = 0;
     AG_CUDA(cudaLaunchKernelEx(&cfg, join, x));
     count_launch();
     return AG_OK;

@@ -158,5 +158,5 @@ def test_refusals_of_the_decode_attention():
         assert L.attention_decode_kv4(*{**good, **change}.values()) == ag.AG_ERR_ARG, change
     assert L.attention_decode_kv4(*{**good, "B": 0}.values()) == ag.AG_OK
     # parts of 8 heads, two a warp and two a block, 2 * 148 blocks at most; shapes that are refused have size 0
-    assert ag.attention_decode_kv4_workspace(1000, 32, 8, 128, 1000) == 18 * 2 * 148 * 8 * (128 * 4 + 8) + 1000 * 8 * 8
+    assert ag.attention_decode_kv4_workspace(1000, 32, 8, 128, 1000) == 18 * 2 * 148 * 8 * (128 * 4 + 8) + 2 * 148 * 8
     assert ag.attention_decode_kv4_workspace(2, 7, 2, 128, 1000) == 0 and ag.attention_decode_kv4_workspace(2, 8, 2, 96, 1000) == 0
