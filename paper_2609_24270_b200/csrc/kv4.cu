@@ -15,11 +15,12 @@ namespace ag {
 // rounded one, so that the rounding costs at most 2^-9 of a step.  All in 32 bits with IEEE rounding: the codes do not depend on the kernel.
 // A group with a value that is not finite, or whose range is not, stands for NaN throughout.
 //
-// D / 8 lanes hold a row (eight elements, one 16-byte load each); a lane's eight K codes are one word of the page, the V codes
-// are transposed across lanes (kv4_transpose) so that a lane writes whole words of the fragment order as well.
+// D / 16 lanes hold a row, sixteen elements each: a lane's K codes are two words of the page, the V codes are transposed across lanes
+// (kv4_transpose) so that a lane writes whole words of the fragment order as well.  With eight elements a lane the part of the work that goes by
+// lanes (addresses, scales, exchanges) took twice as long: 86 and 51 us for 46k tokens x 8 heads, bound by instructions.
 //
 // A block takes U times 128 / L neighbouring tokens of one head: the words of neighbouring V rows share sectors, and U rows a lane are in
-// flight together (a row's chain slot -> page -> row is some 2 us long: one row a lane moved 2.9 TB/s, four are bound by the memory).
+// flight together (a row's chain slot -> page -> row is some 2 us long).
 __device__ __forceinline__ uint32_t min_bf16x2(uint32_t a, uint32_t b) {
     uint32_t r;
     asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
@@ -32,85 +33,93 @@ __device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
 }
 
 constexpr int KS_THREADS = 256;
-constexpr int KS_ROWS = 4;                           // U of large calls; small ones take 1, for more blocks
+constexpr int KS_ROWS = 2;                           // U of large calls; small ones take 1, for more blocks
 
 template <int D, int U>
 __global__ void __launch_bounds__(KS_THREADS) k_kv4_store(uint8_t* __restrict__ pages, long long n_slots, int H_kv, const uint16_t* __restrict__ K,
                                                           const uint16_t* __restrict__ V, long long n_tokens, long long k_stride, long long v_stride,
                                                           const int32_t* __restrict__ slot) {
-    constexpr int L = D / 8, TOK = KS_THREADS / 2 / L;              // lanes of a row, tokens of the block side by side
+    constexpr int L = D / 16, TOK = KS_THREADS / 2 / L;             // lanes of a row, tokens of the block side by side
     const int l = threadIdx.x % L, which = threadIdx.x / 32 & 1;    // a warp has rows of K or rows of V
     const int head = blockIdx.x % H_kv;
     const long long tok0 = (long long)(blockIdx.x / H_kv) * (TOK * U) + threadIdx.x / 64 * (32 / L) + threadIdx.x % 32 / L;
     const long long stride = which ? v_stride : k_stride;
-    const uint16_t* from = (which ? V : K) + head * D + l * 8 + tok0 * stride;
+    const uint16_t* from = (which ? V : K) + head * D + l * 16 + tok0 * stride;
     const int rest = (int)min(n_tokens - tok0, (long long)TOK * U);  // tokens of the block from this lane's first on
     const int32_t* slots = slot + tok0;
     int at[U];
-    uint4 raw[U];
+    uint4 raw[U][2];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         at[u] = -1;
-        raw[u] = make_uint4(0, 0, 0, 0);
+        raw[u][0] = raw[u][1] = make_uint4(0, 0, 0, 0);
         if (u * TOK < rest) {
             at[u] = slots[u * TOK];
-            raw[u] = *reinterpret_cast<const uint4*>(from);
+            raw[u][0] = reinterpret_cast<const uint4*>(from)[0];
+            raw[u][1] = reinterpret_cast<const uint4*>(from)[1];
         }
         from += TOK * stride;
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
+        const uint32_t in[8] = {raw[u][0].x, raw[u][0].y, raw[u][0].z, raw[u][0].w, raw[u][1].x, raw[u][1].y, raw[u][1].z, raw[u][1].w};
         // extremes of the group, in pairs; NaN wins, and an infinity makes the range infinite or NaN
-        uint32_t lo2 = min_bf16x2(min_bf16x2(raw[u].x, raw[u].y), min_bf16x2(raw[u].z, raw[u].w));
-        uint32_t hi2 = max_bf16x2(max_bf16x2(raw[u].x, raw[u].y), max_bf16x2(raw[u].z, raw[u].w));
+        uint32_t lo2 = in[0], hi2 = in[0];
 #pragma unroll
-        for (int o = 1; o < 4; o <<= 1) {
-            lo2 = min_bf16x2(lo2, __shfl_xor_sync(0xffffffffu, lo2, o));
-            hi2 = max_bf16x2(hi2, __shfl_xor_sync(0xffffffffu, hi2, o));
+        for (int i = 1; i < 8; ++i) {
+            lo2 = min_bf16x2(lo2, in[i]);
+            hi2 = max_bf16x2(hi2, in[i]);
         }
+        lo2 = min_bf16x2(lo2, __shfl_xor_sync(0xffffffffu, lo2, 1));
+        hi2 = max_bf16x2(hi2, __shfl_xor_sync(0xffffffffu, hi2, 1));
         const float lo = bf16_lo(min_bf16x2(lo2, lo2 >> 16)), hi = bf16_lo(max_bf16x2(hi2, hi2 >> 16));
         const __nv_bfloat16 sb = __float2bfloat16_rn(__fdiv_rn(__fsub_rn(hi, lo), 15.f));
         const float s = __bfloat162float(sb);
         const bool fine = s <= 3.4e38f;                             // false for NaN and infinity
         // rint((x - lo) / s): the quotient from the correctly rounded reciprocal and one step on the exact remainder, which is the correctly
         // rounded quotient (Markstein) while nothing over- or underflows; four codes are gathered as one number in base 16.
-        const uint32_t in[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
-        uint32_t w = 0;
+        uint32_t w[2] = {0, 0};
         if (s >= 0x1p-90f && s <= 0x1p100f) {
             constexpr float M = 12582912.f;                         // 1.5 * 2^23: adding it rounds to an integer, halves to even
             const float inv = __frcp_rn(s);
-            float number[2] = {0.f, 0.f};
+            float number[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int i = 7; i >= 0; --i) {
+            for (int i = 15; i >= 0; --i) {
                 const float d = __fsub_rn(i & 1 ? bf16_hi(in[i >> 1]) : bf16_lo(in[i >> 1]), lo);
                 const float q1 = __fmul_rn(d, inv), q = __fmaf_rn(__fmaf_rn(-q1, s, d), inv, q1);
                 number[i >> 2] = __fmaf_rn(number[i >> 2], 16.f, __fsub_rn(__fadd_rn(q, M), M));
             }
-            w = __byte_perm(__float_as_uint(number[0] + 8388608.f), __float_as_uint(number[1] + 8388608.f), 0x5410);
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                w[k] = __byte_perm(__float_as_uint(number[2 * k] + 8388608.f), __float_as_uint(number[2 * k + 1] + 8388608.f), 0x5410);
         } else if (fine && s > 0.f) {
-#pragma unroll 1
-            for (int i = 0; i < 8; ++i) {
-                const uint32_t two = i < 4 ? (i < 2 ? in[0] : in[1]) : (i < 6 ? in[2] : in[3]);
-                const float d = __fsub_rn(i & 1 ? bf16_hi(two) : bf16_lo(two), lo);
-                w |= (uint32_t)min(15, __float2int_rn(__fdiv_rn(d, s))) << (4 * i);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float d = __fsub_rn(i & 1 ? bf16_hi(in[i >> 1]) : bf16_lo(in[i >> 1]), lo);
+                w[i >> 3] |= (uint32_t)min(15, __float2int_rn(__fdiv_rn(d, s))) << (4 * (i & 7));
             }
         }
-        if (which) w = kv4_transpose<D / 16, 2>(w, l >> 1);         // lanes of equal parity hold elements 16 i + 8 (l & 1) + j
+        if (which) {                                                // lane l has elements 16 l + 8 j + g, word j: then word j holds elements 16 i + 8 j + l
+            w[0] = kv4_transpose<D / 16, 1>(w[0], l);
+            w[1] = kv4_transpose<D / 16, 1>(w[1], l);
+        }
         if (at[u] < 0 || at[u] >= n_slots) continue;
         uint8_t* block = pages + ((size_t)(at[u] / KV4_PAGE) * H_kv + head) * kv4_head_bytes(D);
         const int r = at[u] % KV4_PAGE;
         if (which == 0) {
-            *reinterpret_cast<uint32_t*>(block + kv4_k_word<D>(r, l >> 2, l & 3)) = w;
+            uint8_t* to = block + kv4_k_word<D>(r, l >> 1, 2 * (l & 1));
+            *reinterpret_cast<uint32_t*>(to) = w[0];
+            *reinterpret_cast<uint32_t*>(to + D / 8) = w[1];
         } else if (D == 128) {
-            *reinterpret_cast<uint32_t*>(block + kv4_v_word<D>(r, l & 1, l >> 1)) = w;
+            *reinterpret_cast<uint2*>(block + kv4_v_word<D>(r, 0, l)) = make_uint2(w[0], w[1]);
         } else {
-            *reinterpret_cast<uint16_t*>(block + kv4_v_word<D>(r, l & 1, l >> 1)) = (uint16_t)w;
-            *reinterpret_cast<uint16_t*>(block + kv4_v_word<D>(r, l & 1, 4 + (l >> 1))) = (uint16_t)(w >> 16);
+            *reinterpret_cast<uint32_t*>(block + kv4_v_word<D>(r, 0, l)) = __byte_perm(w[0], w[1], 0x5410);
+            *reinterpret_cast<uint32_t*>(block + kv4_v_word<D>(r, 0, 4 + l)) = __byte_perm(w[0], w[1], 0x7632);
         }
-        if ((l & 3) == 0) {
+        if ((l & 1) == 0) {
             const uint32_t nan = 0x7fc07fc0u;
             const uint32_t pair = (uint32_t)__bfloat16_as_ushort(sb) | (__float_as_uint(lo) & 0xffff0000u);
-            *reinterpret_cast<uint32_t*>(block + kv4_scale_word<D>(which, r, l >> 2)) = fine ? pair : nan;
+            *reinterpret_cast<uint32_t*>(block + kv4_scale_word<D>(which, r, l >> 1)) = fine ? pair : nan;
         }
     }
 }
@@ -119,16 +128,16 @@ template <int D, int U>
 __global__ void __launch_bounds__(KS_THREADS) k_kv4_load(const uint8_t* __restrict__ pages, long long n_slots, int H_kv, uint16_t* __restrict__ K,
                                                          uint16_t* __restrict__ V, long long n_tokens, long long k_stride, long long v_stride,
                                                          const int32_t* __restrict__ slot) {
-    constexpr int L = D / 8, TOK = KS_THREADS / 2 / L;
+    constexpr int L = D / 16, TOK = KS_THREADS / 2 / L;
     const int l = threadIdx.x % L, which = threadIdx.x / 32 & 1;    // a warp has rows of K or rows of V
     const int head = blockIdx.x % H_kv;
     const long long tok0 = (long long)(blockIdx.x / H_kv) * (TOK * U) + threadIdx.x / 64 * (32 / L) + threadIdx.x % 32 / L;
     const long long stride = which ? v_stride : k_stride;
-    uint16_t* to = (which ? V : K) + head * D + l * 8 + tok0 * stride;
+    uint16_t* to = (which ? V : K) + head * D + l * 16 + tok0 * stride;
     const int rest = (int)min(n_tokens - tok0, (long long)TOK * U);
     const int32_t* slots = slot + tok0;
     int at[U];
-    uint32_t w[U], pair[U];
+    uint32_t w[U][2], pair[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         at[u] = u * TOK < rest ? slots[u * TOK] : -1;
@@ -136,34 +145,50 @@ __global__ void __launch_bounds__(KS_THREADS) k_kv4_load(const uint8_t* __restri
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        w[u] = pair[u] = 0;
+        w[u][0] = w[u][1] = pair[u] = 0;
         if (at[u] >= 0) {
             const uint8_t* block = pages + ((size_t)(at[u] / KV4_PAGE) * H_kv + head) * kv4_head_bytes(D);
             const int r = at[u] % KV4_PAGE;
-            if (which == 0) w[u] = *reinterpret_cast<const uint32_t*>(block + kv4_k_word<D>(r, l >> 2, l & 3));
-            else if (D == 128) w[u] = *reinterpret_cast<const uint32_t*>(block + kv4_v_word<D>(r, l & 1, l >> 1));
-            else w[u] = *reinterpret_cast<const uint16_t*>(block + kv4_v_word<D>(r, l & 1, l >> 1)) |
-                        (uint32_t)*reinterpret_cast<const uint16_t*>(block + kv4_v_word<D>(r, l & 1, 4 + (l >> 1))) << 16;
-            pair[u] = *reinterpret_cast<const uint32_t*>(block + kv4_scale_word<D>(which, r, l >> 2));
+            if (which == 0) {
+                const uint8_t* from = block + kv4_k_word<D>(r, l >> 1, 2 * (l & 1));
+                w[u][0] = *reinterpret_cast<const uint32_t*>(from);
+                w[u][1] = *reinterpret_cast<const uint32_t*>(from + D / 8);
+            } else if (D == 128) {
+                const uint2 two = *reinterpret_cast<const uint2*>(block + kv4_v_word<D>(r, 0, l));
+                w[u][0] = two.x;
+                w[u][1] = two.y;
+            } else {
+                const uint32_t a = *reinterpret_cast<const uint32_t*>(block + kv4_v_word<D>(r, 0, l));
+                const uint32_t b = *reinterpret_cast<const uint32_t*>(block + kv4_v_word<D>(r, 0, 4 + l));
+                w[u][0] = __byte_perm(a, b, 0x5410);
+                w[u][1] = __byte_perm(a, b, 0x7632);
+            }
+            pair[u] = *reinterpret_cast<const uint32_t*>(block + kv4_scale_word<D>(which, r, l >> 1));
         }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        uint32_t c = w[u];
-        if (which) c = kv4_transpose<D / 16, 2>(c, l >> 1);
+        uint32_t c[2] = {w[u][0], w[u][1]};
+        if (which) {
+            c[0] = kv4_transpose<D / 16, 1>(c[0], l);
+            c[1] = kv4_transpose<D / 16, 1>(c[1], l);
+        }
         uint16_t* row = to;
         to += TOK * stride;
         if (at[u] < 0) continue;
         // two elements at a time, i and i + 4: bf16 0x4300 | u is 128 + u; u and s u + b in bf16, the latter rounded once
         const uint32_t s2 = __byte_perm(pair[u], 0, 0x1010), b2 = __byte_perm(pair[u], 0, 0x3232);
-        uint32_t v[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t c128 = ((c >> (4 * i)) & 0x000f000fu) | 0x43004300u;
-            asm("{\n .reg .b32 t;\n add.rn.bf16x2 t, %1, %2;\n fma.rn.bf16x2 %0, t, %3, %4;\n}" : "=r"(v[i]) : "r"(c128), "r"(0xC300C300u), "r"(s2), "r"(b2));
+        for (int k = 0; k < 2; ++k) {
+            uint32_t v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t c128 = ((c[k] >> (4 * i)) & 0x000f000fu) | 0x43004300u;
+                asm("{\n .reg .b32 t;\n add.rn.bf16x2 t, %1, %2;\n fma.rn.bf16x2 %0, t, %3, %4;\n}" : "=r"(v[i]) : "r"(c128), "r"(0xC300C300u), "r"(s2), "r"(b2));
+            }
+            reinterpret_cast<uint4*>(row)[k] = make_uint4(__byte_perm(v[0], v[1], 0x5410), __byte_perm(v[2], v[3], 0x5410), __byte_perm(v[0], v[1], 0x7632),
+                                                          __byte_perm(v[2], v[3], 0x7632));
         }
-        uint32_t out[4] = {__byte_perm(v[0], v[1], 0x5410), __byte_perm(v[2], v[3], 0x5410), __byte_perm(v[0], v[1], 0x7632), __byte_perm(v[2], v[3], 0x7632)};
-        *reinterpret_cast<uint4*>(row) = make_uint4(out[0], out[1], out[2], out[3]);
     }
 }
 
@@ -517,8 +542,8 @@ static ag_status kv4_rows(bool store, const ag_kv4_pool* pool, const void* K, co
     const int64_t width = (int64_t)pool->H_kv * pool->D;
     if (!K || !V || !slot || (((uintptr_t)K | (uintptr_t)V) & 15u) || ((uintptr_t)slot & 3u) || k_stride < width || v_stride < width || (k_stride % 8) || (v_stride % 8))
         return AG_ERR_ARG;
-    // four rows a lane once that leaves two rounds of blocks for 148 SMs
-    const int one = KS_THREADS / 2 / (pool->D / 8);
+    // several rows a lane once that leaves two rounds of blocks for 148 SMs
+    const int one = KS_THREADS / 2 / (pool->D / 16);
     const bool many = n_tokens * pool->H_kv >= 2ll * 148 * 8 * KS_ROWS * one;
     const int block_tokens = one * (many ? KS_ROWS : 1);
     const long long blocks = (n_tokens + block_tokens - 1) / block_tokens * pool->H_kv;
