@@ -39,6 +39,8 @@ template <int D, int U>
 __global__ void __launch_bounds__(KS_THREADS) k_kv4_store(uint8_t* __restrict__ pages, long long n_slots, int H_kv, const uint16_t* __restrict__ K,
                                                           const uint16_t* __restrict__ V, long long n_tokens, long long k_stride, long long v_stride,
                                                           const int32_t* __restrict__ slot) {
+    dep_wait();
+    dep_release();
     constexpr int L = D / 16, TOK = KS_THREADS / 2 / L;             // lanes of a row, tokens of the block side by side
     const int l = threadIdx.x % L, which = threadIdx.x / 32 & 1;    // a warp has rows of K or rows of V
     const int head = blockIdx.x % H_kv;
@@ -128,6 +130,8 @@ template <int D, int U>
 __global__ void __launch_bounds__(KS_THREADS) k_kv4_load(const uint8_t* __restrict__ pages, long long n_slots, int H_kv, uint16_t* __restrict__ K,
                                                          uint16_t* __restrict__ V, long long n_tokens, long long k_stride, long long v_stride,
                                                          const int32_t* __restrict__ slot) {
+    dep_wait();
+    dep_release();
     constexpr int L = D / 16, TOK = KS_THREADS / 2 / L;
     const int l = threadIdx.x % L, which = threadIdx.x / 32 & 1;    // a warp has rows of K or rows of V
     const int head = blockIdx.x % H_kv;
@@ -316,6 +320,7 @@ __device__ __forceinline__ int slot_of(const TableArgs& t, const int32_t* row, c
 __global__ void __launch_bounds__(KT_THREADS) k_kv4_extend(const TableArgs t, const int32_t* __restrict__ row, const int32_t* __restrict__ new_off,
                                                            int n, int32_t* __restrict__ slot, int inline_tokens, int32_t* ok) {
     __shared__ union { GrantShared grant; FirstShared first; } sh;
+    dep_wait();
     dep_release();
     const int i = threadIdx.x;
     int r = i < n ? row[i] : -1;
@@ -347,6 +352,7 @@ __global__ void __launch_bounds__(KT_THREADS) k_kv4_extend(const TableArgs t, co
 __global__ void __launch_bounds__(256) k_kv4_slots(const TableArgs t, const int32_t* row, const int32_t* new_off, int n,
                                                    int32_t* __restrict__ slot, int n_tokens, const int32_t* ok) {
     dep_wait();
+    dep_release();
     const int j = blockIdx.x * 256 + threadIdx.x;
     if (j < n_tokens) slot[j] = slot_of(t, row, new_off, ok, n, j);
 }
@@ -354,6 +360,7 @@ __global__ void __launch_bounds__(256) k_kv4_slots(const TableArgs t, const int3
 __global__ void __launch_bounds__(KT_THREADS) k_kv4_fork_plan(const TableArgs t, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
                                                               int n, int32_t* __restrict__ ok) {
     __shared__ union { GrantShared grant; FirstShared first; } sh;
+    dep_wait();
     dep_release();
     const int i = threadIdx.x;
     int r = i < n ? dst[i] : -1;
@@ -397,6 +404,7 @@ __device__ __forceinline__ void copy16(uint4* __restrict__ to, const uint4* __re
 __global__ void __launch_bounds__(256) k_kv4_fork_copy(const TableArgs t, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
                                                        const int32_t* __restrict__ ok, uint8_t* __restrict__ pages, size_t page_bytes, int parts) {
     dep_wait();
+    dep_release();
     const int i = blockIdx.x / parts, part = blockIdx.x - i * parts;
     if (!ok[i]) return;
     const int r = dst[i], len = t.len[r];
@@ -420,6 +428,8 @@ __global__ void __launch_bounds__(256) k_kv4_fork_copy(const TableArgs t, const 
 
 // a page is given back by whoever takes it out of the table, so that a row named twice gives it back once
 __global__ void __launch_bounds__(256) k_kv4_free(const TableArgs t, const int32_t* __restrict__ row) {
+    dep_wait();
+    dep_release();
     const int r = row[blockIdx.x];
     if (r < 0 || r >= t.n_rows) return;
     int32_t* entry = t.page_of + (size_t)r * t.max_pages;
@@ -436,6 +446,7 @@ __global__ void __launch_bounds__(KT_THREADS) k_kv4_compact_plan(const TableArgs
     __shared__ int warp_sum[32];
     __shared__ int holes_before[KT_THREADS + 1];
     __shared__ int hole[KT_HOLES];                                         // the first so many holes, in order
+    dep_wait();
     dep_release();
     const int per = pages_per_thread(t.n_pages);
     const long long p0 = (long long)threadIdx.x * per;
@@ -486,6 +497,7 @@ __global__ void __launch_bounds__(KT_THREADS) k_kv4_compact_plan(const TableArgs
 __global__ void __launch_bounds__(256) k_kv4_compact_move(const TableArgs t, const int32_t* __restrict__ moved, uint8_t* __restrict__ pages,
                                                           size_t page_bytes, int parts) {
     dep_wait();
+    dep_release();
     const long long n_entries = (long long)t.n_rows * t.max_pages, step = (long long)gridDim.x * blockDim.x;
     for (long long e = (long long)blockIdx.x * blockDim.x + threadIdx.x; e < n_entries; e += step) {
         const int p = t.page_of[e];
@@ -510,7 +522,7 @@ static TableArgs table_args(const ag_kv4_pool* pool, const ag_kv4_table* t) {
     return TableArgs{t->page_of, t->len, t->refs, t->n_rows, t->max_pages, (int)pool->n_pages};
 }
 
-// Launch that may come up while the launch before it on the stream finishes; the kernel itself waits for it (dep_wait).
+// Launch that may come up while the launch before it on the stream finishes; the kernel itself waits for it (dep_wait) before it touches memory.
 template <class... P, class... A>
 static cudaError_t launch_dependent(void (*kernel)(P...), unsigned grid, unsigned block, cudaStream_t stream, A... args) {
     cudaLaunchConfig_t cfg;
@@ -555,14 +567,13 @@ static ag_status kv4_rows(bool store, const ag_kv4_pool* pool, const void* K, co
     uint8_t* pages = (uint8_t*)pool->pages;
     if (store) {
         auto kernel = pool->D == 128 ? (many ? k_kv4_store<128, KS_ROWS> : k_kv4_store<128, 1>) : (many ? k_kv4_store<64, KS_ROWS> : k_kv4_store<64, 1>);
-        kernel<<<(unsigned)blocks, KS_THREADS, 0, stream>>>(pages, n_slots, pool->H_kv, (const uint16_t*)K, (const uint16_t*)V, n_tokens, k_stride, v_stride, slot);
+        AG_CUDA(launch_dependent(kernel, (unsigned)blocks, KS_THREADS, stream, pages, n_slots, pool->H_kv, (const uint16_t*)K, (const uint16_t*)V, n_tokens, k_stride, v_stride, slot));
     } else {
         auto kernel = pool->D == 128 ? (many ? k_kv4_load<128, KS_ROWS> : k_kv4_load<128, 1>) : (many ? k_kv4_load<64, KS_ROWS> : k_kv4_load<64, 1>);
-        kernel<<<(unsigned)blocks, KS_THREADS, 0, stream>>>(pages, n_slots, pool->H_kv, (uint16_t*)const_cast<void*>(K), (uint16_t*)const_cast<void*>(V), n_tokens,
-                                                            k_stride, v_stride, slot);
+        AG_CUDA(launch_dependent(kernel, (unsigned)blocks, KS_THREADS, stream, pages, n_slots, pool->H_kv, (uint16_t*)const_cast<void*>(K),
+                                 (uint16_t*)const_cast<void*>(V), n_tokens, k_stride, v_stride, slot));
     }
     count_launch();
-    AG_CUDA(cudaGetLastError());
     return AG_OK;
 }
 
@@ -586,8 +597,7 @@ extern "C" ag_status ag_kv4_extend(const ag_kv4_pool* pool, const ag_kv4_table* 
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
     const TableArgs t = table_args(pool, table);
     const bool one = n_tokens <= KT_INLINE_TOKENS;
-    k_kv4_extend<<<1, KT_THREADS, 0, stream>>>(t, row, new_off, n, slot, one ? (int)n_tokens : 0, ok);
-    AG_CUDA(cudaGetLastError());
+    AG_CUDA(launch_dependent(k_kv4_extend, 1, KT_THREADS, stream, t, row, new_off, n, slot, one ? (int)n_tokens : 0, ok));
     count_launch();
     if (!one) {
         AG_CUDA(launch_dependent(k_kv4_slots, (unsigned)((n_tokens + 255) / 256), 256, stream, t, row, new_off, n, slot, (int)n_tokens, ok));
@@ -606,8 +616,7 @@ extern "C" ag_status ag_kv4_fork(const ag_kv4_pool* pool, const ag_kv4_table* ta
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
     const TableArgs t = table_args(pool, table);
     const size_t page_bytes = ag_kv4_page_bytes(pool->H_kv, pool->D);
-    k_kv4_fork_plan<<<1, KT_THREADS, 0, stream>>>(t, src, dst, n, ok);
-    AG_CUDA(cudaGetLastError());
+    AG_CUDA(launch_dependent(k_kv4_fork_plan, 1, KT_THREADS, stream, t, src, dst, n, ok));
     count_launch();
     const int parts = (int)std::max<size_t>(1, page_bytes / 16384);       // a block copies 16 to 32 KB
     AG_CUDA(launch_dependent(k_kv4_fork_copy, (unsigned)(n * parts), 256, stream, t, src, dst, (const int32_t*)ok, (uint8_t*)pool->pages, page_bytes, parts));
@@ -621,8 +630,7 @@ extern "C" ag_status ag_kv4_free(const ag_kv4_pool* pool, const ag_kv4_table* ta
     if (!row) return AG_ERR_ARG;
     ag_status st = check_arch();
     if (st != AG_OK) return st;
-    k_kv4_free<<<(unsigned)n, 256, 0, reinterpret_cast<cudaStream_t>(cuda_stream)>>>(table_args(pool, table), row);
-    AG_CUDA(cudaGetLastError());
+    AG_CUDA(launch_dependent(k_kv4_free, (unsigned)n, 256, reinterpret_cast<cudaStream_t>(cuda_stream), table_args(pool, table), row));
     count_launch();
     return AG_OK;
 }
@@ -634,8 +642,7 @@ extern "C" ag_status ag_kv4_compact(const ag_kv4_pool* pool, const ag_kv4_table*
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
     const TableArgs t = table_args(pool, table);
     const size_t page_bytes = ag_kv4_page_bytes(pool->H_kv, pool->D);
-    k_kv4_compact_plan<<<1, KT_THREADS, 0, stream>>>(t, moved);
-    AG_CUDA(cudaGetLastError());
+    AG_CUDA(launch_dependent(k_kv4_compact_plan, 1, KT_THREADS, stream, t, moved));
     count_launch();
     const int parts = (int)std::max<size_t>(1, page_bytes / 16384);
     const long long work = std::max((long long)t.n_pages * parts, ((long long)t.n_rows * t.max_pages + 255) / 256);
