@@ -69,8 +69,8 @@ struct PCfg {
     static constexpr int smem_bytes = 2 * q_bytes + PA_STAGES * kv_bytes + (int)((sizeof(PromptCtl) + 1023) / 1024 * 1024) + 1024;
 };
 static_assert(PCfg<128>::smem_bytes <= 227 * 1024, "does not fit");
-// one block per SM, whatever else the tile size would allow: the plan counts on it
-constexpr int PA_MIN_SMEM = 120 * 1024;
+// one block per SM, whatever else the tile size would allow: the plan counts on it, and the block takes all of the SM's tensor memory
+constexpr int PA_MIN_SMEM = 200 * 1024;
 
 // D[tmem] (+)= A[tmem] * B[smem desc]: A is 128 lanes x 16 bf16, two per 32-bit column
 __device__ __forceinline__ void tc_mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
@@ -155,7 +155,7 @@ __device__ __forceinline__ int last_key(const PromptArgs& x, const PromptSeq& s,
 __device__ __forceinline__ int key_tiles(const PromptArgs& x, const PromptSeq& s, int t0, int w) {
     const int first = t0 + w * x.tpt;
     if (first >= s.q_len) return 0;
-    return (last_key(x, s, min(first + x.tpt, s.q_len) - 1) + PA_N) / PA_N;
+    return max(0, last_key(x, s, min(first + x.tpt, s.q_len) - 1) + PA_N) / PA_N;
 }
 
 // A row whose result is not finite, computed again over exactly the keys it sees when a key that it does not see, in the tiles that it shares

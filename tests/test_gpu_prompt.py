@@ -92,6 +92,22 @@ def test_packed_sequences_with_and_without_a_past(D):
         assert (got[:a] == 7.0).all() and (got[b:] == 7.0).all()
 
 
+@pytest.mark.parametrize("k_lens", [[9, 0, 300], [0, 0, 0], [130, 1, 0]])
+def test_far_more_queries_than_keys(k_lens):
+    """Whole tiles, and whole units, whose rows see nothing."""
+    q_lens = [700, 500, 1000]
+    q_off, kv_off = offsets(q_lens), offsets(k_lens)
+    Q, K, V = rows(2200, 8, 128, 33), rows(max(1, sum(k_lens)), 2, 128, 34), rows(max(1, sum(k_lens)), 2, 128, 35)
+    for causal in (True, False):
+        check(run(Q, K, V, q_off, kv_off, causal), *oa.prompt(Q, K, V, q_off, kv_off, causal))
+    if not sum(k_lens):
+        plan, dQ, off, koff = plan_for(), dev(Q), dev(q_off), dev(kv_off)
+        O = torch.full((2200, 8, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+        ag.attention_prompt(dQ.data_ptr(), None, None, O.data_ptr(), 8, 2, 128, off.data_ptr(), koff.data_ptr(), 3, 2200, 0, plan)      # no keys at all
+        torch.cuda.synchronize()
+        assert plan.last_status() == ag.AG_OK and not O.any()
+
+
 def test_growing_maxima_and_a_scale():
     """Scores that keep rising along the keys make the reference move again and again; so do peaked ones."""
     n, D = 700, 128
