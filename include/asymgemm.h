@@ -612,7 +612,7 @@ typedef struct {
  * attention_prompt_persistent - O = softmax(scale Q K^T) V, per sequence and head.  A token that sees no key (no keys at all, or more
  * queries than keys) gets zeros.  What a token does not see (other sequences, later keys) has no influence, whatever it holds.  Scores, softmax statistics and outputs
  * are accumulated in 32 bits, probabilities are rounded to bf16.
- * One launch per 1024 sequences.  Asynchronous on cuda_stream.  Errors as gemm_persistent; device-side status via ag_last_status.
+ * O must not overlap Q, K or V.  One launch per 1024 sequences.  Asynchronous on cuda_stream.  Errors as gemm_persistent; device-side status via ag_last_status.
  */
 ag_status attention_prompt_persistent(const ag_prompt_attention* a, const ag_plan* plan, void* cuda_stream);
 
@@ -644,7 +644,7 @@ typedef struct {
 
 /* Which pages a row (a request's place in the tables) holds.  An empty row has len 0 and entries -1; a page with count 0 is free.
  * Several pools (layers) may share one table: call the functions that change it once, and copy the pages of the other layers with
- * the list that ag_kv4_compact returns. */
+ * ag_kv4_copy. */
 typedef struct {
     int32_t* page_of;   /* device [n_rows][max_pages]: page of the row's tokens 64 c .. 64 c + 63, -1 = none */
     int32_t* len;       /* device [n_rows]: tokens */
@@ -672,7 +672,7 @@ ag_status ag_kv4_load(const ag_kv4_pool* pool, const int32_t* slot, int64_t n_to
  * Free pages are dealt in ascending order, request by request; a request whose pages are not all there (counting those of the
  * requests in front of it, granted or not) is refused and its row stays as it is.  Refused too: a row outside the table, a row named
  * earlier in the same call, a length that max_pages cannot hold.  Never reports an error for these: ok[i] = 0.
- *   row, ok  device [n], new_off device [n + 1] ascending;  n <= AG_KV4_MAX_ROWS
+ *   row, ok  device [n], new_off device [n + 1] ascending;  1 <= n <= AG_KV4_MAX_ROWS (n = 0 only without tokens)
  *   slot     device [n_tokens], out: the slot of token j (of request i when new_off[i] <= j < new_off[i + 1]), -1 where its request was
  *            refused or no request has it
  */
@@ -692,15 +692,23 @@ ag_status ag_kv4_free(const ag_kv4_pool* pool, const ag_kv4_table* table, const 
 /*
  * ag_kv4_compact - move the pages in use to the front of the buffer: with n_used pages in use, the k-th used page from page n_used
  * on goes to the k-th free page below it (contents, count and every table entry).
- *   moved  device [n_pages], out: where page p is now, -1 for a page that was free (for tables of the caller's own, or for other
- *          layers' buffers)
+ *   moved  device [n_pages], out: where page p is now, -1 for a page that was free (for tables of the caller's own, and for other
+ *          layers' buffers: ag_kv4_copy)
  */
 ag_status ag_kv4_compact(const ag_kv4_pool* pool, const ag_kv4_table* table, int32_t* moved, void* cuda_stream);
+/*
+ * ag_kv4_copy - copy pages: page from[i] to page to[i].  For the other layers' buffers of a shared table: after ag_kv4_compact with from =
+ * NULL (page i), to = moved, n = n_pages; after ag_kv4_fork with the rows' open pages.
+ *   from  device [n], or NULL for 0 .. n - 1;  to  device [n].  Pairs with a page outside the pool, or of a page with itself, are passed
+ *         over.  The pairs run in no order: a page that is written must not be named by another pair
+ */
+ag_status ag_kv4_copy(const ag_kv4_pool* pool, const int32_t* from, const int32_t* to, int64_t n, void* cuda_stream);
 
 /*
  * attention_decode_kv4 - O[b][hq][:] = softmax_j(Q[b][hq] . K[j] / sqrt(D)) V[j] over the tokens j of table row row[b], K and V what the cache
- * holds of KV head hq / (H_q / H_kv): the decode step on the 4-bit cache.  The values are s * code + lo (keys without further
- * rounding, values rounded to bf16), probabilities are rounded to bf16, sums and softmax statistics are in 32 bits.
+ * holds of KV head hq / (H_q / H_kv): the decode step on the 4-bit cache.  Keys enter as they stand in the cache (s * code + lo, without
+ * further rounding), values are rounded by at most 2^-12 of themselves or 2^-38 of the largest of the row's values, whichever is more,
+ * probabilities by 2^-12 of themselves or 2^-35 of the largest; sums and softmax statistics are in 32 bits.
  *   Q, O       device, [B][H_q][D] bf16, 16-byte aligned; H_q a multiple of H_kv, H_q / H_kv <= 1024
  *   row        device [B], or NULL for row b (then B <= table->n_rows); a row outside the table, or an empty one, gives zeros
  *   table      lengths are clamped to 0 .. 64 max_pages; tokens whose page is not one of the pool's are left out

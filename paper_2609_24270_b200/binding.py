@@ -31,7 +31,7 @@ EXPORTED = [
     "ag_topo_load", "ag_group_desc_create", "ag_group_desc_destroy", "ag_pack_weights_grouped",
     "gemm_persistent_grouped", "ag_strerror", "ag_last_cuda_error",
     "ag_kernel_launch_count", "ag_kv_pack", "ag_kv_info", "ag_kv_append", "ag_kv_destroy", "attention_decode_persistent",
-    "ag_kv4_page_bytes", "ag_kv4_store", "ag_kv4_load", "ag_kv4_extend", "ag_kv4_fork", "ag_kv4_free", "ag_kv4_compact",
+    "ag_kv4_page_bytes", "ag_kv4_store", "ag_kv4_load", "ag_kv4_extend", "ag_kv4_fork", "ag_kv4_free", "ag_kv4_compact", "ag_kv4_copy",
     "attention_decode_kv4", "ag_attention_decode_kv4_workspace", "attention_prompt_persistent",
 ]
 
@@ -189,6 +189,7 @@ def lib() -> C.CDLL:
     L.ag_kv4_fork.argtypes = [pool, table, vp, vp, C.c_int, vp, vp]
     L.ag_kv4_free.argtypes = [pool, table, vp, C.c_int, vp]
     L.ag_kv4_compact.argtypes = [pool, table, vp, vp]
+    L.ag_kv4_copy.argtypes = [pool, vp, vp, i64, vp]
     L.attention_prompt_persistent.argtypes = [C.POINTER(PromptAttention), vp, vp]
     L.attention_decode_kv4.argtypes = [vp, pool, table, vp, vp, C.c_int, C.c_int, vp, sz, vp]
     L.ag_attention_decode_kv4_workspace.argtypes = [C.c_int] * 5
@@ -651,6 +652,11 @@ def kv4_free(pool: KV4Pool, table: KV4Table, row_ptr: int, n: int, stream: int =
 def kv4_compact(pool: KV4Pool, table: KV4Table, moved_ptr: int, stream: int = 0):
     """Moves the used pages to the front; moved[p] = the new place of page p, -1 for a free one."""
     _check(lib().ag_kv4_compact(C.byref(pool), C.byref(table), moved_ptr, stream), "ag_kv4_compact")
+
+
+def kv4_copy(pool: KV4Pool, from_ptr, to_ptr: int, n: int, stream: int = 0):
+    """Page from[i] (from_ptr None: page i) to page to[i]."""
+    _check(lib().ag_kv4_copy(C.byref(pool), from_ptr, to_ptr, n, stream), "ag_kv4_copy")
 
 
 def attention_decode_kv4_workspace(B: int, H_q: int, H_kv: int, D: int, max_pages: int) -> int:

@@ -518,6 +518,21 @@ __global__ void __launch_bounds__(256) k_kv4_compact_move(const TableArgs t, con
     }
 }
 
+__global__ void __launch_bounds__(256) k_kv4_copy(const int32_t* __restrict__ from, const int32_t* __restrict__ to, long long n, long long n_pages,
+                                                  uint8_t* __restrict__ pages, size_t page_bytes, int parts) {
+    dep_wait();
+    dep_release();
+    const int units = (int)(page_bytes / 16);
+    for (long long w = blockIdx.x; w < n * parts; w += gridDim.x) {
+        const long long i = w / parts;
+        const int part = (int)(w - i * parts);
+        const long long a = from ? from[i] : i, b = to[i];
+        if (a < 0 || a >= n_pages || b < 0 || b >= n_pages || a == b) continue;
+        const int u0 = (int)((long long)units * part / parts), u1 = (int)((long long)units * (part + 1) / parts);
+        copy16(reinterpret_cast<uint4*>(pages + (size_t)b * page_bytes) + u0, reinterpret_cast<const uint4*>(pages + (size_t)a * page_bytes) + u0, u1 - u0);
+    }
+}
+
 static TableArgs table_args(const ag_kv4_pool* pool, const ag_kv4_table* t) {
     return TableArgs{t->page_of, t->len, t->refs, t->n_rows, t->max_pages, (int)pool->n_pages};
 }
@@ -648,6 +663,20 @@ extern "C" ag_status ag_kv4_compact(const ag_kv4_pool* pool, const ag_kv4_table*
     const long long work = std::max((long long)t.n_pages * parts, ((long long)t.n_rows * t.max_pages + 255) / 256);
     AG_CUDA(launch_dependent(k_kv4_compact_move, (unsigned)std::min<long long>(work, 148 * 8), 256, stream, t, (const int32_t*)moved, (uint8_t*)pool->pages,
                              page_bytes, parts));
+    count_launch();
+    return AG_OK;
+}
+
+extern "C" ag_status ag_kv4_copy(const ag_kv4_pool* pool, const int32_t* from, const int32_t* to, int64_t n, void* cuda_stream) {
+    if (!kv4_pool_ok(pool) || n < 0 || n > pool->n_pages) return AG_ERR_ARG;
+    if (n == 0) return AG_OK;
+    if (!to || (((uintptr_t)to | (uintptr_t)from) & 3u)) return AG_ERR_ARG;
+    ag_status st = check_arch();
+    if (st != AG_OK) return st;
+    const size_t page_bytes = ag_kv4_page_bytes(pool->H_kv, pool->D);
+    const int parts = (int)std::max<size_t>(1, page_bytes / 16384);
+    AG_CUDA(launch_dependent(k_kv4_copy, (unsigned)std::min<long long>(n * parts, 148 * 8), 256, reinterpret_cast<cudaStream_t>(cuda_stream), from, to, (long long)n,
+                             (long long)pool->n_pages, (uint8_t*)pool->pages, page_bytes, parts));
     count_launch();
     return AG_OK;
 }

@@ -205,6 +205,33 @@ def test_many_pages_rows_and_tokens():
     c.check()
 
 
+@pytest.mark.parametrize("H_kv,D", [(1, 64), (8, 128)])
+def test_other_layers_follow_by_copies(H_kv, D):
+    """Two buffers under one table: what fork and compact do to the first, ag_kv4_copy does to the second."""
+    c, other = Cache(30, H_kv, D, 6, 6, seed=1), Cache(30, H_kv, D, 1, 1, seed=2)
+    c.extend([0, 1, 2, 3], [0, 100, 164, 400, 420])
+    before = other.pages.copy()
+    c.fork([0, 2, 2], [4, 5, 0])                    # (row 0 is not empty: refused)
+    src = [int(c.page_of[0, 1]), int(c.page_of[2, 3]), -1, 30, 7]
+    dst = [int(c.page_of[4, 1]), int(c.page_of[5, 3]), 5, 6, 7]
+    d_src, d_dst = dev(np.array(src, np.int32)), dev(np.array(dst, np.int32))
+    ag.kv4_copy(other.pool, d_src.data_ptr(), d_dst.data_ptr(), 5)
+    for a, b in list(zip(src, dst))[:2]:
+        other.pages[b] = before[a]
+    c.free([1])
+    refs = c.refs.copy()
+    moved = torch.empty(30, dtype=torch.int32, device="cuda")
+    ag.kv4_compact(c.pool, c.table, moved.data_ptr())
+    ag.kv4_copy(other.pool, None, moved.data_ptr(), 30)
+    want = kv4.compact(c.pages, c.page_of, c.refs)
+    c.check()
+    for p in range(30):
+        if refs[p] > 0 and want[p] != p:
+            other.pages[want[p]] = other.pages[p]
+    assert (moved.cpu().numpy() == want).all()
+    other.check()
+
+
 def test_on_a_side_stream_and_in_a_graph():
     """A decode step's bookkeeping (extend, store) captured once and replayed: every replay appends the next token."""
     c = Cache(12, 2, 128, 3, 4)

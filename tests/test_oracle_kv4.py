@@ -98,6 +98,7 @@ def test_refusals_of_the_cache_functions():
         assert L.ag_kv4_fork(p, r(table), P, P, 1, P, None) == ag.AG_ERR_ARG
         assert L.ag_kv4_free(p, r(table), P, 1, None) == ag.AG_ERR_ARG
         assert L.ag_kv4_compact(p, r(table), P, None) == ag.AG_ERR_ARG
+        assert L.ag_kv4_copy(p, P, P, 1, None) == ag.AG_ERR_ARG
     for t in bad_tables + [None]:
         t = r(t) if t is not None else None
         assert L.ag_kv4_extend(r(pool), t, P, P, 1, P, 1, P, None) == ag.AG_ERR_ARG
@@ -118,6 +119,9 @@ def test_refusals_of_the_cache_functions():
     assert L.ag_kv4_fork(r(pool), r(table), P, None, 1, P, None) == ag.AG_ERR_ARG
     assert L.ag_kv4_free(r(pool), r(table), None, 1, None) == ag.AG_ERR_ARG
     assert L.ag_kv4_compact(r(pool), r(table), None, None) == ag.AG_ERR_ARG
+    for args in [(P, None, 1), (P + 2, P, 1), (None, P + 1, 1), (P, P, -1), (P, P, 11)]:
+        assert L.ag_kv4_copy(r(pool), *args, None) == ag.AG_ERR_ARG, args
+    assert L.ag_kv4_copy(r(pool), None, P, 0, None) == ag.AG_OK
     # nothing to do is not an error
     assert L.ag_kv4_store(r(pool), P, P, 0, 256, 256, P, None) == ag.AG_OK
     assert L.ag_kv4_free(r(pool), r(table), P, 0, None) == ag.AG_OK
