@@ -611,7 +611,7 @@ typedef struct {
 /*
  * attention_prompt_persistent - O = softmax(scale Q K^T) V, per sequence and head.  A token that sees no key (no keys at all, or more
  * queries than keys) gets zeros.  What a token does not see (other sequences, later keys) has no influence, whatever it holds.  Scores, softmax statistics and outputs
- * are accumulated in 32 bits, probabilities are rounded to bf16.
+ * are accumulated in 32 bits, probabilities are rounded to bf16.  (Outputs are normalised at the end: values beyond 2^119 / number of keys may overflow.)
  * O must not overlap Q, K or V.  One launch per 1024 sequences.  Asynchronous on cuda_stream.  Errors as gemm_persistent; device-side status via ag_last_status.
  */
 ag_status attention_prompt_persistent(const ag_prompt_attention* a, const ag_plan* plan, void* cuda_stream);
@@ -707,8 +707,9 @@ ag_status ag_kv4_copy(const ag_kv4_pool* pool, const int32_t* from, const int32_
 /*
  * attention_decode_kv4 - O[b][hq][:] = softmax_j(Q[b][hq] . K[j] / sqrt(D)) V[j] over the tokens j of table row row[b], K and V what the cache
  * holds of KV head hq / (H_q / H_kv): the decode step on the 4-bit cache.  Keys enter as they stand in the cache (s * code + lo, without
- * further rounding), values are rounded by at most 2^-12 of themselves or 2^-38 of the largest of the row's values, whichever is more,
- * probabilities by 2^-12 of themselves or 2^-35 of the largest; sums and softmax statistics are in 32 bits.
+ * further rounding), values are rounded by at most 2^-11 of their group's largest or 2^-32 of the row's largest value, whichever is more
+ * (a step of the quantisation is some 2^-4 of the group's largest), probabilities by 2^-12 of themselves or 2^-35 of the largest; sums and
+ * softmax statistics are in 32 bits.
  *   Q, O       device, [B][H_q][D] bf16, 16-byte aligned; H_q a multiple of H_kv, H_q / H_kv <= 1024
  *   row        device [B], or NULL for row b (then B <= table->n_rows); a row outside the table, or an empty one, gives zeros
  *   table      lengths are clamped to 0 .. 64 max_pages; tokens whose page is not one of the pool's are left out

@@ -7,7 +7,8 @@
 // A code of K becomes an fp16 operand with one logic instruction, 0x6400 | u = 1024 + u or 0x5400 | u << 4 = 64 + u; what that adds to the
 // scores leaves again, together with the bases' part, through two MMAs of the pairs against sums over q kept in three bf16 parts (24
 // bits), so scores carry no rounding besides the 32-bit sums.  V varies its scale along the contraction: its codes become 16 + u
-// (0x4C00 | u << 6) and then s u + b with one multiply-add, in fp16 under a power of two that follows the largest value, rounded at 2^-12;
+// (0x4C00 | u << 6) and then s u + b with one multiply-add, in fp16 under a power of two that follows the largest value (rounded at 2^-12 of the group's
+// largest, or 2^-32 of the row's);
 // P, times 2^10, is fp16 as well.  (An fp8 MMA would take the codes as they are, but mma.sync on this chip converts fp8 operands to fp16
 // first: measured, slower than the above.)
 //
@@ -40,7 +41,7 @@ struct DecodeKv4Args {
     uint16_t* O;                  // [B][H_q][D]
     const uint8_t* pages;
     const int32_t *page_of, *len, *row;
-    float4* part;                 // [slots][NB][D / 16][32 lanes]: unnormalised outputs in fragment order; slots: 2 per warp, 2 per block
+    float4* part;                 // [slots][NB][D / 16][32 lanes]: outputs (normalised) in fragment order; slots: 2 per warp, 2 per block
     float2* stats;                // [slots][8 NB]: maximum (in units of log2), sum
     int2* crossing;               // [blocks]: the unit that begins in the block and goes on beyond it (-1: none), the blocks that it has
     int B, n_pages, H_kv, G, n_rows, max_pages, h_blocks, n_blocks;
@@ -115,12 +116,16 @@ __device__ __forceinline__ int run_holding(long long at, long long total, int n)
 
 // f a + g b, where a factor of zero means "not there", whatever stands beside it
 __device__ __forceinline__ float weighted(float f, float a, float g, float b) { return (f == 0.f ? 0.f : f * a) + (g == 0.f ? 0.f : g * b); }
-// A part (maximum pm, sum pl) joins what there is (m, l): factors f of the outputs so far and g of the part's.  pl = 0: a part without keys, g = 0.
+// Parts carry normalised outputs (no larger than the values, whatever the sums): a part with maximum pm and sum pl joins what there is (m, l), f and g being
+// the shares of the outputs so far and of the part's.  pl = 0: a part without keys, g = 0.
 __device__ __forceinline__ void join_weights(float& m, float& l, float pm, float pl, float& f, float& g) {
     const float top = fmaxf(m, pm);
-    f = l == 0.f ? 0.f : m == top ? 1.f : ex2_ftz(m - top);
-    g = pl == 0.f ? 0.f : pm == top ? 1.f : ex2_ftz(pm - top);
-    l = weighted(f, l, g, pl);
+    f = l == 0.f ? 0.f : m == top ? l : ex2_ftz(m - top) * l;
+    g = pl == 0.f ? 0.f : pm == top ? pl : ex2_ftz(pm - top) * pl;
+    l = f + g;
+    const float r = l == 0.f ? 0.f : 1.f / l;
+    f *= r;
+    g *= r;
     m = pl == 0.f ? m : top;
 }
 
@@ -295,18 +300,17 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
     int v_exp = 0;                                 // outputs are kept times 2^(13 - v_exp)
     bool fresh = true;                             // the page in hand is the first of a unit for this warp
     bool whole = p_first == 0;                     // this warp has had the unit from its first page
-    // the outputs in hand, normalised.  Lanes (g, t) have heads 2 t, 2 t + 1 of d = 16 i + g, + 8; transposed, head g of d = 16 i + 2 t, + 1, ...
+    // the (normalised) outputs in hand.  Lanes (g, t) have heads 2 t, 2 t + 1 of d = 16 i + g, + 8; transposed, head g of d = 16 i + 2 t, + 1, ...
     auto write_unit = [&](int unit) {
         const int bu = unit / heads, hu = unit - bu * heads, head0 = hu % x.h_blocks * 8 * NB;
         uint16_t* out = x.O + ((size_t)(bu * x.H_kv + hu / x.h_blocks) * x.G + head0) * D;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-            const float r0 = l[nb][0] == 0.f ? 0.f : 1.f / l[nb][0], r1 = l[nb][1] == 0.f ? 0.f : 1.f / l[nb][1];
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const uint32_t v = movm_trans(pack_bf16(o[nb][i][2 * e] * r0, o[nb][i][2 * e + 1] * r1));
+                    const uint32_t v = movm_trans(pack_bf16(o[nb][i][2 * e], o[nb][i][2 * e + 1]));
                     if (head0 + nb * 8 + g < x.G) *reinterpret_cast<uint32_t*>(out + (nb * 8 + g) * D + i * 16 + e * 8 + 2 * t) = v;
                 }
         }
@@ -648,10 +652,12 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
                     for (int w = 4; w < 32; w <<= 1) l[nb][e] += __shfl_xor_sync(0xffffffffu, l[nb][e], w);
                     m[nb][e] = m[nb][e] == -INFINITY ? -INFINITY : m[nb][e] * unscale[nb][e];      // in units of log2 from here on
                 }
+                // normalised here, while the outputs are in their own exponent: the sum of p v itself may be beyond 32 bits
+                const float r[2] = {l[nb][0] == 0.f ? 0.f : unexp / l[nb][0], l[nb][1] == 0.f ? 0.f : unexp / l[nb][1]};
 #pragma unroll
                 for (int i = 0; i < MT; ++i)
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) o[nb][i][c] *= unexp;
+                    for (int c = 0; c < 4; ++c) o[nb][i][c] *= r[c & 1];
             }
             const int unit = at->now_unit;
             if (whole && ends) {
@@ -725,7 +731,7 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
 }
 
 // Block i joins the unit that began in block i of the main kernel and went on beyond it, thread (j, y): fragment j of the output, parts y,
-// y + blockDim.y, ...:  O = sum_c 2^(m_c - m) O_c / sum_c 2^(m_c - m) l_c.  A part without a key that counts has m_c = -inf, l_c = 0 and is left out.
+// y + blockDim.y, ...:  O = sum_c w_c O_c / sum_c w_c, w_c = 2^(m_c - m) l_c.  A part without a key that counts has m_c = -inf, l_c = 0 and is left out.
 // Requests without keys get their zeros here too.
 template <int D, int NB>
 __global__ void __launch_bounds__(NB * D * 2 * dk_join_lanes(D, NB)) k_attn_join_kv4(const DecodeKv4Args x) {
@@ -772,13 +778,12 @@ __global__ void __launch_bounds__(NB * D * 2 * dk_join_lanes(D, NB)) k_attn_join
     for (int k = 0; k < (int)blockDim.y - 1; ++k) {
         join(stat[k][j], acc[k][j]);
     }
-    const float r0 = l0 == 0.f ? 0.f : 1.f / l0, r1 = l1 == 0.f ? 0.f : 1.f / l1;
     uint16_t* out = x.O + ((size_t)(b * x.H_kv + hh / x.h_blocks) * x.G + head) * D + 16 * i + g;
-    out[0] = __bfloat16_as_ushort(__float2bfloat16_rn(v.x * r0));
-    out[8] = __bfloat16_as_ushort(__float2bfloat16_rn(v.z * r0));
+    out[0] = __bfloat16_as_ushort(__float2bfloat16_rn(v.x));
+    out[8] = __bfloat16_as_ushort(__float2bfloat16_rn(v.z));
     if (head + 1 < x.G) {
-        out[D] = __bfloat16_as_ushort(__float2bfloat16_rn(v.y * r1));
-        out[D + 8] = __bfloat16_as_ushort(__float2bfloat16_rn(v.w * r1));
+        out[D] = __bfloat16_as_ushort(__float2bfloat16_rn(v.y));
+        out[D + 8] = __bfloat16_as_ushort(__float2bfloat16_rn(v.w));
     }
 }
 

@@ -159,17 +159,18 @@ def test_values_that_are_not_finite_show():
     assert np.isnan(run(queries(2, 2, 64, 9), c, fill=0.0)[1]).all()
 
 
-@pytest.mark.parametrize("step", [1.0, 8.0, 60.0])
+@pytest.mark.parametrize("step", [1.0, 4.0, 12.0])
 @pytest.mark.parametrize("D", [64, 128])
 def test_values_of_very_different_sizes(D, step):
-    """Pages whose values grow (and shrink) by powers of two from one to the next: the common exponent has to follow.  Beside the usual bound a value may be
-    off by 2^-38 of the row's largest."""
+    """Pages whose values grow (and shrink) by powers of two from one to the next: the common exponent has to follow.  Beside the usual bound a value
+    may be off by 2^-32 of the row's largest: fp16 has steps of 2^-24 at its lower end, so s, taken 16 + u <= 31 times, b - 16 s and the sum are off by at most 33 half steps,
+    33 * 2^-25 < 2^-19, where the largest value is kept at 2^13 or more."""
     c = make([700, 64 * 9 + 1], 1, D, seed=17)
     sb = c.pages[:, :, 72 * D:].reshape(c.pages.shape[0], 1, -1).copy().view(np.uint16)
     for r in range(2):
         for i, p in enumerate(c.page_of[r]):
             if p >= 0:
-                f = 2.0 ** (round((i if r == 0 else -i) * step / 4) * 4 / 4)
+                f = 2.0 ** round((i if r == 0 else -i) * step)
                 sb[p] = kv4.bf16_bits((bf16_to_f64(sb[p]) * f).astype(np.float32))
     c.pages[:, :, 72 * D:] = sb.view(np.uint8)
     c.push()
@@ -179,7 +180,7 @@ def test_values_of_very_different_sizes(D, step):
     for r in range(2):
         n = int(c.len[r])
         slots = np.repeat(c.page_of[r].astype(np.int64), 64)[:n] * 64 + np.arange(n) % 64
-        bound = 2.0 ** -8 * np.abs(want[r]) + 5 * 2.0 ** -9 * mass[r] + 2.0 ** -38 * np.abs(V[slots]).max()
+        bound = 2.0 ** -8 * np.abs(want[r]) + 5 * 2.0 ** -9 * mass[r] + 2.0 ** -32 * np.abs(V[slots]).max()
         assert np.isfinite(got[r]).all() and (np.abs(got[r] - want[r]) <= bound).all()
 
 
