@@ -1,4 +1,6 @@
 """The paged 4-bit key/value cache on the GPU against its oracle: codes and tables equal bit for bit."""
+import gc
+
 import numpy as np
 import pytest
 import torch
@@ -8,6 +10,15 @@ from paper_2609_24270_b200 import binding as ag
 from paper_2609_24270_b200 import inputs
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True, scope="module")
+def give_memory_back():
+    """Tests that look at addresses or at free memory find torch's allocator without blocks of these."""
+    yield
+    gc.collect()
+    torch.cuda.empty_cache()
+
 
 
 def dev(a):

@@ -4,6 +4,8 @@ Tolerance: an output is sum_j p_j v_j / sum_j p_j.  v_j is rounded to bf16 once,
 Scores are 32-bit sums that carry up to 1024 q s on the way: |error| <= 2^-23 * 1024 * sum |q| s / sqrt D =: e, and for the inputs here (sum |q| s < 200 at
 D = 128, half at 64) e < 1.2 * 2^-9; an output moves by at most 2 e sum p |v| / sum p.  Together less than 5 * 2^-9 of sum p |v| / sum p (from the
 oracle, with |v|); the output's own rounding adds 2^-8 |want|."""
+import gc
+
 import numpy as np
 import pytest
 import torch
@@ -11,9 +13,18 @@ import torch
 from oracle import kv4
 from oracle.attention import bf16_to_f64
 from paper_2609_24270_b200 import binding as ag
-from tests.test_gpu_kv4 import Cache, dev
+from tests.test_serving_kv4 import Cache, dev
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True, scope="module")
+def give_memory_back():
+    """Tests that look at addresses or at free memory find torch's allocator without blocks of these."""
+    yield
+    gc.collect()
+    torch.cuda.empty_cache()
+
 
 
 def reference(Q, c, row=None):

@@ -4,6 +4,8 @@ Tolerance: the probabilities (relative to a reference, up to 2^8) are rounded to
 at most 2^-8 * sum p |v| / sum p.  Scores are exact bf16 products summed in 32 bits, off by at most 2^-16 * sum |q k| scale (128 adds), and sum |q k| scale < 60 for
 the inputs here: below 2^-10, which moves an output by at most 2 * 2^-10 of the same sum; the exponential's 2^-22 is nothing beside it.
 The output is rounded to bf16: 2^-8 |want|.  Together 2^-8 |want| + 1.5 * 2^-8 * sum p |v| / sum p."""
+import gc
+
 import numpy as np
 import pytest
 import torch
@@ -14,6 +16,15 @@ from paper_2609_24270_b200 import inputs
 from tests.gpu_util import device_topo
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True, scope="module")
+def give_memory_back():
+    """Tests that look at addresses or at free memory find torch's allocator without blocks of these."""
+    yield
+    gc.collect()
+    torch.cuda.empty_cache()
+
 _plans = {}
 
 

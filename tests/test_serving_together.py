@@ -1,6 +1,8 @@
 """The serving operators together, as a server uses them: prompts are attended and stored, a prompt's beginning is shared by forks, tokens are decoded and
 stored one by one, a later chunk attends over its cached past, requests leave, the pages are put together.  Every attention is compared with its
 64-bit oracle on the values that the cache holds."""
+import gc
+
 import numpy as np
 import pytest
 import torch
@@ -8,12 +10,21 @@ import torch
 from oracle import attention as oa
 from oracle import kv4
 from paper_2609_24270_b200 import binding as ag
-from tests.test_gpu_kv4 import dev
-from tests.test_gpu_kv4_decode import check as check_decode
-from tests.test_gpu_prompt import check as check_prompt
-from tests.test_gpu_prompt import plan_for, rows
+from tests.test_serving_kv4 import dev
+from tests.test_serving_kv4_decode import check as check_decode
+from tests.test_serving_prompt import check as check_prompt
+from tests.test_serving_prompt import plan_for, rows
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True, scope="module")
+def give_memory_back():
+    """Tests that look at addresses or at free memory find torch's allocator without blocks of these."""
+    yield
+    gc.collect()
+    torch.cuda.empty_cache()
+
 
 
 class Server:
