@@ -199,7 +199,8 @@ __global__ void __launch_bounds__(KS_THREADS) k_kv4_load(const uint8_t* __restri
 // ---- page tables ------------------------------------------------------------------------------------------------------
 constexpr int KT_THREADS = 1024;
 constexpr int KT_MAX = AG_KV4_MAX_ROWS;              // requests of one call: one thread each
-constexpr int KT_HOLES = 4096;                       // holes that compaction lists in shared memory; it looks for those beyond
+constexpr int KT_SCAN = 8;                           // runs of 32 counts that a warp has in flight as it walks over the pages
+constexpr int KT_SEGMENTS = 4096;                    // stretches of pages that compaction counts by: of 32 pages up to 131072 of them
 constexpr int KT_INLINE_TOKENS = 8192;               // up to so many slots are written by the allocating block itself
 
 // exclusive sum over the block of one value per thread; *total = the sum
@@ -229,9 +230,6 @@ __device__ __forceinline__ T block_scan(T v, T* warp_sum, T* total) {
     return inc - v + (warp ? warp_sum[warp - 1] : 0);
 }
 
-// the pages of thread i: [i per, (i + 1) per)
-__device__ __forceinline__ int pages_per_thread(int n_pages) { return (n_pages + KT_THREADS - 1) / KT_THREADS; }
-
 struct TableArgs {
     int32_t *page_of, *len, *refs;
     int n_rows, max_pages, n_pages;
@@ -240,6 +238,8 @@ struct TableArgs {
 // Request i (thread i) wants need[i] pages; free pages are dealt in ascending order to the requests in order, request i getting the
 // ranks before[i] .. before[i] + need[i] - 1.  A request is granted when all of them exist.  Ends with the pages entered in the
 // tables (column first[i] on) and counted.  Returns whether this thread's request is granted.
+// Every warp walks over its thirty-second of the pages, neighbouring lanes at neighbouring counts: 128 rows grow in 4 us among 2048 pages, TIME
+// among 65536 (39 with neighbouring counts in one thread's hands).
 struct GrantShared {
     long long warp_sum64[32];
     long long before[KT_MAX];                        // 64 bits: 1024 requests of up to 2^25 pages each
@@ -254,25 +254,39 @@ __device__ inline bool grant_pages(const TableArgs& t, int n, int need, int firs
     sh->need[threadIdx.x] = need;
     sh->first[threadIdx.x] = first;
     sh->row[threadIdx.x] = row;
-    const int per = pages_per_thread(t.n_pages);
-    const long long p0 = (long long)threadIdx.x * per;
-    const int p1 = (int)min((long long)t.n_pages, p0 + per);
+    const int lane = threadIdx.x & 31, seg = (t.n_pages + KT_THREADS - 1) / KT_THREADS * 32;
+    const int p0 = (int)min((long long)(threadIdx.x >> 5) * seg, (long long)t.n_pages), p1 = min(p0 + seg, t.n_pages);
     int mine = 0;
-    for (int p = (int)p0; p < p1; ++p) mine += t.refs[p] <= 0;
+    for (int p = p0 + lane; p < p1; p += 32 * KT_SCAN) {
+        int refs[KT_SCAN];
+#pragma unroll
+        for (int u = 0; u < KT_SCAN; ++u) refs[u] = p + 32 * u < p1 ? t.refs[p + 32 * u] : 1;
+#pragma unroll
+        for (int u = 0; u < KT_SCAN; ++u) mine += refs[u] <= 0;
+    }
     int rank = block_scan(mine, sh->warp_sum, &total_free);       // (its barriers also publish before, need, first, row)
-    for (int p = (int)p0; p < p1 && rank < total_need; ++p) {
-        if (t.refs[p] > 0) continue;
-        int a = 0, b = n - 1;                                       // the last request with before <= rank
-        while (a < b) {
-            const int m = (a + b + 1) >> 1;
-            if (sh->before[m] <= rank) a = m; else b = m - 1;
+    rank = __shfl_sync(0xffffffffu, rank, 0);                     // free pages in front of the warp's
+    for (int p = p0; p < p1 && rank < total_need; p += 32 * KT_SCAN) {
+        int refs[KT_SCAN];
+#pragma unroll
+        for (int u = 0; u < KT_SCAN; ++u) refs[u] = p + 32 * u + lane < p1 ? t.refs[p + 32 * u + lane] : 1;
+#pragma unroll
+        for (int u = 0; u < KT_SCAN; ++u) {
+            const unsigned open = __ballot_sync(0xffffffffu, refs[u] <= 0);
+            const int at = rank + __popc(open & ((1u << lane) - 1u));
+            rank += __popc(open);
+            if (refs[u] > 0 || at >= total_need) continue;
+            int a = 0, b = n - 1;                                   // the last request with before <= at
+            while (a < b) {
+                const int m = (a + b + 1) >> 1;
+                if (sh->before[m] <= at) a = m; else b = m - 1;
+            }
+            const int k = (int)(at - sh->before[a]);
+            if (k < sh->need[a] && sh->before[a] + sh->need[a] <= total_free) {
+                t.page_of[(size_t)sh->row[a] * t.max_pages + sh->first[a] + k] = p + 32 * u + lane;
+                t.refs[p + 32 * u + lane] = 1;
+            }
         }
-        const int k = (int)(rank - sh->before[a]);
-        if (k < sh->need[a] && sh->before[a] + sh->need[a] <= total_free) {
-            t.page_of[(size_t)sh->row[a] * t.max_pages + sh->first[a] + k] = p;
-            t.refs[p] = 1;
-        }
-        ++rank;
     }
     return before + need <= total_free;
 }
@@ -441,59 +455,131 @@ __global__ void __launch_bounds__(256) k_kv4_free(const TableArgs t, const int32
     if (threadIdx.x == 0) t.len[r] = 0;
 }
 
-// Where every page goes: with n_used pages in use, the k-th used page above n_used takes the k-th free page below.
+// Where every page goes: with n_used pages in use, the k-th used page from n_used on takes the k-th free page below.  What is counted is the
+// used pages in front of a segment of 32 pages (a multiple in large pools), u(a): a used page's number among the movers is the used
+// pages in front of it less those below n_used, and hole k lies in the last segment a with pages(a) - u(a) <= k.
+// TIME us for 65536 pages; 238 with neighbouring counts in one thread's hands.
 __global__ void __launch_bounds__(KT_THREADS) k_kv4_compact_plan(const TableArgs t, int32_t* __restrict__ moved) {
     __shared__ int warp_sum[32];
-    __shared__ int holes_before[KT_THREADS + 1];
-    __shared__ int hole[KT_HOLES];                                         // the first so many holes, in order
+    __shared__ int used_before[KT_SEGMENTS];
+    __shared__ uint32_t used_mask[KT_SEGMENTS];                            // with segments of 32 pages
     dep_wait();
     dep_release();
-    const int per = pages_per_thread(t.n_pages);
-    const long long p0 = (long long)threadIdx.x * per;
-    const int p1 = (int)min((long long)t.n_pages, p0 + per);
-    int used = 0, n_used, n_holes, n_movers;
-    for (int p = (int)p0; p < p1; ++p) used += t.refs[p] > 0;
-    block_scan(used, warp_sum, &n_used);
-    int holes = 0, movers = 0;
-    for (int p = (int)p0; p < p1; ++p) {
-        if (p < n_used) holes += t.refs[p] <= 0;
-        else movers += t.refs[p] > 0;
-    }
-    int hole_rank = block_scan(holes, warp_sum, &n_holes);
-    holes_before[threadIdx.x] = hole_rank;
-    for (int p = (int)p0; p < min(p1, n_used); ++p)
-        if (t.refs[p] <= 0) {
-            if (hole_rank < KT_HOLES) hole[hole_rank] = p;
-            ++hole_rank;
-        }
-    int rank = block_scan(movers, warp_sum, &n_movers);                    // n_movers = n_holes
-    if (threadIdx.x == 0) holes_before[KT_THREADS] = n_holes;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int words = (t.n_pages + 31) / 32;
+    const bool small = words <= KT_SEGMENTS;
+    const int seg_words = small ? 1 : ((words + KT_SEGMENTS - 1) / KT_SEGMENTS + KT_SCAN - 1) / KT_SCAN * KT_SCAN;
+    const int seg = 32 * seg_words, n_seg = (words + seg_words - 1) / seg_words;
+    const int per_warp = small ? KT_SCAN : 1;                              // segments that a warp takes at a time
+    for (int a = threadIdx.x; a < KT_SEGMENTS; a += KT_THREADS) used_before[a] = 0;
     __syncthreads();
-    for (int p = (int)p0; p < p1; ++p) {
-        int to = -1;
-        if (t.refs[p] > 0) {
-            to = p;
-            if (p >= n_used) {
-                if (rank < KT_HOLES) {
-                    to = hole[rank];
-                } else {
-                    int a = 0, b = KT_THREADS - 1;                          // the thread whose pages hold hole number `rank`
-                    while (a < b) {
-                        const int m = (a + b + 1) >> 1;
-                        if (holes_before[m] <= rank) a = m; else b = m - 1;
-                    }
-                    int k = rank - holes_before[a];
-                    for (int q = a * per; q < n_used; ++q)
-                        if (t.refs[q] <= 0 && k-- == 0) { to = q; break; }
+    for (int a0 = warp * per_warp; a0 < n_seg; a0 += 32 * per_warp)
+        for (int i = 0; i < seg_words; i += KT_SCAN) {
+            const int p = a0 * seg + 32 * i + lane;
+            int refs[KT_SCAN];
+#pragma unroll
+            for (int u = 0; u < KT_SCAN; ++u) refs[u] = p + 32 * u < t.n_pages ? t.refs[p + 32 * u] : 0;
+#pragma unroll
+            for (int u = 0; u < KT_SCAN; ++u) {
+                const uint32_t mask = __ballot_sync(0xffffffffu, refs[u] > 0);
+                const int a = small ? a0 + u : a0;
+                if (lane == 0 && a < n_seg) {
+                    used_before[a] += __popc(mask);
+                    used_mask[a] = mask;
                 }
-                ++rank;
             }
         }
-        moved[p] = to;
+    __syncthreads();
+    constexpr int PER = KT_SEGMENTS / KT_THREADS;
+    int c[PER], sum = 0, n_used;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        c[i] = used_before[threadIdx.x * PER + i];
+        sum += c[i];
+    }
+    sum = block_scan(sum, warp_sum, &n_used);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        used_before[threadIdx.x * PER + i] = sum;
+        sum += c[i];
+    }
+    __syncthreads();
+    int used_below = 0;                                                    // used pages below n_used, which stay
+    for (int p = n_used / seg * seg + lane; p < n_used; p += 32) used_below += t.refs[p] > 0;
+    used_below = __reduce_add_sync(0xffffffffu, used_below) + (n_used < t.n_pages ? used_before[n_used / seg] : n_used);
+    for (int a = warp; a < n_seg; a += 32) {
+        int rank = used_before[a] - used_below;                            // movers in front, once at n_used
+        for (int i = 0; i < seg_words; ++i) {
+            const int p = a * seg + 32 * i + lane;
+            const bool used = small ? used_mask[a] >> lane & 1u : p < t.n_pages && t.refs[p] > 0;
+            const uint32_t mask = small ? used_mask[a] : __ballot_sync(0xffffffffu, used);
+            int to = used ? p : -1;
+            if (used && p >= n_used) {
+                int k = rank + __popc(mask & ((1u << lane) - 1u));
+                int lo = 0, hi = n_seg - 1;
+                while (lo < hi) {
+                    const int m = (lo + hi + 1) >> 1;
+                    if (m * seg - used_before[m] <= k) lo = m; else hi = m - 1;
+                }
+                k -= lo * seg - used_before[lo];
+                to = lo * seg;
+                if (small) {                                               // free page k of the word, by halves
+                    uint32_t open = ~used_mask[lo];
+#pragma unroll
+                    for (int half = 16; half; half >>= 1) {
+                        const int below = __popc(open & ((1u << half) - 1u));
+                        if (k >= below) {
+                            k -= below;
+                            open >>= half;
+                            to += half;
+                        }
+                    }
+                } else {
+                    for (; to < n_used; ++to)
+                        if (t.refs[to] <= 0 && k-- == 0) break;
+                }
+            }
+            if (p < t.n_pages) moved[p] = to;
+            rank += __popc(mask);
+        }
     }
 }
 
-// page (and its count) by page, in parts; and the tables, entry by entry
+// Copies page from[i] (from = NULL: i) to page to[i], in parts; pairs with a page outside the pool, or of a page with itself, are passed over.  A
+// block's threads look for work side by side, as most pages of a large pool stay where they are.  With `refs` the pages' counts move too.
+__device__ __forceinline__ void copy_pages(const int32_t* __restrict__ from, const int32_t* __restrict__ to, long long n, long long n_pages,
+                                           uint8_t* __restrict__ pages, size_t page_bytes, int parts, int32_t* refs) {
+    __shared__ int work_from[256], work_to[256], work_part[256], n_found;
+    const int units = (int)(page_bytes / 16);
+    const long long n_work = n * parts;
+    for (long long w0 = blockIdx.x; w0 < n_work; w0 += (long long)gridDim.x * 256) {
+        if (threadIdx.x == 0) n_found = 0;
+        __syncthreads();
+        const long long w = w0 + (long long)threadIdx.x * gridDim.x;
+        if (w < n_work) {
+            const long long i = w / parts, a = from ? from[i] : i, b = to[i];
+            if (a >= 0 && a < n_pages && b >= 0 && b < n_pages && a != b) {
+                const int k = atomicAdd(&n_found, 1);                      // (in any order: the copies are independent)
+                work_from[k] = (int)a;
+                work_to[k] = (int)b;
+                work_part[k] = (int)(w - i * parts);
+            }
+        }
+        __syncthreads();
+        for (int k = 0; k < n_found; ++k) {
+            const int a = work_from[k], b = work_to[k], part = work_part[k];
+            const int u0 = (int)((long long)units * part / parts), u1 = (int)((long long)units * (part + 1) / parts);
+            copy16(reinterpret_cast<uint4*>(pages + (size_t)b * page_bytes) + u0, reinterpret_cast<const uint4*>(pages + (size_t)a * page_bytes) + u0, u1 - u0);
+            if (refs && part == 0 && threadIdx.x == 0) {
+                refs[b] = refs[a];
+                refs[a] = 0;
+            }
+        }
+        __syncthreads();                                                   // the list has been read
+    }
+}
+
+// page (and its count) by page, and the tables, entry by entry
 __global__ void __launch_bounds__(256) k_kv4_compact_move(const TableArgs t, const int32_t* __restrict__ moved, uint8_t* __restrict__ pages,
                                                           size_t page_bytes, int parts) {
     dep_wait();
@@ -503,34 +589,18 @@ __global__ void __launch_bounds__(256) k_kv4_compact_move(const TableArgs t, con
         const int p = t.page_of[e];
         if (p >= 0) t.page_of[e] = p < t.n_pages ? moved[p] : -1;
     }
-    const int units = (int)(page_bytes / 16);
-    const long long n_work = (long long)t.n_pages * parts;
-    for (long long w = blockIdx.x; w < n_work; w += gridDim.x) {
-        const int p = (int)(w / parts), part = (int)(w - (long long)p * parts);
-        const int to = moved[p];
-        if (to < 0 || to == p) continue;
-        const int u0 = (int)((long long)units * part / parts), u1 = (int)((long long)units * (part + 1) / parts);
-        copy16(reinterpret_cast<uint4*>(pages + (size_t)to * page_bytes) + u0, reinterpret_cast<const uint4*>(pages + (size_t)p * page_bytes) + u0, u1 - u0);
-        if (part == 0 && threadIdx.x == 0) {
-            t.refs[to] = t.refs[p];
-            t.refs[p] = 0;
-        }
-    }
+    copy_pages(nullptr, moved, t.n_pages, t.n_pages, pages, page_bytes, parts, t.refs);
 }
 
 __global__ void __launch_bounds__(256) k_kv4_copy(const int32_t* __restrict__ from, const int32_t* __restrict__ to, long long n, long long n_pages,
                                                   uint8_t* __restrict__ pages, size_t page_bytes, int parts) {
     dep_wait();
     dep_release();
-    const int units = (int)(page_bytes / 16);
-    for (long long w = blockIdx.x; w < n * parts; w += gridDim.x) {
-        const long long i = w / parts;
-        const int part = (int)(w - i * parts);
-        const long long a = from ? from[i] : i, b = to[i];
-        if (a < 0 || a >= n_pages || b < 0 || b >= n_pages || a == b) continue;
-        const int u0 = (int)((long long)units * part / parts), u1 = (int)((long long)units * (part + 1) / parts);
-        copy16(reinterpret_cast<uint4*>(pages + (size_t)b * page_bytes) + u0, reinterpret_cast<const uint4*>(pages + (size_t)a * page_bytes) + u0, u1 - u0);
-    }
+    copy_pages(from, to, n, n_pages, pages, page_bytes, parts, nullptr);
+}
+
+static bool misaligned(const int32_t* a, const int32_t* b = nullptr, const int32_t* c = nullptr) {
+    return ((uintptr_t)a | (uintptr_t)b | (uintptr_t)c) & 3u;
 }
 
 static TableArgs table_args(const ag_kv4_pool* pool, const ag_kv4_table* t) {
@@ -606,7 +676,7 @@ extern "C" ag_status ag_kv4_extend(const ag_kv4_pool* pool, const ag_kv4_table* 
                                    int64_t n_tokens, int32_t* ok, void* cuda_stream) {
     if (!kv4_pool_ok(pool) || !kv4_table_ok(table) || n < 0 || n > KT_MAX || n_tokens < 0 || n_tokens > (1ll << 31) - 1) return AG_ERR_ARG;
     if (n == 0 && n_tokens == 0) return AG_OK;
-    if (!row || !new_off || !ok || (n_tokens > 0 && !slot) || n == 0) return AG_ERR_ARG;
+    if (!row || !new_off || !ok || (n_tokens > 0 && !slot) || n == 0 || misaligned(row, new_off, ok) || misaligned(slot)) return AG_ERR_ARG;
     ag_status st = check_arch();
     if (st != AG_OK) return st;
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
@@ -625,7 +695,7 @@ extern "C" ag_status ag_kv4_fork(const ag_kv4_pool* pool, const ag_kv4_table* ta
                                  void* cuda_stream) {
     if (!kv4_pool_ok(pool) || !kv4_table_ok(table) || n < 0 || n > KT_MAX) return AG_ERR_ARG;
     if (n == 0) return AG_OK;
-    if (!src || !dst || !ok) return AG_ERR_ARG;
+    if (!src || !dst || !ok || misaligned(src, dst, ok)) return AG_ERR_ARG;
     ag_status st = check_arch();
     if (st != AG_OK) return st;
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
@@ -642,7 +712,7 @@ extern "C" ag_status ag_kv4_fork(const ag_kv4_pool* pool, const ag_kv4_table* ta
 extern "C" ag_status ag_kv4_free(const ag_kv4_pool* pool, const ag_kv4_table* table, const int32_t* row, int n, void* cuda_stream) {
     if (!kv4_pool_ok(pool) || !kv4_table_ok(table) || n < 0 || n > KT_MAX) return AG_ERR_ARG;
     if (n == 0) return AG_OK;
-    if (!row) return AG_ERR_ARG;
+    if (!row || misaligned(row)) return AG_ERR_ARG;
     ag_status st = check_arch();
     if (st != AG_OK) return st;
     AG_CUDA(launch_dependent(k_kv4_free, (unsigned)n, 256, reinterpret_cast<cudaStream_t>(cuda_stream), table_args(pool, table), row));

@@ -805,7 +805,8 @@ static bool decode_kv4_shape(long long B, int H_q, int H_kv, int D, int max_page
     // up to 16 pages a row and a block for every unit: two pages a warp at most, and no second launch
     s->aligned = max_pages <= 2 * DK_WARPS && s->units <= most;
     s->n_blocks = s->aligned ? (int)s->units : (int)std::min<long long>(most, (s->units * max_pages + DK_WARPS - 1) / DK_WARPS);
-    return s->units <= 0x7fffffffll;
+    // a warp's run is counted in 31 bits
+    return s->units <= 0x7fffffffll && s->units * max_pages <= 1ll << 40;
 }
 static size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 

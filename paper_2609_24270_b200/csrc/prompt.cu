@@ -159,39 +159,73 @@ __device__ __forceinline__ int key_tiles(const PromptArgs& x, const PromptSeq& s
 }
 
 // A row whose result is not finite, computed again over exactly the keys it sees when a key that it does not see, in the tiles that it shares
-// with rows that do, holds a value that is not finite (a probability of zero times it has spoilt the row).  One thread, 32-bit
-// arithmetic, no shared state; reached by such rows only.
-__device__ __noinline__ void repair_row(const PromptArgs& x, const PromptSeq& s, int D, int tok, int head, int last, int tiles, uint16_t* out) {
-    const uint16_t* k0 = x.K + (size_t)s.k0 * x.k_stride + (size_t)(head / x.G) * D;
-    const uint16_t* v0 = x.V + (size_t)s.k0 * x.v_stride + (size_t)(head / x.G) * D;
-    bool foreign = false;
-    for (int j = last + 1; j < min(tiles * PA_N, s.k_len) && !foreign; ++j)
-        for (int d = 0; d < D; ++d) foreign |= (v0[(size_t)j * x.v_stride + d] & 0x7f80u) == 0x7f80u;
-    if (!foreign) return;
-    const uint16_t* q = x.Q + (size_t)(s.q0 + tok) * x.q_stride + (size_t)head * D;
-    auto score = [&](int j) {
-        const uint16_t* k = k0 + (size_t)j * x.k_stride;
-        float a = 0.f;
-        for (int d = 0; d < D; ++d) a = fmaf(__uint_as_float((uint32_t)q[d] << 16), __uint_as_float((uint32_t)k[d] << 16), a);
-        return a * x.scale_log2e;
+// with rows that do, holds a value that is not finite (a probability of zero times it has spoilt the row).  One warp, its lanes side by side
+// on the row's elements, in 32 bits; reached by such rows only.  (One thread a row took so long that the other warps' waits could run out.)
+template <int D>
+__device__ __noinline__ void repair_row(const PromptArgs& x, const PromptSeq& s, int tok, int head, int last, int tiles) {
+    constexpr int E = D / 32, U = 8;
+    const int lane = threadIdx.x & 31;
+    const uint16_t* k0 = x.K + (size_t)s.k0 * x.k_stride + (size_t)(head / x.G) * D + lane * E;
+    const uint16_t* v0 = x.V + (size_t)s.k0 * x.v_stride + (size_t)(head / x.G) * D + lane * E;
+    auto load = [](const uint16_t* from, float (&v)[E]) {
+        uint32_t w[E / 2];
+        if (E == 4) *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(from);
+        else w[0] = *reinterpret_cast<const uint32_t*>(from);
+#pragma unroll
+        for (int i = 0; i < E; ++i) v[i] = __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
     };
-    float m = -INFINITY;
-    for (int j = 0; j <= last; ++j) m = fmaxf(m, score(j));
-    if (m == -INFINITY) m = 0.f;
-    for (int c = 0; c < D; c += 16) {
-        float o[16], l = 0.f;
-        for (int i = 0; i < 16; ++i) o[i] = 0.f;
-        for (int j = 0; j <= last; ++j) {
-            const float w = exp2_fast(score(j) - m);
-            l += w;
-            for (int i = 0; i < 16; ++i) o[i] = fmaf(w, __uint_as_float((uint32_t)v0[(size_t)j * x.v_stride + c + i] << 16), o[i]);
-        }
-        for (int i = 0; i < 16; i += 2) {
-            const uint32_t pair = bf16_pair(l == 0.f ? 0.f : o[i] / l, l == 0.f ? 0.f : o[i + 1] / l);
-            out[c + i] = (uint16_t)pair;
-            out[c + i + 1] = (uint16_t)(pair >> 16);
-        }
+    bool foreign = false;
+    for (int j = last + 1; j < min(tiles * PA_N, s.k_len); ++j) {
+        float v[E];
+        load(v0 + (size_t)j * x.v_stride, v);
+#pragma unroll
+        for (int i = 0; i < E; ++i) foreign |= !(fabsf(v[i]) <= 3.4e38f);
     }
+    if (!__any_sync(0xffffffffu, foreign)) return;
+    float q[E], o[E], m = -INFINITY, l = 0.f;
+    load(x.Q + (size_t)(s.q0 + tok) * x.q_stride + (size_t)head * D + lane * E, q);
+#pragma unroll
+    for (int i = 0; i < E; ++i) o[i] = 0.f;
+    for (int j0 = 0; j0 <= last; j0 += U) {
+        float k[U][E], v[U][E], a[U], top = m;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int j = min(j0 + u, last);
+            load(k0 + (size_t)j * x.k_stride, k[u]);
+            load(v0 + (size_t)j * x.v_stride, v[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            a[u] = 0.f;
+#pragma unroll
+            for (int i = 0; i < E; ++i) a[u] = fmaf(q[i], k[u][i], a[u]);
+        }
+#pragma unroll
+        for (int w = 1; w < 32; w <<= 1)
+#pragma unroll
+            for (int u = 0; u < U; ++u) a[u] += __shfl_xor_sync(0xffffffffu, a[u], w);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            a[u] *= x.scale_log2e;
+            if (j0 + u <= last) top = fmaxf(top, a[u]);
+        }
+        const float ref = top == -INFINITY ? 0.f : top, f = exp2_fast(m - ref);
+        l *= f;
+#pragma unroll
+        for (int i = 0; i < E; ++i) o[i] *= f;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (j0 + u <= last) {
+                const float w = exp2_fast(a[u] - ref);
+                l += w;
+#pragma unroll
+                for (int i = 0; i < E; ++i) o[i] = fmaf(w, v[u][i], o[i]);
+            }
+        m = top;
+    }
+    uint16_t* out = x.O + (size_t)(s.q0 + tok) * x.o_stride + (size_t)head * D + lane * E;
+#pragma unroll
+    for (int i = 0; i < E; i += 2) *reinterpret_cast<uint32_t*>(out + i) = bf16_pair(l == 0.f ? 0.f : o[i] / l, l == 0.f ? 0.f : o[i + 1] / l);
 }
 
 template <int D>
@@ -283,19 +317,21 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         __syncthreads();
     }
     if (warp == 0) {
-        int sum = 0;
+        const long long most = 0x7fffffff / x.H_kv;   // units are counted in 31 bits; only sequences that lie over one another could need more
+        long long sum = 0;
         for (int i0 = 0; i0 < x.n_seq; i0 += 32) {
             const int i = i0 + lane;
-            int v = i < x.n_seq ? (ctl->seq[i].q_len + block_tokens - 1) / block_tokens : 0, inc = v;
+            const int v = i < x.n_seq ? (ctl->seq[i].q_len + block_tokens - 1) / block_tokens : 0;
+            long long inc = v;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
-                const int u = __shfl_up_sync(0xffffffffu, inc, o);
+                const long long u = __shfl_up_sync(0xffffffffu, inc, o);
                 if (lane >= o) inc += u;
             }
-            if (i < x.n_seq) ctl->blocks_before[i] = sum + inc - v;
+            if (i < x.n_seq) ctl->blocks_before[i] = (int)min(sum + inc - v, most);
             sum += __shfl_sync(0xffffffffu, inc, 31);
         }
-        if (lane == 0) ctl->blocks_before[x.n_seq] = sum;
+        if (lane == 0) ctl->blocks_before[x.n_seq] = (int)min(sum, most);
     }
     if (warp == 8) {
         tmem_alloc(smem_u32(&ctl->tmem_base), 512);
@@ -690,7 +726,12 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                 }
             }
             tc_fence_before();
-            if (odd != 0.f && x.causal) repair_row(x, s, D, tok, head * x.G + row_head, last, n, out);
+            __syncwarp();
+            unsigned spoilt = __ballot_sync(0xffffffffu, x.causal && odd != 0.f);
+            for (; spoilt; spoilt &= spoilt - 1) {
+                const int r0 = (warp & 3) * 32 + __ffs(spoilt) - 1, tok0 = t0 + w * x.tpt + r0 / x.G;
+                repair_row<D>(x, s, tok0, head * x.G + r0 % x.G, last_key(x, s, tok0), n);
+            }
         }
     }
     tc_fence_before();

@@ -119,6 +119,14 @@ def test_refusals_of_the_cache_functions():
     assert L.ag_kv4_fork(r(pool), r(table), P, None, 1, P, None) == ag.AG_ERR_ARG
     assert L.ag_kv4_free(r(pool), r(table), None, 1, None) == ag.AG_ERR_ARG
     assert L.ag_kv4_compact(r(pool), r(table), None, None) == ag.AG_ERR_ARG
+    for odd in range(4):
+        a = [P + 2 if i == odd else P for i in range(4)]
+        assert L.ag_kv4_extend(r(pool), r(table), a[0], a[1], 1, a[2], 1, a[3], None) == ag.AG_ERR_ARG
+        if odd < 3:
+            assert L.ag_kv4_fork(r(pool), r(table), a[0], a[1], 1, a[2], None) == ag.AG_ERR_ARG
+        if odd < 1:
+            assert L.ag_kv4_free(r(pool), r(table), a[0], 1, None) == ag.AG_ERR_ARG
+            assert L.ag_kv4_compact(r(pool), r(table), a[0], None) == ag.AG_ERR_ARG
     for args in [(P, None, 1), (P + 2, P, 1), (None, P + 1, 1), (P, P, -1), (P, P, 11)]:
         assert L.ag_kv4_copy(r(pool), *args, None) == ag.AG_ERR_ARG, args
     assert L.ag_kv4_copy(r(pool), None, P, 0, None) == ag.AG_OK
@@ -161,6 +169,9 @@ def test_refusals_of_the_decode_attention():
     for change in (dict(ws=None), dict(wsb=need - 1), dict(ws=P + 8)):
         assert L.attention_decode_kv4(*{**good, **change}.values()) == ag.AG_ERR_ARG, change
     assert L.attention_decode_kv4(*{**good, "B": 0}.values()) == ag.AG_OK
+    long_table = pool_and_table(max_pages=(1 << 25) - 1)[1]                # a run of pages is counted in 31 bits
+    for change in (dict(table=r(long_table), B=1 << 15, row=P), dict(table=r(long_table), B=1 << 30, row=P)):
+        assert L.attention_decode_kv4(*{**good, **change}.values()) == ag.AG_ERR_ARG, change
     # parts of 8 heads, two a warp and two a block, 2 * 148 blocks at most; shapes that are refused have size 0
     assert ag.attention_decode_kv4_workspace(1000, 32, 8, 128, 1000) == 18 * 2 * 148 * 8 * (128 * 4 + 8) + 2 * 148 * 8
     assert ag.attention_decode_kv4_workspace(2, 7, 2, 128, 1000) == 0 and ag.attention_decode_kv4_workspace(2, 8, 2, 96, 1000) == 0

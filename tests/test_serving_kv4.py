@@ -216,6 +216,54 @@ def test_many_pages_rows_and_tokens():
     c.check()
 
 
+@pytest.mark.parametrize("n_pages", [31, 32, 33, 1023, 4097, 131072, 131073, 200000])
+def test_pools_of_every_size(n_pages):
+    """Free pages scattered over small and large pools: dealt in ascending order, and closed up again.  Contents: a page's first word is its number."""
+    rng = np.random.default_rng(n_pages)
+    rows, max_pages = 40, n_pages // 8 + 2
+    pages = torch.zeros(n_pages, ag.kv4_page_bytes(1, 64) // 4, dtype=torch.int32, device="cuda")
+    pages[:, 0] = torch.arange(n_pages, device="cuda")
+    pages[:, -1] = -pages[:, 0]
+    refs = (rng.random(n_pages) < 0.6).astype(np.int32)
+    refs[n_pages // 3: n_pages // 2] = 0
+    page_of, length = np.full((rows, max_pages), -1, np.int32), np.zeros(rows, np.int32)
+    used = np.flatnonzero(refs)[: max_pages]
+    page_of[0, : len(used)] = used
+    length[0] = 64 * len(used)
+    want_page_of, want_len, want_refs = page_of.copy(), length.copy(), refs.copy()
+    d_page_of, d_len, d_refs = dev(page_of), dev(length), dev(refs)
+    pool, table = ag.KV4Pool(pages.data_ptr(), n_pages, 1, 64), ag.KV4Table(d_page_of.data_ptr(), d_len.data_ptr(), d_refs.data_ptr(), rows, max_pages)
+    grow = np.arange(1, rows, dtype=np.int32)
+    off = np.concatenate([[0], np.cumsum(rng.integers(0, 64 * max(2, n_pages // 150), rows - 1))]).astype(np.int32)
+    d_row, d_off, slot, ok = dev(grow), dev(off), torch.empty(int(off[-1]), dtype=torch.int32, device="cuda"), torch.empty(rows, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    ag.kv4_extend(pool, table, d_row.data_ptr(), d_off.data_ptr(), rows - 1, slot.data_ptr(), int(off[-1]), ok.data_ptr())
+    want_slot, want_ok = kv4.extend(want_page_of, want_len, want_refs, list(grow), list(off), int(off[-1]))
+    torch.cuda.synchronize()
+    assert (ok.cpu().numpy()[: rows - 1] == want_ok).all() and (slot.cpu().numpy() == want_slot).all()
+    for d, w in ((d_page_of, want_page_of), (d_len, want_len), (d_refs, want_refs)):
+        assert (d.cpu().numpy() == w).all()
+    moved = torch.full((n_pages,), -7, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    ag.kv4_compact(pool, table, moved.data_ptr())
+    torch.cuda.synchronize()
+    held = np.flatnonzero(want_refs > 0)
+    n_used = len(held)
+    want = np.full(n_pages, -1, np.int32)
+    want[held[held < n_used]] = held[held < n_used]
+    holes = np.flatnonzero(want_refs[:n_used] <= 0)
+    want[held[held >= n_used]] = holes
+    assert (moved.cpu().numpy() == want).all()
+    back = np.zeros(n_pages, np.int64)
+    back[want[held]] = held
+    assert (pages[:n_used, 0].cpu().numpy() == back[:n_used]).all() and (pages[:n_used, -1].cpu().numpy() == -back[:n_used]).all()
+    want_page_of[want_page_of >= 0] = want[want_page_of[want_page_of >= 0]]
+    assert (d_page_of.cpu().numpy() == want_page_of).all()
+    after = np.zeros(n_pages, np.int32)
+    after[:n_used] = want_refs[back[:n_used]]
+    assert (d_refs.cpu().numpy() == after).all()
+
+
 @pytest.mark.parametrize("H_kv,D", [(1, 64), (8, 128)])
 def test_other_layers_follow_by_copies(H_kv, D):
     """Two buffers under one table: what fork and compact do to the first, ag_kv4_copy does to the second."""

@@ -166,6 +166,19 @@ def test_later_values_however_large_never_enter():
     assert np.array_equal(got[:150], clean[:150])
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_nan_behind_rows_with_a_long_past(D):
+    """Rows that share a key tile with a later token's NaN, at the end of 65536 keys: computed again, in time, and right."""
+    n, m, at = 40, 65536, 65536 - 10
+    Q, K, V = rows(n, 4, D, 33), rows(m, 1, D, 34), rows(m, 1, D, 35)
+    want, mass = oa.prompt(Q, K, V, [0, n], [0, m])
+    V2 = V.copy()
+    V2[at] = 0x7FC0
+    got = run(Q, K, V2, np.array([0, n], np.int32), np.array([0, m], np.int32))
+    check(got[: n - 10], want[: n - 10], mass[: n - 10])
+    assert np.isnan(got[n - 10:]).all()
+
+
 def test_parts_of_a_fused_projection():
     n, Hq, Hkv, D = 150, 6, 2, 64
     qkv = rows(n, Hq + 2 * Hkv, D, 16)
