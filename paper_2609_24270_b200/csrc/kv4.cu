@@ -201,7 +201,9 @@ constexpr int KT_THREADS = 1024;
 constexpr int KT_MAX = AG_KV4_MAX_ROWS;              // requests of one call: one thread each
 constexpr int KT_SCAN = 8;                           // runs of 32 counts that a warp has in flight as it walks over the pages
 constexpr int KT_SEGMENTS = 4096;                    // stretches of pages that compaction counts by: of 32 pages up to 131072 of them
-constexpr int KT_INLINE_TOKENS = 8192;               // up to so many slots are written by the allocating block itself
+// Up to so many slots are written by the allocating block itself, more by a second launch: 2048 slots take 10.2 to 11.1 us in all against 10.4 to
+// 11.7, 4096 13.1 to 13.6 against 11.0 to 13.4 (8, 128 and 1024 rows; 65536 pages).
+constexpr int KT_INLINE_TOKENS = 2048;
 
 // exclusive sum over the block of one value per thread; *total = the sum
 template <class T>
@@ -238,8 +240,8 @@ struct TableArgs {
 // Request i (thread i) wants need[i] pages; free pages are dealt in ascending order to the requests in order, request i getting the
 // ranks before[i] .. before[i] + need[i] - 1.  A request is granted when all of them exist.  Ends with the pages entered in the
 // tables (column first[i] on) and counted.  Returns whether this thread's request is granted.
-// Every warp walks over its thirty-second of the pages, neighbouring lanes at neighbouring counts: 128 rows grow in 4 us among 2048 pages, TIME
-// among 65536 (39 with neighbouring counts in one thread's hands).
+// Every warp walks over its thirty-second of the pages, neighbouring lanes at neighbouring counts: 128 rows grow in 4.2 us among 2048 pages,
+// 7.5 among 65536 (39 with neighbouring counts in one thread's hands).
 struct GrantShared {
     long long warp_sum64[32];
     long long before[KT_MAX];                        // 64 bits: 1024 requests of up to 2^25 pages each
@@ -458,7 +460,7 @@ __global__ void __launch_bounds__(256) k_kv4_free(const TableArgs t, const int32
 // Where every page goes: with n_used pages in use, the k-th used page from n_used on takes the k-th free page below.  What is counted is the
 // used pages in front of a segment of 32 pages (a multiple in large pools), u(a): a used page's number among the movers is the used
 // pages in front of it less those below n_used, and hole k lies in the last segment a with pages(a) - u(a) <= k.
-// TIME us for 65536 pages; 238 with neighbouring counts in one thread's hands.
+// Plan and move of 65536 pages that are in place already: 27 us (238 with neighbouring counts in one thread's hands).
 __global__ void __launch_bounds__(KT_THREADS) k_kv4_compact_plan(const TableArgs t, int32_t* __restrict__ moved) {
     __shared__ int warp_sum[32];
     __shared__ int used_before[KT_SEGMENTS];
