@@ -136,8 +136,8 @@ struct WarpWalk {
     int b, hh, len, row, now_unit, now_pages;
 };
 
-template <int D>
-constexpr int dk_smem_bytes() { return DK_WARPS * kv4_head_bytes(D); }
+template <int D, int NB>
+constexpr int dk_smem_bytes() { return DK_WARPS * (kv4_head_bytes(D) + NB * 8 * D * 2); }      // a head's page and a block of queries for each warp
 
 template <int D, int NB>
 __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4(const DecodeKv4Args x) {
@@ -148,7 +148,8 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
     __shared__ long long warp_sum[DK_WARPS];
     __shared__ int tokens_of[DK_THREADS], row_of[DK_THREADS];      // of the requests, up to DK_THREADS of them
     __shared__ int slot_unit[2 * DK_WARPS];        // units that a warp has only a part of: one that began before its run, one that goes on behind it
-    __shared__ int slot_ends[2 * DK_WARPS];        // the part includes the unit's last page
+    __shared__ int slot_ends[2 * DK_WARPS];        // bit 0: the part includes the unit's last page; bit 1: it lies in the workspace, not in the warp's buffer
+    __shared__ __align__(16) float2 slot_stats[2 * DK_WARPS][8 * NB];
     __shared__ WarpWalk walk[DK_WARPS];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     dep_wait();
@@ -200,6 +201,12 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
         __syncthreads();
         total = before[DK_THREADS] * heads;
         n_blocks = (int)min((long long)x.n_blocks, (total + DK_WARPS - 1) / DK_WARPS);      // at least a page for every warp
+        for (int i = blockIdx.x; i < x.B; i += gridDim.x) {         // requests without keys: zeros
+            int r;
+            if ((per > 1 ? row_tokens(x, i, &r) : tokens_of[i]) != 0) continue;
+            uint4* out = reinterpret_cast<uint4*>(x.O + (size_t)i * x.H_kv * x.G * D);
+            for (int k = threadIdx.x; k < x.H_kv * x.G * D / 8; k += DK_THREADS) out[k] = make_uint4(0, 0, 0, 0);
+        }
         if ((int)blockIdx.x >= n_blocks) {
             if (threadIdx.x == 0) x.crossing[blockIdx.x] = make_int2(-1, 0);
             return;
@@ -221,7 +228,8 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
 
     uint8_t* kbuf = smem + warp * kv4_head_bytes(D);          // codes of K, then K's pairs
     uint8_t* vbuf = kbuf + 40 * D;
-    const uint32_t kbuf_a = smem_u32(kbuf), vbuf_a = smem_u32(vbuf);
+    uint8_t* qbuf = smem + DK_WARPS * kv4_head_bytes(D) + warp * (NB * 8 * D * 2);
+    const uint32_t kbuf_a = smem_u32(kbuf), vbuf_a = smem_u32(vbuf), qbuf_a = smem_u32(qbuf);
     // copies the runs of 16 tokens that hold keys: codes (8 D bytes a run) and pairs (2 D bytes a run)
     auto fetch = [&](int which, const uint8_t* src, int nv) {
         if (nv > 0) {
@@ -240,6 +248,13 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
             }
         }
         cp_async_commit();
+    };
+
+    // copies the query rows of KV head and block hh of request b
+    auto fetch_q = [&](int b, int hh) {
+        const int head0 = hh % x.h_blocks * 8 * NB, rows = min(x.G - head0, 8 * NB);
+        const uint8_t* src = reinterpret_cast<const uint8_t*>(x.Q + (((size_t)b * x.H_kv + hh / x.h_blocks) * x.G + head0) * D);
+        for (int j = lane * 16; j < rows * 2 * D; j += 512) cp_async16(qbuf_a + j, src + j);
     };
 
     // ---- the first page of the run
@@ -287,6 +302,8 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
         src_next = x.pages + ((size_t)(nv_next ? id : 0) * x.H_kv + at->hh / x.h_blocks) * kv4_head_bytes(D);
     };
     if (left > 0) {
+        fetch_q(b, hh);                            // (in front of the pages, so as not to queue behind everybody's)
+        cp_async_commit();
         locate();
         fetch(0, src_next, nv_next);
         fetch(1, src_next, nv_next);
@@ -300,28 +317,17 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
     int v_exp = 0;                                 // outputs are kept times 2^(13 - v_exp)
     bool fresh = true;                             // the page in hand is the first of a unit for this warp
     bool whole = p_first == 0;                     // this warp has had the unit from its first page
-    // the (normalised) outputs in hand.  Lanes (g, t) have heads 2 t, 2 t + 1 of d = 16 i + g, + 8; transposed, head g of d = 16 i + 2 t, + 1, ...
-    auto write_unit = [&](int unit) {
-        const int bu = unit / heads, hu = unit - bu * heads, head0 = hu % x.h_blocks * 8 * NB;
-        uint16_t* out = x.O + ((size_t)(bu * x.H_kv + hu / x.h_blocks) * x.G + head0) * D;
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const uint32_t v = movm_trans(pack_bf16(o[nb][i][2 * e], o[nb][i][2 * e + 1]));
-                    if (head0 + nb * 8 + g < x.G) *reinterpret_cast<uint32_t*>(out + (nb * 8 + g) * D + i * 16 + e * 8 + 2 * t) = v;
-                }
-        }
+    // Where the outputs of a unit go.  Fragments have heads 2 t, 2 t + 1 of d = 16 i + g, + 8 in lane (g, t); transposed, head g of d = 16 i + 2 t, + 1, ...
+    auto out_of = [&](int unit, int* head0) {
+        const int bu = unit / heads, hu = unit - bu * heads;
+        *head0 = hu % x.h_blocks * 8 * NB;
+        return x.O + (((size_t)bu * x.H_kv + hu / x.h_blocks) * x.G + *head0 + g) * D + 2 * t;
     };
-    auto write_part = [&](size_t slot) {
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-            if (g == 0) *reinterpret_cast<float4*>(&x.stats[slot * 8 * NB + nb * 8 + 2 * t]) = make_float4(m[nb][0], l[nb][0], m[nb][1], l[nb][1]);
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
-                x.part[((slot * NB + nb) * MT + i) * 32 + lane] = make_float4(o[nb][i][0], o[nb][i][1], o[nb][i][2], o[nb][i][3]);
+    auto write_fragment = [&](uint16_t* out, int head0, int nb, int i, float v0, float v1, float v2, float v3) {
+        const uint32_t lo = movm_trans(pack_bf16(v0, v1)), hi = movm_trans(pack_bf16(v2, v3));
+        if (head0 + nb * 8 + g < x.G) {
+            *reinterpret_cast<uint32_t*>(out + nb * 8 * D + i * 16) = lo;
+            *reinterpret_cast<uint32_t*>(out + nb * 8 * D + i * 16 + 8) = hi;
         }
     };
     while (left > 0) {
@@ -332,7 +338,8 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
             at->now_unit = b_now * heads + hh_now;
             at->now_pages = np;
             at->now_begin = at->unit_begin;
-            const uint16_t* q_rows = x.Q + ((size_t)b_now * x.H_kv + hh_now / x.h_blocks) * x.G * D;
+            cp_async_wait<2>();                    // the queries have landed
+            __syncwarp();
             // ---- queries as B operands: q times a power of two c (the head's largest |q| between 128 and 256) in fp16, exact down to
             // 2^-22 of the largest.  Lane (g, t) holds head g, elements 32 grp + 8 t + {0, 4}, {1, 5}, {2, 6}, {3, 7}.  Even elements meet
             // 1024 + u, odd ones 64 + u (see the scores): what the 1024 and 64 add is taken out with the bases, by MMAs of the
@@ -344,7 +351,7 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
 #pragma unroll
                 for (int grp = 0; grp < NG; ++grp) {
                     uint4 v = make_uint4(0, 0, 0, 0);
-                    if (head < x.G) v = *reinterpret_cast<const uint4*>(q_rows + (size_t)head * D + grp * 32 + t * 8);
+                    if (head < x.G) v = *reinterpret_cast<const uint4*>(qbuf + (nb * 8 + g) * D * 2 + grp * 64 + t * 16);
                     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
@@ -471,6 +478,7 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
         }
         __syncwarp();                              // every lane has read K
         // ---- on to the next page: same unit, next head, next request that has any
+        // (the queries were read at the unit's first page, in front of a barrier since)
         const bool ends = p + 1 == np;
         --left;
         nv_next = 0;
@@ -496,9 +504,11 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
                 }
                 at->hh = hn;
                 __syncwarp();
+                fetch_q(at->b, hn);
             }
             locate();
         }
+        cp_async_commit();
         fetch(0, src_next, nv_next);
         if (nv > 0) {
             // ---- softmax, with the running maximum in the scores' own units; keys past the end count as -inf
@@ -547,7 +557,7 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
                     }
             }
         }
-        cp_async_wait<1>();                        // V of this page has landed
+        cp_async_wait<2>();                        // V of this page has landed
         __syncwarp();
         if (nv > 0) {
             // The pairs of two keys side by side (s, s') and (c, c'), c = b - 16 s, in fp16 times 2^(13 - v_exp): |b| + 31 s, the largest a value
@@ -661,13 +671,25 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
             }
             const int unit = at->now_unit;
             if (whole && ends) {
-                write_unit(unit);
+                int head0;
+                uint16_t* out = out_of(unit, &head0);
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) write_fragment(out, head0, nb, i, o[nb][i][0], o[nb][i][1], o[nb][i][2], o[nb][i][3]);
             } else {
+                // a part: into the warp's own buffer when that has been read for the last time (64 D of its 80 D bytes, or half of it)
                 const int slot = 2 * warp + (whole ? 1 : 0);
-                write_part(2 * DK_WARPS * (size_t)blockIdx.x + slot);
+                float4* to = left == 0 ? reinterpret_cast<float4*>(kbuf) : x.part + (2 * DK_WARPS * (size_t)blockIdx.x + slot) * NB * MT * 32;
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    if (g == 0) *reinterpret_cast<float4*>(&slot_stats[slot][nb * 8 + 2 * t]) = make_float4(m[nb][0], l[nb][0], m[nb][1], l[nb][1]);
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) to[(nb * MT + i) * 32 + lane] = make_float4(o[nb][i][0], o[nb][i][1], o[nb][i][2], o[nb][i][3]);
+                }
                 if (lane == 0) {
                     slot_unit[slot] = unit;
-                    slot_ends[slot] = ends;
+                    slot_ends[slot] = (ends ? 1 : 0) | (left == 0 ? 0 : 2);
                 }
             }
             if (left == 0 && warp == DK_WARPS - 1 && lane == 0 && !x.aligned) {      // the block's last page (no warp behind this one's has any)
@@ -682,57 +704,76 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
     }
     cp_async_wait<0>();
 
-    // ---- parts of one unit that several warps of the block have: the warp with the first one adds them up
+    // ---- parts of units that several warps have: O = sum_c w_c O_c / sum_c w_c, w_c = 2^(m_c - m) l_c, over the parts c with keys that count.  The slots
+    // are in the order of the line, so a unit's parts are neighbours.  The warps share the work by fragments.
     __syncthreads();
-#pragma unroll 1
-    for (int k = 0; k < 2; ++k) {
-        const int own = 2 * warp + k, unit = slot_unit[own];
-        if (unit < 0) continue;
-        bool first = true;
-        for (int c = 0; c < own; ++c) first &= slot_unit[c] != unit;
-        if (!first) continue;
+    const int slot_u = lane < 2 * DK_WARPS ? slot_unit[lane] : -1;
+    const unsigned there = __ballot_sync(0xffffffffu, slot_u >= 0), in_front = there & ((1u << lane) - 1u);
+    const unsigned with_end = __ballot_sync(0xffffffffu, slot_u >= 0 && (slot_ends[lane % (2 * DK_WARPS)] & 1));
+    const unsigned far = __ballot_sync(0xffffffffu, slot_u >= 0 && (slot_ends[lane % (2 * DK_WARPS)] & 2));
+    const int prev_u = __shfl_sync(0xffffffffu, slot_u, in_front ? 31 - __clz(in_front) : 0);
+    const unsigned firsts = __ballot_sync(0xffffffffu, slot_u >= 0 && !(in_front && prev_u == slot_u));
+    const int n_items = __popc(firsts) * MT, k1 = n_items * (warp + 1) / DK_WARPS;       // the fragments of all units in one line, cut into equal runs
+    for (int k = n_items * warp / DK_WARPS; k < k1;) {
+        unsigned rest = firsts;
+        for (int q = k / MT; q; --q) rest &= rest - 1;
+        const int own = __ffs(rest) - 1, unit = __shfl_sync(0xffffffffu, slot_u, own), i0 = k % MT, i1 = min(MT, i0 + k1 - k);
+        k += i1 - i0;
+        const unsigned parts = __ballot_sync(0xffffffffu, slot_u == unit);
+        const bool starts = (own & 1) || x.aligned;
+        const size_t joint = 2 * DK_WARPS * (size_t)x.n_blocks + 2 * (size_t)blockIdx.x + (starts ? 1 : 0);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
+            float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
+            for (unsigned c = parts; c; c &= c - 1) {
+                const float4 st = *reinterpret_cast<const float4*>(&slot_stats[__ffs(c) - 1][nb * 8 + 2 * t]);
+                if (st.y != 0.f) m0 = fmaxf(m0, st.x);
+                if (st.w != 0.f) m1 = fmaxf(m1, st.z);
+            }
+            auto weight = [](float pm, float pl, float top) { return pl == 0.f ? 0.f : pm == top ? pl : ex2_ftz(pm - top) * pl; };
+            for (unsigned c = parts; c; c &= c - 1) {
+                const float4 st = *reinterpret_cast<const float4*>(&slot_stats[__ffs(c) - 1][nb * 8 + 2 * t]);
+                l0 += weight(st.x, st.y, m0);
+                l1 += weight(st.z, st.w, m1);
+            }
+            const float r0 = l0 == 0.f ? 0.f : 1.f / l0, r1 = l1 == 0.f ? 0.f : 1.f / l1;
+            float4 v[MT];
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) o[nb][i][c] = 0.f;
-            m[nb][0] = m[nb][1] = -INFINITY;
-            l[nb][0] = l[nb][1] = 0.f;
-        }
-        bool ends = false;
-#pragma unroll 1
-        for (int c = own; c < 2 * DK_WARPS; ++c) {
-            if (slot_unit[c] != unit) continue;
-            ends |= slot_ends[c] != 0;
-            const size_t slot = 2 * DK_WARPS * (size_t)blockIdx.x + c;
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-                const float4 st = __ldcg(reinterpret_cast<const float4*>(&x.stats[slot * 8 * NB + nb * 8 + 2 * t]));
-                float4 u[MT];
-#pragma unroll
-                for (int i = 0; i < MT; ++i) u[i] = __ldcg(&x.part[((slot * NB + nb) * MT + i) * 32 + lane]);
-                float f0, f1, g0, g1;
-                join_weights(m[nb][0], l[nb][0], st.x, st.y, f0, g0);
-                join_weights(m[nb][1], l[nb][1], st.z, st.w, f1, g1);
+            for (int i = 0; i < MT; ++i) v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (unsigned c = parts; c; c &= c - 1) {
+                const int slot = __ffs(c) - 1;
+                const float4 st = *reinterpret_cast<const float4*>(&slot_stats[slot][nb * 8 + 2 * t]);
+                const float4* from = (far >> slot & 1 ? x.part + (2 * DK_WARPS * (size_t)blockIdx.x + slot) * NB * MT * 32
+                                                      : reinterpret_cast<const float4*>(smem + (slot >> 1) * kv4_head_bytes(D))) + nb * MT * 32 + lane;
+                const float w0 = weight(st.x, st.y, m0) * r0, w1 = weight(st.z, st.w, m1) * r1;      // (a weight of zero: whatever stands there)
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
-                    o[nb][i][0] = weighted(f0, o[nb][i][0], g0, u[i].x);
-                    o[nb][i][1] = weighted(f1, o[nb][i][1], g1, u[i].y);
-                    o[nb][i][2] = weighted(f0, o[nb][i][2], g0, u[i].z);
-                    o[nb][i][3] = weighted(f1, o[nb][i][3], g1, u[i].w);
+                    if (i < i0 || i >= i1) continue;
+                    const float4 u = from[i * 32];
+                    v[i].x += w0 == 0.f ? 0.f : w0 * u.x;
+                    v[i].y += w1 == 0.f ? 0.f : w1 * u.y;
+                    v[i].z += w0 == 0.f ? 0.f : w0 * u.z;
+                    v[i].w += w1 == 0.f ? 0.f : w1 * u.w;
                 }
             }
+            if (starts && (with_end & parts)) {
+                int head0;
+                uint16_t* out = out_of(unit, &head0);
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+                    if (i >= i0 && i < i1) write_fragment(out, head0, nb, i, v[i].x, v[i].y, v[i].z, v[i].w);
+            } else {
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+                    if (i >= i0 && i < i1) x.part[((joint * NB + nb) * MT + i) * 32 + lane] = v[i];
+                if (i0 == 0 && g == 0) *reinterpret_cast<float4*>(&x.stats[joint * 8 * NB + nb * 8 + 2 * t]) = make_float4(m0, l0, m1, l1);
+            }
         }
-        const bool starts = own & 1 || (x.aligned != 0);
-        if (starts && ends) write_unit(unit);
-        else write_part(2 * DK_WARPS * (size_t)x.n_blocks + 2 * (size_t)blockIdx.x + (starts ? 1 : 0));
     }
 }
 
 // Block i joins the unit that began in block i of the main kernel and went on beyond it, thread (j, y): fragment j of the output, parts y,
 // y + blockDim.y, ...:  O = sum_c w_c O_c / sum_c w_c, w_c = 2^(m_c - m) l_c.  A part without a key that counts has m_c = -inf, l_c = 0 and is left out.
-// Requests without keys get their zeros here too.
 template <int D, int NB>
 __global__ void __launch_bounds__(NB * D * 2 * dk_join_lanes(D, NB)) k_attn_join_kv4(const DecodeKv4Args x) {
     constexpr int MT = D / 16, NF = NB * MT * 32, LANES = dk_join_lanes(D, NB);
@@ -741,11 +782,6 @@ __global__ void __launch_bounds__(NB * D * 2 * dk_join_lanes(D, NB)) k_attn_join
     dep_wait();
     const int j = threadIdx.x, y = threadIdx.y, lane = j & 31, g = lane >> 2, t = lane & 3, i = (j >> 5) % MT, nb = (j >> 5) / MT;
     const int2 pc = x.crossing[blockIdx.x];
-    for (int r, b = blockIdx.x; b < x.B; b += gridDim.x)
-        if (row_tokens(x, b, &r) == 0) {
-            uint4* out = reinterpret_cast<uint4*>(x.O + (size_t)b * x.H_kv * x.G * D);
-            for (int k = y * blockDim.x + j; k < x.H_kv * x.G * D / 8; k += blockDim.x * blockDim.y) out[k] = make_uint4(0, 0, 0, 0);
-        }
     if (pc.x < 0) return;
     const int heads = x.H_kv * x.h_blocks, b = pc.x / heads, hh = pc.x - b * heads;
     const int head = hh % x.h_blocks * 8 * NB + nb * 8 + 2 * t;
@@ -852,9 +888,11 @@ extern "C" ag_status attention_decode_kv4(const void* Q, const ag_kv4_pool* pool
                                                  : (s.nb == 2 ? k_attn_join_kv4<64, 2> : k_attn_join_kv4<64, 1>);
     static std::atomic<unsigned long long> attr_done{0};
     const cudaError_t attr_err = once_per_device(attr_done, [] {
-        cudaError_t e = cudaFuncSetAttribute(k_attn_decode_kv4<128, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, dk_smem_bytes<128>());
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(k_attn_decode_kv4<128, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, dk_smem_bytes<128>());
-        return e;                                  // D = 64 needs 40 KB, which every kernel may have
+        cudaError_t e = cudaFuncSetAttribute(k_attn_decode_kv4<128, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, dk_smem_bytes<128, 1>());
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(k_attn_decode_kv4<128, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, dk_smem_bytes<128, 2>());
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(k_attn_decode_kv4<64, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, dk_smem_bytes<64, 1>());
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(k_attn_decode_kv4<64, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, dk_smem_bytes<64, 2>());
+        return e;
     });
     if (attr_err != cudaSuccess) return cuda_fail(attr_err);
     // both launches may come up while the one before them on the stream finishes, and wait for it on the device
@@ -865,7 +903,7 @@ extern "C" ag_status attention_decode_kv4(const void* Q, const ag_kv4_pool* pool
     memset(&cfg, 0, sizeof cfg);
     cfg.gridDim = dim3((unsigned)s.n_blocks);
     cfg.blockDim = dim3(DK_THREADS);
-    cfg.dynamicSmemBytes = pool->D == 128 ? dk_smem_bytes<128>() : dk_smem_bytes<64>();
+    cfg.dynamicSmemBytes = pool->D == 128 ? (s.nb == 2 ? dk_smem_bytes<128, 2>() : dk_smem_bytes<128, 1>()) : (s.nb == 2 ? dk_smem_bytes<64, 2>() : dk_smem_bytes<64, 1>());
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
