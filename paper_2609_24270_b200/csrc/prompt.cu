@@ -141,6 +141,15 @@ __device__ __forceinline__ f32x2 exp2_cubic(f32x2 v) {
     unpack2(t, t0, t1);
     return mul2(q, pack2(__uint_as_float(__float_as_uint(t0) << 23), __uint_as_float(__float_as_uint(t1) << 23)));
 }
+// 32 bytes: in one store where the address allows
+__device__ __forceinline__ void store32(uint16_t* to, const uint32_t (&v)[8], bool wide) {
+    if (wide) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+    } else {
+        reinterpret_cast<uint4*>(to)[0] = make_uint4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<uint4*>(to)[1] = make_uint4(v[4], v[5], v[6], v[7]);
+    }
+}
 __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -598,6 +607,7 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t t_s = tmem + lanes + w * PA_N, t_o = tmem + lanes + 256 + w * D;
         const int row_tok = r / x.G, row_head = r - row_tok * x.G;
+        const bool wide = (((uintptr_t)x.O | (uintptr_t)(2 * x.o_stride)) & 31) == 0;
         uint32_t ns = 0;                           // score tiles so far = value products so far
         bool ok = true;
         for (uint32_t it = 0; ok; ++it) {
@@ -715,13 +725,11 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
 #pragma unroll
                     for (int i = 0; i < 32; ++i) odd = fmaf(__uint_as_float(ov[i]), 0.f, odd);
 #pragma unroll
-                    for (int i = 0; i < 32; i += 8) {
-                        uint4 v;
-                        v.x = bf16_pair(__uint_as_float(ov[i]) * inv, __uint_as_float(ov[i + 1]) * inv);
-                        v.y = bf16_pair(__uint_as_float(ov[i + 2]) * inv, __uint_as_float(ov[i + 3]) * inv);
-                        v.z = bf16_pair(__uint_as_float(ov[i + 4]) * inv, __uint_as_float(ov[i + 5]) * inv);
-                        v.w = bf16_pair(__uint_as_float(ov[i + 6]) * inv, __uint_as_float(ov[i + 7]) * inv);
-                        *reinterpret_cast<uint4*>(out + c + i) = v;
+                    for (int i = 0; i < 32; i += 16) {
+                        uint32_t v[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) v[k] = bf16_pair(__uint_as_float(ov[i + 2 * k]) * inv, __uint_as_float(ov[i + 2 * k + 1]) * inv);
+                        store32(out + c + i, v, wide);
                     }
                 }
             }
