@@ -4,9 +4,9 @@
 //     S[key][q]  = sum over groups of 32 d:  s (sum_d u q_d) + b (sum_d q_d)      m16n8k16 MMA (fp16): 16 keys x 8 heads x 16 d
 //     P = 2^((S - max) log2 e / sqrt D)                                           running maximum and sum per warp
 //     O[d][q]   += sum_key V[key][d] P[key][q]                                    m16n8k16 MMA (fp16): 16 d x 8 heads x 16 keys
-// A code of K becomes an fp16 operand with one logic instruction, 0x6400 | u = 1024 + u or 0x5400 | u << 4 = 64 + u; what that adds to the
-// scores leaves again, together with the bases' part, through two MMAs of the pairs against sums over q kept in three bf16 parts (24
-// bits), so scores carry no rounding besides the 32-bit sums.  V varies its scale along the contraction: its codes become 16 + u
+// A code of K becomes an fp16 operand with one logic instruction: a nibble masked out of its word is the subnormal u 2^-24, or u 2^-20, and
+// the MMA takes subnormals as they are.  The bases' part comes from an MMA against sums over q kept in three bf16 parts (24 bits),
+// so scores carry no rounding besides the 32-bit sums.  V varies its scale along the contraction: its codes become 16 + u
 // (0x4C00 | u << 6) and then s u + b with one multiply-add, in fp16 under a power of two that follows the largest value (rounded at 2^-12 of the group's
 // largest, or 2^-32 of the row's);
 // P, times 2^10, is fp16 as well.  (An fp8 MMA would take the codes as they are, but mma.sync on this chip converts fp8 operands to fp16
@@ -52,11 +52,6 @@ __device__ __forceinline__ float ex2_ftz(float v) {      // 2^v, relative error 
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
-}
-__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ void mma_bf16_new(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
@@ -313,7 +308,7 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
     }
 
     uint32_t qf[NB][NG][4];
-    uint32_t qb[NB][2], qs[NB][2];
+    uint32_t qb[NB][2];
     float unscale[NB][2];                          // log2 e / (c sqrt D) of heads 2 t and 2 t + 1
     float o[NB][MT][4];
     float m[NB][2], l[NB][2];
@@ -343,10 +338,10 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
             at->now_begin = at->unit_begin;
             cp_async_wait<2>();                    // the queries have landed
             __syncwarp();
-            // ---- queries as B operands: q times a power of two c (the head's largest |q| between 128 and 256) in fp16, exact down to
-            // 2^-22 of the largest.  Lane (g, t) holds head g, elements 32 grp + 8 t + {0, 4}, {1, 5}, {2, 6}, {3, 7}.  Even elements meet
-            // 1024 + u, odd ones 64 + u (see the scores): what the 1024 and 64 add is taken out with the bases, by MMAs of the
-            // pairs against the groups' sums of q (qb) and of what is added (qs), 24 bits each in three bf16 parts.
+            // ---- queries as B operands: q times a power of two c (the head's largest |q| between 2^14 and 2^15) in fp16, exact down to
+            // 2^-24 of the largest.  Lane (g, t) holds head g, elements 32 grp + 8 t + {0, 4}, {1, 5}, {2, 6}, {3, 7}.  Even elements meet
+            // 2^-24 u, odd ones, kept at a sixteenth, 2^-20 u (see the scores).  The bases meet the groups' sums of q, times 2^-24 c, 24 bits in
+            // three bf16 parts.
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
                 const int head = head0 + nb * 8 + g;
@@ -365,50 +360,37 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
                 }
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                const uint32_t e = min(246u, 261u - (__float_as_uint(top) >> 23));        // exponent field of c
+                const uint32_t e = min(246u, 268u - (__float_as_uint(top) >> 23));        // exponent field of c
                 const float c = __uint_as_float(e << 23);
-                float even[NG], odd[NG];
+                float total[NG];
 #pragma unroll
                 for (int grp = 0; grp < NG; ++grp) {
-                    even[grp] = odd[grp] = 0.f;
+                    total[grp] = 0.f;
 #pragma unroll
-                    for (int i = 0; i < 8; i += 2) {
+                    for (int i = 0; i < 8; ++i) {
                         q[grp][i] *= c;
-                        q[grp][i + 1] *= c;
-                        even[grp] += q[grp][i];
-                        odd[grp] += q[grp][i + 1];
+                        total[grp] += q[grp][i];
+                        if (i & 1) q[grp][i] *= 0x1p-4f;
                     }
 #pragma unroll
                     for (int i = 0; i < 4; ++i) qf[nb][grp][i] = pack_f16(q[grp][i], q[grp][i + 4]);
 #pragma unroll
-                    for (int w = 1; w < 4; w <<= 1) {
-                        even[grp] += __shfl_xor_sync(0xffffffffu, even[grp], w);
-                        odd[grp] += __shfl_xor_sync(0xffffffffu, odd[grp], w);
-                    }
+                    for (int w = 1; w < 4; w <<= 1) total[grp] += __shfl_xor_sync(0xffffffffu, total[grp], w);
                 }
                 // D = 128: k = 2 t, 2 t + 1 are groups 2 (t & 1), + 1 of part t / 2, k + 8 part 2 of them (t < 2); D = 64: both groups, part t
                 const bool upper = D == 128 && (t & 1);
                 const int part = D == 128 ? t >> 1 : t;
-                uint32_t sums[3], adds[3];                 // the lane's two groups, bf16 side by side
-                {
-                    const float e0 = upper ? even[NG - 2] : even[0], e1 = upper ? even[NG - 1] : even[1];
-                    const float o0 = upper ? odd[NG - 2] : odd[0], o1 = upper ? odd[NG - 1] : odd[1];
-                    float s0 = e0 + o0, s1 = e1 + o1, a0 = -1024.f * e0 - 64.f * o0, a1 = -1024.f * e1 - 64.f * o1;
+                uint32_t sums[3];                          // the lane's two groups, bf16 side by side
+                float s0 = 0x1p-24f * (upper ? total[NG - 2] : total[0]), s1 = 0x1p-24f * (upper ? total[NG - 1] : total[1]);
 #pragma unroll
-                    for (int k = 0; k < 3; ++k) {
-                        sums[k] = pack_bf16(s0, s1);
-                        adds[k] = pack_bf16(a0, a1);
-                        s0 -= bf16_lo(sums[k]);
-                        s1 -= bf16_hi(sums[k]);
-                        a0 -= bf16_lo(adds[k]);
-                        a1 -= bf16_hi(adds[k]);
-                    }
+                for (int k = 0; k < 3; ++k) {
+                    sums[k] = pack_bf16(s0, s1);
+                    s0 -= bf16_lo(sums[k]);
+                    s1 -= bf16_hi(sums[k]);
                 }
                 qb[nb][0] = part == 0 ? sums[0] : part == 1 ? sums[1] : part == 2 ? sums[2] : 0u;
-                qs[nb][0] = part == 0 ? adds[0] : part == 1 ? adds[1] : part == 2 ? adds[2] : 0u;
                 qb[nb][1] = D == 128 && t < 2 ? sums[2] : 0u;
-                qs[nb][1] = D == 128 && t < 2 ? adds[2] : 0u;
-                const float f = x.scale_log2e * __uint_as_float((254u - e) << 23);
+                const float f = x.scale_log2e * 0x1p24f * __uint_as_float((254u - e) << 23);
                 unscale[nb][0] = __shfl_sync(0xffffffffu, f, 8 * t);
                 unscale[nb][1] = __shfl_sync(0xffffffffu, f, 8 * t + 4);
             }
@@ -430,7 +412,7 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
         if (nv > 0) {
 #pragma unroll
             for (int run = 0; run < 4; ++run) {
-                uint32_t w[2][NG], sb[2][NG], bb[2], ss[2];     // rows g and g + 8 of the run: codes, pairs, two groups' bases and scales as A operands
+                uint32_t w[2][NG], sb[2][NG], bb[2];            // rows g and g + 8 of the run: codes, pairs, two groups' bases as A operands
 #pragma unroll
                 for (int hh = 0; hh < 2; ++hh) {
                     const uint8_t* at = kbuf + run * 8 * D + hh * 4 * D + lane * (D / 8);
@@ -440,31 +422,26 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
                         *reinterpret_cast<uint4*>(&sb[hh][0]) = *reinterpret_cast<const uint4*>(ps);
                         const uint2 two = *reinterpret_cast<const uint2*>(ps + (t & 1) * 8);
                         bb[hh] = __byte_perm(two.x, two.y, 0x7632);
-                        ss[hh] = __byte_perm(two.x, two.y, 0x5410);
                     } else {
                         *reinterpret_cast<uint2*>(&w[hh][0]) = *reinterpret_cast<const uint2*>(at);
                         *reinterpret_cast<uint2*>(&sb[hh][0]) = *reinterpret_cast<const uint2*>(ps);
                         bb[hh] = __byte_perm(sb[hh][0], sb[hh][1], 0x7632);
-                        ss[hh] = __byte_perm(sb[hh][0], sb[hh][1], 0x5410);
                     }
                 }
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) {
-                    mma_bf16_new(s[nb][run], bb[0], bb[1], D == 128 ? bb[0] : 0u, D == 128 ? bb[1] : 0u, qb[nb][0], qb[nb][1]);
-                    mma_bf16(s[nb][run], ss[0], ss[1], D == 128 ? ss[0] : 0u, D == 128 ? ss[1] : 0u, qs[nb][0], qs[nb][1]);
-                }
+                for (int nb = 0; nb < NB; ++nb) mma_bf16_new(s[nb][run], bb[0], bb[1], D == 128 ? bb[0] : 0u, D == 128 ? bb[1] : 0u, qb[nb][0], qb[nb][1]);
 #pragma unroll
                 for (int grp = 0; grp < NG; ++grp) {
                     const float s0 = bf16_lo(sb[0][grp]), s1 = bf16_lo(sb[1][grp]);
-                    // fp16 0x6400 | u = 1024 + u; 0x5400 | u << 4 = 64 + u: two nibbles of a half word without a shift
+                    // a nibble by itself is a subnormal fp16, u 2^-24 or (one nibble up) u 2^-20
                     uint32_t a[2][4];
 #pragma unroll
                     for (int hh = 0; hh < 2; ++hh) {
                         const uint32_t w8 = w[hh][grp] >> 8;
-                        a[hh][0] = and_or(w[hh][grp], 0x000f000fu, 0x64006400u);
-                        a[hh][1] = and_or(w[hh][grp], 0x00f000f0u, 0x54005400u);
-                        a[hh][2] = and_or(w8, 0x000f000fu, 0x64006400u);
-                        a[hh][3] = and_or(w8, 0x00f000f0u, 0x54005400u);
+                        a[hh][0] = w[hh][grp] & 0x000f000fu;
+                        a[hh][1] = w[hh][grp] & 0x00f000f0u;
+                        a[hh][2] = w8 & 0x000f000fu;
+                        a[hh][3] = w8 & 0x00f000f0u;
                     }
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb) {
