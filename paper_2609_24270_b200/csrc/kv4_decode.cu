@@ -6,7 +6,8 @@
 //     O[d][q]   += sum_key V[key][d] P[key][q]                                    m16n8k16 MMA (fp16): 16 d x 8 heads x 16 keys
 // A code of K becomes an fp16 operand with one logic instruction: a nibble masked out of its word is the subnormal u 2^-24, or u 2^-20, and
 // the MMA takes subnormals as they are.  The bases' part comes from an MMA against sums over q kept in three bf16 parts (24 bits),
-// so scores carry no rounding besides the 32-bit sums.  V varies its scale along the contraction: its codes become 16 + u
+// so scores carry no rounding besides the 32-bit sums (in which a subnormal operand counts as 2^-14 when the MMA lines its products up: steps of 2^-24 of 1024 q s,
+// which scores do not feel; outputs would, so V's codes are not taken this way).  V varies its scale along the contraction: its codes become 16 + u
 // (0x4C00 | u << 6) and then s u + b with one multiply-add, in fp16 under a power of two that follows the largest value (rounded at 2^-12 of the group's
 // largest, or 2^-32 of the row's);
 // P, times 2^10, is fp16 as well.  (An fp8 MMA would take the codes as they are, but mma.sync on this chip converts fp8 operands to fp16
