@@ -711,7 +711,7 @@ ag_status ag_kv4_copy(const ag_kv4_pool* pool, const int32_t* from, const int32_
  * (a step of the quantisation is some 2^-4 of the group's largest), probabilities by 2^-12 of themselves or 2^-35 of the largest; sums and
  * softmax statistics are in 32 bits.
  *   Q, O       device, [B][H_q][D] bf16, 16-byte aligned; H_q a multiple of H_kv, H_q / H_kv <= 1024;
- *              O must not overlap Q.  B H_q max_pages <= 2^40
+ *              O must not overlap Q.  Queries of 2^120 and more may give NaN.  B H_q max_pages <= 2^40
  *   row        device [B], or NULL for row b (then B <= table->n_rows); a row outside the table, or an empty one, gives zeros
  *   table      lengths are clamped to 0 .. 64 max_pages; tokens whose page is not one of the pool's are left out
  *   workspace  device, 16-byte aligned, ag_attention_decode_kv4_workspace bytes (at most about 25 MB).  Its contents mean nothing between calls; calls that may run at the same time need one each
