@@ -107,6 +107,8 @@ __device__ __forceinline__ int row_tokens(const DecodeKv4Args& x, int b, int* ro
     return r >= 0 && r < x.n_rows ? min(max(x.len[r], 0), x.max_pages * KV4_PAGE) : 0;
 }
 __device__ __forceinline__ int pages_of(int tokens) { return (tokens + KV4_PAGE - 1) / KV4_PAGE; }
+// blocks that the line is cut for: at least a page for every warp
+__device__ __forceinline__ int blocks_of(const DecodeKv4Args& x, long long total) { return (int)min((long long)x.n_blocks, (total + DK_WARPS - 1) / DK_WARPS); }
 // the warp whose run holds place `at` of the line: run w begins at total * w / n
 __device__ __forceinline__ int run_holding(long long at, long long total, int n) { return (int)(((at + 1) * n - 1) / total); }
 
@@ -150,6 +152,7 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
     __shared__ int slot_ends[2 * DK_WARPS];        // bit 0: the part includes the unit's last page; bit 1: it lies in the workspace, not in the warp's buffer
     __shared__ __align__(16) float2 slot_stats[2 * DK_WARPS][8 * NB];
     __shared__ WarpWalk walk[DK_WARPS];
+    __shared__ long long line[2];                  // all pages of the line; the block's first place: needed again at the end, so they do not take registers
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     dep_wait();
     dep_release();
@@ -158,7 +161,7 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
     const int heads = x.H_kv * x.h_blocks;
     const int per = (x.B + DK_THREADS - 1) / DK_THREADS;
     long long total = 0, block_begin, block_end, first_unit_begin = 0;
-    int n_blocks = x.n_blocks, b, hh = 0, p = 0, np, len, row;     // request b, KV head and block hh, page p of np
+    int b, hh = 0, p = 0, np, len, row;     // request b, KV head and block hh, page p of np
     if (x.aligned) {
         b = blockIdx.x / heads;
         hh = blockIdx.x - b * heads;
@@ -199,7 +202,7 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
         if (threadIdx.x == DK_THREADS - 1) before[DK_THREADS] = add + inc;
         __syncthreads();
         total = before[DK_THREADS] * heads;
-        n_blocks = (int)min((long long)x.n_blocks, (total + DK_WARPS - 1) / DK_WARPS);      // at least a page for every warp
+        const int n_blocks = blocks_of(x, total);
         for (int i = blockIdx.x; i < x.B; i += gridDim.x) {         // requests without keys: zeros
             int r;
             if ((per > 1 ? row_tokens(x, i, &r) : tokens_of[i]) != 0) continue;
@@ -221,6 +224,10 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
         return tokens_of[i];
     };
     if (threadIdx.x < 2 * DK_WARPS) slot_unit[threadIdx.x] = -1;
+    if (threadIdx.x == 0) {
+        line[0] = total;
+        line[1] = block_begin;
+    }
     __syncthreads();
     const long long begin = block_begin + (block_end - block_begin) * warp / DK_WARPS;
     int left = (int)(block_begin + (block_end - block_begin) * (warp + 1) / DK_WARPS - begin);
@@ -308,7 +315,6 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
         fetch(1, src_next, nv_next);
     }
 
-    uint32_t qf[NB][NG][4];
     uint32_t qb[NB][2];
     float unscale[NB][2];                          // log2 e / (c sqrt D) of heads 2 t and 2 t + 1
     float o[NB][MT][4];
@@ -343,6 +349,7 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
             // 2^-24 of the largest.  Lane (g, t) holds head g, elements 32 grp + 8 t + {0, 4}, {1, 5}, {2, 6}, {3, 7}.  Even elements meet
             // 2^-24 u, odd ones, kept at a sixteenth, 2^-20 u (see the scores).  The bases meet the groups' sums of q, times 2^-24 c, 24 bits in
             // three bf16 parts.
+            uint32_t qf[NB][NG][4];
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
                 const int head = head0 + nb * 8 + g;
@@ -395,6 +402,12 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
                 unscale[nb][0] = __shfl_sync(0xffffffffu, f, 8 * t);
                 unscale[nb][1] = __shfl_sync(0xffffffffu, f, 8 * t + 4);
             }
+            __syncwarp();                          // every lane has read its rows; the operands take their place, and are fetched once a page
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int grp = 0; grp < NG; ++grp)
+                    *reinterpret_cast<uint4*>(qbuf + ((nb * NG + grp) * 32 + lane) * 16) = make_uint4(qf[nb][grp][0], qf[nb][grp][1], qf[nb][grp][2], qf[nb][grp][3]);
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
@@ -411,6 +424,11 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
         // (the runs behind the last key are computed with the others: what they hold does not count, see below)
         float s[NB][4][4];
         if (nv > 0) {
+            uint4 qf[NB][NG];
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int grp = 0; grp < NG; ++grp) qf[nb][grp] = *reinterpret_cast<const uint4*>(qbuf + ((nb * NG + grp) * 32 + lane) * 16);
 #pragma unroll
             for (int run = 0; run < 4; ++run) {
                 uint32_t w[2][NG], sb[2][NG], bb[2];            // rows g and g + 8 of the run: codes, pairs, two groups' bases as A operands
@@ -447,8 +465,8 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb) {
                         float acc[4];
-                        mma_f16_new(acc, a[0][0], a[1][0], a[0][1], a[1][1], qf[nb][grp][0], qf[nb][grp][1]);
-                        mma_f16(acc, a[0][2], a[1][2], a[0][3], a[1][3], qf[nb][grp][2], qf[nb][grp][3]);
+                        mma_f16_new(acc, a[0][0], a[1][0], a[0][1], a[1][1], qf[nb][grp].x, qf[nb][grp].y);
+                        mma_f16(acc, a[0][2], a[1][2], a[0][3], a[1][3], qf[nb][grp].z, qf[nb][grp].w);
                         s[nb][run][0] = fmaf(s0, acc[0], s[nb][run][0]);
                         s[nb][run][1] = fmaf(s0, acc[1], s[nb][run][1]);
                         s[nb][run][2] = fmaf(s1, acc[2], s[nb][run][2]);
@@ -459,7 +477,7 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
         }
         __syncwarp();                              // every lane has read K
         // ---- on to the next page: same unit, next head, next request that has any
-        // (the queries were read at the unit's first page, in front of a barrier since)
+        // (the queries' operands have been read as well)
         const bool ends = p + 1 == np;
         --left;
         nv_next = 0;
@@ -675,8 +693,9 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
             }
             if (left == 0 && warp == DK_WARPS - 1 && lane == 0 && !x.aligned) {      // the block's last page (no warp behind this one's has any)
                 int2 cross = make_int2(-1, 0);
-                if (!ends && at->now_begin >= block_begin)
-                    cross = make_int2(unit, run_holding(at->now_begin + at->now_pages - 1, total, n_blocks) - (int)blockIdx.x + 1);
+                const long long all = line[0];
+                if (!ends && at->now_begin >= line[1])
+                    cross = make_int2(unit, run_holding(at->now_begin + at->now_pages - 1, all, blocks_of(x, all)) - (int)blockIdx.x + 1);
                 x.crossing[blockIdx.x] = cross;
             }
             whole = true;                          // whatever comes next begins in this warp's run
