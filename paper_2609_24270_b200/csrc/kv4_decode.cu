@@ -13,7 +13,9 @@
 // P, times 2^10, is fp16 as well.  (An fp8 MMA would take the codes as they are, but mma.sync on this chip converts fp8 operands to fp16
 // first: measured, slower than the above.)
 //
-// Bound by memory: 1.25 D bytes per key and head.  A byte costs about ten times the arithmetic instructions of a bf16 cache's, so
+// Memory: 1.25 D bytes per key and head, read once.  A byte costs about ten times the arithmetic instructions of a bf16 cache's, and those bound
+// it: 61 % of the issue slots are used, the rest are fixed latencies of four warps a scheduler.  4 requests of 131072 keys, 32 query heads on 8, D = 128:
+// 132 us, 5.0 TB/s (0.76 of the measured copy); 128 requests of 200 to 1024 keys: 36.5 us, half of it until the first page is there and from the last on.  So
 // the operands are unpacked in registers, straight into the MMA's fragments - tcgen05.mma would want them in shared memory, one more
 // write and read of the unpacked (four times larger) tile.  The cache stores the codes in fragment order, so a warp's share of a
 // page is read with conflict-free vector loads.
@@ -22,8 +24,8 @@
 // once (two blocks of eight warps per SM).  A warp walks its run alone - one buffer each for K and V, refilled by 16-byte asynchronous
 // copies as soon as it has been read: K of the next page comes in during the softmax and V's products, V during the next page's scores, while
 // the SM's other warps are in other phases.  Uneven lengths, few long requests and many short ones are the same case.  Warps of a block that
-// share a unit put their parts together at the end (fragment order, through the workspace); a unit that goes beyond a block is left in one
-// part per block for a second kernel.
+// share a unit put their parts together at the end (fragment order, in the buffers that are free by then); a unit that goes beyond a block is left in
+// one part per block for a second kernel.
 #include <string.h>
 
 #include <algorithm>

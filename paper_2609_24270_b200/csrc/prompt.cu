@@ -12,8 +12,10 @@
 // While the softmax of one tile runs, the tensor core works on the other: PV_0(j), S_0(j + 1), PV_1(j), S_1(j + 1), ...  The reference
 // m of a row moves only when its maximum has grown by more than 8 (in log2 units): then, and only then, the outputs are rescaled.  P is
 // at most 2^8, sums and outputs are in 32 bits, so this changes no rounding.
-// Bound by the tensor pipe and, as closely, by the exponentials: a pair of 128 x 128 tiles takes 2 x 1024 cycles of MMAs (D = 128) and 2 x 1024
-// cycles of the special-function units (16 per cycle and SM).
+// The tensor pipe and, as closely, the exponentials: a pair of 128 x 128 tiles takes 2 x 1024 cycles of MMAs (D = 128) and 2 x 1024 cycles of the
+// special-function units (16 per cycle and SM).  What bounds it is a tile's own chain, 1760 cycles of softmax and 1280 until its next scores are there;
+// more tiles in flight do not fit tensor memory.  8192 tokens, 32 query heads on 8, D = 128, causal: 445 us, 1235 TFLOP/s (0.74 of the
+// measured product of matrices; 517 us once the power cap holds); D = 64: 384.
 #include <string.h>
 
 #include <algorithm>
@@ -32,7 +34,7 @@ constexpr int PA_MAXSEQ = 1024;           // sequences of one launch
 constexpr int PA_CONSUMERS = 8 + 3;       // warps that read the unit: softmax, MMA, K, V
 constexpr float PA_LAZY = 8.f;
 // One pair in eight takes its exponentials from the multiply-add units (exp2_cubic): at 8192 tokens x 32 heads, D = 128, 464 us with none,
-// 456 with one, 459 with two, 475 with three; D = 64: 440, 396, 449, 446.
+// 456 with one, 459 with two, 475 with three; D = 64: 440, 396, 449, 446 (figures of that step).
 constexpr int PA_CUBIC = 1;
 
 struct PromptArgs {
@@ -141,7 +143,8 @@ __device__ __forceinline__ f32x2 exp2_cubic(f32x2 v) {
     unpack2(t, t0, t1);
     return mul2(q, pack2(__uint_as_float(__float_as_uint(t0) << 23), __uint_as_float(__float_as_uint(t1) << 23)));
 }
-// 32 bytes: in one store where the address allows
+// 32 bytes: in one store where the address allows (lanes are rows apart, and the other warps' barriers queue behind such stores: 4 units of one
+// key tile a block took 38.3 us with 16-byte stores, 35.3 with these)
 __device__ __forceinline__ void store32(uint16_t* to, const uint32_t (&v)[8], bool wide) {
     if (wide) {
         asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
