@@ -109,6 +109,26 @@ def test_packed_tokens_beyond_four_gigabytes():
     assert (O[lo:hi, Hq * D:] == 7.0).all() and (O[lo - 1] == 7.0).all() and (O[hi:] == 7.0).all()
 
 
+@pytest.mark.parametrize("offset,pad", [(0, 0), (8, 0), (0, 8), (8, 24), (16, 16)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_outputs_on_sixteen_byte_boundaries(D, offset, pad):
+    """Rows of O that begin on 16 but not on 32 bytes: what lies between them stays."""
+    n, Hq, Hkv = 150, 6, 2
+    Q, K, V = rows(n, Hq, D, 1), rows(n, Hkv, D, 2), rows(n, Hkv, D, 3)
+    dQ, dK, dV, off = dev(Q), dev(K), dev(V), dev(np.array([0, 33, n], np.int32))
+    width = Hq * D + pad
+    buf = torch.full((offset + n * width + 8,), 7.0, dtype=torch.bfloat16, device="cuda")
+    plan = plan_for()
+    torch.cuda.synchronize()
+    ag.attention_prompt(dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), buf.data_ptr() + 2 * offset, Hq, Hkv, D, off.data_ptr(), None, 2, n, n, plan, o_stride=width)
+    torch.cuda.synchronize()
+    assert plan.last_status() == ag.AG_OK
+    O = buf[offset:offset + n * width].view(n, width)
+    want, mass = oa.prompt(Q, K, V, [0, 33, n])
+    check_prompt(O[:, :Hq * D].float().cpu().numpy().astype(np.float64).reshape(n, Hq, D), want, mass)
+    assert (buf[:offset] == 7.0).all() and (O[:, Hq * D:] == 7.0).all() and (buf[offset + n * width:] == 7.0).all()
+
+
 def test_more_requests_than_threads():
     """600 requests (the blocks count several requests a thread), every fifth without keys, and rows in another order with strangers among them."""
     rng = np.random.default_rng(6)
