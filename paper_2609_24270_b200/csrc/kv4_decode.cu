@@ -153,6 +153,8 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
     __shared__ int slot_unit[2 * DK_WARPS];        // units that a warp has only a part of: one that began before its run, one that goes on behind it
     __shared__ int slot_ends[2 * DK_WARPS];        // bit 0: the part includes the unit's last page; bit 1: it lies in the workspace, not in the warp's buffer
     __shared__ __align__(16) float2 slot_stats[2 * DK_WARPS][8 * NB];
+    __shared__ float2 joint_stats[2 * DK_WARPS][8 * NB];           // of the unit that a part belongs to, over the block's parts
+    __shared__ __align__(8) float slot_weight[2 * DK_WARPS][8 * NB];
     __shared__ WarpWalk walk[DK_WARPS];
     __shared__ long long line[2];                  // all pages of the line; the block's first place: needed again at the end, so they do not take registers
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -715,6 +717,27 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
     const unsigned far = __ballot_sync(0xffffffffu, slot_u >= 0 && (slot_ends[lane % (2 * DK_WARPS)] & 2));
     const int prev_u = __shfl_sync(0xffffffffu, slot_u, in_front ? 31 - __clz(in_front) : 0);
     const unsigned firsts = __ballot_sync(0xffffffffu, slot_u >= 0 && !(in_front && prev_u == slot_u));
+    const unsigned same = __match_any_sync(0xffffffffu, slot_u) & there;            // the parts of the lane's slot's unit
+    static_assert(2 * DK_WARPS * 8 * NB <= DK_THREADS, "a thread for every part and head");
+    {
+        const int slot = threadIdx.x / (8 * NB), head = threadIdx.x % (8 * NB);
+        const unsigned parts = __shfl_sync(0xffffffffu, same, slot % (2 * DK_WARPS));
+        if (slot < 2 * DK_WARPS && (parts >> slot & 1)) {
+            float top = -INFINITY, sum = 0.f;
+            for (unsigned c = parts; c; c &= c - 1) {
+                const float2 st = slot_stats[__ffs(c) - 1][head];
+                if (st.y != 0.f) top = fmaxf(top, st.x);
+            }
+            for (unsigned c = parts; c; c &= c - 1) {
+                const float2 st = slot_stats[__ffs(c) - 1][head];
+                sum += part_weight(st.x, st.y, top);
+            }
+            const float2 st = slot_stats[slot][head];
+            slot_weight[slot][head] = sum == 0.f ? 0.f : part_weight(st.x, st.y, top) / sum;
+            joint_stats[slot][head] = make_float2(top, sum);
+        }
+    }
+    __syncthreads();
     const int n_items = __popc(firsts) * MT, k1 = n_items * (warp + 1) / DK_WARPS;       // the fragments of all units in one line, cut into equal runs
     for (int k = n_items * warp / DK_WARPS; k < k1;) {
         unsigned rest = firsts;
@@ -726,35 +749,22 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
         const size_t joint = 2 * DK_WARPS * (size_t)x.n_blocks + 2 * (size_t)blockIdx.x + (starts ? 1 : 0);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-            float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
-            for (unsigned c = parts; c; c &= c - 1) {
-                const float4 st = *reinterpret_cast<const float4*>(&slot_stats[__ffs(c) - 1][nb * 8 + 2 * t]);
-                if (st.y != 0.f) m0 = fmaxf(m0, st.x);
-                if (st.w != 0.f) m1 = fmaxf(m1, st.z);
-            }
-            for (unsigned c = parts; c; c &= c - 1) {
-                const float4 st = *reinterpret_cast<const float4*>(&slot_stats[__ffs(c) - 1][nb * 8 + 2 * t]);
-                l0 += part_weight(st.x, st.y, m0);
-                l1 += part_weight(st.z, st.w, m1);
-            }
-            const float r0 = l0 == 0.f ? 0.f : 1.f / l0, r1 = l1 == 0.f ? 0.f : 1.f / l1;
             float4 v[MT];
 #pragma unroll
             for (int i = 0; i < MT; ++i) v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
             for (unsigned c = parts; c; c &= c - 1) {
                 const int slot = __ffs(c) - 1;
-                const float4 st = *reinterpret_cast<const float4*>(&slot_stats[slot][nb * 8 + 2 * t]);
+                const float2 w = *reinterpret_cast<const float2*>(&slot_weight[slot][nb * 8 + 2 * t]);     // (a weight of zero: whatever stands there)
                 const float4* from = (far >> slot & 1 ? x.part + (2 * DK_WARPS * (size_t)blockIdx.x + slot) * NB * MT * 32
                                                       : reinterpret_cast<const float4*>(smem + (slot >> 1) * kv4_head_bytes(D))) + nb * MT * 32 + lane;
-                const float w0 = part_weight(st.x, st.y, m0) * r0, w1 = part_weight(st.z, st.w, m1) * r1;      // (a weight of zero: whatever stands there)
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
                     if (i < i0 || i >= i1) continue;
                     const float4 u = from[i * 32];
-                    v[i].x += w0 == 0.f ? 0.f : w0 * u.x;
-                    v[i].y += w1 == 0.f ? 0.f : w1 * u.y;
-                    v[i].z += w0 == 0.f ? 0.f : w0 * u.z;
-                    v[i].w += w1 == 0.f ? 0.f : w1 * u.w;
+                    v[i].x += w.x == 0.f ? 0.f : w.x * u.x;
+                    v[i].y += w.y == 0.f ? 0.f : w.y * u.y;
+                    v[i].z += w.x == 0.f ? 0.f : w.x * u.z;
+                    v[i].w += w.y == 0.f ? 0.f : w.y * u.w;
                 }
             }
             if (starts && (with_end & parts)) {
@@ -767,7 +777,7 @@ __global__ void __launch_bounds__(DK_THREADS, NB == 1 ? 2 : 1) k_attn_decode_kv4
 #pragma unroll
                 for (int i = 0; i < MT; ++i)
                     if (i >= i0 && i < i1) x.part[((joint * NB + nb) * MT + i) * 32 + lane] = v[i];
-                if (i0 == 0 && g == 0) *reinterpret_cast<float4*>(&x.stats[joint * 8 * NB + nb * 8 + 2 * t]) = make_float4(m0, l0, m1, l1);
+                if (i0 == 0 && lane < 8) x.stats[joint * 8 * NB + nb * 8 + lane] = joint_stats[own][nb * 8 + lane];
             }
         }
     }
