@@ -15,7 +15,7 @@
 //
 // Memory: 1.25 D bytes per key and head, read once.  A byte costs about ten times the arithmetic instructions of a bf16 cache's, and those bound
 // it: 61 % of the issue slots are used, the rest are fixed latencies of four warps a scheduler.  4 requests of 131072 keys, 32 query heads on 8, D = 128:
-// 132 us, 5.0 TB/s (0.76 of the measured copy); 128 requests of 200 to 1024 keys: 36.5 us, half of it until the first page is there and from the last on.  So
+// 131 us, 5.0 TB/s (0.77 of the measured copy); 128 requests of 200 to 1024 keys: 35 us, half of it until the first page is there and from the last on.  So
 // the operands are unpacked in registers, straight into the MMA's fragments - tcgen05.mma would want them in shared memory, one more
 // write and read of the unpacked (four times larger) tile.  The cache stores the codes in fragment order, so a warp's share of a
 // page is read with conflict-free vector loads.
@@ -921,7 +921,7 @@ extern "C" ag_status attention_decode_kv4(const void* Q, const ag_kv4_pool* pool
     AG_CUDA(cudaLaunchKernelEx(&cfg, kernel, x));
     count_launch();
     if (s.aligned) return AG_OK;
-    // Side by side: 2 parts where a unit goes over few blocks (smaller blocks come up sooner: 128 requests of some 850 keys take 47.3 us with 2, 50.3 with 4),
+    // Side by side: 2 parts where a unit goes over few blocks (smaller blocks come up sooner: 128 requests of some 850 keys took 47.3 us with 2, 50.3 with 4 at that step),
     // 4 where there are more blocks than that (1 request of 131072 keys: 61.5 and 55.6)
     cfg.blockDim = dim3(s.nb * pool->D * 2, s.units * 4 >= s.n_blocks ? 2 : dk_join_lanes(pool->D, s.nb));
     cfg.dynamicSmemBytes = 0;
