@@ -670,7 +670,8 @@ ag_status ag_kv4_load(const ag_kv4_pool* pool, const int32_t* slot, int64_t n_to
 /*
  * ag_kv4_extend - make room for new tokens: row[i] grows by new_off[i + 1] - new_off[i] tokens (new_off as the q_off of attention_prompt_persistent).
  * Free pages are dealt in ascending order, request by request; a request whose pages are not all there (counting those of the
- * requests in front of it, granted or not) is refused and its row stays as it is.  Refused too: a row outside the table, a row named
+ * requests in front of it, granted or not) is refused and its row stays as it is; one that needs no page, because its tokens fit the row's last one
+ * or it has none, is not refused for want of pages.  Refused too: a row outside the table, a row named
  * earlier in the same call, a length that max_pages cannot hold.  Never reports an error for these: ok[i] = 0.
  *   row, ok  device [n], new_off device [n + 1] ascending;  1 <= n <= AG_KV4_MAX_ROWS (n = 0 only without tokens)
  *   slot     device [n_tokens], out: the slot of token j (of request i when new_off[i] <= j < new_off[i + 1]), -1 where its request was
@@ -682,7 +683,7 @@ ag_status ag_kv4_extend(const ag_kv4_pool* pool, const ag_kv4_table* table, cons
  * ag_kv4_fork - row dst[i], empty so far, becomes a copy of row src[i]: it shares the full pages (their counts go up) and gets a copy of the
  * open last page, so that both can grow on their own.  The tables are read as they were before the call.  Refused (ok[i] = 0, nothing
  * changes): a row outside the table, dst[i] not empty, equal to src[i] or named earlier in the call, no free page for the copy (dealt
- * as in ag_kv4_extend).  n <= AG_KV4_MAX_ROWS.
+ * as in ag_kv4_extend; a row that ends with a full page needs none).  n <= AG_KV4_MAX_ROWS.
  */
 ag_status ag_kv4_fork(const ag_kv4_pool* pool, const ag_kv4_table* table, const int32_t* src, const int32_t* dst, int n, int32_t* ok,
                       void* cuda_stream);

@@ -111,11 +111,12 @@ def _pages(n):
 
 
 def _grant(refs, wants):
-    """Pages for a list of wants: free pages ascending, request by request, all or nothing; refused requests keep their place."""
+    """Pages for a list of wants: free pages ascending, request by request, all or nothing; refused requests keep their place.  Who wants none gets none,
+    whether there are any or not."""
     free = [p for p in range(len(refs)) if refs[p] <= 0]
     at, out = 0, []
     for w in wants:
-        out.append(free[at:at + w] if at + w <= len(free) else None)
+        out.append(free[at:at + w] if w == 0 or at + w <= len(free) else None)
         at += w
     for pages in out:
         for p in pages or []:

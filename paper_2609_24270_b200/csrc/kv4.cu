@@ -239,7 +239,8 @@ struct TableArgs {
 };
 
 // Request i (thread i) wants need[i] pages; free pages are dealt in ascending order to the requests in order, request i getting the
-// ranks before[i] .. before[i] + need[i] - 1.  A request is granted when all of them exist.  Ends with the pages entered in the
+// ranks before[i] .. before[i] + need[i] - 1.  A request is granted when all of them exist; one that needs none always is (a token in a page that the
+// row owns does not wait for another row's page).  Ends with the pages entered in the
 // tables (column first[i] on) and counted.  Returns whether this thread's request is granted.
 // Every warp walks over its thirty-second of the pages, neighbouring lanes at neighbouring counts: 128 rows grow in 4.2 us among 2048 pages,
 // 7.5 among 65536 (39 with neighbouring counts in one thread's hands).
@@ -291,7 +292,7 @@ __device__ inline bool grant_pages(const TableArgs& t, int n, int need, int firs
             }
         }
     }
-    return before + need <= total_free;
+    return need == 0 || before + need <= total_free;
 }
 
 // Whether request i is the first of the call that names `key` (a row; -1: none).  Open addressing in shared memory, twice as many places as requests.
