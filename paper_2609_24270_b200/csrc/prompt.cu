@@ -16,6 +16,11 @@
 // special-function units (16 per cycle and SM).  What bounds it is a tile's own chain, 1760 cycles of softmax and 1280 until its next scores are there;
 // more tiles in flight do not fit tensor memory.  8192 tokens, 32 query heads on 8, D = 128, causal: 445 us, 1235 TFLOP/s (0.74 of the
 // measured product of matrices; 517 us once the power cap holds); D = 64: 384.
+//
+// A probability of zero times a later token's infinity or NaN, in a key tile that rows share, spoils a row that does not see that token.  A causal unit
+// with a result that is not finite is therefore run a second time, with the values that are not finite taken as zeros while the first of
+// each kind is noted for every column: what a row sees of them decides what it adds to the row (second pass, below).  Twice the work and
+// the scan of the value tiles, for such units only.
 #include <string.h>
 
 #include <algorithm>
@@ -55,8 +60,10 @@ struct PromptCtl {
     uint64_t kv_full[PA_STAGES], kv_empty[PA_STAGES];
     uint64_t s_full[2], p_full[2], pv_done[2];
     uint64_t unit_full, unit_empty;
-    uint64_t tail, mma_drain;
-    int unit[4];                          // sequence (in order of work), KV head, first token; sequence -1: the end
+    uint64_t tail, mma_drain, scanned[2];
+    int unit[4];                          // sequence (in order of work; -1: the end), KV head, first token, 1: second pass
+    uint32_t spoilt[4];                   // k + 1 in place k mod 4: the k-th unit had a result that is not finite
+    int first_odd[2][3][128];             // second pass, units in turn: the first key with a NaN, an infinity, a negative one in the column
     uint32_t tmem_base;
     int abort_flag, member, slot;
     int blocks_before[PA_MAXSEQ + 1];     // units of one head in front of the i-th sequence of work
@@ -170,74 +177,56 @@ __device__ __forceinline__ int key_tiles(const PromptArgs& x, const PromptSeq& s
     return max(0, last_key(x, s, min(first + x.tpt, s.q_len) - 1) + PA_N) / PA_N;
 }
 
-// A row whose result is not finite, computed again over exactly the keys it sees when a key that it does not see, in the tiles that it shares
-// with rows that do, holds a value that is not finite (a probability of zero times it has spoilt the row).  One warp, its lanes side by side
-// on the row's elements, in 32 bits; reached by such rows only.  (One thread a row took so long that the other warps' waits could run out.)
+// true for every thread of the block when one of them says so; all come here the same number of times
+__device__ __forceinline__ bool block_any(bool mine) {
+    uint32_t r;
+    asm volatile(
+        "{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.or.pred q, 1, %2, p;\n selp.u32 %0, 1, 0, q;\n}"
+        : "=r"(r) : "r"((uint32_t)mine), "n"(PA_THREADS) : "memory");
+    return r != 0;
+}
+
+// Second pass: a landed tile of values (64-column blocks of 128 rows of 128 bytes, 16-byte pieces swizzled by the row), rows 0 .. valid - 1 are keys
+// key0 .. of the sequence.  One warp, a lane keeps to eight columns: what is not finite becomes zero, the first of each kind is noted by column.
+// Two elements a word: without their signs, 0x80 more makes bit 15 of what is not finite, 0x7f more that of a NaN.
 template <int D>
-__device__ __noinline__ void repair_row(const PromptArgs& x, const PromptSeq& s, int tok, int head, int last, int tiles) {
-    constexpr int E = D / 32, U = 8;
-    const int lane = threadIdx.x & 31;
-    const uint16_t* k0 = x.K + (size_t)s.k0 * x.k_stride + (size_t)(head / x.G) * D + lane * E;
-    const uint16_t* v0 = x.V + (size_t)s.k0 * x.v_stride + (size_t)(head / x.G) * D + lane * E;
-    auto load = [](const uint16_t* from, float (&v)[E]) {
-        uint32_t w[E / 2];
-        if (E == 4) *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(from);
-        else w[0] = *reinterpret_cast<const uint32_t*>(from);
+__device__ __forceinline__ void take_out_odd(uint8_t* tile, int valid, int key0, int (*first_odd)[128]) {
+    const int lane = threadIdx.x & 31, piece = lane & 7;
+#pragma unroll 1
+    for (int d = 0; d < D / 64; ++d) {
+        uint32_t noted[3][4] = {};                 // by this lane, of this tile
+#pragma unroll 1
+        for (int row = lane >> 3; row < valid; row += 4) {
+            uint4* at = reinterpret_cast<uint4*>(tile + d * (PA_N * 128) + row * 128 + ((piece ^ (row & 7)) << 4));
+            const uint4 v = *at;
+            uint32_t w[4] = {v.x, v.y, v.z, v.w}, kind[3][4], any = 0, fresh = 0;
 #pragma unroll
-        for (int i = 0; i < E; ++i) v[i] = __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
-    };
-    bool foreign = false;
-    for (int j = last + 1; j < min(tiles * PA_N, s.k_len); ++j) {
-        float v[E];
-        load(v0 + (size_t)j * x.v_stride, v);
+            for (int k = 0; k < 4; ++k) any |= (w[k] & 0x7fff7fffu) + 0x00800080u;
+            if (!(any & 0x80008000u)) continue;
 #pragma unroll
-        for (int i = 0; i < E; ++i) foreign |= !(fabsf(v[i]) <= 3.4e38f);
-    }
-    if (!__any_sync(0xffffffffu, foreign)) return;
-    float q[E], o[E], m = -INFINITY, l = 0.f;
-    load(x.Q + (size_t)(s.q0 + tok) * x.q_stride + (size_t)head * D + lane * E, q);
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t t = w[k] & 0x7fff7fffu, bad = (t + 0x00800080u) & 0x80008000u;
+                kind[0][k] = (t + 0x007f007fu) & 0x80008000u;
+                kind[1][k] = (bad ^ kind[0][k]) & ~w[k];
+                kind[2][k] = (bad ^ kind[0][k]) & w[k];
+                w[k] &= ~((bad >> 15) * 0xffffu);
 #pragma unroll
-    for (int i = 0; i < E; ++i) o[i] = 0.f;
-    for (int j0 = 0; j0 <= last; j0 += U) {
-        float k[U][E], v[U][E], a[U], top = m;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int j = min(j0 + u, last);
-            load(k0 + (size_t)j * x.k_stride, k[u]);
-            load(v0 + (size_t)j * x.v_stride, v[u]);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            a[u] = 0.f;
-#pragma unroll
-            for (int i = 0; i < E; ++i) a[u] = fmaf(q[i], k[u][i], a[u]);
-        }
-#pragma unroll
-        for (int w = 1; w < 32; w <<= 1)
-#pragma unroll
-            for (int u = 0; u < U; ++u) a[u] += __shfl_xor_sync(0xffffffffu, a[u], w);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            a[u] *= x.scale_log2e;
-            if (j0 + u <= last) top = fmaxf(top, a[u]);
-        }
-        const float ref = top == -INFINITY ? 0.f : top, f = exp2_fast(m - ref);
-        l *= f;
-#pragma unroll
-        for (int i = 0; i < E; ++i) o[i] *= f;
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (j0 + u <= last) {
-                const float w = exp2_fast(a[u] - ref);
-                l += w;
-#pragma unroll
-                for (int i = 0; i < E; ++i) o[i] = fmaf(w, v[u][i], o[i]);
+                for (int i = 0; i < 3; ++i) {
+                    kind[i][k] &= ~noted[i][k];
+                    noted[i][k] |= kind[i][k];
+                    fresh |= kind[i][k];
+                }
             }
-        m = top;
-    }
-    uint16_t* out = x.O + (size_t)(s.q0 + tok) * x.o_stride + (size_t)head * D + lane * E;
+            if (fresh) {
 #pragma unroll
-    for (int i = 0; i < E; i += 2) *reinterpret_cast<uint32_t*>(out + i) = bf16_pair(l == 0.f ? 0.f : o[i] / l, l == 0.f ? 0.f : o[i + 1] / l);
+                for (int i = 0; i < 3; ++i)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (kind[i][k >> 1] & (k & 1 ? 0x80000000u : 0x8000u)) atomicMin(&first_odd[i][d * 64 + piece * 8 + k], key0 + row);
+            }
+            *at = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
 }
 
 template <int D>
@@ -268,6 +257,8 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         }
         mbar_init(smem_u32(&ctl->unit_full), 1);
         mbar_init(smem_u32(&ctl->unit_empty), PA_CONSUMERS);
+        for (int i = 0; i < 4; ++i) ctl->spoilt[i] = 0xffffffffu;
+        for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&ctl->scanned[i]), 1);
         mbar_init(smem_u32(&ctl->tail), 1);
         mbar_init(smem_u32(&ctl->mma_drain), 1);
         mbar_fence_init();
@@ -357,7 +348,7 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     const uint32_t idesc_s = make_idesc_bf16(PA_M, PA_N, 0, 0), idesc_o = make_idesc_bf16(PA_M, D, 0, 1);
 
     // the next unit: warp-uniform; false when a wait ran out.  Every consumer warp reads every unit once.
-    auto next_unit = [&](uint32_t it, int& seq, int& head, int& t0) -> bool {
+    auto next_unit = [&](uint32_t it, int& seq, int& head, int& t0, int& second) -> bool {
         if (!mbar_wait_all(smem_u32(&ctl->unit_full), it & 1, abort_flag, limit)) {
             if (lane == 0) report_timeout(p, 3);
             return false;
@@ -365,9 +356,20 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         seq = ctl->unit[0];
         head = ctl->unit[1];
         t0 = ctl->unit[2];
+        second = ctl->unit[3];
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&ctl->unit_empty));
         return true;
+    };
+
+    // After the end (unit `it`) every warp comes here, and on unless the unit in front of it has to be run once more.  A warp that gave up comes
+    // here too, once, and ends it for all.
+    bool over = false;
+    auto all_done = [&](uint32_t it) {
+        tc_fence_before();
+        __syncwarp();
+        over = block_any(false) || *reinterpret_cast<volatile uint32_t*>(&ctl->spoilt[(it - 1) & 3]) != it;
+        return over;
     };
 
     // The softmax threads hold a row of 128 scores: 2 x 128 x 208 + 128 x 88 registers, as many as 384 x 168 at launch.
@@ -379,62 +381,80 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         // planned SMs that never got a block (whose slots are then taken, so that the plan counts as manned).
         const int n_units = ctl->blocks_before[x.n_seq] * x.H_kv;
         uint32_t nq[2] = {0, 0};
-        int phase = 0, scan = 0;
+        int phase = 0, scan = 0, u = -1;
+        bool in_hand = false;                      // u is the next unit (-1: there is none)
+        int3 last1 = make_int3(-1, 0, 0), last2 = last1;       // the two units before
         for (uint32_t it = 0;; ++it) {
-            int u = -1;
-            if (phase == 0) {
-                phase = 1;
-                if (ctl->slot < n_units) u = ctl->slot;
-            }
-            if (u < 0 && phase == 1) {
-                if (n_units > p.b) {
-                    if (lane == 0) u = pop_queue(&p.ctrl->die_head[0], p.epoch, n_units - p.b);
-                    u = __shfl_sync(0xffffffffu, u, 0);
-                    if (u >= 0) u += p.b;
+            if (!in_hand) {
+                u = -1;
+                if (phase == 0) {
+                    phase = 1;
+                    if (ctl->slot < n_units) u = ctl->slot;
                 }
-                if (u < 0) phase = 2;
-            }
-            while (u < 0 && scan < p.b) {
-                const int i = scan + lane;
-                const unsigned open = __ballot_sync(0xffffffffu, i < p.b && !slot_taken(p, i));
-                if (!open) {
-                    scan += 32;
-                    continue;
+                if (u < 0 && phase == 1) {
+                    if (n_units > p.b) {
+                        if (lane == 0) u = pop_queue(&p.ctrl->die_head[0], p.epoch, n_units - p.b);
+                        u = __shfl_sync(0xffffffffu, u, 0);
+                        if (u >= 0) u += p.b;
+                    }
+                    if (u < 0) phase = 2;
                 }
-                const int slot = scan + __ffs(open) - 1;
-                int got = 0;
-                if (lane == 0) got = atomicMax(&p.claimed[slot], p.epoch) < p.epoch;
-                got = __shfl_sync(0xffffffffu, got, 0);
-                if (got && slot < n_units) u = slot;
-                scan = slot + 1;
+                while (u < 0 && scan < p.b) {
+                    const int i = scan + lane;
+                    const unsigned open = __ballot_sync(0xffffffffu, i < p.b && !slot_taken(p, i));
+                    if (!open) {
+                        scan += 32;
+                        continue;
+                    }
+                    const int slot = scan + __ffs(open) - 1;
+                    int got = 0;
+                    if (lane == 0) got = atomicMax(&p.claimed[slot], p.epoch) < p.epoch;
+                    got = __shfl_sync(0xffffffffu, got, 0);
+                    if (got && slot < n_units) u = slot;
+                    scan = slot + 1;
+                }
             }
-            int seq = -1, head = 0, t0 = 0;
+            int3 now = make_int3(-1, 0, 0);        // sequence, KV head, first token
             if (u >= 0) {
                 const int e = u / x.H_kv;
-                head = u - e * x.H_kv;
+                now.y = u - e * x.H_kv;
                 int a = 0, b = x.n_seq - 1;
                 while (a < b) {
                     const int m = (a + b + 1) >> 1;
                     if (ctl->blocks_before[m] <= e) a = m; else b = m - 1;
                 }
-                seq = a;
-                t0 = (ctl->blocks_before[a + 1] - 1 - e) * block_tokens;
+                now.x = a;
+                now.z = (ctl->blocks_before[a + 1] - 1 - e) * block_tokens;
             }
-            int ok = 1;
-            if (lane == 0 && !mbar_wait_idle(smem_u32(&ctl->unit_empty), (it & 1) ^ 1, abort_flag, limit)) {
-                report_timeout(p, 1);
-                ok = 0;
+            // Once everybody has read the unit before this one, the outputs of the one before that are out.
+            int ok = 1, second = 0;
+            if (lane == 0) {
+                if (!mbar_wait_idle(smem_u32(&ctl->unit_empty), (it & 1) ^ 1, abort_flag, limit)) {
+                    report_timeout(p, 1);
+                    ok = 0;
+                }
+                second = it >= 2 && *reinterpret_cast<volatile uint32_t*>(&ctl->spoilt[(it - 2) & 3]) == it - 1;
             }
             ok = __shfl_sync(0xffffffffu, ok, 0);
+            second = __shfl_sync(0xffffffffu, second, 0);
             if (!ok) break;
+            if (second) now = last2;
+            in_hand = second || u < 0;
+            last2 = last1;
+            last1 = now;
+            const int seq = now.x, t0 = now.z, head = now.y;
             if (lane == 0) {
                 ctl->unit[0] = seq;
                 ctl->unit[1] = head;
                 ctl->unit[2] = t0;
+                ctl->unit[3] = second;
                 mbar_arrive(smem_u32(&ctl->unit_full));
             }
             __syncwarp();
-            if (seq < 0) break;
+            if (seq < 0) {
+                if (all_done(it)) break;
+                continue;
+            }
             const PromptSeq s = ctl->seq[seq];
             for (int w = 0; w < 2; ++w) {
                 if (key_tiles(x, s, t0, w) == 0) continue;
@@ -461,17 +481,26 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         uint32_t n = 0, n_tail = 0;                // tiles of this kind so far
         bool ok = true;
         for (uint32_t it = 0; ok; ++it) {
-            int seq, head, t0;
-            if (!next_unit(it, seq, head, t0) || seq < 0) break;
+            int seq, head, t0, second;
+            if (!next_unit(it, seq, head, t0, second)) break;
+            if (seq < 0) {
+                if (all_done(it)) break;
+                continue;
+            }
             const PromptSeq s = ctl->seq[seq];
             const int tiles = max(key_tiles(x, s, t0, 0), key_tiles(x, s, t0, 1));
+            const bool scan = which && second;
+            if (scan) {                            // (the unit before the one before has been read by everybody: its notes are free)
+                for (int i = lane; i < 3 * 128; i += 32) ctl->first_odd[it & 1][0][i] = 0x7fffffff;
+                __syncwarp();
+            }
             for (int j = 0; j < tiles && ok; ++j, ++n) {
                 const uint32_t st = 2 * (n & 1) + which, ph = ((n >> 1) & 1) ^ 1;
                 const uint32_t bar = smem_u32(&ctl->kv_full[st]), dst = kv_base + st * C::kv_bytes;
-                const int valid = s.k_len - j * PA_N;
+                const int valid = min(s.k_len - j * PA_N, PA_N);
                 // The rows behind a sequence's last key belong to the next sequence (or to nothing).  Their scores are masked, but a
                 // probability of zero must not meet an infinite or NaN value: the last tile's surplus value rows are cleared.
-                const bool clear = which && valid < PA_N;
+                const bool clear = which && (valid < PA_N || scan);
                 if (!mbar_wait_all(smem_u32(&ctl->kv_empty[st]), ph, abort_flag, limit)) {
                     if (lane == 0) report_timeout(p, 2);
                     ok = false;
@@ -492,6 +521,7 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                     }
                     ++n_tail;
                     uint8_t* tile = smem + (dst - base);
+                    if (scan) take_out_odd<D>(tile, valid, j * PA_N, ctl->first_odd[it & 1]);
 #pragma unroll
                     for (int d = 0; d < D / 64; ++d)
                         for (int i = valid * 128 + lane * 16; i < PA_N * 128; i += 512) *reinterpret_cast<uint4*>(tile + d * (PA_N * 128) + i) = make_uint4(0, 0, 0, 0);
@@ -500,6 +530,7 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                     if (lane == 0) mbar_arrive(bar);
                 }
             }
+            if (scan && ok && lane == 0) mbar_arrive(smem_u32(&ctl->scanned[it & 1]));
         }
         if (!ok && lane == 0) {
             // gave up: linger (bounded) so that copies already in flight land before the block leaves
@@ -534,8 +565,12 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
             __syncwarp();
         };
         for (uint32_t it = 0; ok; ++it) {
-            int seq, head, t0;
-            if (!next_unit(it, seq, head, t0) || seq < 0) break;
+            int seq, head, t0, second;
+            if (!next_unit(it, seq, head, t0, second)) break;
+            if (seq < 0) {
+                if (all_done(it)) break;
+                continue;
+            }
             const PromptSeq s = ctl->seq[seq];
             const int n0 = key_tiles(x, s, t0, 0), n1 = key_tiles(x, s, t0, 1), nt = max(n0, n1);
             if (nt == 0) continue;
@@ -612,10 +647,15 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         const int row_tok = r / x.G, row_head = r - row_tok * x.G;
         const bool wide = (((uintptr_t)x.O | (uintptr_t)(2 * x.o_stride)) & 31) == 0;
         uint32_t ns = 0;                           // score tiles so far = value products so far
+        uint32_t scans = 0;                        // parity of the second passes so far, of even units and of odd ones
         bool ok = true;
         for (uint32_t it = 0; ok; ++it) {
-            int seq, head, t0;
-            if (!next_unit(it, seq, head, t0) || seq < 0) break;
+            int seq, head, t0, second;
+            if (!next_unit(it, seq, head, t0, second)) break;
+            if (seq < 0) {
+                if (all_done(it)) break;
+                continue;
+            }
             const PromptSeq s = ctl->seq[seq];
             const int n = key_tiles(x, s, t0, w);
             const int tok = t0 + w * x.tpt + row_tok;
@@ -707,6 +747,8 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
             }
             if (!ok) break;
             uint16_t* out = x.O + (size_t)(s.q0 + tok) * x.o_stride + (size_t)(head * x.G + row_head) * D;
+            const uint32_t scan_parity = scans >> (it & 1) & 1;
+            if (second) scans ^= 1u << (it & 1);
             if (n == 0) {
                 if (live)
                     for (int c = 0; c < D; c += 8) *reinterpret_cast<uint4*>(out + c) = make_uint4(0, 0, 0, 0);
@@ -718,6 +760,33 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
             }
             tc_fence_after();
             const float inv = l == 0.f ? 0.f : 1.f / l;                        // a row that sees no key: zeros
+            if (second) {
+                // The products are without what is not finite.  What the row sees of that decides: a NaN, or infinities of both signs, make a NaN, one kind
+                // of infinity stays, and without any the product stands.  The probabilities are above zero, whatever their rounding.
+                if (!mbar_wait_all(smem_u32(&ctl->scanned[it & 1]), scan_parity, abort_flag, limit)) {
+                    if (lane == 0) report_timeout(p, 7);
+                    break;
+                }
+                const int(*first_odd)[128] = ctl->first_odd[it & 1];
+#pragma unroll 1
+                for (int c = 0; c < D; c += 32) {
+                    uint32_t ov[32];
+                    tmem_ld_32x32(t_o + c, ov);
+                    tmem_ld_wait();
+                    if (live) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            const bool nan = last >= first_odd[0][c + i], up = last >= first_odd[1][c + i], down = last >= first_odd[2][c + i];
+                            float v = __uint_as_float(ov[i]) * inv;
+                            if (nan || up || down) v += __uint_as_float(nan || (up && down) ? 0x7fc00000u : up ? 0x7f800000u : 0xff800000u);
+                            out[c + i] = (uint16_t)bf16_pair(v, v);
+                        }
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                continue;
+            }
             float odd = 0.f;                                                   // NaN once an output is not finite
 #pragma unroll
             for (int c = 0; c < D; c += 32) {
@@ -738,15 +807,14 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
             }
             tc_fence_before();
             __syncwarp();
-            unsigned spoilt = __ballot_sync(0xffffffffu, x.causal && odd != 0.f);
-            for (; spoilt; spoilt &= spoilt - 1) {
-                const int r0 = (warp & 3) * 32 + __ffs(spoilt) - 1, tok0 = t0 + w * x.tpt + r0 / x.G;
-                repair_row<D>(x, s, tok0, head * x.G + r0 % x.G, last_key(x, s, tok0), n);
-            }
+            if (__any_sync(0xffffffffu, x.causal && odd != 0.f) && lane == 0) *reinterpret_cast<volatile uint32_t*>(&ctl->spoilt[it & 3]) = it + 1;
         }
     }
-    tc_fence_before();
-    __syncthreads();
+    if (!over) {                                   // gave up
+        tc_fence_before();
+        __syncwarp();
+        block_any(true);
+    }
     if (warp == 8) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);
