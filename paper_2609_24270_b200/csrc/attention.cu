@@ -649,8 +649,8 @@ k_attn_decode(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
 // Chunked requests: one block per (request, KV head), thread = output column d.  With m_c, l_c, O_c the maximum (in
 // units of log2 e / sqrt D), the sum of probabilities and the unnormalised outputs of chunk c:
 // O = sum_c 2^(m_c - m) O_c / sum_c 2^(m_c - m) l_c, m = max_c m_c; chunks without keys (l_c = 0) are left out.
-__global__ void __launch_bounds__(AT_D) k_attn_combine(const float* __restrict__ o_part, const float2* __restrict__ stats,
-                                                        float* __restrict__ O, int n_chunks, int G) {
+__global__ void __launch_bounds__(AT_D) k_attn_combine(const float* o_part, const float2* stats,
+                                                        float* O, int n_chunks, int G) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int bh = blockIdx.x / G, q = blockIdx.x - bh * G, d = threadIdx.x;     // one block per (request, KV head, query row)

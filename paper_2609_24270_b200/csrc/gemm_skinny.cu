@@ -673,7 +673,7 @@ k_gemm_skinny(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ 
 
 // Zeroes C for the in-memory split-K mode.  Its dependents (the GEMM launched right after it) are released at
 // once, so the GEMM's start-up overlaps the zeroing; the GEMM waits for this kernel only before its first add.
-__global__ void k_zero_f32(float4* __restrict__ p, size_t n_vec) {
+__global__ void k_zero_f32(float4* p, size_t n_vec) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     // with overlap_launches this kernel itself may have started early: the GEMM before it may still be adding to C
     asm volatile("griddepcontrol.wait;" ::: "memory");

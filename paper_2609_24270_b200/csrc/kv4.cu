@@ -37,9 +37,9 @@ constexpr int KS_THREADS = 256;
 constexpr int KS_ROWS = 2;                           // U of large calls; small ones take 1, for more blocks
 
 template <int D, int U>
-__global__ void __launch_bounds__(KS_THREADS) k_kv4_store(uint8_t* __restrict__ pages, long long n_slots, int H_kv, const uint16_t* __restrict__ K,
-                                                          const uint16_t* __restrict__ V, long long n_tokens, long long k_stride, long long v_stride,
-                                                          const int32_t* __restrict__ slot) {
+__global__ void __launch_bounds__(KS_THREADS) k_kv4_store(uint8_t* pages, long long n_slots, int H_kv, const uint16_t* K,
+                                                          const uint16_t* V, long long n_tokens, long long k_stride, long long v_stride,
+                                                          const int32_t* slot) {
     dep_wait();
     dep_release();
     constexpr int L = D / 16, TOK = KS_THREADS / 2 / L;             // lanes of a row, tokens of the block side by side
@@ -128,9 +128,9 @@ __global__ void __launch_bounds__(KS_THREADS) k_kv4_store(uint8_t* __restrict__ 
 }
 
 template <int D, int U>
-__global__ void __launch_bounds__(KS_THREADS) k_kv4_load(const uint8_t* __restrict__ pages, long long n_slots, int H_kv, uint16_t* __restrict__ K,
-                                                         uint16_t* __restrict__ V, long long n_tokens, long long k_stride, long long v_stride,
-                                                         const int32_t* __restrict__ slot) {
+__global__ void __launch_bounds__(KS_THREADS) k_kv4_load(const uint8_t* pages, long long n_slots, int H_kv, uint16_t* K,
+                                                         uint16_t* V, long long n_tokens, long long k_stride, long long v_stride,
+                                                         const int32_t* slot) {
     dep_wait();
     dep_release();
     constexpr int L = D / 16, TOK = KS_THREADS / 2 / L;
@@ -335,8 +335,8 @@ __device__ __forceinline__ int slot_of(const TableArgs& t, const int32_t* row, c
     return page >= 0 && page < t.n_pages ? page * KV4_PAGE + pos % KV4_PAGE : -1;
 }
 
-__global__ void __launch_bounds__(KT_THREADS) k_kv4_extend(const TableArgs t, const int32_t* __restrict__ row, const int32_t* __restrict__ new_off,
-                                                           int n, int32_t* __restrict__ slot, int inline_tokens, int32_t* ok) {
+__global__ void __launch_bounds__(KT_THREADS) k_kv4_extend(const TableArgs t, const int32_t* row, const int32_t* new_off,
+                                                           int n, int32_t* slot, int inline_tokens, int32_t* ok) {
     __shared__ union { GrantShared grant; FirstShared first; } sh;
     dep_wait();
     dep_release();
@@ -368,15 +368,15 @@ __global__ void __launch_bounds__(KT_THREADS) k_kv4_extend(const TableArgs t, co
 }
 
 __global__ void __launch_bounds__(256) k_kv4_slots(const TableArgs t, const int32_t* row, const int32_t* new_off, int n,
-                                                   int32_t* __restrict__ slot, int n_tokens, const int32_t* ok) {
+                                                   int32_t* slot, int n_tokens, const int32_t* ok) {
     dep_wait();
     dep_release();
     const int j = blockIdx.x * 256 + threadIdx.x;
     if (j < n_tokens) slot[j] = slot_of(t, row, new_off, ok, n, j);
 }
 
-__global__ void __launch_bounds__(KT_THREADS) k_kv4_fork_plan(const TableArgs t, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
-                                                              int n, int32_t* __restrict__ ok) {
+__global__ void __launch_bounds__(KT_THREADS) k_kv4_fork_plan(const TableArgs t, const int32_t* src, const int32_t* dst,
+                                                              int n, int32_t* ok) {
     __shared__ union { GrantShared grant; FirstShared first; } sh;
     dep_wait();
     dep_release();
@@ -405,7 +405,7 @@ __global__ void __launch_bounds__(KT_THREADS) k_kv4_fork_plan(const TableArgs t,
 }
 
 // copies `units` pieces of 16 bytes, a block's threads side by side, four loads in flight a thread
-__device__ __forceinline__ void copy16(uint4* __restrict__ to, const uint4* __restrict__ from, int units) {
+__device__ __forceinline__ void copy16(uint4* to, const uint4* from, int units) {
     int i = threadIdx.x;
     const int step = blockDim.x;
     for (; i + 3 * step < units; i += 4 * step) {
@@ -419,8 +419,8 @@ __device__ __forceinline__ void copy16(uint4* __restrict__ to, const uint4* __re
 }
 
 // block (request, part): part 0 also shares the full pages; every part copies its share of the open page
-__global__ void __launch_bounds__(256) k_kv4_fork_copy(const TableArgs t, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
-                                                       const int32_t* __restrict__ ok, uint8_t* __restrict__ pages, size_t page_bytes, int parts) {
+__global__ void __launch_bounds__(256) k_kv4_fork_copy(const TableArgs t, const int32_t* src, const int32_t* dst,
+                                                       const int32_t* ok, uint8_t* pages, size_t page_bytes, int parts) {
     dep_wait();
     dep_release();
     const int i = blockIdx.x / parts, part = blockIdx.x - i * parts;
@@ -445,7 +445,7 @@ __global__ void __launch_bounds__(256) k_kv4_fork_copy(const TableArgs t, const 
 }
 
 // a page is given back by whoever takes it out of the table, so that a row named twice gives it back once
-__global__ void __launch_bounds__(256) k_kv4_free(const TableArgs t, const int32_t* __restrict__ row) {
+__global__ void __launch_bounds__(256) k_kv4_free(const TableArgs t, const int32_t* row) {
     dep_wait();
     dep_release();
     const int r = row[blockIdx.x];
@@ -463,7 +463,7 @@ __global__ void __launch_bounds__(256) k_kv4_free(const TableArgs t, const int32
 // used pages in front of a segment of 32 pages (a multiple in large pools), u(a): a used page's number among the movers is the used
 // pages in front of it less those below n_used, and hole k lies in the last segment a with pages(a) - u(a) <= k.
 // Plan and move of 65536 pages that are in place already: 27 us (238 with neighbouring counts in one thread's hands).
-__global__ void __launch_bounds__(KT_THREADS) k_kv4_compact_plan(const TableArgs t, int32_t* __restrict__ moved) {
+__global__ void __launch_bounds__(KT_THREADS) k_kv4_compact_plan(const TableArgs t, int32_t* moved) {
     __shared__ int warp_sum[32];
     __shared__ int used_before[KT_SEGMENTS];
     __shared__ uint32_t used_mask[KT_SEGMENTS];                            // with segments of 32 pages
@@ -551,8 +551,8 @@ __global__ void __launch_bounds__(KT_THREADS) k_kv4_compact_plan(const TableArgs
 
 // Copies page from[i] (from = NULL: i) to page to[i], in parts; pairs with a page outside the pool, or of a page with itself, are passed over.  A
 // block's threads look for work side by side, as most pages of a large pool stay where they are.  With `refs` the pages' counts move too.
-__device__ __forceinline__ void copy_pages(const int32_t* __restrict__ from, const int32_t* __restrict__ to, long long n, long long n_pages,
-                                           uint8_t* __restrict__ pages, size_t page_bytes, int parts, int32_t* refs) {
+__device__ __forceinline__ void copy_pages(const int32_t* from, const int32_t* to, long long n, long long n_pages,
+                                           uint8_t* pages, size_t page_bytes, int parts, int32_t* refs) {
     __shared__ int work_from[256], work_to[256], work_part[256], n_found;
     const int units = (int)(page_bytes / 16);
     const long long n_work = n * parts;
@@ -584,7 +584,7 @@ __device__ __forceinline__ void copy_pages(const int32_t* __restrict__ from, con
 }
 
 // page (and its count) by page, and the tables, entry by entry
-__global__ void __launch_bounds__(256) k_kv4_compact_move(const TableArgs t, const int32_t* __restrict__ moved, uint8_t* __restrict__ pages,
+__global__ void __launch_bounds__(256) k_kv4_compact_move(const TableArgs t, const int32_t* moved, uint8_t* pages,
                                                           size_t page_bytes, int parts) {
     dep_wait();
     dep_release();
@@ -596,8 +596,8 @@ __global__ void __launch_bounds__(256) k_kv4_compact_move(const TableArgs t, con
     copy_pages(nullptr, moved, t.n_pages, t.n_pages, pages, page_bytes, parts, t.refs);
 }
 
-__global__ void __launch_bounds__(256) k_kv4_copy(const int32_t* __restrict__ from, const int32_t* __restrict__ to, long long n, long long n_pages,
-                                                  uint8_t* __restrict__ pages, size_t page_bytes, int parts) {
+__global__ void __launch_bounds__(256) k_kv4_copy(const int32_t* from, const int32_t* to, long long n, long long n_pages,
+                                                  uint8_t* pages, size_t page_bytes, int parts) {
     dep_wait();
     dep_release();
     copy_pages(from, to, n, n_pages, pages, page_bytes, parts, nullptr);

@@ -53,7 +53,8 @@ __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w 
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
 // Waits until the launch before this one on the stream has completed (launches of this library with the programmatic
-// attribute), and lets the next one come up.
+// attribute), and lets the next one come up.  A kernel that waits here takes no `__restrict__` pointers: what it reads may have been
+// written while it was up already, and the qualifier would let the compiler read it in front of the wait or through a cache that is not coherent.
 __device__ __forceinline__ void dep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void dep_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
