@@ -707,10 +707,14 @@ ag_status ag_kv4_copy(const ag_kv4_pool* pool, const int32_t* from, const int32_
 
 /*
  * attention_decode_kv4 - O[b][hq][:] = softmax_j(Q[b][hq] . K[j] / sqrt(D)) V[j] over the tokens j of table row row[b], K and V what the cache
- * holds of KV head hq / (H_q / H_kv): the decode step on the 4-bit cache.  Keys enter as they stand in the cache (s * code + lo, without
- * further rounding), values are rounded by at most 2^-11 of their group's largest or 2^-32 of the row's largest value, whichever is more
- * (a step of the quantisation is some 2^-4 of the group's largest), probabilities by 2^-12 of themselves or 2^-35 of the largest; sums and
- * softmax statistics are in 32 bits.
+ * holds of KV head hq / (H_q / H_kv): the decode step on the 4-bit cache.  Roundings, beside the output's own:
+ *   values         2^-11 (|v| + |lo - 16 s|) for v = s * code + lo, some 2^-10 of the group's largest (a step of the quantisation is 2^-4 of it); at least
+ *                  2^-32 of the row's largest value
+ *   probabilities  2^-11 of themselves, or 2^-35 of the largest
+ *   scores         keys enter as they stand in the cache and are summed in 32 bits, in steps that follow the largest query element: off by at most
+ *                  2^-13 sum_d |q_d| s_d / sqrt D, s_d the scale of the key's group (measured, queries up to 10^4 and with one dominant channel: 2^-19 of
+ *                  the sum).  Half a step of the quantisation in every element, for comparison, is 2^-1 of it
+ *   sums and softmax statistics are in 32 bits.
  *   Q, O       device, [B][H_q][D] bf16, 16-byte aligned; H_q a multiple of H_kv, H_q / H_kv <= 1024;
  *              O must not overlap Q.  Queries of 2^120 and more may give NaN.  B H_q max_pages <= 2^40
  *   row        device [B], or NULL for row b (then B <= table->n_rows); a row outside the table, or an empty one, gives zeros

@@ -6,11 +6,13 @@
 //     O[d][q]   += sum_key V[key][d] P[key][q]                                    m16n8k16 MMA (fp16): 16 d x 8 heads x 16 keys
 // A code of K becomes an fp16 operand with one logic instruction: a nibble masked out of its word is the subnormal u 2^-24, or u 2^-20, and
 // the MMA takes subnormals as they are.  The bases' part comes from an MMA against sums over q kept in three bf16 parts (24 bits),
-// so scores carry no rounding besides the 32-bit sums (in which a subnormal operand counts as 2^-14 when the MMA lines its products up: steps of 2^-24 of 1024 q s,
-// which scores do not feel; outputs would, so V's codes are not taken this way).  V varies its scale along the contraction: its codes become 16 + u
-// (0x4C00 | u << 6) and then s u + b with one multiply-add, in fp16 under a power of two that follows the largest value (rounded at 2^-12 of the group's
-// largest, or 2^-32 of the row's);
-// P, times 2^10, is fp16 as well.  (An fp8 MMA would take the codes as they are, but mma.sync on this chip converts fp8 operands to fp16
+// so scores carry no rounding besides the 32-bit sums.  A subnormal operand may count as 2^-14 when the MMA lines its products up, in steps of 2^-24 of 1024 q s:
+// 2^-13 sum |q| s / sqrt D for a score at most.  Measured with pairs of keys: 2^-19 of that sum, for queries up to 10^4 and with one channel that outweighs the
+// others; the codes shifted up to 2^-18 u (three more instructions a word) measured the same and took 137.4 instead of 131.2 us for the long rows below.
+// Outputs would feel it, so V's codes are not taken this way.  V varies its scale along the contraction: its codes become 16 + u
+// (0x4C00 | u << 6) and then s u + b with one multiply-add, in fp16 under a power of two that follows the largest value: off by at most half
+// a step of b - 16 s and half a step of the value, 2^-11 (|v| + |b - 16 s|), some 2^-10 of the group's largest, or 2^-32 of the row's largest;
+// P, times 2^10, is fp16 as well, off by half a step, 2^-11 of itself.  (An fp8 MMA would take the codes as they are, but mma.sync on this chip converts fp8 operands to fp16
 // first: measured, slower than the above.)
 //
 // Memory: 1.25 D bytes per key and head, read once.  A byte costs about ten times the arithmetic instructions of a bf16 cache's, and those bound
