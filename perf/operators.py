@@ -121,16 +121,19 @@ def work(case):
 
 
 # ---- states -----------------------------------------------------------------------------------------------------------
-_kept = {}
+_topo, _plans = {}, {}
 
 
-def _plan():
-    """The whole chip, found once per process."""
-    if "plan" not in _kept:
+def _plan(stream):
+    """A plan of the whole chip for each stream (of each device), since calls of one plan must not run at the same time; found once."""
+    plan = _plans.get(stream)
+    if plan is None:
         from paper_2609_24270_b200 import binding as ag
-        topo = ag.topo_discover(ag.AG_TOPO_CENSUS | ag.AG_TOPO_CLUSTER | ag.AG_TOPO_LATENCY)
-        _kept["plan"] = ag.sched_build(topo, None, topo.n_sm, ag.make_policy(kind=ag.AG_DIE_COMPACT, M=128, N=256, K=64))
-    return _kept["plan"]
+        if stream.device not in _topo:
+            _topo[stream.device] = ag.topo_discover(ag.AG_TOPO_CENSUS | ag.AG_TOPO_CLUSTER | ag.AG_TOPO_LATENCY)
+        topo = _topo[stream.device]
+        plan = _plans[stream] = ag.sched_build(topo, None, topo.n_sm, ag.make_policy(kind=ag.AG_DIE_COMPACT, M=128, N=256, K=64))
+    return plan
 
 
 def _random_pages(gen, n_pages, H_kv, D):
@@ -179,7 +182,7 @@ def prepare(case, seed):
         off = lambda v: torch.tensor([0] + list(torch.tensor(v).cumsum(0)), dtype=torch.int32).cuda()  # noqa: E731
         st.update(q_off=off(q), kv_off=off(k), q_max=max(q), kv_max=max(k), O=torch.empty(sum(q), H_q, D, dtype=BF16, device="cuda"))
         if own:
-            st["plan"] = _plan()
+            _plan(torch.cuda.current_stream())
     elif op == "decode":
         n = _lens(case, case["B"], case["len_min"], case["len_max"])
         max_pages = _pages(max(n))
@@ -233,11 +236,10 @@ def run(st):
 
 def _own_prompt(st):
     from paper_2609_24270_b200 import binding as ag
-    c = st["case"]
+    c, stream = st["case"], torch.cuda.current_stream()
     ag.attention_prompt(st["Q"].data_ptr(), st["K"].data_ptr(), st["V"].data_ptr(), st["O"].data_ptr(), c["H_q"], c["H_kv"], c["D"],
-                        st["q_off"].data_ptr(), st["kv_off"].data_ptr(), c["n_seq"], st["Q"].shape[0], st["K"].shape[0], st["plan"],
-                        q_stride=st["Q"].stride(0), k_stride=st["K"].stride(0), v_stride=st["V"].stride(0),
-                        stream=torch.cuda.current_stream().cuda_stream)
+                        st["q_off"].data_ptr(), st["kv_off"].data_ptr(), c["n_seq"], st["Q"].shape[0], st["K"].shape[0], _plan(stream),
+                        q_stride=st["Q"].stride(0), k_stride=st["K"].stride(0), v_stride=st["V"].stride(0), stream=stream.cuda_stream)
     return st["O"]
 
 
