@@ -13,7 +13,7 @@ namespace ag {
 constexpr int kThreads = 192;       // warp 0 scheduler+producer, warp 1 MMA issuer, warps 2-5 epilogue
 constexpr int kRing = 8;            // depth of the unit-id ring between the scheduler and its consumers
 constexpr int kEpiWarps = 4;
-constexpr uint64_t kWaitLimitNs = 2000000000ull;  // every device-side wait gives up after 2 s
+constexpr uint64_t kWaitLimitNs = 2000000000ull;  // every device-side wait gives up after 2 s (prompts: and 0.2 us a key, since a wait may last a unit)
 
 struct PersistParams {
     const int32_t* image;   // plan image (device)

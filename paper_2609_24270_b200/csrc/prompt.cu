@@ -889,6 +889,7 @@ extern "C" ag_status attention_prompt_persistent(const ag_prompt_attention* a, c
         x.kv_off = (a->kv_off ? a->kv_off : a->q_off) + s0;
         if ((st = renew_epochs_if_needed(plan, stream)) != AG_OK) return st;
         PersistParams gp = make_persist_params(plan, 0, 0, 0);
+        gp.wait_limit_ns += 200ull * a->kv_tokens;       // a wait may last a unit: up to 17 us for 128 keys (second pass, D = 128)
         const unsigned grid = plan->grid_blocks > 0 ? plan->grid_blocks : plan->lay.n_sm;
         if (a->D == 128) k_attn_prompt<128><<<grid, PA_THREADS, smem128, stream>>>(tm_q, tm_k, tm_v, gp, x);
         else k_attn_prompt<64><<<grid, PA_THREADS, smem64, stream>>>(tm_q, tm_k, tm_v, gp, x);

@@ -161,3 +161,20 @@ def test_a_model_that_has_diverged():
     assert O.isnan().all()
     print(f"finite {took[0] * 1000:.0f} us, all NaN {took[1] * 1000:.0f} us")
     assert took[1] < 20 * took[0]
+
+
+def test_units_that_last_longer_than_two_seconds():
+    """Twenty-five million keys, every value a NaN: a unit and its second pass take some 2.9 s, most of it the second pass, while the next one waits for its turn."""
+    n, m, G, D = 130, 24 << 20, 4, 128
+    Q = torch.ones(n, G, D, dtype=torch.bfloat16, device="cuda")
+    K, V = torch.zeros(m, 1, D, dtype=torch.bfloat16, device="cuda"), torch.full((m, 1, D), float("nan"), dtype=torch.bfloat16, device="cuda")
+    O = torch.zeros_like(Q)
+    off, koff, plan = dev(np.array([0, n], np.int32)), dev(np.array([0, m], np.int32)), plan_for(1)
+    e = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+    s = torch.cuda.current_stream()
+    e[0].record()
+    ag.attention_prompt(Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(), G, 1, D, off.data_ptr(), koff.data_ptr(), 1, n, m, plan, stream=s.cuda_stream)
+    e[1].record()
+    torch.cuda.synchronize()
+    print(f"three units, twice: {e[0].elapsed_time(e[1]) / 1000:.2f} s")
+    assert plan.last_status() == ag.AG_OK and O.isnan().all()
