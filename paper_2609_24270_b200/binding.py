@@ -663,9 +663,10 @@ def attention_decode_kv4_workspace(B: int, H_q: int, H_kv: int, D: int, max_page
     return int(lib().ag_attention_decode_kv4_workspace(B, H_q, H_kv, D, max_pages))
 
 
-def attention_decode_kv4(q_ptr: int, pool: KV4Pool, table: KV4Table, row_ptr, o_ptr: int, B: int, H_q: int, workspace_ptr=None,
-                         workspace_bytes: int = 0, stream: int = 0):
-    """One query token per request over the 4-bit cache; request b reads table row row[b] (row_ptr None: row b)."""
+def attention_decode_kv4(q_ptr: int, pool: KV4Pool, table: KV4Table, row_ptr, o_ptr: int, B: int, H_q: int, workspace_ptr: int,
+                         workspace_bytes: int, stream: int = 0):
+    """One query token per request over the 4-bit cache; request b reads table row row[b] (row_ptr None: row b).  The workspace (device, at least
+    attention_decode_kv4_workspace bytes) is the caller's and always needed."""
     _check(lib().attention_decode_kv4(q_ptr, C.byref(pool), C.byref(table), row_ptr, o_ptr, B, H_q, workspace_ptr, workspace_bytes, stream),
            "attention_decode_kv4")
 
