@@ -53,11 +53,6 @@ struct DecodeKv4Args {
     int aligned;                  // 1: block = unit (short rows, few units)
     float scale_log2e;
 };
-__device__ __forceinline__ float ex2_ftz(float v) {      // 2^v, relative error 2^-22; 2^-inf = 0
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-    return r;
-}
 __device__ __forceinline__ void mma_bf16_new(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
         : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
@@ -76,11 +71,6 @@ __device__ __forceinline__ void mma_f16_new(float (&d)[4], uint32_t a0, uint32_t
 __device__ __forceinline__ uint32_t movm_trans(uint32_t v) {      // 8 x 8 matrix of 16-bit elements, transposed across the warp
     uint32_t r;
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
-    return r;
-}
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-    uint32_t r;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {

@@ -24,8 +24,6 @@
 #include <string.h>
 
 #include <algorithm>
-#include <mutex>
-#include <new>
 
 #include "persist.cuh"
 
@@ -68,7 +66,6 @@ struct PromptCtl {
     int abort_flag, member, slot;
     int blocks_before[PA_MAXSEQ + 1];     // units of one head in front of the i-th sequence of work
     PromptSeq seq[PA_MAXSEQ];
-    int warp_sum[PA_THREADS / 32];
 };
 
 template <int D>
@@ -101,11 +98,6 @@ __device__ __forceinline__ void tmem_st_32x32(uint32_t taddr, const uint32_t (&v
         : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ float exp2_fast(float v) {     // 2^v, relative error 2^-22; 2^-inf = 0
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-    return r;
-}
 // pairs of floats in one register pair: two results for one issue slot
 typedef unsigned long long f32x2;
 __device__ __forceinline__ f32x2 pack2(float a, float b) {
@@ -159,11 +151,6 @@ __device__ __forceinline__ void store32(uint16_t* to, const uint32_t (&v)[8], bo
         reinterpret_cast<uint4*>(to)[0] = make_uint4(v[0], v[1], v[2], v[3]);
         reinterpret_cast<uint4*>(to)[1] = make_uint4(v[4], v[5], v[6], v[7]);
     }
-}
-__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
-    uint32_t r;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
 }
 
 // keys that token i of a sequence sees: 0 .. last_key(i); may be negative
@@ -699,7 +686,7 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                         break;
                     }
                     tc_fence_after();
-                    const float f = !grow ? 1.f : m == -INFINITY ? 0.f : exp2_fast((m - top) * x.scale_log2e);
+                    const float f = !grow ? 1.f : m == -INFINITY ? 0.f : ex2_ftz((m - top) * x.scale_log2e);
                     if (grow) m = top;
                     l *= f;
 #pragma unroll 1
@@ -728,12 +715,12 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                             unpack2(v, a, b);
                         } else {
                             unpack2(v, a, b);
-                            a = exp2_fast(a);
-                            b = exp2_fast(b);
+                            a = ex2_ftz(a);
+                            b = ex2_ftz(b);
                             v = pack2(a, b);
                         }
                         sum = add2(sum, v);
-                        pv[i] = bf16_pair(a, b);
+                        pv[i] = pack_bf16(a, b);
                     }
                     tmem_st_32x32(t_s + half * 32, pv);
                 }
@@ -779,7 +766,7 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                             const bool nan = last >= first_odd[0][c + i], up = last >= first_odd[1][c + i], down = last >= first_odd[2][c + i];
                             float v = __uint_as_float(ov[i]) * inv;
                             if (nan || up || down) v += __uint_as_float(nan || (up && down) ? 0x7fc00000u : up ? 0x7f800000u : 0xff800000u);
-                            out[c + i] = (uint16_t)bf16_pair(v, v);
+                            out[c + i] = (uint16_t)pack_bf16(v, v);
                         }
                     }
                 }
@@ -800,7 +787,7 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                     for (int i = 0; i < 32; i += 16) {
                         uint32_t v[8];
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) v[k] = bf16_pair(__uint_as_float(ov[i + 2 * k]) * inv, __uint_as_float(ov[i + 2 * k + 1]) * inv);
+                        for (int k = 0; k < 8; ++k) v[k] = pack_bf16(__uint_as_float(ov[i + 2 * k]) * inv, __uint_as_float(ov[i + 2 * k + 1]) * inv);
                         store32(out + c + i, v, wide);
                     }
                 }
