@@ -78,7 +78,8 @@ __device__ inline void wait_until_manned(const PersistParams& p) {
         int ok = 1;
         for (int i = threadIdx.x; i < p.b; i += blockDim.x) ok &= slot_taken(p, i) ? 1 : 0;
         if (__syncthreads_and(ok)) break;
-        if (globaltimer_ns() - t0 > p.manned_wait_ns) break;
+        // one thread's clock decides for the block: no thread leaves while others go on to the barrier above
+        if (__syncthreads_or(threadIdx.x == 0 && globaltimer_ns() - t0 > p.manned_wait_ns)) break;
         __nanosleep(200);
     }
 }
