@@ -611,8 +611,11 @@ typedef struct {
 /*
  * attention_prompt_persistent - O = softmax(scale Q K^T) V, per sequence and head.  A token that sees no key (no keys at all, or more
  * queries than keys) gets zeros.  What a token does not see (other sequences, later keys) has no influence, whatever it holds.  Scores, softmax statistics and outputs
- * are accumulated in 32 bits, probabilities are rounded to bf16.  (Outputs are normalised at the end: values beyond 2^119 / number of keys may overflow.)
+ * are accumulated in 32 bits, probabilities are rounded to bf16 (one exponential in eight is off by up to 7.5e-5 before that, the others by 2^-22).  (Outputs are
+ * normalised at the end: values beyond 2^119 / number of keys may overflow.)
  * O must not overlap Q, K or V.  One launch per 1024 sequences.  Asynchronous on cuda_stream.  Errors as gemm_persistent; device-side status via ag_last_status.
+ * Beside kernels that hold the planned SMs for long (attention_decode_kv4 over long rows is one), blocks that come to other SMs leave after 40 us: the call may
+ * then run on fewer SMs than planned, and when no block came to a planned SM nothing has run and the status is AG_ERR_UNMANNED_SM.
  */
 ag_status attention_prompt_persistent(const ag_prompt_attention* a, const ag_plan* plan, void* cuda_stream);
 
@@ -720,6 +723,7 @@ ag_status ag_kv4_copy(const ag_kv4_pool* pool, const int32_t* from, const int32_
  *   row        device [B], or NULL for row b (then B <= table->n_rows); a row outside the table, or an empty one, gives zeros
  *   table      lengths are clamped to 0 .. 64 max_pages; tokens whose page is not one of the pool's are left out
  *   workspace  device, 16-byte aligned, ag_attention_decode_kv4_workspace bytes (at most about 25 MB).  Its contents mean nothing between calls; calls that may run at the same time need one each
+ * The cache is read once for groups of up to 16 heads, once for every 16 of them beyond.  The launch takes every SM of the chip (no plan).
  * Asynchronous on cuda_stream, may be captured into a graph (lengths and tables are read when it runs).  The work is split by
  * the shape and the lengths of the whole batch, nothing else, so results are reproducible bit for bit; a request's bits may change with
  * the other requests of its batch.

@@ -18,7 +18,7 @@ namespace ag {
 // D / 16 lanes hold a row, sixteen elements each: a lane's K codes are two words of the page, the V codes are transposed across lanes
 // (kv4_transpose) so that a lane writes whole words of the fragment order as well.  With eight elements a lane the part of the work that goes by
 // lanes (addresses, scales, exchanges) took twice as long: 86 and 51 us for 46k tokens x 8 heads stored and read back,
-// now 64 and 44; the store is bound by instructions still, the load by its scattered eight-byte pieces of V.
+// now 60 and 42; the store is bound by instructions still (82 % of the issue slots), the load by its scattered eight-byte pieces of V.
 //
 // A block takes U times 128 / L neighbouring tokens of one head: the words of neighbouring V rows share sectors, and U rows a lane are in
 // flight together (a row's chain slot -> page -> row is some 2 us long).

@@ -15,11 +15,11 @@
 // P, times 2^10, is fp16 as well, off by half a step, 2^-11 of itself.  (An fp8 MMA would take the codes as they are, but mma.sync on this chip converts fp8 operands to fp16
 // first: measured, slower than the above.)
 //
-// Memory: 1.25 D bytes per key and head, read once.  A byte costs about ten times the arithmetic instructions of a bf16 cache's, and those bound
-// it: 61 % of the issue slots are used, the rest are fixed latencies of four warps a scheduler.  4 requests of 131072 keys, 32 query heads on 8, D = 128:
+// Memory: 1.25 D bytes per key and head, read once for every 16 heads of a group.  A byte costs about ten times the arithmetic instructions of a bf16 cache's, and those bound
+// it: 60 % of the issue slots are used, no pipe is at its limit (logic 50 %, tensor 20), the rest are fixed latencies of four warps a scheduler.  4 requests of 131072 keys, 32 query heads on 8, D = 128:
 // 131 us, 5.0 TB/s (0.77 of the measured copy); 128 requests of 200 to 1024 keys: 35 us, half of it until the first page is there and from the last on.  So
-// the operands are unpacked in registers, straight into the MMA's fragments - tcgen05.mma would want them in shared memory, one more
-// write and read of the unpacked (four times larger) tile.  The cache stores the codes in fragment order, so a warp's share of a
+// the operands are unpacked in registers, straight into the MMA's fragments (for tcgen05.mma they would go on into tensor memory; not built).  Groups of 9 to 16 heads
+// take one block an SM (70 us against 50 for up to 8, 4 x 32768 keys), each 16 heads more another pass (121 us for 32, 218 for 64).  The cache stores the codes in fragment order, so a warp's share of a
 // page is read with conflict-free vector loads.
 //
 // Work: all pages of all (request, KV head) units in one line, cut into equal runs, one per warp, every warp of the launch resident at

@@ -14,8 +14,8 @@
 // at most 2^8, sums and outputs are in 32 bits, so this changes no rounding.
 // The tensor pipe and, as closely, the exponentials: a pair of 128 x 128 tiles takes 2 x 1024 cycles of MMAs (D = 128) and 2 x 1024 cycles of the
 // special-function units (16 per cycle and SM).  What bounds it is a tile's own chain, 1760 cycles of softmax and 1280 until its next scores are there;
-// more tiles in flight do not fit tensor memory.  8192 tokens, 32 query heads on 8, D = 128, causal: 445 us, 1235 TFLOP/s (0.74 of the
-// measured product of matrices; 517 us once the power cap holds); D = 64: 384.
+// more tiles in flight do not fit tensor memory at D = 128 (at 64 a third score tile would; not built).  8192 tokens, 32 query heads on 8, D = 128,
+// causal: 445 us, 1235 TFLOP/s (0.74 of the measured product of matrices; 520 us once the power cap holds), not causal 850; D = 64: 390 and 740.
 //
 // A probability of zero times a later token's infinity or NaN, in a key tile that rows share, spoils a row that does not see that token.  A causal unit
 // with a result that is not finite is therefore run a second time, with the values that are not finite taken as zeros while the first of
