@@ -61,14 +61,13 @@ def test_fewer_blocks_than_planned_sms(elsewhere):
     print({k: seen.count(k) for k in set(seen)})
 
 
-@pytest.mark.parametrize("budget", [74, 20])
-def test_beside_long_decodes(budget):
+def test_beside_long_decodes():
     """Decode steps over long rows fill the whole chip, one behind the other, on another stream."""
     c = make([30000, 30000], 8, 64, seed=3)
     Q = dev(queries(2, 32, 64, 4))
     size = ag.attention_decode_kv4_workspace(2, 32, 8, 64, c.page_of.shape[1])
     ws, out = torch.empty(size, dtype=torch.uint8, device="cuda"), torch.empty(2, 32, 64, dtype=torch.bfloat16, device="cuda")
-    p, plan = Prompt([700, 300, 64]), plan_for(budget)
+    p, plan = Prompt([700, 300, 64]), plan_for(74)
     main, other = torch.cuda.Stream(), torch.cuda.Stream()
 
     def step():
@@ -79,7 +78,7 @@ def test_beside_long_decodes(budget):
     torch.cuda.synchronize()
     assert plan.last_status() == ag.AG_OK
     want = p.o.clone(), out.clone()
-    for i in range(20):
+    for i in range(8):
         p.o.zero_()
         out.zero_()
         torch.cuda.synchronize()
