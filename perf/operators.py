@@ -126,13 +126,14 @@ _topo, _plans = {}, {}
 
 def _plan(stream):
     """A plan of the whole chip for each stream (of each device), since calls of one plan must not run at the same time; found once."""
-    plan = _plans.get(stream)
+    key = stream.device_index, stream.cuda_stream
+    plan = _plans.get(key)
     if plan is None:
         from paper_2609_24270_b200 import binding as ag
-        if stream.device not in _topo:
-            _topo[stream.device] = ag.topo_discover(ag.AG_TOPO_CENSUS | ag.AG_TOPO_CLUSTER | ag.AG_TOPO_LATENCY)
-        topo = _topo[stream.device]
-        plan = _plans[stream] = ag.sched_build(topo, None, topo.n_sm, ag.make_policy(kind=ag.AG_DIE_COMPACT, M=128, N=256, K=64))
+        if key[0] not in _topo:
+            _topo[key[0]] = ag.topo_discover(ag.AG_TOPO_CENSUS | ag.AG_TOPO_CLUSTER | ag.AG_TOPO_LATENCY)
+        topo = _topo[key[0]]
+        plan = _plans[key] = ag.sched_build(topo, None, topo.n_sm, ag.make_policy(kind=ag.AG_DIE_COMPACT, M=128, N=256, K=64))
     return plan
 
 
