@@ -619,6 +619,56 @@ typedef struct {
  */
 ag_status attention_prompt_persistent(const ag_prompt_attention* a, const ag_plan* plan, void* cuda_stream);
 
+/* ---- rotary positions ----------------------------------------------------------------------------------------------------
+ * The first `rot` elements of a head are pairs (a, b) that are turned by the angle position * freq of the pair:
+ *     a' = bf16(a c - b s),  b' = bf16(b c + a s),   c = float(cos(position * freq) * magnitude),  s = float(sin(...) * magnitude)
+ * Angles, cosines and sines are taken in 64 bits (an angle of 10^6 radians is off by 10^-10 then, by 0.06 in 32), c and s are rounded to 32, each product
+ * and the sum too.  The elements behind the first `rot` stay as they are.
+ */
+#define AG_ROTARY_HALVES 0 /* pairs (i, i + rot / 2) */
+#define AG_ROTARY_PAIRS 1  /* pairs (2 i, 2 i + 1) */
+typedef struct {
+    const double* freq;    /* device [rot / 2]: radians a position; 8-byte aligned */
+    int32_t rot;           /* a multiple of 16, 16 .. D */
+    int32_t layout;        /* AG_ROTARY_HALVES or AG_ROTARY_PAIRS */
+    double magnitude;      /* of cosine and sine; 1 without scaling */
+} ag_rotary;
+
+/* Frequencies f_i = base^(-2 i / rot), i < rot / 2, stretched for contexts `factor` times as long as the `context` that a model was trained on. */
+#define AG_ROTARY_PLAIN 0  /* f_i */
+#define AG_ROTARY_LINEAR 1 /* f_i / factor */
+#define AG_ROTARY_BANDS 2  /* by the turns t_i = context f_i / 2 pi: f_i / factor up to `low` turns, f_i from `high` on, between them blended by (t_i - low) / (high - low) */
+#define AG_ROTARY_RAMP 3   /* by the place of i between the pairs that turn `high` times and `low` times over the context: with
+                              place(t) = rot ln(context / (2 pi t)) / (2 ln base), a = max(0, floor(place(high))), b = min(rot - 1, ceil(place(low))), the share of
+                              f_i / factor goes from 0 at i = a to 1 at i = b (a step where they coincide); magnitude 0.1 ln(factor) + 1 */
+typedef struct {
+    int32_t rot;           /* even, 2 .. 1024 */
+    int32_t scaling;       /* AG_ROTARY_PLAIN .. _RAMP */
+    double base;           /* > 1 */
+    double factor;         /* >= 1; not looked at by PLAIN */
+    double context, low, high;  /* BANDS and RAMP: > 0, 0 < low < high */
+} ag_rotary_scaling;
+/* ag_rotary_frequencies - host arithmetic: freq (host, [rot / 2]) and the magnitude that go into ag_rotary.  Errors: AG_ERR_ARG. */
+ag_status ag_rotary_frequencies(const ag_rotary_scaling* s, double* freq, double* magnitude);
+
+/* Rows of tokens that are turned.  Device pointers, bf16, 16-byte aligned; token i's row at Q + i * q_stride, [H_q][D] (K and V: [H_kv][D]); strides in elements,
+ * multiples of 8, at least the row (parts of one fused projection are fine). */
+typedef struct {
+    const void *Q, *K, *V;    /* Q or K may be NULL (with its output); V: ag_kv4_append_rotary only */
+    void *Q_out, *K_out;      /* the turned rows; may be Q and K themselves (same stride, from = NULL), must not overlap them or one another otherwise */
+    int64_t q_stride, k_stride, v_stride, q_out_stride, k_out_stride;
+    int32_t H_q, H_kv, D;     /* D = 64 or 128; H_q, H_kv 1 .. 4096 (of what is not NULL) */
+    int64_t n_tokens;         /* below 2^31 */
+    const int32_t* pos;       /* device [n_tokens]: positions, any int32 */
+    const int32_t* from;      /* device [n_tokens]: token i takes row from[i] of Q, K and V, a token whose from is not in 0 .. n_rows - 1 is passed over; NULL: row i */
+    int64_t n_rows;           /* rows of Q, K and V (with `from`) */
+} ag_rotary_rows;
+/*
+ * ag_rotary_apply - Q and K turned to their positions.  (H_kv and D are the struct's.)  Asynchronous on cuda_stream, may be captured into a graph.
+ * Errors: AG_ERR_ARG, AG_ERR_UNSUPPORTED_ARCH, AG_ERR_CUDA.
+ */
+ag_status ag_rotary_apply(const ag_rotary* r, const ag_rotary_rows* x, void* cuda_stream);
+
 /* ---- 4-bit key/value cache in pages ----------------------------------------------------------------------------------
  * A cache that requests grow in, share and leave again: pages of AG_KV4_PAGE tokens (all KV heads of one layer) in a buffer of
  * the caller, 4-bit codes with a (scale, base) pair for every 32 elements - 0.31 of the bytes of bf16.  The functions below work
@@ -732,6 +782,77 @@ ag_status ag_kv4_copy(const ag_kv4_pool* pool, const int32_t* from, const int32_
 ag_status attention_decode_kv4(const void* Q, const ag_kv4_pool* pool, const ag_kv4_table* table, const int32_t* row, void* O, int B, int H_q,
                                void* workspace, size_t workspace_bytes, void* cuda_stream);
 size_t ag_attention_decode_kv4_workspace(int B, int H_q, int H_kv, int D, int max_pages);
+
+/*
+ * ag_kv4_append_rotary - a step's new tokens on their way into the cache, in one launch: K is turned to its position and rounded to bf16, K and V are quantised
+ * into the slots, the turned queries are written (Q_out; Q may be NULL), and the turned keys where K_out is not NULL.  The same bits as ag_rotary_apply followed by ag_kv4_store.
+ *   r     NULL: nothing is turned (pos may be NULL then); with x->from that stores chosen rows, such as the drafts that ag_verify_drafts has accepted
+ *   x     K and V; H_kv and D are the pool's
+ *   slot  device [n_tokens], as in ag_kv4_store: a token whose slot is outside the pool is not stored, its Q_out and K_out are written all the same
+ * Errors: AG_ERR_ARG, AG_ERR_UNSUPPORTED_ARCH, AG_ERR_CUDA.
+ */
+ag_status ag_kv4_append_rotary(const ag_kv4_pool* pool, const ag_rotary* r, const ag_rotary_rows* x, const int32_t* slot, void* cuda_stream);
+
+/* ---- drafted tokens -----------------------------------------------------------------------------------------------------------
+ * A request's drafted tokens form a tree: token 0 is the last one of its text (not in the cache yet), parent[i] < i is the place of the token that token i follows, counted
+ * from the request's first.  Requests lie packed one behind the other, request s owns tokens off[s] .. off[s + 1] - 1 (offsets beyond n_tokens are clamped).
+ */
+#define AG_TREE_MAX 64 /* tokens of a tree */
+typedef struct {
+    const void *Q, *K, *V;  /* device, bf16: token i's rows at Q + i * q_stride, [H_q][D] (K, V: [H_kv][D], the drafted tokens' own); 16-byte aligned */
+    void* O;                /* device, bf16, as Q; must not overlap Q, K or V; rows of tokens that belong to no request are left as they were */
+    int64_t q_stride, k_stride, v_stride, o_stride;  /* elements, multiples of 8, at least the row */
+    int32_t H_q;            /* a multiple of the pool's H_kv, at most 64 times as many */
+    int32_t n_seq;
+    const int32_t* row;     /* device [n_seq]: the requests' table rows; NULL: row s (then n_seq <= table->n_rows).  A row outside the table has no cached tokens */
+    const int32_t* off;     /* device [n_seq + 1] */
+    const int32_t* parent;  /* device [n_tokens]; values outside 0 .. i - 1: none.  NULL: a chain (token i follows token i - 1) */
+    int64_t n_tokens;       /* below 2^30 */
+    int32_t max_tokens;     /* 1 .. AG_TREE_MAX: the most tokens that a request has; tokens beyond get zeros */
+    float scale;            /* 0 = 1 / sqrt(D) */
+} ag_tree_attention;
+/*
+ * attention_tree_kv4 - O[i][hq] = softmax(scale q k) v over what token i sees: every token of its request's cached row, its ancestors in the tree, itself.
+ * Keys and values of the cache are what ag_kv4_load gives (bf16).  Other drafted tokens have no influence, whatever they hold.
+ * Scores, softmax statistics and outputs are accumulated in 32 bits, probabilities are rounded to bf16.  (Values beyond 2^119 / number of keys may overflow.)
+ *   table      lengths are clamped to 0 .. 64 max_pages; tokens whose page is not one of the pool's are left out
+ *   workspace  device, 16-byte aligned, ag_attention_tree_kv4_workspace bytes; its contents mean nothing between calls; calls that may run at the same time need one each
+ * The launch takes every SM of the chip (no plan).  Asynchronous on cuda_stream, may be captured into a graph.  Results are reproducible bit for bit; a request's bits may
+ * change with the other requests of its batch.  Errors: AG_ERR_ARG, AG_ERR_UNSUPPORTED_ARCH, AG_ERR_CUDA.
+ */
+ag_status attention_tree_kv4(const ag_tree_attention* a, const ag_kv4_pool* pool, const ag_kv4_table* table, void* workspace, size_t workspace_bytes,
+                             void* cuda_stream);
+size_t ag_attention_tree_kv4_workspace(int n_seq, int max_tokens, int H_q, int H_kv, int D, int max_pages);
+
+#define AG_F32 0
+#define AG_BF16 1
+typedef struct {
+    const void* P;            /* device, [n_tokens][vocab]: the target's probabilities of what follows token i, at P + i * p_stride; finite, not negative (their sum need not be 1) */
+    const void* Q;            /* device, the same of the drafting model: what token i's children were drawn from.  NULL: drafts that were not drawn (q is 1 at the draft) */
+    int64_t p_stride, q_stride;  /* elements, at least vocab */
+    int32_t type;             /* AG_F32 or AG_BF16, of both */
+    int32_t vocab;            /* 1 .. 2^24 */
+    int32_t distinct;         /* 1: siblings were drawn without repetition (q is 0 at the ones tried before, and divided by what is left of 1); 0: independently */
+    int32_t n_seq;
+    int64_t n_tokens;         /* below 2^30 */
+    const int32_t* off;       /* device [n_seq + 1] */
+    const int32_t* parent;    /* device [n_tokens], as in ag_tree_attention; NULL: chains */
+    const int32_t* token;     /* device [n_tokens]: the drafted tokens (not looked at for a request's first); one outside 0 .. vocab - 1 is not accepted */
+    const float* u;           /* device [n_tokens]: random numbers in [0, 1) for the acceptance (not looked at for a request's first) */
+    const float* u_next;      /* device [n_seq]: the same for the token that follows */
+    int32_t* accepted;        /* device [n_tokens], out: 1 for a request's first token and for every accepted draft, 0 for the others */
+    int32_t* next;            /* device [n_seq], out: the token that follows the last accepted one; -1 for a request without tokens, or where no weight is above 0 */
+    int32_t* new_off;         /* device [n_seq + 1], out: accepted tokens in front of request s, for ag_kv4_extend (both or neither of new_off and from may be NULL) */
+    int32_t* from;            /* device [n_tokens], out: the accepted tokens in order, -1 behind them, for ag_kv4_append_rotary */
+} ag_draft_verification;
+/*
+ * ag_verify_drafts - which drafts stand, and what follows them, such that the text is distributed as if the target had drawn every token itself.  From the first token
+ * on: r = p of the token in hand; its children are tried in order.  Child x is accepted when u q(x) < r(x), and is in hand then; otherwise r becomes max(r - q, 0) / sum
+ * (and stays as it is where that sum is 0).  Where no child is left, the next token is the first v with r(0) + .. + r(v) > u_next * sum of r.
+ * All arithmetic on probabilities is in 64 bits.  Tokens beyond a request's first AG_TREE_MAX are not accepted.
+ * Asynchronous on cuda_stream, may be captured into a graph.  Errors: AG_ERR_ARG, AG_ERR_UNSUPPORTED_ARCH, AG_ERR_CUDA.
+ */
+ag_status ag_verify_drafts(const ag_draft_verification* v, void* cuda_stream);
 
 /*
  * ag_wait_probe - self test of the bounded device-side wait that every kernel of this library

@@ -33,6 +33,7 @@ EXPORTED = [
     "ag_kernel_launch_count", "ag_kv_pack", "ag_kv_info", "ag_kv_append", "ag_kv_destroy", "attention_decode_persistent",
     "ag_kv4_page_bytes", "ag_kv4_store", "ag_kv4_load", "ag_kv4_extend", "ag_kv4_fork", "ag_kv4_free", "ag_kv4_compact", "ag_kv4_copy",
     "attention_decode_kv4", "ag_attention_decode_kv4_workspace", "attention_prompt_persistent",
+    "ag_rotary_frequencies", "ag_rotary_apply", "ag_kv4_append_rotary", "attention_tree_kv4", "ag_attention_tree_kv4_workspace", "ag_verify_drafts",
 ]
 
 
@@ -110,6 +111,41 @@ class PromptAttention(C.Structure):
                 ("H_q", C.c_int32), ("H_kv", C.c_int32), ("D", C.c_int32), ("n_seq", C.c_int32),
                 ("q_off", C.c_void_p), ("kv_off", C.c_void_p), ("q_tokens", C.c_int64), ("kv_tokens", C.c_int64),
                 ("causal", C.c_int32), ("scale", C.c_float)]
+
+
+AG_ROTARY_HALVES, AG_ROTARY_PAIRS = 0, 1
+AG_ROTARY_PLAIN, AG_ROTARY_LINEAR, AG_ROTARY_BANDS, AG_ROTARY_RAMP = range(4)
+AG_TREE_MAX = 64
+AG_F32, AG_BF16 = 0, 1
+
+
+class Rotary(C.Structure):
+    """How heads are turned: Rotary(device pointer to rot / 2 float64 frequencies, rot, AG_ROTARY_HALVES or _PAIRS, magnitude)."""
+    _fields_ = [("freq", C.c_void_p), ("rot", C.c_int32), ("layout", C.c_int32), ("magnitude", C.c_double)]
+
+
+class RotaryScaling(C.Structure):
+    _fields_ = [("rot", C.c_int32), ("scaling", C.c_int32), ("base", C.c_double), ("factor", C.c_double), ("context", C.c_double), ("low", C.c_double),
+                ("high", C.c_double)]
+
+
+class RotaryRows(C.Structure):
+    _fields_ = [("Q", C.c_void_p), ("K", C.c_void_p), ("V", C.c_void_p), ("Q_out", C.c_void_p), ("K_out", C.c_void_p),
+                ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64), ("q_out_stride", C.c_int64), ("k_out_stride", C.c_int64),
+                ("H_q", C.c_int32), ("H_kv", C.c_int32), ("D", C.c_int32), ("n_tokens", C.c_int64), ("pos", C.c_void_p), ("from_", C.c_void_p), ("n_rows", C.c_int64)]
+
+
+class TreeAttention(C.Structure):
+    _fields_ = [("Q", C.c_void_p), ("K", C.c_void_p), ("V", C.c_void_p), ("O", C.c_void_p),
+                ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64), ("o_stride", C.c_int64),
+                ("H_q", C.c_int32), ("n_seq", C.c_int32), ("row", C.c_void_p), ("off", C.c_void_p), ("parent", C.c_void_p), ("n_tokens", C.c_int64),
+                ("max_tokens", C.c_int32), ("scale", C.c_float)]
+
+
+class DraftVerification(C.Structure):
+    _fields_ = [("P", C.c_void_p), ("Q", C.c_void_p), ("p_stride", C.c_int64), ("q_stride", C.c_int64), ("type", C.c_int32), ("vocab", C.c_int32),
+                ("distinct", C.c_int32), ("n_seq", C.c_int32), ("n_tokens", C.c_int64), ("off", C.c_void_p), ("parent", C.c_void_p), ("token", C.c_void_p),
+                ("u", C.c_void_p), ("u_next", C.c_void_p), ("accepted", C.c_void_p), ("next", C.c_void_p), ("new_off", C.c_void_p), ("from_", C.c_void_p)]
 
 
 class AgError(RuntimeError):
@@ -194,6 +230,13 @@ def lib() -> C.CDLL:
     L.attention_decode_kv4.argtypes = [vp, pool, table, vp, vp, C.c_int, C.c_int, vp, sz, vp]
     L.ag_attention_decode_kv4_workspace.argtypes = [C.c_int] * 5
     L.ag_attention_decode_kv4_workspace.restype = sz
+    L.ag_rotary_frequencies.argtypes = [C.POINTER(RotaryScaling), vp, C.POINTER(C.c_double)]
+    L.ag_rotary_apply.argtypes = [C.POINTER(Rotary), C.POINTER(RotaryRows), vp]
+    L.ag_kv4_append_rotary.argtypes = [pool, C.POINTER(Rotary), C.POINTER(RotaryRows), vp, vp]
+    L.attention_tree_kv4.argtypes = [C.POINTER(TreeAttention), pool, table, vp, sz, vp]
+    L.ag_attention_tree_kv4_workspace.argtypes = [C.c_int] * 6
+    L.ag_attention_tree_kv4_workspace.restype = sz
+    L.ag_verify_drafts.argtypes = [C.POINTER(DraftVerification), vp]
     L.ag_cluster_capacity.argtypes = [vp, C.POINTER(TopoMap), C.c_int, C.POINTER(C.c_int32)]
     L.ag_probe_cluster_layout.argtypes = [C.c_int, C.c_int, vp]
     L.ag_topo_save.argtypes = [C.POINTER(TopoMap), C.c_char_p]
@@ -669,6 +712,60 @@ def attention_decode_kv4(q_ptr: int, pool: KV4Pool, table: KV4Table, row_ptr, o_
     attention_decode_kv4_workspace bytes) is the caller's and always needed."""
     _check(lib().attention_decode_kv4(q_ptr, C.byref(pool), C.byref(table), row_ptr, o_ptr, B, H_q, workspace_ptr, workspace_bytes, stream),
            "attention_decode_kv4")
+
+
+# ---- rotary positions and drafted tokens --------------------------------------------------------------
+def rotary_frequencies(rot: int, base: float = 10000.0, scaling: int = AG_ROTARY_PLAIN, factor: float = 1.0, context: float = 0.0, low: float = 0.0,
+                       high: float = 0.0):
+    """(float64 array of rot / 2 radians a position, magnitude) for Rotary; the array belongs on the device."""
+    freq, magnitude = np.empty(max(rot // 2, 1), dtype=np.float64), C.c_double()
+    spec = RotaryScaling(rot, scaling, base, factor, context, low, high)
+    _check(lib().ag_rotary_frequencies(C.byref(spec), freq.ctypes.data, C.byref(magnitude)), "ag_rotary_frequencies")
+    return freq, magnitude.value
+
+
+def rotary_apply(rotary: Rotary, pos_ptr: int, n_tokens: int, D: int, q_ptr=None, q_out_ptr=None, H_q: int = 0, k_ptr=None, k_out_ptr=None, H_kv: int = 0,
+                 q_stride: int | None = None, k_stride: int | None = None, q_out_stride: int | None = None, k_out_stride: int | None = None, from_ptr=None,
+                 n_rows: int = 0, stream: int = 0):
+    """Rows of Q and K ([H][D] bf16, strides in elements; either may be left out) turned to the positions pos[i]."""
+    wq, wk = H_q * D, H_kv * D
+    x = RotaryRows(q_ptr, k_ptr, None, q_out_ptr, k_out_ptr, wq if q_stride is None else q_stride, wk if k_stride is None else k_stride, 0,
+                   wq if q_out_stride is None else q_out_stride, wk if k_out_stride is None else k_out_stride, H_q, H_kv, D, n_tokens, pos_ptr, from_ptr, n_rows)
+    _check(lib().ag_rotary_apply(C.byref(rotary), C.byref(x), stream), "ag_rotary_apply")
+
+
+def kv4_append_rotary(pool: KV4Pool, rotary: Rotary | None, pos_ptr, slot_ptr: int, n_tokens: int, k_ptr: int, v_ptr: int, k_out_ptr=None, q_ptr=None,
+                      q_out_ptr=None, H_q: int = 0, k_stride: int | None = None, v_stride: int | None = None, q_stride: int | None = None,
+                      q_out_stride: int | None = None, k_out_stride: int | None = None, from_ptr=None, n_rows: int = 0, stream: int = 0):
+    """K turned and stored, V stored, Q turned beside them (rotary None: nothing is turned); from_ptr: the rows to take, out of n_rows."""
+    wq, wk = H_q * pool.D, pool.H_kv * pool.D
+    x = RotaryRows(q_ptr, k_ptr, v_ptr, q_out_ptr, k_out_ptr, wq if q_stride is None else q_stride, wk if k_stride is None else k_stride,
+                   wk if v_stride is None else v_stride, wq if q_out_stride is None else q_out_stride, wk if k_out_stride is None else k_out_stride, H_q, pool.H_kv,
+                   pool.D, n_tokens, pos_ptr, from_ptr, n_rows)
+    _check(lib().ag_kv4_append_rotary(C.byref(pool), None if rotary is None else C.byref(rotary), C.byref(x), slot_ptr, stream), "ag_kv4_append_rotary")
+
+
+def attention_tree_kv4_workspace(n_seq: int, max_tokens: int, H_q: int, H_kv: int, D: int, max_pages: int) -> int:
+    return int(lib().ag_attention_tree_kv4_workspace(n_seq, max_tokens, H_q, H_kv, D, max_pages))
+
+
+def attention_tree_kv4(q_ptr: int, k_ptr: int, v_ptr: int, o_ptr: int, pool: KV4Pool, table: KV4Table, row_ptr, off_ptr: int, parent_ptr, n_seq: int, n_tokens: int,
+                       max_tokens: int, H_q: int, workspace_ptr: int, workspace_bytes: int, q_stride: int | None = None, k_stride: int | None = None,
+                       v_stride: int | None = None, o_stride: int | None = None, scale: float = 0.0, stream: int = 0):
+    """Drafted tokens over the 4-bit cache and their ancestors among themselves; request s reads table row row[s] (row_ptr None: row s), parent_ptr None: chains."""
+    wq, wk = H_q * pool.D, pool.H_kv * pool.D
+    a = TreeAttention(q_ptr, k_ptr, v_ptr, o_ptr, wq if q_stride is None else q_stride, wk if k_stride is None else k_stride, wk if v_stride is None else v_stride,
+                      wq if o_stride is None else o_stride, H_q, n_seq, row_ptr, off_ptr, parent_ptr, n_tokens, max_tokens, scale)
+    _check(lib().attention_tree_kv4(C.byref(a), C.byref(pool), C.byref(table), workspace_ptr, workspace_bytes, stream), "attention_tree_kv4")
+
+
+def verify_drafts(p_ptr: int, q_ptr, vocab: int, token_ptr: int, parent_ptr, off_ptr: int, n_seq: int, n_tokens: int, u_ptr: int, u_next_ptr: int, accepted_ptr: int,
+                  next_ptr: int, new_off_ptr=None, from_ptr=None, p_stride: int | None = None, q_stride: int | None = None, bf16: bool = False, distinct: bool = False,
+                  stream: int = 0):
+    """Accepts drafts against the target's probabilities p (drawn from q; q_ptr None: not drawn) and samples the token behind them."""
+    v = DraftVerification(p_ptr, q_ptr, vocab if p_stride is None else p_stride, vocab if q_stride is None else q_stride, AG_BF16 if bf16 else AG_F32, vocab,
+                          1 if distinct else 0, n_seq, n_tokens, off_ptr, parent_ptr, token_ptr, u_ptr, u_next_ptr, accepted_ptr, next_ptr, new_off_ptr, from_ptr)
+    _check(lib().ag_verify_drafts(C.byref(v), stream), "ag_verify_drafts")
 
 
 def suggest_k_splits(N: int, K: int, sm_budget: int, overlapping_full_chip: bool = False) -> int:

@@ -10,11 +10,6 @@
 namespace ag {
 
 // ---- store and load ---------------------------------------------------------------------------------------------------
-// Quantisation of a group x_0 .. x_31: lo = min, s = bf16((max - lo) / 15), code = rint((x - lo) / s) in 0 .. 15, and an element
-// stands for s code + lo.  lo is an element, so it is a bf16 already; s is rounded to bf16 first and the codes are taken for the
-// rounded one, so that the rounding costs at most 2^-9 of a step.  All in 32 bits with IEEE rounding: the codes do not depend on the kernel.
-// A group with a value that is not finite, or whose range is not, stands for NaN throughout.
-//
 // D / 16 lanes hold a row, sixteen elements each: a lane's K codes are two words of the page, the V codes are transposed across lanes
 // (kv4_transpose) so that a lane writes whole words of the fragment order as well.  With eight elements a lane the part of the work that goes by
 // lanes (addresses, scales, exchanges) took twice as long: 86 and 51 us for 46k tokens x 8 heads stored and read back,
@@ -22,17 +17,6 @@ namespace ag {
 //
 // A block takes U times 128 / L neighbouring tokens of one head: the words of neighbouring V rows share sectors, and U rows a lane are in
 // flight together (a row's chain slot -> page -> row is some 2 us long).
-__device__ __forceinline__ uint32_t min_bf16x2(uint32_t a, uint32_t b) {
-    uint32_t r;
-    asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
-}
-__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
-    uint32_t r;
-    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
-}
-
 constexpr int KS_THREADS = 256;
 constexpr int KS_ROWS = 2;                           // U of large calls; small ones take 1, for more blocks
 
@@ -66,64 +50,10 @@ __global__ void __launch_bounds__(KS_THREADS) k_kv4_store(uint8_t* pages, long l
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const uint32_t in[8] = {raw[u][0].x, raw[u][0].y, raw[u][0].z, raw[u][0].w, raw[u][1].x, raw[u][1].y, raw[u][1].z, raw[u][1].w};
-        // extremes of the group, in pairs; NaN wins, and an infinity makes the range infinite or NaN
-        uint32_t lo2 = in[0], hi2 = in[0];
-#pragma unroll
-        for (int i = 1; i < 8; ++i) {
-            lo2 = min_bf16x2(lo2, in[i]);
-            hi2 = max_bf16x2(hi2, in[i]);
-        }
-        lo2 = min_bf16x2(lo2, __shfl_xor_sync(0xffffffffu, lo2, 1));
-        hi2 = max_bf16x2(hi2, __shfl_xor_sync(0xffffffffu, hi2, 1));
-        const float lo = bf16_lo(min_bf16x2(lo2, lo2 >> 16)), hi = bf16_lo(max_bf16x2(hi2, hi2 >> 16));
-        const __nv_bfloat16 sb = __float2bfloat16_rn(__fdiv_rn(__fsub_rn(hi, lo), 15.f));
-        const float s = __bfloat162float(sb);
-        const bool fine = s <= 3.4e38f;                             // false for NaN and infinity
-        // rint((x - lo) / s): the quotient from the correctly rounded reciprocal and one step on the exact remainder, which is the correctly
-        // rounded quotient (Markstein) while nothing over- or underflows; four codes are gathered as one number in base 16.
-        uint32_t w[2] = {0, 0};
-        if (s >= 0x1p-90f && s <= 0x1p100f) {
-            constexpr float M = 12582912.f;                         // 1.5 * 2^23: adding it rounds to an integer, halves to even
-            const float inv = __frcp_rn(s);
-            float number[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int i = 15; i >= 0; --i) {
-                const float d = __fsub_rn(i & 1 ? bf16_hi(in[i >> 1]) : bf16_lo(in[i >> 1]), lo);
-                const float q1 = __fmul_rn(d, inv), q = __fmaf_rn(__fmaf_rn(-q1, s, d), inv, q1);
-                number[i >> 2] = __fmaf_rn(number[i >> 2], 16.f, __fsub_rn(__fadd_rn(q, M), M));
-            }
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-                w[k] = __byte_perm(__float_as_uint(number[2 * k] + 8388608.f), __float_as_uint(number[2 * k + 1] + 8388608.f), 0x5410);
-        } else if (fine && s > 0.f) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float d = __fsub_rn(i & 1 ? bf16_hi(in[i >> 1]) : bf16_lo(in[i >> 1]), lo);
-                w[i >> 3] |= (uint32_t)min(15, __float2int_rn(__fdiv_rn(d, s))) << (4 * (i & 7));
-            }
-        }
-        if (which) {                                                // lane l has elements 16 l + 8 j + g, word j: then word j holds elements 16 i + 8 j + l
-            w[0] = kv4_transpose<D / 16, 1>(w[0], l);
-            w[1] = kv4_transpose<D / 16, 1>(w[1], l);
-        }
+        uint32_t w[2];
+        const uint32_t pair = kv4_quantise<D>(in, which, l, w);
         if (at[u] < 0 || at[u] >= n_slots) continue;
-        uint8_t* block = pages + ((size_t)(at[u] / KV4_PAGE) * H_kv + head) * kv4_head_bytes(D);
-        const int r = at[u] % KV4_PAGE;
-        if (which == 0) {
-            uint8_t* to = block + kv4_k_word<D>(r, l >> 1, 2 * (l & 1));
-            *reinterpret_cast<uint32_t*>(to) = w[0];
-            *reinterpret_cast<uint32_t*>(to + D / 8) = w[1];
-        } else if (D == 128) {
-            *reinterpret_cast<uint2*>(block + kv4_v_word<D>(r, 0, l)) = make_uint2(w[0], w[1]);
-        } else {
-            *reinterpret_cast<uint32_t*>(block + kv4_v_word<D>(r, 0, l)) = __byte_perm(w[0], w[1], 0x5410);
-            *reinterpret_cast<uint32_t*>(block + kv4_v_word<D>(r, 0, 4 + l)) = __byte_perm(w[0], w[1], 0x7632);
-        }
-        if ((l & 1) == 0) {
-            const uint32_t nan = 0x7fc07fc0u;
-            const uint32_t pair = (uint32_t)__bfloat16_as_ushort(sb) | (__float_as_uint(lo) & 0xffff0000u);
-            *reinterpret_cast<uint32_t*>(block + kv4_scale_word<D>(which, r, l >> 1)) = fine ? pair : nan;
-        }
+        kv4_put<D>(pages + ((size_t)(at[u] / KV4_PAGE) * H_kv + head) * kv4_head_bytes(D), which, at[u] % KV4_PAGE, l, w, pair);
     }
 }
 
@@ -607,22 +537,6 @@ static bool misaligned(const int32_t* a, const int32_t* b = nullptr, const int32
 
 static TableArgs table_args(const ag_kv4_pool* pool, const ag_kv4_table* t) {
     return TableArgs{t->page_of, t->len, t->refs, t->n_rows, t->max_pages, (int)pool->n_pages};
-}
-
-// Launch that may come up while the launch before it on the stream finishes; the kernel itself waits for it (dep_wait) before it touches memory.
-template <class... P, class... A>
-static cudaError_t launch_dependent(void (*kernel)(P...), unsigned grid, unsigned block, cudaStream_t stream, A... args) {
-    cudaLaunchConfig_t cfg;
-    memset(&cfg, 0, sizeof cfg);
-    cfg.gridDim = dim3(grid);
-    cfg.blockDim = dim3(block);
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
 }
 
 }  // namespace ag
