@@ -1,15 +1,48 @@
 // Attention of drafted tokens over the 4-bit cache and over one another (a tree): see include/asymgemm.h, "drafted tokens".
+//
+// Work unit = (request, KV head, up to 256 rows), a row being a (token, head of the group) pair: all rows of a unit share every key.  A unit's keys are tiles of 128:
+// tile 0 the drafted tokens themselves (64 at most), tile t two pages of the cache.  With 128 rows and 128 keys a tile is
+//     S = Q K^T              tcgen05.mma, 128 x 128 x D, fp16 operands, scores in tensor memory
+//     P = 2^(S - m)          one thread a row; P as fp16 back into tensor memory, over the scores
+//     O += P V               tcgen05.mma with the A operand in tensor memory
+// Two tiles are in flight, w = 0, 1, each with scores, statistics and outputs of its own:
+//     more than 128 rows     w = half of the rows, both see every key tile: keys and values are decoded once for 256 rows
+//     up to 128 rows         w = parity of the key tile
+//     up to 64 (32) rows     besides, the 128 lanes hold the rows twice (four times), each copy has one half (quarter) of the tile's keys and zeros as the other
+//                            probabilities: the MMAs cost the same, the exponentials a half (a quarter)
+// and the statistics and outputs of all copies are put together at the end of the unit.
+//
+// Codes become fp16 operands in shared memory: a nibble in the lowest (or next) four bits of a half is the subnormal u 2^-24 (u 2^-20), and one multiply-add
+// with s 2^24 (s 2^20) and the base gives s u + b, rounded once.  For that a tile's values are taken at a power of two that puts the largest below 2^-5: K's for every
+// tile on its own (scores are multiplied back with the row's factor), V's for the run of a unit (outputs move when it grows).  Inside a chunk of eight operand elements
+// the order is that of the nibbles, (0, 4), (1, 5), (2, 6), (3, 7); Q is laid out the same, and V's columns are put back when the outputs are written.
+//
+// All tiles of all units stand in one line that is cut into equal runs, one per block: uneven lengths, one long request or many short ones are the same case.  Units that
+// two or more blocks share leave parts (normalised outputs, maximum, sum) in the workspace, which a second launch puts together.
+//
+// 640 threads: warps 0-7 softmax and epilogue (two groups of four), 8 MMA, 9 units and copies, 10 exponents, 11 idle, 12-19 decoding into operands.
 #include <math.h>
 #include <string.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "kv4.cuh"
 
 namespace ag {
 
-constexpr int TA_THREADS = 256;
-constexpr int TA_ROWS = 4;                 // rows (token, head of the group) of a warp
+constexpr int TA_TILE = 128;
+constexpr int TA_OPS = 3, TA_CODES = 5, TA_SCALES = 4;     // stages: operands; raw codes; raw (scale, base) pairs
+constexpr int TA_INFO = 8, TA_UNITS = 4;
+constexpr int TA_SOFT = 8, TA_DECODERS = 8;                // warps
+constexpr int TA_THREADS = 640;
+constexpr int TA_READERS = TA_SOFT + TA_DECODERS + 2;      // warps that read a unit: and MMA, exponents
+constexpr int TA_REGS_SOFT = 144, TA_REGS_OTHER = 64;      // 256 x 144 + 384 x 64 = 640 x 96
+constexpr int TA_BLOCKS = 148;
+constexpr int TA_LEAST = 4;                                // tiles of a block's run, at least
+constexpr float TA_LAZY = 5.f;                             // the reference m of a row moves when its maximum has grown by more than 2^5
+constexpr float TA_SHIFT = 10.f;                           // P is taken times 2^10: at most 2^15, down to 2^-35 of the largest without rounding to zero
+constexpr uint64_t TA_LIMIT_NS = 4000000000ull;
 
 struct TreeArgs {
     const uint16_t *Q, *K, *V;
@@ -17,130 +50,985 @@ struct TreeArgs {
     const uint8_t* pages;
     long long q_stride, k_stride, v_stride, o_stride, n_tokens;
     const int32_t *row, *off, *parent, *page_of, *len;
-    int H_q, H_kv, G, n_seq, n_rows, max_pages, n_pages, max_tokens, tiles;
+    int H_q, H_kv, G, n_seq, n_rows, max_pages, n_pages, max_tokens, part_rows;
     float scale_log2e;
+    int32_t* status;
+    struct TreeCross* cross;               // [blocks]: the unit that begins in block i and goes on beyond it
+    float2* stats;                         // [2 blocks][part_rows]
+    float* part;                           // [2 blocks][part_rows][D]
+};
+struct TreeCross {
+    long long begin, quota;                // place of the unit's first tile in the line; tiles of a run
+    int weight, tiles, token0, row0, rows, head, pad[2];
+};
+
+struct TreeUnit {
+    int token0, n;                         // the request's first drafted token, their number
+    int row0, rows;                        // of the request's rows
+    int len, table_row, head;
+    int tile0, tile1, tiles;               // this block's tiles, the unit's
+    int two, copies, buf;                  // rows in both halves; copies of the rows; buffer of Q (two: both)
+    int slot;                              // part slot, -1: the whole unit is here
+    int stop, pad;
+};
+struct TreeInfo {
+    int ek, ev, v0, v1, odd;               // exponents of K and V; keys that count in the tile's halves; a drafted value is not finite
+};
+
+struct TreeCtl {
+    uint64_t q_full[2], q_empty[2], op_full[TA_OPS], op_empty[TA_OPS], codes_full[TA_CODES], codes_empty[TA_CODES];
+    uint64_t scales_full[TA_SCALES], scales_ready[TA_SCALES], scales_empty[TA_SCALES];
+    uint64_t s_full[2], p_full[2], pv_done[2], unit_full[TA_UNITS], unit_empty[TA_UNITS], together, drain;
+    unsigned long long sees[2][AG_TREE_MAX];
+    float row_scale[2][TA_TILE];
+    float2 stats[2 * TA_TILE];
+    TreeUnit unit[TA_UNITS];
+    TreeInfo info[TA_INFO];
+    int valid[TA_INFO][2];
+    long long warp_sum[TA_THREADS / 32];
+    long long total, start_before;
+    uint32_t tmem_base;
+    int abort_flag, start_seq, odd;
 };
 
 template <int D>
-__global__ void __launch_bounds__(TA_THREADS) k_tree(const TreeArgs x) {
-    constexpr int WARPS = TA_THREADS / 32, BLOCK_ROWS = WARPS * TA_ROWS;
-    extern __shared__ float tree_smem[];
-    float* ks = tree_smem;                                     // [64][D + 1]
-    float* vs = ks + 64 * (D + 1);                             // [64][D]
-    float* qs = vs + 64 * D;                                   // [BLOCK_ROWS][D]
-    __shared__ unsigned long long sees[AG_TREE_MAX];
-    __shared__ float ps[WARPS][64];
+struct TCfg {
+    static constexpr int op_bytes = TA_TILE * D * 2;       // a tile of operands, and of Q
+    static constexpr int code_bytes = 2 * 32 * D;          // K's or V's codes of two pages
+    static constexpr int scale_bytes = 2 * 16 * D;         // K's and V's pairs of two pages
+    static constexpr int smem_bytes = (2 + TA_OPS) * op_bytes + TA_CODES * code_bytes + TA_SCALES * scale_bytes + (int)((sizeof(TreeCtl) + 127) / 128 * 128) + 1024;
+};
+static_assert(TCfg<128>::smem_bytes <= 227 * 1024, "does not fit");
+constexpr int TA_MIN_SMEM = 120 * 1024;                    // one block an SM: it takes all of the tensor memory
+
+__device__ __forceinline__ float pow2i(int k) { return __uint_as_float((uint32_t)(127 + k) << 23); }     // -126 .. 127
+// v 2^k for any k of -250 .. 250
+__device__ __forceinline__ float times_pow2(float v, int k) { return v * pow2i(k >> 1) * pow2i(k - (k >> 1)); }
+
+// Eight codes of a word times scales plus bases, as four pairs (0, 4), (1, 5), (2, 6), (3, 7): a (scales 2^24 and 2^20, bases) for the first two, b for the others.
+struct Scale2 {
+    uint32_t s24, s20, base;
+};
+__device__ __forceinline__ uint4 decode_word(uint32_t w, const Scale2& a, const Scale2& b) {
+    const uint32_t v = w >> 8;
+    return make_uint4(fma_f16x2(w & 0x000f000fu, a.s24, a.base), fma_f16x2(w & 0x00f000f0u, a.s20, a.base), fma_f16x2(v & 0x000f000fu, b.s24, b.base),
+                      fma_f16x2(v & 0x00f000f0u, b.s20, b.base));
+}
+// k24 = 2^(24 - exponent): scales and bases of two groups side by side
+__device__ __forceinline__ Scale2 scale_pair(uint32_t lo, uint32_t hi, float k24) {
+    const float k20 = k24 * 0.0625f, k0 = k20 * 0x1p-20f;
+    const float s0 = bf16_lo(lo), s1 = bf16_lo(hi);
+    return Scale2{pack_f16(s0 * k24, s1 * k24), pack_f16(s0 * k20, s1 * k20), pack_f16(bf16_hi(lo) * k0, bf16_hi(hi) * k0)};
+}
+
+// A request: its drafted tokens, cached tokens and place in the line (for every KV head `per_head` tiles).
+struct TreeSeq {
+    int first, n, rows, len, table_row, tiles, weight;     // weight: of all units of a head, a unit of more than 128 rows counting twice
+    __device__ __forceinline__ long long line(int H_kv) const { return (long long)H_kv * weight * tiles; }
+};
+__device__ __forceinline__ TreeSeq tree_seq(const TreeArgs& x, int s) {
+    TreeSeq r;
+    const long long first = min(max((long long)x.off[s], 0ll), x.n_tokens), stop = min(max((long long)x.off[s + 1], first), x.n_tokens);
+    r.first = (int)first;
+    r.n = (int)min(stop - first, (long long)x.max_tokens);
+    r.rows = r.n * x.G;
+    r.table_row = x.row ? x.row[s] : s;
+    r.len = r.table_row >= 0 && r.table_row < x.n_rows ? (int)min((long long)max(x.len[r.table_row], 0), 64ll * x.max_pages) : 0;
+    r.tiles = (r.len + TA_TILE - 1) / TA_TILE + 1;
+    const int rest = r.rows % 256;
+    r.weight = r.rows / 256 * 2 + (rest > 128 ? 2 : rest > 0 ? 1 : 0);
+    return r;
+}
+// tiles of the unit at place `begin` of the line that lie in the run [p0, p1)
+__device__ __forceinline__ int tiles_before(long long place, long long begin, int weight, int tiles) {
+    return (int)min(max((place - begin + weight - 1) / weight, 0ll), (long long)tiles);
+}
+
+template <int D>
+__global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs x) {
+    using C = TCfg<D>;
+    constexpr int NG = D / 32;
+    extern __shared__ uint8_t tree_smem[];
+    uint8_t* smem = tree_smem + ((1024 - (smem_u32(tree_smem) & 1023)) & 1023);
+    uint8_t* q_smem = smem;
+    uint8_t* op_smem = q_smem + 2 * C::op_bytes;
+    uint8_t* code_smem = op_smem + TA_OPS * C::op_bytes;
+    uint8_t* scale_smem = code_smem + TA_CODES * C::code_bytes;
+    TreeCtl* ctl = reinterpret_cast<TreeCtl*>(scale_smem + TA_SCALES * C::scale_bytes);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    volatile int* abort_flag = &ctl->abort_flag;
+
+    if (tid == 0) {
+        ctl->abort_flag = 0;
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&ctl->q_full[i]), TA_DECODERS);
+            mbar_init(smem_u32(&ctl->q_empty[i]), TA_SOFT);
+            mbar_init(smem_u32(&ctl->s_full[i]), 2);
+            mbar_init(smem_u32(&ctl->p_full[i]), 4);
+            mbar_init(smem_u32(&ctl->pv_done[i]), 1);
+        }
+        for (int i = 0; i < TA_OPS; ++i) {
+            mbar_init(smem_u32(&ctl->op_full[i]), TA_DECODERS);
+            mbar_init(smem_u32(&ctl->op_empty[i]), 1);
+        }
+        for (int i = 0; i < TA_CODES; ++i) {
+            mbar_init(smem_u32(&ctl->codes_full[i]), 1);
+            mbar_init(smem_u32(&ctl->codes_empty[i]), TA_DECODERS);
+        }
+        for (int i = 0; i < TA_SCALES; ++i) {
+            mbar_init(smem_u32(&ctl->scales_full[i]), 1);
+            mbar_init(smem_u32(&ctl->scales_ready[i]), 1);
+            mbar_init(smem_u32(&ctl->scales_empty[i]), TA_DECODERS);
+        }
+        for (int i = 0; i < TA_UNITS; ++i) {
+            mbar_init(smem_u32(&ctl->unit_full[i]), 1);
+            mbar_init(smem_u32(&ctl->unit_empty[i]), TA_READERS);
+        }
+        mbar_init(smem_u32(&ctl->together), TA_SOFT);
+        mbar_init(smem_u32(&ctl->drain), 1);
+        mbar_fence_init();
+    }
+    if (warp == 8) {
+        tmem_alloc(smem_u32(&ctl->tmem_base), 512);
+        tmem_relinquish();
+    }
     dep_wait();
     dep_release();
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int tile = blockIdx.x % x.tiles, hk = blockIdx.x / x.tiles % x.H_kv, seq = blockIdx.x / x.tiles / x.H_kv;
-    const long long first = min(max((long long)x.off[seq], 0ll), x.n_tokens), stop = min(max((long long)x.off[seq + 1], first), x.n_tokens);
-    const int n = (int)min(stop - first, (long long)x.max_tokens);
-    if (tile == 0)
-        for (long long i = first + n; i < stop; ++i)
-            for (int d = tid; d < x.G * D; d += TA_THREADS) x.O[i * x.o_stride + (long long)hk * x.G * D + d] = 0;
-    const int rows = n * x.G, r0 = tile * BLOCK_ROWS;
-    if (r0 >= rows) return;
-    const int table_row = x.row ? x.row[seq] : seq;
-    const int len = table_row >= 0 && table_row < x.n_rows ? (int)min((long long)max(x.len[table_row], 0), 64ll * x.max_pages) : 0;
-    if (tid < n) {
-        unsigned long long m = 0;
-        for (int i = tid; i >= 0;) {
-            m |= 1ull << i;
-            const int p = x.parent ? x.parent[first + i] : i - 1;
-            i = p < i ? p : -1;
+
+    // ---- the block's run of the line
+    const int per = (x.n_seq + TA_THREADS - 1) / TA_THREADS, s0 = min(tid * per, x.n_seq), s1 = min(s0 + per, x.n_seq);
+    long long mine = 0;
+    for (int s = s0; s < s1; ++s) mine += tree_seq(x, s).line(x.H_kv);
+    long long inc = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long up = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += up;
+    }
+    if (lane == 31) ctl->warp_sum[warp] = inc;
+    __syncthreads();
+    long long before = inc - mine, total = 0;
+    for (int w = 0; w < TA_THREADS / 32; ++w) {
+        if (w < warp) before += ctl->warp_sum[w];
+        total += ctl->warp_sum[w];
+    }
+    const long long quota = max((total + gridDim.x - 1) / gridDim.x, (long long)TA_LEAST);
+    const long long p0 = min(quota * blockIdx.x, total), p1 = min(p0 + quota, total);
+    if (p0 < p1 && before <= p0 && p0 < before + mine) {
+        long long at = before;
+        int s = s0;
+        for (; s < s1; ++s) {
+            const long long l = tree_seq(x, s).line(x.H_kv);
+            if (p0 < at + l) break;
+            at += l;
         }
-        sees[tid] = m;
+        ctl->start_seq = s;
+        ctl->start_before = at;
     }
-    for (int i = tid; i < BLOCK_ROWS * D; i += TA_THREADS) {
-        const int r = r0 + i / D;
-        qs[i] = r < rows ? __uint_as_float((uint32_t)x.Q[(first + r / x.G) * x.q_stride + (hk * x.G + r % x.G) * D + i % D] << 16) * x.scale_log2e : 0.f;
+    if (tid == 0) {
+        if (blockIdx.x == 0) *x.status = AG_OK;
+        x.cross[blockIdx.x].rows = 0;
     }
-    float m[TA_ROWS], l[TA_ROWS], o[TA_ROWS][D / 32];
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = ctl->tmem_base;
+    const uint64_t limit = TA_LIMIT_NS;
+    bool ok = true;
+    auto wait = [&](uint64_t* b, uint32_t parity) -> bool {
+        if (ok && !mbar_wait_all(smem_u32(b), parity, abort_flag, limit)) {
+            if (lane == 0) *x.status = AG_ERR_TIMEOUT;
+            ok = false;
+        }
+        return ok;
+    };
+    auto next_unit = [&](uint32_t u, TreeUnit& r) -> bool {
+        if (!wait(&ctl->unit_full[u % TA_UNITS], (u / TA_UNITS) & 1)) return false;
+        r = ctl->unit[u % TA_UNITS];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&ctl->unit_empty[u % TA_UNITS]));
+        return !r.stop;
+    };
+    TreeUnit un;
+
+    if (warp >= TA_SOFT) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(TA_REGS_OTHER));
+    if (warp == 9) {
+        // ------------------------------------------------ units, and copies of their pages
+        uint32_t u = 0, n_tile = 0, n_code = 0, toggle = 0;
+        long long at = ctl->start_before;
+        int s = p0 < p1 ? ctl->start_seq : x.n_seq;
+        while (ok && s < x.n_seq && at < p1) {
+            const TreeSeq q = tree_seq(x, s);
+            const long long line = q.line(x.H_kv), per_head = (long long)q.weight * q.tiles;
+            const int units = (q.rows + 255) / 256;
+            for (int h = at < p0 && line > 0 ? (int)((p0 - at) / per_head) : 0; ok && h < x.H_kv && line > 0; ++h) {
+                if (at + h * per_head >= p1) break;
+                for (int i = 0; ok && i < units; ++i) {
+                    const long long begin = at + h * per_head + (long long)i * 2 * q.tiles;
+                    const int rows = min(q.rows - i * 256, 256), weight = rows > 128 ? 2 : 1;
+                    const int t0 = tiles_before(p0, begin, weight, q.tiles), t1 = tiles_before(p1, begin, weight, q.tiles);
+                    if (t0 >= t1) continue;
+                    if (!wait(&ctl->unit_empty[u % TA_UNITS], ((u / TA_UNITS) & 1) ^ 1)) break;
+                    const int two = rows > 128, buf = two ? 0 : (int)(toggle & 1);
+                    toggle += two ? 0 : 1;
+                    if (lane == 0) {
+                        TreeUnit r;
+                        r.token0 = q.first; r.n = q.n; r.row0 = i * 256; r.rows = rows; r.len = q.len; r.table_row = q.table_row; r.head = h;
+                        r.tile0 = t0; r.tile1 = t1; r.tiles = q.tiles; r.two = two; r.copies = rows <= 32 ? 4 : rows <= 64 ? 2 : 1; r.buf = buf;
+                        r.slot = t0 == 0 && t1 == q.tiles ? -1 : 2 * (int)blockIdx.x + (t1 < q.tiles ? 1 : 0);
+                        r.stop = 0; r.pad = 0;
+                        ctl->unit[u % TA_UNITS] = r;
+                        mbar_arrive(smem_u32(&ctl->unit_full[u % TA_UNITS]));
+                        if (t0 == 0 && t1 < q.tiles) {
+                            TreeCross c;
+                            c.begin = begin; c.quota = quota; c.weight = weight; c.tiles = q.tiles; c.token0 = q.first; c.row0 = i * 256; c.rows = rows; c.head = h;
+                            c.pad[0] = c.pad[1] = 0;
+                            x.cross[blockIdx.x] = c;
+                        }
+                    }
+                    __syncwarp();
+                    ++u;
+                    // pages of the next 16 tiles in the lanes: lane l has page 32 window + l of the row
+                    int window = -1, page = -1;
+                    const int nt = t1 - t0, lead = two ? 1 : 2;
+                    auto copy = [&](int which, int j) {
+                        const int t = t0 + j;
+                        const uint32_t n = n_tile + j;
+                        if (which == 0 && !wait(&ctl->scales_empty[n % TA_SCALES], ((n / TA_SCALES) & 1) ^ 1)) return;
+                        if (t == 0) {                              // the drafted tokens: nothing to copy
+                            if (which == 0 && lane == 0) {
+                                ctl->valid[n % TA_INFO][0] = min(q.n, 64);
+                                ctl->valid[n % TA_INFO][1] = 0;
+                                mbar_arrive(smem_u32(&ctl->scales_full[n % TA_SCALES]));
+                            }
+                            __syncwarp();
+                            return;
+                        }
+                        const int c = 2 * (t - 1);
+                        if (c / 32 != window) {
+                            window = c / 32;
+                            page = window * 32 + lane < (q.len + 63) / 64 ? x.page_of[(size_t)q.table_row * x.max_pages + window * 32 + lane] : -1;
+                        }
+                        if (!wait(&ctl->codes_empty[n_code % TA_CODES], ((n_code / TA_CODES) & 1) ^ 1)) return;
+                        int id[2], v[2];
 #pragma unroll
-    for (int i = 0; i < TA_ROWS; ++i) {
-        m[i] = -INFINITY;
-        l[i] = 0.f;
-#pragma unroll
-        for (int d = 0; d < D / 32; ++d) o[i][d] = 0.f;
-    }
-    const int pages = (len + 63) / 64;
-#pragma unroll 1
-    for (int c = 0; c <= pages; ++c) {                         // the pages, then the drafted tokens
-        __syncthreads();
-        unsigned long long there = ~0ull;
-        if (c < pages) {
-            const int page = x.page_of[(size_t)table_row * x.max_pages + c];
-            if (page < 0 || page >= x.n_pages) continue;
-            if (len - c * 64 < 64) there = (1ull << (len - c * 64)) - 1;
-            const uint8_t* block = x.pages + ((size_t)page * x.H_kv + hk) * kv4_head_bytes(D);
-            for (int i = tid; i < 2 * 64 * D; i += TA_THREADS) {
-                const int which = i / (64 * D), tok = i / D % 64, d = i % D;
-                int at, high;
-                if (which == 0) {
-                    at = kv4_k_word<D>(tok, d / 32, d % 32 / 8) + d % 8 / 2;
-                    high = d & 1;
-                } else {
-                    at = kv4_v_word<D>(tok, d % 16 / 8, d % 8) + d / 32;
-                    high = d / 16 & 1;
+                        for (int k = 0; k < 2; ++k) {
+                            id[k] = __shfl_sync(0xffffffffu, page, (c + k) & 31);
+                            v[k] = id[k] >= 0 && id[k] < x.n_pages ? min(max(q.len - 64 * (c + k), 0), 64) : 0;
+                        }
+                        if (lane == 0) {
+                            const uint32_t bar = smem_u32(&ctl->codes_full[n_code % TA_CODES]), sbar = smem_u32(&ctl->scales_full[n % TA_SCALES]);
+                            const int there = (v[0] > 0) + (v[1] > 0);
+                            if (which == 0) {
+                                ctl->valid[n % TA_INFO][0] = v[0];
+                                ctl->valid[n % TA_INFO][1] = v[1];
+                                mbar_expect_tx(sbar, there * 16 * D);
+                            }
+                            mbar_expect_tx(bar, there * 32 * D);
+                            for (int k = 0; k < 2; ++k) {
+                                if (v[k] == 0) continue;
+                                const uint8_t* block = x.pages + ((size_t)id[k] * x.H_kv + h) * kv4_head_bytes(D);
+                                if (which == 0) bulk_load(smem_u32(scale_smem + (n % TA_SCALES) * C::scale_bytes + k * 16 * D), block + 64 * D, 16 * D, sbar);
+                                bulk_load(smem_u32(code_smem + (n_code % TA_CODES) * C::code_bytes + k * 32 * D), block + which * 32 * D, 32 * D, bar);
+                            }
+                        }
+                        __syncwarp();
+                        ++n_code;
+                    };
+                    for (int j = 0; j < min(lead, nt) && ok; ++j) copy(0, j);
+                    for (int j = 0; j < nt && ok; ++j) {
+                        copy(1, j);
+                        if (j + lead < nt && ok) copy(0, j + lead);
+                    }
+                    n_tile += nt;
                 }
-                const uint32_t pair = *reinterpret_cast<const uint32_t*>(block + kv4_scale_word<D>(which, tok, d / 32));
-                const float v = __bfloat162float(__float2bfloat16_rn(fmaf((float)(block[at] >> (4 * high) & 15), bf16_lo(pair), bf16_hi(pair))));
-                (which ? vs + tok * D : ks + tok * (D + 1))[d] = v;
             }
-        } else {
-            there = n < 64 ? (1ull << n) - 1 : ~0ull;
-            for (int i = tid; i < 2 * n * D; i += TA_THREADS) {
-                const int which = i / (n * D), tok = i / D % n, d = i % D;
-                const uint16_t* from = which ? x.V + (first + tok) * x.v_stride : x.K + (first + tok) * x.k_stride;
-                (which ? vs + tok * D : ks + tok * (D + 1))[d] = __uint_as_float((uint32_t)from[hk * D + d] << 16);
+            at += line;
+            ++s;
+        }
+        if (wait(&ctl->unit_empty[u % TA_UNITS], ((u / TA_UNITS) & 1) ^ 1) && lane == 0) {
+            ctl->unit[u % TA_UNITS].stop = 1;
+            mbar_arrive(smem_u32(&ctl->unit_full[u % TA_UNITS]));
+        }
+        __syncwarp();
+        if (!ok && lane == 0) {
+            // gave up: linger (bounded) so that copies already in flight land before the block leaves
+            const uint64_t t0 = globaltimer_ns();
+            while (globaltimer_ns() - t0 < 2000000ull) __nanosleep(1000);
+        }
+    } else if (warp == 10) {
+        // ------------------------------------------------ exponents of the tiles
+        uint32_t n_tile = 0;
+        for (uint32_t u = 0; next_unit(u, un); ++u) {
+            int ev = 1000;                                         // none yet
+            for (int j = 0; j < un.tile1 - un.tile0; ++j) {
+                const uint32_t n = n_tile + j;
+                if (!wait(&ctl->scales_full[n % TA_SCALES], (n / TA_SCALES) & 1)) break;
+                const int v0 = ctl->valid[n % TA_INFO][0], v1 = ctl->valid[n % TA_INFO][1];
+                float top[2] = {0.f, 0.f};
+                int odd = 0;
+                if (un.tile0 + j == 0) {
+                    for (int i = lane; i < un.n * (D / 8); i += 32) {
+                        const long long token = un.token0 + i / (D / 8);
+                        const int d = un.head * D + i % (D / 8) * 8;
+                        const uint4 raw[2] = {*reinterpret_cast<const uint4*>(x.K + token * x.k_stride + d), *reinterpret_cast<const uint4*>(x.V + token * x.v_stride + d)};
+#pragma unroll
+                        for (int which = 0; which < 2; ++which) {
+                            const uint32_t w[4] = {raw[which].x, raw[which].y, raw[which].z, raw[which].w};
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) {
+                                const float v = fabsf(k & 1 ? bf16_hi(w[k >> 1]) : bf16_lo(w[k >> 1]));
+                                if (v < INFINITY) top[which] = fmaxf(top[which], v);
+                                else odd |= which;
+                            }
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int tok = (k & 1) * 32 + lane;
+                        if (tok >= (k >> 1 ? v1 : v0)) continue;
+                        const uint8_t* at = scale_smem + (n % TA_SCALES) * C::scale_bytes + (k >> 1) * 16 * D + tok * 4 * NG;
+#pragma unroll
+                        for (int which = 0; which < 2; ++which)
+#pragma unroll
+                            for (int g = 0; g < NG; ++g) {
+                                const uint32_t pair = reinterpret_cast<const uint32_t*>(at + which * 8 * D)[g];
+                                top[which] = fmaxf(top[which], fmaf(15.f, fabsf(bf16_lo(pair)), fabsf(bf16_hi(pair))));
+                            }
+                    }
+                }
+                int e[2];
+#pragma unroll
+                for (int which = 0; which < 2; ++which) {
+                    const uint32_t bits = __reduce_max_sync(0xffffffffu, __float_as_uint(top[which]));
+                    e[which] = bits == 0 ? -1000 : min(max((int)(bits >> 23) - 127 + 6, -100), 133);
+                }
+                odd = __any_sync(0xffffffffu, odd);
+                if (e[1] > -1000 && (ev == 1000 || e[1] > ev)) ev = min(e[1] + 2, 133);     // (two binades of room, so that it seldom grows)
+                if (lane == 0) {
+                    TreeInfo& f = ctl->info[n % TA_INFO];
+                    f.ek = e[0] == -1000 ? 0 : e[0];
+                    f.ev = ev == 1000 ? 0 : ev;
+                    f.v0 = v0; f.v1 = v1; f.odd = odd;
+                    mbar_arrive(smem_u32(&ctl->scales_ready[n % TA_SCALES]));
+                }
+                __syncwarp();
+                if (ev == 1000) ev = 1000;
+            }
+            n_tile += un.tile1 - un.tile0;
+            if (!ok) break;
+        }
+    } else if (warp == 11) {
+        // ------------------------------------------------ tokens beyond the most that a request may have
+        for (int s = blockIdx.x; s < x.n_seq; s += gridDim.x) {
+            const long long first = min(max((long long)x.off[s], 0ll), x.n_tokens), stop = min(max((long long)x.off[s + 1], first), x.n_tokens);
+            for (long long t = first + x.max_tokens; t < stop; ++t)
+                for (int d = lane * 8; d < x.H_q * D; d += 256) *reinterpret_cast<uint4*>(x.O + t * x.o_stride + d) = make_uint4(0, 0, 0, 0);
+        }
+    } else if (warp == 8) {
+        // ------------------------------------------------ MMA issuer (the warp runs converged, one elected lane issues)
+        const uint32_t idesc_s = make_idesc_f16(TA_TILE, TA_TILE, 0, 0), idesc_o = make_idesc_f16(TA_TILE, D, 0, 1);
+        const uint64_t dk_t = make_smem_desc(0, 16, 1024, 2);                  // Q, K: K-major, 128-byte swizzle
+        const uint64_t dv_t = make_smem_desc(0, TA_TILE * 128, 1024, 2);       // V: N-major, 64-column blocks 16 KB apart
+        const uint32_t q_base = smem_u32(q_smem), op_base = smem_u32(op_smem);
+        uint32_t n_op = 0, n_q[2] = {0, 0}, n_p[2] = {0, 0};
+        auto op_wait = [&](uint32_t n) { return wait(&ctl->op_full[n % TA_OPS], (n / TA_OPS) & 1); };
+        auto op_done = [&](uint32_t n) {
+            if (elect_one()) tc_commit(smem_u32(&ctl->op_empty[n % TA_OPS]));
+            __syncwarp();
+        };
+        auto scores = [&](int w, int buf, uint32_t n) {
+            const uint64_t dq = dk_t | (uint64_t)((q_base + buf * C::op_bytes) >> 4), dk = dk_t | (uint64_t)((op_base + n % TA_OPS * C::op_bytes) >> 4);
+            if (elect_one()) {
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k)
+                    tc_mma_f16(tmem + w * TA_TILE, dq + (k >> 2) * (TA_TILE * 128 >> 4) + (k & 3) * 2, dk + (k >> 2) * (TA_TILE * 128 >> 4) + (k & 3) * 2, idesc_s, k ? 1u : 0u);
+                tc_commit(smem_u32(&ctl->s_full[w]));
+                mbar_arrive(smem_u32(&ctl->s_full[w]));    // (with what this warp has seen: the tile's exponents, the rows' factors)
+            }
+            __syncwarp();
+        };
+        auto outputs = [&](int w, bool first, uint32_t n) {
+            if (!wait(&ctl->p_full[w], n_p[w] & 1)) return;
+            ++n_p[w];
+            tc_fence_after();
+            const uint64_t dv = dv_t | (uint64_t)((op_base + n % TA_OPS * C::op_bytes) >> 4);
+            if (elect_one()) {
+#pragma unroll
+                for (int k = 0; k < TA_TILE / 16; ++k)                         // P of keys 64 h .. 64 h + 63 lies at columns 64 h .. 64 h + 31
+                    tc_mma_f16_ts(tmem + 256 + w * D, tmem + w * TA_TILE + (k >> 2) * 64 + (k & 3) * 8, dv + k * (2048 >> 4), idesc_o, first && k == 0 ? 0u : 1u);
+                tc_commit(smem_u32(&ctl->pv_done[w]));
+            }
+            __syncwarp();
+        };
+        for (uint32_t u = 0; next_unit(u, un); ++u) {
+            const int nt = un.tile1 - un.tile0;
+            for (int b = 0; b < 2; ++b)
+                if (un.two || un.buf == b) {
+                    wait(&ctl->q_full[b], n_q[b] & 1);
+                    ++n_q[b];
+                }
+            if (!ok) break;
+            if (!un.two) {
+                // operands in the order K_0 K_1 V_0 K_2 V_1 ..
+                for (int j = 0; j < min(2, nt) && ok; ++j) {
+                    if (!op_wait(n_op)) break;
+                    tc_fence_after();
+                    scores(j, un.buf, n_op);
+                    op_done(n_op++);
+                }
+                for (int j = 0; j < nt && ok; ++j) {
+                    if (!op_wait(n_op)) break;
+                    outputs(j & 1, j < 2, n_op);
+                    if (!ok) break;
+                    op_done(n_op++);
+                    if (j + 2 < nt) {
+                        if (!op_wait(n_op)) break;
+                        tc_fence_after();
+                        scores(j & 1, un.buf, n_op);
+                        op_done(n_op++);
+                    }
+                }
+            } else {
+                // K_0 V_0 K_1 V_1 ..
+                if (!op_wait(n_op)) break;
+                tc_fence_after();
+                scores(0, 0, n_op);
+                scores(1, 1, n_op);
+                op_done(n_op++);
+                for (int j = 0; j < nt && ok; ++j) {
+                    const uint32_t nv = n_op, nk = n_op + 1;
+                    if (!op_wait(nv)) break;
+                    for (int w = 0; w < 2 && ok; ++w) {
+                        outputs(w, j == 0, nv);
+                        if (j + 1 < nt && ok) {
+                            if (w == 0 && !op_wait(nk)) break;
+                            tc_fence_after();
+                            scores(w, w, nk);
+                        }
+                    }
+                    if (!ok) break;
+                    op_done(nv);
+                    ++n_op;
+                    if (j + 1 < nt) {
+                        op_done(nk);
+                        ++n_op;
+                    }
+                }
             }
         }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < TA_ROWS; ++i) {
-            const int r = r0 + warp * TA_ROWS + i;
-            if (r >= rows) break;
-            const unsigned long long seen = c < pages ? there : there & sees[r / x.G];
-            const float* q = qs + (warp * TA_ROWS + i) * D;
-            float s0 = 0.f, s1 = 0.f;
-            for (int d = 0; d < D; ++d) {
-                s0 = fmaf(q[d], ks[lane * (D + 1) + d], s0);
-                s1 = fmaf(q[d], ks[(lane + 32) * (D + 1) + d], s1);
+        __syncwarp();
+        if (*abort_flag) {
+            // let issued MMAs retire before tensor memory is released
+            if (elect_one()) {
+                tc_commit(smem_u32(&ctl->drain));
+                int dummy = 0;
+                mbar_wait(smem_u32(&ctl->drain), 0, &dummy, 2000000ull);
             }
-            if (!(seen >> lane & 1)) s0 = -INFINITY;
-            if (!(seen >> (lane + 32) & 1)) s1 = -INFINITY;
-            float top = fmaxf(s0, s1);
-            for (int w = 1; w < 32; w <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
-            const float now = fmaxf(m[i], top), ref = now == -INFINITY ? 0.f : now;
-            const float f = m[i] == -INFINITY ? 0.f : ex2_ftz(m[i] - ref);
-            m[i] = now;
-            const float p0 = ex2_ftz(s0 - ref), p1 = ex2_ftz(s1 - ref);
-            float sum = p0 + p1;
-            for (int w = 1; w < 32; w <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
-            l[i] = l[i] * f + sum;
-#pragma unroll
-            for (int d = 0; d < D / 32; ++d) o[i][d] *= f;
             __syncwarp();
-            ps[warp][lane] = p0;
-            ps[warp][lane + 32] = p1;
+        }
+    } else {
+        // ------------------------------------------------ decoders: Q, the drafted tokens and the cache's codes as operands
+        const int dt = tid - 12 * 32, dwarp = warp - 12;
+        const int token = dt & 127, half = dt >> 7, page = token >> 6, tk = token & 63;
+        const uint32_t row_at = token * 128, sw = token & 7;       // operand row: chunk c at (c / 8) 16 KB + 128 row + 16 ((c ^ row) mod 8)
+        uint32_t n_op = 0, n_code = 0, n_tile = 0, n_q[2] = {0, 0};
+        auto arrive = [&](uint64_t* b) {
             __syncwarp();
-#pragma unroll 1
-            for (int j = 0; j < 64; ++j) {
-                const float p = ps[warp][j];
-                if (!(seen >> j & 1)) continue;
+            if (lane == 0) mbar_arrive(smem_u32(b));
+        };
+        for (uint32_t u = 0; next_unit(u, un); ++u) {
+            const int nt = un.tile1 - un.tile0, lead = un.two ? 1 : 2;
+            // ---- Q: rows times a power of two that puts their largest element at 2^7
+            for (int b = 0; b < 2; ++b) {
+                if (!un.two && un.buf != b) continue;
+                if (!wait(&ctl->q_empty[b], (n_q[b] & 1) ^ 1)) break;
+                ++n_q[b];
+                if (dwarp == 0) {
+                    // who sees whom among the drafted tokens: paths to the root by doubling, two tokens a lane
+                    unsigned long long anc[2];
+                    int jump[2];
 #pragma unroll
-                for (int d = 0; d < D / 32; ++d) o[i][d] = fmaf(p, vs[j * D + d * 32 + lane], o[i][d]);
+                    for (int k = 0; k < 2; ++k) {
+                        const int i = lane + 32 * k;
+                        const int p = i < un.n ? x.parent ? x.parent[un.token0 + i] : i - 1 : -1;
+                        jump[k] = p >= 0 && p < i ? p : -1;
+                        anc[k] = 1ull << i;
+                    }
+                    for (int step = 0; step < 6; ++step) {
+                        unsigned long long more[2];
+                        int far[2];
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const int j = max(jump[k], 0) & 31;
+                            const unsigned long long a0 = __shfl_sync(0xffffffffu, anc[0], j), a1 = __shfl_sync(0xffffffffu, anc[1], j);
+                            const int f0 = __shfl_sync(0xffffffffu, jump[0], j), f1 = __shfl_sync(0xffffffffu, jump[1], j);
+                            more[k] = jump[k] < 0 ? 0 : jump[k] < 32 ? a0 : a1;
+                            far[k] = jump[k] < 0 ? -1 : jump[k] < 32 ? f0 : f1;
+                        }
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            anc[k] |= more[k];
+                            jump[k] = far[k];
+                        }
+                    }
+                    ctl->sees[b][lane] = anc[0];
+                    ctl->sees[b][lane + 32] = anc[1];
+                }
+                constexpr int L = D / 8, R = 32 / L;               // lanes of a row, rows of a warp
+                const int unit_row0 = un.two ? b * TA_TILE : 0, rows = min(un.rows - unit_row0, TA_TILE), distinct = TA_TILE / un.copies;
+                const int c = lane % L;
+                for (int r0 = dwarp * R * 4; r0 < distinct; r0 += TA_DECODERS * R * 4) {
+                    uint4 raw[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int r = r0 + k * R + lane / L, at = un.row0 + unit_row0 + r;
+                        raw[k] = make_uint4(0, 0, 0, 0);
+                        if (r < rows) raw[k] = *reinterpret_cast<const uint4*>(x.Q + (long long)(un.token0 + at / x.G) * x.q_stride + (un.head * x.G + at % x.G) * D + c * 8);
+                    }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int r = r0 + k * R + lane / L;
+                        const uint32_t w[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
+                        float v[8], top = 0.f;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            v[i] = i & 1 ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]);
+                            if (fabsf(v[i]) < INFINITY) top = fmaxf(top, fabsf(v[i]));
+                        }
+#pragma unroll
+                        for (int o = 1; o < L; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                        const int shift = top == 0.f ? 0 : min(7 - ((int)(__float_as_uint(top) >> 23) - 127), 120);
+                        const float f = pow2i(shift);
+                        const uint4 out = make_uint4(pack_f16(v[0] * f, v[4] * f), pack_f16(v[1] * f, v[5] * f), pack_f16(v[2] * f, v[6] * f), pack_f16(v[3] * f, v[7] * f));
+                        if (r < distinct) {
+                            for (int to = r; to < TA_TILE; to += distinct)
+                                *reinterpret_cast<uint4*>(q_smem + b * C::op_bytes + (c >> 3) * (TA_TILE * 128) + to * 128 + (((c ^ to) & 7) << 4)) = out;
+                            if (c == 0) ctl->row_scale[b][r] = x.scale_log2e * pow2i(-shift);
+                        }
+                    }
+                }
+                fence_proxy_async_smem();
+                arrive(&ctl->q_full[b]);
             }
+            if (!ok) break;
+            // ---- operands
+            auto make = [&](int which, int j) {
+                const uint32_t n = n_tile + j;
+                if (which == 0 && !wait(&ctl->scales_ready[n % TA_SCALES], (n / TA_SCALES) & 1)) return;
+                const TreeInfo& f = ctl->info[n % TA_INFO];
+                const int e = which ? f.ev : f.ek;
+                uint8_t* to = op_smem + n_op % TA_OPS * C::op_bytes;
+                if (un.tile0 + j > 0) {
+                    const bool valid = tk < (page ? f.v1 : f.v0);
+                    const float k24 = pow2i(24 - e);
+                    const uint8_t* sc = scale_smem + (n % TA_SCALES) * C::scale_bytes + page * 16 * D + which * 8 * D + tk * 4 * NG;
+                    const uint8_t* codes = code_smem + (n_code % TA_CODES) * C::code_bytes + page * 32 * D;
+                    Scale2 a, b;
+                    if (which == 0) {
+                        // this thread: half of the groups, of all four runs t of a group
+                        const int h = half ^ ((tk >> (D == 128 ? 3 : 4)) & 1);
+                        uint32_t pair[2];
+                        if (D == 128) *reinterpret_cast<uint2*>(pair) = *reinterpret_cast<const uint2*>(sc + 8 * h);
+                        else pair[0] = pair[1] = *reinterpret_cast<const uint32_t*>(sc + 4 * h);
+                        if (!valid) pair[0] = pair[1] = 0;
+                        a = scale_pair(pair[0], pair[0], k24);
+                        b = scale_pair(pair[1], pair[1], k24);
+                        if (!wait(&ctl->codes_full[n_code % TA_CODES], (n_code / TA_CODES) & 1) || !wait(&ctl->op_empty[n_op % TA_OPS], ((n_op / TA_OPS) & 1) ^ 1)) return;
+                        const int turn = (tk >> (D == 128 ? 1 : 2)) & 3;
+#pragma unroll
+                        for (int t0 = 0; t0 < 4; ++t0) {
+                            const int t = t0 ^ turn;
+                            if (D == 128) {
+                                const uint2 w = *reinterpret_cast<const uint2*>(codes + tk * 64 + t * 16 + 8 * h);
+                                uint8_t* p = to + h * (TA_TILE * 128) + row_at;                 // chunks 8 h + t and 8 h + 4 + t
+                                *reinterpret_cast<uint4*>(p + ((t ^ sw) << 4)) = decode_word(w.x, a, a);
+                                *reinterpret_cast<uint4*>(p + (((t ^ 4) ^ sw) << 4)) = decode_word(w.y, b, b);
+                            } else {
+                                const uint32_t w = *reinterpret_cast<const uint32_t*>(codes + tk * 32 + t * 8 + 4 * h);
+                                *reinterpret_cast<uint4*>(to + row_at + (((4 * h + t) ^ sw) << 4)) = decode_word(w, a, a);
+                            }
+                        }
+                    } else {
+                        uint32_t pair[NG];
+                        if (D == 128) *reinterpret_cast<uint4*>(pair) = *reinterpret_cast<const uint4*>(sc);
+                        else *reinterpret_cast<uint2*>(pair) = *reinterpret_cast<const uint2*>(sc);
+                        if (!valid) {
+#pragma unroll
+                            for (int g = 0; g < NG; ++g) pair[g] = 0;
+                        }
+                        a = D == 128 ? scale_pair(pair[0], pair[NG / 2], k24) : scale_pair(pair[0], pair[0], k24);
+                        b = D == 128 ? scale_pair(pair[1], pair[NG - 1], k24) : scale_pair(pair[1], pair[1], k24);
+                        if (!wait(&ctl->codes_full[n_code % TA_CODES], (n_code / TA_CODES) & 1) || !wait(&ctl->op_empty[n_op % TA_OPS], ((n_op / TA_OPS) & 1) ^ 1)) return;
+                        const uint8_t* from = codes + (tk >> 3) * 4 * D + ((tk >> 1) & 3) * (D / 8) + (tk & 1) * (D / 16);
+                        const int turn = D == 128 ? (tk >> 3) & 1 : (tk >> 3) & 3;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int g = (4 * half + i) ^ turn;
+                            if (D == 128) {
+                                const uint2 w = *reinterpret_cast<const uint2*>(from + g * 64);
+                                uint8_t* p = to + (g >> 2) * (TA_TILE * 128) + row_at;          // chunks 2 g and 2 g + 1
+                                *reinterpret_cast<uint4*>(p + (((2 * g) ^ sw) & 7) * 16) = decode_word(w.x, a, b);
+                                *reinterpret_cast<uint4*>(p + (((2 * g + 1) ^ sw) & 7) * 16) = decode_word(w.y, a, b);
+                            } else {
+                                const uint32_t w = *reinterpret_cast<const uint32_t*>(from + g * 32);
+                                *reinterpret_cast<uint4*>(to + row_at + ((g ^ sw) << 4)) = decode_word(w, a, b);
+                            }
+                        }
+                    }
+                    arrive(&ctl->codes_empty[n_code % TA_CODES]);
+                    ++n_code;
+                } else {
+                    if (!wait(&ctl->op_empty[n_op % TA_OPS], ((n_op / TA_OPS) & 1) ^ 1)) return;
+                    // drafted tokens: thread (token of 64, quarter of the chunks); the rows behind them are zeros
+                    const int tok = dt & 63, quarter = dt >> 6;
+                    const float k0 = times_pow2(1.f, -e);
+                    const uint16_t* from = (which ? x.V + (un.token0 + (long long)tok) * x.v_stride : x.K + (un.token0 + (long long)tok) * x.k_stride) + un.head * D;
+#pragma unroll
+                    for (int i = 0; i < D / 32; ++i) {
+                        const int c = quarter * (D / 32) + i;
+                        float v[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            // K: elements 8 c + (0, 4, 1, 5, ..); V: column 8 c + k is element 16 (k / 2 + 4 (k mod 2)) + 8 (c mod 2) + c / 2, D = 64: 16 (k / 2) + 8 (k mod 2) + c
+                            const int d = which == 0 ? 8 * c + (k >> 1) + 4 * (k & 1) : D == 128 ? 16 * ((k >> 1) + 4 * (k & 1)) + 8 * (c & 1) + (c >> 1) : 16 * (k >> 1) + 8 * (k & 1) + c;
+                            v[k] = tok < un.n ? __uint_as_float((uint32_t)from[d] << 16) * k0 : 0.f;
+                            if (which && !(fabsf(v[k]) < INFINITY)) v[k] = 0.f;            // put back at the end, for the rows that see it
+                        }
+                        const int at = (c >> 3) * (TA_TILE * 128) + tok * 128 + (((c ^ tok) & 7) << 4);
+                        *reinterpret_cast<uint4*>(to + at) = make_uint4(pack_f16(v[0], v[1]), pack_f16(v[2], v[3]), pack_f16(v[4], v[5]), pack_f16(v[6], v[7]));
+                        *reinterpret_cast<uint4*>(to + at + 64 * 128) = make_uint4(0, 0, 0, 0);
+                    }
+                }
+                fence_proxy_async_smem();
+                arrive(&ctl->op_full[n_op % TA_OPS]);
+                if (which) arrive(&ctl->scales_empty[n % TA_SCALES]);
+                ++n_op;
+            };
+            for (int j = 0; j < min(lead, nt) && ok; ++j) make(0, j);
+            for (int j = 0; j < nt && ok; ++j) {
+                make(1, j);
+                if (j + lead < nt && ok) make(0, j + lead);
+            }
+            if (!ok) break;
+            n_tile += nt;
         }
     }
-    for (int i = 0; i < TA_ROWS; ++i) {
-        const int r = r0 + warp * TA_ROWS + i;
-        if (r >= rows) break;
-        const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
-        uint16_t* out = x.O + (first + r / x.G) * x.o_stride + (hk * x.G + r % x.G) * D;
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(TA_REGS_SOFT));
+        // ------------------------------------------------ softmax and epilogue: thread = lane of tile w
+        const int w = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+        const uint32_t t_s = tmem + lanes + w * TA_TILE, t_o = tmem + lanes + 256 + w * D;
+        uint32_t n_s = 0, n_tile = 0, n_together = 0;      // score tiles of this slot so far; tiles so far
+        auto together = [&]() -> bool {            // a barrier of the softmax warps, with the limit of every wait
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&ctl->together));
+            return wait(&ctl->together, n_together++ & 1);
+        };
+        for (uint32_t u = 0; next_unit(u, un); ++u) {
+            const int nt = un.tile1 - un.tile0, step = un.two ? 1 : 2, j0 = un.two ? 0 : w;
+            const int distinct = TA_TILE / un.copies, copy = r / distinct, row = (un.two ? w * TA_TILE : 0) + r % distinct;   // row of the unit
+            const bool live = row < un.rows;
+            const int buf = un.two ? w : un.buf;
+            float m = -INFINITY, l = 0.f, rs = 0.f;
+            int ev = 0, odd = 0;
+            for (int j = j0; j < nt; j += step, ++n_s) {
+                if (!wait(&ctl->s_full[w], n_s & 1)) break;
+                tc_fence_after();
+                const TreeInfo f = ctl->info[(n_tile + j) % TA_INFO];
+                const bool drafts = un.tile0 + j == 0;
+                if (j == j0) rs = ctl->row_scale[buf][r % distinct];
+                const float c = fminf(fmaxf(times_pow2(rs, f.ek), 1e-37f), 3e38f);    // (not 0 or infinite: scores at -inf, scores of 0)
+                uint32_t seen[4];
+                const bool masked = drafts || f.v0 < 64 || f.v1 < 64;
+                if (masked) {
+                    unsigned long long a = f.v0 >= 64 ? ~0ull : (1ull << f.v0) - 1, b = f.v1 >= 64 ? ~0ull : (1ull << f.v1) - 1;
+                    if (drafts) {
+                        odd = f.odd;
+                        a = live ? ctl->sees[buf][(un.row0 + row) / x.G] : 0ull;
+                    }
+                    seen[0] = (uint32_t)a;
+                    seen[1] = (uint32_t)(a >> 32);
+                    seen[2] = (uint32_t)b;
+                    seen[3] = (uint32_t)(b >> 32);
+                }
+                auto load32 = [&](int block, uint32_t(&v)[32]) {               // scores 32 block .. + 31, those that are not seen at -inf
+                    tmem_ld_32x32(t_s + block * 32, v);
+                    tmem_ld_wait();
+                    if (masked) {
+                        const uint32_t see = seen[block];
 #pragma unroll
-        for (int d = 0; d < D / 32; ++d) out[d * 32 + lane] = __bfloat16_as_ushort(__float2bfloat16_rn(o[i][d] * inv));
+                        for (int i = 0; i < 32; ++i)
+                            if (!(see >> i & 1)) v[i] = 0xff800000u;
+                    }
+                };
+                auto top_of = [&](const uint32_t(&v)[32]) {
+                    float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) t[i & 3] = fmaxf(t[i & 3], __uint_as_float(v[i]));
+                    return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+                };
+                // the reference, once the tile's largest score is known; outputs so far follow it
+                auto refer = [&](float raw_top) -> bool {
+                    const float top = raw_top * c;
+                    const bool grow = top > m && !(top - m <= TA_LAZY);
+                    if (j == j0) {
+                        m = top;
+                        ev = f.ev;
+                    } else if (__any_sync(0xffffffffu, grow) || ev != f.ev) {
+                        if (!wait(&ctl->pv_done[w], (n_s - 1) & 1)) return false;
+                        tc_fence_after();
+                        const float g = !grow ? 1.f : m == -INFINITY ? 0.f : ex2_ftz(m - top);
+                        if (grow) m = top;
+                        l *= g;
+                        const float go = ev == f.ev ? g : ev - f.ev < -126 ? 0.f : g * pow2i(min(ev - f.ev, 127));
+                        ev = f.ev;
+#pragma unroll 1
+                        for (int d = 0; d < D; d += 32) {
+                            uint32_t ov[32];
+                            tmem_ld_32x32(t_o + d, ov);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) ov[i] = __float_as_uint(__uint_as_float(ov[i]) * go);
+                            tmem_st_32x32(t_o + d, ov);
+                        }
+                        tmem_st_wait();
+                    }
+                    return true;
+                };
+                f32x2 sum = pack2(0.f, 0.f);
+                const f32x2 c2 = pack2(c, c);
+                auto exps = [&](const uint32_t(&v)[32], f32x2 ref2, uint32_t(&p)[16]) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        float a, b;
+                        unpack2(fma2(pack2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), c2, ref2), a, b);
+                        a = ex2_ftz(a);
+                        b = ex2_ftz(b);
+                        sum = add2(sum, pack2(a, b));
+                        p[i] = pack_f16(a, b);
+                    }
+                };
+                auto ref_of = [&] {
+                    const float s = (m == -INFINITY ? 0.f : -m) + TA_SHIFT;
+                    return pack2(s, s);
+                };
+                uint32_t v[32], p[16];
+                if (un.copies == 1) {
+                    uint32_t v2[32];
+                    load32(0, v);
+                    float top = top_of(v);
+                    load32(1, v);
+                    top = fmaxf(top, top_of(v));
+                    load32(2, v);
+                    load32(3, v2);
+                    if (!refer(fmaxf(top, fmaxf(top_of(v), top_of(v2))))) break;
+                    const f32x2 ref2 = ref_of();
+                    exps(v, ref2, p);
+                    tmem_st_32x16(t_s + 64, p);
+                    exps(v2, ref2, p);
+                    tmem_st_32x16(t_s + 80, p);
+                    load32(0, v);
+                    load32(1, v2);
+                    exps(v, ref2, p);
+                    tmem_st_32x16(t_s, p);
+                    exps(v2, ref2, p);
+                    tmem_st_32x16(t_s + 16, p);
+                } else if (un.copies == 2) {
+                    uint32_t v2[32];
+                    load32(2 * copy, v);
+                    load32(2 * copy + 1, v2);
+                    if (!refer(fmaxf(top_of(v), top_of(v2)))) break;
+                    const f32x2 ref2 = ref_of();
+                    exps(v, ref2, p);
+                    tmem_st_32x16(t_s + 64 * copy, p);
+                    exps(v2, ref2, p);
+                    tmem_st_32x16(t_s + 64 * copy + 16, p);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) p[i] = 0;
+                    tmem_st_32x16(t_s + 64 * (1 - copy), p);
+                    tmem_st_32x16(t_s + 64 * (1 - copy) + 16, p);
+                } else {
+                    load32(copy, v);
+                    if (!refer(top_of(v))) break;
+                    exps(v, ref_of(), p);
+                    tmem_st_32x16(t_s + 64 * (copy >> 1) + 16 * (copy & 1), p);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) p[i] = 0;
+                    for (int k = 0; k < 4; ++k)
+                        if (k != copy) tmem_st_32x16(t_s + 64 * (k >> 1) + 16 * (k & 1), p);
+                }
+                float sum0, sum1;
+                unpack2(sum, sum0, sum1);
+                l += sum0 + sum1;
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&ctl->p_full[w]));
+            }
+            if (!ok) break;
+            n_tile += nt;
+            const bool have = j0 < nt;
+            if (have) {
+                if (!wait(&ctl->pv_done[w], (n_s - 1) & 1)) break;
+                tc_fence_after();
+            }
+            // ---- the end of the unit, or of this block's share of it
+            const int at = un.row0 + row;
+            uint16_t* out = x.O + (long long)(un.token0 + at / x.G) * x.o_stride + (long long)(un.head * x.G + at % x.G) * D;
+            float* part = x.part + ((size_t)max(un.slot, 0) * x.part_rows + row) * D;
+            // N values of the row from element d0 on: to the output, or to the part
+            auto put = [&](auto count, int d0, float* v) {
+                constexpr int N = decltype(count)::value;
+                if (odd) {                                                     // what the row sees of drafted values that are not finite
+                    const unsigned long long sees = ctl->sees[buf][at / x.G];
+                    for (int i = 0; i < un.n; ++i) {
+                        if (!(sees >> i & 1)) continue;
+                        const uint16_t* from = x.V + (un.token0 + (long long)i) * x.v_stride + un.head * D + d0;
+#pragma unroll
+                        for (int k = 0; k < N; ++k) {
+                            const float y = __uint_as_float((uint32_t)from[k] << 16);
+                            if (!(fabsf(y) < INFINITY)) v[k] += y;
+                        }
+                    }
+                }
+                if (un.slot >= 0) {
+#pragma unroll
+                    for (int k = 0; k < N; k += 2) *reinterpret_cast<float2*>(part + d0 + k) = make_float2(v[k], v[k + 1]);
+                } else {
+                    uint32_t b[N / 2];
+#pragma unroll
+                    for (int k = 0; k < N / 2; ++k) b[k] = pack_bf16(v[2 * k], v[2 * k + 1]);
+                    if constexpr (N == 2) {
+                        *reinterpret_cast<uint32_t*>(out + d0) = b[0];
+                    } else if constexpr (N == 4) {
+                        *reinterpret_cast<uint2*>(out + d0) = make_uint2(b[0], b[1]);
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < N / 2; k += 4) *reinterpret_cast<uint4*>(out + d0 + 2 * k) = make_uint4(b[k], b[k + 1], b[k + 2], b[k + 3]);
+                    }
+                }
+            };
+            constexpr int CW = D / 4;                                          // columns of a round: elements 16 i .. + 15 (and, D = 128, 64 + 16 i .. + 15)
+            auto columns = [&](int i, float f1, float f2, float (&v)[CW]) {
+                uint32_t o[CW];
+#pragma unroll
+                for (int g = 0; g < D / 8; ++g) {
+                    if (D == 128) tmem_ld_32x2(t_o + g * 8 + 2 * i, o[8 * (g & 1) + (g >> 1)], o[16 + 8 * (g & 1) + (g >> 1)]);
+                    else tmem_ld_32x2(t_o + g * 8 + 2 * i, o[g], o[8 + g]);
+                }
+                tmem_ld_wait();
+#pragma unroll
+                for (int k = 0; k < CW; ++k) v[k] = f1 == 0.f ? 0.f : __uint_as_float(o[k]) * f1 * f2;
+            };
+            const float half1 = pow2i(ev >> 1), half2 = pow2i(ev - (ev >> 1));
+            if (un.two) {
+                const float inv = l == 0.f ? 0.f : half1 / l;
+                if (un.slot >= 0 && live) x.stats[(size_t)un.slot * x.part_rows + row] = make_float2(m, l);
+                for (int i = 0; i < 4; ++i) {
+                    float v[CW];
+                    columns(i, inv, half2, v);
+                    if (live) {
+                        put(std::integral_constant<int, 16>{}, 16 * i, v);
+                        if constexpr (D == 128) put(std::integral_constant<int, 16>{}, 64 + 16 * i, v + 16);
+                    }
+                }
+            } else {
+                // parts of a row: (w, copy)
+                const int parts = 2 * un.copies, me = w * un.copies + copy;
+                ctl->stats[w * TA_TILE + r] = make_float2(m, have ? l : 0.f);
+                if (warp == 0 && lane == 0) ctl->odd = odd;
+                if (!together()) break;
+                odd = ctl->odd;
+                float top = -INFINITY, all = 0.f;
+                for (int k = 0; k < parts; ++k) top = fmaxf(top, ctl->stats[k / un.copies * TA_TILE + k % un.copies * distinct + r % distinct].x);
+                const float ref = top == -INFINITY ? 0.f : top;
+                for (int k = 0; k < parts; ++k) {
+                    const float2 s = ctl->stats[k / un.copies * TA_TILE + k % un.copies * distinct + r % distinct];
+                    all += s.y == 0.f ? 0.f : s.y * ex2_ftz(s.x - ref);
+                }
+                const float f = !have || l == 0.f ? 0.f : (all == 0.f ? 0.f : ex2_ftz(m - ref) / all);
+                if (un.slot >= 0 && live && me == 0) x.stats[(size_t)un.slot * x.part_rows + row] = make_float2(ref, all);
+                float* stage = reinterpret_cast<float*>(q_smem + un.buf * C::op_bytes);        // the unit's Q has been used up
+                for (int i = 0; i < 4; ++i) {
+                    float v[CW];
+                    if (have) {
+                        columns(i, f * half1, half2, v);
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < CW; ++k) v[k] = 0.f;
+                    }
+                    float* mine_at = stage + (w * TA_TILE + r) * CW;
+#pragma unroll
+                    for (int k = 0; k < CW; ++k) mine_at[k ^ (lane & (CW - 1))] = v[k];
+                    if (!together()) break;
+                    auto collect = [&](auto count) {
+                        constexpr int N = decltype(count)::value;
+                        float s[N];
+#pragma unroll
+                        for (int k = 0; k < N; ++k) s[k] = 0.f;
+                        for (int p = 0; p < parts; ++p) {
+                            const int from = p / un.copies * TA_TILE + p % un.copies * distinct + r % distinct;
+#pragma unroll
+                            for (int k = 0; k < N; ++k) s[k] += stage[from * CW + ((me * N + k) ^ (from & (CW - 1)))];
+                        }
+                        const int k0 = me * N;
+                        if (live) put(count, D == 128 && k0 >= 16 ? 64 + 16 * i + k0 - 16 : 16 * i + k0, s);
+                    };
+                    if (un.copies == 1) collect(std::integral_constant<int, CW / 2>{});
+                    else if (un.copies == 2) collect(std::integral_constant<int, CW / 4>{});
+                    else collect(std::integral_constant<int, CW / 8>{});
+                    if (!together()) break;
+                }
+                if (!ok) break;
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0)
+                for (int b = 0; b < 2; ++b)
+                    if (un.two || un.buf == b) mbar_arrive(smem_u32(&ctl->q_empty[b]));
+        }
+        tc_fence_before();
+    }
+    __syncthreads();
+    if (warp == 8) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+// Units that several blocks share: O = sum_c w_c O_c / sum_c w_c, w_c = 2^(m_c - m) l_c.  Block (i, y): rows y, y + gridDim.y, .. of the unit that began in block i of the main
+// kernel and went on beyond it.
+template <int D>
+__global__ void __launch_bounds__(D) k_attn_tree_join(const TreeArgs x, int blocks) {
+    dep_wait();
+    const TreeCross c = x.cross[blockIdx.x];
+    if (c.rows == 0) return;
+    for (int row = blockIdx.y; row < c.rows; row += gridDim.y) {
+        float top = -INFINITY, sum = 0.f, o = 0.f;
+        for (int pass = 0; pass < 2; ++pass) {
+            for (int b = blockIdx.x; b < blocks; ++b) {
+                const int t0 = tiles_before(c.quota * b, c.begin, c.weight, c.tiles), t1 = tiles_before(c.quota * (b + 1), c.begin, c.weight, c.tiles);
+                if (t0 < t1) {
+                    const size_t at = (size_t)(2 * b + (t1 < c.tiles ? 1 : 0)) * x.part_rows + row;
+                    const float2 s = __ldcg(&x.stats[at]);
+                    if (pass == 0) {
+                        if (s.y != 0.f) top = fmaxf(top, s.x);
+                    } else {
+                        const float f = s.y == 0.f ? 0.f : ex2_ftz(s.x - (top == -INFINITY ? 0.f : top)) * s.y, v = __ldcg(&x.part[at * D + threadIdx.x]);
+                        sum += f;
+                        o += f == 0.f && fabsf(v) < INFINITY ? 0.f : f * v;
+                    }
+                }
+                if (t1 >= c.tiles) break;
+            }
+        }
+        const int at = c.row0 + row;
+        x.O[(long long)(c.token0 + at / x.G) * x.o_stride + (long long)(c.head * x.G + at % x.G) * D + threadIdx.x] =
+            __bfloat16_as_ushort(__float2bfloat16_rn(sum == 0.f ? 0.f : o / sum));
     }
 }
 
@@ -148,13 +1036,17 @@ static bool tree_shape_ok(long long n_seq, int max_tokens, int H_q, int H_kv, in
     return n_seq >= 1 && max_tokens >= 1 && max_tokens <= AG_TREE_MAX && H_kv >= 1 && H_kv <= 1024 && H_q >= H_kv && H_q % H_kv == 0 && H_q / H_kv <= 64 &&
            (D == 64 || D == 128) && max_pages >= 1 && max_pages < (1 << 25);
 }
+static int tree_part_rows(int max_tokens, int G) { return std::min(256, max_tokens * G); }
+static size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
 }  // namespace ag
 
 using namespace ag;
 
 extern "C" size_t ag_attention_tree_kv4_workspace(int n_seq, int max_tokens, int H_q, int H_kv, int D, int max_pages) {
-    return tree_shape_ok(n_seq, max_tokens, H_q, H_kv, D, max_pages) ? 16 : 0;
+    if (!tree_shape_ok(n_seq, max_tokens, H_q, H_kv, D, max_pages)) return 0;
+    const size_t rows = (size_t)tree_part_rows(max_tokens, H_q / H_kv);
+    return 256 + round256(TA_BLOCKS * sizeof(TreeCross)) + round256(2 * TA_BLOCKS * rows * sizeof(float2)) + 2 * TA_BLOCKS * rows * D * sizeof(float);
 }
 
 extern "C" ag_status attention_tree_kv4(const ag_tree_attention* a, const ag_kv4_pool* pool, const ag_kv4_table* table, void* workspace, size_t workspace_bytes,
@@ -173,6 +1065,20 @@ extern "C" ag_status attention_tree_kv4(const ag_tree_attention* a, const ag_kv4
         return AG_ERR_ARG;
     ag_status st = check_arch();
     if (st != AG_OK) return st;
+    constexpr int smem128 = TCfg<128>::smem_bytes, smem64 = TCfg<64>::smem_bytes > TA_MIN_SMEM ? TCfg<64>::smem_bytes : TA_MIN_SMEM;
+    static std::atomic<unsigned long long> attr_done{0};
+    const cudaError_t attr_err = once_per_device(attr_done, [] {
+        cudaError_t e = cudaFuncSetAttribute(k_attn_tree_kv4<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem128);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(k_attn_tree_kv4<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem64);
+        // the softmax warps ask for registers out of those that the block is launched with: fewer would be waited for without end
+        for (const void* k : {(const void*)k_attn_tree_kv4<128>, (const void*)k_attn_tree_kv4<64>}) {
+            cudaFuncAttributes fa;
+            if (e == cudaSuccess) e = cudaFuncGetAttributes(&fa, k);
+            if (e == cudaSuccess && fa.numRegs * TA_THREADS < TA_SOFT * 32 * TA_REGS_SOFT + (TA_THREADS - TA_SOFT * 32) * TA_REGS_OTHER) e = cudaErrorInvalidConfiguration;
+        }
+        return e;
+    });
+    if (attr_err != cudaSuccess) return cuda_fail(attr_err);
     TreeArgs x;
     memset(&x, 0, sizeof x);
     x.Q = (const uint16_t*)a->Q; x.K = (const uint16_t*)a->K; x.V = (const uint16_t*)a->V; x.O = (uint16_t*)a->O;
@@ -181,22 +1087,33 @@ extern "C" ag_status attention_tree_kv4(const ag_tree_attention* a, const ag_kv4
     x.row = a->row; x.off = a->off; x.parent = a->parent; x.page_of = table->page_of; x.len = table->len;
     x.H_q = a->H_q; x.H_kv = H_kv; x.G = a->H_q / H_kv; x.n_seq = a->n_seq; x.n_rows = table->n_rows; x.max_pages = table->max_pages; x.n_pages = (int)pool->n_pages;
     x.max_tokens = a->max_tokens;
-    x.tiles = (a->max_tokens * x.G + TA_THREADS / 32 * TA_ROWS - 1) / (TA_THREADS / 32 * TA_ROWS);
+    x.part_rows = tree_part_rows(a->max_tokens, x.G);
     x.scale_log2e = 1.4426950408889634f * (a->scale > 0.f ? a->scale : 1.f / sqrtf((float)D));
-    const long long blocks = (long long)x.tiles * H_kv * a->n_seq;
-    if (blocks > 0x7fffffffll) return AG_ERR_ARG;
-    const int smem = (64 * (2 * D + 1) + TA_THREADS / 32 * TA_ROWS * D) * (int)sizeof(float);
-    static std::atomic<unsigned long long> attr_done{0};
-    const cudaError_t attr_err = once_per_device(attr_done, [] {
-        cudaError_t e = cudaFuncSetAttribute(k_tree<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, 128 * 1024);
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(k_tree<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, 128 * 1024);
-        return e;
-    });
-    if (attr_err != cudaSuccess) return cuda_fail(attr_err);
-    cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
-    if (D == 128) k_tree<128><<<(unsigned)blocks, TA_THREADS, smem, stream>>>(x);
-    else k_tree<64><<<(unsigned)blocks, TA_THREADS, smem, stream>>>(x);
-    AG_CUDA(cudaGetLastError());
+    uint8_t* ws = (uint8_t*)workspace;
+    x.status = (int32_t*)ws;
+    x.cross = (TreeCross*)(ws + 256);
+    x.stats = (float2*)((uint8_t*)x.cross + round256(TA_BLOCKS * sizeof(TreeCross)));
+    x.part = (float*)((uint8_t*)x.stats + round256(2 * TA_BLOCKS * (size_t)x.part_rows * sizeof(float2)));
+    // no more blocks than there can be runs of TA_LEAST tiles
+    const long long unit_weight = (a->max_tokens * x.G + 127) / 128, most = (long long)a->n_seq * H_kv * unit_weight * ((table->max_pages + 1) / 2 + 1);
+    const int blocks = (int)std::min<long long>(TA_BLOCKS, (most + TA_LEAST - 1) / TA_LEAST);
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof cfg);
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3(TA_THREADS);
+    cfg.dynamicSmemBytes = D == 128 ? smem128 : smem64;
+    cfg.stream = reinterpret_cast<cudaStream_t>(cuda_stream);
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    AG_CUDA(cudaLaunchKernelEx(&cfg, D == 128 ? k_attn_tree_kv4<128> : k_attn_tree_kv4<64>, x));
+    count_launch();
+    cfg.gridDim = dim3((unsigned)blocks, 4);
+    cfg.blockDim = dim3((unsigned)D);
+    cfg.dynamicSmemBytes = 0;
+    AG_CUDA(cudaLaunchKernelEx(&cfg, D == 128 ? k_attn_tree_join<128> : k_attn_tree_join<64>, x, blocks));
     count_launch();
     return AG_OK;
 }
