@@ -20,12 +20,11 @@
 // All tiles of all units stand in one line that is cut into equal runs, one per block: uneven lengths, one long request or many short ones are the same case.  Units that
 // two or more blocks share leave parts (normalised outputs, maximum, sum) in the workspace, which a second launch puts together.
 //
-// 640 threads: warps 0-7 softmax and epilogue (two groups of four), 8 MMA, 9 units and copies, 10 exponents, 11 idle, 12-19 decoding into operands.
+// 640 threads: warps 0-7 softmax and epilogue (two groups of four), 8 MMA, 9 units and copies of keys, 10 exponents, 11 copies of values, 12-15 decoding of keys, 16-19 of values.
 #include <math.h>
 #include <string.h>
 
 #include <algorithm>
-#include <type_traits>
 
 #include "kv4.cuh"
 
@@ -36,13 +35,13 @@ constexpr int TA_OPS = 3, TA_CODES = 5, TA_SCALES = 4;     // stages: operands; 
 constexpr int TA_INFO = 8, TA_UNITS = 4;
 constexpr int TA_SOFT = 8, TA_DECODERS = 8;                // warps
 constexpr int TA_THREADS = 640;
-constexpr int TA_READERS = TA_SOFT + TA_DECODERS + 2;      // warps that read a unit: and MMA, exponents
-constexpr int TA_REGS_SOFT = 144, TA_REGS_OTHER = 64;      // 256 x 144 + 384 x 64 = 640 x 96
+constexpr int TA_READERS = TA_SOFT + TA_DECODERS + 3;      // warps that read a unit: and MMA, exponents, values' copies
+constexpr int TA_REGS_SOFT = 112, TA_REGS_OTHER = 80;      // 256 x 112 + 384 x 80 <= 640 x 96
 constexpr int TA_BLOCKS = 148;
 constexpr int TA_LEAST = 4;                                // tiles of a block's run, at least
 constexpr float TA_LAZY = 5.f;                             // the reference m of a row moves when its maximum has grown by more than 2^5
 constexpr float TA_SHIFT = 10.f;                           // P is taken times 2^10: at most 2^15, down to 2^-35 of the largest without rounding to zero
-constexpr uint64_t TA_LIMIT_NS = 4000000000ull;
+constexpr uint32_t TA_POLLS = 1u << 27;                    // of a barrier that does not come: some seconds
 
 struct TreeArgs {
     const uint16_t *Q, *K, *V;
@@ -67,7 +66,7 @@ struct TreeUnit {
     int row0, rows;                        // of the request's rows
     int len, table_row, head;
     int tile0, tile1, tiles;               // this block's tiles, the unit's
-    int two, copies, buf;                  // rows in both halves; copies of the rows; buffer of Q (two: both)
+    int two, copies, buf;                  // rows in both halves; log2 of the copies of the rows; buffer of Q (two: both)
     int slot;                              // part slot, -1: the whole unit is here
     int stop, pad;
 };
@@ -144,6 +143,13 @@ __device__ __forceinline__ int tiles_before(long long place, long long begin, in
     return (int)min(max((place - begin + weight - 1) / weight, 0ll), (long long)tiles);
 }
 
+// A unit's operands are made and used in the order K_0 .. K_{ahead - 1}, V_0 K_ahead V_1 K_{ahead + 1} .., the remaining V.  The place of K_j (which = 0) or V_j (1) among them,
+// without the drafted tokens' (tile 0), which have no codes, when `drafts` is 1.
+__device__ __forceinline__ int operand_place(int which, int j, int n, int ahead, int drafts) {
+    const int place = which ? (j < n - ahead ? ahead + 2 * j : n + j) : j < ahead ? j : 2 * j - ahead + 1;
+    return place - (drafts ? (place > 0) + (place > ahead) : 0);
+}
+
 template <int D>
 __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs x) {
     using C = TCfg<D>;
@@ -155,7 +161,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
     uint8_t* code_smem = op_smem + TA_OPS * C::op_bytes;
     uint8_t* scale_smem = code_smem + TA_CODES * C::code_bytes;
     TreeCtl* ctl = reinterpret_cast<TreeCtl*>(scale_smem + TA_SCALES * C::scale_bytes);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;      // (from one lane: known to be the same for the warp)
     volatile int* abort_flag = &ctl->abort_flag;
 
     if (tid == 0) {
@@ -168,12 +174,12 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
             mbar_init(smem_u32(&ctl->pv_done[i]), 1);
         }
         for (int i = 0; i < TA_OPS; ++i) {
-            mbar_init(smem_u32(&ctl->op_full[i]), TA_DECODERS);
+            mbar_init(smem_u32(&ctl->op_full[i]), TA_DECODERS / 2);
             mbar_init(smem_u32(&ctl->op_empty[i]), 1);
         }
         for (int i = 0; i < TA_CODES; ++i) {
             mbar_init(smem_u32(&ctl->codes_full[i]), 1);
-            mbar_init(smem_u32(&ctl->codes_empty[i]), TA_DECODERS);
+            mbar_init(smem_u32(&ctl->codes_empty[i]), TA_DECODERS / 2);
         }
         for (int i = 0; i < TA_SCALES; ++i) {
             mbar_init(smem_u32(&ctl->scales_full[i]), 1);
@@ -233,29 +239,86 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = ctl->tmem_base;
-    const uint64_t limit = TA_LIMIT_NS;
     bool ok = true;
+    // Every wait is bounded.  (Few instructions: there are some forty of them, and twenty warps in eight roles share the instruction caches.)
     auto wait = [&](uint64_t* b, uint32_t parity) -> bool {
-        if (ok && !mbar_wait_all(smem_u32(b), parity, abort_flag, limit)) {
-            if (lane == 0) *x.status = AG_ERR_TIMEOUT;
-            ok = false;
-        }
+        const uint32_t bar = smem_u32(b);
+        bool there = ok;
+        for (uint32_t polls = 0; there && !mbar_try_wait(bar, parity); ++polls)
+            if (polls > TA_POLLS || *abort_flag) {
+                *abort_flag = 1;
+                there = false;
+            }
+        ok = __all_sync(0xffffffffu, there);
         return ok;
     };
-    auto next_unit = [&](uint32_t u, TreeUnit& r) -> bool {
-        if (!wait(&ctl->unit_full[u % TA_UNITS], (u / TA_UNITS) & 1)) return false;
-        r = ctl->unit[u % TA_UNITS];
+    // unit u, which stays where it is until every reader has left it
+    auto next_unit = [&](uint32_t u) -> bool { return wait(&ctl->unit_full[u % TA_UNITS], (u / TA_UNITS) & 1) && !ctl->unit[u % TA_UNITS].stop; };
+    auto leave_unit = [&](uint32_t u) {
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&ctl->unit_empty[u % TA_UNITS]));
-        return !r.stop;
     };
-    TreeUnit un;
 
     if (warp >= TA_SOFT) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(TA_REGS_OTHER));
+    uint32_t n_tile = 0, n_code = 0;               // tiles, and tiles of codes, before the unit in hand
+    // copies of a unit's pages: K's codes and all pairs (which = 0), V's codes (1)
+    auto copies = [&](int which, const TreeUnit& un) {
+        const int nt = un.tile1 - un.tile0, ahead = min(un.two ? 1 : 2, nt), drafts = un.tile0 == 0, len = un.len;
+        const uint8_t* heads = x.pages + (size_t)un.head * kv4_head_bytes(D);
+        const int32_t* pages = x.page_of + (size_t)max(un.table_row, 0) * x.max_pages;
+        int window = -1, page = -1;                // pages of 16 tiles in the lanes: lane l has page 32 window + l of the row
+#pragma unroll 1
+        for (int j = 0; j < nt; ++j) {
+            const uint32_t n = n_tile + j;
+            const int t = un.tile0 + j, c = 2 * (t - 1);
+            if (which == 0 && !wait(&ctl->scales_empty[n % TA_SCALES], ((n / TA_SCALES) & 1) ^ 1)) return;
+            if (t == 0) {                          // the drafted tokens: nothing to copy
+                if (which == 0 && elect_one()) {
+                    ctl->valid[n % TA_INFO][0] = min(un.n, 64);
+                    ctl->valid[n % TA_INFO][1] = 0;
+                    mbar_arrive(smem_u32(&ctl->scales_full[n % TA_SCALES]));
+                }
+                __syncwarp();
+                continue;
+            }
+            if (c >> 5 != window) {
+                window = c >> 5;
+                page = window * 32 + lane < (len + 63) / 64 ? pages[window * 32 + lane] : -1;
+            }
+            const uint32_t code = n_code + operand_place(which, j, nt, ahead, drafts);
+            if (!wait(&ctl->codes_empty[code % TA_CODES], ((code / TA_CODES) & 1) ^ 1)) return;
+            const int id0 = __shfl_sync(0xffffffffu, page, c & 31), id1 = __shfl_sync(0xffffffffu, page, (c + 1) & 31);
+            const int v0 = id0 >= 0 && id0 < x.n_pages ? min(max(len - 64 * c, 0), 64) : 0, v1 = id1 >= 0 && id1 < x.n_pages ? min(max(len - 64 * c - 64, 0), 64) : 0;
+            if (elect_one()) {
+                const uint32_t bar = smem_u32(&ctl->codes_full[code % TA_CODES]), sbar = smem_u32(&ctl->scales_full[n % TA_SCALES]);
+                const uint32_t to = smem_u32(code_smem + (code % TA_CODES) * C::code_bytes), sto = smem_u32(scale_smem + (n % TA_SCALES) * C::scale_bytes);
+                const int there = (v0 > 0) + (v1 > 0);
+                const uint8_t *p0 = heads + (size_t)max(id0, 0) * x.H_kv * kv4_head_bytes(D), *p1 = heads + (size_t)max(id1, 0) * x.H_kv * kv4_head_bytes(D);
+                if (which == 0) {
+                    ctl->valid[n % TA_INFO][0] = v0;
+                    ctl->valid[n % TA_INFO][1] = v1;
+                    mbar_expect_tx(sbar, there * 16 * D);
+                    if (v0 > 0) bulk_load(sto, p0 + 64 * D, 16 * D, sbar);
+                    if (v1 > 0) bulk_load(sto + 16 * D, p1 + 64 * D, 16 * D, sbar);
+                }
+                mbar_expect_tx(bar, there * 32 * D);
+                if (v0 > 0) bulk_load(to, p0 + which * 32 * D, 32 * D, bar);
+                if (v1 > 0) bulk_load(to + 32 * D, p1 + which * 32 * D, 32 * D, bar);
+            }
+            __syncwarp();
+        }
+        n_tile += nt;
+        n_code += 2 * (nt - drafts);
+    };
+    // gave up: linger (bounded) so that copies already in flight land before the block leaves
+    auto linger = [&] {
+        const uint64_t t0 = globaltimer_ns();
+        while (globaltimer_ns() - t0 < 2000000ull) __nanosleep(1000);
+    };
     if (warp == 9) {
-        // ------------------------------------------------ units, and copies of their pages
-        uint32_t u = 0, n_tile = 0, n_code = 0, toggle = 0;
+        // ------------------------------------------------ units; copies of keys
+        uint32_t u = 0, toggle = 0;
         long long at = ctl->start_before;
         int s = p0 < p1 ? ctl->start_seq : x.n_seq;
         while (ok && s < x.n_seq && at < p1) {
@@ -275,7 +338,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                     if (lane == 0) {
                         TreeUnit r;
                         r.token0 = q.first; r.n = q.n; r.row0 = i * 256; r.rows = rows; r.len = q.len; r.table_row = q.table_row; r.head = h;
-                        r.tile0 = t0; r.tile1 = t1; r.tiles = q.tiles; r.two = two; r.copies = rows <= 32 ? 4 : rows <= 64 ? 2 : 1; r.buf = buf;
+                        r.tile0 = t0; r.tile1 = t1; r.tiles = q.tiles; r.two = two; r.copies = rows <= 32 ? 2 : rows <= 64 ? 1 : 0; r.buf = buf;
                         r.slot = t0 == 0 && t1 == q.tiles ? -1 : 2 * (int)blockIdx.x + (t1 < q.tiles ? 1 : 0);
                         r.stop = 0; r.pad = 0;
                         ctl->unit[u % TA_UNITS] = r;
@@ -289,59 +352,8 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                     }
                     __syncwarp();
                     ++u;
-                    // pages of the next 16 tiles in the lanes: lane l has page 32 window + l of the row
-                    int window = -1, page = -1;
-                    const int nt = t1 - t0, lead = two ? 1 : 2;
-                    auto copy = [&](int which, int j) {
-                        const int t = t0 + j;
-                        const uint32_t n = n_tile + j;
-                        if (which == 0 && !wait(&ctl->scales_empty[n % TA_SCALES], ((n / TA_SCALES) & 1) ^ 1)) return;
-                        if (t == 0) {                              // the drafted tokens: nothing to copy
-                            if (which == 0 && lane == 0) {
-                                ctl->valid[n % TA_INFO][0] = min(q.n, 64);
-                                ctl->valid[n % TA_INFO][1] = 0;
-                                mbar_arrive(smem_u32(&ctl->scales_full[n % TA_SCALES]));
-                            }
-                            __syncwarp();
-                            return;
-                        }
-                        const int c = 2 * (t - 1);
-                        if (c / 32 != window) {
-                            window = c / 32;
-                            page = window * 32 + lane < (q.len + 63) / 64 ? x.page_of[(size_t)q.table_row * x.max_pages + window * 32 + lane] : -1;
-                        }
-                        if (!wait(&ctl->codes_empty[n_code % TA_CODES], ((n_code / TA_CODES) & 1) ^ 1)) return;
-                        int id[2], v[2];
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            id[k] = __shfl_sync(0xffffffffu, page, (c + k) & 31);
-                            v[k] = id[k] >= 0 && id[k] < x.n_pages ? min(max(q.len - 64 * (c + k), 0), 64) : 0;
-                        }
-                        if (lane == 0) {
-                            const uint32_t bar = smem_u32(&ctl->codes_full[n_code % TA_CODES]), sbar = smem_u32(&ctl->scales_full[n % TA_SCALES]);
-                            const int there = (v[0] > 0) + (v[1] > 0);
-                            if (which == 0) {
-                                ctl->valid[n % TA_INFO][0] = v[0];
-                                ctl->valid[n % TA_INFO][1] = v[1];
-                                mbar_expect_tx(sbar, there * 16 * D);
-                            }
-                            mbar_expect_tx(bar, there * 32 * D);
-                            for (int k = 0; k < 2; ++k) {
-                                if (v[k] == 0) continue;
-                                const uint8_t* block = x.pages + ((size_t)id[k] * x.H_kv + h) * kv4_head_bytes(D);
-                                if (which == 0) bulk_load(smem_u32(scale_smem + (n % TA_SCALES) * C::scale_bytes + k * 16 * D), block + 64 * D, 16 * D, sbar);
-                                bulk_load(smem_u32(code_smem + (n_code % TA_CODES) * C::code_bytes + k * 32 * D), block + which * 32 * D, 32 * D, bar);
-                            }
-                        }
-                        __syncwarp();
-                        ++n_code;
-                    };
-                    for (int j = 0; j < min(lead, nt) && ok; ++j) copy(0, j);
-                    for (int j = 0; j < nt && ok; ++j) {
-                        copy(1, j);
-                        if (j + lead < nt && ok) copy(0, j + lead);
-                    }
-                    n_tile += nt;
+                    copies(0, ctl->unit[(u - 1) % TA_UNITS]);
+                    if (!ok) break;
                 }
             }
             at += line;
@@ -352,15 +364,11 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
             mbar_arrive(smem_u32(&ctl->unit_full[u % TA_UNITS]));
         }
         __syncwarp();
-        if (!ok && lane == 0) {
-            // gave up: linger (bounded) so that copies already in flight land before the block leaves
-            const uint64_t t0 = globaltimer_ns();
-            while (globaltimer_ns() - t0 < 2000000ull) __nanosleep(1000);
-        }
+        if (!ok && lane == 0) linger();
     } else if (warp == 10) {
         // ------------------------------------------------ exponents of the tiles
-        uint32_t n_tile = 0;
-        for (uint32_t u = 0; next_unit(u, un); ++u) {
+        for (uint32_t u = 0; next_unit(u); ++u) {
+            const TreeUnit& un = ctl->unit[u % TA_UNITS];
             int ev = 1000;                                         // none yet
             for (int j = 0; j < un.tile1 - un.tile0; ++j) {
                 const uint32_t n = n_tile + j;
@@ -415,109 +423,89 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                     mbar_arrive(smem_u32(&ctl->scales_ready[n % TA_SCALES]));
                 }
                 __syncwarp();
-                if (ev == 1000) ev = 1000;
             }
             n_tile += un.tile1 - un.tile0;
             if (!ok) break;
+            leave_unit(u);
         }
     } else if (warp == 11) {
-        // ------------------------------------------------ tokens beyond the most that a request may have
+        // ------------------------------------------------ copies of values; before them, tokens beyond the most that a request may have
         for (int s = blockIdx.x; s < x.n_seq; s += gridDim.x) {
             const long long first = min(max((long long)x.off[s], 0ll), x.n_tokens), stop = min(max((long long)x.off[s + 1], first), x.n_tokens);
             for (long long t = first + x.max_tokens; t < stop; ++t)
                 for (int d = lane * 8; d < x.H_q * D; d += 256) *reinterpret_cast<uint4*>(x.O + t * x.o_stride + d) = make_uint4(0, 0, 0, 0);
         }
+        for (uint32_t u = 0; next_unit(u); ++u) {
+            copies(1, ctl->unit[u % TA_UNITS]);
+            if (!ok) break;
+            leave_unit(u);
+        }
+        if (!ok && lane == 0) linger();
     } else if (warp == 8) {
         // ------------------------------------------------ MMA issuer (the warp runs converged, one elected lane issues)
         const uint32_t idesc_s = make_idesc_f16(TA_TILE, TA_TILE, 0, 0), idesc_o = make_idesc_f16(TA_TILE, D, 0, 1);
         const uint64_t dk_t = make_smem_desc(0, 16, 1024, 2);                  // Q, K: K-major, 128-byte swizzle
         const uint64_t dv_t = make_smem_desc(0, TA_TILE * 128, 1024, 2);       // V: N-major, 64-column blocks 16 KB apart
         const uint32_t q_base = smem_u32(q_smem), op_base = smem_u32(op_smem);
-        uint32_t n_op = 0, n_q[2] = {0, 0}, n_p[2] = {0, 0};
-        auto op_wait = [&](uint32_t n) { return wait(&ctl->op_full[n % TA_OPS], (n / TA_OPS) & 1); };
-        auto op_done = [&](uint32_t n) {
-            if (elect_one()) tc_commit(smem_u32(&ctl->op_empty[n % TA_OPS]));
+        uint32_t n_op = 0, q_parity = 0, p_parity = 0;      // parities: a bit for each barrier
+        auto commit = [&](uint64_t* b) {
+            if (elect_one()) tc_commit(smem_u32(b));
             __syncwarp();
         };
-        auto scores = [&](int w, int buf, uint32_t n) {
-            const uint64_t dq = dk_t | (uint64_t)((q_base + buf * C::op_bytes) >> 4), dk = dk_t | (uint64_t)((op_base + n % TA_OPS * C::op_bytes) >> 4);
-            if (elect_one()) {
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k)
-                    tc_mma_f16(tmem + w * TA_TILE, dq + (k >> 2) * (TA_TILE * 128 >> 4) + (k & 3) * 2, dk + (k >> 2) * (TA_TILE * 128 >> 4) + (k & 3) * 2, idesc_s, k ? 1u : 0u);
-                tc_commit(smem_u32(&ctl->s_full[w]));
-                mbar_arrive(smem_u32(&ctl->s_full[w]));    // (with what this warp has seen: the tile's exponents, the rows' factors)
-            }
-            __syncwarp();
-        };
-        auto outputs = [&](int w, bool first, uint32_t n) {
-            if (!wait(&ctl->p_full[w], n_p[w] & 1)) return;
-            ++n_p[w];
-            tc_fence_after();
-            const uint64_t dv = dv_t | (uint64_t)((op_base + n % TA_OPS * C::op_bytes) >> 4);
-            if (elect_one()) {
-#pragma unroll
-                for (int k = 0; k < TA_TILE / 16; ++k)                         // P of keys 64 h .. 64 h + 63 lies at columns 64 h .. 64 h + 31
-                    tc_mma_f16_ts(tmem + 256 + w * D, tmem + w * TA_TILE + (k >> 2) * 64 + (k & 3) * 8, dv + k * (2048 >> 4), idesc_o, first && k == 0 ? 0u : 1u);
-                tc_commit(smem_u32(&ctl->pv_done[w]));
-            }
-            __syncwarp();
-        };
-        for (uint32_t u = 0; next_unit(u, un); ++u) {
-            const int nt = un.tile1 - un.tile0;
+        for (uint32_t u = 0; next_unit(u); ++u) {
+            const TreeUnit& un = ctl->unit[u % TA_UNITS];
+            const int nt = __shfl_sync(0xffffffffu, un.tile1 - un.tile0, 0), two = __shfl_sync(0xffffffffu, un.two, 0), buf = __shfl_sync(0xffffffffu, un.buf, 0), lead = two ? 1 : 2;
+#pragma unroll 1
             for (int b = 0; b < 2; ++b)
-                if (un.two || un.buf == b) {
-                    wait(&ctl->q_full[b], n_q[b] & 1);
-                    ++n_q[b];
+                if (two || buf == b) {
+                    wait(&ctl->q_full[b], q_parity >> b & 1);
+                    q_parity ^= 1u << b;
                 }
-            if (!ok) break;
-            if (!un.two) {
-                // operands in the order K_0 K_1 V_0 K_2 V_1 ..
-                for (int j = 0; j < min(2, nt) && ok; ++j) {
-                    if (!op_wait(n_op)) break;
-                    tc_fence_after();
-                    scores(j, un.buf, n_op);
-                    op_done(n_op++);
-                }
-                for (int j = 0; j < nt && ok; ++j) {
-                    if (!op_wait(n_op)) break;
-                    outputs(j & 1, j < 2, n_op);
-                    if (!ok) break;
-                    op_done(n_op++);
-                    if (j + 2 < nt) {
-                        if (!op_wait(n_op)) break;
+            // step j: the products of V_j, the scores of K_{j + lead}, for one tile of rows or for both in turn; operands come in this order
+#pragma unroll 1
+            for (int j = -lead; j < nt && ok; ++j) {
+                const bool pv = j >= 0, qk = j + lead < nt;
+                const uint32_t nv = n_op, nk = n_op + (pv ? 1 : 0);
+                n_op = nk + (qk ? 1 : 0);
+                if (pv && !wait(&ctl->op_full[nv % TA_OPS], (nv / TA_OPS) & 1)) break;
+                const int w0 = two ? 0 : j & 1, w1 = two ? 1 : j & 1;
+#pragma unroll 1
+                for (int w = w0; w <= w1; ++w) {
+                    if (pv) {
+                        if (!wait(&ctl->p_full[w], p_parity >> w & 1)) break;
+                        p_parity ^= 1u << w;
                         tc_fence_after();
-                        scores(j & 1, un.buf, n_op);
-                        op_done(n_op++);
-                    }
-                }
-            } else {
-                // K_0 V_0 K_1 V_1 ..
-                if (!op_wait(n_op)) break;
-                tc_fence_after();
-                scores(0, 0, n_op);
-                scores(1, 1, n_op);
-                op_done(n_op++);
-                for (int j = 0; j < nt && ok; ++j) {
-                    const uint32_t nv = n_op, nk = n_op + 1;
-                    if (!op_wait(nv)) break;
-                    for (int w = 0; w < 2 && ok; ++w) {
-                        outputs(w, j == 0, nv);
-                        if (j + 1 < nt && ok) {
-                            if (w == 0 && !op_wait(nk)) break;
-                            tc_fence_after();
-                            scores(w, w, nk);
+                        const uint64_t dv = dv_t | (uint64_t)((op_base + nv % TA_OPS * C::op_bytes) >> 4);
+                        const uint32_t first = j < lead ? 0u : 1u, d = tmem + 256 + w * D, p = tmem + w * TA_TILE;
+                        if (elect_one()) {
+#pragma unroll
+                            for (int k = 0; k < TA_TILE / 16; ++k)                     // P of keys 64 h .. 64 h + 63 lies at columns 64 h .. 64 h + 31
+                                tc_mma_f16_ts(d, p + (k >> 2) * 64 + (k & 3) * 8, dv + k * (2048 >> 4), idesc_o, k == 0 ? first : 1u);
+                            tc_commit(smem_u32(&ctl->pv_done[w]));
                         }
+                        __syncwarp();
                     }
-                    if (!ok) break;
-                    op_done(nv);
-                    ++n_op;
-                    if (j + 1 < nt) {
-                        op_done(nk);
-                        ++n_op;
+                    if (qk) {
+                        if (w == w0 && !wait(&ctl->op_full[nk % TA_OPS], (nk / TA_OPS) & 1)) break;
+                        tc_fence_after();
+                        const uint64_t dq = dk_t | (uint64_t)((q_base + (two ? w : buf) * C::op_bytes) >> 4), dk = dk_t | (uint64_t)((op_base + nk % TA_OPS * C::op_bytes) >> 4);
+                        if (elect_one()) {
+#pragma unroll
+                            for (int k = 0; k < D / 16; ++k)
+                                tc_mma_f16(tmem + w * TA_TILE, dq + (k >> 2) * (TA_TILE * 128 >> 4) + (k & 3) * 2, dk + (k >> 2) * (TA_TILE * 128 >> 4) + (k & 3) * 2, idesc_s,
+                                           k ? 1u : 0u);
+                            tc_commit(smem_u32(&ctl->s_full[w]));
+                            mbar_arrive(smem_u32(&ctl->s_full[w]));    // (with what this warp has seen: the tile's exponents, the rows' factors)
+                        }
+                        __syncwarp();
                     }
                 }
+                if (!ok) break;
+                if (pv) commit(&ctl->op_empty[nv % TA_OPS]);
+                if (qk) commit(&ctl->op_empty[nk % TA_OPS]);
             }
+            if (!ok) break;
+            leave_unit(u);
         }
         __syncwarp();
         if (*abort_flag) {
@@ -532,20 +520,20 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
     } else {
         // ------------------------------------------------ decoders: Q, the drafted tokens and the cache's codes as operands
         const int dt = tid - 12 * 32, dwarp = warp - 12;
-        const int token = dt & 127, half = dt >> 7, page = token >> 6, tk = token & 63;
-        const uint32_t row_at = token * 128, sw = token & 7;       // operand row: chunk c at (c / 8) 16 KB + 128 row + 16 ((c ^ row) mod 8)
-        uint32_t n_op = 0, n_code = 0, n_tile = 0, n_q[2] = {0, 0};
+        const int token = dt & 127, which = dt >> 7, page = token >> 6, tk = token & 63, sw = token & 7;
+        uint32_t n_op = 0, q_parity = 0;
         auto arrive = [&](uint64_t* b) {
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(b));
         };
-        for (uint32_t u = 0; next_unit(u, un); ++u) {
+        for (uint32_t u = 0; next_unit(u); ++u) {
+            const TreeUnit& un = ctl->unit[u % TA_UNITS];
             const int nt = un.tile1 - un.tile0, lead = un.two ? 1 : 2;
             // ---- Q: rows times a power of two that puts their largest element at 2^7
             for (int b = 0; b < 2; ++b) {
                 if (!un.two && un.buf != b) continue;
-                if (!wait(&ctl->q_empty[b], (n_q[b] & 1) ^ 1)) break;
-                ++n_q[b];
+                if (!wait(&ctl->q_empty[b], (q_parity >> b & 1) ^ 1)) break;
+                q_parity ^= 1u << b;
                 if (dwarp == 0) {
                     // who sees whom among the drafted tokens: paths to the root by doubling, two tokens a lane
                     unsigned long long anc[2];
@@ -578,7 +566,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                     ctl->sees[b][lane + 32] = anc[1];
                 }
                 constexpr int L = D / 8, R = 32 / L;               // lanes of a row, rows of a warp
-                const int unit_row0 = un.two ? b * TA_TILE : 0, rows = min(un.rows - unit_row0, TA_TILE), distinct = TA_TILE / un.copies;
+                const int unit_row0 = un.two ? b * TA_TILE : 0, rows = min(un.rows - unit_row0, TA_TILE), distinct = TA_TILE >> un.copies;
                 const int c = lane % L;
                 for (int r0 = dwarp * R * 4; r0 < distinct; r0 += TA_DECODERS * R * 4) {
                     uint4 raw[4];
@@ -614,106 +602,103 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                 arrive(&ctl->q_full[b]);
             }
             if (!ok) break;
-            // ---- operands
-            auto make = [&](int which, int j) {
+            // ---- operands: warps 12-15 make K's, warps 16-19 V's; thread = token of the tile
+            const int ahead = min(lead, nt), drafts = un.tile0 == 0;
+#pragma unroll 1
+            for (int j = 0; j < nt; ++j) {
                 const uint32_t n = n_tile + j;
-                if (which == 0 && !wait(&ctl->scales_ready[n % TA_SCALES], (n / TA_SCALES) & 1)) return;
+                const uint32_t op = n_op + operand_place(which, j, nt, ahead, 0), code = n_code + operand_place(which, j, nt, ahead, drafts);
+                if (!wait(&ctl->scales_ready[n % TA_SCALES], (n / TA_SCALES) & 1)) break;
                 const TreeInfo& f = ctl->info[n % TA_INFO];
                 const int e = which ? f.ev : f.ek;
-                uint8_t* to = op_smem + n_op % TA_OPS * C::op_bytes;
-                if (un.tile0 + j > 0) {
-                    const bool valid = tk < (page ? f.v1 : f.v0);
-                    const float k24 = pow2i(24 - e);
+                uint8_t* to = op_smem + op % TA_OPS * C::op_bytes + token * 128;       // operand row: chunk c at (c / 8) 16 KB + 128 row + 16 ((c ^ row) mod 8)
+                if (j > 0 || !drafts) {
+                    uint32_t pair[NG];
                     const uint8_t* sc = scale_smem + (n % TA_SCALES) * C::scale_bytes + page * 16 * D + which * 8 * D + tk * 4 * NG;
-                    const uint8_t* codes = code_smem + (n_code % TA_CODES) * C::code_bytes + page * 32 * D;
-                    Scale2 a, b;
-                    if (which == 0) {
-                        // this thread: half of the groups, of all four runs t of a group
-                        const int h = half ^ ((tk >> (D == 128 ? 3 : 4)) & 1);
-                        uint32_t pair[2];
-                        if (D == 128) *reinterpret_cast<uint2*>(pair) = *reinterpret_cast<const uint2*>(sc + 8 * h);
-                        else pair[0] = pair[1] = *reinterpret_cast<const uint32_t*>(sc + 4 * h);
-                        if (!valid) pair[0] = pair[1] = 0;
-                        a = scale_pair(pair[0], pair[0], k24);
-                        b = scale_pair(pair[1], pair[1], k24);
-                        if (!wait(&ctl->codes_full[n_code % TA_CODES], (n_code / TA_CODES) & 1) || !wait(&ctl->op_empty[n_op % TA_OPS], ((n_op / TA_OPS) & 1) ^ 1)) return;
-                        const int turn = (tk >> (D == 128 ? 1 : 2)) & 3;
+                    if (D == 128) *reinterpret_cast<uint4*>(pair) = *reinterpret_cast<const uint4*>(sc);
+                    else *reinterpret_cast<uint2*>(pair) = *reinterpret_cast<const uint2*>(sc);
+                    if (tk >= (page ? f.v1 : f.v0)) {
 #pragma unroll
+                        for (int g = 0; g < NG; ++g) pair[g] = 0;
+                    }
+                    const float k24 = pow2i(24 - e);
+                    const uint8_t* codes = code_smem + (code % TA_CODES) * C::code_bytes + page * 32 * D;
+                    if (which == 0) {
+                        Scale2 g[NG];
+#pragma unroll
+                        for (int k = 0; k < NG; ++k) g[k] = scale_pair(pair[k], pair[k], k24);
+                        if (!wait(&ctl->codes_full[code % TA_CODES], (code / TA_CODES) & 1) || !wait(&ctl->op_empty[op % TA_OPS], ((op / TA_OPS) & 1) ^ 1)) break;
+                        const int turn = (tk >> (D == 128 ? 1 : 2)) & 3;               // (neighbouring lanes at different runs: no bank twice)
+#pragma unroll 1
                         for (int t0 = 0; t0 < 4; ++t0) {
                             const int t = t0 ^ turn;
                             if (D == 128) {
-                                const uint2 w = *reinterpret_cast<const uint2*>(codes + tk * 64 + t * 16 + 8 * h);
-                                uint8_t* p = to + h * (TA_TILE * 128) + row_at;                 // chunks 8 h + t and 8 h + 4 + t
-                                *reinterpret_cast<uint4*>(p + ((t ^ sw) << 4)) = decode_word(w.x, a, a);
-                                *reinterpret_cast<uint4*>(p + (((t ^ 4) ^ sw) << 4)) = decode_word(w.y, b, b);
+                                const uint4 w = *reinterpret_cast<const uint4*>(codes + tk * 64 + t * 16);
+                                uint8_t *p = to + ((t ^ sw) << 4), *q = to + (((t ^ 4) ^ sw) << 4);      // chunks t, 4 + t, 8 + t, 12 + t
+                                *reinterpret_cast<uint4*>(p) = decode_word(w.x, g[0], g[0]);
+                                *reinterpret_cast<uint4*>(q) = decode_word(w.y, g[1], g[1]);
+                                *reinterpret_cast<uint4*>(p + TA_TILE * 128) = decode_word(w.z, g[NG - 2], g[NG - 2]);
+                                *reinterpret_cast<uint4*>(q + TA_TILE * 128) = decode_word(w.w, g[NG - 1], g[NG - 1]);
                             } else {
-                                const uint32_t w = *reinterpret_cast<const uint32_t*>(codes + tk * 32 + t * 8 + 4 * h);
-                                *reinterpret_cast<uint4*>(to + row_at + (((4 * h + t) ^ sw) << 4)) = decode_word(w, a, a);
+                                const uint2 w = *reinterpret_cast<const uint2*>(codes + tk * 32 + t * 8);
+                                *reinterpret_cast<uint4*>(to + ((t ^ sw) << 4)) = decode_word(w.x, g[0], g[0]);
+                                *reinterpret_cast<uint4*>(to + (((t ^ 4) ^ sw) << 4)) = decode_word(w.y, g[1], g[1]);
                             }
                         }
                     } else {
-                        uint32_t pair[NG];
-                        if (D == 128) *reinterpret_cast<uint4*>(pair) = *reinterpret_cast<const uint4*>(sc);
-                        else *reinterpret_cast<uint2*>(pair) = *reinterpret_cast<const uint2*>(sc);
-                        if (!valid) {
-#pragma unroll
-                            for (int g = 0; g < NG; ++g) pair[g] = 0;
-                        }
-                        a = D == 128 ? scale_pair(pair[0], pair[NG / 2], k24) : scale_pair(pair[0], pair[0], k24);
-                        b = D == 128 ? scale_pair(pair[1], pair[NG - 1], k24) : scale_pair(pair[1], pair[1], k24);
-                        if (!wait(&ctl->codes_full[n_code % TA_CODES], (n_code / TA_CODES) & 1) || !wait(&ctl->op_empty[n_op % TA_OPS], ((n_op / TA_OPS) & 1) ^ 1)) return;
+                        const Scale2 a = D == 128 ? scale_pair(pair[0], pair[NG / 2], k24) : scale_pair(pair[0], pair[0], k24);
+                        const Scale2 b = D == 128 ? scale_pair(pair[1], pair[NG - 1], k24) : scale_pair(pair[1], pair[1], k24);
+                        if (!wait(&ctl->codes_full[code % TA_CODES], (code / TA_CODES) & 1) || !wait(&ctl->op_empty[op % TA_OPS], ((op / TA_OPS) & 1) ^ 1)) break;
                         const uint8_t* from = codes + (tk >> 3) * 4 * D + ((tk >> 1) & 3) * (D / 8) + (tk & 1) * (D / 16);
                         const int turn = D == 128 ? (tk >> 3) & 1 : (tk >> 3) & 3;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int g = (4 * half + i) ^ turn;
+#pragma unroll 1
+                        for (int i = 0; i < 8; ++i) {
+                            const int h = i ^ turn;                                    // element 16 i' + 8 j' + h of the token
                             if (D == 128) {
-                                const uint2 w = *reinterpret_cast<const uint2*>(from + g * 64);
-                                uint8_t* p = to + (g >> 2) * (TA_TILE * 128) + row_at;          // chunks 2 g and 2 g + 1
-                                *reinterpret_cast<uint4*>(p + (((2 * g) ^ sw) & 7) * 16) = decode_word(w.x, a, b);
-                                *reinterpret_cast<uint4*>(p + (((2 * g + 1) ^ sw) & 7) * 16) = decode_word(w.y, a, b);
+                                const uint2 w = *reinterpret_cast<const uint2*>(from + h * 64);
+                                uint8_t* p = to + (h >> 2) * (TA_TILE * 128);          // chunks 2 h and 2 h + 1
+                                const int c = ((2 * h) ^ sw) & 7;
+                                *reinterpret_cast<uint4*>(p + c * 16) = decode_word(w.x, a, b);
+                                *reinterpret_cast<uint4*>(p + (c ^ 1) * 16) = decode_word(w.y, a, b);
                             } else {
-                                const uint32_t w = *reinterpret_cast<const uint32_t*>(from + g * 32);
-                                *reinterpret_cast<uint4*>(to + row_at + ((g ^ sw) << 4)) = decode_word(w, a, b);
+                                const uint32_t w = *reinterpret_cast<const uint32_t*>(from + h * 32);
+                                *reinterpret_cast<uint4*>(to + ((h ^ sw) << 4)) = decode_word(w, a, b);
                             }
                         }
                     }
-                    arrive(&ctl->codes_empty[n_code % TA_CODES]);
-                    ++n_code;
+                    arrive(&ctl->codes_empty[code % TA_CODES]);
                 } else {
-                    if (!wait(&ctl->op_empty[n_op % TA_OPS], ((n_op / TA_OPS) & 1) ^ 1)) return;
-                    // drafted tokens: thread (token of 64, quarter of the chunks); the rows behind them are zeros
-                    const int tok = dt & 63, quarter = dt >> 6;
+                    if (!wait(&ctl->op_empty[op % TA_OPS], ((op / TA_OPS) & 1) ^ 1)) break;
+                    // drafted tokens: rows of up to 64, the others are zeros
                     const float k0 = times_pow2(1.f, -e);
-                    const uint16_t* from = (which ? x.V + (un.token0 + (long long)tok) * x.v_stride : x.K + (un.token0 + (long long)tok) * x.k_stride) + un.head * D;
-#pragma unroll
-                    for (int i = 0; i < D / 32; ++i) {
-                        const int c = quarter * (D / 32) + i;
+                    const uint16_t* from = (which ? x.V + (un.token0 + (long long)token) * x.v_stride : x.K + (un.token0 + (long long)token) * x.k_stride) + un.head * D;
+#pragma unroll 1
+                    for (int c = 0; c < D / 8; ++c) {
                         float v[8];
 #pragma unroll
                         for (int k = 0; k < 8; ++k) {
                             // K: elements 8 c + (0, 4, 1, 5, ..); V: column 8 c + k is element 16 (k / 2 + 4 (k mod 2)) + 8 (c mod 2) + c / 2, D = 64: 16 (k / 2) + 8 (k mod 2) + c
                             const int d = which == 0 ? 8 * c + (k >> 1) + 4 * (k & 1) : D == 128 ? 16 * ((k >> 1) + 4 * (k & 1)) + 8 * (c & 1) + (c >> 1) : 16 * (k >> 1) + 8 * (k & 1) + c;
-                            v[k] = tok < un.n ? __uint_as_float((uint32_t)from[d] << 16) * k0 : 0.f;
+                            v[k] = token < un.n ? __uint_as_float((uint32_t)from[d] << 16) * k0 : 0.f;
                             if (which && !(fabsf(v[k]) < INFINITY)) v[k] = 0.f;            // put back at the end, for the rows that see it
                         }
-                        const int at = (c >> 3) * (TA_TILE * 128) + tok * 128 + (((c ^ tok) & 7) << 4);
-                        *reinterpret_cast<uint4*>(to + at) = make_uint4(pack_f16(v[0], v[1]), pack_f16(v[2], v[3]), pack_f16(v[4], v[5]), pack_f16(v[6], v[7]));
-                        *reinterpret_cast<uint4*>(to + at + 64 * 128) = make_uint4(0, 0, 0, 0);
+                        *reinterpret_cast<uint4*>(to + (c >> 3) * (TA_TILE * 128) + (((c ^ token) & 7) << 4)) =
+                            make_uint4(pack_f16(v[0], v[1]), pack_f16(v[2], v[3]), pack_f16(v[4], v[5]), pack_f16(v[6], v[7]));
                     }
                 }
                 fence_proxy_async_smem();
-                arrive(&ctl->op_full[n_op % TA_OPS]);
-                if (which) arrive(&ctl->scales_empty[n % TA_SCALES]);
-                ++n_op;
-            };
-            for (int j = 0; j < min(lead, nt) && ok; ++j) make(0, j);
-            for (int j = 0; j < nt && ok; ++j) {
-                make(1, j);
-                if (j + lead < nt && ok) make(0, j + lead);
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(smem_u32(&ctl->op_full[op % TA_OPS]));
+                    mbar_arrive(smem_u32(&ctl->scales_empty[n % TA_SCALES]));
+                }
+                __syncwarp();
             }
             if (!ok) break;
+            n_op += 2 * nt;
+            n_code += 2 * (nt - drafts);
             n_tile += nt;
+            leave_unit(u);
         }
     }
     } else {
@@ -728,9 +713,10 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
             if (lane == 0) mbar_arrive(smem_u32(&ctl->together));
             return wait(&ctl->together, n_together++ & 1);
         };
-        for (uint32_t u = 0; next_unit(u, un); ++u) {
+        for (uint32_t u = 0; next_unit(u); ++u) {
+            const TreeUnit& un = ctl->unit[u % TA_UNITS];
             const int nt = un.tile1 - un.tile0, step = un.two ? 1 : 2, j0 = un.two ? 0 : w;
-            const int distinct = TA_TILE / un.copies, copy = r / distinct, row = (un.two ? w * TA_TILE : 0) + r % distinct;   // row of the unit
+            const int copies = un.copies, distinct = TA_TILE >> copies, copy = r >> (7 - copies), row = (un.two ? w * TA_TILE : 0) + (r & (distinct - 1));   // row of the unit
             const bool live = row < un.rows;
             const int buf = un.two ? w : un.buf;
             float m = -INFINITY, l = 0.f, rs = 0.f;
@@ -740,37 +726,28 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                 tc_fence_after();
                 const TreeInfo f = ctl->info[(n_tile + j) % TA_INFO];
                 const bool drafts = un.tile0 + j == 0;
-                if (j == j0) rs = ctl->row_scale[buf][r % distinct];
+                if (j == j0) rs = ctl->row_scale[buf][r & (distinct - 1)];
                 const float c = fminf(fmaxf(times_pow2(rs, f.ek), 1e-37f), 3e38f);    // (not 0 or infinite: scores at -inf, scores of 0)
-                uint32_t seen[4];
-                const bool masked = drafts || f.v0 < 64 || f.v1 < 64;
-                if (masked) {
-                    unsigned long long a = f.v0 >= 64 ? ~0ull : (1ull << f.v0) - 1, b = f.v1 >= 64 ? ~0ull : (1ull << f.v1) - 1;
+                if (drafts || f.v0 < 64 || f.v1 < 64) {
+                    // what is not seen: -inf, written over the scores (the drafted tokens, a row's last tile)
+                    unsigned long long see[2] = {f.v0 >= 64 ? ~0ull : (1ull << f.v0) - 1, f.v1 >= 64 ? ~0ull : (1ull << f.v1) - 1};
                     if (drafts) {
                         odd = f.odd;
-                        a = live ? ctl->sees[buf][(un.row0 + row) / x.G] : 0ull;
+                        see[0] = live ? ctl->sees[buf][(un.row0 + row) / x.G] : 0ull;
                     }
-                    seen[0] = (uint32_t)a;
-                    seen[1] = (uint32_t)(a >> 32);
-                    seen[2] = (uint32_t)b;
-                    seen[3] = (uint32_t)(b >> 32);
-                }
-                auto load32 = [&](int block, uint32_t(&v)[32]) {               // scores 32 block .. + 31, those that are not seen at -inf
-                    tmem_ld_32x32(t_s + block * 32, v);
-                    tmem_ld_wait();
-                    if (masked) {
-                        const uint32_t see = seen[block];
+#pragma unroll 1
+                    for (int b = 0; b < 4; ++b) {
+                        uint32_t v[32];
+                        tmem_ld_32x32(t_s + b * 32, v);
+                        tmem_ld_wait();
+                        const uint32_t bits = (uint32_t)((b & 2 ? see[1] : see[0]) >> (32 * (b & 1)));
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
-                            if (!(see >> i & 1)) v[i] = 0xff800000u;
+                            if (!(bits >> i & 1)) v[i] = 0xff800000u;
+                        tmem_st_32x32(t_s + b * 32, v);
                     }
-                };
-                auto top_of = [&](const uint32_t(&v)[32]) {
-                    float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) t[i & 3] = fmaxf(t[i & 3], __uint_as_float(v[i]));
-                    return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
-                };
+                    tmem_st_wait();
+                }
                 // the reference, once the tile's largest score is known; outputs so far follow it
                 auto refer = [&](float raw_top) -> bool {
                     const float top = raw_top * c;
@@ -801,7 +778,15 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                 };
                 f32x2 sum = pack2(0.f, 0.f);
                 const f32x2 c2 = pack2(c, c);
-                auto exps = [&](const uint32_t(&v)[32], f32x2 ref2, uint32_t(&p)[16]) {
+                // scores from column `at` on, in pieces of 32: their maximum; their probabilities, as fp16 at column `to`
+                auto top_of = [](const uint32_t(&v)[32]) {
+                    float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) t[i & 3] = fmaxf(t[i & 3], __uint_as_float(v[i]));
+                    return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+                };
+                auto exps = [&](const uint32_t(&v)[32], f32x2 ref2, uint32_t to) {
+                    uint32_t p[16];
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         float a, b;
@@ -811,55 +796,35 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                         sum = add2(sum, pack2(a, b));
                         p[i] = pack_f16(a, b);
                     }
+                    tmem_st_32x16(to, p);
                 };
-                auto ref_of = [&] {
-                    const float s = (m == -INFINITY ? 0.f : -m) + TA_SHIFT;
-                    return pack2(s, s);
-                };
-                uint32_t v[32], p[16];
-                if (un.copies == 1) {
-                    uint32_t v2[32];
-                    load32(0, v);
-                    float top = top_of(v);
-                    load32(1, v);
+                // this copy's blocks of 32 keys
+                const int blocks = 4 >> copies, b0 = copy * blocks;
+                uint32_t v[32];
+                float top = -INFINITY;
+#pragma unroll 1
+                for (int b = b0 + blocks - 1; b >= b0; --b) {
+                    tmem_ld_32x32(t_s + 32 * b, v);
+                    tmem_ld_wait();
                     top = fmaxf(top, top_of(v));
-                    load32(2, v);
-                    load32(3, v2);
-                    if (!refer(fmaxf(top, fmaxf(top_of(v), top_of(v2))))) break;
-                    const f32x2 ref2 = ref_of();
-                    exps(v, ref2, p);
-                    tmem_st_32x16(t_s + 64, p);
-                    exps(v2, ref2, p);
-                    tmem_st_32x16(t_s + 80, p);
-                    load32(0, v);
-                    load32(1, v2);
-                    exps(v, ref2, p);
-                    tmem_st_32x16(t_s, p);
-                    exps(v2, ref2, p);
-                    tmem_st_32x16(t_s + 16, p);
-                } else if (un.copies == 2) {
-                    uint32_t v2[32];
-                    load32(2 * copy, v);
-                    load32(2 * copy + 1, v2);
-                    if (!refer(fmaxf(top_of(v), top_of(v2)))) break;
-                    const f32x2 ref2 = ref_of();
-                    exps(v, ref2, p);
-                    tmem_st_32x16(t_s + 64 * copy, p);
-                    exps(v2, ref2, p);
-                    tmem_st_32x16(t_s + 64 * copy + 16, p);
+                }
+                if (!refer(top)) break;
+                const float ref = (m == -INFINITY ? 0.f : -m) + TA_SHIFT;
+                const f32x2 ref2 = pack2(ref, ref);
+#pragma unroll 1
+                for (int b = b0;;) {
+                    exps(v, ref2, t_s + 64 * (b >> 1) + 16 * (b & 1));         // (over scores that have been read: block 0's lie there, or block 2's)
+                    if (++b == b0 + blocks) break;
+                    tmem_ld_32x32(t_s + 32 * b, v);
+                    tmem_ld_wait();
+                }
+                if (copies) {
+                    uint32_t zero[16];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) p[i] = 0;
-                    tmem_st_32x16(t_s + 64 * (1 - copy), p);
-                    tmem_st_32x16(t_s + 64 * (1 - copy) + 16, p);
-                } else {
-                    load32(copy, v);
-                    if (!refer(top_of(v))) break;
-                    exps(v, ref_of(), p);
-                    tmem_st_32x16(t_s + 64 * (copy >> 1) + 16 * (copy & 1), p);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) p[i] = 0;
-                    for (int k = 0; k < 4; ++k)
-                        if (k != copy) tmem_st_32x16(t_s + 64 * (k >> 1) + 16 * (k & 1), p);
+                    for (int i = 0; i < 16; ++i) zero[i] = 0;
+#pragma unroll 1
+                    for (int b = 0; b < 4; ++b)
+                        if ((b >> (2 - copies)) != copy) tmem_st_32x16(t_s + 64 * (b >> 1) + 16 * (b & 1), zero);
                 }
                 float sum0, sum1;
                 unpack2(sum, sum0, sum1);
@@ -876,160 +841,153 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                 if (!wait(&ctl->pv_done[w], (n_s - 1) & 1)) break;
                 tc_fence_after();
             }
-            // ---- the end of the unit, or of this block's share of it
-            const int at = un.row0 + row;
-            uint16_t* out = x.O + (long long)(un.token0 + at / x.G) * x.o_stride + (long long)(un.head * x.G + at % x.G) * D;
-            float* part = x.part + ((size_t)max(un.slot, 0) * x.part_rows + row) * D;
-            // N values of the row from element d0 on: to the output, or to the part
-            auto put = [&](auto count, int d0, float* v) {
-                constexpr int N = decltype(count)::value;
-                if (odd) {                                                     // what the row sees of drafted values that are not finite
-                    const unsigned long long sees = ctl->sees[buf][at / x.G];
-                    for (int i = 0; i < un.n; ++i) {
-                        if (!(sees >> i & 1)) continue;
-                        const uint16_t* from = x.V + (un.token0 + (long long)i) * x.v_stride + un.head * D + d0;
-#pragma unroll
-                        for (int k = 0; k < N; ++k) {
-                            const float y = __uint_as_float((uint32_t)from[k] << 16);
-                            if (!(fabsf(y) < INFINITY)) v[k] += y;
-                        }
-                    }
-                }
-                if (un.slot >= 0) {
-#pragma unroll
-                    for (int k = 0; k < N; k += 2) *reinterpret_cast<float2*>(part + d0 + k) = make_float2(v[k], v[k + 1]);
-                } else {
-                    uint32_t b[N / 2];
-#pragma unroll
-                    for (int k = 0; k < N / 2; ++k) b[k] = pack_bf16(v[2 * k], v[2 * k + 1]);
-                    if constexpr (N == 2) {
-                        *reinterpret_cast<uint32_t*>(out + d0) = b[0];
-                    } else if constexpr (N == 4) {
-                        *reinterpret_cast<uint2*>(out + d0) = make_uint2(b[0], b[1]);
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < N / 2; k += 4) *reinterpret_cast<uint4*>(out + d0 + 2 * k) = make_uint4(b[k], b[k + 1], b[k + 2], b[k + 3]);
-                    }
-                }
-            };
-            constexpr int CW = D / 4;                                          // columns of a round: elements 16 i .. + 15 (and, D = 128, 64 + 16 i .. + 15)
-            auto columns = [&](int i, float f1, float f2, float (&v)[CW]) {
+            // ---- the end of the unit, or of this block's share of it: what the copies of a row have becomes one, in rounds of D / 4 columns by way of shared memory
+            constexpr int CW = D / 4;
+            // (elements 16 i .. 16 i + 15 and, D = 128, 64 + 16 i .. + 15
+            const int parts = un.two ? 1 : 2 << copies;                        // of a row: (w, copy)
+            auto lane_of = [&](int row, int p) { return un.two ? row : (p >> copies) * TA_TILE + (p & ((1 << copies) - 1)) * distinct + row; };
+            ctl->stats[w * TA_TILE + r] = make_float2(m, have ? l : 0.f);
+            if (warp == 0 && lane == 0) ctl->odd = odd;
+            if (!together()) break;
+            float top = -INFINITY, all = 0.f;
+            for (int k = 0; k < parts; ++k) top = fmaxf(top, ctl->stats[lane_of(row, k)].x);
+            const float ref = top == -INFINITY ? 0.f : top;
+            for (int k = 0; k < parts; ++k) {
+                const float2 s = ctl->stats[lane_of(row, k)];
+                all += s.y == 0.f ? 0.f : s.y * ex2_ftz(s.x - ref);
+            }
+            const float f = !have || l == 0.f || all == 0.f ? 0.f : ex2_ftz(m - ref) / all;
+            if (un.slot >= 0 && live) x.stats[(size_t)un.slot * x.part_rows + row] = make_float2(ref, all);    // (the copies of a row write the same)
+            const float f1 = f * pow2i(ev >> 1), f2 = pow2i(ev - (ev >> 1));
+            float* stage = reinterpret_cast<float*>(q_smem + un.buf * C::op_bytes);        // the unit's Q has been used up
+            const int items = un.rows * (CW / 4);
+#pragma unroll 1
+            for (int i = 0; i < 4; ++i) {
                 uint32_t o[CW];
 #pragma unroll
-                for (int g = 0; g < D / 8; ++g) {
-                    if (D == 128) tmem_ld_32x2(t_o + g * 8 + 2 * i, o[8 * (g & 1) + (g >> 1)], o[16 + 8 * (g & 1) + (g >> 1)]);
-                    else tmem_ld_32x2(t_o + g * 8 + 2 * i, o[g], o[8 + g]);
-                }
-                tmem_ld_wait();
+                for (int k = 0; k < CW; ++k) o[k] = 0;
+                if (have) {
 #pragma unroll
-                for (int k = 0; k < CW; ++k) v[k] = f1 == 0.f ? 0.f : __uint_as_float(o[k]) * f1 * f2;
-            };
-            const float half1 = pow2i(ev >> 1), half2 = pow2i(ev - (ev >> 1));
-            if (un.two) {
-                const float inv = l == 0.f ? 0.f : half1 / l;
-                if (un.slot >= 0 && live) x.stats[(size_t)un.slot * x.part_rows + row] = make_float2(m, l);
-                for (int i = 0; i < 4; ++i) {
-                    float v[CW];
-                    columns(i, inv, half2, v);
-                    if (live) {
-                        put(std::integral_constant<int, 16>{}, 16 * i, v);
-                        if constexpr (D == 128) put(std::integral_constant<int, 16>{}, 64 + 16 * i, v + 16);
+                    for (int g = 0; g < D / 8; ++g) {
+                        if (D == 128) tmem_ld_32x2(t_o + g * 8 + 2 * i, o[8 * (g & 1) + (g >> 1)], o[CW / 2 + 8 * (g & 1) + (g >> 1)]);
+                        else tmem_ld_32x2(t_o + g * 8 + 2 * i, o[g], o[8 + g]);
                     }
+                    tmem_ld_wait();
                 }
-            } else {
-                // parts of a row: (w, copy)
-                const int parts = 2 * un.copies, me = w * un.copies + copy;
-                ctl->stats[w * TA_TILE + r] = make_float2(m, have ? l : 0.f);
-                if (warp == 0 && lane == 0) ctl->odd = odd;
+                float* mine_at = stage + (w * TA_TILE + r) * CW;
+#pragma unroll
+                for (int k = 0; k < CW; ++k) mine_at[k ^ (lane & (CW - 1))] = f == 0.f ? 0.f : __uint_as_float(o[k]) * f1 * f2;
                 if (!together()) break;
-                odd = ctl->odd;
-                float top = -INFINITY, all = 0.f;
-                for (int k = 0; k < parts; ++k) top = fmaxf(top, ctl->stats[k / un.copies * TA_TILE + k % un.copies * distinct + r % distinct].x);
-                const float ref = top == -INFINITY ? 0.f : top;
-                for (int k = 0; k < parts; ++k) {
-                    const float2 s = ctl->stats[k / un.copies * TA_TILE + k % un.copies * distinct + r % distinct];
-                    all += s.y == 0.f ? 0.f : s.y * ex2_ftz(s.x - ref);
-                }
-                const float f = !have || l == 0.f ? 0.f : (all == 0.f ? 0.f : ex2_ftz(m - ref) / all);
-                if (un.slot >= 0 && live && me == 0) x.stats[(size_t)un.slot * x.part_rows + row] = make_float2(ref, all);
-                float* stage = reinterpret_cast<float*>(q_smem + un.buf * C::op_bytes);        // the unit's Q has been used up
-                for (int i = 0; i < 4; ++i) {
-                    float v[CW];
-                    if (have) {
-                        columns(i, f * half1, half2, v);
-                    } else {
+#pragma unroll 1
+                for (int item = tid; item < items; item += TA_SOFT * 32) {     // four elements of a row
+                    const int to_row = item / (CW / 4), k0 = item % (CW / 4) * 4, d0 = (D == 128 && k0 >= 16 ? 48 : 0) + 16 * i + k0, at = un.row0 + to_row;
+                    float v[4] = {0.f, 0.f, 0.f, 0.f};
+                    for (int p = 0; p < parts; ++p) {
+                        const int from = lane_of(to_row, p);
 #pragma unroll
-                        for (int k = 0; k < CW; ++k) v[k] = 0.f;
+                        for (int k = 0; k < 4; ++k) v[k] += stage[from * CW + ((k0 + k) ^ (from & (CW - 1)))];
                     }
-                    float* mine_at = stage + (w * TA_TILE + r) * CW;
-#pragma unroll
-                    for (int k = 0; k < CW; ++k) mine_at[k ^ (lane & (CW - 1))] = v[k];
-                    if (!together()) break;
-                    auto collect = [&](auto count) {
-                        constexpr int N = decltype(count)::value;
-                        float s[N];
-#pragma unroll
-                        for (int k = 0; k < N; ++k) s[k] = 0.f;
-                        for (int p = 0; p < parts; ++p) {
-                            const int from = p / un.copies * TA_TILE + p % un.copies * distinct + r % distinct;
-#pragma unroll
-                            for (int k = 0; k < N; ++k) s[k] += stage[from * CW + ((me * N + k) ^ (from & (CW - 1)))];
-                        }
-                        const int k0 = me * N;
-                        if (live) put(count, D == 128 && k0 >= 16 ? 64 + 16 * i + k0 - 16 : 16 * i + k0, s);
-                    };
-                    if (un.copies == 1) collect(std::integral_constant<int, CW / 2>{});
-                    else if (un.copies == 2) collect(std::integral_constant<int, CW / 4>{});
-                    else collect(std::integral_constant<int, CW / 8>{});
-                    if (!together()) break;
+                    if (ctl->odd) {                                            // what the row sees of drafted values that are not finite
+                        const unsigned long long sees = ctl->sees[un.buf][at / x.G];
+                        for (int t = 0; t < un.n; ++t)
+                            for (int k = 0; k < 4; ++k) {
+                                const float y = __uint_as_float((uint32_t)x.V[(un.token0 + (long long)t) * x.v_stride + un.head * D + d0 + k] << 16);
+                                if ((sees >> t & 1) && !(fabsf(y) < INFINITY)) {
+                                    v[0] += k == 0 ? y : 0.f;
+                                    v[1] += k == 1 ? y : 0.f;
+                                    v[2] += k == 2 ? y : 0.f;
+                                    v[3] += k == 3 ? y : 0.f;
+                                }
+                            }
+                    }
+                    if (un.slot >= 0)
+                        *reinterpret_cast<float4*>(x.part + ((size_t)un.slot * x.part_rows + to_row) * D + d0) = make_float4(v[0], v[1], v[2], v[3]);
+                    else
+                        *reinterpret_cast<uint2*>(x.O + (long long)(un.token0 + at / x.G) * x.o_stride + (long long)(un.head * x.G + at % x.G) * D + d0) =
+                            make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
                 }
-                if (!ok) break;
+                if (!together()) break;
             }
+            if (!ok) break;
             tc_fence_before();
             __syncwarp();
             if (lane == 0)
                 for (int b = 0; b < 2; ++b)
                     if (un.two || un.buf == b) mbar_arrive(smem_u32(&ctl->q_empty[b]));
+            leave_unit(u);
         }
         tc_fence_before();
     }
     __syncthreads();
+    if (tid == 0 && *abort_flag) *x.status = AG_ERR_TIMEOUT;
     if (warp == 8) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
 }
 
-// Units that several blocks share: O = sum_c w_c O_c / sum_c w_c, w_c = 2^(m_c - m) l_c.  Block (i, y): rows y, y + gridDim.y, .. of the unit that began in block i of the main
-// kernel and went on beyond it.
+// Units that several blocks share: O = sum_c w_c O_c / sum_c w_c, w_c = 2^(m_c - m) l_c.  Column i of the grid joins the unit that began in block i of the main kernel and
+// went on beyond it, a warp for each of its rows: the lanes weigh the parts side by side, then each adds up its elements of all of them.
+constexpr int TJ_WARPS = 8;
 template <int D>
-__global__ void __launch_bounds__(D) k_attn_tree_join(const TreeArgs x, int blocks) {
+__global__ void __launch_bounds__(TJ_WARPS * 32) k_attn_tree_join(const TreeArgs x, int blocks) {
+    constexpr int E = D / 32;                      // elements of a lane
+    __shared__ float weight[TJ_WARPS][TA_BLOCKS];
+    __shared__ int slot[TJ_WARPS][TA_BLOCKS];
     dep_wait();
     const TreeCross c = x.cross[blockIdx.x];
-    if (c.rows == 0) return;
-    for (int row = blockIdx.y; row < c.rows; row += gridDim.y) {
-        float top = -INFINITY, sum = 0.f, o = 0.f;
-        for (int pass = 0; pass < 2; ++pass) {
-            for (int b = blockIdx.x; b < blocks; ++b) {
-                const int t0 = tiles_before(c.quota * b, c.begin, c.weight, c.tiles), t1 = tiles_before(c.quota * (b + 1), c.begin, c.weight, c.tiles);
-                if (t0 < t1) {
-                    const size_t at = (size_t)(2 * b + (t1 < c.tiles ? 1 : 0)) * x.part_rows + row;
-                    const float2 s = __ldcg(&x.stats[at]);
-                    if (pass == 0) {
-                        if (s.y != 0.f) top = fmaxf(top, s.x);
-                    } else {
-                        const float f = s.y == 0.f ? 0.f : ex2_ftz(s.x - (top == -INFINITY ? 0.f : top)) * s.y, v = __ldcg(&x.part[at * D + threadIdx.x]);
-                        sum += f;
-                        o += f == 0.f && fabsf(v) < INFINITY ? 0.f : f * v;
-                    }
-                }
-                if (t1 >= c.tiles) break;
-            }
-        }
-        const int at = c.row0 + row;
-        x.O[(long long)(c.token0 + at / x.G) * x.o_stride + (long long)(c.head * x.G + at % x.G) * D + threadIdx.x] =
-            __bfloat16_as_ushort(__float2bfloat16_rn(sum == 0.f ? 0.f : o / sum));
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.y * TJ_WARPS + warp;
+    if (row >= c.rows) return;
+    // blocks from this one on, while they have tiles of the unit
+    const int last = (int)min((long long)blocks - 1, (c.begin + (long long)c.weight * c.tiles - 1) / c.quota), n = last - (int)blockIdx.x + 1;
+    float top = -INFINITY;
+    for (int i = lane; i < n; i += 32) {
+        const int b = blockIdx.x + i;
+        const int t0 = tiles_before(c.quota * b, c.begin, c.weight, c.tiles), t1 = tiles_before(c.quota * (b + 1), c.begin, c.weight, c.tiles);
+        const int at = 2 * b + (t1 < c.tiles ? 1 : 0);
+        slot[warp][i] = t0 < t1 ? at : -1;
+        const float2 s = t0 < t1 ? __ldcg(&x.stats[(size_t)at * x.part_rows + row]) : make_float2(-INFINITY, 0.f);
+        weight[warp][i] = s.y;
+        if (s.y != 0.f) top = fmaxf(top, s.x);
     }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const float ref = top == -INFINITY ? 0.f : top;
+    float sum = 0.f;
+    for (int i = lane; i < n; i += 32) {
+        const float l = weight[warp][i];
+        const float f = l == 0.f ? 0.f : l * ex2_ftz(__ldcg(&x.stats[(size_t)slot[warp][i] * x.part_rows + row]).x - ref);
+        weight[warp][i] = f;
+        sum += f;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    __syncwarp();
+    float v[E];
+#pragma unroll
+    for (int k = 0; k < E; ++k) v[k] = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) {
+        const int at = slot[warp][i];
+        if (at < 0) continue;
+        const float f = weight[warp][i];
+        const float* from = x.part + ((size_t)at * x.part_rows + row) * D + lane * E;
+        float u[E];
+        if constexpr (E == 4) {
+            const float4 q = __ldcg(reinterpret_cast<const float4*>(from));
+            u[0] = q.x; u[1] = q.y; u[E - 2] = q.z; u[E - 1] = q.w;
+        } else {
+            const float2 q = __ldcg(reinterpret_cast<const float2*>(from));
+            u[0] = q.x; u[1] = q.y;
+        }
+#pragma unroll
+        for (int k = 0; k < E; ++k) v[k] += f == 0.f && fabsf(u[k]) < INFINITY ? 0.f : f * u[k];
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const int at = c.row0 + row;
+    uint16_t* out = x.O + (long long)(c.token0 + at / x.G) * x.o_stride + (long long)(c.head * x.G + at % x.G) * D + lane * E;
+#pragma unroll
+    for (int k = 0; k < E; k += 2) *reinterpret_cast<uint32_t*>(out + k) = pack_bf16(v[k] * inv, v[k + 1] * inv);
 }
 
 static bool tree_shape_ok(long long n_seq, int max_tokens, int H_q, int H_kv, int D, int max_pages) {
@@ -1110,8 +1068,8 @@ extern "C" ag_status attention_tree_kv4(const ag_tree_attention* a, const ag_kv4
     cfg.numAttrs = 1;
     AG_CUDA(cudaLaunchKernelEx(&cfg, D == 128 ? k_attn_tree_kv4<128> : k_attn_tree_kv4<64>, x));
     count_launch();
-    cfg.gridDim = dim3((unsigned)blocks, 4);
-    cfg.blockDim = dim3((unsigned)D);
+    cfg.gridDim = dim3((unsigned)blocks, (unsigned)((x.part_rows + TJ_WARPS - 1) / TJ_WARPS));
+    cfg.blockDim = dim3(TJ_WARPS * 32);
     cfg.dynamicSmemBytes = 0;
     AG_CUDA(cudaLaunchKernelEx(&cfg, D == 128 ? k_attn_tree_join<128> : k_attn_tree_join<64>, x, blocks));
     count_launch();
