@@ -50,6 +50,7 @@ struct TreeArgs {
     long long q_stride, k_stride, v_stride, o_stride, n_tokens;
     const int32_t *row, *off, *parent, *page_of, *len;
     int H_q, H_kv, G, n_seq, n_rows, max_pages, n_pages, max_tokens, part_rows;
+    uint32_t by_g;                         // 2^32 / G, rounded up (G > 1)
     float scale_log2e;
     int32_t* status;
     struct TreeCross* cross;               // [blocks]: the unit that begins in block i and goes on beyond it
@@ -70,7 +71,7 @@ struct TreeUnit {
     int slot;                              // part slot, -1: the whole unit is here
     int stop, pad;
 };
-struct TreeInfo {
+struct alignas(16) TreeInfo {
     int ek, ev, v0, v1, odd;               // exponents of K and V; keys that count in the tile's halves; a drafted value is not finite
 };
 
@@ -138,9 +139,11 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeArgs& x, int s) {
     r.weight = r.rows / 256 * 2 + (rest > 128 ? 2 : rest > 0 ? 1 : 0);
     return r;
 }
+// token of a request's row (below 4096; G at most 64)
+__device__ __forceinline__ int token_of(const TreeArgs& x, int row) { return x.G == 1 ? row : (int)__umulhi((uint32_t)row, x.by_g); }
 // tiles of the unit at place `begin` of the line that lie in the run [p0, p1)
 __device__ __forceinline__ int tiles_before(long long place, long long begin, int weight, int tiles) {
-    return (int)min(max((place - begin + weight - 1) / weight, 0ll), (long long)tiles);
+    return (int)min(max((place - begin + weight - 1) >> (weight - 1), 0ll), (long long)tiles);      // (weight: 1 or 2)
 }
 
 // A unit's operands are made and used in the order K_0 .. K_{ahead - 1}, V_0 K_ahead V_1 K_{ahead + 1} .., the remaining V.  The place of K_j (which = 0) or V_j (1) among them,
@@ -204,6 +207,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
     // ---- the block's run of the line
     const int per = (x.n_seq + TA_THREADS - 1) / TA_THREADS, s0 = min(tid * per, x.n_seq), s1 = min(s0 + per, x.n_seq);
     long long mine = 0;
+#pragma unroll 1
     for (int s = s0; s < s1; ++s) mine += tree_seq(x, s).line(x.H_kv);
     long long inc = mine;
 #pragma unroll
@@ -214,6 +218,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
     if (lane == 31) ctl->warp_sum[warp] = inc;
     __syncthreads();
     long long before = inc - mine, total = 0;
+#pragma unroll 1
     for (int w = 0; w < TA_THREADS / 32; ++w) {
         if (w < warp) before += ctl->warp_sum[w];
         total += ctl->warp_sum[w];
@@ -256,13 +261,13 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
     auto next_unit = [&](uint32_t u) -> bool { return wait(&ctl->unit_full[u % TA_UNITS], (u / TA_UNITS) & 1) && !ctl->unit[u % TA_UNITS].stop; };
     auto leave_unit = [&](uint32_t u) {
         __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&ctl->unit_empty[u % TA_UNITS]));
+        if (elect_one()) mbar_arrive(smem_u32(&ctl->unit_empty[u % TA_UNITS]));
     };
 
     if (warp >= TA_SOFT) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(TA_REGS_OTHER));
     uint32_t n_tile = 0, n_code = 0;               // tiles, and tiles of codes, before the unit in hand
-    // copies of a unit's pages: K's codes and all pairs (which = 0), V's codes (1)
+    // copies of a unit's pages: warp 9 K's codes and all pairs (which = 0), warp 11 V's codes (1)
     auto copies = [&](int which, const TreeUnit& un) {
         const int nt = un.tile1 - un.tile0, ahead = min(un.two ? 1 : 2, nt), drafts = un.tile0 == 0, len = un.len;
         const uint8_t* heads = x.pages + (size_t)un.head * kv4_head_bytes(D);
@@ -377,6 +382,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                 float top[2] = {0.f, 0.f};
                 int odd = 0;
                 if (un.tile0 + j == 0) {
+#pragma unroll 1
                     for (int i = lane; i < un.n * (D / 8); i += 32) {
                         const long long token = un.token0 + i / (D / 8);
                         const int d = un.head * D + i % (D / 8) * 8;
@@ -393,7 +399,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                         }
                     }
                 } else {
-#pragma unroll
+#pragma unroll 1
                     for (int k = 0; k < 4; ++k) {
                         const int tok = (k & 1) * 32 + lane;
                         if (tok >= (k >> 1 ? v1 : v0)) continue;
@@ -432,7 +438,9 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
         // ------------------------------------------------ copies of values; before them, tokens beyond the most that a request may have
         for (int s = blockIdx.x; s < x.n_seq; s += gridDim.x) {
             const long long first = min(max((long long)x.off[s], 0ll), x.n_tokens), stop = min(max((long long)x.off[s + 1], first), x.n_tokens);
+#pragma unroll 1
             for (long long t = first + x.max_tokens; t < stop; ++t)
+#pragma unroll 1
                 for (int d = lane * 8; d < x.H_q * D; d += 256) *reinterpret_cast<uint4*>(x.O + t * x.o_stride + d) = make_uint4(0, 0, 0, 0);
         }
         for (uint32_t u = 0; next_unit(u); ++u) {
@@ -524,12 +532,13 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
         uint32_t n_op = 0, q_parity = 0;
         auto arrive = [&](uint64_t* b) {
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(b));
+            if (elect_one()) mbar_arrive(smem_u32(b));
         };
         for (uint32_t u = 0; next_unit(u); ++u) {
             const TreeUnit& un = ctl->unit[u % TA_UNITS];
             const int nt = un.tile1 - un.tile0, lead = un.two ? 1 : 2;
             // ---- Q: rows times a power of two that puts their largest element at 2^7
+#pragma unroll 1
             for (int b = 0; b < 2; ++b) {
                 if (!un.two && un.buf != b) continue;
                 if (!wait(&ctl->q_empty[b], (q_parity >> b & 1) ^ 1)) break;
@@ -545,6 +554,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                         jump[k] = p >= 0 && p < i ? p : -1;
                         anc[k] = 1ull << i;
                     }
+#pragma unroll 1
                     for (int step = 0; step < 6; ++step) {
                         unsigned long long more[2];
                         int far[2];
@@ -568,16 +578,17 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                 constexpr int L = D / 8, R = 32 / L;               // lanes of a row, rows of a warp
                 const int unit_row0 = un.two ? b * TA_TILE : 0, rows = min(un.rows - unit_row0, TA_TILE), distinct = TA_TILE >> un.copies;
                 const int c = lane % L;
-                for (int r0 = dwarp * R * 4; r0 < distinct; r0 += TA_DECODERS * R * 4) {
-                    uint4 raw[4];
+#pragma unroll 1
+                for (int r0 = dwarp * R * 2; r0 < distinct; r0 += TA_DECODERS * R * 2) {
+                    uint4 raw[2];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
+                    for (int k = 0; k < 2; ++k) {
                         const int r = r0 + k * R + lane / L, at = un.row0 + unit_row0 + r;
                         raw[k] = make_uint4(0, 0, 0, 0);
-                        if (r < rows) raw[k] = *reinterpret_cast<const uint4*>(x.Q + (long long)(un.token0 + at / x.G) * x.q_stride + (un.head * x.G + at % x.G) * D + c * 8);
+                        if (r < rows) raw[k] = *reinterpret_cast<const uint4*>(x.Q + (long long)(un.token0 + token_of(x, at)) * x.q_stride + (un.head * x.G + at - token_of(x, at) * x.G) * D + c * 8);
                     }
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
+                    for (int k = 0; k < 2; ++k) {
                         const int r = r0 + k * R + lane / L;
                         const uint32_t w[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
                         float v[8], top = 0.f;
@@ -592,6 +603,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                         const float f = pow2i(shift);
                         const uint4 out = make_uint4(pack_f16(v[0] * f, v[4] * f), pack_f16(v[1] * f, v[5] * f), pack_f16(v[2] * f, v[6] * f), pack_f16(v[3] * f, v[7] * f));
                         if (r < distinct) {
+#pragma unroll 1
                             for (int to = r; to < TA_TILE; to += distinct)
                                 *reinterpret_cast<uint4*>(q_smem + b * C::op_bytes + (c >> 3) * (TA_TILE * 128) + to * 128 + (((c ^ to) & 7) << 4)) = out;
                             if (c == 0) ctl->row_scale[b][r] = x.scale_log2e * pow2i(-shift);
@@ -688,7 +700,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                 }
                 fence_proxy_async_smem();
                 __syncwarp();
-                if (lane == 0) {
+                if (elect_one()) {
                     mbar_arrive(smem_u32(&ctl->op_full[op % TA_OPS]));
                     mbar_arrive(smem_u32(&ctl->scales_empty[n % TA_SCALES]));
                 }
@@ -710,12 +722,12 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
         uint32_t n_s = 0, n_tile = 0, n_together = 0;      // score tiles of this slot so far; tiles so far
         auto together = [&]() -> bool {            // a barrier of the softmax warps, with the limit of every wait
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&ctl->together));
+            if (elect_one()) mbar_arrive(smem_u32(&ctl->together));
             return wait(&ctl->together, n_together++ & 1);
         };
         for (uint32_t u = 0; next_unit(u); ++u) {
             const TreeUnit& un = ctl->unit[u % TA_UNITS];
-            const int nt = un.tile1 - un.tile0, step = un.two ? 1 : 2, j0 = un.two ? 0 : w;
+            const int t0 = un.tile0, nt = un.tile1 - t0, step = un.two ? 1 : 2, j0 = un.two ? 0 : w;
             const int copies = un.copies, distinct = TA_TILE >> copies, copy = r >> (7 - copies), row = (un.two ? w * TA_TILE : 0) + (r & (distinct - 1));   // row of the unit
             const bool live = row < un.rows;
             const int buf = un.two ? w : un.buf;
@@ -725,7 +737,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                 if (!wait(&ctl->s_full[w], n_s & 1)) break;
                 tc_fence_after();
                 const TreeInfo f = ctl->info[(n_tile + j) % TA_INFO];
-                const bool drafts = un.tile0 + j == 0;
+                const bool drafts = t0 + j == 0;
                 if (j == j0) rs = ctl->row_scale[buf][r & (distinct - 1)];
                 const float c = fminf(fmaxf(times_pow2(rs, f.ek), 1e-37f), 3e38f);    // (not 0 or infinite: scores at -inf, scores of 0)
                 if (drafts || f.v0 < 64 || f.v1 < 64) {
@@ -733,7 +745,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                     unsigned long long see[2] = {f.v0 >= 64 ? ~0ull : (1ull << f.v0) - 1, f.v1 >= 64 ? ~0ull : (1ull << f.v1) - 1};
                     if (drafts) {
                         odd = f.odd;
-                        see[0] = live ? ctl->sees[buf][(un.row0 + row) / x.G] : 0ull;
+                        see[0] = live ? ctl->sees[buf][token_of(x, un.row0 + row)] : 0ull;
                     }
 #pragma unroll 1
                     for (int b = 0; b < 4; ++b) {
@@ -778,13 +790,16 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                 };
                 f32x2 sum = pack2(0.f, 0.f);
                 const f32x2 c2 = pack2(c, c);
-                // scores from column `at` on, in pieces of 32: their maximum; their probabilities, as fp16 at column `to`
                 auto top_of = [](const uint32_t(&v)[32]) {
-                    float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    float t[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) t[i & 3] = fmaxf(t[i & 3], __uint_as_float(v[i]));
-                    return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+                    for (int i = 0; i < 32; i += 4) {
+                        t[0] = max3(t[0], __uint_as_float(v[i]), __uint_as_float(v[i + 1]));
+                        t[1] = max3(t[1], __uint_as_float(v[i + 2]), __uint_as_float(v[i + 3]));
+                    }
+                    return fmaxf(t[0], t[1]);
                 };
+                // probabilities of 32 scores, as fp16 at column `to`
                 auto exps = [&](const uint32_t(&v)[32], f32x2 ref2, uint32_t to) {
                     uint32_t p[16];
 #pragma unroll
@@ -832,7 +847,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&ctl->p_full[w]));
+                if (elect_one()) mbar_arrive(smem_u32(&ctl->p_full[w]));
             }
             if (!ok) break;
             n_tile += nt;
@@ -850,8 +865,10 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
             if (warp == 0 && lane == 0) ctl->odd = odd;
             if (!together()) break;
             float top = -INFINITY, all = 0.f;
+#pragma unroll 1
             for (int k = 0; k < parts; ++k) top = fmaxf(top, ctl->stats[lane_of(row, k)].x);
             const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll 1
             for (int k = 0; k < parts; ++k) {
                 const float2 s = ctl->stats[lane_of(row, k)];
                 all += s.y == 0.f ? 0.f : s.y * ex2_ftz(s.x - ref);
@@ -880,16 +897,19 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                 if (!together()) break;
 #pragma unroll 1
                 for (int item = tid; item < items; item += TA_SOFT * 32) {     // four elements of a row
-                    const int to_row = item / (CW / 4), k0 = item % (CW / 4) * 4, d0 = (D == 128 && k0 >= 16 ? 48 : 0) + 16 * i + k0, at = un.row0 + to_row;
+                    const int to_row = item / (CW / 4), k0 = item % (CW / 4) * 4, d0 = (D == 128 && k0 >= 16 ? 48 : 0) + 16 * i + k0, at = un.row0 + to_row, token = token_of(x, at);
                     float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
                     for (int p = 0; p < parts; ++p) {
                         const int from = lane_of(to_row, p);
 #pragma unroll
                         for (int k = 0; k < 4; ++k) v[k] += stage[from * CW + ((k0 + k) ^ (from & (CW - 1)))];
                     }
                     if (ctl->odd) {                                            // what the row sees of drafted values that are not finite
-                        const unsigned long long sees = ctl->sees[un.buf][at / x.G];
+                        const unsigned long long sees = ctl->sees[un.buf][token];
+#pragma unroll 1
                         for (int t = 0; t < un.n; ++t)
+#pragma unroll 1
                             for (int k = 0; k < 4; ++k) {
                                 const float y = __uint_as_float((uint32_t)x.V[(un.token0 + (long long)t) * x.v_stride + un.head * D + d0 + k] << 16);
                                 if ((sees >> t & 1) && !(fabsf(y) < INFINITY)) {
@@ -903,7 +923,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                     if (un.slot >= 0)
                         *reinterpret_cast<float4*>(x.part + ((size_t)un.slot * x.part_rows + to_row) * D + d0) = make_float4(v[0], v[1], v[2], v[3]);
                     else
-                        *reinterpret_cast<uint2*>(x.O + (long long)(un.token0 + at / x.G) * x.o_stride + (long long)(un.head * x.G + at % x.G) * D + d0) =
+                        *reinterpret_cast<uint2*>(x.O + (long long)(un.token0 + token) * x.o_stride + (un.head * x.G + at - token * x.G) * D + d0) =
                             make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
                 }
                 if (!together()) break;
@@ -984,8 +1004,8 @@ __global__ void __launch_bounds__(TJ_WARPS * 32) k_attn_tree_join(const TreeArgs
         for (int k = 0; k < E; ++k) v[k] += f == 0.f && fabsf(u[k]) < INFINITY ? 0.f : f * u[k];
     }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    const int at = c.row0 + row;
-    uint16_t* out = x.O + (long long)(c.token0 + at / x.G) * x.o_stride + (long long)(c.head * x.G + at % x.G) * D + lane * E;
+    const int at = c.row0 + row, token = token_of(x, at);
+    uint16_t* out = x.O + (long long)(c.token0 + token) * x.o_stride + (c.head * x.G + at - token * x.G) * D + lane * E;
 #pragma unroll
     for (int k = 0; k < E; k += 2) *reinterpret_cast<uint32_t*>(out + k) = pack_bf16(v[k] * inv, v[k + 1] * inv);
 }
@@ -1045,6 +1065,7 @@ extern "C" ag_status attention_tree_kv4(const ag_tree_attention* a, const ag_kv4
     x.row = a->row; x.off = a->off; x.parent = a->parent; x.page_of = table->page_of; x.len = table->len;
     x.H_q = a->H_q; x.H_kv = H_kv; x.G = a->H_q / H_kv; x.n_seq = a->n_seq; x.n_rows = table->n_rows; x.max_pages = table->max_pages; x.n_pages = (int)pool->n_pages;
     x.max_tokens = a->max_tokens;
+    x.by_g = x.G > 1 ? (uint32_t)((0x100000000ull + x.G - 1) / x.G) : 0;
     x.part_rows = tree_part_rows(a->max_tokens, x.G);
     x.scale_log2e = 1.4426950408889634f * (a->scale > 0.f ? a->scale : 1.f / sqrtf((float)D));
     uint8_t* ws = (uint8_t*)workspace;
