@@ -38,7 +38,8 @@ constexpr int TA_THREADS = 640;
 constexpr int TA_READERS = TA_SOFT + TA_DECODERS + 3;      // warps that read a unit: and MMA, exponents, values' copies
 constexpr int TA_REGS_SOFT = 112, TA_REGS_OTHER = 80;      // 256 x 112 + 384 x 80 <= 640 x 96
 constexpr int TA_BLOCKS = 148;
-constexpr int TA_LEAST = 4;                                // tiles of a block's run, at least
+constexpr int TA_LEAST = 4;                                // places of a block's run, at least
+constexpr int TA_UNIT = 4;                                 // places of the line that a unit takes beside its tiles: Q, drafts, its end
 constexpr float TA_LAZY = 5.f;                             // the reference m of a row moves when its maximum has grown by more than 2^5
 constexpr float TA_SHIFT = 10.f;                           // P is taken times 2^10: at most 2^15, down to 2^-35 of the largest without rounding to zero
 constexpr uint32_t TA_POLLS = 1u << 27;                    // of a barrier that does not come: some seconds
@@ -121,10 +122,10 @@ __device__ __forceinline__ Scale2 scale_pair(uint32_t lo, uint32_t hi, float k24
     return Scale2{pack_f16(s0 * k24, s1 * k24), pack_f16(s0 * k20, s1 * k20), pack_f16(bf16_hi(lo) * k0, bf16_hi(hi) * k0)};
 }
 
-// A request: its drafted tokens, cached tokens and place in the line (for every KV head `per_head` tiles).
+// A request: its drafted tokens, cached tokens and places in the line.
 struct TreeSeq {
     int first, n, rows, len, table_row, tiles, weight;     // weight: of all units of a head, a unit of more than 128 rows counting twice
-    __device__ __forceinline__ long long line(int H_kv) const { return (long long)H_kv * weight * tiles; }
+    __device__ __forceinline__ long long per_head() const { return (long long)weight * tiles + (rows + 255) / 256 * TA_UNIT; }
 };
 __device__ __forceinline__ TreeSeq tree_seq(const TreeArgs& x, int s) {
     TreeSeq r;
@@ -143,7 +144,7 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeArgs& x, int s) {
 __device__ __forceinline__ int token_of(const TreeArgs& x, int row) { return x.G == 1 ? row : (int)__umulhi((uint32_t)row, x.by_g); }
 // tiles of the unit at place `begin` of the line that lie in the run [p0, p1)
 __device__ __forceinline__ int tiles_before(long long place, long long begin, int weight, int tiles) {
-    return (int)min(max((place - begin + weight - 1) >> (weight - 1), 0ll), (long long)tiles);      // (weight: 1 or 2)
+    return (int)min(max((place - begin - TA_UNIT + weight - 1) >> (weight - 1), 0ll), (long long)tiles);      // (weight: 1 or 2)
 }
 
 // A unit's operands are made and used in the order K_0 .. K_{ahead - 1}, V_0 K_ahead V_1 K_{ahead + 1} .., the remaining V.  The place of K_j (which = 0) or V_j (1) among them,
@@ -208,7 +209,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
     const int per = (x.n_seq + TA_THREADS - 1) / TA_THREADS, s0 = min(tid * per, x.n_seq), s1 = min(s0 + per, x.n_seq);
     long long mine = 0;
 #pragma unroll 1
-    for (int s = s0; s < s1; ++s) mine += tree_seq(x, s).line(x.H_kv);
+    for (int s = s0; s < s1; ++s) mine += tree_seq(x, s).per_head() * x.H_kv;
     long long inc = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -229,7 +230,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
         long long at = before;
         int s = s0;
         for (; s < s1; ++s) {
-            const long long l = tree_seq(x, s).line(x.H_kv);
+            const long long l = tree_seq(x, s).per_head() * x.H_kv;
             if (p0 < at + l) break;
             at += l;
         }
@@ -328,12 +329,12 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
         int s = p0 < p1 ? ctl->start_seq : x.n_seq;
         while (ok && s < x.n_seq && at < p1) {
             const TreeSeq q = tree_seq(x, s);
-            const long long line = q.line(x.H_kv), per_head = (long long)q.weight * q.tiles;
+            const long long per_head = q.per_head(), line = per_head * x.H_kv;
             const int units = (q.rows + 255) / 256;
             for (int h = at < p0 && line > 0 ? (int)((p0 - at) / per_head) : 0; ok && h < x.H_kv && line > 0; ++h) {
                 if (at + h * per_head >= p1) break;
                 for (int i = 0; ok && i < units; ++i) {
-                    const long long begin = at + h * per_head + (long long)i * 2 * q.tiles;
+                    const long long begin = at + h * per_head + (long long)i * (2 * q.tiles + TA_UNIT);
                     const int rows = min(q.rows - i * 256, 256), weight = rows > 128 ? 2 : 1;
                     const int t0 = tiles_before(p0, begin, weight, q.tiles), t1 = tiles_before(p1, begin, weight, q.tiles);
                     if (t0 >= t1) continue;
@@ -876,7 +877,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
             const float f = !have || l == 0.f || all == 0.f ? 0.f : ex2_ftz(m - ref) / all;
             if (un.slot >= 0 && live) x.stats[(size_t)un.slot * x.part_rows + row] = make_float2(ref, all);    // (the copies of a row write the same)
             const float f1 = f * pow2i(ev >> 1), f2 = pow2i(ev - (ev >> 1));
-            float* stage = reinterpret_cast<float*>(q_smem + un.buf * C::op_bytes);        // the unit's Q has been used up
+            float4* stage = reinterpret_cast<float4*>(q_smem + un.buf * C::op_bytes);        // the unit's Q has been used up
             const int items = un.rows * (CW / 4);
 #pragma unroll 1
             for (int i = 0; i < 4; ++i) {
@@ -891,9 +892,14 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                     }
                     tmem_ld_wait();
                 }
-                float* mine_at = stage + (w * TA_TILE + r) * CW;
+                float4* mine_at = stage + (w * TA_TILE + r) * (CW / 4);
 #pragma unroll
-                for (int k = 0; k < CW; ++k) mine_at[k ^ (lane & (CW - 1))] = f == 0.f ? 0.f : __uint_as_float(o[k]) * f1 * f2;
+                for (int k = 0; k < CW; k += 4) {
+                    float v[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) v[q] = f == 0.f ? 0.f : __uint_as_float(o[k + q]) * f1 * f2;
+                    mine_at[(k / 4) ^ (lane & (CW / 4 - 1))] = make_float4(v[0], v[1], v[2], v[3]);
+                }
                 if (!together()) break;
 #pragma unroll 1
                 for (int item = tid; item < items; item += TA_SOFT * 32) {     // four elements of a row
@@ -902,8 +908,11 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
 #pragma unroll 1
                     for (int p = 0; p < parts; ++p) {
                         const int from = lane_of(to_row, p);
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) v[k] += stage[from * CW + ((k0 + k) ^ (from & (CW - 1)))];
+                        const float4 y = stage[from * (CW / 4) + ((k0 / 4) ^ (from & (CW / 4 - 1)))];
+                        v[0] += y.x;
+                        v[1] += y.y;
+                        v[2] += y.z;
+                        v[3] += y.w;
                     }
                     if (ctl->odd) {                                            // what the row sees of drafted values that are not finite
                         const unsigned long long sees = ctl->sees[un.buf][token];
@@ -959,7 +968,7 @@ __global__ void __launch_bounds__(TJ_WARPS * 32) k_attn_tree_join(const TreeArgs
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.y * TJ_WARPS + warp;
     if (row >= c.rows) return;
     // blocks from this one on, while they have tiles of the unit
-    const int last = (int)min((long long)blocks - 1, (c.begin + (long long)c.weight * c.tiles - 1) / c.quota), n = last - (int)blockIdx.x + 1;
+    const int last = (int)min((long long)blocks - 1, (c.begin + TA_UNIT + (long long)c.weight * c.tiles - 1) / c.quota), n = last - (int)blockIdx.x + 1;
     float top = -INFINITY;
     for (int i = lane; i < n; i += 32) {
         const int b = blockIdx.x + i;
@@ -1074,7 +1083,7 @@ extern "C" ag_status attention_tree_kv4(const ag_tree_attention* a, const ag_kv4
     x.stats = (float2*)((uint8_t*)x.cross + round256(TA_BLOCKS * sizeof(TreeCross)));
     x.part = (float*)((uint8_t*)x.stats + round256(2 * TA_BLOCKS * (size_t)x.part_rows * sizeof(float2)));
     // no more blocks than there can be runs of TA_LEAST tiles
-    const long long unit_weight = (a->max_tokens * x.G + 127) / 128, most = (long long)a->n_seq * H_kv * unit_weight * ((table->max_pages + 1) / 2 + 1);
+    const long long unit_weight = (a->max_tokens * x.G + 127) / 128, most = (long long)a->n_seq * H_kv * unit_weight * ((table->max_pages + 1) / 2 + 1 + TA_UNIT);
     const int blocks = (int)std::min<long long>(TA_BLOCKS, (most + TA_LEAST - 1) / TA_LEAST);
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
