@@ -12,6 +12,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "kv4.cuh"
 
@@ -46,54 +47,158 @@ __device__ __forceinline__ double peer_double(const double* own, uint32_t rank) 
     asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(a) : "memory");
     return v;
 }
-template <class T>
-__device__ __forceinline__ double entry(const T* row, long long v);
-template <>
-__device__ __forceinline__ double entry<float>(const float* row, long long v) { return (double)row[v]; }
-template <>
-__device__ __forceinline__ double entry<uint16_t>(const uint16_t* row, long long v) { return (double)__uint_as_float((uint32_t)row[v] << 16); }
-
 // The rejected children of the token in hand: r_j = max(r_{j-1} - q_j, 0) / sum_j, q_j = q / left_j without the tokens tried before.
 struct Rejected {
     int n;                                 // of them
+    int kept;                              // some sum was 0: r stayed as it was there
     int tried[VD_MAX];
-    double left[VD_MAX], inv_sum[VD_MAX];  // what is left of q's 1 for child j; 1 / sum_j (0: r stays as it is; 1 for the last one: its scale does not matter)
+    double inv_left[VD_MAX], inv_sum[VD_MAX];  // 1 / what is left of q's 1 for child j; 1 / sum_j (0: r stays; 1 for the last one: its scale does not matter)
 };
-
-// r of entry v after the first `n` rejected children; q: its q entry (drawn) or nothing (not drawn)
+// r of entry v after the first n rejected children, from p's entry and q's
 template <bool DRAWN>
-__device__ __forceinline__ double rest_of(double p, double q, int v, const Rejected& rj, int n, bool distinct) {
+__device__ __noinline__ double rest_of(double p, double q, int v, const Rejected* rj, int n, bool distinct) {
     double r = p;
     bool tried = false;
+#pragma unroll 1
     for (int j = 0; j < n; ++j) {
-        if (DRAWN) {
-            const double d = fmax(r - (tried ? 0.0 : q / rj.left[j]), 0.0);
-            if (rj.inv_sum[j] != 0.0) r = d * rj.inv_sum[j];
-            if (distinct && rj.tried[j] == v) tried = true;
-        } else {
-            if (rj.inv_sum[j] != 0.0) r = rj.tried[j] == v ? 0.0 : r * rj.inv_sum[j];
-        }
+        const double is = rj->inv_sum[j], d = DRAWN ? r - (tried ? 0.0 : q * rj->inv_left[j]) : rj->tried[j] == v ? 0.0 : r;
+        if (is != 0.0) r = (d > 0.0 ? d : 0.0) * is;
+        if (distinct && rj->tried[j] == v) tried = true;
     }
     return r;
 }
 
 struct VerifyShared {
-    int parent[VD_MAX], token[VD_MAX], accepted[VD_MAX];
+    int parent[VD_MAX], token[VD_MAX], accepted[VD_MAX], passes[VD_MAX], more[VD_MAX];   // passes: as its parent's first child; more: siblings behind it
     float u[VD_MAX];
     double p[VD_MAX], q[VD_MAX];           // entries of the tokens in their parents' rows
     Rejected rj;
-    double warp_sum[VD_WARPS], block_sum, scan[VD_WARPS];
+    double tried_q, left;                  // of the child tried last
+    double warp_sum[VD_WARPS], block_sum[2], scan[VD_WARPS];
+    int low[VD_WARPS], high[VD_WARPS];
     int hand, tried_at, state, found;
     double base;
 };
+__device__ __forceinline__ double value_of(float v) { return (double)v; }
+__device__ __forceinline__ double value_of(uint16_t v) { return (double)__uint_as_float((uint32_t)v << 16); }
+// a vector of a row as words; its entry e
+template <class T, int W>
+__device__ __forceinline__ uint4 load_vector(const T* at) {
+    if constexpr (W == 1 && sizeof(T) == 4) return make_uint4(__float_as_uint(*at), 0, 0, 0);
+    else if constexpr (W == 1) return make_uint4(*at, 0, 0, 0);
+    else return *reinterpret_cast<const uint4*>(at);
+}
+template <class T>
+__device__ __forceinline__ double from_word(const uint32_t (&w)[4], int e) {
+    return (double)(sizeof(T) == 4 ? __uint_as_float(w[e % 4]) : e & 1 ? bf16_hi(w[e / 2 % 4]) : bf16_lo(w[e / 2 % 4]));
+}
 
-template <class T, bool DRAWN>
-__global__ void __launch_bounds__(VD_THREADS) k_verify(const VerifyArgs x) {
+// A row in vectors of W entries: vector i has entries i W - lead .. i W - lead + W - 1 and, W > 1, starts on a multiple of 16 bytes in p and in q.
+struct Scan {
+    double sum;                            // of r over the thread's vectors
+    int last, cross;                       // the last entry above 0; the first at which before + sum is above the target; -1: none
+};
+// Vectors i0, i0 + step, .. below i1, of r after m rejected children; FIND: also the last and the first entry of Scan.  (Functions of their own: they are called from
+// several places, and a call that verifies one request is bound by fetching its instructions.)
+template <class T, bool DRAWN, int W, bool FIND>
+__device__ __noinline__ Scan scan_row(const T* p, const T* q, int i0, int i1, int step, int lead, int vocab, const Rejected* rj, int m, bool distinct, double before, double target) {
+    constexpr int U = FIND ? 1 : W == 1 ? 4 : sizeof(T) == 4 ? 2 : 1;      // vectors in flight, of each row
+    Scan s{before, -1, -1};
+    const bool with_q = DRAWN && m > 0, kept = rj->kept != 0;
+    const double il0 = with_q ? rj->inv_left[0] : 0.0;
+    p -= lead;
+    q -= lead;
+#pragma unroll 1
+    for (int i = i0; i < i1; i += U * step) {
+        uint4 pv[U], qv[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const int at = i + k * step, e = at * W - lead;
+            pv[k] = qv[k] = make_uint4(0, 0, 0, 0);
+            if (at < i1 && e >= 0 && e + W <= vocab) {
+                pv[k] = load_vector<T, W>(p + (long long)at * W);
+                if (with_q) qv[k] = load_vector<T, W>(q + (long long)at * W);
+            } else if (at < i1) {                              // a row's ends: entry by entry
+#pragma unroll 1
+                for (int x = 0; x < W; ++x) {
+                    if (e + x < 0 || e + x >= vocab) continue;
+                    const T a = p[(long long)at * W + x], c = with_q ? q[(long long)at * W + x] : T(0);
+                    uint32_t wa, wc;
+                    if constexpr (sizeof(T) == 4) wa = __float_as_uint(a), wc = __float_as_uint(c);
+                    else wa = (uint32_t)a << (16 * (x & 1)), wc = (uint32_t)c << (16 * (x & 1));
+                    const int word = x * (int)sizeof(T) / 4;
+                    (word == 0 ? pv[k].x : word == 1 ? pv[k].y : word == 2 ? pv[k].z : pv[k].w) |= wa;
+                    (word == 0 ? qv[k].x : word == 1 ? qv[k].y : word == 2 ? qv[k].z : qv[k].w) |= wc;
+                }
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const int e0 = (i + k * step) * W - lead;
+            const uint32_t pw[4] = {pv[k].x, pv[k].y, pv[k].z, pv[k].w}, qw[4] = {qv[k].x, qv[k].y, qv[k].z, qv[k].w};
+            double r[W];
+            // (nothing beyond the ends: zeros of p stay zeros)
+            if (DRAWN && !kept) {
+#pragma unroll
+                for (int e = 0; e < W; ++e) {
+                    const double d = from_word<T>(pw, e) - from_word<T>(qw, e) * il0;
+                    r[e] = d > 0.0 ? d : 0.0;
+                }
+#pragma unroll 1
+                for (int j = 1; j < m; ++j) {
+                    const double is = rj->inv_sum[j - 1], il = rj->inv_left[j];
+#pragma unroll
+                    for (int e = 0; e < W; ++e) {
+                        const double d = r[e] * is - from_word<T>(qw, e) * il;
+                        r[e] = d > 0.0 ? d : 0.0;
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < W; ++e) r[e] = from_word<T>(pw, e);
+#pragma unroll 1
+                for (int j = 0; j < m && !DRAWN; ++j) {
+                    const double is = rj->inv_sum[j];
+                    if (is == 0.0) continue;
+#pragma unroll
+                    for (int e = 0; e < W; ++e) r[e] = rj->tried[j] == e0 + e ? 0.0 : r[e] * is;
+                }
+                if (DRAWN) {
+#pragma unroll
+                    for (int e = 0; e < W; ++e) r[e] = rest_of<DRAWN>(r[e], from_word<T>(qw, e), e0 + e, rj, m, distinct);
+                }
+            }
+            double all = r[0];
+#pragma unroll
+            for (int e = 1; e < W; ++e) all += r[e];
+            if (FIND) {
+                double run = s.sum;
+#pragma unroll
+                for (int e = 0; e < W; ++e) {
+                    run += r[e];
+                    if (r[e] > 0.0) {
+                        s.last = e0 + e;
+                        if (s.cross < 0 && run > target) s.cross = e0 + e;
+                    }
+                }
+            }
+            s.sum += all;
+        }
+    }
+    s.sum -= before;
+    return s;
+}
+
+// VEC: rows of p and of q lie alike with respect to 16 bytes
+template <class T, bool DRAWN, bool VEC>
+__global__ void __launch_bounds__(VD_THREADS, 2) k_verify(const VerifyArgs x) {
+    constexpr int W = VEC ? 16 / (int)sizeof(T) : 1;
     __shared__ VerifyShared sh;
     dep_wait();
     dep_release();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = x.cluster > 1 ? (int)cluster_rank() : 0;
     const int seq = blockIdx.x / x.cluster;
+    const bool distinct = x.distinct != 0;
     const long long first = min(max((long long)x.off[seq], 0ll), x.n_tokens), stop = min(max((long long)x.off[seq + 1], first), x.n_tokens);
     const int n = (int)min(stop - first, (long long)VD_MAX);
     const T *P = (const T*)x.P + first * x.p_stride, *Q = (const T*)x.Q + first * x.q_stride;
@@ -103,205 +208,187 @@ __global__ void __launch_bounds__(VD_THREADS) k_verify(const VerifyArgs x) {
         if (rank == 0 && tid == 0) x.next[seq] = -1;
         return;
     }
+    const float u_next = x.u_next[seq];
     if (tid < n) {
         const int parent = x.parent ? x.parent[first + tid] : tid - 1, token = x.token[first + tid];
         const bool fine = tid > 0 && parent >= 0 && parent < tid && token >= 0 && token < x.vocab;
+        const float u = tid > 0 ? x.u[first + tid] : 0.f;
+        const double p = fine ? value_of(P[parent * x.p_stride + token]) : 0.0, q = DRAWN && fine ? value_of(Q[parent * x.q_stride + token]) : 1.0;
         sh.parent[tid] = fine ? parent : -1;
         sh.token[tid] = token;
-        sh.u[tid] = tid > 0 ? x.u[first + tid] : 0.f;
+        sh.u[tid] = u;
         sh.accepted[tid] = tid == 0;
-        sh.p[tid] = fine ? entry(P + parent * x.p_stride, token) : 0.0;
-        sh.q[tid] = DRAWN && fine ? entry(Q + parent * x.q_stride, token) : 1.0;
+        sh.p[tid] = p;
+        sh.q[tid] = q;
+        sh.passes[tid] = fine && (double)u * q < p;
     }
     if (tid == 0) {
         sh.hand = 0;
         sh.tried_at = 1;
-        sh.rj.n = 0;
+        sh.rj.n = sh.rj.kept = 0;
     }
-    // this block's stretch of the vocabulary, and the warp's of it
-    const int per_block = (x.vocab + x.cluster - 1) / x.cluster, b0 = min(rank * per_block, x.vocab), b1 = min(b0 + per_block, x.vocab);
-    const int per_warp = ((b1 - b0 + VD_WARPS - 1) / VD_WARPS + 31) / 32 * 32, w0 = min(b0 + warp * per_warp, b1), w1 = min(w0 + per_warp, b1);
-
-    // sum of r after m rejected children (the last of them not divided yet) over the warp's stretch; all blocks' sum in return
-    auto row_sum = [&](int m) -> double {
-        const T *p = P + sh.hand * x.p_stride, *q = Q + sh.hand * x.q_stride;
-        double sum = 0.0;
-        for (int v = w0 + lane; v < w1; v += 32) sum += rest_of<DRAWN>(entry(p, v), DRAWN && m > 0 ? entry(q, v) : 0.0, v, sh.rj, m, x.distinct != 0);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        __syncthreads();
-        if (lane == 0) sh.warp_sum[warp] = sum;
-        __syncthreads();
-        if (tid == 0) {
-            double all = 0.0;
-            for (int w = 0; w < VD_WARPS; ++w) all += sh.warp_sum[w];
-            sh.block_sum = all;
-        }
-        if (x.cluster == 1) {
-            __syncthreads();
-            return sh.block_sum;
-        }
-        cluster_arrive_wait();
-        double all = 0.0;
-        for (int c = 0; c < x.cluster; ++c) all += peer_double(&sh.block_sum, c);
-        cluster_arrive_wait();                                 // (block_sum has been read by everybody)
-        return all;
-    };
-
-    // ---- the walk: every block of the cluster takes it alike
+    __syncthreads();
+    if (tid < n) {
+        int more = 0;
+#pragma unroll 1
+        for (int k = tid + 1; k < n; ++k) more |= sh.parent[k] == sh.parent[tid];
+        sh.more[tid] = more;
+    }
+    int lead = 0, b0 = 0, b1 = 0, per_warp = 0, sums = 0;
+    double others = 0.0;                                       // lane c: the sum of block c of the cluster
+    double total;
     for (;;) {
         __syncthreads();
+        // ---- the walk: every block of the cluster takes it alike, up to a rejected child with siblings behind it (state 1: the sum of what is left is wanted) or the end
         if (tid == 0) {
-            int state = 0;                                     // 1: a sum is wanted
-            for (int i = sh.tried_at; i < n && !state; ++i) {
-                if (sh.parent[i] != sh.hand) continue;
-                Rejected& rj = sh.rj;
+            int state = 0, hand = sh.hand, i = sh.tried_at;
+            Rejected& rj = sh.rj;
+#pragma unroll 1
+            for (; i < n && !state; ++i) {
+                if (sh.parent[i] != hand) continue;
+                bool stands = sh.passes[i] != 0;
                 const int t = sh.token[i];
-                const double r = rest_of<DRAWN>(sh.p[i], sh.q[i], t, rj, rj.n, x.distinct != 0);
                 double left = 1.0, q = sh.q[i];
-                if (DRAWN && x.distinct) {
-                    if (rj.n) {
-                        // what the child before left, without that child itself
-                        left = rj.left[rj.n - 1];
-                        bool again = false;
-                        for (int j = 0; j + 1 < rj.n; ++j) again |= rj.tried[j] == rj.tried[rj.n - 1];
-                        for (int k = 1; k < n && !again; ++k)
-                            if (sh.parent[k] == sh.hand && sh.token[k] == rj.tried[rj.n - 1]) {
-                                left -= sh.q[k];
-                                again = true;
-                            }
+                if (rj.n) {
+                    if (DRAWN && distinct) {
+                        left = sh.left - sh.tried_q;
+#pragma unroll 1
+                        for (int j = 0; j < rj.n; ++j)
+                            if (rj.tried[j] == t) q = 0.0;
                     }
-                    for (int j = 0; j < rj.n; ++j)
-                        if (rj.tried[j] == t) q = 0.0;
+                    stands = (double)sh.u[i] * (DRAWN ? q / left : 1.0) < rest_of<DRAWN>(sh.p[i], sh.q[i], t, &rj, rj.n, distinct);
                 }
-                if ((double)sh.u[i] * (DRAWN ? q / left : 1.0) < r) {
+                if (stands) {
                     sh.accepted[i] = 1;
-                    sh.hand = i;
-                    rj.n = 0;
+                    hand = i;
+                    rj.n = rj.kept = 0;
                 } else {
                     rj.tried[rj.n] = t;
-                    rj.left[rj.n] = left;
+                    rj.inv_left[rj.n] = 1.0 / left;
                     rj.inv_sum[rj.n] = 1.0;                    // (until the sum is there)
                     ++rj.n;
-                    sh.tried_at = i + 1;
-                    for (int k = i + 1; k < n; ++k)
-                        if (sh.parent[k] == sh.hand) state = 1;
+                    sh.left = left;
+                    sh.tried_q = q;
+                    state = sh.more[i];
+                    if (!state) break;
                 }
             }
+            sh.hand = hand;
+            sh.tried_at = i;
             sh.state = state;
         }
         __syncthreads();
-        if (sh.state == 0) break;
-        const double sum = row_sum(sh.rj.n);
-        if (tid == 0) sh.rj.inv_sum[sh.rj.n - 1] = sum > 0.0 ? 1.0 / sum : 0.0;
+        const int m = sh.rj.n, state = sh.state;
+        // ---- the sum of r: a block has a stretch of the row's vectors, each warp a part of that
+        const T *p = P + sh.hand * x.p_stride, *q = Q + sh.hand * x.q_stride;
+        lead = VEC ? (int)(((uintptr_t)p & 15u) / sizeof(T)) : 0;
+        const int vectors = (x.vocab + lead + W - 1) / W, per_block = (vectors + x.cluster - 1) / x.cluster;
+        b0 = min(rank * per_block, vectors);
+        b1 = min(b0 + per_block, vectors);
+        per_warp = (b1 - b0 + VD_WARPS - 1) / VD_WARPS;
+        const int w0 = min(b0 + warp * per_warp, b1), w1 = min(w0 + per_warp, b1);
+        double sum = scan_row<T, DRAWN, W, false>(p, q, w0 + lane, w1, 32, lead, x.vocab, &sh.rj, m, distinct, 0.0, INFINITY).sum;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (lane == 0) sh.warp_sum[warp] = sum;
+        __syncthreads();
+        double* block_sum = &sh.block_sum[sums++ & 1];         // (two in turn: one barrier a sum)
+        if (warp == 0) {
+            double all = lane < VD_WARPS ? sh.warp_sum[lane] : 0.0;
+#pragma unroll
+            for (int o = VD_WARPS / 2; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+            if (lane == 0) *block_sum = all;
+        }
+        if (x.cluster > 1) cluster_arrive_wait();
+        else __syncthreads();
+        others = lane >= x.cluster ? 0.0 : x.cluster > 1 ? peer_double(block_sum, lane) : *block_sum;
+        total = others;
+#pragma unroll
+        for (int o = 4; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+        total = __shfl_sync(0xffffffffu, total, 0);
+        if (state == 1) {
+            if (tid == 0) {
+                sh.rj.inv_sum[m - 1] = total > 0.0 ? 1.0 / total : 0.0;
+                sh.rj.kept |= !(total > 0.0);
+            }
+        } else if (total == 0.0 && m > 0 && sh.rj.inv_sum[m - 1] != 0.0) {
+            // nothing is left above q: r stays (nobody is left to be tried: the walk ends at once)
+            __syncthreads();
+            if (tid == 0) {
+                sh.rj.inv_sum[m - 1] = 0.0;
+                sh.rj.kept = 1;
+                sh.tried_at = n;
+            }
+        } else {
+            break;
+        }
     }
 
-    // ---- the token that follows
-    const int m = sh.rj.n;
-    double total = row_sum(m);
-    if (total == 0.0 && m > 0 && sh.rj.inv_sum[m - 1] != 0.0) {    // nothing is left above q (the two are equal but for roundings): r stays
-        __syncthreads();
-        if (tid == 0) sh.rj.inv_sum[m - 1] = 0.0;
-        __syncthreads();
-        total = row_sum(m);
-    }
-    const double target = (double)x.u_next[seq] * total;
+    // ---- the token that follows: the block, then the warp's part, then the entry that holds the border - the first whose running sum is above it, or the last with any weight
+    const double target = (double)u_next * total;
     if (rank == 0 && tid < n) x.accepted[first + tid] = sh.accepted[tid];
-    // the block, then the warp's stretch, then the entry that holds the border: the first whose running sum is above it, or the last with any weight
-    if (tid == 0) {
-        double before = 0.0, at = 0.0;
-        int mine = -1, last = -1;
-        double last_before = 0.0;
-        for (int c = 0; c < x.cluster; ++c) {
-            const double s = x.cluster == 1 ? sh.block_sum : peer_double(&sh.block_sum, c);
-            if (mine < 0 && s > 0.0) {
-                last = c;
-                last_before = before;
-                if (before + s > target) {
-                    mine = c;
-                    at = before;
-                }
-            }
-            before += s;
-        }
-        if (mine < 0) {
-            mine = last;
-            at = last_before;
-        }
-        sh.found = -1;
-        if (mine == rank) {
-            int w_last = -1;
-            double w_before = at, l_before = at;
-            sh.found = -2;
-            for (int w = 0; w < VD_WARPS; ++w) {
-                if (sh.warp_sum[w] > 0.0) {
-                    w_last = w;
-                    l_before = w_before;
-                    if (w_before + sh.warp_sum[w] > target) break;
-                }
-                w_before += sh.warp_sum[w];
-            }
-            sh.found = w_last;
-            sh.base = l_before;
-        } else if (mine < 0 && rank == 0) {
-            x.next[seq] = -1;
-        }
-    }
-    if (x.cluster > 1) cluster_arrive_wait();                  // nobody leaves while its sum is still read
-    else __syncthreads();
-    if (sh.found < 0) return;
-    // thread t looks at a run of the found warp's stretch
-    const int s0 = min(b0 + sh.found * per_warp, b1), s1 = min(s0 + per_warp, b1), run = (s1 - s0 + VD_THREADS - 1) / VD_THREADS;
-    const int t0 = min(s0 + tid * run, s1), t1 = min(t0 + run, s1);
-    const T *p = P + sh.hand * x.p_stride, *q = Q + sh.hand * x.q_stride;
-    auto weight = [&](int v) { return rest_of<DRAWN>(entry(p, v), DRAWN && m > 0 ? entry(q, v) : 0.0, v, sh.rj, m, x.distinct != 0); };
-    double sum = 0.0;
-    int last = -1;
-    for (int v = t0; v < t1; ++v) {
-        const double w = weight(v);
-        if (w > 0.0) last = v;
-        sum += w;
-    }
-    double inc = sum;
+    if (warp == 0) {
+        // among `count` sums, lane by lane: the first that takes the running sum above the target, else the last above 0; the running sum in front of it
+        auto choose = [&](double v, double from, double& before) -> int {
+            double inc = v;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const double up = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += up;
-    }
-    if (lane == 31) sh.scan[warp] = inc;
-    __syncthreads();
-    double before = sh.base + inc - sum;
-    for (int w = 0; w < warp; ++w) before += sh.scan[w];
-    // the first thread whose run crosses the border, or the last one with weight
-    int cross = x.vocab, any = -1;
-    if (last >= 0) {
-        any = last;
-        double at = before;
-        for (int v = t0; v < t1; ++v) {
-            const double w = weight(v);
-            at += w;
-            if (w > 0.0 && at > target) {
-                cross = v;
-                break;
+            for (int o = 1; o < 32; o <<= 1) {
+                const double up = __shfl_up_sync(0xffffffffu, inc, o);
+                if (lane >= o) inc += up;
             }
+            const unsigned some = __ballot_sync(0xffffffffu, v > 0.0), above = __ballot_sync(0xffffffffu, v > 0.0 && from + inc > target);
+            const int at = above ? __ffs(above) - 1 : some ? 31 - __clz(some) : -1;
+            before = from + __shfl_sync(0xffffffffu, inc - v, max(at, 0));
+            return at;
+        };
+        double before, base;
+        const int block = choose(others, 0.0, before);
+        int found = -1;
+        if (block == rank) found = choose(lane < VD_WARPS ? sh.warp_sum[lane] : 0.0, before, base);
+        if (lane == 0) {
+            sh.found = found;
+            if (found >= 0) sh.base = base;
+            if (block < 0 && rank == 0) x.next[seq] = -1;
         }
     }
-    cross = __reduce_min_sync(0xffffffffu, cross);
-    any = __reduce_max_sync(0xffffffffu, any);
     __syncthreads();
-    int* lows = reinterpret_cast<int*>(sh.warp_sum);
-    if (lane == 0) {
-        lows[2 * warp] = cross;
-        lows[2 * warp + 1] = any;
-    }
-    __syncthreads();
-    if (tid == 0) {
-        for (int w = 0; w < VD_WARPS; ++w) {
-            cross = min(cross, lows[2 * w]);
-            any = max(any, lows[2 * w + 1]);
+    if (sh.found >= 0) {
+        // thread t looks at a run of the found warp's vectors; then the one whose run holds the border looks for the entry
+        const int m = sh.rj.n;
+        const T *p = P + sh.hand * x.p_stride, *q = Q + sh.hand * x.q_stride;
+        const int s0 = min(b0 + sh.found * per_warp, b1), s1 = min(s0 + per_warp, b1), run = (s1 - s0 + VD_THREADS - 1) / VD_THREADS;
+        const int t0 = min(s0 + tid * run, s1), t1 = min(t0 + run, s1);
+        double before = 0.0;
+        Scan s{0.0, -1, -1};
+#pragma unroll 1
+        for (int pass = 0; pass < 2; ++pass) {
+            if (pass == 0 || (s.sum > 0.0 && before + s.sum > target)) s = scan_row<T, DRAWN, W, true>(p, q, t0, t1, 1, lead, x.vocab, &sh.rj, m, distinct, before, pass ? target : INFINITY);
+            if (pass) break;
+            double inc = s.sum;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const double up = __shfl_up_sync(0xffffffffu, inc, o);
+                if (lane >= o) inc += up;
+            }
+            if (lane == 31) sh.scan[warp] = inc;
+            __syncthreads();
+            before = lane < warp ? sh.scan[lane % VD_WARPS] : 0.0;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
+            before += sh.base + inc - s.sum;
         }
-        x.next[seq] = cross < x.vocab ? cross : any;
+        const int cross = __reduce_min_sync(0xffffffffu, s.cross < 0 ? x.vocab : s.cross), last = __reduce_max_sync(0xffffffffu, s.last);
+        if (lane == 0) {
+            sh.low[warp] = cross;
+            sh.high[warp] = last;
+        }
+        __syncthreads();
+        if (warp == 0) {
+            const int low = __reduce_min_sync(0xffffffffu, sh.low[lane % VD_WARPS]), high = __reduce_max_sync(0xffffffffu, sh.high[lane % VD_WARPS]);
+            if (lane == 0) x.next[seq] = low < x.vocab ? low : high;
+        }
     }
+    if (x.cluster > 1) cluster_arrive_wait();                  // nobody leaves while its sum may still be read
 }
 
 // new_off[s] = accepted tokens in front of request s, from[j] = the j-th accepted token: one block, thread by thread over the tokens
@@ -369,7 +456,14 @@ extern "C" ag_status ag_verify_drafts(const ag_draft_verification* v, void* cuda
     x.cluster = 8;
     while (x.cluster > 1 && (long long)v->n_seq * x.cluster > 2 * 148) x.cluster /= 2;
     if ((long long)v->n_seq * x.cluster > 0x7fffffffll) return AG_ERR_ARG;
-    void (*kernel)(VerifyArgs) = v->type == AG_F32 ? (v->Q ? k_verify<float, true> : k_verify<float, false>) : (v->Q ? k_verify<uint16_t, true> : k_verify<uint16_t, false>);
+    // both models' rows alike with respect to 16 bytes
+    const int64_t size = v->type == AG_F32 ? 4 : 2;
+    const bool vec = !v->Q || (((uintptr_t)v->P - (uintptr_t)v->Q) % 16 == 0 && (v->p_stride - v->q_stride) * size % 16 == 0);
+    auto pick = [&](auto type) {
+        using T = decltype(type);
+        return v->Q ? (vec ? k_verify<T, true, true> : k_verify<T, true, false>) : k_verify<T, false, true>;
+    };
+    void (*kernel)(VerifyArgs) = v->type == AG_F32 ? pick(0.f) : pick((uint16_t)0);
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof cfg);
     cfg.gridDim = dim3((unsigned)(v->n_seq * x.cluster));
