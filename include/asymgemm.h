@@ -622,8 +622,8 @@ ag_status attention_prompt_persistent(const ag_prompt_attention* a, const ag_pla
 /* ---- rotary positions ----------------------------------------------------------------------------------------------------
  * The first `rot` elements of a head are pairs (a, b) that are turned by the angle position * freq of the pair:
  *     a' = bf16(a c - b s),  b' = bf16(b c + a s),   c = float(cos(position * freq) * magnitude),  s = float(sin(...) * magnitude)
- * Angles, cosines and sines are taken in 64 bits (an angle of 10^6 radians is off by 10^-10 then, by 0.06 in 32), c and s are rounded to 32, each product
- * and the sum too.  The elements behind the first `rot` stay as they are.
+ * Angles, cosines and sines are taken in 64 bits (an angle of 10^6 radians is off by 10^-10 then, by 0.06 in 32), c and s are rounded to 32, then
+ * a c (b c), and what a multiply-add with the other product makes of it.  The elements behind the first `rot` stay as they are.
  */
 #define AG_ROTARY_HALVES 0 /* pairs (i, i + rot / 2) */
 #define AG_ROTARY_PAIRS 1  /* pairs (2 i, 2 i + 1) */

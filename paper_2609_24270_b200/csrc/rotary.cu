@@ -8,15 +8,16 @@
 
 namespace ag {
 
-// A warp has one token (or a stretch of its heads): D / 16 lanes hold a row, sixteen elements each, as in the store of the cache, so that a warp takes 4 (D = 128)
-// or 8 rows at a time, and every lane keeps the cosines and sines of its sixteen elements in registers for all heads of the token.  The angles' 64-bit
-// cosines and sines are shared out over the lanes, two each at rot = 128: one in six of the warp's issue slots for 48 heads.
-//   a' = a c - b s,  b' = b c + a s
-// both as own * c + partner * s' (s' = -s for the first of a pair), every product and the sum rounded to 32 bits.  The partner of an element is in the same word
-// ("pairs") or comes from another lane ("halves"), where it lies rot / 16 eight-element chunks away.
+// A warp has one token (or a stretch of its heads): D / 16 lanes hold a row, sixteen elements each, so that a warp takes 4 (D = 128) or 8 rows at a time, and every lane
+// keeps the cosines and sines of its eight pairs in registers for all heads of the token.  The angles' 64-bit cosines and sines are shared out over the lanes.
+//   a' = a c - b s,  b' = b c + a s      a c and b c rounded to 32 bits, the rest by one multiply-add, two at a time
+// "Halves": a lane has the two chunks of eight elements that are turned with one another, rot / 2 apart (the lanes behind those have neighbouring chunks, which stay);
+// "pairs": two neighbouring chunks.  Quantisation wants neighbouring chunks, so keys on their way into the cache are passed from lane to lane once they have been turned.
+// Bound: instructions, 60 for a step of Q (with the chunks of a lane side by side, partners fetched from other lanes and one element at a time they were 320:
+// 16384 tokens x 40 heads took 76 us), then memory.
 constexpr int RO_THREADS = 256;
 constexpr int RO_WARPS = RO_THREADS / 32;
-constexpr int RO_ROWS = 2;                 // steps whose loads are in flight together
+constexpr int RO_ROWS = 4;                 // steps whose loads are in flight together
 
 struct RotaryArgs {
     const uint16_t *Q, *K, *V;
@@ -30,6 +31,22 @@ struct RotaryArgs {
     int H_q, H_kv, rot, pairs;
     int q_steps, k_steps, v_steps, parts;  // steps of 512 / D heads; stretches that a token's steps are cut into
 };
+
+// the lane's pairs (w[0 .. 3] with w[4 .. 7], or the halves of a word) turned
+template <bool PAIRS>
+__device__ __forceinline__ void turn(uint32_t (&w)[8], const f32x2 (&c)[4], const f32x2 (&s)[4], const f32x2 (&minus_s)[4]) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        // four elements of pairs 2 k and 2 k + 1 of the lane: a in x, b in y
+        uint32_t u = w[PAIRS ? 2 * k : k], v = w[PAIRS ? 2 * k + 1 : 4 + k];
+        const f32x2 x = PAIRS ? pack2(bf16_lo(u), bf16_lo(v)) : pack2(bf16_lo(u), bf16_hi(u)), y = PAIRS ? pack2(bf16_hi(u), bf16_hi(v)) : pack2(bf16_lo(v), bf16_hi(v));
+        float a0, a1, b0, b1;
+        unpack2(fma2(y, minus_s[k], mul2(x, c[k])), a0, a1);
+        unpack2(fma2(x, s[k], mul2(y, c[k])), b0, b1);
+        w[PAIRS ? 2 * k : k] = PAIRS ? pack_bf16(a0, b0) : pack_bf16(a0, a1);
+        w[PAIRS ? 2 * k + 1 : 4 + k] = PAIRS ? pack_bf16(a1, b1) : pack_bf16(b0, b1);
+    }
+}
 
 template <int D, bool PAIRS>
 __global__ void __launch_bounds__(RO_THREADS) k_rotary(const RotaryArgs x) {
@@ -45,96 +62,102 @@ __global__ void __launch_bounds__(RO_THREADS) k_rotary(const RotaryArgs x) {
     const long long row = x.from ? x.from[token] : token;
     if (x.from && (row < 0 || row >= x.n_rows)) return;
     const int at = x.slot ? x.slot[token] : -1;
+    uint8_t* page = at >= 0 && at < x.n_slots ? x.pages + (size_t)(at / KV4_PAGE) * x.H_kv * kv4_head_bytes(D) : nullptr;
 
-    uint4 raw[U][2];
-    // step st: its kind (0 Q, 1 K, 2 V) and the lane's head
-    auto kind_of = [&](int st) { return st < x.q_steps ? 0 : st < x.q_steps + x.k_steps ? 1 : 2; };
-    auto head_of = [&](int st, int kind) { return (st - (kind == 0 ? 0 : kind == 1 ? x.q_steps : x.q_steps + x.k_steps)) * ROWS + lane / L; };
-    auto load = [&](int st, uint4 (&to)[2]) {
-        to[0] = to[1] = make_uint4(0, 0, 0, 0);
-        if (st >= end) return;
-        const int kind = kind_of(st), head = head_of(st, kind);
-        if (head >= (kind == 0 ? x.H_q : x.H_kv)) return;
-        const uint16_t* p = (kind == 0 ? x.Q + row * x.q_stride : kind == 1 ? x.K + row * x.k_stride : x.V + row * x.v_stride) + head * D + l * 16;
-        to[0] = reinterpret_cast<const uint4*>(p)[0];
-        to[1] = reinterpret_cast<const uint4*>(p)[1];
+    // the lane's chunks
+    const int o = x.rot / 16;
+    const bool turned = l < o;                                 // (pairs: chunks 2 l and 2 l + 1 of the first 2 o; halves: l and l + o)
+    const int e0 = !PAIRS && turned ? 8 * l : 16 * l, e1 = !PAIRS && turned ? 8 * (l + o) : 16 * l + 8;
+    auto load = [&](const uint16_t* rows, int f0, int f1, int head, int heads, int st, int st_end, uint32_t(&w)[8]) {
+        uint4 a = make_uint4(0, 0, 0, 0), b = a;
+        if (head < heads && st < st_end) {
+            a = *reinterpret_cast<const uint4*>(rows + head * D + f0);
+            b = *reinterpret_cast<const uint4*>(rows + head * D + f1);
+        }
+        w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
+        w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
     };
+    auto store = [&](uint16_t* rows, int head, const uint32_t(&w)[8]) {
+        *reinterpret_cast<uint4*>(rows + head * D + e0) = make_uint4(w[0], w[1], w[2], w[3]);
+        *reinterpret_cast<uint4*>(rows + head * D + e1) = make_uint4(w[4], w[5], w[6], w[7]);
+    };
+    const int q0 = min(first, x.q_steps), q1 = min(end, x.q_steps), k0 = max(first - x.q_steps, 0), k1 = min(end - x.q_steps, x.k_steps);
+    const int v0 = max(first - x.q_steps - x.k_steps, 0), v1 = end - x.q_steps - x.k_steps;
+    const uint16_t *q_rows = x.Q + row * x.q_stride, *k_rows = x.K + row * x.k_stride, *v_rows = x.V + row * x.v_stride;
+    uint32_t w[U][8];
+    if (q0 < q1) {                                             // (on their way while the angles are taken)
 #pragma unroll
-    for (int u = 0; u < U; ++u) load(first + u, raw[u]);
-
-    // the token's cosines and sines, then the lane's own
-    const int half = x.rot / 2, o = x.rot / 16;
-    constexpr int N = PAIRS ? 8 : 16;
-    float c[N], s[N];
+        for (int u = 0; u < U; ++u) load(q_rows, e0, e1, (q0 + u) * ROWS + lane / L, x.H_q, q0 + u, q1, w[u]);
+    }
+    f32x2 c[4], s[4], minus_s[4];
     if (x.rot && first < x.q_steps + x.k_steps) {
         const double pos = (double)x.pos[token];
-        for (int i = lane; i < half; i += 32) {
+        for (int i = lane; i < x.rot / 2; i += 32) {
             double sn, cs;
             sincos(pos * x.freq[i], &sn, &cs);
             turns[warp][i] = make_float2((float)(cs * x.magnitude), (float)(sn * x.magnitude));
         }
         __syncwarp();
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const int e = l * 16 + (PAIRS ? 2 * j : j);
-            const float2 t = turns[warp][e >= x.rot ? 0 : PAIRS ? e >> 1 : e < half ? e : e - half];
-            c[j] = t.x;
-            s[j] = !PAIRS && e < half ? -t.y : t.y;
+        for (int k = 0; k < 4; ++k) {
+            const float2 t0 = turns[warp][turned ? 8 * l + 2 * k : 0], t1 = turns[warp][turned ? 8 * l + 2 * k + 1 : 0];
+            c[k] = pack2(t0.x, t1.x);
+            s[k] = pack2(t0.y, t1.y);
+            minus_s[k] = pack2(-t0.y, -t1.y);
         }
     }
-    for (int st0 = first; st0 < end; st0 += U) {
-        uint32_t in[U][8];
+    for (int st = q0; st < q1; st += U) {
+        if (st > q0) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const uint32_t v[8] = {raw[u][0].x, raw[u][0].y, raw[u][0].z, raw[u][0].w, raw[u][1].x, raw[u][1].y, raw[u][1].z, raw[u][1].w};
-#pragma unroll
-            for (int k = 0; k < 8; ++k) in[u][k] = v[k];
-            load(st0 + U + u, raw[u]);
+            for (int u = 0; u < U; ++u) load(q_rows, e0, e1, (st + u) * ROWS + lane / L, x.H_q, st + u, q1, w[u]);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int st = st0 + u;
-            if (st >= end) break;
-            const int kind = kind_of(st), head = head_of(st, kind);
-            const bool live = head < (kind == 0 ? x.H_q : x.H_kv);
-            if (kind < 2 && x.rot) {
-                if (PAIRS) {
+            const int head = (st + u) * ROWS + lane / L;
+            if (turned) turn<PAIRS>(w[u], c, s, minus_s);
+            if (st + u < q1 && head < x.H_q) store(x.Q_out + token * x.q_out_stride, head, w[u]);
+        }
+    }
+    for (int st = k0; st < k1; st += 2) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float a = bf16_lo(in[u][j]), b = bf16_hi(in[u][j]);
-                        const uint32_t w = pack_bf16(__fsub_rn(__fmul_rn(a, c[j]), __fmul_rn(b, s[j])), __fadd_rn(__fmul_rn(b, c[j]), __fmul_rn(a, s[j])));
-                        if (l * 16 + 2 * j < x.rot) in[u][j] = w;
-                    }
-                } else {
-                    const bool odd = o & 1;
-                    uint32_t other[8];
+        for (int u = 0; u < 2; ++u) load(k_rows, e0, e1, (st + u) * ROWS + lane / L, x.H_kv, st + u, k1, w[u]);
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {                  // chunk 2 l + h; its partner o chunks up or down
-                        const int chunk = 2 * l + h, partner = chunk < o ? chunk + o : chunk < 2 * o ? chunk - o : chunk;
+        for (int u = 0; u < 2; ++u) {
+            const int head = (st + u) * ROWS + lane / L;
+            const bool live = st + u < k1 && head < x.H_kv;
+            if (turned) turn<PAIRS>(w[u], c, s, minus_s);
+            if (x.K_out && live) store(x.K_out + token * x.k_out_stride, head, w[u]);
+            if (!x.pages) continue;
+            uint32_t in[8];
+            if (PAIRS || !x.rot) {
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            other[4 * h + k] = __shfl_sync(0xffffffffu, odd ? in[u][4 * (1 - h) + k] : in[u][4 * h + k], lane - l + (partner >> 1));
-                    }
+                for (int k = 0; k < 8; ++k) in[k] = w[u][k];
+            } else {
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const float a = __fadd_rn(__fmul_rn(bf16_lo(in[u][k]), c[2 * k]), __fmul_rn(bf16_lo(other[k]), s[2 * k]));
-                        const float b = __fadd_rn(__fmul_rn(bf16_hi(in[u][k]), c[2 * k + 1]), __fmul_rn(bf16_hi(other[k]), s[2 * k + 1]));
-                        if (l * 16 + 2 * k < x.rot) in[u][k] = pack_bf16(a, b);
+                for (int h = 0; h < 2; ++h) {                  // chunk 2 l + h is with another lane, as its first chunk or its second
+                    const int chunk = 2 * l + h, from = lane - l + (chunk < o ? chunk : chunk < 2 * o ? chunk - o : chunk >> 1);
+                    const bool second = chunk < 2 * o ? chunk >= o : chunk & 1;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const uint32_t a = __shfl_sync(0xffffffffu, w[u][k], from), b = __shfl_sync(0xffffffffu, w[u][4 + k], from);
+                        in[4 * h + k] = second ? b : a;
                     }
                 }
             }
-            uint16_t* out = kind == 0 ? x.Q_out : kind == 1 ? x.K_out : nullptr;
-            if (out && live) {
-                out += token * (kind == 0 ? x.q_out_stride : x.k_out_stride) + head * D + l * 16;
-                reinterpret_cast<uint4*>(out)[0] = make_uint4(in[u][0], in[u][1], in[u][2], in[u][3]);
-                reinterpret_cast<uint4*>(out)[1] = make_uint4(in[u][4], in[u][5], in[u][6], in[u][7]);
-            }
-            if (kind > 0 && x.pages) {
-                uint32_t w[2];
-                const uint32_t pair = kv4_quantise<D>(in[u], kind - 1, l, w);
-                if (live && at >= 0 && at < x.n_slots)
-                    kv4_put<D>(x.pages + ((size_t)(at / KV4_PAGE) * x.H_kv + head) * kv4_head_bytes(D), kind - 1, at % KV4_PAGE, l, w, pair);
-            }
+            uint32_t codes[2];
+            const uint32_t pair = kv4_quantise<D>(in, 0, l, codes);
+            if (live && page) kv4_put<D>(page + (size_t)head * kv4_head_bytes(D), 0, at % KV4_PAGE, l, codes, pair);
+        }
+    }
+    for (int st = v0; st < v1; st += 2) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) load(v_rows, 16 * l, 16 * l + 8, (st + u) * ROWS + lane / L, x.H_kv, st + u, v1, w[u]);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int head = (st + u) * ROWS + lane / L;
+            uint32_t codes[2];
+            const uint32_t pair = kv4_quantise<D>(w[u], 1, l, codes);
+            if (st + u < v1 && head < x.H_kv && page) kv4_put<D>(page + (size_t)head * kv4_head_bytes(D), 1, at % KV4_PAGE, l, codes, pair);
         }
     }
 }
