@@ -813,10 +813,14 @@ typedef struct {
 } ag_tree_attention;
 /*
  * attention_tree_kv4 - O[i][hq] = softmax(scale q k) v over what token i sees: every token of its request's cached row, its ancestors in the tree, itself.
- * Keys and values of the cache are what ag_kv4_load gives (bf16).  Other drafted tokens have no influence, whatever they hold.
- * Scores, softmax statistics and outputs are accumulated in 32 bits, probabilities are rounded to bf16.  (Values beyond 2^119 / number of keys may overflow.)
+ * Other drafted tokens have no influence, whatever they hold; a value that is not finite leaves the outputs of those that see it not finite.  Roundings, beside the output's own:
+ *   keys, values   s * code + base (of the cache) and the drafted tokens' own enter the products as fp16 under a power of two: off by 2^-11 of themselves, or 2^-19 (values: 2^-17) of the
+ *                  largest |base| + 15 s beside them (keys: of the same 128 tokens; values: of the row's tokens so far)
+ *   queries        exact, or 2^-32 of the row's largest element
+ *   probabilities  2^-11 of themselves, or 2^-35 of the largest;  scores, softmax statistics and outputs are summed in 32 bits
  *   table      lengths are clamped to 0 .. 64 max_pages; tokens whose page is not one of the pool's are left out
- *   workspace  device, 16-byte aligned, ag_attention_tree_kv4_workspace bytes; its contents mean nothing between calls; calls that may run at the same time need one each
+ *   workspace  device, 16-byte aligned, ag_attention_tree_kv4_workspace bytes (at most 39 MB); calls that may run at the same time need one each.  Its first int32 is
+ *              the call's status once it has run (AG_OK, or AG_ERR_TIMEOUT when a bounded wait ran out), the rest means nothing between calls
  * The launch takes every SM of the chip (no plan).  Asynchronous on cuda_stream, may be captured into a graph.  Results are reproducible bit for bit; a request's bits may
  * change with the other requests of its batch.  Errors: AG_ERR_ARG, AG_ERR_UNSUPPORTED_ARCH, AG_ERR_CUDA.
  */

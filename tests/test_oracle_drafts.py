@@ -1,0 +1,101 @@
+"""CPU: the oracle of a drafted step against closed forms, and the host's rotary frequencies against the oracle."""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import drafts, kv4
+from oracle.attention import bf16_to_f64
+from paper_2609_24270_b200 import binding as ag
+
+SCALINGS = [dict(), dict(scaling=ag.AG_ROTARY_LINEAR, factor=4.0), dict(scaling=ag.AG_ROTARY_BANDS, factor=8.0, context=8192.0, low=1.0, high=4.0),
+            dict(scaling=ag.AG_ROTARY_RAMP, factor=16.0, context=4096.0, low=1.0, high=32.0), dict(scaling=ag.AG_ROTARY_RAMP, factor=2.0, context=10.0, low=1.0, high=32.0)]
+
+
+@pytest.mark.parametrize("kw", SCALINGS)
+@pytest.mark.parametrize("rot,base", [(2, 10000.0), (64, 10000.0), (128, 500000.0), (96, 10.0)])
+def test_frequencies(kw, rot, base):
+    got, magnitude = ag.rotary_frequencies(rot, base, **kw)
+    want, m = drafts.frequencies(rot, base, **kw)
+    assert np.allclose(got, want, rtol=1e-13, atol=0) and abs(magnitude - m) < 1e-14
+    assert got[0] <= 1.0 + 1e-12 and (got > 0).all() and (np.diff(got) <= 0).all()
+
+
+def test_frequencies_refused():
+    for bad in (dict(rot=3), dict(rot=0), dict(rot=2048), dict(rot=64, base=1.0), dict(rot=64, base=float("nan")), dict(rot=64, scaling=4), dict(rot=64, scaling=-1),
+                dict(rot=64, scaling=ag.AG_ROTARY_LINEAR, factor=0.5), dict(rot=64, scaling=ag.AG_ROTARY_LINEAR, factor=float("inf")),
+                dict(rot=64, scaling=ag.AG_ROTARY_BANDS, factor=2.0, context=0.0, low=1.0, high=4.0),
+                dict(rot=64, scaling=ag.AG_ROTARY_RAMP, factor=2.0, context=4096.0, low=4.0, high=4.0)):
+        with pytest.raises(ag.AgError) as e:
+            ag.rotary_frequencies(**bad)
+        assert e.value.status == ag.AG_ERR_ARG
+    assert ag.lib().ag_rotary_frequencies(None, None, None) == ag.AG_ERR_ARG
+
+
+@pytest.mark.parametrize("pairs", [False, True])
+def test_a_rotation_keeps_what_a_rotation_keeps(pairs):
+    rng = np.random.default_rng(1)
+    x, y, freq = rng.standard_normal((3, 2, 64)), rng.standard_normal((3, 2, 64)), drafts.frequencies(32)[0]
+    at = np.array([5, 700, -3])
+    rx = drafts.rotate(x, at, freq, pairs=pairs)
+    assert (rx[..., 32:] == x[..., 32:]).all() and np.allclose((rx ** 2).sum(-1), (x ** 2).sum(-1))
+    # products depend on the distance alone
+    one = (rx * drafts.rotate(y, at + 11, freq, pairs=pairs)).sum(-1)
+    two = (drafts.rotate(x, at * 0, freq, pairs=pairs) * drafts.rotate(y, at * 0 + 11, freq, pairs=pairs)).sum(-1)
+    assert np.allclose(one, two)
+    assert np.allclose(drafts.rotate(x, [0, 0, 0], freq, pairs=pairs), x)
+
+
+def test_who_sees_whom():
+    assert (drafts.ancestors(None, 4) == np.tril(np.ones((4, 4), bool))).all()
+    sees = drafts.ancestors([-1, 0, 0, 1, 9, 4], 6)
+    assert [np.flatnonzero(r).tolist() for r in sees] == [[0], [0, 1], [0, 2], [0, 1, 3], [4], [4, 5]]
+
+
+def test_a_tree_of_one_path_is_a_causal_prompt():
+    from oracle import attention as oa
+    rng = np.random.default_rng(2)
+    bits = lambda *s: kv4.bf16_bits(kv4.f32_to_bf16_value(rng.standard_normal(s).astype(np.float32)))  # noqa: E731
+    Q, K, V = bits(7, 4, 64), bits(7, 2, 64), bits(7, 2, 64)
+    past = [(bits(5, 2, 64), bits(5, 2, 64)), (bits(0, 2, 64), bits(0, 2, 64))]
+    cache = lambda r, h: tuple(bf16_to_f64(x[:, h]) for x in past[r])  # noqa: E731
+    got, _, _ = drafts.tree(Q, K, V, cache, [0, 4, 7], None, 2)
+    kk, vv = np.concatenate([past[0][0], K[:4], K[4:]]), np.concatenate([past[0][1], V[:4], V[4:]])
+    want, _ = oa.prompt(Q, kk, vv, [0, 4, 7], [0, 9, 12])
+    assert np.allclose(got, want)
+
+
+def test_verification_by_hand():
+    P = np.array([[.5, .3, .2], [.1, .2, .7], [.4, .4, .2]])
+    Q = np.array([[.2, .6, .2], [.3, .3, .4], [1, 0, 0]])
+    v = lambda tok, u, un, **k: drafts.verify(P, k.pop("Q", Q), [0] + tok, k.pop("parent", None), [0, 3], [0] + u, [un], **k)  # noqa: E731
+    # 1 is accepted while u .6 < .3, then 2 while u .4 < .7
+    a, n, off, rows = v([1, 2], [.49, .99], .5)
+    assert a.tolist() == [1, 1, 1] and n[0] == 1 and off.tolist() == [0, 3] and rows.tolist() == [0, 1, 2]
+    # rejected at once: max(p - q, 0) = .3 0 0
+    a, n, off, rows = v([1, 2], [.51, .0], .999)
+    assert a.tolist() == [1, 0, 0] and n[0] == 0 and off.tolist() == [0, 1] and rows.tolist() == [0, -1, -1]
+    # two siblings: after 1, r = (1, 0, 0); 0 is accepted then whatever u is
+    a, n, _, rows = v([1, 0], [.51, .999], .85, parent=[-1, 0, 0])
+    assert a.tolist() == [1, 0, 1] and rows.tolist() == [0, 2, -1] and n[0] == 2
+    # not drawn: 1 is accepted while u < .3; after that r = (.5, 0, .2) / .7
+    a, n, _, _ = v([1, 2], [.31, .5], .72, Q=None)
+    assert a.tolist() == [1, 0, 0] and n[0] == 2
+
+
+@pytest.mark.parametrize("distinct", [False, True])
+def test_verified_text_has_the_targets_distribution(distinct):
+    """Over all pairs of drafts and a fine grid of random numbers: the first token behind the root is distributed as p."""
+    p, q = np.array([.1, .25, .4, .25]), np.array([.4, .3, .2, .1])
+    got, grid = np.zeros(4), (np.arange(25) + .5) / 25
+    for x in range(4):
+        for y in range(4):
+            w = q[x] * ((q[y] / (1 - q[x]) if y != x else 0) if distinct else q[y])
+            if w == 0:
+                continue
+            for u1 in grid:
+                for u2 in grid:
+                    for un in grid[::6]:
+                        a, n, _, rows = drafts.verify(np.stack([p] * 3), np.stack([q] * 3), [0, x, y], [-1, 0, 0], [0, 3], [0, u1, u2], [un], distinct)
+                        got[[x, y][rows[1] - 1] if rows[1] > 0 else n[0]] += w / 625 / len(grid[::6])
+    assert abs(got.sum() - 1) < 1e-9 and np.abs(got - p).max() < 0.02      # (a grid of 25 steps)
