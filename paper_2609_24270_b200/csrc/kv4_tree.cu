@@ -31,7 +31,9 @@
 namespace ag {
 
 constexpr int TA_TILE = 128;
-constexpr int TA_OPS = 3, TA_CODES = 5, TA_SCALES = 4;     // stages: operands; raw codes; raw (scale, base) pairs
+// stages: operands; raw codes of K and of V, each with one copying warp and one group of decoders (in a ring that both share, one copying warp could come round twice before the other's
+// stage had been read); raw (scale, base) pairs
+constexpr int TA_OPS = 3, TA_KCODES = 3, TA_VCODES = 2, TA_CODES = TA_KCODES + TA_VCODES, TA_SCALES = 4;
 constexpr int TA_INFO = 8, TA_UNITS = 4;
 constexpr int TA_SOFT = 8, TA_DECODERS = 8;                // warps
 constexpr int TA_THREADS = 640;
@@ -147,13 +149,6 @@ __device__ __forceinline__ int tiles_before(long long place, long long begin, in
     return (int)min(max((place - begin - TA_UNIT + weight - 1) >> (weight - 1), 0ll), (long long)tiles);      // (weight: 1 or 2)
 }
 
-// A unit's operands are made and used in the order K_0 .. K_{ahead - 1}, V_0 K_ahead V_1 K_{ahead + 1} .., the remaining V.  The place of K_j (which = 0) or V_j (1) among them,
-// without the drafted tokens' (tile 0), which have no codes, when `drafts` is 1.
-__device__ __forceinline__ int operand_place(int which, int j, int n, int ahead, int drafts) {
-    const int place = which ? (j < n - ahead ? ahead + 2 * j : n + j) : j < ahead ? j : 2 * j - ahead + 1;
-    return place - (drafts ? (place > 0) + (place > ahead) : 0);
-}
-
 template <int D>
 __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs x) {
     using C = TCfg<D>;
@@ -267,10 +262,16 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
 
     if (warp >= TA_SOFT) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(TA_REGS_OTHER));
-    uint32_t n_tile = 0, n_code = 0;               // tiles, and tiles of codes, before the unit in hand
+    uint32_t n_tile = 0, n_code = 0;               // tiles, and tiles with codes, before the unit in hand
+    // the stage of the c-th tile of codes, of K (which = 0) or V, and its turn's parity
+    auto code_stage_of = [&](int which, uint32_t c, uint32_t& parity) -> uint32_t {
+        const uint32_t turn = which ? c / TA_VCODES : c / TA_KCODES;
+        parity = turn & 1;
+        return which ? TA_KCODES + c - turn * TA_VCODES : c - turn * TA_KCODES;
+    };
     // copies of a unit's pages: warp 9 K's codes and all pairs (which = 0), warp 11 V's codes (1)
     auto copies = [&](int which, const TreeUnit& un) {
-        const int nt = un.tile1 - un.tile0, ahead = min(un.two ? 1 : 2, nt), drafts = un.tile0 == 0, len = un.len;
+        const int nt = un.tile1 - un.tile0, drafts = un.tile0 == 0, len = un.len;
         const uint8_t* heads = x.pages + (size_t)un.head * kv4_head_bytes(D);
         const int32_t* pages = x.page_of + (size_t)max(un.table_row, 0) * x.max_pages;
         int window = -1, page = -1;                // pages of 16 tiles in the lanes: lane l has page 32 window + l of the row
@@ -292,13 +293,14 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                 window = c >> 5;
                 page = window * 32 + lane < (len + 63) / 64 ? pages[window * 32 + lane] : -1;
             }
-            const uint32_t code = n_code + operand_place(which, j, nt, ahead, drafts);
-            if (!wait(&ctl->codes_empty[code % TA_CODES], ((code / TA_CODES) & 1) ^ 1)) return;
+            uint32_t turn;
+            const uint32_t stage = code_stage_of(which, n_code + j - drafts, turn);
+            if (!wait(&ctl->codes_empty[stage], turn ^ 1)) return;
             const int id0 = __shfl_sync(0xffffffffu, page, c & 31), id1 = __shfl_sync(0xffffffffu, page, (c + 1) & 31);
             const int v0 = id0 >= 0 && id0 < x.n_pages ? min(max(len - 64 * c, 0), 64) : 0, v1 = id1 >= 0 && id1 < x.n_pages ? min(max(len - 64 * c - 64, 0), 64) : 0;
             if (elect_one()) {
-                const uint32_t bar = smem_u32(&ctl->codes_full[code % TA_CODES]), sbar = smem_u32(&ctl->scales_full[n % TA_SCALES]);
-                const uint32_t to = smem_u32(code_smem + (code % TA_CODES) * C::code_bytes), sto = smem_u32(scale_smem + (n % TA_SCALES) * C::scale_bytes);
+                const uint32_t bar = smem_u32(&ctl->codes_full[stage]), sbar = smem_u32(&ctl->scales_full[n % TA_SCALES]);
+                const uint32_t to = smem_u32(code_smem + stage * C::code_bytes), sto = smem_u32(scale_smem + (n % TA_SCALES) * C::scale_bytes);
                 const int there = (v0 > 0) + (v1 > 0);
                 const uint8_t *p0 = heads + (size_t)max(id0, 0) * x.H_kv * kv4_head_bytes(D), *p1 = heads + (size_t)max(id1, 0) * x.H_kv * kv4_head_bytes(D);
                 if (which == 0) {
@@ -315,7 +317,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
             __syncwarp();
         }
         n_tile += nt;
-        n_code += 2 * (nt - drafts);
+        n_code += nt - drafts;
     };
     // gave up: linger (bounded) so that copies already in flight land before the block leaves
     auto linger = [&] {
@@ -529,7 +531,12 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
     } else {
         // ------------------------------------------------ decoders: Q, the drafted tokens and the cache's codes as operands
         const int dt = tid - 12 * 32, dwarp = warp - 12;
-        const int token = dt & 127, which = dt >> 7, page = token >> 6, tk = token & 63, sw = token & 7;
+        const int token = dt & 127, which = __shfl_sync(0xffffffffu, dt >> 7, 0), page = token >> 6, tk = token & 63, sw = token & 7;
+        // Where the thread's codes are read and its operands written: K's run t (chunks t, 4 + t ..), V's words of elements 16 i' + 8 j' + h (chunks 2 h and 2 h + 1, or h), each with
+        // t or h turned by the token so that neighbouring lanes meet no bank twice.  Operand row: chunk c at (c / 8) 16 KB + 128 row + 16 ((c ^ row) mod 8).
+        const int turn = which == 0 ? (tk >> (D == 128 ? 1 : 2)) & 3 : D == 128 ? (tk >> 3) & 1 : (tk >> 3) & 3;
+        const int src = page * 32 * D + (which == 0 ? tk * (D / 2) + turn * (D / 8) : (tk >> 3) * 4 * D + ((tk >> 1) & 3) * (D / 8) + (tk & 1) * (D / 16) + turn * (D / 2));
+        const int dst = token * 128 + (((which && D == 128 ? 2 * turn : turn) ^ sw) & 7) * 16;
         uint32_t n_op = 0, q_parity = 0;
         auto arrive = [&](uint64_t* b) {
             __syncwarp();
@@ -617,15 +624,22 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
             if (!ok) break;
             // ---- operands: warps 12-15 make K's, warps 16-19 V's; thread = token of the tile
             const int ahead = min(lead, nt), drafts = un.tile0 == 0;
+            // the place among the unit's operands, which are made and used in the order K_0 .. K_{ahead - 1}, V_0 K_ahead V_1 K_{ahead + 1} .., the remaining V
+            int place = which ? ahead : 0;
 #pragma unroll 1
             for (int j = 0; j < nt; ++j) {
                 const uint32_t n = n_tile + j;
-                const uint32_t op = n_op + operand_place(which, j, nt, ahead, 0), code = n_code + operand_place(which, j, nt, ahead, drafts);
+                // the operand's stage, and the place of its codes
+                if (j > 0) place += which ? (j <= nt - ahead ? 2 : 1) : (j < ahead ? 1 : 2);
+                const uint32_t op = n_op + place, stage = op % TA_OPS, op_parity = (op / TA_OPS & 1) ^ 1;
+                uint32_t code_parity;
+                const uint32_t code_stage = code_stage_of(which, n_code + j - drafts, code_parity);
                 if (!wait(&ctl->scales_ready[n % TA_SCALES], (n / TA_SCALES) & 1)) break;
                 const TreeInfo& f = ctl->info[n % TA_INFO];
                 const int e = which ? f.ev : f.ek;
-                uint8_t* to = op_smem + op % TA_OPS * C::op_bytes + token * 128;       // operand row: chunk c at (c / 8) 16 KB + 128 row + 16 ((c ^ row) mod 8)
-                if (j > 0 || !drafts) {
+                uint8_t* to = op_smem + stage * C::op_bytes;
+                const bool coded = j > 0 || !drafts;
+                if (coded) {
                     uint32_t pair[NG];
                     const uint8_t* sc = scale_smem + (n % TA_SCALES) * C::scale_bytes + page * 16 * D + which * 8 * D + tk * 4 * NG;
                     if (D == 128) *reinterpret_cast<uint4*>(pair) = *reinterpret_cast<const uint4*>(sc);
@@ -635,53 +649,49 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                         for (int g = 0; g < NG; ++g) pair[g] = 0;
                     }
                     const float k24 = pow2i(24 - e);
-                    const uint8_t* codes = code_smem + (code % TA_CODES) * C::code_bytes + page * 32 * D;
+                    const uint8_t* codes = code_smem + code_stage * C::code_bytes;
                     if (which == 0) {
                         Scale2 g[NG];
 #pragma unroll
                         for (int k = 0; k < NG; ++k) g[k] = scale_pair(pair[k], pair[k], k24);
-                        if (!wait(&ctl->codes_full[code % TA_CODES], (code / TA_CODES) & 1) || !wait(&ctl->op_empty[op % TA_OPS], ((op / TA_OPS) & 1) ^ 1)) break;
-                        const int turn = (tk >> (D == 128 ? 1 : 2)) & 3;               // (neighbouring lanes at different runs: no bank twice)
+                        if (!wait(&ctl->codes_full[code_stage], code_parity) || !wait(&ctl->op_empty[stage], op_parity)) break;
 #pragma unroll 1
-                        for (int t0 = 0; t0 < 4; ++t0) {
-                            const int t = t0 ^ turn;
+                        for (int t = 0; t < 4; ++t) {                                  // (t ^ turn: exclusive ors of the addresses' bits)
+                            uint8_t *p = to + (dst ^ t * 16), *q = to + (dst ^ t * 16 ^ 64);
                             if (D == 128) {
-                                const uint4 w = *reinterpret_cast<const uint4*>(codes + tk * 64 + t * 16);
-                                uint8_t *p = to + ((t ^ sw) << 4), *q = to + (((t ^ 4) ^ sw) << 4);      // chunks t, 4 + t, 8 + t, 12 + t
+                                const uint4 w = *reinterpret_cast<const uint4*>(codes + (src ^ t * 16));
                                 *reinterpret_cast<uint4*>(p) = decode_word(w.x, g[0], g[0]);
                                 *reinterpret_cast<uint4*>(q) = decode_word(w.y, g[1], g[1]);
                                 *reinterpret_cast<uint4*>(p + TA_TILE * 128) = decode_word(w.z, g[NG - 2], g[NG - 2]);
                                 *reinterpret_cast<uint4*>(q + TA_TILE * 128) = decode_word(w.w, g[NG - 1], g[NG - 1]);
                             } else {
-                                const uint2 w = *reinterpret_cast<const uint2*>(codes + tk * 32 + t * 8);
-                                *reinterpret_cast<uint4*>(to + ((t ^ sw) << 4)) = decode_word(w.x, g[0], g[0]);
-                                *reinterpret_cast<uint4*>(to + (((t ^ 4) ^ sw) << 4)) = decode_word(w.y, g[1], g[1]);
+                                const uint2 w = *reinterpret_cast<const uint2*>(codes + (src ^ t * 8));
+                                *reinterpret_cast<uint4*>(p) = decode_word(w.x, g[0], g[0]);
+                                *reinterpret_cast<uint4*>(q) = decode_word(w.y, g[1], g[1]);
                             }
                         }
                     } else {
                         const Scale2 a = D == 128 ? scale_pair(pair[0], pair[NG / 2], k24) : scale_pair(pair[0], pair[0], k24);
                         const Scale2 b = D == 128 ? scale_pair(pair[1], pair[NG - 1], k24) : scale_pair(pair[1], pair[1], k24);
-                        if (!wait(&ctl->codes_full[code % TA_CODES], (code / TA_CODES) & 1) || !wait(&ctl->op_empty[op % TA_OPS], ((op / TA_OPS) & 1) ^ 1)) break;
-                        const uint8_t* from = codes + (tk >> 3) * 4 * D + ((tk >> 1) & 3) * (D / 8) + (tk & 1) * (D / 16);
-                        const int turn = D == 128 ? (tk >> 3) & 1 : (tk >> 3) & 3;
+                        if (!wait(&ctl->codes_full[code_stage], code_parity) || !wait(&ctl->op_empty[stage], op_parity)) break;
 #pragma unroll 1
-                        for (int i = 0; i < 8; ++i) {
-                            const int h = i ^ turn;                                    // element 16 i' + 8 j' + h of the token
+                        for (int h = 0; h < 4; ++h) {
+                            uint8_t *p = to + (dst ^ h * (D == 128 ? 32 : 16)), *q = to + (dst ^ (D == 128 ? h * 32 ^ 16 : h * 16 ^ 64));
+                            const uint8_t* from = codes + (src ^ h * (D / 2));
                             if (D == 128) {
-                                const uint2 w = *reinterpret_cast<const uint2*>(from + h * 64);
-                                uint8_t* p = to + (h >> 2) * (TA_TILE * 128);          // chunks 2 h and 2 h + 1
-                                const int c = ((2 * h) ^ sw) & 7;
-                                *reinterpret_cast<uint4*>(p + c * 16) = decode_word(w.x, a, b);
-                                *reinterpret_cast<uint4*>(p + (c ^ 1) * 16) = decode_word(w.y, a, b);
+                                const uint2 w = *reinterpret_cast<const uint2*>(from), y = *reinterpret_cast<const uint2*>(from + 2 * D);
+                                *reinterpret_cast<uint4*>(p) = decode_word(w.x, a, b);
+                                *reinterpret_cast<uint4*>(q) = decode_word(w.y, a, b);
+                                *reinterpret_cast<uint4*>(p + TA_TILE * 128) = decode_word(y.x, a, b);
+                                *reinterpret_cast<uint4*>(q + TA_TILE * 128) = decode_word(y.y, a, b);
                             } else {
-                                const uint32_t w = *reinterpret_cast<const uint32_t*>(from + h * 32);
-                                *reinterpret_cast<uint4*>(to + ((h ^ sw) << 4)) = decode_word(w, a, b);
+                                *reinterpret_cast<uint4*>(p) = decode_word(*reinterpret_cast<const uint32_t*>(from), a, b);
+                                *reinterpret_cast<uint4*>(q) = decode_word(*reinterpret_cast<const uint32_t*>(from + 2 * D), a, b);
                             }
                         }
                     }
-                    arrive(&ctl->codes_empty[code % TA_CODES]);
                 } else {
-                    if (!wait(&ctl->op_empty[op % TA_OPS], ((op / TA_OPS) & 1) ^ 1)) break;
+                    if (!wait(&ctl->op_empty[stage], op_parity)) break;
                     // drafted tokens: rows of up to 64, the others are zeros
                     const float k0 = times_pow2(1.f, -e);
                     const uint16_t* from = (which ? x.V + (un.token0 + (long long)token) * x.v_stride : x.K + (un.token0 + (long long)token) * x.k_stride) + un.head * D;
@@ -695,21 +705,22 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                             v[k] = token < un.n ? __uint_as_float((uint32_t)from[d] << 16) * k0 : 0.f;
                             if (which && !(fabsf(v[k]) < INFINITY)) v[k] = 0.f;            // put back at the end, for the rows that see it
                         }
-                        *reinterpret_cast<uint4*>(to + (c >> 3) * (TA_TILE * 128) + (((c ^ token) & 7) << 4)) =
+                        *reinterpret_cast<uint4*>(to + token * 128 + (c >> 3) * (TA_TILE * 128) + (((c ^ token) & 7) << 4)) =
                             make_uint4(pack_f16(v[0], v[1]), pack_f16(v[2], v[3]), pack_f16(v[4], v[5]), pack_f16(v[6], v[7]));
                     }
                 }
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (elect_one()) {
-                    mbar_arrive(smem_u32(&ctl->op_full[op % TA_OPS]));
+                    mbar_arrive(smem_u32(&ctl->op_full[stage]));
                     mbar_arrive(smem_u32(&ctl->scales_empty[n % TA_SCALES]));
+                    if (coded) mbar_arrive(smem_u32(&ctl->codes_empty[code_stage]));
                 }
                 __syncwarp();
             }
             if (!ok) break;
             n_op += 2 * nt;
-            n_code += 2 * (nt - drafts);
+            n_code += nt - drafts;
             n_tile += nt;
             leave_unit(u);
         }
@@ -761,79 +772,72 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                     }
                     tmem_st_wait();
                 }
-                // the reference, once the tile's largest score is known; outputs so far follow it
-                auto refer = [&](float raw_top) -> bool {
-                    const float top = raw_top * c;
+                // This copy's blocks of 32 keys, one after the other: where a row's maximum has grown too far beyond the reference (or V's exponent has), what there is follows.
+                const int blocks = 4 >> copies, b0 = copy * blocks;
+                const f32x2 c2 = pack2(c, c);
+                f32x2 sum = pack2(0.f, 0.f);
+                if (j == j0) ev = f.ev;
+#pragma unroll 1
+                for (int b = b0; b < b0 + blocks; ++b) {
+                    uint32_t v[32];
+                    tmem_ld_32x32(t_s + 32 * b, v);
+                    tmem_ld_wait();
+                    float t0 = -INFINITY, t1 = -INFINITY;
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4) {
+                        t0 = max3(t0, __uint_as_float(v[i]), __uint_as_float(v[i + 1]));
+                        t1 = max3(t1, __uint_as_float(v[i + 2]), __uint_as_float(v[i + 3]));
+                    }
+                    const float top = fmaxf(t0, t1) * c;
                     const bool grow = top > m && !(top - m <= TA_LAZY);
-                    if (j == j0) {
-                        m = top;
-                        ev = f.ev;
-                    } else if (__any_sync(0xffffffffu, grow) || ev != f.ev) {
-                        if (!wait(&ctl->pv_done[w], (n_s - 1) & 1)) return false;
-                        tc_fence_after();
+                    if (__any_sync(0xffffffffu, grow) || ev != f.ev) {
                         const float g = !grow ? 1.f : m == -INFINITY ? 0.f : ex2_ftz(m - top);
                         if (grow) m = top;
                         l *= g;
-                        const float go = ev == f.ev ? g : ev - f.ev < -126 ? 0.f : g * pow2i(min(ev - f.ev, 127));
-                        ev = f.ev;
+                        sum = mul2(sum, pack2(g, g));
+                        if (j != j0) {                                         // the outputs, once the last product has landed
+                            if (!wait(&ctl->pv_done[w], (n_s - 1) & 1)) break;
+                            tc_fence_after();
+                            const float go = ev == f.ev ? g : ev - f.ev < -126 ? 0.f : g * pow2i(min(ev - f.ev, 127));
 #pragma unroll 1
-                        for (int d = 0; d < D; d += 32) {
-                            uint32_t ov[32];
-                            tmem_ld_32x32(t_o + d, ov);
+                            for (int d = 0; d < D; d += 16) {
+                                uint32_t ov[16];
+                                tmem_ld_32x16(t_o + d, ov);
+                                tmem_ld_wait();
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) ov[i] = __float_as_uint(__uint_as_float(ov[i]) * go);
+                                tmem_st_32x16(t_o + d, ov);
+                            }
+                        }
+                        ev = f.ev;
+                        const uint32_t g2 = pack_f16(g, g);
+#pragma unroll 1
+                        for (int e = b0; e < b; ++e) {                         // this tile's probabilities so far
+                            uint32_t q[16];
+                            tmem_st_wait();
+                            tmem_ld_32x16(t_s + 64 * (e >> 1) + 16 * (e & 1), q);
                             tmem_ld_wait();
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) ov[i] = __float_as_uint(__uint_as_float(ov[i]) * go);
-                            tmem_st_32x32(t_o + d, ov);
+                            for (int i = 0; i < 16; ++i) q[i] = mul_f16x2(q[i], g2);
+                            tmem_st_32x16(t_s + 64 * (e >> 1) + 16 * (e & 1), q);
                         }
                         tmem_st_wait();
                     }
-                    return true;
-                };
-                f32x2 sum = pack2(0.f, 0.f);
-                const f32x2 c2 = pack2(c, c);
-                auto top_of = [](const uint32_t(&v)[32]) {
-                    float t[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-                    for (int i = 0; i < 32; i += 4) {
-                        t[0] = max3(t[0], __uint_as_float(v[i]), __uint_as_float(v[i + 1]));
-                        t[1] = max3(t[1], __uint_as_float(v[i + 2]), __uint_as_float(v[i + 3]));
-                    }
-                    return fmaxf(t[0], t[1]);
-                };
-                // probabilities of 32 scores, as fp16 at column `to`
-                auto exps = [&](const uint32_t(&v)[32], f32x2 ref2, uint32_t to) {
+                    const float ref = (m == -INFINITY ? 0.f : -m) + TA_SHIFT;
+                    const f32x2 ref2 = pack2(ref, ref);
                     uint32_t p[16];
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        float a, b;
-                        unpack2(fma2(pack2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), c2, ref2), a, b);
-                        a = ex2_ftz(a);
-                        b = ex2_ftz(b);
-                        sum = add2(sum, pack2(a, b));
-                        p[i] = pack_f16(a, b);
+                        float x0, x1;
+                        unpack2(fma2(pack2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), c2, ref2), x0, x1);
+                        x0 = ex2_ftz(x0);
+                        x1 = ex2_ftz(x1);
+                        sum = add2(sum, pack2(x0, x1));
+                        p[i] = pack_f16(x0, x1);
                     }
-                    tmem_st_32x16(to, p);
-                };
-                // this copy's blocks of 32 keys
-                const int blocks = 4 >> copies, b0 = copy * blocks;
-                uint32_t v[32];
-                float top = -INFINITY;
-#pragma unroll 1
-                for (int b = b0 + blocks - 1; b >= b0; --b) {
-                    tmem_ld_32x32(t_s + 32 * b, v);
-                    tmem_ld_wait();
-                    top = fmaxf(top, top_of(v));
+                    tmem_st_32x16(t_s + 64 * (b >> 1) + 16 * (b & 1), p);      // (over scores that have been read: block 0's lie there, or block 2's)
                 }
-                if (!refer(top)) break;
-                const float ref = (m == -INFINITY ? 0.f : -m) + TA_SHIFT;
-                const f32x2 ref2 = pack2(ref, ref);
-#pragma unroll 1
-                for (int b = b0;;) {
-                    exps(v, ref2, t_s + 64 * (b >> 1) + 16 * (b & 1));         // (over scores that have been read: block 0's lie there, or block 2's)
-                    if (++b == b0 + blocks) break;
-                    tmem_ld_32x32(t_s + 32 * b, v);
-                    tmem_ld_wait();
-                }
+                if (!ok) break;
                 if (copies) {
                     uint32_t zero[16];
 #pragma unroll
