@@ -40,19 +40,20 @@ constexpr int TA_THREADS = 640;
 constexpr int TA_READERS = TA_SOFT + TA_DECODERS + 3;      // warps that read a unit: and MMA, exponents, values' copies
 constexpr int TA_REGS_SOFT = 112, TA_REGS_OTHER = 80;      // 256 x 112 + 384 x 80 <= 640 x 96
 constexpr int TA_BLOCKS = 148;
-constexpr int TA_LEAST = 4;                                // places of a block's run, at least
-constexpr int TA_UNIT = 4;                                 // places of the line that a unit takes beside its tiles: Q, drafts, its end
+// places of the line that a unit takes beside its tiles: Q, drafts, its end.  None where every tile can have a block of its own, since then the longest run counts, not the sum
+// (with it, a short request's tiles would be handled one after the other by a few blocks)
+constexpr int TA_UNIT = 4;
 constexpr float TA_LAZY = 5.f;                             // the reference m of a row moves when its maximum has grown by more than 2^5
 constexpr float TA_SHIFT = 10.f;                           // P is taken times 2^10: at most 2^15, down to 2^-35 of the largest without rounding to zero
-constexpr uint32_t TA_POLLS = 1u << 27;                    // of a barrier that does not come: some seconds
+constexpr uint32_t TA_POLLS = 1u << 26;                    // of a barrier that does not come: some seconds
 
 struct TreeArgs {
     const uint16_t *Q, *K, *V;
     uint16_t* O;
     const uint8_t* pages;
-    long long q_stride, k_stride, v_stride, o_stride, n_tokens;
+    long long q_stride, k_stride, v_stride, o_stride;
     const int32_t *row, *off, *parent, *page_of, *len;
-    int H_q, H_kv, G, n_seq, n_rows, max_pages, n_pages, max_tokens, part_rows;
+    int H_q, H_kv, G, n_seq, n_rows, max_pages, n_pages, n_tokens, max_tokens, most_len, part_rows;
     uint32_t by_g;                         // 2^32 / G, rounded up (G > 1)
     float scale_log2e;
     int32_t* status;
@@ -62,7 +63,7 @@ struct TreeArgs {
 };
 struct TreeCross {
     long long begin, quota;                // place of the unit's first tile in the line; tiles of a run
-    int weight, tiles, token0, row0, rows, head, pad[2];
+    int weight, tiles, token0, row0, rows, head, unit_places, pad;
 };
 
 struct TreeUnit {
@@ -88,10 +89,10 @@ struct TreeCtl {
     TreeUnit unit[TA_UNITS];
     TreeInfo info[TA_INFO];
     int valid[TA_INFO][2];
-    long long warp_sum[TA_THREADS / 32];
+    long long warp_sum[TA_THREADS / 32][2];
     long long total, start_before;
     uint32_t tmem_base;
-    int abort_flag, start_seq, odd;
+    int abort_flag, start_seq, odd, ev[TA_SOFT];
 };
 
 template <int D>
@@ -124,29 +125,35 @@ __device__ __forceinline__ Scale2 scale_pair(uint32_t lo, uint32_t hi, float k24
     return Scale2{pack_f16(s0 * k24, s1 * k24), pack_f16(s0 * k20, s1 * k20), pack_f16(bf16_hi(lo) * k0, bf16_hi(hi) * k0)};
 }
 
+__device__ __forceinline__ float odd_part(float v) { return fabsf(v) < INFINITY ? 0.f : v; }
+
 // A request: its drafted tokens, cached tokens and places in the line.
 struct TreeSeq {
     int first, n, rows, len, table_row, tiles, weight;     // weight: of all units of a head, a unit of more than 128 rows counting twice
-    __device__ __forceinline__ long long per_head() const { return (long long)weight * tiles + (rows + 255) / 256 * TA_UNIT; }
+    __device__ __forceinline__ int units() const { return (rows + 255) / 256; }
+    __device__ __forceinline__ int per_head(int unit_places) const { return weight * tiles + units() * unit_places; }     // (below 2^30)
 };
 __device__ __forceinline__ TreeSeq tree_seq(const TreeArgs& x, int s) {
     TreeSeq r;
-    const long long first = min(max((long long)x.off[s], 0ll), x.n_tokens), stop = min(max((long long)x.off[s + 1], first), x.n_tokens);
-    r.first = (int)first;
-    r.n = (int)min(stop - first, (long long)x.max_tokens);
+    const int first = min(max(x.off[s], 0), x.n_tokens), stop = min(max(x.off[s + 1], first), x.n_tokens);
+    r.first = first;
+    r.n = min(stop - first, x.max_tokens);
     r.rows = r.n * x.G;
     r.table_row = x.row ? x.row[s] : s;
-    r.len = r.table_row >= 0 && r.table_row < x.n_rows ? (int)min((long long)max(x.len[r.table_row], 0), 64ll * x.max_pages) : 0;
-    r.tiles = (r.len + TA_TILE - 1) / TA_TILE + 1;
+    r.len = r.table_row >= 0 && r.table_row < x.n_rows ? min(max(x.len[r.table_row], 0), x.most_len) : 0;
+    r.tiles = (int)((r.len + (TA_TILE - 1u)) / TA_TILE) + 1;
     const int rest = r.rows % 256;
     r.weight = r.rows / 256 * 2 + (rest > 128 ? 2 : rest > 0 ? 1 : 0);
     return r;
 }
+// a / b, without the division of 64 bits where the numbers are small (some 600 cycles, and most of a small call's first 3 us are like these)
+__device__ __forceinline__ long long quotient(long long a, long long b) { return (a | b) >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b); }
 // token of a request's row (below 4096; G at most 64)
 __device__ __forceinline__ int token_of(const TreeArgs& x, int row) { return x.G == 1 ? row : (int)__umulhi((uint32_t)row, x.by_g); }
-// tiles of the unit at place `begin` of the line that lie in the run [p0, p1)
-__device__ __forceinline__ int tiles_before(long long place, long long begin, int weight, int tiles) {
-    return (int)min(max((place - begin - TA_UNIT + weight - 1) >> (weight - 1), 0ll), (long long)tiles);      // (weight: 1 or 2)
+// tiles of the unit at place `begin` of the line that lie in front of `place`
+__device__ __forceinline__ int tiles_before(long long place, long long begin, int unit_places, int weight, int tiles) {
+    const int d = (int)min(max(place - begin, 0ll), 1ll << 30);
+    return min(max((d - unit_places + weight - 1) >> (weight - 1), 0), tiles);      // (weight: 1 or 2)
 }
 
 template <int D>
@@ -161,7 +168,6 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
     uint8_t* scale_smem = code_smem + TA_CODES * C::code_bytes;
     TreeCtl* ctl = reinterpret_cast<TreeCtl*>(scale_smem + TA_SCALES * C::scale_bytes);
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;      // (from one lane: known to be the same for the warp)
-    volatile int* abort_flag = &ctl->abort_flag;
 
     if (tid == 0) {
         ctl->abort_flag = 0;
@@ -202,30 +208,50 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
 
     // ---- the block's run of the line
     const int per = (x.n_seq + TA_THREADS - 1) / TA_THREADS, s0 = min(tid * per, x.n_seq), s1 = min(s0 + per, x.n_seq);
-    long long mine = 0;
+    long long mine = 0, mine_units = 0;            // places of tiles, units
 #pragma unroll 1
-    for (int s = s0; s < s1; ++s) mine += tree_seq(x, s).per_head() * x.H_kv;
-    long long inc = mine;
+    for (int s = s0; s < s1; ++s) {
+        const TreeSeq q = tree_seq(x, s);
+        mine += (long long)q.per_head(0) * x.H_kv;
+        mine_units += (long long)q.units() * x.H_kv;
+    }
+    long long inc = mine, inc_units = mine_units;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const long long up = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += up;
+        const long long up = __shfl_up_sync(0xffffffffu, inc, o), up_units = __shfl_up_sync(0xffffffffu, inc_units, o);
+        if (lane >= o) {
+            inc += up;
+            inc_units += up_units;
+        }
     }
-    if (lane == 31) ctl->warp_sum[warp] = inc;
+    if (lane == 31) {
+        ctl->warp_sum[warp][0] = inc;
+        ctl->warp_sum[warp][1] = inc_units;
+    }
     __syncthreads();
-    long long before = inc - mine, total = 0;
+    long long before = inc - mine, total = 0, before_units = inc_units - mine_units, total_units = 0;
 #pragma unroll 1
-    for (int w = 0; w < TA_THREADS / 32; ++w) {
-        if (w < warp) before += ctl->warp_sum[w];
-        total += ctl->warp_sum[w];
+    for (int w = 0; w < (min(x.n_seq, TA_THREADS) + 31) / 32; ++w) {           // (the other warps have no request)
+        const long long a = ctl->warp_sum[w][0], b = ctl->warp_sum[w][1];
+        if (w < warp) {
+            before += a;
+            before_units += b;
+        }
+        total += a;
+        total_units += b;
     }
-    const long long quota = max((total + gridDim.x - 1) / gridDim.x, (long long)TA_LEAST);
+    const int unit_places = total <= (long long)gridDim.x ? 0 : TA_UNIT;
+    total += total_units * unit_places;
+    before += before_units * unit_places;
+    mine += mine_units * unit_places;
+    const long long quota = max(quotient(total + gridDim.x - 1, gridDim.x), 1ll);
     const long long p0 = min(quota * blockIdx.x, total), p1 = min(p0 + quota, total);
     if (p0 < p1 && before <= p0 && p0 < before + mine) {
         long long at = before;
         int s = s0;
+#pragma unroll 1
         for (; s < s1; ++s) {
-            const long long l = tree_seq(x, s).per_head() * x.H_kv;
+            const long long l = (long long)tree_seq(x, s).per_head(unit_places) * x.H_kv;
             if (p0 < at + l) break;
             at += l;
         }
@@ -241,16 +267,9 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
     tc_fence_after();
     const uint32_t tmem = ctl->tmem_base;
     bool ok = true;
-    // Every wait is bounded.  (Few instructions: there are some forty of them, and twenty warps in eight roles share the instruction caches.)
+    // Every wait is bounded.  (Few instructions: there are some thirty of them, and twenty warps in eight roles share the instruction caches.)
     auto wait = [&](uint64_t* b, uint32_t parity) -> bool {
-        const uint32_t bar = smem_u32(b);
-        bool there = ok;
-        for (uint32_t polls = 0; there && !mbar_try_wait(bar, parity); ++polls)
-            if (polls > TA_POLLS || *abort_flag) {
-                *abort_flag = 1;
-                there = false;
-            }
-        ok = __all_sync(0xffffffffu, there);
+        ok = __all_sync(0xffffffffu, mbar_wait_polls(smem_u32(b), parity, ok ? TA_POLLS : 1u));
         return ok;
     };
     // unit u, which stays where it is until every reader has left it
@@ -329,16 +348,20 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
         uint32_t u = 0, toggle = 0;
         long long at = ctl->start_before;
         int s = p0 < p1 ? ctl->start_seq : x.n_seq;
+#pragma unroll 1
         while (ok && s < x.n_seq && at < p1) {
             const TreeSeq q = tree_seq(x, s);
-            const long long per_head = q.per_head(), line = per_head * x.H_kv;
-            const int units = (q.rows + 255) / 256;
-            for (int h = at < p0 && line > 0 ? (int)((p0 - at) / per_head) : 0; ok && h < x.H_kv && line > 0; ++h) {
-                if (at + h * per_head >= p1) break;
+            const long long line = (long long)q.per_head(unit_places) * x.H_kv;
+            const int per_head = q.per_head(unit_places);
+            const int units = q.units();
+#pragma unroll 1
+            for (int h = at < p0 && line > 0 ? (int)quotient(p0 - at, per_head) : 0; ok && h < x.H_kv && line > 0; ++h) {
+                if (at + (long long)h * per_head >= p1) break;
+#pragma unroll 1
                 for (int i = 0; ok && i < units; ++i) {
-                    const long long begin = at + h * per_head + (long long)i * (2 * q.tiles + TA_UNIT);
+                    const long long begin = at + (long long)h * per_head + i * (2 * q.tiles + unit_places);
                     const int rows = min(q.rows - i * 256, 256), weight = rows > 128 ? 2 : 1;
-                    const int t0 = tiles_before(p0, begin, weight, q.tiles), t1 = tiles_before(p1, begin, weight, q.tiles);
+                    const int t0 = tiles_before(p0, begin, unit_places, weight, q.tiles), t1 = tiles_before(p1, begin, unit_places, weight, q.tiles);
                     if (t0 >= t1) continue;
                     if (!wait(&ctl->unit_empty[u % TA_UNITS], ((u / TA_UNITS) & 1) ^ 1)) break;
                     const int two = rows > 128, buf = two ? 0 : (int)(toggle & 1);
@@ -354,7 +377,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                         if (t0 == 0 && t1 < q.tiles) {
                             TreeCross c;
                             c.begin = begin; c.quota = quota; c.weight = weight; c.tiles = q.tiles; c.token0 = q.first; c.row0 = i * 256; c.rows = rows; c.head = h;
-                            c.pad[0] = c.pad[1] = 0;
+                            c.unit_places = unit_places; c.pad = 0;
                             x.cross[blockIdx.x] = c;
                         }
                     }
@@ -375,9 +398,11 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
         if (!ok && lane == 0) linger();
     } else if (warp == 10) {
         // ------------------------------------------------ exponents of the tiles
+#pragma unroll 1
         for (uint32_t u = 0; next_unit(u); ++u) {
             const TreeUnit& un = ctl->unit[u % TA_UNITS];
             int ev = 1000;                                         // none yet
+#pragma unroll 1
             for (int j = 0; j < un.tile1 - un.tile0; ++j) {
                 const uint32_t n = n_tile + j;
                 if (!wait(&ctl->scales_full[n % TA_SCALES], (n / TA_SCALES) & 1)) break;
@@ -385,19 +410,35 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                 float top[2] = {0.f, 0.f};
                 int odd = 0;
                 if (un.tile0 + j == 0) {
+                    // the largest magnitudes by their bits, two elements of a word side by side; four pieces of 16 bytes of K and of V in flight
+                    uint32_t most[2] = {0, 0};
+                    const int pieces = un.n * (D / 8);
 #pragma unroll 1
-                    for (int i = lane; i < un.n * (D / 8); i += 32) {
-                        const long long token = un.token0 + i / (D / 8);
-                        const int d = un.head * D + i % (D / 8) * 8;
-                        const uint4 raw[2] = {*reinterpret_cast<const uint4*>(x.K + token * x.k_stride + d), *reinterpret_cast<const uint4*>(x.V + token * x.v_stride + d)};
+                    for (int i0 = lane; i0 < pieces; i0 += 128) {
+                        uint4 raw[8];
 #pragma unroll
-                        for (int which = 0; which < 2; ++which) {
-                            const uint32_t w[4] = {raw[which].x, raw[which].y, raw[which].z, raw[which].w};
+                        for (int q = 0; q < 4; ++q) {
+                            const int i = i0 + 32 * q < pieces ? i0 + 32 * q : i0, d = un.head * D + i % (D / 8) * 8;
+                            raw[q] = *reinterpret_cast<const uint4*>(x.K + (un.token0 + (long long)(i / (D / 8))) * x.k_stride + d);
+                            raw[4 + q] = *reinterpret_cast<const uint4*>(x.V + (un.token0 + (long long)(i / (D / 8))) * x.v_stride + d);
+                        }
 #pragma unroll
-                            for (int k = 0; k < 8; ++k) {
-                                const float v = fabsf(k & 1 ? bf16_hi(w[k >> 1]) : bf16_lo(w[k >> 1]));
-                                if (v < INFINITY) top[which] = fmaxf(top[which], v);
-                                else odd |= which;
+                        for (int q = 0; q < 8; ++q) {
+                            most[q >> 2] = __vmaxu2(most[q >> 2], __vmaxu2(__vmaxu2(raw[q].x & 0x7fff7fffu, raw[q].y & 0x7fff7fffu), __vmaxu2(raw[q].z & 0x7fff7fffu, raw[q].w & 0x7fff7fffu)));
+                        }
+                    }
+#pragma unroll
+                    for (int which = 0; which < 2; ++which) {
+                        const uint32_t bits = max(most[which] & 0xffffu, most[which] >> 16);
+                        top[which] = __uint_as_float(bits << 16);
+                        if (__any_sync(0xffffffffu, bits >= 0x7f80u)) {            // some are not finite: the largest of the others
+                            odd |= which;
+                            top[which] = 0.f;
+                            const uint16_t* rows = (which ? x.V + (long long)un.token0 * x.v_stride : x.K + (long long)un.token0 * x.k_stride) + un.head * D;
+#pragma unroll 1
+                            for (int i = lane; i < un.n * D; i += 32) {
+                                const float v = __uint_as_float((uint32_t)rows[i / D * (which ? x.v_stride : x.k_stride) + i % D] << 16);
+                                if (fabsf(v) < INFINITY) top[which] = fmaxf(top[which], fabsf(v));
                             }
                         }
                     }
@@ -439,13 +480,15 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
         }
     } else if (warp == 11) {
         // ------------------------------------------------ copies of values; before them, tokens beyond the most that a request may have
+#pragma unroll 1
         for (int s = blockIdx.x; s < x.n_seq; s += gridDim.x) {
-            const long long first = min(max((long long)x.off[s], 0ll), x.n_tokens), stop = min(max((long long)x.off[s + 1], first), x.n_tokens);
+            const int first = min(max(x.off[s], 0), x.n_tokens), stop = min(max(x.off[s + 1], first), x.n_tokens);
 #pragma unroll 1
-            for (long long t = first + x.max_tokens; t < stop; ++t)
+            for (int t = first + x.max_tokens; t < stop; ++t)
 #pragma unroll 1
-                for (int d = lane * 8; d < x.H_q * D; d += 256) *reinterpret_cast<uint4*>(x.O + t * x.o_stride + d) = make_uint4(0, 0, 0, 0);
+                for (int d = lane * 8; d < x.H_q * D; d += 256) *reinterpret_cast<uint4*>(x.O + (long long)t * x.o_stride + d) = make_uint4(0, 0, 0, 0);
         }
+#pragma unroll 1
         for (uint32_t u = 0; next_unit(u); ++u) {
             copies(1, ctl->unit[u % TA_UNITS]);
             if (!ok) break;
@@ -463,6 +506,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
             if (elect_one()) tc_commit(smem_u32(b));
             __syncwarp();
         };
+#pragma unroll 1
         for (uint32_t u = 0; next_unit(u); ++u) {
             const TreeUnit& un = ctl->unit[u % TA_UNITS];
             const int nt = __shfl_sync(0xffffffffu, un.tile1 - un.tile0, 0), two = __shfl_sync(0xffffffffu, un.two, 0), buf = __shfl_sync(0xffffffffu, un.buf, 0), lead = two ? 1 : 2;
@@ -486,7 +530,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                         if (!wait(&ctl->p_full[w], p_parity >> w & 1)) break;
                         p_parity ^= 1u << w;
                         tc_fence_after();
-                        const uint64_t dv = dv_t | (uint64_t)((op_base + nv % TA_OPS * C::op_bytes) >> 4);
+                        const uint64_t dv = dv_t | (uint64_t)__shfl_sync(0xffffffffu, (op_base + nv % TA_OPS * C::op_bytes) >> 4, 0);
                         const uint32_t first = j < lead ? 0u : 1u, d = tmem + 256 + w * D, p = tmem + w * TA_TILE;
                         if (elect_one()) {
 #pragma unroll
@@ -499,7 +543,8 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                     if (qk) {
                         if (w == w0 && !wait(&ctl->op_full[nk % TA_OPS], (nk / TA_OPS) & 1)) break;
                         tc_fence_after();
-                        const uint64_t dq = dk_t | (uint64_t)((q_base + (two ? w : buf) * C::op_bytes) >> 4), dk = dk_t | (uint64_t)((op_base + nk % TA_OPS * C::op_bytes) >> 4);
+                        const uint64_t dq = dk_t | (uint64_t)__shfl_sync(0xffffffffu, (q_base + (two ? w : buf) * C::op_bytes) >> 4, 0);
+                        const uint64_t dk = dk_t | (uint64_t)__shfl_sync(0xffffffffu, (op_base + nk % TA_OPS * C::op_bytes) >> 4, 0);
                         if (elect_one()) {
 #pragma unroll
                             for (int k = 0; k < D / 16; ++k)
@@ -519,7 +564,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
             leave_unit(u);
         }
         __syncwarp();
-        if (*abort_flag) {
+        if (!ok) {
             // let issued MMAs retire before tensor memory is released
             if (elect_one()) {
                 tc_commit(smem_u32(&ctl->drain));
@@ -542,6 +587,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
             __syncwarp();
             if (elect_one()) mbar_arrive(smem_u32(b));
         };
+#pragma unroll 1
         for (uint32_t u = 0; next_unit(u); ++u) {
             const TreeUnit& un = ctl->unit[u % TA_UNITS];
             const int nt = un.tile1 - un.tile0, lead = un.two ? 1 : 2;
@@ -551,7 +597,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                 if (!un.two && un.buf != b) continue;
                 if (!wait(&ctl->q_empty[b], (q_parity >> b & 1) ^ 1)) break;
                 q_parity ^= 1u << b;
-                if (dwarp == 0) {
+                if (dwarp == TA_DECODERS - 1) {
                     // who sees whom among the drafted tokens: paths to the root by doubling, two tokens a lane
                     unsigned long long anc[2];
                     int jump[2];
@@ -563,7 +609,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                         anc[k] = 1ull << i;
                     }
 #pragma unroll 1
-                    for (int step = 0; step < 6; ++step) {
+                    while (__any_sync(0xffffffffu, jump[0] >= 0 || jump[1] >= 0)) {    // (a parent is in front of its child: six times at most)
                         unsigned long long more[2];
                         int far[2];
 #pragma unroll
@@ -692,21 +738,42 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                     }
                 } else {
                     if (!wait(&ctl->op_empty[stage], op_parity)) break;
-                    // drafted tokens: rows of up to 64, the others are zeros
+                    // drafted tokens: 16 bytes of a row at a time, neighbouring threads at neighbouring ones; values' rows behind them are zeros
                     const float k0 = times_pow2(1.f, -e);
-                    const uint16_t* from = (which ? x.V + (un.token0 + (long long)token) * x.v_stride : x.K + (un.token0 + (long long)token) * x.k_stride) + un.head * D;
+                    const uint16_t* rows = which ? x.V + (long long)un.token0 * x.v_stride + un.head * D : x.K + (long long)un.token0 * x.k_stride + un.head * D;
+                    const long long stride = which ? x.v_stride : x.k_stride;
+                    constexpr int CH = D / 8;
 #pragma unroll 1
-                    for (int c = 0; c < D / 8; ++c) {
-                        float v[8];
+                    for (int i = token; i < un.n * CH; i += TA_TILE) {
+                        const int t = i / CH, c = i % CH;
+                        const uint4 raw = *reinterpret_cast<const uint4*>(rows + t * stride + c * 8);
+                        const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+                        uint8_t* line = to + t * 128;
+                        if (which == 0) {                                              // elements (0, 4, 1, 5, ..) of the chunk
+                            uint32_t h[4];
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            // K: elements 8 c + (0, 4, 1, 5, ..); V: column 8 c + k is element 16 (k / 2 + 4 (k mod 2)) + 8 (c mod 2) + c / 2, D = 64: 16 (k / 2) + 8 (k mod 2) + c
-                            const int d = which == 0 ? 8 * c + (k >> 1) + 4 * (k & 1) : D == 128 ? 16 * ((k >> 1) + 4 * (k & 1)) + 8 * (c & 1) + (c >> 1) : 16 * (k >> 1) + 8 * (k & 1) + c;
-                            v[k] = token < un.n ? __uint_as_float((uint32_t)from[d] << 16) * k0 : 0.f;
-                            if (which && !(fabsf(v[k]) < INFINITY)) v[k] = 0.f;            // put back at the end, for the rows that see it
+                            for (int k = 0; k < 4; ++k) {
+                                const uint32_t u = w[k >> 1], v = w[2 + (k >> 1)];
+                                h[k] = pack_f16((k & 1 ? bf16_hi(u) : bf16_lo(u)) * k0, (k & 1 ? bf16_hi(v) : bf16_lo(v)) * k0);
+                            }
+                            *reinterpret_cast<uint4*>(line + (c >> 3) * (TA_TILE * 128) + (((c ^ t) & 7) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+                        } else {
+                            // element 16 i' + 8 j' + g is place 2 (i' mod 4) + i' / 4 of chunk 2 g + j', D = 64: place 2 i' + j' of chunk g
+                            const int place = D == 128 ? 2 * ((c >> 1) & 3) + (c >> 3) : 2 * (c >> 1) + (c & 1);
+#pragma unroll
+                            for (int g = 0; g < 8; ++g) {
+                                const float v = (g & 1 ? bf16_hi(w[g >> 1]) : bf16_lo(w[g >> 1])) * k0;
+                                const int chunk = D == 128 ? 2 * g + (c & 1) : g;
+                                // (what is not finite is put back at the end, for the rows that see it)
+                                *reinterpret_cast<uint16_t*>(line + (chunk >> 3) * (TA_TILE * 128) + (((chunk ^ t) & 7) << 4) + 2 * place) =
+                                    (uint16_t)pack_f16(fabsf(v) < INFINITY ? v : 0.f, 0.f);
+                            }
                         }
-                        *reinterpret_cast<uint4*>(to + token * 128 + (c >> 3) * (TA_TILE * 128) + (((c ^ token) & 7) << 4)) =
-                            make_uint4(pack_f16(v[0], v[1]), pack_f16(v[2], v[3]), pack_f16(v[4], v[5]), pack_f16(v[6], v[7]));
+                    }
+#pragma unroll 1
+                    for (int i = un.n * 8 + token; i < TA_TILE * 8 && which; i += TA_TILE) {
+                        *reinterpret_cast<uint4*>(to + i * 16) = make_uint4(0, 0, 0, 0);
+                        if (D == 128) *reinterpret_cast<uint4*>(to + TA_TILE * 128 + i * 16) = make_uint4(0, 0, 0, 0);
                     }
                 }
                 fence_proxy_async_smem();
@@ -737,6 +804,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
             if (elect_one()) mbar_arrive(smem_u32(&ctl->together));
             return wait(&ctl->together, n_together++ & 1);
         };
+#pragma unroll 1
         for (uint32_t u = 0; next_unit(u); ++u) {
             const TreeUnit& un = ctl->unit[u % TA_UNITS];
             const int t0 = un.tile0, nt = un.tile1 - t0, step = un.two ? 1 : 2, j0 = un.two ? 0 : w;
@@ -745,6 +813,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
             const int buf = un.two ? w : un.buf;
             float m = -INFINITY, l = 0.f, rs = 0.f;
             int ev = 0, odd = 0;
+#pragma unroll 1
             for (int j = j0; j < nt; j += step, ++n_s) {
                 if (!wait(&ctl->s_full[w], n_s & 1)) break;
                 tc_fence_after();
@@ -861,86 +930,118 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                 if (!wait(&ctl->pv_done[w], (n_s - 1) & 1)) break;
                 tc_fence_after();
             }
-            // ---- the end of the unit, or of this block's share of it: what the copies of a row have becomes one, in rounds of D / 4 columns by way of shared memory
-            constexpr int CW = D / 4;
-            // (elements 16 i .. 16 i + 15 and, D = 128, 64 + 16 i .. + 15
-            const int parts = un.two ? 1 : 2 << copies;                        // of a row: (w, copy)
-            auto lane_of = [&](int row, int p) { return un.two ? row : (p >> copies) * TA_TILE + (p & ((1 << copies) - 1)) * distinct + row; };
-            ctl->stats[w * TA_TILE + r] = make_float2(m, have ? l : 0.f);
+            // ---- the end of the unit, or of this block's share of it.  What the copies of a row have becomes one: a warp reads both slots' outputs of its lanes, group w of warps
+            // the columns of rounds 2 w and 2 w + 1 (with more than 128 rows: its own slot's, all of them); copies in other lanes follow by way of shared memory.
+            constexpr int CW = D / 4, CQ = CW / 4;                             // columns of a round: elements 16 i .. 16 i + 15 and, D = 128, 64 + 16 i .. + 15; in fours
+            const bool two = un.two, to_part = un.slot >= 0;
+            float2* stats = &ctl->stats[w * TA_TILE + r];
+            *stats = make_float2(m, have ? l : 0.f);
+            if (lane == 0) ctl->ev[warp] = ev;
             if (warp == 0 && lane == 0) ctl->odd = odd;
+            tc_fence_before();
             if (!together()) break;
-            float top = -INFINITY, all = 0.f;
-#pragma unroll 1
-            for (int k = 0; k < parts; ++k) top = fmaxf(top, ctl->stats[lane_of(row, k)].x);
-            const float ref = top == -INFINITY ? 0.f : top;
-#pragma unroll 1
-            for (int k = 0; k < parts; ++k) {
-                const float2 s = ctl->stats[lane_of(row, k)];
-                all += s.y == 0.f ? 0.f : s.y * ex2_ftz(s.x - ref);
-            }
-            const float f = !have || l == 0.f || all == 0.f ? 0.f : ex2_ftz(m - ref) / all;
-            if (un.slot >= 0 && live) x.stats[(size_t)un.slot * x.part_rows + row] = make_float2(ref, all);    // (the copies of a row write the same)
-            const float f1 = f * pow2i(ev >> 1), f2 = pow2i(ev - (ev >> 1));
-            float4* stage = reinterpret_cast<float4*>(q_smem + un.buf * C::op_bytes);        // the unit's Q has been used up
-            const int items = un.rows * (CW / 4);
-#pragma unroll 1
-            for (int i = 0; i < 4; ++i) {
-                uint32_t o[CW];
+            tc_fence_after();
+            float ref, all = 0.f;
+            {
+                // the row's 1, 2, 4 or 8 parts, `distinct` lanes apart: each is read 8, 4, 2 or 1 times, by all lanes of the row in the same order
+                const int apart = two ? 0 : distinct, at0 = two ? w * TA_TILE + r : r & (distinct - 1);
+                float2 part[8];
+                float top = -INFINITY;
 #pragma unroll
-                for (int k = 0; k < CW; ++k) o[k] = 0;
-                if (have) {
+                for (int k = 0; k < 8; ++k) {
+                    part[k] = ctl->stats[(at0 + k * apart) & (2 * TA_TILE - 1)];
+                    top = fmaxf(top, part[k].x);
+                }
+                ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) all += part[k].y == 0.f ? 0.f : part[k].y * ex2_ftz(part[k].x - ref);
+                all *= two ? 0.125f : 0.25f * (1 << copies);
+            }
+            if (to_part && live) x.stats[(size_t)un.slot * x.part_rows + row] = make_float2(ref, all);    // (the copies of a row write the same)
+            float4* stage = reinterpret_cast<float4*>(q_smem + un.buf * C::op_bytes);        // the unit's Q has been used up
+            const bool any_odd = ctl->odd != 0, direct = copies == 0 && !any_odd;
+            const int items = un.rows * CQ;
+#pragma unroll 1
+            for (int i = two ? 0 : 2 * w; i < (two ? 4 : 2 * w + 2); ++i) {
+                float o[CW];
+#pragma unroll
+                for (int k = 0; k < CW; ++k) o[k] = 0.f;
+#pragma unroll 1
+                for (int v = two ? w : 0; v <= (two ? w : 1); ++v) {
+                    if (v >= nt && !two) break;                                // no tile has gone there
+                    const float2 s = ctl->stats[v * TA_TILE + r];
+                    const int e = ctl->ev[v * 4 + quarter];
+                    const float f = s.y != 0.f && all != 0.f ? ex2_ftz(s.x - ref) / all : 0.f, f1 = f * pow2i(e >> 1), f2 = pow2i(e - (e >> 1));
+                    const uint32_t from = tmem + lanes + 256 + v * D + 2 * i;
+                    uint32_t y[CW];
 #pragma unroll
                     for (int g = 0; g < D / 8; ++g) {
-                        if (D == 128) tmem_ld_32x2(t_o + g * 8 + 2 * i, o[8 * (g & 1) + (g >> 1)], o[CW / 2 + 8 * (g & 1) + (g >> 1)]);
-                        else tmem_ld_32x2(t_o + g * 8 + 2 * i, o[g], o[8 + g]);
+                        if (D == 128) tmem_ld_32x2(from + g * 8, y[8 * (g & 1) + (g >> 1)], y[CW / 2 + 8 * (g & 1) + (g >> 1)]);
+                        else tmem_ld_32x2(from + g * 8, y[g], y[8 + g]);
                     }
                     tmem_ld_wait();
-                }
-                float4* mine_at = stage + (w * TA_TILE + r) * (CW / 4);
 #pragma unroll
-                for (int k = 0; k < CW; k += 4) {
-                    float v[4];
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) v[q] = f == 0.f ? 0.f : __uint_as_float(o[k + q]) * f1 * f2;
-                    mine_at[(k / 4) ^ (lane & (CW / 4 - 1))] = make_float4(v[0], v[1], v[2], v[3]);
+                    for (int k = 0; k < CW; ++k) o[k] += f != 0.f ? __uint_as_float(y[k]) * f1 * f2 : 0.f;    // (what stands there otherwise does not count)
                 }
-                if (!together()) break;
-#pragma unroll 1
-                for (int item = tid; item < items; item += TA_SOFT * 32) {     // four elements of a row
-                    const int to_row = item / (CW / 4), k0 = item % (CW / 4) * 4, d0 = (D == 128 && k0 >= 16 ? 48 : 0) + 16 * i + k0, at = un.row0 + to_row, token = token_of(x, at);
-                    float v[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 1
-                    for (int p = 0; p < parts; ++p) {
-                        const int from = lane_of(to_row, p);
-                        const float4 y = stage[from * (CW / 4) + ((k0 / 4) ^ (from & (CW / 4 - 1)))];
-                        v[0] += y.x;
-                        v[1] += y.y;
-                        v[2] += y.z;
-                        v[3] += y.w;
+                if (direct) {                                                  // a lane has its row to itself
+                    if (live) {
+                        const int at = un.row0 + row, token = token_of(x, at);
+                        float* part = x.part + ((size_t)max(un.slot, 0) * x.part_rows + row) * D + 16 * i;
+                        uint16_t* out = x.O + (long long)(un.token0 + token) * x.o_stride + (un.head * x.G + at - token * x.G) * D + 16 * i;
+                        if (to_part) {
+#pragma unroll
+                            for (int k = 0; k < CW; k += 4) *reinterpret_cast<float4*>(part + (k >= 16 ? 48 : 0) + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+                        } else {
+#pragma unroll
+                            for (int k = 0; k < CW; k += 8)
+                                *reinterpret_cast<uint4*>(out + (k >= 16 ? 48 : 0) + k) =
+                                    make_uint4(pack_bf16(o[k], o[k + 1]), pack_bf16(o[k + 2], o[k + 3]), pack_bf16(o[k + 4], o[k + 5]), pack_bf16(o[k + 6], o[k + 7]));
+                        }
                     }
-                    if (ctl->odd) {                                            // what the row sees of drafted values that are not finite
+                    __syncwarp();
+                    continue;
+                }
+#pragma unroll
+                for (int k = 0; k < CQ; ++k) stage[(w * TA_TILE + r) * CQ + (k ^ (lane & (CQ - 1)))] = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+                if (!together()) break;
+                // four elements of a row: of both halves of the warps' rounds, or of both halves of the rows
+#pragma unroll 1
+                for (int item = tid; item < (two ? items : 2 * items); item += TA_SOFT * 32) {
+                    const int half = two ? 0 : item >= items, to_row = (item - half * items) / CQ, k0 = (item - half * items) % CQ;
+                    const int d0 = (D == 128 && k0 >= 4 ? 48 : 0) + 16 * (two ? i : 2 * half + (i & 1)) + 4 * k0;
+                    const float4* from = stage + (half * TA_TILE + to_row) * CQ + (k0 ^ (to_row & (CQ - 1)));      // (the copies' lanes: the same swizzle)
+                    float4 v = *from;
+#pragma unroll 1
+                    for (int p = 1; p < 1 << copies; ++p) {
+                        from += distinct * CQ;
+                        const float4 y = *from;
+                        v.x += y.x;
+                        v.y += y.y;
+                        v.z += y.z;
+                        v.w += y.w;
+                    }
+                    const int at = un.row0 + to_row, token = token_of(x, at);
+                    if (any_odd) {                                             // what the row sees of drafted values that are not finite
                         const unsigned long long sees = ctl->sees[un.buf][token];
 #pragma unroll 1
-                        for (int t = 0; t < un.n; ++t)
-#pragma unroll 1
-                            for (int k = 0; k < 4; ++k) {
-                                const float y = __uint_as_float((uint32_t)x.V[(un.token0 + (long long)t) * x.v_stride + un.head * D + d0 + k] << 16);
-                                if ((sees >> t & 1) && !(fabsf(y) < INFINITY)) {
-                                    v[0] += k == 0 ? y : 0.f;
-                                    v[1] += k == 1 ? y : 0.f;
-                                    v[2] += k == 2 ? y : 0.f;
-                                    v[3] += k == 3 ? y : 0.f;
-                                }
-                            }
+                        for (int t = 0; t < un.n; ++t) {
+                            if (!(sees >> t & 1)) continue;
+                            const uint2 y = *reinterpret_cast<const uint2*>(x.V + (un.token0 + (long long)t) * x.v_stride + un.head * D + d0);
+                            v.x += odd_part(bf16_lo(y.x));
+                            v.y += odd_part(bf16_hi(y.x));
+                            v.z += odd_part(bf16_lo(y.y));
+                            v.w += odd_part(bf16_hi(y.y));
+                        }
                     }
-                    if (un.slot >= 0)
-                        *reinterpret_cast<float4*>(x.part + ((size_t)un.slot * x.part_rows + to_row) * D + d0) = make_float4(v[0], v[1], v[2], v[3]);
+                    if (to_part)
+                        *reinterpret_cast<float4*>(x.part + ((size_t)un.slot * x.part_rows + to_row) * D + d0) = v;
                     else
                         *reinterpret_cast<uint2*>(x.O + (long long)(un.token0 + token) * x.o_stride + (un.head * x.G + at - token * x.G) * D + d0) =
-                            make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+                            make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
                 }
                 if (!together()) break;
             }
+            if (!ok || !together()) break;         // (the outputs of either slot and the statistics have been read)
             if (!ok) break;
             tc_fence_before();
             __syncwarp();
@@ -951,8 +1052,9 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
         }
         tc_fence_before();
     }
+    if (!ok) ctl->abort_flag = 1;
     __syncthreads();
-    if (tid == 0 && *abort_flag) *x.status = AG_ERR_TIMEOUT;
+    if (tid == 0 && ctl->abort_flag) *x.status = AG_ERR_TIMEOUT;
     if (warp == 8) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);
@@ -972,11 +1074,12 @@ __global__ void __launch_bounds__(TJ_WARPS * 32) k_attn_tree_join(const TreeArgs
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.y * TJ_WARPS + warp;
     if (row >= c.rows) return;
     // blocks from this one on, while they have tiles of the unit
-    const int last = (int)min((long long)blocks - 1, (c.begin + TA_UNIT + (long long)c.weight * c.tiles - 1) / c.quota), n = last - (int)blockIdx.x + 1;
+    const int last = (int)min((long long)blocks - 1, (c.begin + c.unit_places + (long long)c.weight * c.tiles - 1) / c.quota), n = last - (int)blockIdx.x + 1;
     float top = -INFINITY;
+#pragma unroll 1
     for (int i = lane; i < n; i += 32) {
         const int b = blockIdx.x + i;
-        const int t0 = tiles_before(c.quota * b, c.begin, c.weight, c.tiles), t1 = tiles_before(c.quota * (b + 1), c.begin, c.weight, c.tiles);
+        const int t0 = tiles_before(c.quota * b, c.begin, c.unit_places, c.weight, c.tiles), t1 = tiles_before(c.quota * (b + 1), c.begin, c.unit_places, c.weight, c.tiles);
         const int at = 2 * b + (t1 < c.tiles ? 1 : 0);
         slot[warp][i] = t0 < t1 ? at : -1;
         const float2 s = t0 < t1 ? __ldcg(&x.stats[(size_t)at * x.part_rows + row]) : make_float2(-INFINITY, 0.f);
@@ -987,6 +1090,7 @@ __global__ void __launch_bounds__(TJ_WARPS * 32) k_attn_tree_join(const TreeArgs
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     const float ref = top == -INFINITY ? 0.f : top;
     float sum = 0.f;
+#pragma unroll 1
     for (int i = lane; i < n; i += 32) {
         const float l = weight[warp][i];
         const float f = l == 0.f ? 0.f : l * ex2_ftz(__ldcg(&x.stats[(size_t)slot[warp][i] * x.part_rows + row]).x - ref);
@@ -1074,10 +1178,11 @@ extern "C" ag_status attention_tree_kv4(const ag_tree_attention* a, const ag_kv4
     memset(&x, 0, sizeof x);
     x.Q = (const uint16_t*)a->Q; x.K = (const uint16_t*)a->K; x.V = (const uint16_t*)a->V; x.O = (uint16_t*)a->O;
     x.pages = (const uint8_t*)pool->pages;
-    x.q_stride = a->q_stride; x.k_stride = a->k_stride; x.v_stride = a->v_stride; x.o_stride = a->o_stride; x.n_tokens = a->n_tokens;
+    x.q_stride = a->q_stride; x.k_stride = a->k_stride; x.v_stride = a->v_stride; x.o_stride = a->o_stride; x.n_tokens = (int)a->n_tokens;
     x.row = a->row; x.off = a->off; x.parent = a->parent; x.page_of = table->page_of; x.len = table->len;
     x.H_q = a->H_q; x.H_kv = H_kv; x.G = a->H_q / H_kv; x.n_seq = a->n_seq; x.n_rows = table->n_rows; x.max_pages = table->max_pages; x.n_pages = (int)pool->n_pages;
     x.max_tokens = a->max_tokens;
+    x.most_len = (int)std::min<long long>(64ll * table->max_pages, 0x7fffffff);
     x.by_g = x.G > 1 ? (uint32_t)((0x100000000ull + x.G - 1) / x.G) : 0;
     x.part_rows = tree_part_rows(a->max_tokens, x.G);
     x.scale_log2e = 1.4426950408889634f * (a->scale > 0.f ? a->scale : 1.f / sqrtf((float)D));
@@ -1086,9 +1191,9 @@ extern "C" ag_status attention_tree_kv4(const ag_tree_attention* a, const ag_kv4
     x.cross = (TreeCross*)(ws + 256);
     x.stats = (float2*)((uint8_t*)x.cross + round256(TA_BLOCKS * sizeof(TreeCross)));
     x.part = (float*)((uint8_t*)x.stats + round256(2 * TA_BLOCKS * (size_t)x.part_rows * sizeof(float2)));
-    // no more blocks than there can be runs of TA_LEAST tiles
-    const long long unit_weight = (a->max_tokens * x.G + 127) / 128, most = (long long)a->n_seq * H_kv * unit_weight * ((table->max_pages + 1) / 2 + 1 + TA_UNIT);
-    const int blocks = (int)std::min<long long>(TA_BLOCKS, (most + TA_LEAST - 1) / TA_LEAST);
+    // no more blocks than there can be tiles
+    const long long unit_weight = (a->max_tokens * x.G + 127) / 128, most = (long long)a->n_seq * H_kv * unit_weight * ((table->max_pages + 1) / 2 + 1);
+    const int blocks = (int)std::min<long long>(TA_BLOCKS, most);
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;

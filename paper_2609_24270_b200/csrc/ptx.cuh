@@ -96,6 +96,17 @@ __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
         : "memory");
     return ok != 0;
 }
+// The shortest bounded wait: at most `polls` tries (each of which the hardware may stretch).
+__device__ __forceinline__ bool mbar_wait_polls(uint32_t bar, uint32_t parity, uint32_t polls) {
+    uint32_t ok;
+    asm volatile(
+        "{\n .reg .pred p, q;\n .reg .u32 n;\n mov.u32 n, %3;\nagain:\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n @p bra done;\n sub.u32 n, n, 1;\n"
+        " setp.ne.u32 q, n, 0;\n @q bra again;\ndone:\n selp.u32 %0, 1, 0, p;\n}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity), "r"(polls)
+        : "memory");
+    return ok != 0;
+}
 // Bounded wait: gives up after `limit_ns` of wall time (checked every 256 polls) or as soon as
 // another role of the block has raised *abort_flag.  Returns false on give-up.
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag,
