@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -135,6 +136,10 @@ class RotaryRows(C.Structure):
                 ("H_q", C.c_int32), ("H_kv", C.c_int32), ("D", C.c_int32), ("n_tokens", C.c_int64), ("pos", C.c_void_p), ("from_", C.c_void_p), ("n_rows", C.c_int64)]
 
 
+# the same as bytes, in a quarter of the time that filling the structure takes (0.2 against 0.7 us; every layer of a small step has such a call)
+_pack_rotary_rows = struct.Struct("@5P5q3i4xq2Pq").pack
+
+
 class TreeAttention(C.Structure):
     _fields_ = [("Q", C.c_void_p), ("K", C.c_void_p), ("V", C.c_void_p), ("O", C.c_void_p),
                 ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64), ("o_stride", C.c_int64),
@@ -231,8 +236,8 @@ def lib() -> C.CDLL:
     L.ag_attention_decode_kv4_workspace.argtypes = [C.c_int] * 5
     L.ag_attention_decode_kv4_workspace.restype = sz
     L.ag_rotary_frequencies.argtypes = [C.POINTER(RotaryScaling), vp, C.POINTER(C.c_double)]
-    L.ag_rotary_apply.argtypes = [C.POINTER(Rotary), C.POINTER(RotaryRows), vp]
-    L.ag_kv4_append_rotary.argtypes = [pool, C.POINTER(Rotary), C.POINTER(RotaryRows), vp, vp]
+    L.ag_rotary_apply.argtypes = [C.POINTER(Rotary), vp, vp]
+    L.ag_kv4_append_rotary.argtypes = [pool, C.POINTER(Rotary), vp, vp, vp]
     L.attention_tree_kv4.argtypes = [C.POINTER(TreeAttention), pool, table, vp, sz, vp]
     L.ag_attention_tree_kv4_workspace.argtypes = [C.c_int] * 6
     L.ag_attention_tree_kv4_workspace.restype = sz
@@ -729,9 +734,10 @@ def rotary_apply(rotary: Rotary, pos_ptr: int, n_tokens: int, D: int, q_ptr=None
                  n_rows: int = 0, stream: int = 0):
     """Rows of Q and K ([H][D] bf16, strides in elements; either may be left out) turned to the positions pos[i]."""
     wq, wk = H_q * D, H_kv * D
-    x = RotaryRows(q_ptr, k_ptr, None, q_out_ptr, k_out_ptr, wq if q_stride is None else q_stride, wk if k_stride is None else k_stride, 0,
-                   wq if q_out_stride is None else q_out_stride, wk if k_out_stride is None else k_out_stride, H_q, H_kv, D, n_tokens, pos_ptr, from_ptr, n_rows)
-    _check(lib().ag_rotary_apply(C.byref(rotary), C.byref(x), stream), "ag_rotary_apply")
+    x = _pack_rotary_rows(q_ptr or 0, k_ptr or 0, 0, q_out_ptr or 0, k_out_ptr or 0, wq if q_stride is None else q_stride, wk if k_stride is None else k_stride, 0,
+                          wq if q_out_stride is None else q_out_stride, wk if k_out_stride is None else k_out_stride, H_q, H_kv, D, n_tokens, pos_ptr or 0, from_ptr or 0,
+                          n_rows)
+    _check(lib().ag_rotary_apply(C.byref(rotary), x, stream), "ag_rotary_apply")
 
 
 def kv4_append_rotary(pool: KV4Pool, rotary: Rotary | None, pos_ptr, slot_ptr: int, n_tokens: int, k_ptr: int, v_ptr: int, k_out_ptr=None, q_ptr=None,
@@ -739,10 +745,10 @@ def kv4_append_rotary(pool: KV4Pool, rotary: Rotary | None, pos_ptr, slot_ptr: i
                       q_out_stride: int | None = None, k_out_stride: int | None = None, from_ptr=None, n_rows: int = 0, stream: int = 0):
     """K turned and stored, V stored, Q turned beside them (rotary None: nothing is turned); from_ptr: the rows to take, out of n_rows."""
     wq, wk = H_q * pool.D, pool.H_kv * pool.D
-    x = RotaryRows(q_ptr, k_ptr, v_ptr, q_out_ptr, k_out_ptr, wq if q_stride is None else q_stride, wk if k_stride is None else k_stride,
-                   wk if v_stride is None else v_stride, wq if q_out_stride is None else q_out_stride, wk if k_out_stride is None else k_out_stride, H_q, pool.H_kv,
-                   pool.D, n_tokens, pos_ptr, from_ptr, n_rows)
-    _check(lib().ag_kv4_append_rotary(C.byref(pool), None if rotary is None else C.byref(rotary), C.byref(x), slot_ptr, stream), "ag_kv4_append_rotary")
+    x = _pack_rotary_rows(q_ptr or 0, k_ptr or 0, v_ptr or 0, q_out_ptr or 0, k_out_ptr or 0, wq if q_stride is None else q_stride, wk if k_stride is None else k_stride,
+                          wk if v_stride is None else v_stride, wq if q_out_stride is None else q_out_stride, wk if k_out_stride is None else k_out_stride, H_q, pool.H_kv,
+                          pool.D, n_tokens, pos_ptr or 0, from_ptr or 0, n_rows)
+    _check(lib().ag_kv4_append_rotary(C.byref(pool), None if rotary is None else C.byref(rotary), x, slot_ptr, stream), "ag_kv4_append_rotary")
 
 
 def attention_tree_kv4_workspace(n_seq: int, max_tokens: int, H_q: int, H_kv: int, D: int, max_pages: int) -> int:

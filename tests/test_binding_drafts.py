@@ -112,3 +112,8 @@ def test_a_device_is_asked_for_only_after_the_arguments():
     r = ag.Rotary(A, 64, 0, 1.0)
     x = ag.RotaryRows(A, None, None, 2 * A, None, 512, 0, 0, 512, 0, 4, 0, 128, 3, A, None, 0)
     assert ag.lib().ag_rotary_apply(C.byref(r), C.byref(x), None) not in (ag.AG_OK, ag.AG_ERR_ARG)
+
+
+def test_packed_rows_are_the_structure():
+    v = [11 << 40, 12, 13, 14, 15, -21, 22, 23, 24, 25 << 33, 31, 32, 33, 34 << 32, 41 << 50, 42, 43]
+    assert ag._pack_rotary_rows(*v) == bytes(ag.RotaryRows(*v))
