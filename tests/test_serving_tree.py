@@ -205,6 +205,29 @@ def test_what_is_not_seen_has_no_influence():
         assert (got[:, :4] == plain[:, :4]).all() and (got[off[1]:] == plain[off[1]:]).all()
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("count", [5, 12, 25, 50])
+@pytest.mark.parametrize("lens", [[1500], [60] * 90])
+def test_values_that_are_not_finite_in_every_layout_of_rows(D, count, lens):
+    """Rows four times, twice and once in a tile and in both tiles, of units that several blocks share and of whole ones: outputs of tokens that see a value which is not finite are
+    not finite where the formula's are not, every other output has the same bits as without it."""
+    c = make(lens, 2, D, seed=61)
+    counts = [count] * len(lens)
+    n, off, par = sum(counts), np.concatenate([[0], np.cumsum(counts)]), parents(counts, 8)
+    Q, K, V = rows(n, 8, D, 1), rows(n, 2, D, 2), rows(n, 2, D, 3)
+    plain = run(Q, K, V, c, off, par, 8, 64)
+    check(plain, Q, K, V, c, off, par, 4)
+    V2 = V.copy()
+    for first in off[:-1:3]:
+        V2[first + 2, 0, 1], V2[first + 3, 0, D - 1], V2[first + 4, 1, 20], V2[first + 2, 1, 20] = 0x7F80, 0xFF80, 0x7F80, 0xFF80
+    got = run(Q, K, V2, c, off, par, 8, 64)
+    with np.errstate(invalid="ignore"):
+        want, _, _ = drafts.tree(Q, K, V2, drafts.cache_of(c.pages, D, c.page_of, c.len), off, par, 4)
+    assert (np.isnan(got) == np.isnan(want)).all() and (np.isposinf(got) == np.isposinf(want)).all() and (np.isneginf(got) == np.isneginf(want)).all()
+    fine = np.isfinite(want)
+    assert (got[fine] == plain[fine]).all() and not fine.all()
+
+
 def test_groups_of_nan_in_the_cache():
     c = make([70, 70], 1, 64, seed=23)
     at = kv4.scale_byte(64, 1, 3, 1)
