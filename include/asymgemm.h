@@ -818,7 +818,7 @@ typedef struct {
  *   keys, values   s * code + base (of the cache) and the drafted tokens' own enter the products as fp16 under a power of two: off by 2^-11 of themselves, or 2^-19 (values: 2^-17) of the
  *                  largest |base| + 15 s beside them (keys: of the same 128 tokens; values: of the row's tokens so far)
  *   queries        exact, or 2^-32 of the row's largest element
- *   probabilities  2^-11 of themselves, or 2^-35 of the largest;  scores, softmax statistics and outputs are summed in 32 bits
+ *   probabilities  2^-11 of themselves, or 2^-29 of the largest;  scores, softmax statistics and outputs are summed in 32 bits
  *   table      lengths are clamped to 0 .. 64 max_pages; tokens whose page is not one of the pool's are left out
  *   workspace  device, 16-byte aligned, ag_attention_tree_kv4_workspace bytes (at most 39 MB); calls that may run at the same time need one each.  Its first int32 is
  *              the call's status once it has run (AG_OK, or AG_ERR_TIMEOUT when a bounded wait ran out), the rest means nothing between calls

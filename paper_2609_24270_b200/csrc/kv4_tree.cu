@@ -43,8 +43,9 @@ constexpr int TA_BLOCKS = 148;
 // places of the line that a unit takes beside its tiles: Q, drafts, its end.  None where every tile can have a block of its own, since then the longest run counts, not the sum
 // (with it, a short request's tiles would be handled one after the other by a few blocks)
 constexpr int TA_UNIT = 4;
-constexpr float TA_LAZY = 5.f;                             // the reference m of a row moves when its maximum has grown by more than 2^5
-constexpr float TA_SHIFT = 10.f;                           // P is taken times 2^10: at most 2^15, down to 2^-35 of the largest without rounding to zero
+// The reference m of a row moves when its maximum has grown by more than 2^11, and P is taken times 2^4: at most 2^15, and 2^-25 is lost of it, 2^-29 of the largest.  (With 2^5 and 2^10
+// it was 2^-35, but one tile in three had a row to move, whose outputs are multiplied and written back while everybody waits: 4 trees over 131072 tokens 371 us instead of 325.)
+constexpr float TA_LAZY = 11.f, TA_SHIFT = 4.f;
 constexpr uint32_t TA_POLLS = 1u << 26;                    // of a barrier that does not come: some seconds
 
 struct TreeArgs {
