@@ -959,51 +959,52 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                 all *= two ? 0.125f : 0.25f * (1 << copies);
             }
             if (to_part && live) x.stats[(size_t)un.slot * x.part_rows + row] = make_float2(ref, all);    // (the copies of a row write the same)
+            // factors of what this lane has in slot 0 (its own slot) and in slot 1; 0: what stands there does not count
+            const int va = two ? w : 0;
+            const bool second = !two && nt > 1;
+            auto factor = [&](int v) -> float {
+                const float2 st = ctl->stats[v * TA_TILE + r];
+                return st.y != 0.f && all != 0.f ? ex2_ftz(st.x - ref) / all : 0.f;
+            };
+            const float fa = factor(va), fb = second ? factor(1) : 0.f;
+            const int ea = ctl->ev[va * 4 + quarter], eb = ctl->ev[4 + quarter];
+            const float a1 = fa * pow2i(ea >> 1), a2 = pow2i(ea - (ea >> 1)), b1 = fb * pow2i(eb >> 1), b2 = pow2i(eb - (eb >> 1));
             float4* stage = reinterpret_cast<float4*>(q_smem + un.buf * C::op_bytes);        // the unit's Q has been used up
             const bool any_odd = ctl->odd != 0, direct = copies == 0 && !any_odd;
-            const int items = un.rows * CQ;
+            const int items = un.rows * CQ, own_at = un.row0 + row, own_token = token_of(x, own_at);
+            float* own_part = x.part + ((size_t)max(un.slot, 0) * x.part_rows + row) * D;
+            uint16_t* own_out = x.O + (long long)(un.token0 + own_token) * x.o_stride + (un.head * x.G + own_at - own_token * x.G) * D;
 #pragma unroll 1
             for (int i = two ? 0 : 2 * w; i < (two ? 4 : 2 * w + 2); ++i) {
-                float o[CW];
-#pragma unroll
-                for (int k = 0; k < CW; ++k) o[k] = 0.f;
+                // four elements at a time, 4 q of the round's first 16 and (D = 128) of the other 16, or of its first and last 8 (a loop: this code runs once a unit, and most of its
+                // time is the fetching of instructions)
 #pragma unroll 1
-                for (int v = two ? w : 0; v <= (two ? w : 1); ++v) {
-                    if (v >= nt && !two) break;                                // no tile has gone there
-                    const float2 s = ctl->stats[v * TA_TILE + r];
-                    const int e = ctl->ev[v * 4 + quarter];
-                    const float f = s.y != 0.f && all != 0.f ? ex2_ftz(s.x - ref) / all : 0.f, f1 = f * pow2i(e >> 1), f2 = pow2i(e - (e >> 1));
-                    const uint32_t from = tmem + lanes + 256 + v * D + 2 * i;
-                    uint32_t y[CW];
+                for (int q = 0; q < CQ / 2; ++q) {
+                    const uint32_t from = tmem + lanes + 256 + va * D + 2 * i + (D == 128 ? ((q & 1) * 8 + (q >> 1)) * 8 : q * 32), also = second ? from + D : from;
+                    uint32_t y[8], z[8];
 #pragma unroll
-                    for (int g = 0; g < D / 8; ++g) {
-                        if (D == 128) tmem_ld_32x2(from + g * 8, y[8 * (g & 1) + (g >> 1)], y[CW / 2 + 8 * (g & 1) + (g >> 1)]);
-                        else tmem_ld_32x2(from + g * 8, y[g], y[8 + g]);
+                    for (int k = 0; k < 4; ++k) {
+                        tmem_ld_32x2(from + k * (D == 128 ? 16 : 8), y[k], y[4 + k]);
+                        tmem_ld_32x2(also + k * (D == 128 ? 16 : 8), z[k], z[4 + k]);
                     }
                     tmem_ld_wait();
+                    float o[8];
 #pragma unroll
-                    for (int k = 0; k < CW; ++k) o[k] += f != 0.f ? __uint_as_float(y[k]) * f1 * f2 : 0.f;    // (what stands there otherwise does not count)
-                }
-                if (direct) {                                                  // a lane has its row to itself
-                    if (live) {
-                        const int at = un.row0 + row, token = token_of(x, at);
-                        float* part = x.part + ((size_t)max(un.slot, 0) * x.part_rows + row) * D + 16 * i;
-                        uint16_t* out = x.O + (long long)(un.token0 + token) * x.o_stride + (un.head * x.G + at - token * x.G) * D + 16 * i;
-                        if (to_part) {
+                    for (int k = 0; k < 8; ++k) {
+                        const float ya = __uint_as_float(y[k]) * a1 * a2, zb = __uint_as_float(z[k]) * b1 * b2;
+                        o[k] = (fa != 0.f ? ya : 0.f) + (fb != 0.f ? zb : 0.f);
+                    }
 #pragma unroll
-                            for (int k = 0; k < CW; k += 4) *reinterpret_cast<float4*>(part + (k >= 16 ? 48 : 0) + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
-                        } else {
-#pragma unroll
-                            for (int k = 0; k < CW; k += 8)
-                                *reinterpret_cast<uint4*>(out + (k >= 16 ? 48 : 0) + k) =
-                                    make_uint4(pack_bf16(o[k], o[k + 1]), pack_bf16(o[k + 2], o[k + 3]), pack_bf16(o[k + 4], o[k + 5]), pack_bf16(o[k + 6], o[k + 7]));
-                        }
+                    for (int h = 0; h < 2; ++h) {
+                        const float4 v = make_float4(o[4 * h], o[4 * h + 1], o[4 * h + 2], o[4 * h + 3]);
+                        const int k = q + h * (CQ / 2), d0 = (D == 128 ? 64 * h : 8 * h) + 16 * i + 4 * q;
+                        if (!direct) stage[(w * TA_TILE + r) * CQ + (k ^ (lane & (CQ - 1)))] = v;
+                        else if (live && to_part) *reinterpret_cast<float4*>(own_part + d0) = v;           // (a lane has its row to itself)
+                        else if (live) *reinterpret_cast<uint2*>(own_out + d0) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
                     }
                     __syncwarp();
-                    continue;
                 }
-#pragma unroll
-                for (int k = 0; k < CQ; ++k) stage[(w * TA_TILE + r) * CQ + (k ^ (lane & (CQ - 1)))] = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+                if (direct) continue;
                 if (!together()) break;
                 // four elements of a row: of both halves of the warps' rounds, or of both halves of the rows
 #pragma unroll 1
