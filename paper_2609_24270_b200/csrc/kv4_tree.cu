@@ -646,14 +646,26 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                     for (int k = 0; k < 2; ++k) {
                         const int r = r0 + k * R + lane / L;
                         const uint32_t w[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
-                        float v[8], top = 0.f;
+                        // the row's largest magnitude by its bits, two elements of a word side by side
+                        uint32_t most = __vmaxu2(__vmaxu2(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu), __vmaxu2(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu));
+                        most = max(most & 0xffffu, most >> 16);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            v[i] = i & 1 ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]);
-                            if (fabsf(v[i]) < INFINITY) top = fmaxf(top, fabsf(v[i]));
+                        for (int o = 1; o < L; o <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+                        float top = __uint_as_float(most << 16);
+                        if (__any_sync(0xffffffffu, most >= 0x7f80u)) {            // some are not finite: the largest of the others
+                            top = 0.f;
+#pragma unroll 1
+                            for (int i = 0; i < 8; ++i) {
+                                const uint32_t word = i < 4 ? i < 2 ? w[0] : w[1] : i < 6 ? w[2] : w[3];
+                                const float v = fabsf(i & 1 ? bf16_hi(word) : bf16_lo(word));
+                                if (v < INFINITY) top = fmaxf(top, v);
+                            }
+#pragma unroll 1
+                            for (int o = 1; o < L; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
                         }
+                        float v[8];
 #pragma unroll
-                        for (int o = 1; o < L; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                        for (int i = 0; i < 8; ++i) v[i] = i & 1 ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]);
                         const int shift = top == 0.f ? 0 : min(7 - ((int)(__float_as_uint(top) >> 23) - 127), 120);
                         const float f = pow2i(shift);
                         const uint4 out = make_uint4(pack_f16(v[0] * f, v[4] * f), pack_f16(v[1] * f, v[5] * f), pack_f16(v[2] * f, v[6] * f), pack_f16(v[3] * f, v[7] * f));
@@ -1043,7 +1055,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                 }
                 if (!together()) break;
             }
-            if (!ok || !together()) break;         // (the outputs of either slot and the statistics have been read)
+            if (!ok || (direct && !together())) break;         // (the outputs of either slot and the statistics have been read)
             if (!ok) break;
             tc_fence_before();
             __syncwarp();
