@@ -13,8 +13,9 @@ namespace ag {
 //   a' = a c - b s,  b' = b c + a s      a c and b c rounded to 32 bits, the rest by one multiply-add, two at a time
 // "Halves": a lane has the two chunks of eight elements that are turned with one another, rot / 2 apart (the lanes behind those have neighbouring chunks, which stay);
 // "pairs": two neighbouring chunks.  Quantisation wants neighbouring chunks, so keys on their way into the cache are passed from lane to lane once they have been turned.
-// Bound: instructions, 60 for a step of Q (with the chunks of a lane side by side, partners fetched from other lanes and one element at a time they were 320:
-// 16384 tokens x 40 heads took 76 us), then memory.
+// Bound: memory, and the latency of its loads where the angles wait in front of them: three blocks on an SM (80 registers) turn 16384 tokens x 40 heads in 55 us (6.1 TB/s, 0.93 of a
+// copy), two (94 registers) in 58, four spill and take 63; appended and loaded back 87, 95 and 95.  A step of Q is 60 instructions; with the chunks of a lane side by side, partners fetched
+// from other lanes and one element at a time it was 320, and the same tokens took 76 us.
 constexpr int RO_THREADS = 256;
 constexpr int RO_WARPS = RO_THREADS / 32;
 constexpr int RO_ROWS = 4;                 // steps whose loads are in flight together
@@ -49,7 +50,7 @@ __device__ __forceinline__ void turn(uint32_t (&w)[8], const f32x2 (&c)[4], cons
 }
 
 template <int D, bool PAIRS>
-__global__ void __launch_bounds__(RO_THREADS) k_rotary(const RotaryArgs x) {
+__global__ void __launch_bounds__(RO_THREADS, 3) k_rotary(const RotaryArgs x) {
     constexpr int L = D / 16, ROWS = 32 / L, U = RO_ROWS;
     __shared__ float2 turns[RO_WARPS][D / 2];
     dep_wait();
