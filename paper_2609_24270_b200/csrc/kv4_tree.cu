@@ -20,12 +20,12 @@
 // All tiles of all units stand in one line that is cut into equal runs, one per block: uneven lengths, one long request or many short ones are the same case.  Units that
 // two or more blocks share leave parts (normalised outputs, maximum, sum) in the workspace, which a second launch puts together.
 //
-// 640 threads: warps 0-7 softmax and epilogue (two groups of four), 8 MMA, 9 units and copies of keys, 10 exponents, 11 copies of values, 12-15 decoding of keys, 16-19 of values.
+// 640 threads: warps 0-7 softmax and epilogue (two groups of four), 8 MMA, 9 units and copies of keys, 10 exponents, 11 copies of values, 12-19 decoding, half of them of keys, half of values.
 //
 // Bound: a tile takes some 6200 warp instructions (decoding 2000, softmax 2500, the rest the roles' bookkeeping) on five warps a scheduler, 2500 cycles; its MMAs take 1300, its
 // exponentials 1024, its bytes 500.  4 requests x 32 tokens x 32 heads over 131072 keys: 319 us at 1.965 GHz (840 TFLOP/s), 370 when it is repeated for seconds (the chip is at its 1000 W
 // then and runs at 1.68 GHz).  Code that runs once a unit costs the fetching of its instructions, six cycles each, so it is loops wherever it can be: with the unit's end written out
-// (88 KB of code in all, 75 now) 64 requests over 200 to 4000 keys took 123 us, now 91.
+// (88 KB of code in all, 75 now) 64 requests over 200 to 4000 keys took 123 us, now 90.
 // Other splits, measured: 16 softmax warps, two threads a row (4 requests as above 372 us against 341 of that time); tiles handed on in halves of 64 keys (418 against 405: QK^T with 64
 // columns takes an MMA as long as with 128); more operand stages where they fit, D = 64 (no difference).
 #include <math.h>
@@ -583,8 +583,10 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
         }
     } else {
         // ------------------------------------------------ decoders: Q, the drafted tokens and the cache's codes as operands
-        const int dt = tid - 12 * 32, dwarp = warp - 12;
-        const int token = dt & 127, which = __shfl_sync(0xffffffffu, dt >> 7, 0), page = token >> 6, tk = token & 63, sw = token & 7;
+        // Whose operands a warp makes, K's or V's: those of one kind stand on the same schedulers, which then fetch the code of that kind only (64 requests 90.1 us; with one of each on
+        // every scheduler 91.8, the long cases alike)
+        const int dwarp = warp - 12, which = dwarp >> 1 & 1;
+        const int token = ((dwarp >> 2) * 2 + (dwarp & 1)) * 32 + lane, page = token >> 6, tk = token & 63, sw = token & 7;
         // Where the thread's codes are read and its operands written: K's run t (chunks t, 4 + t ..), V's words of elements 16 i' + 8 j' + h (chunks 2 h and 2 h + 1, or h), each with
         // t or h turned by the token so that neighbouring lanes meet no bank twice.  Operand row: chunk c at (c / 8) 16 KB + 128 row + 16 ((c ^ row) mod 8).
         const int turn = which == 0 ? (tk >> (D == 128 ? 1 : 2)) & 3 : D == 128 ? (tk >> 3) & 1 : (tk >> 3) & 3;
@@ -688,7 +690,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                 arrive(&ctl->q_full[b]);
             }
             if (!ok) break;
-            // ---- operands: warps 12-15 make K's, warps 16-19 V's; thread = token of the tile
+            // ---- operands: four warps make K's, four V's; thread = token of the tile
             const int ahead = min(lead, nt), drafts = un.tile0 == 0;
             // the place among the unit's operands, which are made and used in the order K_0 .. K_{ahead - 1}, V_0 K_ahead V_1 K_{ahead + 1} .., the remaining V
             int place = which ? ahead : 0;
