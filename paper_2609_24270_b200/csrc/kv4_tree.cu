@@ -25,7 +25,7 @@
 // Bound: a tile takes some 6200 warp instructions (decoding 2000, softmax 2500, the rest the roles' bookkeeping) on five warps a scheduler, 2500 cycles; its MMAs take 1300, its
 // exponentials 1024, its bytes 500.  4 requests x 32 tokens x 32 heads over 131072 keys: 319 us at 1.965 GHz (840 TFLOP/s), 370 when it is repeated for seconds (the chip is at its 1000 W
 // then and runs at 1.68 GHz).  Code that runs once a unit costs the fetching of its instructions, six cycles each, so it is loops wherever it can be: with the unit's end written out
-// (88 KB of code in all, 75 now) 64 requests over 200 to 4000 keys took 123 us, now 90.
+// (88 KB of code in all, 75 now) 64 requests over 200 to 4000 keys took 123 us, now 87.
 // Other splits, measured: 16 softmax warps, two threads a row (4 requests as above 372 us against 341 of that time); tiles handed on in halves of 64 keys (418 against 405: QK^T with 64
 // columns takes an MMA as long as with 128); more operand stages where they fit, D = 64 (no difference).
 #include <math.h>
@@ -47,9 +47,10 @@ constexpr int TA_THREADS = 640;
 constexpr int TA_READERS = TA_SOFT + TA_DECODERS + 3;      // warps that read a unit: and MMA, exponents, values' copies
 constexpr int TA_REGS_SOFT = 112, TA_REGS_OTHER = 80;      // 256 x 112 + 384 x 80 <= 640 x 96
 constexpr int TA_BLOCKS = 148;
-// places of the line that a unit takes beside its tiles: Q, drafts, its end.  None where every tile can have a block of its own, since then the longest run counts, not the sum
-// (with it, a short request's tiles would be handled one after the other by a few blocks)
-constexpr int TA_UNIT = 4;
+// Places of the line that a unit takes beside its tiles, for Q, drafts and its end: measured, five to six tiles' time (64 requests over 200 to 4000 keys 86.7 us, with 4 of them 90.1, with 2
+// 96.6), and even, since tiles of more than 128 rows take two places (16 trees of 40 to 64 tokens 83.0 us, with 5 95.6).  None where every tile can have a block of its own, since
+// then the longest run counts, not the sum (with it, a short request's tiles would be handled one after the other by a few blocks).
+constexpr int TA_UNIT = 6;
 // The reference m of a row moves when its maximum has grown by more than 2^11, and P is taken times 2^4: at most 2^15, and 2^-25 is lost of it, 2^-29 of the largest.  (With 2^5 and 2^10
 // it was 2^-35, but one tile in three had a row to move, whose outputs are multiplied and written back while everybody waits: 4 trees over 131072 tokens 371 us instead of 325.)
 constexpr float TA_LAZY = 11.f, TA_SHIFT = 4.f;
@@ -583,7 +584,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
         }
     } else {
         // ------------------------------------------------ decoders: Q, the drafted tokens and the cache's codes as operands
-        // Whose operands a warp makes, K's or V's: those of one kind stand on the same schedulers, which then fetch the code of that kind only (64 requests 90.1 us; with one of each on
+        // Whose operands a warp makes, K's or V's: those of one kind stand on the same schedulers, which then fetch the code of that kind only (64 requests 90.1 us at the time; with one of each on
         // every scheduler 91.8, the long cases alike)
         const int dwarp = warp - 12, which = dwarp >> 1 & 1;
         const int token = ((dwarp >> 2) * 2 + (dwarp & 1)) * 32 + lane, page = token >> 6, tk = token & 63, sw = token & 7;
