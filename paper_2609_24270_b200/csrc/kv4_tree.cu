@@ -84,8 +84,9 @@ struct TreeUnit {
     int slot;                              // part slot, -1: the whole unit is here
     int stop, pad;
 };
+constexpr int TA_ODD = 1, TA_WIDE = 2;     // a drafted value is not in the products; drafts are so unequal that large ones are taken on their own
 struct alignas(16) TreeInfo {
-    int ek, ev, v0, v1, odd;               // exponents of K and V; keys that count in the tile's halves; a drafted value is not finite
+    int ek, ev, v0, v1, odd;               // exponents of K and V; keys that count in the tile's halves; of drafts: TA_ODD, TA_WIDE
 };
 
 struct TreeCtl {
@@ -94,7 +95,9 @@ struct TreeCtl {
     uint64_t s_full[2], p_full[2], pv_done[2], unit_full[TA_UNITS], unit_empty[TA_UNITS], together, drain;
     unsigned long long sees[2][AG_TREE_MAX];
     float row_scale[2][TA_TILE];
-    float2 stats[2 * TA_TILE];
+    float2 stats[2 * TA_TILE], sums[2 * TA_TILE];          // of a lane's row: its own part's (maximum, sum); all parts'
+    uint32_t draft_top[TA_UNITS][AG_TREE_MAX];             // WIDE: largest finite element of a large drafted key, as bf16; 0: the key has the tile's exponent
+    unsigned long long big[TA_UNITS];                      // WIDE: drafted tokens whose values stay out of the products
     TreeUnit unit[TA_UNITS];
     TreeInfo info[TA_INFO];
     int valid[TA_INFO][2];
@@ -134,7 +137,10 @@ __device__ __forceinline__ Scale2 scale_pair(uint32_t lo, uint32_t hi, float k24
     return Scale2{pack_f16(s0 * k24, s1 * k24), pack_f16(s0 * k20, s1 * k20), pack_f16(bf16_hi(lo) * k0, bf16_hi(hi) * k0)};
 }
 
-__device__ __forceinline__ float odd_part(float v) { return fabsf(v) < INFINITY ? 0.f : v; }
+// exponent under which a drafted key is taken: a large one's own, or the tile's
+__device__ __forceinline__ int key_exponent(uint32_t top, int ek) { return top ? min((int)(top >> 7) - 127 + 6, 133) : ek; }
+// what a row sees of a drafted value that is not in the products: with the probability p of a token whose value is large, 0 otherwise
+__device__ __forceinline__ float left_out(float p, float v) { return fabsf(v) < INFINITY ? (p == 0.f ? 0.f : p * v) : v; }
 
 // A request: its drafted tokens, cached tokens and places in the line.
 struct TreeSeq {
@@ -420,7 +426,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                 int odd = 0;
                 if (un.tile0 + j == 0) {
                     // the largest magnitudes by their bits, two elements of a word side by side; four pieces of 16 bytes of K and of V in flight
-                    uint32_t most[2] = {0, 0};
+                    uint32_t most[2] = {0, 0}, first = 0;                       // (first: of this lane's piece of the first token, K's high, V's low)
                     const int pieces = un.n * (D / 8);
 #pragma unroll 1
                     for (int i0 = lane; i0 < pieces; i0 += 128) {
@@ -433,23 +439,48 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                         }
 #pragma unroll
                         for (int q = 0; q < 8; ++q) {
-                            most[q >> 2] = __vmaxu2(most[q >> 2], __vmaxu2(__vmaxu2(raw[q].x & 0x7fff7fffu, raw[q].y & 0x7fff7fffu), __vmaxu2(raw[q].z & 0x7fff7fffu, raw[q].w & 0x7fff7fffu)));
+                            const uint32_t m = __vmaxu2(__vmaxu2(raw[q].x & 0x7fff7fffu, raw[q].y & 0x7fff7fffu), __vmaxu2(raw[q].z & 0x7fff7fffu, raw[q].w & 0x7fff7fffu));
+                            most[q >> 2] = __vmaxu2(most[q >> 2], m);
+                            if ((q & 3) == 0 && i0 < D / 8) first |= max(m & 0xffffu, m >> 16) << (q ? 0 : 16);
                         }
                     }
+                    uint32_t all[2], of_first[2];
 #pragma unroll
                     for (int which = 0; which < 2; ++which) {
-                        const uint32_t bits = max(most[which] & 0xffffu, most[which] >> 16);
-                        top[which] = __uint_as_float(bits << 16);
-                        if (__any_sync(0xffffffffu, bits >= 0x7f80u)) {            // some are not finite: the largest of the others
-                            odd |= which;
-                            top[which] = 0.f;
-                            const uint16_t* rows = (which ? x.V + (long long)un.token0 * x.v_stride : x.K + (long long)un.token0 * x.k_stride) + un.head * D;
+                        all[which] = __reduce_max_sync(0xffffffffu, max(most[which] & 0xffffu, most[which] >> 16));
+                        of_first[which] = __reduce_max_sync(0xffffffffu, which ? first & 0xffffu : first >> 16);
+                        top[which] = __uint_as_float(all[which] << 16);
+                    }
+                    // A draft may be far larger than those that the rows beside it see (a branch gone astray, padding), or not finite.  Above 2^6 times the first token's, a key is taken under a
+                    // power of two of its own, and a value stays out of the products: rows that see it get it at the end of the unit.
+                    constexpr uint32_t room = 6 << 7;                              // 2^6 in the bits of a bf16
+                    if (max(all[0], all[1]) >= 0x7f80u || (of_first[0] && all[0] > of_first[0] + room) || (of_first[1] && all[1] > of_first[1] + room)) {
+                        uint32_t* tops = ctl->draft_top[u % TA_UNITS];
+                        int not_finite = 0;
 #pragma unroll 1
-                            for (int i = lane; i < un.n * D; i += 32) {
-                                const float v = __uint_as_float((uint32_t)rows[i / D * (which ? x.v_stride : x.k_stride) + i % D] << 16);
-                                if (fabsf(v) < INFINITY) top[which] = fmaxf(top[which], fabsf(v));
+                        for (int t = 0; t < un.n; ++t) {
+                            uint32_t m[2] = {0, 0};
+#pragma unroll 1
+                            for (int d = lane; d < D; d += 32) {
+                                const uint32_t k = x.K[(un.token0 + (long long)t) * x.k_stride + un.head * D + d] & 0x7fffu, v = x.V[(un.token0 + (long long)t) * x.v_stride + un.head * D + d] & 0x7fffu;
+                                m[0] = max(m[0], k < 0x7f80u ? k : 0u);
+                                m[1] = max(m[1], v < 0x7f80u ? v : 0u);
+                                not_finite |= v >= 0x7f80u;
                             }
+                            const uint32_t both = __reduce_max_sync(0xffffffffu, m[0]) << 16 | __reduce_max_sync(0xffffffffu, m[1]);
+                            if (lane == 0) tops[t] = both;
                         }
+                        __syncwarp();
+                        const uint32_t t0 = lane < un.n ? tops[lane] : 0, t1 = lane + 32 < un.n ? tops[lane + 32] : 0, of0 = __shfl_sync(0xffffffffu, t0, 0);
+                        const uint32_t limit = of0 & 0xffffu ? (of0 & 0xffffu) + room : 0xffffu, key_limit = of0 >> 16 ? (of0 >> 16) + room : 0xffffu;
+                        const uint32_t k0 = t0 >> 16, k1 = t1 >> 16, w0 = t0 & 0xffffu, w1 = t1 & 0xffffu;
+                        const unsigned long long big = __ballot_sync(0xffffffffu, w0 > limit) | (unsigned long long)__ballot_sync(0xffffffffu, w1 > limit) << 32;
+                        if (lane == 0) ctl->big[u % TA_UNITS] = big;
+                        tops[lane] = k0 > key_limit ? k0 : 0;
+                        tops[lane + 32] = k1 > key_limit ? k1 : 0;
+                        top[0] = __uint_as_float(max(k0 > key_limit ? 0u : k0, k1 > key_limit ? 0u : k1) << 16);
+                        top[1] = __uint_as_float(max(w0 > limit ? 0u : w0, w1 > limit ? 0u : w1) << 16);
+                        odd = TA_WIDE | (not_finite || big ? TA_ODD : 0);
                     }
                 } else {
 #pragma unroll 1
@@ -472,7 +503,8 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                     const uint32_t bits = __reduce_max_sync(0xffffffffu, __float_as_uint(top[which]));
                     e[which] = bits == 0 ? -1000 : min(max((int)(bits >> 23) - 127 + 6, -100), 133);
                 }
-                odd = __any_sync(0xffffffffu, odd);
+                odd = (int)__reduce_or_sync(0xffffffffu, (unsigned)odd);
+                __syncwarp();
                 if (e[1] > -1000 && (ev == 1000 || e[1] > ev)) ev = min(e[1] + 2, 133);     // (two binades of room, so that it seldom grows)
                 if (lane == 0) {
                     TreeInfo& f = ctl->info[n % TA_INFO];
@@ -762,7 +794,8 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                 } else {
                     if (!wait(&ctl->op_empty[stage], op_parity)) break;
                     // drafted tokens: 16 bytes of a row at a time, neighbouring threads at neighbouring ones; values' rows behind them are zeros
-                    const float k0 = times_pow2(1.f, -e);
+                    const bool wide = f.odd & TA_WIDE;
+                    const unsigned long long big = wide ? ctl->big[u % TA_UNITS] : 0;
                     const uint16_t* rows = which ? x.V + (long long)un.token0 * x.v_stride + un.head * D : x.K + (long long)un.token0 * x.k_stride + un.head * D;
                     const long long stride = which ? x.v_stride : x.k_stride;
                     constexpr int CH = D / 8;
@@ -772,6 +805,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                         const uint4 raw = *reinterpret_cast<const uint4*>(rows + t * stride + c * 8);
                         const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
                         uint8_t* line = to + t * 128;
+                        const float k0 = times_pow2(1.f, -(wide && !which ? key_exponent(ctl->draft_top[u % TA_UNITS][t], e) : e));
                         if (which == 0) {                                              // elements (0, 4, 1, 5, ..) of the chunk
                             uint32_t h[4];
 #pragma unroll
@@ -787,9 +821,9 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                             for (int g = 0; g < 8; ++g) {
                                 const float v = (g & 1 ? bf16_hi(w[g >> 1]) : bf16_lo(w[g >> 1])) * k0;
                                 const int chunk = D == 128 ? 2 * g + (c & 1) : g;
-                                // (what is not finite is put back at the end, for the rows that see it)
+                                // (what is not finite, or far larger than the rest, is put back at the end, for the rows that see it)
                                 *reinterpret_cast<uint16_t*>(line + (chunk >> 3) * (TA_TILE * 128) + (((chunk ^ t) & 7) << 4) + 2 * place) =
-                                    (uint16_t)pack_f16(fabsf(v) < INFINITY ? v : 0.f, 0.f);
+                                    (uint16_t)pack_f16(fabsf(v) < INFINITY && !(big >> t & 1) ? v : 0.f, 0.f);
                             }
                         }
                     }
@@ -843,12 +877,29 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                 const TreeInfo f = ctl->info[(n_tile + j) % TA_INFO];
                 const bool drafts = t0 + j == 0;
                 if (j == j0) rs = ctl->row_scale[buf][r & (distinct - 1)];
+                const bool wide = drafts && (f.odd & TA_WIDE);
                 const float c = fminf(fmaxf(times_pow2(rs, f.ek), 1e-37f), 3e38f);    // (not 0 or infinite: scores at -inf, scores of 0)
+                if (wide) {                                                    // scores from their keys' exponents to the tile's
+                    const uint32_t* tops = ctl->draft_top[u % TA_UNITS];
+#pragma unroll 1
+                    for (int b = 0; b < 4; ++b) {
+                        uint32_t v[16];
+                        tmem_ld_32x16(t_s + b * 16, v);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int e = key_exponent(tops[b * 16 + i], f.ek) - f.ek;
+                            v[i] = __float_as_uint(__uint_as_float(v[i]) * pow2i(e >> 1) * pow2i(e - (e >> 1)));
+                        }
+                        tmem_st_32x16(t_s + b * 16, v);
+                    }
+                    tmem_st_wait();
+                }
                 if (drafts || f.v0 < 64 || f.v1 < 64) {
                     // what is not seen: -inf, written over the scores (the drafted tokens, a row's last tile)
                     unsigned long long see[2] = {f.v0 >= 64 ? ~0ull : (1ull << f.v0) - 1, f.v1 >= 64 ? ~0ull : (1ull << f.v1) - 1};
                     if (drafts) {
-                        odd = f.odd;
+                        odd = f.odd & TA_ODD;
                         see[0] = live ? ctl->sees[buf][token_of(x, un.row0 + row)] : 0ull;
                     }
 #pragma unroll 1
@@ -980,6 +1031,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                 for (int k = 0; k < 8; ++k) all += part[k].y == 0.f ? 0.f : part[k].y * ex2_ftz(part[k].x - ref);
                 all *= two ? 0.125f : 0.25f * (1 << copies);
             }
+            ctl->sums[w * TA_TILE + r] = make_float2(ref, all);
             if (to_part && live) x.stats[(size_t)un.slot * x.part_rows + row] = make_float2(ref, all);    // (the copies of a row write the same)
             // factors of what this lane has in slot 0 (its own slot) and in slot 1; 0: what stands there does not count
             const int va = two ? w : 0;
@@ -1045,16 +1097,26 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                         v.w += y.w;
                     }
                     const int at = un.row0 + to_row, token = token_of(x, at);
-                    if (any_odd) {                                             // what the row sees of drafted values that are not finite
-                        const unsigned long long sees = ctl->sees[un.buf][token];
+                    if (any_odd) {                                             // what the row sees of drafted values that are not in the products
+                        const unsigned long long sees = ctl->sees[un.buf][token], big = ctl->big[u % TA_UNITS];
+                        const uint16_t* q = x.Q + (long long)(un.token0 + token) * x.q_stride + (un.head * x.G + at - token * x.G) * D;
 #pragma unroll 1
                         for (int t = 0; t < un.n; ++t) {
                             if (!(sees >> t & 1)) continue;
+                            float p = 0.f;
+                            if (big >> t & 1) {
+                                const uint16_t* key = x.K + (un.token0 + (long long)t) * x.k_stride + un.head * D;
+                                float dot = 0.f;
+#pragma unroll 1
+                                for (int d = 0; d < D; ++d) dot = fmaf(__uint_as_float((uint32_t)q[d] << 16), __uint_as_float((uint32_t)key[d] << 16), dot);
+                                const float2 of = ctl->sums[to_row];
+                                p = ex2_ftz(dot * x.scale_log2e - of.x + TA_SHIFT) / of.y;
+                            }
                             const uint2 y = *reinterpret_cast<const uint2*>(x.V + (un.token0 + (long long)t) * x.v_stride + un.head * D + d0);
-                            v.x += odd_part(bf16_lo(y.x));
-                            v.y += odd_part(bf16_hi(y.x));
-                            v.z += odd_part(bf16_lo(y.y));
-                            v.w += odd_part(bf16_hi(y.y));
+                            v.x += left_out(p, bf16_lo(y.x));
+                            v.y += left_out(p, bf16_hi(y.x));
+                            v.z += left_out(p, bf16_lo(y.y));
+                            v.w += left_out(p, bf16_hi(y.y));
                         }
                     }
                     if (to_part)
@@ -1124,6 +1186,7 @@ __global__ void __launch_bounds__(TJ_WARPS * 32) k_attn_tree_join(const TreeArgs
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     __syncwarp();
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
     float v[E];
 #pragma unroll
     for (int k = 0; k < E; ++k) v[k] = 0.f;
@@ -1131,7 +1194,7 @@ __global__ void __launch_bounds__(TJ_WARPS * 32) k_attn_tree_join(const TreeArgs
     for (int i = 0; i < n; ++i) {
         const int at = slot[warp][i];
         if (at < 0) continue;
-        const float f = weight[warp][i];
+        const float f = weight[warp][i] * inv;
         const float* from = x.part + ((size_t)at * x.part_rows + row) * D + lane * E;
         float u[E];
         if constexpr (E == 4) {
@@ -1144,11 +1207,10 @@ __global__ void __launch_bounds__(TJ_WARPS * 32) k_attn_tree_join(const TreeArgs
 #pragma unroll
         for (int k = 0; k < E; ++k) v[k] += f == 0.f && fabsf(u[k]) < INFINITY ? 0.f : f * u[k];
     }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
     const int at = c.row0 + row, token = token_of(x, at);
     uint16_t* out = x.O + (long long)(c.token0 + token) * x.o_stride + (c.head * x.G + at - token * x.G) * D + lane * E;
 #pragma unroll
-    for (int k = 0; k < E; k += 2) *reinterpret_cast<uint32_t*>(out + k) = pack_bf16(v[k] * inv, v[k + 1] * inv);
+    for (int k = 0; k < E; k += 2) *reinterpret_cast<uint32_t*>(out + k) = pack_bf16(v[k], v[k + 1]);
 }
 
 static bool tree_shape_ok(long long n_seq, int max_tokens, int H_q, int H_kv, int D, int max_pages) {

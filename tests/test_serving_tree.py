@@ -228,6 +228,36 @@ def test_values_that_are_not_finite_in_every_layout_of_rows(D, count, lens):
     assert (got[fine] == plain[fine]).all() and not fine.all()
 
 
+@pytest.mark.parametrize("D,counts,lens", [(64, [9, 30], [100, 0]), (128, [20, 4], [900, 70]), (128, [60], [300]), (64, [12] * 60, [50] * 60)])
+def test_drafts_far_larger_than_the_others(D, counts, lens):
+    """Keys and values up to the type's lowest value in single drafts (padding, say): tokens that do not see them are as the formula has them, and those that see such a value as well."""
+    c = make([max(x, 1) for x in lens], 2, D, seed=67)
+    n, off = sum(counts), np.concatenate([[0], np.cumsum(counts)])
+    par = parents(counts, 9)
+    sees = [drafts.ancestors(par[a:b], b - a) for a, b in zip(off[:-1], off[1:])]
+    Q, K, V = rows(n, 8, D, 1), rows(n, 2, D, 2), rows(n, 2, D, 3)
+    plain = run(Q, K, V, c, off, par, 8, 64)
+    check(plain, Q, K, V, c, off, par, 4)
+    for scale, which in ((2.0 ** 7, "V"), (2.0 ** 40, "V"), (2.0 ** 127, "V"), (2.0 ** 20, "K"), (2.0 ** 127, "K"), (2.0 ** 127, "KV")):
+        K2, V2, touched = K.copy(), V.copy(), np.zeros(n, bool)
+        for s, (a, b) in enumerate(zip(off[:-1], off[1:])):
+            for t in (2, int(b - a) - 1):
+                for x in which:
+                    X = K2 if x == "K" else V2
+                    X[a + t] = 0xFF7F if scale == 2.0 ** 127 else kv4.bf16_bits(kv4.f32_to_bf16_value((bf16_to_f64(X[a + t]) * scale).astype(np.float32)))
+                touched[a:b] |= [bool(sees[s][i, t]) for i in range(b - a)]
+        got = run(Q, K2, V2, c, off, par, 8, 64)
+        with np.errstate(over="ignore", invalid="ignore"):
+            want, mass, reach = drafts.tree(Q, K2, V2, drafts.cache_of(c.pages, D, c.page_of, c.len), off, par, 4)
+        # values below 12 (the cache's largest base + 15 scales beside them), or up to 2^6 times a first token's that are in the products; larger ones by probabilities in 32 bits
+        e = 2.0 ** -11 * reach + 2.0 ** -19 * np.abs(bf16_to_f64(Q)).sum(-1, keepdims=True) * 12 / np.sqrt(D)
+        bound = 2.0 ** -8 * np.abs(want) + (2.0 ** -9 + 4 * e + 2.0 ** -20) * mass + 2.0 ** -17 * 2.0 ** 6 * 12 + 1e-30
+        assert (np.abs(got - want) <= bound)[~touched].all() and touched.any() and not touched.all()
+        if which == "V":
+            fine = touched & (np.abs(want).max((1, 2)) < 3e38)
+            assert (np.abs(got - want) <= bound)[fine].all(), float((np.abs(got - want) / bound)[fine].max())
+
+
 def test_groups_of_nan_in_the_cache():
     c = make([70, 70], 1, 64, seed=23)
     at = kv4.scale_byte(64, 1, 3, 1)
