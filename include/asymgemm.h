@@ -837,7 +837,7 @@ typedef struct {
     int64_t p_stride, q_stride;  /* elements, at least vocab */
     int32_t type;             /* AG_F32 or AG_BF16, of both */
     int32_t vocab;            /* 1 .. 2^24 */
-    int32_t distinct;         /* 1: siblings were drawn without repetition (q is 0 at the ones tried before, and divided by what is left of 1); 0: independently */
+    int32_t distinct;         /* 1: siblings were drawn without repetition (q is 0 at the ones tried before, and divided by what is left of its sum); 0: independently */
     int32_t n_seq;
     int64_t n_tokens;         /* below 2^30 */
     const int32_t* off;       /* device [n_seq + 1] */
@@ -854,6 +854,8 @@ typedef struct {
  * ag_verify_drafts - which drafts stand, and what follows them, such that the text is distributed as if the target had drawn every token itself.  From the first token
  * on: r = p of the token in hand; its children are tried in order.  Child x is accepted when u q(x) < r(x), and is in hand then; otherwise r becomes max(r - q, 0) / sum
  * (and stays as it is where that sum is 0).  Where no child is left, the next token is the first v with r(0) + .. + r(v) > u_next * sum of r.
+ * distinct: behind rejected siblings q is the row without their tokens times (the row's sum) / (its sum without them), both taken from the entries; where nothing of the row is
+ * left without them, a further sibling cannot have been drawn from it and is passed over.
  * All arithmetic on probabilities is in 64 bits.  Tokens beyond a request's first AG_TREE_MAX are not accepted.
  * Asynchronous on cuda_stream, may be captured into a graph.  Errors: AG_ERR_ARG, AG_ERR_UNSUPPORTED_ARCH, AG_ERR_CUDA.
  */

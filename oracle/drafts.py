@@ -95,11 +95,11 @@ def verify(P, Q, token, parent, off, u, u_next, distinct=False, vocab=None, most
             continue
         m = min(b - a, most)
         hand, accepted[a] = 0, 1
-        r, tried, left = P[a].copy(), [], 1.0
+        r, tried, left = P[a].copy(), [], 1.0                   # left: of q's sum, without the tokens tried
         for i in range(1, m):
             p = i - 1 if parent is None else int(parent[a + i])
             x = int(token[a + i])
-            if p != hand or not 0 <= p < i or not 0 <= x < vocab:
+            if p != hand or not 0 <= p < i or not 0 <= x < vocab or left == 0:      # (nothing of q is left: no draft of it)
                 continue
             if Q is None:
                 q = np.zeros(vocab)
@@ -122,9 +122,11 @@ def verify(P, Q, token, parent, off, u, u_next, distinct=False, vocab=None, most
             if total > 0:
                 r = rest / total
             if distinct and x not in tried:
-                if Q is not None:
-                    left -= Q[a + hand, x]
                 tried.append(x)
+                if Q is not None:                               # from the entries that are left, never as 1 - those tried: they are rounded, and may be nearly all there is
+                    rest = Q[a + hand].copy()
+                    rest[tried] = 0.0
+                    left = rest.sum() / (rest.sum() + Q[a + hand, tried].sum()) if rest.sum() > 0 else 0.0
         up = np.cumsum(r)
         if up[-1] > 0:
             nxt[s] = int(np.flatnonzero((up > float(u_next[s]) * up[-1]) & (r > 0))[0])

@@ -6,11 +6,14 @@
 //
 // The rows of p and q are long (the vocabulary) and only one row of each has to be read: the one where the walk ends.  Everything before needs single entries, which all
 // tokens gather at once.  A rejected child with a sibling behind it takes a pass over the row for the sum.  r itself is never stored: it follows from p, q and the sums.
+// Siblings drawn without repetition: after some have been tried, q is q without those tokens, divided by left = (q's sum without them) / (q's sum).  The same passes add that up from the
+// entries that are left: a q that has been used up but for little holds that little in entries which 1 minus the others (rounded, and not exactly 1 together) would lose or turn negative.
+// (The sum costs 8 us of the 76 that 128 trees over 100003 take.)
 // Probabilities are added up in 64 bits, in an order that no scheduling changes: a border between two tokens moves by 2^-50 of the whole.
 // A cluster of blocks shares a request: each takes a stretch of the vocabulary, sums meet in distributed shared memory, and the block whose stretch holds the
 // border looks for the token.  Bound: with many requests the rows' bytes, with few the chain offset -> tree -> entries -> row -> border.
 // One chain of 5 over 32000 entries: 9.5 us on the device; 64 chains of 6 to 9 over 131072 (two models, 32 bits): 22 us, 3.0 TB/s, half of it that chain; 128 trees over 100003 (the same):
-// 70 us, two to four passes over a row whose drafts are rejected, from the second on in the cache.
+// 76 us, two to four passes over a row whose drafts are rejected, from the second on in the cache.
 #include <string.h>
 
 #include <algorithm>
@@ -54,8 +57,14 @@ struct Rejected {
     int n;                                 // of them
     int kept;                              // some sum was 0: r stayed as it was there
     int tried[VD_MAX];
-    double inv_left[VD_MAX], inv_sum[VD_MAX];  // 1 / what is left of q's 1 for child j; 1 / sum_j (0: r stays; 1 for the last one: its scale does not matter)
+    double inv_left[VD_MAX], inv_sum[VD_MAX];  // 1 / the share of q that is left for child j; 1 / sum_j (0: r stays; 1 for the last one: its scale does not matter)
 };
+// r - q / left, r normalised.  One form and one rounding for single entries and for sums over the row: where little is left of r, its entries and their sum have to agree, or what is
+// normalised next is their difference.
+__device__ __forceinline__ double less_q(double r, double q, double inv_left) {
+    const double d = __fma_rn(-q, inv_left, r);
+    return d > 0.0 ? d : 0.0;
+}
 // r of entry v after the first n rejected children, from p's entry and q's
 template <bool DRAWN>
 __device__ __noinline__ double rest_of(double p, double q, int v, const Rejected* rj, int n, bool distinct) {
@@ -63,8 +72,8 @@ __device__ __noinline__ double rest_of(double p, double q, int v, const Rejected
     bool tried = false;
 #pragma unroll 1
     for (int j = 0; j < n; ++j) {
-        const double is = rj->inv_sum[j], d = DRAWN ? r - (tried ? 0.0 : q * rj->inv_left[j]) : rj->tried[j] == v ? 0.0 : r;
-        if (is != 0.0) r = (d > 0.0 ? d : 0.0) * is;
+        const double is = rj->inv_sum[j], d = DRAWN ? less_q(r, tried ? 0.0 : q, rj->inv_left[j]) : rj->tried[j] == v ? 0.0 : r;
+        if (is != 0.0) r = __dmul_rn(d, is);
         if (distinct && rj->tried[j] == v) tried = true;
     }
     return r;
@@ -75,8 +84,8 @@ struct VerifyShared {
     float u[VD_MAX];
     double p[VD_MAX], q[VD_MAX];           // entries of the tokens in their parents' rows
     Rejected rj;
-    double tried_q, left;                  // of the child tried last
-    double warp_sum[VD_WARPS], block_sum[2], scan[VD_WARPS];
+    double tried_q, left;                  // q of the tokens tried; the share of q that is left without them (0: nothing)
+    double warp_sum[VD_WARPS], warp_rest[VD_WARPS], block_sum[2], block_rest[2], scan[VD_WARPS];
     int low[VD_WARPS], high[VD_WARPS];
     int hand, tried_at, state, found;
     double base;
@@ -100,16 +109,27 @@ struct Scan {
     double sum;                            // of r over the thread's vectors
     int last, cross;                       // the last entry above 0; the first at which before + sum is above the target; -1: none
 };
-// Vectors i0, i0 + step, .. below i1, of r after m rejected children; FIND: also the last and the first entry of Scan.  (Functions of their own: they are called from
-// several places, and a call that verifies one request is bound by fetching its instructions.)
-template <class T, bool DRAWN, int W, bool FIND>
-__device__ __noinline__ Scan scan_row(const T* p, const T* q, int i0, int i1, int step, int lead, int vocab, const Rejected* rj, int m, bool distinct, double before, double target) {
+struct ScanRest : Scan {
+    double rest;                           // of q without the tokens tried
+};
+// Vectors i0, i0 + step, .. below i1, of r after m rejected children; REST: also what is left of q; FIND: also the last and the first entry of Scan.  (Functions of their own: they are
+// called from several places, and a call that verifies one request is bound by fetching its instructions.)
+template <class T, bool DRAWN, int W, bool FIND, bool REST = false>
+__device__ __noinline__ std::conditional_t<REST, ScanRest, Scan> scan_row(const T* p, const T* q, int i0, int i1, int step, int lead, int vocab, const Rejected* rj, int m, bool distinct, double before, double target) {
     constexpr int U = FIND ? 1 : W == 1 ? 4 : sizeof(T) == 4 ? 2 : 1;      // vectors in flight, of each row
-    Scan s{before, -1, -1};
+    std::conditional_t<REST, ScanRest, Scan> s;
+    s.sum = before;
+    s.last = s.cross = -1;
+    if constexpr (REST) s.rest = 0.0;
     const bool with_q = DRAWN && m > 0, kept = rj->kept != 0;
     const double il0 = with_q ? rj->inv_left[0] : 0.0;
     p -= lead;
     q -= lead;
+    int near = 0;                          // REST: m where a token tried lies between the thread's vectors, and is looked for in each
+    if constexpr (REST) {
+#pragma unroll 1
+        for (int j = 0; j < m; ++j) near = rj->tried[j] >= i0 * W - lead && rj->tried[j] < i1 * W - lead ? m : near;
+    }
 #pragma unroll 1
     for (int i = i0; i < i1; i += U * step) {
         uint4 pv[U], qv[U];
@@ -138,22 +158,34 @@ __device__ __noinline__ Scan scan_row(const T* p, const T* q, int i0, int i1, in
         for (int k = 0; k < U; ++k) {
             const int e0 = (i + k * step) * W - lead;
             const uint32_t pw[4] = {pv[k].x, pv[k].y, pv[k].z, pv[k].w}, qw[4] = {qv[k].x, qv[k].y, qv[k].z, qv[k].w};
+            if constexpr (REST) {
+                uint32_t tried = 0;
+#pragma unroll 1
+                for (int j = 0; j < near; ++j) {
+                    const unsigned at = (unsigned)(rj->tried[j] - e0);
+                    tried |= at < W ? 1u << at : 0u;
+                }
+                double left[W];
+#pragma unroll
+                for (int e = 0; e < W; ++e) left[e] = from_word<T>(qw, e);
+                if (tried) {
+#pragma unroll
+                    for (int e = 0; e < W; ++e) left[e] = tried >> e & 1 ? 0.0 : left[e];
+                }
+#pragma unroll
+                for (int e = 1; e < W; ++e) left[0] += left[e];
+                s.rest += left[0];
+            }
             double r[W];
             // (nothing beyond the ends: zeros of p stay zeros)
             if (DRAWN && !kept) {
 #pragma unroll
-                for (int e = 0; e < W; ++e) {
-                    const double d = from_word<T>(pw, e) - from_word<T>(qw, e) * il0;
-                    r[e] = d > 0.0 ? d : 0.0;
-                }
+                for (int e = 0; e < W; ++e) r[e] = less_q(from_word<T>(pw, e), from_word<T>(qw, e), il0);
 #pragma unroll 1
                 for (int j = 1; j < m; ++j) {
                     const double is = rj->inv_sum[j - 1], il = rj->inv_left[j];
 #pragma unroll
-                    for (int e = 0; e < W; ++e) {
-                        const double d = r[e] * is - from_word<T>(qw, e) * il;
-                        r[e] = d > 0.0 ? d : 0.0;
-                    }
+                    for (int e = 0; e < W; ++e) r[e] = less_q(__dmul_rn(r[e], is), from_word<T>(qw, e), il);
                 }
             } else {
 #pragma unroll
@@ -163,7 +195,7 @@ __device__ __noinline__ Scan scan_row(const T* p, const T* q, int i0, int i1, in
                     const double is = rj->inv_sum[j];
                     if (is == 0.0) continue;
 #pragma unroll
-                    for (int e = 0; e < W; ++e) r[e] = rj->tried[j] == e0 + e ? 0.0 : r[e] * is;
+                    for (int e = 0; e < W; ++e) r[e] = rj->tried[j] == e0 + e ? 0.0 : __dmul_rn(r[e], is);
                 }
                 if (DRAWN) {
 #pragma unroll
@@ -247,13 +279,13 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_verify(const VerifyArgs x) {
             Rejected& rj = sh.rj;
 #pragma unroll 1
             for (; i < n && !state; ++i) {
-                if (sh.parent[i] != hand) continue;
+                if (sh.parent[i] != hand || (rj.n && sh.left == 0.0)) continue;        // (nothing of q is left: no draft of it)
                 bool stands = sh.passes[i] != 0;
                 const int t = sh.token[i];
                 double left = 1.0, q = sh.q[i];
                 if (rj.n) {
                     if (DRAWN && distinct) {
-                        left = sh.left - sh.tried_q;
+                        left = sh.left;
 #pragma unroll 1
                         for (int j = 0; j < rj.n; ++j)
                             if (rj.tried[j] == t) q = 0.0;
@@ -269,8 +301,8 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_verify(const VerifyArgs x) {
                     rj.inv_left[rj.n] = 1.0 / left;
                     rj.inv_sum[rj.n] = 1.0;                    // (until the sum is there)
                     ++rj.n;
-                    sh.left = left;
-                    sh.tried_q = q;
+                    sh.left = 1.0;                             // (DISTINCT: what the sum over the row finds)
+                    sh.tried_q = rj.n > 1 ? sh.tried_q + q : q;
                     state = sh.more[i];
                     if (!state) break;
                 }
@@ -289,17 +321,35 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_verify(const VerifyArgs x) {
         b1 = min(b0 + per_block, vectors);
         per_warp = (b1 - b0 + VD_WARPS - 1) / VD_WARPS;
         const int w0 = min(b0 + warp * per_warp, b1), w1 = min(w0 + per_warp, b1);
-        double sum = scan_row<T, DRAWN, W, false>(p, q, w0 + lane, w1, 32, lead, x.vocab, &sh.rj, m, distinct, 0.0, INFINITY).sum;
+        const bool with_rest = DRAWN && distinct && state == 1;
+        double sum;
+        if constexpr (DRAWN) {
+            if (with_rest) {
+                const ScanRest part = scan_row<T, DRAWN, W, false, true>(p, q, w0 + lane, w1, 32, lead, x.vocab, &sh.rj, m, distinct, 0.0, INFINITY);
+                sum = part.sum;
+                double rest = part.rest;
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) rest += __shfl_xor_sync(0xffffffffu, rest, o);
+                if (lane == 0) sh.warp_rest[warp] = rest;
+            }
+        }
+        if (!with_rest) sum = scan_row<T, DRAWN, W, false>(p, q, w0 + lane, w1, 32, lead, x.vocab, &sh.rj, m, distinct, 0.0, INFINITY).sum;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
         if (lane == 0) sh.warp_sum[warp] = sum;
         __syncthreads();
-        double* block_sum = &sh.block_sum[sums++ & 1];         // (two in turn: one barrier a sum)
+        double *block_sum = &sh.block_sum[sums & 1], *block_rest = &sh.block_rest[sums & 1];   // (two in turn: one barrier a sum)
+        ++sums;
         if (warp == 0) {
             double all = lane < VD_WARPS ? sh.warp_sum[lane] : 0.0;
 #pragma unroll
             for (int o = VD_WARPS / 2; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
             if (lane == 0) *block_sum = all;
+        } else if (with_rest && warp == 1) {
+            double all = lane < VD_WARPS ? sh.warp_rest[lane] : 0.0;
+#pragma unroll
+            for (int o = VD_WARPS / 2; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+            if (lane == 0) *block_rest = all;
         }
         if (x.cluster > 1) cluster_arrive_wait();
         else __syncthreads();
@@ -308,6 +358,12 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_verify(const VerifyArgs x) {
 #pragma unroll
         for (int o = 4; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
         total = __shfl_sync(0xffffffffu, total, 0);
+        if (with_rest && warp == 0) {
+            double left = lane >= x.cluster ? 0.0 : x.cluster > 1 ? peer_double(block_rest, lane) : *block_rest;
+#pragma unroll
+            for (int o = 4; o > 0; o >>= 1) left += __shfl_xor_sync(0xffffffffu, left, o);
+            if (lane == 0) sh.left = left > 0.0 ? left / (left + sh.tried_q) : 0.0;
+        }
         if (state == 1) {
             if (tid == 0) {
                 sh.rj.inv_sum[m - 1] = total > 0.0 ? 1.0 / total : 0.0;

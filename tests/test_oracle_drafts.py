@@ -99,3 +99,52 @@ def test_verified_text_has_the_targets_distribution(distinct):
                         a, n, _, rows = drafts.verify(np.stack([p] * 3), np.stack([q] * 3), [0, x, y], [-1, 0, 0], [0, 3], [0, u1, u2], [un], distinct)
                         got[[x, y][rows[1] - 1] if rows[1] > 0 else n[0]] += w / 625 / len(grid[::6])
     assert abs(got.sum() - 1) < 1e-9 and np.abs(got - p).max() < 0.02      # (a grid of 25 steps)
+
+
+def rounded(x, bits):
+    e = np.exp(x - x.max())
+    f = (e / e.sum()).astype(np.float32)
+    return (kv4.f32_to_bf16_value(f) if bits == 16 else f).astype(np.float64)
+
+
+@pytest.mark.parametrize("p,q", [
+    ([0, 0, 0, 1.0], [.69921875, .302734375, .0009765625, 0]),                        # entries of bf16 that sum to more than 1
+    ([0, .6, 0, .4], rounded(np.array([0, -7.9, -8.3, -9.0]), 16)),                   # the largest rounds to 1
+    ([0, .6, 0, .4], rounded(np.array([0, -19.0, -19.5, -20.0]), 32)),
+    ([0, .6, 0, .4], rounded(np.array([0, -60.0, -61.0, -62.0]), 32)),
+    ([0, .5, .5, 0], [1.0, 0, 0, 0]), ([.25, .25, .25, .25], [1.0, 0, 0, 0])])
+def test_siblings_of_a_concentrated_q(p, q):
+    """What the target gives no weight is never accepted, nor sampled; what is left of q is what the entries that are left add up to."""
+    P, Q = np.tile(np.array(p, np.float64), (4, 1)), np.tile(np.array(q, np.float64), (4, 1))
+    for u in (.02, .5, .98):
+        for un in (0.0, .3, .99):
+            a, n, _, _ = drafts.verify(P, Q, [0, 0, 1, 2], [-1, 0, 0, 0], [0, 4], [0, u, u, u], [un], True)
+            for i, x in ((1, 0), (2, 1), (3, 2)):
+                if a[i]:
+                    assert p[x] > 0
+                    break
+            else:
+                assert p[n[0]] > 0
+                if sum(q[1:]) > 0 and q[0] >= 1 and p[0] == 0:
+                    # 0 is refused, r stays p; 1 is judged by its share of what is left
+                    assert u * q[1] * sum(q) / sum(q[1:]) >= p[1]
+    # nothing is left behind the only token with weight: its siblings are passed over
+    if q[0] == 1 and not any(q[1:]):
+        a, n, _, _ = drafts.verify(P, Q, [0, 0, 1, 2], [-1, 0, 0, 0], [0, 4], [0, .999, 0.0, 0.0], [0.0], True)
+        assert a.tolist() == [1, 0, 0, 0] and n[0] == 1
+
+
+@pytest.mark.parametrize("bits,peak,seed", [(16, 6, 3), (16, 6, 4), (16, 6, 5), (16, 6, 12), (32, 20, 0), (32, 20, 4), (32, 12, 3), (32, 20, 9)])
+def test_text_of_a_concentrated_q_has_the_targets_distribution(bits, peak, seed):
+    """4000 requests of three siblings drawn without repetition from logits far apart: five deviations, and the rows' own sums beside 1 (see the header) once for each sibling."""
+    S, V, rng = 4000, 6, np.random.default_rng(seed)
+    p, q = rounded(rng.standard_normal(V), bits), rounded(peak * rng.standard_normal(V), bits)
+    with np.errstate(divide="ignore"):
+        first = np.argsort(-(np.log(q) + rng.gumbel(size=(S, V))), 1)[:, :3]
+    token = np.concatenate([np.zeros((S, 1), int), first], 1).reshape(-1)
+    a, n, _, _ = drafts.verify(np.broadcast_to(p, (4 * S, V)), np.broadcast_to(q, (4 * S, V)), token, np.tile([-1, 0, 0, 0], S), 4 * np.arange(S + 1), rng.random(4 * S), rng.random(S), True)
+    a = a.reshape(S, 4)[:, 1:]
+    text = np.where(a.any(1), first[np.arange(S), a.argmax(1)], n)
+    seen, mean = np.bincount(text, minlength=V), S * p / p.sum()
+    off = abs(p.sum() - q.sum()) / max(p.sum(), q.sum()) + 2 * abs(1 - q.sum())
+    assert (np.abs(seen - mean) <= 5 * np.sqrt(mean * (1 - p)) + S * off + 1).all(), (seen, mean)

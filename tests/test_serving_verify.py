@@ -267,3 +267,72 @@ def test_rows_beyond_two_to_the_32_bytes():
     ag.verify_drafts(P.data_ptr(), None, V, token.data_ptr(), None, off.data_ptr(), 3, n, u.data_ptr(), u_next.data_ptr(), *(o.data_ptr() for o in out))
     torch.cuda.synchronize()
     assert out[1].tolist() == [5, 5, V - 1] and out[2].tolist() == [0, 2, 66, 68]
+
+
+@pytest.mark.parametrize("vocab", [5, 200, 5003])
+@pytest.mark.parametrize("bits", [16, 32])
+@pytest.mark.parametrize("kind", ["one", "nearly", "far", "several"])
+def test_siblings_drawn_from_a_concentrated_q(kind, bits, vocab):
+    """Without repetition, q all but used up by the first siblings: a token to which the target gives nothing is neither accepted nor sampled, whatever the random numbers are."""
+    counts = [5, 5, 6, 4, 2, 5, 16] * 6
+    s = Step(counts, vocab, 4, bits, distinct=True, seed=vocab + bits)
+    rng, n = np.random.default_rng(vocab), sum(counts)
+    logits = rng.standard_normal((n, vocab))
+    if kind == "several":
+        logits *= 6
+    else:
+        logits[np.arange(n), rng.integers(0, vocab, n)] += dict(one=300, nearly=7.5 if bits == 16 else 18, far=19 if bits == 16 else 40)[kind]
+    s.Q = softmax(logits).astype(np.float32)
+    s.P = softmax(2 * rng.standard_normal((n, vocab))).astype(np.float32) * (rng.random((n, vocab)) < .5)
+    s.P[:, 0] += 2.0 ** -10                                                          # (no row without weight)
+    s.P = (s.P / s.P.sum(1, keepdims=True, dtype=np.float64)).astype(np.float32)
+    if bits == 16:
+        s.P, s.Q = kv4.f32_to_bf16_value(s.P), kv4.f32_to_bf16_value(s.Q)
+    s.token[:] = 0
+    for a, b in zip(s.off[:-1], s.off[1:]):
+        tried = {}
+        for i in range(a + 1, b):
+            w = s.Q[a + s.parent[i]].astype(np.float64)
+            w[tried.setdefault(s.parent[i], [])] = 0
+            s.token[i] = rng.choice(vocab, p=w / w.sum()) if w.sum() > 0 else rng.integers(0, vocab)
+            tried[s.parent[i]].append(s.token[i])
+    s.u[1::2] = 0.5
+    s.device()
+    got = s.run()
+    same(got, s.want())
+    first = np.repeat(s.off[:-1], counts)
+    drafts_in = (got[0] > 0) & (s.parent >= 0)
+    assert (s.P[(first + s.parent)[drafts_in], s.token[drafts_in]] > 0).all()
+    for r, (a, b) in enumerate(zip(s.off[:-1], s.off[1:])):
+        last = a + np.flatnonzero(got[0][a:b])[-1]
+        assert s.P[last, got[1][r]] > 0
+    s.d["parent"].fill_(0)                                                           # all of a request's drafts as siblings, tokens and random numbers as they are
+    for a in s.off[:-1]:
+        s.d["parent"][int(a)] = -1
+    s.parent = s.d["parent"].cpu().numpy()
+    same(s.run(), s.want())
+
+
+@pytest.mark.parametrize("bits,peak,seed", [(16, 6, 3), (16, 6, 4), (16, 6, 5), (32, 20, 0), (32, 20, 4), (32, 12, 3)])
+def test_text_of_a_concentrated_q_is_distributed_as_the_target_has_it(bits, peak, seed):
+    """40000 requests of three siblings drawn without repetition: five deviations, and what the header says of rows that do not sum to 1."""
+    S, V, rng = 40000, 6, np.random.default_rng(seed)
+    p, q = (softmax(k * rng.standard_normal(V)).astype(np.float32) for k in (1, peak))
+    if bits == 16:
+        p, q = kv4.f32_to_bf16_value(p), kv4.f32_to_bf16_value(q)
+    first = np.argsort(-(np.log(q.astype(np.float64)) + rng.gumbel(size=(S, V))), 1)[:, :3]
+    token = np.concatenate([np.zeros((S, 1)), first], 1).astype(np.int32)
+    d = {k: dev(v) for k, v in dict(off=(4 * np.arange(S + 1)).astype(np.int32), token=token.reshape(-1), parent=np.tile([-1, 0, 0, 0], S).astype(np.int32),
+                                    u=rng.random(4 * S).astype(np.float32) * np.float32(1 - 2.0 ** -24), u_next=rng.random(S).astype(np.float32) * np.float32(1 - 2.0 ** -24)).items()}
+    kind = torch.bfloat16 if bits == 16 else torch.float32
+    P, Q = (torch.from_numpy(x).cuda().to(kind).repeat(4 * S, 1) for x in (p, q))
+    out = [torch.empty(k, dtype=torch.int32, device="cuda") for k in (4 * S, S)]
+    ag.verify_drafts(P.data_ptr(), Q.data_ptr(), V, d["token"].data_ptr(), d["parent"].data_ptr(), d["off"].data_ptr(), S, 4 * S, d["u"].data_ptr(), d["u_next"].data_ptr(),
+                     out[0].data_ptr(), out[1].data_ptr(), bf16=bits == 16, distinct=True)
+    torch.cuda.synchronize()
+    acc, nxt = out[0].cpu().numpy().reshape(S, 4)[:, 1:], out[1].cpu().numpy()
+    text = np.where(acc.any(1), first[np.arange(S), acc.argmax(1)], nxt)
+    p, q = p.astype(np.float64), q.astype(np.float64)
+    seen, mean = np.bincount(text, minlength=V), S * p / p.sum()
+    off = abs(p.sum() - q.sum()) / max(p.sum(), q.sum()) + 2 * abs(1 - q.sum())
+    assert (np.abs(seen - mean) <= 5 * np.sqrt(mean * (1 - p)) + S * off + 1).all(), (seen, mean)
