@@ -832,7 +832,7 @@ size_t ag_attention_tree_kv4_workspace(int n_seq, int max_tokens, int H_q, int H
 #define AG_F32 0
 #define AG_BF16 1
 typedef struct {
-    const void* P;            /* device, [n_tokens][vocab]: the target's probabilities of what follows token i, at P + i * p_stride; finite, not negative (their sum need not be 1) */
+    const void* P;            /* device, [n_tokens][vocab]: the target's probabilities of what follows token i, at P + i * p_stride; finite, not negative, of sum 1 (see below) */
     const void* Q;            /* device, the same of the drafting model: what token i's children were drawn from.  NULL: drafts that were not drawn (q is 1 at the draft) */
     int64_t p_stride, q_stride;  /* elements, at least vocab */
     int32_t type;             /* AG_F32 or AG_BF16, of both */
@@ -856,6 +856,9 @@ typedef struct {
  * (and stays as it is where that sum is 0).  Where no child is left, the next token is the first v with r(0) + .. + r(v) > u_next * sum of r.
  * distinct: behind rejected siblings q is the row without their tokens times (the row's sum) / (its sum without them), both taken from the entries; where nothing of the row is
  * left without them, a further sibling cannot have been drawn from it and is passed over.
+ * Rows of P and Q are taken as they are, so each has to sum to 1: a caller who masks a row divides it by what is left.  With sums a of the row of P and b of the row of Q a token's
+ * distribution is off by at most |a - b| / max(a, b) in total variation (Q NULL: |1 - a|), and by |1 - b| / max(1, b) for every rejected draft with a sibling behind it; rounded to bf16,
+ * softmax rows have sums within 2^-8 of 1.
  * All arithmetic on probabilities is in 64 bits.  Tokens beyond a request's first AG_TREE_MAX are not accepted.
  * Asynchronous on cuda_stream, may be captured into a graph.  Errors: AG_ERR_ARG, AG_ERR_UNSUPPORTED_ARCH, AG_ERR_CUDA.
  */

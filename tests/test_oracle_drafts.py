@@ -148,3 +148,25 @@ def test_text_of_a_concentrated_q_has_the_targets_distribution(bits, peak, seed)
     seen, mean = np.bincount(text, minlength=V), S * p / p.sum()
     off = abs(p.sum() - q.sum()) / max(p.sum(), q.sum()) + 2 * abs(1 - q.sum())
     assert (np.abs(seen - mean) <= 5 * np.sqrt(mean * (1 - p)) + S * off + 1).all(), (seen, mean)
+
+
+@pytest.mark.parametrize("siblings,p,q", [(1, [.25, .25, 0], [.9, .1, 0]), (1, [.6, .3, .3], [.2, .3, .5]), (2, [.5, .2, .1], [.3, .4, .1]), (2, [.4, .4, .2], [.7, .2, .3]),
+                                          (1, [.2, .3, .1], None), (2, [.5, .5, .2], None), (1, [.5, .5, 0], [.9, .1, 0])])
+def test_rows_that_do_not_sum_to_one(siblings, p, q):
+    """The text is off by no more than what the header says of the rows' sums, in total variation; five deviations of 3000 requests beside it."""
+    S, rng = 3000, np.random.default_rng(5)
+    p = np.array(p)
+    drawn = np.array([.2, .5, .3] if q is None else q)
+    first = rng.choice(3, p=drawn / drawn.sum(), size=(S, siblings))
+    n = siblings + 1
+    token = np.concatenate([np.zeros((S, 1), int), first], 1).reshape(-1)
+    Q = None if q is None else np.broadcast_to(drawn, (n * S, 3))
+    a, nxt, _, _ = drafts.verify(np.broadcast_to(p, (n * S, 3)), Q, token, np.tile([-1] + [0] * siblings, S), n * np.arange(S + 1), rng.random(n * S), rng.random(S))
+    a = a.reshape(S, n)[:, 1:]
+    text = np.where(a.any(1), first[np.arange(S), a.argmax(1)], nxt)
+    seen, want = np.bincount(text, minlength=3) / S, p / p.sum()
+    sa, sb = p.sum(), drawn.sum()
+    bound = abs(1 - sa) if q is None else abs(sa - sb) / max(sa, sb) + (siblings - 1) * abs(1 - sb) / max(1, sb)
+    assert np.abs(seen - want).sum() / 2 <= bound + 5 * math.sqrt(.25 * 3 / S)
+    if q is not None and siblings == 1 and p.sum() == .5:
+        assert np.abs(seen - [.25, .75, 0]).max() < .04                # by hand: .9 * .25 / .9, and all the rest
