@@ -859,7 +859,8 @@ typedef struct {
  * Rows of P and Q are taken as they are, so each has to sum to 1: a caller who masks a row divides it by what is left.  With sums a of the row of P and b of the row of Q a token's
  * distribution is off by at most |a - b| / max(a, b) in total variation (Q NULL: |1 - a|), and by |1 - b| / max(1, b) for every rejected draft with a sibling behind it; rounded to bf16,
  * softmax rows have sums within 2^-8 of 1.
- * All arithmetic on probabilities is in 64 bits.  Tokens beyond a request's first AG_TREE_MAX are not accepted.
+ * All arithmetic on probabilities is in 64 bits.  Tokens beyond a request's first AG_TREE_MAX are not accepted.  With n_tokens = 0 whatever holds tokens may be NULL, `from` included:
+ * next is -1 everywhere, new_off (where it is not NULL) 0.
  * Asynchronous on cuda_stream, may be captured into a graph.  Errors: AG_ERR_ARG, AG_ERR_UNSUPPORTED_ARCH, AG_ERR_CUDA.
  */
 ag_status ag_verify_drafts(const ag_draft_verification* v, void* cuda_stream);

@@ -497,7 +497,8 @@ extern "C" ag_status ag_verify_drafts(const ag_draft_verification* v, void* cuda
     if (!v || v->n_seq < 0 || v->n_tokens < 0 || v->n_tokens >= (1ll << 30)) return AG_ERR_ARG;
     if (v->n_seq == 0) return AG_OK;
     if ((v->type != AG_F32 && v->type != AG_BF16) || v->vocab < 1 || v->vocab > (1 << 24) || v->p_stride < v->vocab || (v->Q && v->q_stride < v->vocab)) return AG_ERR_ARG;
-    if (!v->off || !v->u_next || !v->next || !v->new_off != !v->from) return AG_ERR_ARG;
+    if (!v->off || !v->u_next || !v->next) return AG_ERR_ARG;
+    if (v->n_tokens > 0 ? !v->new_off != !v->from : v->from && !v->new_off) return AG_ERR_ARG;       // (an array of no tokens may be NULL)
     if (v->n_tokens > 0 && (!v->P || !v->token || !v->u || !v->accepted)) return AG_ERR_ARG;
     const uintptr_t word = (uintptr_t)v->off | (uintptr_t)v->parent | (uintptr_t)v->token | (uintptr_t)v->u | (uintptr_t)v->u_next | (uintptr_t)v->accepted |
                            (uintptr_t)v->next | (uintptr_t)v->new_off | (uintptr_t)v->from;

@@ -117,3 +117,15 @@ def test_a_device_is_asked_for_only_after_the_arguments():
 def test_packed_rows_are_the_structure():
     v = [11 << 40, 12, 13, 14, 15, -21, 22, 23, 24, 25 << 33, 31, 32, 33, 34 << 32, 41 << 50, 42, 43]
     assert ag._pack_rotary_rows(*v) == bytes(ag.RotaryRows(*v))
+
+
+def test_verification_of_no_tokens_is_not_refused():
+    """Requests without a token among them all: arrays of no entries have no address."""
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("would run")
+    f = dict(P=None, Q=None, p_stride=1000, q_stride=1000, type=ag.AG_F32, vocab=1000, distinct=0, n_seq=2, n_tokens=0, off=A, parent=None, token=None, u=None, u_next=A, accepted=None,
+             next=A, new_off=A, from_=None)
+    call = lambda **kw: ag.lib().ag_verify_drafts(C.byref(ag.DraftVerification(**{**f, **kw})), None)  # noqa: E731
+    assert call() not in (ag.AG_OK, ag.AG_ERR_ARG) and call(from_=A) != ag.AG_ERR_ARG and call(new_off=None) != ag.AG_ERR_ARG
+    assert call(from_=A, new_off=None) == ag.AG_ERR_ARG and call(next=None) == ag.AG_ERR_ARG

@@ -336,3 +336,13 @@ def test_text_of_a_concentrated_q_is_distributed_as_the_target_has_it(bits, peak
     seen, mean = np.bincount(text, minlength=V), S * p / p.sum()
     off = abs(p.sum() - q.sum()) / max(p.sum(), q.sum()) + 2 * abs(1 - q.sum())
     assert (np.abs(seen - mean) <= 5 * np.sqrt(mean * (1 - p)) + S * off + 1).all(), (seen, mean)
+
+
+@pytest.mark.parametrize("S", [1, 3, 700])
+def test_no_tokens_at_all(S):
+    off, u_next = torch.zeros(S + 1, dtype=torch.int32, device="cuda"), torch.zeros(S, device="cuda")
+    nxt, new_off = torch.full((S,), -9, dtype=torch.int32, device="cuda"), torch.full((S + 1,), -9, dtype=torch.int32, device="cuda")
+    none = torch.empty(0, dtype=torch.int32, device="cuda").data_ptr() or None
+    ag.verify_drafts(none, none, 100, none, none, off.data_ptr(), S, 0, none, u_next.data_ptr(), none, nxt.data_ptr(), new_off.data_ptr(), none)
+    torch.cuda.synchronize()
+    assert (nxt == -1).all() and (new_off == 0).all()
