@@ -51,9 +51,10 @@ constexpr int TA_BLOCKS = 148;
 // 96.6), and even, since tiles of more than 128 rows take two places (16 trees of 40 to 64 tokens 83.0 us, with 5 95.6).  None where every tile can have a block of its own, since
 // then the longest run counts, not the sum (with it, a short request's tiles would be handled one after the other by a few blocks).
 constexpr int TA_UNIT = 6;
-// The reference m of a row moves when its maximum has grown by more than 2^11, and P is taken times 2^4: at most 2^15, and 2^-25 is lost of it, 2^-29 of the largest.  (With 2^5 and 2^10
-// it was 2^-35, but one tile in three had a row to move, whose outputs are multiplied and written back while everybody waits: 4 trees over 131072 tokens 371 us instead of 325.)
-constexpr float TA_LAZY = 11.f, TA_SHIFT = 4.f;
+// The reference m of a row moves when its maximum is more than 2^11.5 times as large, and P is taken times 2^4: at most 2^15.5, and 2^-25 is lost of it, 2^-29 of the largest.  m is a whole number
+// (2^m at most the maximum when it moves), so that what there is by then (sums, outputs, the tile's probabilities so far) is multiplied by a power of two and loses no more than that.  (With 2^5 and 2^10 2^-35 was lost, but one tile in
+// three had a row to move, whose outputs are multiplied and written back while everybody waits: 4 trees over 131072 tokens 371 us instead of 325.)
+constexpr float TA_LAZY = 11.5f, TA_SHIFT = 4.f;
 constexpr uint32_t TA_POLLS = 1u << 26;                    // of a barrier that does not come: some seconds
 
 struct TreeArgs {
@@ -934,8 +935,8 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                     const float top = fmaxf(t0, t1) * c;
                     const bool grow = top > m && !(top - m <= TA_LAZY);
                     if (__any_sync(0xffffffffu, grow) || ev != f.ev) {
-                        const float g = !grow ? 1.f : m == -INFINITY ? 0.f : ex2_ftz(m - top);
-                        if (grow) m = top;
+                        const float to = floorf(top), g = !grow ? 1.f : m - to < -126.f ? 0.f : pow2i((int)(m - to));
+                        if (grow) m = to;
                         l *= g;
                         sum = mul2(sum, pack2(g, g));
                         if (j != j0) {                                         // the outputs, once the last product has landed
@@ -953,15 +954,17 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                             }
                         }
                         ev = f.ev;
-                        const uint32_t g2 = pack_f16(g, g);
+                        // this tile's probabilities so far: times 2^-24 at the least (fp16 has no smaller power), and what is left of g before that, whose rounding the 2^-24 makes small
+                        const float g1 = fmaxf(g, 0x1p-24f), g0 = g >= 0x1p-24f ? 1.f : g * 0x1p24f;
+                        const uint32_t g12 = pack_f16(g1, g1), g02 = pack_f16(g0, g0);
 #pragma unroll 1
-                        for (int e = b0; e < b; ++e) {                         // this tile's probabilities so far
+                        for (int e = b0; e < b; ++e) {
                             uint32_t q[16];
                             tmem_st_wait();
                             tmem_ld_32x16(t_s + 64 * (e >> 1) + 16 * (e & 1), q);
                             tmem_ld_wait();
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) q[i] = mul_f16x2(q[i], g2);
+                            for (int i = 0; i < 16; ++i) q[i] = mul_f16x2(mul_f16x2(q[i], g02), g12);
                             tmem_st_32x16(t_s + 64 * (e >> 1) + 16 * (e & 1), q);
                         }
                         tmem_st_wait();

@@ -380,3 +380,34 @@ def test_pages_beyond_two_to_the_32_bytes():
     want = run(Q, K, V, few, [0, 4], None, 16, 4)
     few.pool, few.table = ag.KV4Pool(pages.data_ptr(), n_pages, H_kv, D), ag.KV4Table(page_of.data_ptr(), length.data_ptr(), refs.data_ptr(), 1, 4)
     assert (run(Q, K, V, few, [0, 4], None, 16, 4) == want).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("rows_of", [8, 40, 64, 100, 128, 200])
+@pytest.mark.parametrize("jump", [19.75, 23.5, 30.0, 37.5])
+@pytest.mark.parametrize("at,below", [(104, 96), (40, 32)])
+def test_a_reference_that_moves_inside_a_tile(D, rows_of, jump, at, below):
+    """Scores that grow by 2^10.9 after a tile of zeros and then by `jump` further on in the same tile: what has been made of the earlier keys keeps its weight.  Keys, queries and scores are exact
+    here (bf16 bases, one element of q that is not 0), log2 e times scale is off by 2^-23 and 2^x by 2^-22: a probability is off by 2^-11 + 2^-15 of itself and 2^-29 of the largest, a value by 2^-17 of
+    the largest."""
+    c = make([384], 1, D, seed=71)
+    score, value = np.zeros(384), np.zeros(384)
+    light = 2.0 ** (10.875 - jump)
+    for tile in (128, 256):
+        score[tile:tile + 128], score[tile:tile + below], score[tile + at] = -40.0, 10.875, jump
+        value[tile:tile + below], value[tile + at] = 1.0, -bf16_to_f64(kv4.bf16_bits(kv4.f32_to_bf16_value(np.array([below * light], np.float32))))[0]
+    c.pages[:] = 0
+    for t in range(384):
+        for which, x in enumerate((score, value)):
+            for g in range(D // 32):
+                b = kv4.scale_byte(D, which, t % 64, g)
+                c.pages[c.page_of[0, t // 64], 0, b + 2:b + 4] = kv4.bf16_bits(kv4.f32_to_bf16_value(x[t:t + 1].astype(np.float32))).view(np.uint8)
+    c.push()
+    G = 8 if rows_of % 8 == 0 else 4
+    count, S, scale = rows_of // G, 160, float(np.float32(np.log(2.0)))
+    Q, zero = np.zeros((S * count, G, D), np.uint16), np.zeros((S * count, 1, D), np.uint16)
+    Q[..., 0] = kv4.bf16_bits(np.float32(1.0))
+    got = run(Q, zero, zero, c, count * np.arange(S + 1), np.full(S * count, -1, np.int32), G, 64, row=[0] * S, scale=scale)
+    want, mass, _ = drafts.tree(Q[:1], zero[:1], zero[:1], drafts.cache_of(c.pages, D, c.page_of, c.len), [0, 1], None, G, None, scale)
+    bound = 2.0 ** -8 * np.abs(want[0]) + (2.0 ** -11 + 2.0 ** -15) * mass[0] + 2.0 ** -17 + 384 * 2.0 ** -29
+    assert (np.abs(got - want[0]) <= bound).all(), float((np.abs(got - want[0]) / bound).max())
