@@ -815,8 +815,10 @@ typedef struct {
  * attention_tree_kv4 - O[i][hq] = softmax(scale q k) v over what token i sees: every token of its request's cached row, its ancestors in the tree, itself.
  * Other drafted tokens have no influence, whatever they hold; a value that is not finite leaves the outputs of those that see it not finite.  Roundings, beside the output's own:
  *   keys, values   s * code + base (of the cache) and the drafted tokens' own enter the products as fp16 under a power of two: off by 2^-11 of themselves, or 2^-19 (values: 2^-17) of the
- *                  largest |base| + 15 s beside them (keys: of the same 128 tokens; values: of the row's tokens so far).  Drafts that are more than 2^6 times as large as the request's
- *                  first token do not count for that: their keys have exponents of their own, their values are added in 32 bits to the outputs that see them
+ *                  largest |base| + 15 s beside them (keys: of the same 128 tokens; values: of the row's tokens so far).  Large drafts do not count for that.  Keys: more than 2^6 times as
+ *                  large as the first token, or, where that is 0, not finite or not the only one without a parent, as the smallest key that is not 0; they have exponents of their own.
+ *                  Values: more than 2^6 times as large as every token without a parent is at least, or as the row's first cached tokens are (where all of that is 0, any value); they are
+ *                  added in 32 bits to the outputs that see them
  *   queries        exact, or 2^-32 of the row's largest element
  *   probabilities  2^-11 of themselves, or 2^-29 of the largest;  scores, softmax statistics and outputs are summed in 32 bits
  *   table      lengths are clamped to 0 .. 64 max_pages; tokens whose page is not one of the pool's are left out

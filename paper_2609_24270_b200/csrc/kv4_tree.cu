@@ -414,6 +414,22 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
         if (!ok && lane == 0) linger();
     } else if (warp == 10) {
         // ------------------------------------------------ exponents of the tiles
+        // the largest |base| + 15 s of this lane's tokens among those of a tile that count, of K and of V
+        auto coded_tops = [&](uint32_t n, int v0, int v1, float (&top)[2]) {
+#pragma unroll 1
+            for (int k = 0; k < 4; ++k) {
+                const int tok = (k & 1) * 32 + lane;
+                if (tok >= (k >> 1 ? v1 : v0)) continue;
+                const uint8_t* at = scale_smem + (n % TA_SCALES) * C::scale_bytes + (k >> 1) * 16 * D + tok * 4 * NG;
+#pragma unroll
+                for (int which = 0; which < 2; ++which)
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) {
+                        const uint32_t pair = reinterpret_cast<const uint32_t*>(at + which * 8 * D)[g];
+                        top[which] = fmaxf(top[which], fmaf(15.f, fabsf(bf16_lo(pair)), fabsf(bf16_hi(pair))));
+                    }
+            }
+        };
 #pragma unroll 1
         for (uint32_t u = 0; next_unit(u); ++u) {
             const TreeUnit& un = ctl->unit[u % TA_UNITS];
@@ -429,6 +445,9 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                     // the largest magnitudes by their bits, two elements of a word side by side; four pieces of 16 bytes of K and of V in flight
                     uint32_t most[2] = {0, 0}, first = 0;                       // (first: of this lane's piece of the first token, K's high, V's low)
                     const int pieces = un.n * (D / 8);
+                    int up[2];                                                  // parents (on their way meanwhile)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) up[k] = lane + 32 * k < un.n && x.parent ? x.parent[un.token0 + lane + 32 * k] : lane + 32 * k - 1;
 #pragma unroll 1
                     for (int i0 = lane; i0 < pieces; i0 += 128) {
                         uint4 raw[8];
@@ -452,51 +471,72 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                         of_first[which] = __reduce_max_sync(0xffffffffu, which ? first & 0xffffu : first >> 16);
                         top[which] = __uint_as_float(all[which] << 16);
                     }
-                    // A draft may be far larger than those that the rows beside it see (a branch gone astray, padding), or not finite.  Above 2^6 times the first token's, a key is taken under a
-                    // power of two of its own, and a value stays out of the products: rows that see it get it at the end of the unit.
+                    // A draft may be far larger than what the rows that do not see it see (a branch gone astray, padding, another tree), or not finite.  Such a key is taken under a power of two of its
+                    // own, such a value stays out of the products: rows that see it get it at the end of the unit.  Every row sees a token without a parent, and one such token alone, finite, not 0,
+                    // and no draft above 2^6 times as large: nothing to do.
                     constexpr uint32_t room = 6 << 7;                              // 2^6 in the bits of a bf16
-                    if (max(all[0], all[1]) >= 0x7f80u || (of_first[0] && all[0] > of_first[0] + room) || (of_first[1] && all[1] > of_first[1] + room)) {
+                    unsigned long long roots = 0;
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const int i = lane + 32 * k;
+                        roots |= (unsigned long long)__ballot_sync(0xffffffffu, i < un.n && !(up[k] >= 0 && up[k] < i)) << (32 * k);
+                    }
+                    if (roots != 1 || max(all[0], all[1]) >= 0x7f80u || !of_first[0] || !of_first[1] || all[0] > of_first[0] + room || all[1] > of_first[1] + room) {
                         uint32_t* tops = ctl->draft_top[u % TA_UNITS];
-                        int not_finite = 0;
+                        // the largest finite magnitudes of every token, K's in the high half, V's in the low
+                        bool not_finite = false;
 #pragma unroll 1
-                        for (int t = 0; t < un.n; ++t) {
-                            uint32_t m[2] = {0, 0};
-#pragma unroll 1
-                            for (int d = lane; d < D; d += 32) {
-                                const uint32_t k = x.K[(un.token0 + (long long)t) * x.k_stride + un.head * D + d] & 0x7fffu, v = x.V[(un.token0 + (long long)t) * x.v_stride + un.head * D + d] & 0x7fffu;
-                                m[0] = max(m[0], k < 0x7f80u ? k : 0u);
-                                m[1] = max(m[1], v < 0x7f80u ? v : 0u);
-                                not_finite |= v >= 0x7f80u;
+                        for (int i0 = 0; i0 < pieces; i0 += 32) {
+                            const int i = i0 + lane, t = i / (D / 8), d = un.head * D + i % (D / 8) * 8;
+                            uint32_t m = 0;
+#pragma unroll
+                            for (int which = 0; which < 2; ++which) {
+                                uint4 raw = make_uint4(0, 0, 0, 0);
+                                if (i < pieces) raw = *reinterpret_cast<const uint4*>(which ? x.V + (un.token0 + (long long)t) * x.v_stride + d : x.K + (un.token0 + (long long)t) * x.k_stride + d);
+                                const uint32_t w[4] = {raw.x & 0x7fff7fffu, raw.y & 0x7fff7fffu, raw.z & 0x7fff7fffu, raw.w & 0x7fff7fffu};
+                                uint32_t top2 = 0;
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) {
+                                    const uint32_t not_here = __vcmpgtu2(w[k], 0x7f7f7f7fu);
+                                    not_finite |= which && not_here;
+                                    top2 = __vmaxu2(top2, w[k] & ~not_here);
+                                }
+                                m |= max(top2 & 0xffffu, top2 >> 16) << (which ? 0 : 16);
                             }
-                            const uint32_t both = __reduce_max_sync(0xffffffffu, m[0]) << 16 | __reduce_max_sync(0xffffffffu, m[1]);
-                            if (lane == 0) tops[t] = both;
+#pragma unroll
+                            for (int o = 1; o < D / 8; o <<= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, o));
+                            if (i < pieces && lane % (D / 8) == 0) tops[t] = m;
                         }
                         __syncwarp();
-                        const uint32_t t0 = lane < un.n ? tops[lane] : 0, t1 = lane + 32 < un.n ? tops[lane + 32] : 0, of0 = __shfl_sync(0xffffffffu, t0, 0);
-                        const uint32_t limit = of0 & 0xffffu ? (of0 & 0xffffu) + room : 0xffffu, key_limit = of0 >> 16 ? (of0 >> 16) + room : 0xffffu;
+                        const uint32_t t0 = lane < un.n ? tops[lane] : 0, t1 = lane + 32 < un.n ? tops[lane + 32] : 0;
                         const uint32_t k0 = t0 >> 16, k1 = t1 >> 16, w0 = t0 & 0xffffu, w1 = t1 & 0xffffu;
+                        auto least = [&](uint32_t a, uint32_t b, bool zeros) { return __reduce_min_sync(0xffffffffu, min(a || zeros ? a : 0xffffu, b || zeros ? b : 0xffffu)); };
+                        // What all rows see at least.  Keys: the smallest that is not 0 (a row of scores 0 has no use for an exponent).  Values: the smallest without a parent, or what the cached
+                        // tile behind this one holds, if there is one; where neither has anything, the smallest that is not 0, or, if cached ones may follow, nothing.
+                        const uint32_t least_key = least(k0, k1, false);
+                        const bool r0 = roots >> lane & 1, r1 = roots >> (lane + 32) & 1;
+                        uint32_t least_value = least(r0 ? w0 : 0xffffu, r1 ? w1 : 0xffffu, true);
+                        if (un.tile1 > 1) {
+                            if (!wait(&ctl->scales_full[(n + 1) % TA_SCALES], ((n + 1) / TA_SCALES) & 1)) break;
+                            float cached[2] = {0.f, 0.f};
+                            coded_tops(n + 1, ctl->valid[(n + 1) % TA_INFO][0], ctl->valid[(n + 1) % TA_INFO][1], cached);
+                            least_value = max(least_value, __reduce_max_sync(0xffffffffu, __float_as_uint(cached[1])) >> 16);
+                        } else if (least_value == 0) {
+                            least_value = least(w0, w1, false);
+                        }
+                        const uint32_t key_limit = least_key + room, limit = least_value ? least_value + room : 0;
                         const unsigned long long big = __ballot_sync(0xffffffffu, w0 > limit) | (unsigned long long)__ballot_sync(0xffffffffu, w1 > limit) << 32;
                         if (lane == 0) ctl->big[u % TA_UNITS] = big;
+                        __syncwarp();
                         tops[lane] = k0 > key_limit ? k0 : 0;
                         tops[lane + 32] = k1 > key_limit ? k1 : 0;
                         top[0] = __uint_as_float(max(k0 > key_limit ? 0u : k0, k1 > key_limit ? 0u : k1) << 16);
                         top[1] = __uint_as_float(max(w0 > limit ? 0u : w0, w1 > limit ? 0u : w1) << 16);
-                        odd = TA_WIDE | (not_finite || big ? TA_ODD : 0);
+                        if (not_finite || big) odd = TA_WIDE | TA_ODD;
+                        else if (k0 > key_limit || k1 > key_limit || all[0] >= 0x7f80u) odd = TA_WIDE;
                     }
                 } else {
-#pragma unroll 1
-                    for (int k = 0; k < 4; ++k) {
-                        const int tok = (k & 1) * 32 + lane;
-                        if (tok >= (k >> 1 ? v1 : v0)) continue;
-                        const uint8_t* at = scale_smem + (n % TA_SCALES) * C::scale_bytes + (k >> 1) * 16 * D + tok * 4 * NG;
-#pragma unroll
-                        for (int which = 0; which < 2; ++which)
-#pragma unroll
-                            for (int g = 0; g < NG; ++g) {
-                                const uint32_t pair = reinterpret_cast<const uint32_t*>(at + which * 8 * D)[g];
-                                top[which] = fmaxf(top[which], fmaf(15.f, fabsf(bf16_lo(pair)), fabsf(bf16_hi(pair))));
-                            }
-                    }
+                    coded_tops(n, v0, v1, top);
                 }
                 int e[2];
 #pragma unroll

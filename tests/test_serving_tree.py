@@ -411,3 +411,87 @@ def test_a_reference_that_moves_inside_a_tile(D, rows_of, jump, at, below):
     want, mass, _ = drafts.tree(Q[:1], zero[:1], zero[:1], drafts.cache_of(c.pages, D, c.page_of, c.len), [0, 1], None, G, None, scale)
     bound = 2.0 ** -8 * np.abs(want[0]) + (2.0 ** -11 + 2.0 ** -15) * mass[0] + 2.0 ** -17 + 384 * 2.0 ** -29
     assert (np.abs(got - want[0]) <= bound).all(), float((np.abs(got - want[0]) / bound).max())
+
+
+def scaled(bits, k):
+    """bf16 bits times 2^k; k None: the type's lowest value."""
+    if k is None:
+        return np.full_like(bits, 0xFF7F)
+    return kv4.bf16_bits(kv4.f32_to_bf16_value((bf16_to_f64(bits) * 2.0 ** k).astype(np.float32)))
+
+
+def check_beside_large_drafts(got, Q, K, V, c, off, par, untouched, seen):
+    """Rows that see nothing large (`untouched`) and rows that see large values (`seen`) against the formula.  Cached elements are below 12 here, those of ordinary drafts as well; values up to 2^6
+    times as large may be in the products, larger ones are added with probabilities in 32 bits."""
+    with np.errstate(over="ignore", invalid="ignore"):
+        want, mass, reach = drafts.tree(Q, K, V, drafts.cache_of(c.pages, c.D, c.page_of, c.len), off, par, Q.shape[1] // K.shape[1])
+    e = 2.0 ** -11 * reach + 2.0 ** -19 * np.abs(bf16_to_f64(Q)).sum(-1, keepdims=True) * 12 / np.sqrt(c.D)
+    bound = 2.0 ** -8 * np.abs(want) + (2.0 ** -9 + 4 * e + 2.0 ** -20) * mass + 2.0 ** -17 * 2.0 ** 6 * 12 + 1e-30
+    assert untouched.any()
+    for rows_ in (untouched, seen & (np.abs(want).max((1, 2)) < 3e38)):
+        assert (np.abs(got - want) <= bound)[rows_].all(), float((np.abs(got - want) / bound)[rows_].max())
+
+
+LARGE = [(64, [9, 30], [100, 0]), (128, [20, 4], [900, 70]), (128, [60], [300]), (64, [12] * 20, [50] * 20), (128, [5], [900]), (128, [6, 3], [0, 0])]
+
+
+@pytest.mark.parametrize("D,counts,lens", LARGE)
+@pytest.mark.parametrize("which", ["K", "V", "KV"])
+@pytest.mark.parametrize("k", [7, 40, 100, None])
+def test_large_drafts_behind_a_first_token_of_zeros(D, counts, lens, which, k):
+    """The first token's key or value is 0, or what is finite of it: drafts that a row does not see have no influence all the same."""
+    c = make(lens, 2, D, seed=73)
+    n, off = sum(counts), np.concatenate([[0], np.cumsum(counts)])
+    par = parents(counts, 10)
+    for a, b in zip(off[:-1], off[1:]):
+        par[b - 1] = 0                                                    # a branch of its own: the others do not see it
+    Q, K, V = rows(n, 8, D, 1), rows(n, 2, D, 2), rows(n, 2, D, 3)
+    for x in which:
+        X = K if x == "K" else V
+        for a, b in zip(off[:-1], off[1:]):
+            X[a] = 0
+            X[b - 1] = scaled(X[b - 1], k)
+    last = np.zeros(n, bool)
+    last[off[1:] - 1] = True
+    check_beside_large_drafts(run(Q, K, V, c, off, par, 8, 64), Q, K, V, c, off, par, ~last, last & (which == "V"))
+
+
+@pytest.mark.parametrize("D,counts,lens", LARGE)
+@pytest.mark.parametrize("which", ["K", "V", "KV"])
+@pytest.mark.parametrize("k", [20, 100, None])
+@pytest.mark.parametrize("place", ["first", "second"])
+def test_large_drafts_in_a_forest(D, counts, lens, which, k, place):
+    """Two trees in a request's drafts (a parent outside is none): the one is as if the other were of ordinary size."""
+    c = make(lens, 2, D, seed=79)
+    n, off = sum(counts), np.concatenate([[0], np.cumsum(counts)])
+    par, large = parents(counts, 11), np.zeros(n, bool)
+    for a, b in zip(off[:-1], off[1:]):
+        h = a + (b - a) // 2
+        par[h] = -1 if h > a else par[h]
+        par[h + 1:b] = np.maximum(par[h + 1:b], h - a)
+        par[a + 1:h] = np.minimum(par[a + 1:h], h - a - 1)
+        large[a:h] = place == "first"
+        large[h:b] = place == "second"
+    Q, K, V = rows(n, 8, D, 1), rows(n, 2, D, 2), rows(n, 2, D, 3)
+    for x in which:
+        X = K if x == "K" else V
+        X[large] = scaled(X[large], k)
+    check_beside_large_drafts(run(Q, K, V, c, off, par, 8, 64), Q, K, V, c, off, par, ~large, large & (which == "V"))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("lens", [[200], [0], [900]])
+def test_large_drafts_beside_padding(D, lens):
+    """Padding of zeros, a root each, behind a tree: its rows are averages of the cache, whatever the tree's values are, and the tree's rows are the formula's."""
+    c = make(lens, 2, D, seed=83)
+    off, par = [0, 40], parents([40], 12)
+    par[12:] = -1
+    Q, K, V = rows(40, 8, D, 1), rows(40, 2, D, 2), rows(40, 2, D, 3)
+    K[12:], V[12:] = 0, 0
+    tree = np.arange(40) < 12
+    check(run(Q, K, V, c, off, par, 8, 64), Q, K, V, c, off, par, 4)
+    for k in (4, 9, 60, None):
+        V2 = V.copy()
+        V2[:12] = scaled(V[:12], k)
+        got = run(Q, K, V2, c, off, par, 8, 64)
+        check_beside_large_drafts(got, Q, K, V2, c, off, par, ~tree, tree if k == 60 else tree & False)
