@@ -495,3 +495,44 @@ def test_large_drafts_beside_padding(D, lens):
         V2[:12] = scaled(V[:12], k)
         got = run(Q, K, V2, c, off, par, 8, 64)
         check_beside_large_drafts(got, Q, K, V2, c, off, par, ~tree, tree if k == 60 else tree & False)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("count", [5, 12, 25, 50])
+@pytest.mark.parametrize("lens", [[300], [0], [60] * 6])
+def test_rows_that_see_large_drafted_keys(D, count, lens):
+    """Keys 2^7 to 2^40 times as large as the others, scores of ordinary size (a small scale): rows that see them weigh them as the formula does.  At 2^20 and the usual scale a large key takes
+    everything or nothing.  Rows four times, twice and once in a tile, and in both tiles."""
+    c = make(lens, 2, D, seed=89)
+    counts = [count] * len(lens)
+    n, off, par = sum(counts), np.concatenate([[0], np.cumsum(counts)]), parents(counts, 14)
+    Q, K, V = rows(n, 8, D, 1), rows(n, 2, D, 2), rows(n, 2, D, 3)
+    cache = drafts.cache_of(c.pages, D, c.page_of, c.len)
+    sees = [drafts.ancestors(par[a:b], b - a) for a, b in zip(off[:-1], off[1:])]
+    for k in (7, 9, 12, 40):
+        K2 = K.copy()
+        for a, b in zip(off[:-1], off[1:]):
+            for t, more in ((1, 0), (3, 1), (int(b - a) - 1, -1)):        # (of several sizes)
+                K2[a + t] = scaled(K[a + t], k + more)
+        scale = 2.0 ** (-k - 1) / np.sqrt(D)
+        got = run(Q, K2, V, c, off, par, 8, 64, scale=scale)
+        want, mass, reach = drafts.tree(Q, K2, V, cache, off, par, 4, None, float(np.float32(scale)))
+        e = 2.0 ** -11 * reach + 2.0 ** -19 * np.abs(bf16_to_f64(Q)).sum(-1, keepdims=True) * 12 * scale
+        bound = 2.0 ** -8 * np.abs(want) + (2.0 ** -9 + 4 * e + 2.0 ** -20) * mass + 2.0 ** -17 * 12 + 1e-30
+        assert (np.abs(got - want) <= bound).all(), (k, float((np.abs(got - want) / bound).max()))
+    K2, first = K.copy(), off[:-1]
+    K2[first + 2] = scaled(K[first + 2], 20)
+    got = run(Q, K2, V, c, off, par, 8, 64)
+    want, mass, _ = drafts.tree(Q, K2, V, cache, off, par, 4)
+    _, _, reach = drafts.tree(Q, K, V, cache, off, par, 4)               # of the keys that decide where the large one is out
+    e = 2.0 ** -11 * reach + 2.0 ** -19 * np.abs(bf16_to_f64(Q)).sum(-1, keepdims=True) * 12 / np.sqrt(D)
+    bound = 2.0 ** -8 * np.abs(want) + (2.0 ** -9 + 4 * e + 2.0 ** -20) * mass + 2.0 ** -17 * 12 + 1e-30
+    taken = 0
+    for s, a in enumerate(first):
+        for i in range(counts[s]):
+            for hq in range(8):
+                x = bf16_to_f64(Q[a + i, hq]) @ bf16_to_f64(K2[a + 2, hq // 4]) / np.sqrt(D) if sees[s][i, 2] else -np.inf
+                if abs(x) > 2.0 ** 12:                                    # (beyond what 2^-11 of 2^20 |q| |k| can turn)
+                    assert (np.abs(got - want) <= bound)[a + i, hq].all(), (s, i, hq, x)
+                    taken += bool(x > 0)
+    assert taken
