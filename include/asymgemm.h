@@ -868,12 +868,14 @@ typedef struct {
 ag_status ag_verify_drafts(const ag_draft_verification* v, void* cuda_stream);
 
 /*
- * ag_wait_probe - self test of the bounded device-side wait that every kernel of this library
- * uses: one thread waits on a barrier that nothing signals, gives up after limit_ns
+ * ag_wait_probe - self test of the bounded device-side wait of this library's kernels: one thread waits on a barrier that nothing signals, gives up after limit_ns
  * (<= 1 second) and the call returns AG_ERR_TIMEOUT, with the time actually waited in *waited_ns
  * (host, may be NULL).  The device stays usable.  Errors: AG_ERR_ARG, AG_ERR_UNSUPPORTED_ARCH, AG_ERR_CUDA.
  */
 ag_status ag_wait_probe(uint64_t limit_ns, uint64_t* waited_ns);
+/* ag_wait_probe_clock - the same for the wait of attention_tree_kv4, which goes by turns of the SM's clock (2^32 cycles, 2.2 s at 1.965 GHz; there it gives up in the second turn): here in
+ * the first, so the call takes up to 2.2 s. */
+ag_status ag_wait_probe_clock(uint64_t* waited_ns);
 
 const char* ag_strerror(ag_status s);
 /* A k_splits value for a decode-shaped plan over N weight columns and K rows on sm_budget SMs, from the measurements

@@ -28,7 +28,7 @@ EXPORTED = [
     "ag_affinity_cycles", "ag_affinity_check_complement", "ag_affinity_fit_hash", "ag_probe_die_bandwidth", "ag_probe_ring_bandwidth", "ag_affinity_destroy",
     "sched_build", "ag_plan_export", "ag_plan_margins", "ag_plan_tile_record", "ag_plan_reset_record",
     "ag_plan_set_grid", "ag_plan_adopted", "ag_cluster_capacity", "ag_probe_cluster_layout", "ag_plan_trace", "ag_plan_unit_times", "ag_last_status", "ag_last_status_where", "ag_suggest_k_splits", "ag_plan_destroy", "gemm_persistent", "ag_pack_weights", "ag_pack_weights_ex", "ag_packed_info", "ag_packed_closed_form", "ag_packed_page_table",
-    "ag_packed_destroy", "gemm_persistent_packed", "gemm_persistent_noalloc", "ag_wait_probe", "ag_topo_save",
+    "ag_packed_destroy", "gemm_persistent_packed", "gemm_persistent_noalloc", "ag_wait_probe", "ag_wait_probe_clock", "ag_topo_save",
     "ag_topo_load", "ag_group_desc_create", "ag_group_desc_destroy", "ag_pack_weights_grouped",
     "gemm_persistent_grouped", "ag_strerror", "ag_last_cuda_error",
     "ag_kernel_launch_count", "ag_kv_pack", "ag_kv_info", "ag_kv_append", "ag_kv_destroy", "attention_decode_persistent",
@@ -215,6 +215,7 @@ def lib() -> C.CDLL:
     L.gemm_persistent_packed.argtypes = [vp, vp, vp, C.c_int, C.c_int, C.c_int, vp, vp]
     L.gemm_persistent_noalloc.argtypes = [vp, vp, vp, C.c_int, C.c_int, C.c_int, vp, vp]
     L.ag_wait_probe.argtypes = [C.c_uint64, C.POINTER(C.c_uint64)]
+    L.ag_wait_probe_clock.argtypes = [C.POINTER(C.c_uint64)]
     L.ag_kv_pack.argtypes = [vp, vp, C.c_int, C.c_int, C.c_int, C.c_int, vp, vp, vp, sz, C.c_int, C.POINTER(vp)]
     L.ag_kv_info.argtypes = [vp, C.POINTER(C.c_int32), C.POINTER(C.c_double)]
     L.ag_kv_append.argtypes = [vp, vp, vp, vp, vp]
@@ -311,6 +312,13 @@ def wait_probe(limit_ns: int):
     """Returns (status, waited_ns) of a device-side wait that is designed to run out."""
     w = C.c_uint64()
     st = lib().ag_wait_probe(limit_ns, C.byref(w))
+    return int(st), int(w.value)
+
+
+def wait_probe_clock():
+    """The same for the wait that attention_tree_kv4 uses."""
+    w = C.c_uint64()
+    st = lib().ag_wait_probe_clock(C.byref(w))
     return int(st), int(w.value)
 
 

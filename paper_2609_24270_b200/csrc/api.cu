@@ -81,11 +81,24 @@ __global__ void k_wait_probe(unsigned long long limit_ns, int* status, unsigned 
         *status = ok ? (int)AG_OK : (int)AG_ERR_TIMEOUT;
     }
 }
-}  // namespace ag
+// The same for the wait of attention_tree_kv4: a whole warp, until the SM's clock has passed a multiple of 2^32 cycles.
+__global__ void k_wait_probe_clock(unsigned long long, int* status, unsigned long long* waited_ns) {
+    __shared__ uint64_t bar;
+    if (threadIdx.x == 0) {
+        mbar_init(smem_u32(&bar), 1);
+        mbar_fence_init();
+    }
+    __syncwarp();
+    const uint64_t t0 = globaltimer_ns();
+    const bool ok = __all_sync(0xffffffffu, mbar_wait_clock(smem_u32(&bar), 0, 0u));
+    if (threadIdx.x == 0) {
+        *waited_ns = globaltimer_ns() - t0;
+        *status = ok ? (int)AG_OK : (int)AG_ERR_TIMEOUT;
+    }
+}
 
-extern "C" ag_status ag_wait_probe(uint64_t limit_ns, uint64_t* waited_ns) {
-    if (limit_ns == 0 || limit_ns > 1000000000ull) return AG_ERR_ARG;  // at most one second
-    ag_status st = ag::check_arch();
+static ag_status run_wait_probe(void (*kernel)(unsigned long long, int*, unsigned long long*), uint64_t limit_ns, uint64_t* waited_ns) {
+    ag_status st = check_arch();
     if (st != AG_OK) return st;
     int* d_status = nullptr;
     unsigned long long* d_waited = nullptr;
@@ -94,8 +107,8 @@ extern "C" ag_status ag_wait_probe(uint64_t limit_ns, uint64_t* waited_ns) {
     int h_status = -1;
     unsigned long long h_waited = 0;
     if (e == cudaSuccess) {
-        ag::k_wait_probe<<<1, 32>>>(limit_ns, d_status, d_waited);
-        ag::count_launch();
+        kernel<<<1, 32>>>(limit_ns, d_status, d_waited);
+        count_launch();
         e = cudaGetLastError();
     }
     if (e == cudaSuccess) e = cudaDeviceSynchronize();
@@ -103,10 +116,18 @@ extern "C" ag_status ag_wait_probe(uint64_t limit_ns, uint64_t* waited_ns) {
     if (e == cudaSuccess) e = cudaMemcpy(&h_waited, d_waited, sizeof(unsigned long long), cudaMemcpyDeviceToHost);
     cudaFree(d_status);
     cudaFree(d_waited);
-    if (e != cudaSuccess) return ag::cuda_fail(e);
+    if (e != cudaSuccess) return cuda_fail(e);
     if (waited_ns) *waited_ns = h_waited;
     return (ag_status)h_status;
 }
+}  // namespace ag
+
+extern "C" ag_status ag_wait_probe(uint64_t limit_ns, uint64_t* waited_ns) {
+    if (limit_ns == 0 || limit_ns > 1000000000ull) return AG_ERR_ARG;  // at most one second
+    return ag::run_wait_probe(ag::k_wait_probe, limit_ns, waited_ns);
+}
+
+extern "C" ag_status ag_wait_probe_clock(uint64_t* waited_ns) { return ag::run_wait_probe(ag::k_wait_probe_clock, 0, waited_ns); }
 
 // ---- topology map on disk ---------------------------------------------------------------------
 // Discovery takes a fraction of a second here but the paper budgets up to a minute per GPU; the map is a

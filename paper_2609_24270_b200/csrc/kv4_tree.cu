@@ -54,8 +54,8 @@ constexpr int TA_UNIT = 6;
 // The reference m of a row moves when its maximum is more than 2^11.5 times as large, and P is taken times 2^4: at most 2^15.5, and 2^-25 is lost of it, 2^-29 of the largest.  m is a whole number
 // (2^m at most the maximum when it moves), so that what there is by then (sums, outputs, the tile's probabilities so far) is multiplied by a power of two and loses no more than that.  (With 2^5 and 2^10 2^-35 was lost, but one tile in
 // three had a row to move, whose outputs are multiplied and written back while everybody waits: 4 trees over 131072 tokens 371 us instead of 325.)
+constexpr uint32_t TA_WAIT = 1;                            // turns of the clock (2.2 to 4.4 s) that a role waits for a barrier: a wait lasts some tiles, microseconds
 constexpr float TA_LAZY = 11.5f, TA_SHIFT = 4.f;
-constexpr uint32_t TA_POLLS = 1u << 26;                    // of a barrier that does not come: some seconds
 
 struct TreeArgs {
     const uint16_t *Q, *K, *V;
@@ -283,9 +283,9 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
     tc_fence_after();
     const uint32_t tmem = ctl->tmem_base;
     bool ok = true;
-    // Every wait is bounded.  (Few instructions: there are some thirty of them, and twenty warps in eight roles share the instruction caches.)
+    // Every wait is bounded, in time; who has given up waits no more.  (Few instructions: there are some thirty of them, and twenty warps in eight roles share the instruction caches.)
     auto wait = [&](uint64_t* b, uint32_t parity) -> bool {
-        ok = __all_sync(0xffffffffu, mbar_wait_polls(smem_u32(b), parity, ok ? TA_POLLS : 1u));
+        ok = __all_sync(0xffffffffu, mbar_wait_clock(smem_u32(b), parity, TA_WAIT));
         return ok;
     };
     // unit u, which stays where it is until every reader has left it
@@ -354,11 +354,6 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
         n_tile += nt;
         n_code += nt - drafts;
     };
-    // gave up: linger (bounded) so that copies already in flight land before the block leaves
-    auto linger = [&] {
-        const uint64_t t0 = globaltimer_ns();
-        while (globaltimer_ns() - t0 < 2000000ull) __nanosleep(1000);
-    };
     if (warp == 9) {
         // ------------------------------------------------ units; copies of keys
         uint32_t u = 0, toggle = 0;
@@ -406,12 +401,11 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
             at += line;
             ++s;
         }
-        if (wait(&ctl->unit_empty[u % TA_UNITS], ((u / TA_UNITS) & 1) ^ 1) && lane == 0) {
+        if (ok && wait(&ctl->unit_empty[u % TA_UNITS], ((u / TA_UNITS) & 1) ^ 1) && lane == 0) {
             ctl->unit[u % TA_UNITS].stop = 1;
             mbar_arrive(smem_u32(&ctl->unit_full[u % TA_UNITS]));
         }
         __syncwarp();
-        if (!ok && lane == 0) linger();
     } else if (warp == 10) {
         // ------------------------------------------------ exponents of the tiles
         // the largest |base| + 15 s of this lane's tokens among those of a tile that count, of K and of V
@@ -576,7 +570,6 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
             if (!ok) break;
             leave_unit(u);
         }
-        if (!ok && lane == 0) linger();
     } else if (warp == 8) {
         // ------------------------------------------------ MMA issuer (the warp runs converged, one elected lane issues)
         const uint32_t idesc_s = make_idesc_f16(TA_TILE, TA_TILE, 0, 0), idesc_o = make_idesc_f16(TA_TILE, D, 0, 1);
@@ -595,7 +588,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
 #pragma unroll 1
             for (int b = 0; b < 2; ++b)
                 if (two || buf == b) {
-                    wait(&ctl->q_full[b], q_parity >> b & 1);
+                    if (!wait(&ctl->q_full[b], q_parity >> b & 1)) break;
                     q_parity ^= 1u << b;
                 }
             // step j: the products of V_j, the scores of K_{j + lead}, for one tile of rows or for both in turn; operands come in this order
@@ -646,15 +639,6 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
             leave_unit(u);
         }
         __syncwarp();
-        if (!ok) {
-            // let issued MMAs retire before tensor memory is released
-            if (elect_one()) {
-                tc_commit(smem_u32(&ctl->drain));
-                int dummy = 0;
-                mbar_wait(smem_u32(&ctl->drain), 0, &dummy, 2000000ull);
-            }
-            __syncwarp();
-        }
     } else {
         // ------------------------------------------------ decoders: Q, the drafted tokens and the cache's codes as operands
         // Whose operands a warp makes, K's or V's: those of one kind stand on the same schedulers, which then fetch the code of that kind only (64 requests 90.1 us at the time; with one of each on
@@ -1179,11 +1163,25 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_attn_tree_kv4(const TreeArgs 
                     if (un.two || un.buf == b) mbar_arrive(smem_u32(&ctl->q_empty[b]));
             leave_unit(u);
         }
+        if (!ok) tmem_st_wait();
         tc_fence_before();
     }
     if (!ok) ctl->abort_flag = 1;
     __syncthreads();
-    if (tid == 0 && ctl->abort_flag) *x.status = AG_ERR_TIMEOUT;
+    if (ctl->abort_flag) {
+        // a role gave up: what the others have issued (products, copies into shared memory) may be in flight still, and is waited for, bounded as well, before the block leaves
+        if (warp == 8 && elect_one()) {
+            tc_commit(smem_u32(&ctl->drain));
+            int dummy = 0;
+            mbar_wait(smem_u32(&ctl->drain), 0, &dummy, 2000000ull);
+        }
+        if (tid == 0) {
+            const uint64_t t0 = globaltimer_ns();
+            while (globaltimer_ns() - t0 < 2000000ull) __nanosleep(1000);
+            *x.status = AG_ERR_TIMEOUT;
+        }
+        __syncthreads();
+    }
     if (warp == 8) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);

@@ -96,17 +96,6 @@ __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
         : "memory");
     return ok != 0;
 }
-// The shortest bounded wait: at most `polls` tries (each of which the hardware may stretch).
-__device__ __forceinline__ bool mbar_wait_polls(uint32_t bar, uint32_t parity, uint32_t polls) {
-    uint32_t ok;
-    asm volatile(
-        "{\n .reg .pred p, q;\n .reg .u32 n;\n mov.u32 n, %3;\nagain:\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n @p bra done;\n sub.u32 n, n, 1;\n"
-        " setp.ne.u32 q, n, 0;\n @q bra again;\ndone:\n selp.u32 %0, 1, 0, p;\n}"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity), "r"(polls)
-        : "memory");
-    return ok != 0;
-}
 // Bounded wait: gives up after `limit_ns` of wall time (checked every 256 polls) or as soon as
 // another role of the block has raised *abort_flag.  Returns false on give-up.
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag,
@@ -123,6 +112,20 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
             }
         }
     }
+}
+
+// The same in few instructions, for a kernel whose code has to stay small: gives up after `turns` to turns + 1 times 2^32 cycles of the SM's clock (2.2 s at 1.965 GHz).  No flag: each role
+// looks at the clock for itself.
+__device__ __forceinline__ bool mbar_wait_clock(uint32_t bar, uint32_t parity, uint32_t turns) {
+    uint32_t ok;
+    asm volatile(
+        "{\n .reg .pred p, q;\n .reg .u32 t, d;\n mov.u32 d, %%clock_hi;\n"
+        "again:\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n @p bra done;\n mov.u32 t, %%clock_hi;\n sub.u32 t, t, d;\n setp.le.u32 q, t, %3;\n @q bra again;\n"
+        "done:\n selp.u32 %0, 1, 0, p;\n}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity), "r"(turns)
+        : "memory");
+    return ok != 0;
 }
 
 // The same wait for a role that is in no hurry (it runs ahead of the others, or waits for a whole work unit):

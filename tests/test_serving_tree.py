@@ -536,3 +536,12 @@ def test_rows_that_see_large_drafted_keys(D, count, lens):
                     assert (np.abs(got - want) <= bound)[a + i, hq].all(), (s, i, hq, x)
                     taken += bool(x > 0)
     assert taken
+
+
+def test_a_wait_of_this_kernel_gives_up_and_leaves_the_device_usable():
+    """A barrier that nothing signals: the wait ends by the SM's clock, 2^32 cycles at most here (of 1 GHz at least)."""
+    st, waited = ag.wait_probe_clock()
+    assert st == ag.AG_ERR_TIMEOUT and waited < 4.3e9
+    c = make([100], 1, 64, seed=97)
+    Q, K, V = rows(5, 2, 64, 1), rows(5, 1, 64, 2), rows(5, 1, 64, 3)
+    check(run(Q, K, V, c, [0, 5], None, 2, 5), Q, K, V, c, [0, 5], None, 2)
