@@ -822,8 +822,9 @@ typedef struct {
  *   queries        exact, or 2^-32 of the row's largest element
  *   probabilities  2^-11 of themselves, or 2^-29 of the largest;  scores, softmax statistics and outputs are summed in 32 bits
  *   table      lengths are clamped to 0 .. 64 max_pages; tokens whose page is not one of the pool's are left out
- *   workspace  device, 16-byte aligned, ag_attention_tree_kv4_workspace bytes (at most 39 MB); calls that may run at the same time need one each.  Its first int32 is
- *              the call's status once it has run (AG_OK, or AG_ERR_TIMEOUT when a bounded wait ran out), the rest means nothing between calls
+ *   workspace  device, 16-byte aligned, ag_attention_tree_kv4_workspace bytes (at most 39.5 MB); calls that may run at the same time need one each.  Its first int32 is
+ *              the call's status once it has run (AG_OK, or AG_ERR_TIMEOUT when a bounded wait ran out), the rest means nothing between calls.  A call with n_seq = 0 or n_tokens = 0
+ *              queues nothing and leaves it as it was, status included
  * The launch takes every SM of the chip (no plan).  Asynchronous on cuda_stream, may be captured into a graph.  Results are reproducible bit for bit; a request's bits may
  * change with the other requests of its batch.  Errors: AG_ERR_ARG, AG_ERR_UNSUPPORTED_ARCH, AG_ERR_CUDA.
  */

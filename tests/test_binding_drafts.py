@@ -129,3 +129,8 @@ def test_verification_of_no_tokens_is_not_refused():
     call = lambda **kw: ag.lib().ag_verify_drafts(C.byref(ag.DraftVerification(**{**f, **kw})), None)  # noqa: E731
     assert call() not in (ag.AG_OK, ag.AG_ERR_ARG) and call(from_=A) != ag.AG_ERR_ARG and call(new_off=None) != ag.AG_ERR_ARG
     assert call(from_=A, new_off=None) == ag.AG_ERR_ARG and call(next=None) == ag.AG_ERR_ARG
+
+
+def test_the_largest_workspace_is_what_the_header_says():
+    sizes = [ag.attention_tree_kv4_workspace(s, t, g * h, h, D, 1 << 20) for s in (1, 1000, 1 << 20) for t in (1, 4, 5, 63, 64) for g in (1, 4, 51, 52, 64) for h in (1, 8, 1024) for D in (64, 128)]
+    assert 39_000_000 < max(sizes) <= 39_500_000
