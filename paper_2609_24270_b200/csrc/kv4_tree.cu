@@ -22,10 +22,10 @@
 //
 // 640 threads: warps 0-7 softmax and epilogue (two groups of four), 8 MMA, 9 units and copies of keys, 10 exponents, 11 copies of values, 12-19 decoding, half of them of keys, half of values.
 //
-// Bound: a tile takes some 6200 warp instructions (decoding 2000, softmax 2500, the rest the roles' bookkeeping) on five warps a scheduler, 2500 cycles; its MMAs take 1300, its
+// Bound: a tile takes some 6360 warp instructions (decoding 2000, softmax 2500, the rest the roles' bookkeeping) on five warps a scheduler, 2500 cycles (2230 with D = 64); its MMAs take 1300, its
 // exponentials 1024, its bytes 500.  4 requests x 32 tokens x 32 heads over 131072 keys: 319 us at 1.965 GHz (840 TFLOP/s), 370 when it is repeated for seconds (the chip is at its 1000 W
 // then and runs at 1.68 GHz).  Code that runs once a unit costs the fetching of its instructions, six cycles each, so it is loops wherever it can be: with the unit's end written out
-// (88 KB of code in all; 83 now, 8 of them for drafts out of the ordinary, which few calls fetch) 64 requests over 200 to 4000 keys took 123 us, now 87.
+// (88 KB of code in all; 86 now, 9 of them for drafts out of the ordinary, which few calls fetch) 64 requests over 200 to 4000 keys took 123 us, now 87 to 88.
 // Other splits, measured: 16 softmax warps, two threads a row (4 requests as above 372 us against 341 of that time); tiles handed on in halves of 64 keys (418 against 405: QK^T with 64
 // columns takes an MMA as long as with 128); more operand stages where they fit, D = 64 (no difference).
 #include <math.h>

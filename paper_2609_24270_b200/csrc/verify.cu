@@ -8,12 +8,13 @@
 // tokens gather at once.  A rejected child with a sibling behind it takes a pass over the row for the sum.  r itself is never stored: it follows from p, q and the sums.
 // Siblings drawn without repetition: after some have been tried, q is q without those tokens, divided by left = (q's sum without them) / (q's sum).  The same passes add that up from the
 // entries that are left: a q that has been used up but for little holds that little in entries which 1 minus the others (rounded, and not exactly 1 together) would lose or turn negative.
-// (The sum costs 8 us of the 76 that 128 trees over 100003 take.)
+// (The sum costs 8 us of the 72 that 128 trees over 100003 take.)
 // Probabilities are added up in 64 bits, in an order that no scheduling changes: a border between two tokens moves by 2^-50 of the whole.
 // A cluster of blocks shares a request: each takes a stretch of the vocabulary, sums meet in distributed shared memory, and the block whose stretch holds the
 // border looks for the token.  Bound: with many requests the rows' bytes, with few the chain offset -> tree -> entries -> row -> border.
-// One chain of 5 over 32000 entries: 9.5 us on the device; 64 chains of 6 to 9 over 131072 (two models, 32 bits): 22 us, 3.0 TB/s, half of it that chain; 128 trees over 100003 (the same):
-// 76 us, two to four passes over a row whose drafts are rejected, from the second on in the cache.
+// On the device: one chain of 5 over 32000 entries 9.9 us; 64 chains of 3 to 9 over 131072 (two models, 32 bits) 21 us, 3.2 TB/s, 12 of it that chain (the time over 2000 entries), 17 where the
+// drafts were not drawn (one model's rows); 128 trees over 100003 without repetition 72 us, 23 of it chains, two to four passes over a row whose drafts are rejected, from the second on in the
+// cache.
 #include <string.h>
 
 #include <algorithm>
