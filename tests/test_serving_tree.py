@@ -420,11 +420,26 @@ def scaled(bits, k):
     return kv4.bf16_bits(kv4.f32_to_bf16_value((bf16_to_f64(bits) * 2.0 ** k).astype(np.float32)))
 
 
-def check_beside_large_drafts(got, Q, K, V, c, off, par, untouched, seen):
+_held = {}
+
+
+def cache_once(c, *key):
+    """drafts.cache_of of a cache that `key` determines, read once."""
+    if key not in _held:
+        _held[key] = kv4.load(c.pages, c.D, np.arange(c.pages.shape[0] * kv4.PAGE))
+    K, V = _held[key]
+
+    def cache(r, h):
+        at = (c.page_of[r].astype(np.int64)[:, None] * kv4.PAGE + np.arange(kv4.PAGE)).reshape(-1)[:c.len[r]]
+        return K[at, h], V[at, h]
+    return cache
+
+
+def check_beside_large_drafts(got, Q, K, V, c, cache, off, par, untouched, seen):
     """Rows that see nothing large (`untouched`) and rows that see large values (`seen`) against the formula.  Cached elements are below 12 here, those of ordinary drafts as well; values up to 2^6
     times as large may be in the products, larger ones are added with probabilities in 32 bits."""
     with np.errstate(over="ignore", invalid="ignore"):
-        want, mass, reach = drafts.tree(Q, K, V, drafts.cache_of(c.pages, c.D, c.page_of, c.len), off, par, Q.shape[1] // K.shape[1])
+        want, mass, reach = drafts.tree(Q, K, V, cache, off, par, Q.shape[1] // K.shape[1])
     e = 2.0 ** -11 * reach + 2.0 ** -19 * np.abs(bf16_to_f64(Q)).sum(-1, keepdims=True) * 12 / np.sqrt(c.D)
     bound = 2.0 ** -8 * np.abs(want) + (2.0 ** -9 + 4 * e + 2.0 ** -20) * mass + 2.0 ** -17 * 2.0 ** 6 * 12 + 1e-30
     assert untouched.any()
@@ -453,7 +468,7 @@ def test_large_drafts_behind_a_first_token_of_zeros(D, counts, lens, which, k):
             X[b - 1] = scaled(X[b - 1], k)
     last = np.zeros(n, bool)
     last[off[1:] - 1] = True
-    check_beside_large_drafts(run(Q, K, V, c, off, par, 8, 64), Q, K, V, c, off, par, ~last, last & (which == "V"))
+    check_beside_large_drafts(run(Q, K, V, c, off, par, 8, 64), Q, K, V, c, cache_once(c, D, *lens, 73), off, par, ~last, last & (which == "V"))
 
 
 @pytest.mark.parametrize("D,counts,lens", LARGE)
@@ -476,7 +491,7 @@ def test_large_drafts_in_a_forest(D, counts, lens, which, k, place):
     for x in which:
         X = K if x == "K" else V
         X[large] = scaled(X[large], k)
-    check_beside_large_drafts(run(Q, K, V, c, off, par, 8, 64), Q, K, V, c, off, par, ~large, large & (which == "V"))
+    check_beside_large_drafts(run(Q, K, V, c, off, par, 8, 64), Q, K, V, c, cache_once(c, D, *lens, 79), off, par, ~large, large & (which == "V"))
 
 
 @pytest.mark.parametrize("D", [64, 128])
@@ -494,7 +509,7 @@ def test_large_drafts_beside_padding(D, lens):
         V2 = V.copy()
         V2[:12] = scaled(V[:12], k)
         got = run(Q, K, V2, c, off, par, 8, 64)
-        check_beside_large_drafts(got, Q, K, V2, c, off, par, ~tree, tree if k == 60 else tree & False)
+        check_beside_large_drafts(got, Q, K, V2, c, cache_once(c, D, *lens, 83), off, par, ~tree, tree if k == 60 else tree & False)
 
 
 @pytest.mark.parametrize("D", [64, 128])
@@ -507,7 +522,7 @@ def test_rows_that_see_large_drafted_keys(D, count, lens):
     counts = [count] * len(lens)
     n, off, par = sum(counts), np.concatenate([[0], np.cumsum(counts)]), parents(counts, 14)
     Q, K, V = rows(n, 8, D, 1), rows(n, 2, D, 2), rows(n, 2, D, 3)
-    cache = drafts.cache_of(c.pages, D, c.page_of, c.len)
+    cache = cache_once(c, D, *lens, 89)
     sees = [drafts.ancestors(par[a:b], b - a) for a, b in zip(off[:-1], off[1:])]
     for k in (7, 9, 12, 40):
         K2 = K.copy()

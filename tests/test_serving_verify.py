@@ -346,3 +346,15 @@ def test_no_tokens_at_all(S):
     ag.verify_drafts(none, none, 100, none, none, off.data_ptr(), S, 0, none, u_next.data_ptr(), none, nxt.data_ptr(), new_off.data_ptr(), none)
     torch.cuda.synchronize()
     assert (nxt == -1).all() and (new_off == 0).all()
+
+
+@pytest.mark.parametrize("pad,q_pad,shift", [(0, 0, 1), (3, 3, 0), (5, 5, 2), (1, 2, 0), (8, 0, 3)])
+@pytest.mark.parametrize("bits", [16, 32])
+def test_what_is_left_of_rows_at_any_stride(pad, q_pad, shift, bits):
+    """Siblings without repetition over rows that begin anywhere, one entry at a time where p's and q's lie differently; tokens at a row's ends among them."""
+    for vocab in (131, 2050):
+        s = Step([6, 11, 3, 16, 9], vocab, 5, bits, distinct=True, seed=pad + vocab, peak=4.0)
+        s.P = np.roll(s.P, 1, 1)                                                      # far from q: many are refused
+        s.token[3::7], s.token[5::7] = 0, vocab - 1
+        s.device(pad, q_pad, shift)
+        same(s.run(), s.want())
